@@ -1,4 +1,4 @@
-"""Build libcfp.so (HIP, gfx950) in-tree with hipcc."""
+"""Build libcfp.so and libcfp_block.so (HIP, gfx950) in-tree with hipcc."""
 from __future__ import annotations
 
 import glob
@@ -10,6 +10,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcfp.so")
+BLOCK_LIB = os.path.join(HERE, "libcfp_block.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [
@@ -32,12 +33,13 @@ FLAGS = [
 ]
 
 
-def sources():
-    return sorted(glob.glob(os.path.join(CSRC, "*.hip")))
+def sources(sub: str = ""):
+    return sorted(glob.glob(os.path.join(CSRC, sub, "*.hip")))
 
 
 def build(verbose: bool = False) -> str:
-    """Compile every source to an object in parallel, then link."""
+    """Compile every source to an object in parallel, then link: the search
+    library from csrc/, the decoder-block operators from csrc/block/."""
     from concurrent.futures import ThreadPoolExecutor
 
     objdir = os.path.join(HERE, "_build")
@@ -52,13 +54,15 @@ def build(verbose: bool = False) -> str:
         subprocess.check_call(cmd)
         return obj
 
-    srcs = sources()
+    libs = {LIB: sources(), BLOCK_LIB: sources("block")}
+    srcs = [s for group in libs.values() for s in group]
     jobs = max(1, min(len(srcs), os.cpu_count() or 1, 16))
     with ThreadPoolExecutor(jobs) as ex:
-        objs = list(ex.map(compile_one, srcs))
-    tmp = LIB + ".tmp"
-    subprocess.check_call([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", tmp])
-    os.replace(tmp, LIB)
+        objs = dict(zip(srcs, ex.map(compile_one, srcs)))
+    for lib, group in libs.items():
+        tmp = lib + ".tmp"
+        subprocess.check_call([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", *(objs[s] for s in group), "-o", tmp])
+        os.replace(tmp, lib)
     return LIB
 
 

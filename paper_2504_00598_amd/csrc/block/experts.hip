@@ -1,0 +1,686 @@
+// The experts' products and their gradient.
+//
+// For an assignment a of token t to expert e with weight w (A assignments, in the
+// order of their expert):
+//     [g u] = x_t W1_e^T,  s = silu(g) u,  o = s W2_e^T,  y_t = sum over t's a of w o.
+// Backwards, with silu'(g) = sg (1 + g (1 - sg)), sg = 1 / (1 + exp(-g)):
+//     p = dy_t W2_e,  dw = s . p,  dg = w p u silu'(g),  du = w p silu(g),
+//     dx_t = sum over t's a of [dg du] W1_e,
+//     dW1_e = sum over e's a of [dg du]^T x_t,  dW2_e = sum over e's a of dy_t^T (w s).
+// All six products run on the matrix units with 32-bit sums.  Rounded to 16 bits
+// between products: s, [dg du] and w s, which the next product takes as operands.
+// Kept in 32 bits: g and u for the backward pass (the gradients and dw are computed
+// from them) and the experts' outputs before the weighted sum over a token's experts.
+// Nothing is added through memory in an order that could change: a token's rows are
+// gathered and summed by the token.
+#include <algorithm>
+#include <type_traits>
+
+#include "block_common.h"
+
+namespace cfp {
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef short i16x8 __attribute__((ext_vector_type(8)));
+typedef bf16_t bf16x8 __attribute__((ext_vector_type(8)));
+typedef f16_t f16x8 __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) void lds_void;
+typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+typedef __attribute__((address_space(1))) const void global_void;
+
+__device__ const uint32_t g_zero[64] = {};  // what a load past the end of the sum's axis reads
+
+template <typename T>
+__device__ __forceinline__ f32x4 mfma(i16x8 a, i16x8 b, f32x4 c) {
+  if constexpr (std::is_same<T, bf16_t>::value)
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+
+constexpr int kStep = 64;  // of the sum's axis in a stage: 128 bytes
+
+// ---------------------------------------------------------------- operands --
+//
+// A stage of an operand is EXT vectors of 64 entries of the sum's axis, 16-byte
+// pieces copied from memory straight into LDS.  An operand whose sum's axis is
+// contiguous in memory ("along") lies as [EXT][8 pieces], piece c of vector r at
+// place c ^ (r & 7); one whose vectors' axis is contiguous ("across") as
+// [64][EXT / 8 pieces] and is transposed by the read (ds_read_b64_tr_b16), with
+// the places permuted so that the 16 rows of one read meet different banks.
+
+template <int EXT>
+__device__ __forceinline__ int across_place(int krow, int c) {
+  return c ^ ((((krow & 3) | ((krow >> 3 & 1) << 2)) << 1) & (EXT / 8 - 1));
+}
+
+__device__ __forceinline__ void copy16(const char *from, char *to) {
+  __builtin_amdgcn_global_load_lds((global_void *)from, (lds_void *)to, 16, 0, 0);
+}
+
+template <int EXT, int THREADS>
+struct Along {
+  static constexpr int kLoads = EXT * 8 / THREADS;
+  const char *p[kLoads];
+  int k;  // first entry of this thread's pieces
+  // row(r): address of vector r
+  template <typename F>
+  __device__ __forceinline__ void init(F row) {
+    const int t = threadIdx.x;
+    k = ((t & 7) ^ (t >> 3 & 7)) * 8;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) p[i] = row(i * (THREADS / 8) + t / 8) + k * 2;
+  }
+  __device__ __forceinline__ void issue(char *lds, int wave, int k0, int K) {
+    const char *zero = reinterpret_cast<const char *>(g_zero);
+    const bool in = k0 + k < K;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      copy16(in ? p[i] : zero, lds + (i * THREADS + wave * 64) * 16);
+      p[i] += kStep * 2;
+    }
+  }
+};
+
+template <int EXT, int THREADS>
+struct Across {
+  static constexpr int kPer = EXT / 8;
+  static constexpr int kLoads = EXT * 8 / THREADS;
+  // row(k): address of row k of the sum's axis, at the tile's first vector; in(c): vector c exists
+  template <typename R>
+  __device__ __forceinline__ void issue(char *lds, int wave, int k0, int K, int ext, R row) {
+    const char *zero = reinterpret_cast<const char *>(g_zero);
+    const int t = threadIdx.x;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int kr = i * (THREADS / kPer) + t / kPer;
+      const int c = across_place<EXT>(kr, t % kPer) * 8;
+      const char *from = row(min(k0 + kr, K - 1)) + (c < ext ? c : 0) * 2;
+      copy16(k0 + kr < K ? from : zero, lds + (i * THREADS + wave * 64) * 16);
+    }
+  }
+};
+
+// Operand of one matrix instruction: 16 vectors from r0, 32 entries from kk * 32.
+template <int EXT, bool ACROSS>
+__device__ __forceinline__ i16x8 operand(const char *lds, int r0, int kk) {
+  const int l = threadIdx.x & 63, j = l & 15, g = l >> 4;
+  if constexpr (!ACROSS) {
+    const int r = r0 + j;
+    return *reinterpret_cast<const i16x8 *>(lds + r * 128 + (((kk * 4 + g) ^ (r & 7)) << 4));
+  } else {
+    i16x8 v;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int kr = kk * 32 + g * 8 + h * 4 + (j >> 2), c = r0 + (j & 3) * 4;
+      const char *at = lds + kr * (EXT * 2) + (across_place<EXT>(kr, c >> 3) << 4) + (c & 7) * 2;
+      const i16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)at);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[h * 4 + i] = x[i];
+    }
+    return v;
+  }
+}
+
+// ------------------------------------------------------------------- tiles --
+
+enum Product { kUp, kDown, kBackUp, kBackDown, kGradW1, kGradW2 };
+
+struct Args {
+  // operands: rows of the tile (assignments, or output rows of a weight gradient), and features
+  const char *row, *feat;
+  int64_t ld_row, ld_feat;     // bytes
+  int64_t feat_expert;         // bytes between experts
+  const int32_t *offsets, *rows;
+  int32_t experts, per_token;  // assignments of a token
+  int32_t K;                   // length of the sum's axis (of the grouped rows: the products over assignments ignore it)
+  int32_t n_row, n_feat;       // extents of the output (n_row: weight gradients)
+  int32_t F, Fp;               // inner width, and as laid out
+  // epilogues
+  void *out;                   // 16-bit or 32-bit rows
+  int64_t ld_out;              // elements
+  float *h;                    // [A][2 Fp]
+  const float *weight;         // [T * k]
+  void *out2;                  // [A][Fp]: w s
+  float *dot;                  // [A][feature tiles]: s . p over a tile
+};
+
+// Which expert and tile the workgroup takes: tiles of all experts in a row, dealt in
+// eight runs, one for each die, whose workgroups then meet the same weights in its cache.
+struct Place {
+  int expert, tile, first, count;  // first and count: the expert's assignments
+};
+
+__device__ __forceinline__ int dealt(int i, int total) {
+  const int x = i & 7, q = total >> 3, r = total & 7;
+  return x * q + min(x, r) + (i >> 3);
+}
+
+// All lanes of a wave; tiles of BR assignments; NT feature tiles each.
+template <int BR>
+__device__ __forceinline__ bool find(const Args &A, int nt, Place &p, int &ft) {
+  const int lane = threadIdx.x & 63;
+  int total = 0;
+  for (int e0 = 0; e0 < A.experts; e0 += 64) {
+    const int e = e0 + lane;
+    int c = e < A.experts ? (A.offsets[e + 1] - A.offsets[e] + BR - 1) / BR : 0;
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) c += __shfl_xor(c, off, 64);
+    total += c;
+  }
+  if ((int64_t)blockIdx.x >= (int64_t)total * nt) return false;
+  const int id = dealt(blockIdx.x, total * nt);
+  const int tile = id / nt;
+  ft = id - tile * nt;
+  int before = 0;
+  for (int e0 = 0; e0 < A.experts; e0 += 64) {
+    const int e = e0 + lane;
+    const int lo = e < A.experts ? A.offsets[e] : 0, hi = e < A.experts ? A.offsets[e + 1] : 0;
+    const int own = (hi - lo + BR - 1) / BR;
+    int c = own;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      const int y = __shfl_up(c, off, 64);
+      if (lane >= off) c += y;
+    }
+    const uint64_t past = __ballot(before + c <= tile);
+    const int k = __popcll(past);
+    if (k < 64) {
+      p.expert = __builtin_amdgcn_readfirstlane(e0 + k);
+      p.tile = __builtin_amdgcn_readfirstlane(tile - before - (__shfl(c, k, 64) - __shfl(own, k, 64)));
+      p.first = __builtin_amdgcn_readfirstlane(__shfl(lo, k, 64));
+      p.count = __builtin_amdgcn_readfirstlane(__shfl(hi, k, 64)) - p.first;
+      return true;
+    }
+    before += __shfl(c, 63, 64);
+  }
+  return false;
+}
+
+__device__ __forceinline__ float sigmoid(float x) { return 1.f / (1.f + __expf(-x)); }
+
+// BR rows x BF features by WR x WF waves.  The features are the matrix instruction's
+// first operand, so that a lane holds four consecutive features of one row.
+template <typename T, int P, int BR, int BF, int WR, int WF>
+__global__ __launch_bounds__(WR *WF * 64) void product_kernel(Args A) {
+  constexpr int THREADS = WR * WF * 64;
+  constexpr int TR = BR / WR, TF = BF / WF, FR = TR / 16, FF = TF / 16;
+  constexpr bool kGrad = P == kGradW1 || P == kGradW2;
+  constexpr bool kRowAcross = kGrad, kFeatAcross = kGrad || P == kBackUp || P == kBackDown;
+  constexpr int kFeatTile = P == kUp ? BF / 2 : BF;  // kUp: half gate, half up
+  constexpr int kBytes = (BR + BF) * kStep * 2;
+  extern __shared__ __align__(16) char smem[];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wr = wave / WF, wf = wave % WF;
+  const int lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
+
+  Place pl;
+  int ft, rt = 0, K;
+  if constexpr (kGrad) {
+    const int nf = (A.n_feat + BF - 1) / BF, nr = (A.n_row + BR - 1) / BR;
+    const int id = dealt(blockIdx.x, gridDim.x);
+    pl.expert = id / (nf * nr);
+    rt = id / nf % nr;
+    ft = id % nf;
+    pl.first = A.offsets[pl.expert];
+    pl.count = A.offsets[pl.expert + 1] - pl.first;
+    K = pl.count;
+  } else {
+    const int nt = ((P == kUp ? A.F : A.n_feat) + kFeatTile - 1) / kFeatTile;
+    if (!find<BR>(A, nt, pl, ft)) return;
+    rt = pl.tile;
+    K = A.K;
+  }
+  const int r0 = rt * BR, f0 = ft * kFeatTile;
+  const int n_rows = kGrad ? A.n_row : pl.count;
+
+  auto token = [&](int i) { return (int64_t)(A.rows[pl.first + i] / A.per_token); };
+  Along<kRowAcross ? 64 : BR, THREADS> ra;
+  Along<kFeatAcross ? 64 : BF, THREADS> fa;
+  Across<BR, THREADS> rx;
+  Across<BF, THREADS> fx;
+  if constexpr (!kRowAcross) {
+    constexpr bool kGather = P == kUp || P == kBackUp;
+    ra.init([&](int r) {
+      const int i = min(r0 + r, n_rows - 1);  // rows past the end repeat the last one and are not written
+      return A.row + (kGather ? token(i) : (int64_t)(pl.first + i)) * A.ld_row;
+    });
+  }
+  if constexpr (!kFeatAcross) {
+    const char *base = A.feat + pl.expert * A.feat_expert;
+    fa.init([&](int n) {
+      if constexpr (P == kUp) {
+        const int w = n / TF, x = n % TF, f = min(f0 + w * (TF / 2) + x % (TF / 2), A.F - 1);
+        return base + (int64_t)(f + (x < TF / 2 ? 0 : A.Fp)) * A.ld_feat;
+      } else {
+        return base + (int64_t)min(f0 + n, A.n_feat - 1) * A.ld_feat;
+      }
+    });
+  }
+  auto issue = [&](int s) {
+    char *at = smem + (s & 1) * kBytes;
+    const int k0 = s * kStep;
+    if constexpr (kRowAcross) {
+      rx.issue(at, wave, k0, K, A.n_row - r0, [&](int k) {
+        return A.row + (P == kGradW2 ? token(k) : (int64_t)(pl.first + k)) * A.ld_row + (int64_t)r0 * 2;
+      });
+    } else {
+      ra.issue(at, wave, k0, K);
+    }
+    if constexpr (kFeatAcross) {
+      fx.issue(at + BR * kStep * 2, wave, k0, K, A.n_feat - f0, [&](int k) {
+        if constexpr (kGrad)
+          return A.feat + (P == kGradW1 ? token(k) : (int64_t)(pl.first + k)) * A.ld_feat + (int64_t)f0 * 2;
+        else
+          return A.feat + pl.expert * A.feat_expert + (int64_t)k * A.ld_feat + (int64_t)f0 * 2;
+      });
+    } else {
+      fa.issue(at + BR * kStep * 2, wave, k0, K);
+    }
+  };
+
+  f32x4 acc[FF][FR];
+#pragma unroll
+  for (int a = 0; a < FF; ++a)
+#pragma unroll
+    for (int b = 0; b < FR; ++b) acc[a][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int steps = (K + kStep - 1) / kStep;
+  if (steps > 0) issue(0);
+  for (int s = 0; s < steps; ++s) {
+    __syncthreads();  // stage s has landed, and the other one has been read
+    if (s + 1 < steps) issue(s + 1);
+    const char *rl = smem + (s & 1) * kBytes, *fl = rl + BR * kStep * 2;
+#pragma unroll
+    for (int kk = 0; kk < kStep / 32; ++kk) {
+      i16x8 fo[FF], ro[FR];
+#pragma unroll
+      for (int a = 0; a < FF; ++a) fo[a] = operand<BF, kFeatAcross>(fl, wf * TF + a * 16, kk);
+#pragma unroll
+      for (int b = 0; b < FR; ++b) ro[b] = operand<BR, kRowAcross>(rl, wr * TR + b * 16, kk);
+#pragma unroll
+      for (int a = 0; a < FF; ++a)
+#pragma unroll
+        for (int b = 0; b < FR; ++b) acc[a][b] = mfma<T>(fo[a], ro[b], acc[a][b]);
+    }
+  }
+
+  // ---- epilogues: lane (j, g) holds features 4 g .. 4 g + 3 of row j of each 16 x 16 block
+  if constexpr (P == kUp) {
+#pragma unroll
+    for (int b = 0; b < FR; ++b) {
+      const int i = r0 + wr * TR + b * 16 + j;
+      if (i >= n_rows) continue;
+      const int64_t a = pl.first + i;
+#pragma unroll
+      for (int q = 0; q < FF / 2; ++q) {
+        const int f = f0 + wf * (TF / 2) + q * 16 + g * 4;
+        if (f >= A.Fp) continue;
+        float s[4], ga[4], up[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const bool in = f + e < A.F;
+          ga[e] = in ? acc[q][b][e] : 0.f;
+          up[e] = in ? acc[q + FF / 2][b][e] : 0.f;
+          s[e] = ga[e] * sigmoid(ga[e]) * up[e];
+        }
+        store_vec<T, 4>(reinterpret_cast<T *>(A.out) + a * A.ld_out + f, s);
+        if (A.h != nullptr) {
+          store_vec<float, 4>(A.h + a * 2 * A.Fp + f, ga);
+          store_vec<float, 4>(A.h + a * 2 * A.Fp + A.Fp + f, up);
+        }
+      }
+    }
+  } else if constexpr (P == kDown || P == kBackDown) {
+#pragma unroll
+    for (int b = 0; b < FR; ++b) {
+      const int i = r0 + wr * TR + b * 16 + j;
+      if (i >= n_rows) continue;
+      float *o = reinterpret_cast<float *>(A.out) + (int64_t)(pl.first + i) * A.ld_out;
+#pragma unroll
+      for (int q = 0; q < FF; ++q) {
+        const int f = f0 + wf * TF + q * 16 + g * 4;
+        if (f < A.ld_out) *reinterpret_cast<f32x4 *>(o + f) = acc[q][b];
+      }
+    }
+  } else if constexpr (P == kBackUp) {
+    float dots[FR];
+#pragma unroll
+    for (int b = 0; b < FR; ++b) {
+      dots[b] = 0.f;
+      const int i = r0 + wr * TR + b * 16 + j;
+      if (i >= n_rows) continue;
+      const int64_t a = pl.first + i;
+      const float w = A.weight[A.rows[a]];
+#pragma unroll
+      for (int q = 0; q < FF; ++q) {
+        const int f = f0 + wf * TF + q * 16 + g * 4;
+        if (f >= A.Fp) continue;
+        float ga[4], up[4], dg[4], du[4], ws[4];
+        load_vec<float, 4>(A.h + a * 2 * A.Fp + f, ga);
+        load_vec<float, 4>(A.h + a * 2 * A.Fp + A.Fp + f, up);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const bool in = f + e < A.F;
+          const float p = in ? acc[q][b][e] : 0.f;
+          const float sg = sigmoid(ga[e]), si = ga[e] * sg, s = si * up[e];
+          dots[b] += in ? s * p : 0.f;
+          dg[e] = w * p * up[e] * sg * (1.f + ga[e] * (1.f - sg));
+          du[e] = w * p * si;
+          ws[e] = w * s;
+        }
+        T *d = reinterpret_cast<T *>(A.out) + a * A.ld_out;
+        store_vec<T, 4>(d + f, dg);
+        store_vec<T, 4>(d + A.Fp + f, du);
+        store_vec<T, 4>(reinterpret_cast<T *>(A.out2) + a * A.Fp + f, ws);
+      }
+    }
+    float *part = reinterpret_cast<float *>(smem);  // [WF][BR]
+    __syncthreads();
+#pragma unroll
+    for (int b = 0; b < FR; ++b) {
+      float v = dots[b];
+      v += __shfl_xor(v, 16, 64);
+      v += __shfl_xor(v, 32, 64);
+      if (g == 0) part[wf * BR + wr * TR + b * 16 + j] = v;
+    }
+    __syncthreads();
+    const int nt = (A.n_feat + BF - 1) / BF;
+    for (int r = threadIdx.x; r < BR; r += THREADS) {
+      if (r0 + r >= n_rows) continue;
+      float v = 0.f;
+#pragma unroll
+      for (int w = 0; w < WF; ++w) v += part[w * BR + r];
+      A.dot[(int64_t)(pl.first + r0 + r) * nt + ft] = v;
+    }
+  } else {  // gradients of the weights: rows of the output, whole or scalar stores by its width
+#pragma unroll
+    for (int b = 0; b < FR; ++b) {
+      int i = r0 + wr * TR + b * 16 + j;
+      if (i >= A.n_row) continue;
+      int64_t orow = i;
+      int64_t per = A.n_row;
+      if constexpr (P == kGradW1) {  // gate and up rows, each Fp as laid out
+        const int half = i >= A.Fp, x = i - half * A.Fp;
+        if (x >= A.F) continue;
+        orow = x + (half ? A.F : 0);
+        per = 2 * A.F;
+      }
+      T *o = reinterpret_cast<T *>(A.out) + (pl.expert * per + orow) * A.ld_out;
+#pragma unroll
+      for (int q = 0; q < FF; ++q) {
+        const int f = f0 + wf * TF + q * 16 + g * 4;
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = acc[q][b][e];
+        const int width = (int)A.ld_out;
+        if (f + 4 <= width && width % 4 == 0) {
+          store_vec<T, 4>(o + f, v);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (f + e < width) o[f + e] = (T)v[e];
+        }
+      }
+    }
+  }
+}
+
+// ------------------------------------------------------ around the products --
+
+// y_t = sum over the token's assignments of w o (weight null: of o), and the gradient
+// of the weights from the feature tiles' sums.
+template <typename T, int V>
+__global__ __launch_bounds__(256) void combine_kernel(const float *o, int64_t ld, const float *weight, const int32_t *slot,
+                                                      int per_token, int H, T *y, const float *dot, int nt, float *dweight) {
+  const int64_t t = blockIdx.x;
+  const int32_t *sl = slot + t * per_token;
+  if (dweight != nullptr && blockIdx.y == 0)
+    for (int q = threadIdx.x; q < per_token; q += 256) {
+      float v = 0.f;
+      if (sl[q] >= 0)
+        for (int i = 0; i < nt; ++i) v += dot[(int64_t)sl[q] * nt + i];
+      dweight[t * per_token + q] = v;
+    }
+  for (int c = (blockIdx.y * 256 + threadIdx.x) * V; c < H; c += gridDim.y * 256 * V) {
+    float v[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = 0.f;
+    for (int q = 0; q < per_token; ++q) {
+      const int a = sl[q];
+      if (a < 0) continue;
+      const float w = weight ? weight[t * per_token + q] : 1.f;
+      float x[V];
+      load_vec<float, V>(o + a * ld + c, x);
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[i] += w * x[i];
+    }
+    store_vec<T, V>(y + t * H + c, v);
+  }
+}
+
+// Copy of [n][rows][cols] with both inner extents padded by zeros (16-bit elements).  `halves`: the rows
+// are two runs of rows / halves that are padded each.
+__global__ __launch_bounds__(256) void pad_kernel(const uint16_t *in, int64_t ld, int64_t rows, int cols, int halves,
+                                                  uint16_t *out, int64_t out_rows, int out_cols, int64_t n) {
+  const int64_t total = n * out_rows * out_cols;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    const int c = (int)(i % out_cols);
+    const int64_t r = i / out_cols % out_rows, e = i / out_cols / out_rows;
+    const int64_t per = out_rows / halves, half = r / per, x = r - half * per, src = rows / halves;
+    out[i] = c < cols && x < src ? in[(e * rows + half * src + x) * ld + c] : (uint16_t)0;
+  }
+}
+
+inline int64_t up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
+
+// Where the parts of the workspace lie.  Copies of operands whose rows do not start on
+// 16 bytes are made for the call.
+struct Region {
+  size_t x = 0, dy = 0, w1 = 0, w2 = 0;  // copies
+  size_t act = 0;                         // s, or w s backwards [A][Fp]
+  size_t out = 0;                         // o, or the rows of dx [A][Hp] 32-bit
+  size_t dgu = 0;                         // [A][2 Fp]
+  size_t dot = 0;                         // [A][feature tiles]
+  size_t total = 0;
+};
+
+bool on16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+constexpr int kMinFeatTile = 128;
+
+Region region(const cfp_experts_desc &d, bool bwd, bool pad_x, bool pad_dy, bool pad_w1, bool pad_w2) {
+  const size_t A = (size_t)d.n_tokens * d.k, Hp = up(d.hidden, 8), Fp = up(d.inner, 8), E = d.n_experts;
+  Region r;
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    const size_t at = off;
+    off = up(off + bytes, 256);
+    return at;
+  };
+  if (pad_x) r.x = take((size_t)d.n_tokens * Hp * 2);
+  if (pad_dy) r.dy = take((size_t)d.n_tokens * Hp * 2);
+  if (pad_w1) r.w1 = take(E * 2 * Fp * Hp * 2);
+  if (pad_w2) r.w2 = take(E * d.hidden * Fp * 2);
+  r.act = take(A * Fp * 2);
+  r.out = take(A * Hp * 4);
+  if (bwd) {
+    r.dgu = take(A * 2 * Fp * 2);
+    r.dot = take(A * ((d.inner + kMinFeatTile - 1) / kMinFeatTile) * 4);
+  }
+  r.total = off;
+  return r;
+}
+
+bool pads_x(const cfp_experts_desc &d, const void *x, int64_t stride) {
+  return d.hidden % 8 != 0 || !on16(x) || (stride % 8 != 0 && d.n_tokens > 1);
+}
+bool pads_w1(const cfp_experts_desc &d) { return d.hidden % 8 != 0 || d.inner % 8 != 0 || !on16(d.w1); }
+bool pads_w2(const cfp_experts_desc &d) { return d.inner % 8 != 0 || !on16(d.w2); }
+
+void pad(const void *in, int64_t ld, int64_t rows, int cols, int halves, void *out, int64_t out_rows, int out_cols,
+         int64_t n, hipStream_t st) {
+  const int64_t total = n * out_rows * out_cols;
+  const unsigned grid = (unsigned)std::min<int64_t>((total + 255) / 256, 16384);
+  pad_kernel<<<grid, 256, 0, st>>>(static_cast<const uint16_t *>(in), ld, rows, cols, halves,
+                                   static_cast<uint16_t *>(out), out_rows, out_cols, n);
+}
+
+template <typename T, int P, int BR, int BF, int WR, int WF>
+hipError_t run_product(const Args &A, int64_t n_assign, hipStream_t st) {
+  constexpr int kFeatTile = P == kUp ? BF / 2 : BF;
+  constexpr size_t lds = 2 * (BR + BF) * kStep * 2;
+  const int64_t nt = ((P == kUp ? A.F : A.n_feat) + kFeatTile - 1) / kFeatTile;
+  int64_t grid;
+  if (P == kGradW1 || P == kGradW2)
+    grid = nt * ((A.n_row + BR - 1) / BR) * A.experts;
+  else
+    grid = nt * (n_assign / BR + std::min<int64_t>(A.experts, n_assign));
+  if (grid > 0x7FFFFFFF) return hipErrorInvalidValue;
+  auto *kernel = product_kernel<T, P, BR, BF, WR, WF>;
+  if (lds > 65536) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
+                                             hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+  }
+  kernel<<<(unsigned)grid, WR * WF * 64, lds, st>>>(A);
+  return hipGetLastError();
+}
+
+template <typename T, int P>
+hipError_t product(const Args &A, int64_t n_assign, hipStream_t st) {
+  return run_product<T, P, 128, 128, 2, 2>(A, n_assign, st);
+}
+
+Args base_args(const cfp_experts_desc &d) {
+  Args A{};
+  A.offsets = d.offsets, A.rows = d.rows, A.experts = d.n_experts, A.per_token = d.k;
+  A.F = d.inner, A.Fp = (int)up(d.inner, 8), A.weight = d.weight;
+  return A;
+}
+
+template <typename T>
+hipError_t combine(const cfp_experts_desc &d, const float *o, const float *weight, void *y, const float *dot, int nt,
+                   float *dweight, hipStream_t st) {
+  const int64_t ld = up(d.hidden, 8);
+  if (d.hidden % 4 == 0 && reinterpret_cast<uintptr_t>(y) % 8 == 0)
+    combine_kernel<T, 4><<<dim3((unsigned)d.n_tokens, (d.hidden + 1023) / 1024), 256, 0, st>>>(
+        o, ld, weight, d.slot, d.k, d.hidden, static_cast<T *>(y), dot, nt, dweight);
+  else
+    combine_kernel<T, 1><<<dim3((unsigned)d.n_tokens, (d.hidden + 1023) / 1024), 256, 0, st>>>(
+        o, ld, weight, d.slot, d.k, d.hidden, static_cast<T *>(y), dot, nt, dweight);
+  return hipGetLastError();
+}
+
+struct Laid {  // operands as the products take them
+  const char *x, *dy, *w1, *w2;
+  int64_t ld_x, ld_dy, Hp, Fp;
+};
+
+Laid lay_out(const cfp_experts_desc &d, const void *dy, int64_t dy_stride, const Region &r, bool px, bool pdy, bool pw1,
+             bool pw2, uint8_t *ws, hipStream_t st) {
+  const int Hp = (int)up(d.hidden, 8), Fp = (int)up(d.inner, 8);
+  Laid L{static_cast<const char *>(d.x), static_cast<const char *>(dy), static_cast<const char *>(d.w1),
+         static_cast<const char *>(d.w2), d.x_stride * 2, dy_stride * 2, Hp, Fp};
+  if (px) {
+    pad(d.x, d.x_stride, d.n_tokens, d.hidden, 1, ws + r.x, d.n_tokens, Hp, 1, st);
+    L.x = reinterpret_cast<const char *>(ws + r.x), L.ld_x = Hp * 2;
+  }
+  if (pdy) {
+    pad(dy, dy_stride, d.n_tokens, d.hidden, 1, ws + r.dy, d.n_tokens, Hp, 1, st);
+    L.dy = reinterpret_cast<const char *>(ws + r.dy), L.ld_dy = Hp * 2;
+  }
+  if (pw1) {
+    pad(d.w1, d.hidden, 2 * (int64_t)d.inner, d.hidden, 2, ws + r.w1, 2 * (int64_t)Fp, Hp, d.n_experts, st);
+    L.w1 = reinterpret_cast<const char *>(ws + r.w1);
+  }
+  if (pw2) {
+    pad(d.w2, d.inner, d.hidden, d.inner, 1, ws + r.w2, d.hidden, Fp, d.n_experts, st);
+    L.w2 = reinterpret_cast<const char *>(ws + r.w2);
+  }
+  return L;
+}
+
+template <typename T>
+hipError_t forward(const cfp_experts_desc &d, void *y, float *h, uint8_t *ws, hipStream_t st) {
+  const bool px = pads_x(d, d.x, d.x_stride), pw1 = pads_w1(d), pw2 = pads_w2(d);
+  const Region r = region(d, false, px, false, pw1, pw2);
+  const Laid L = lay_out(d, nullptr, 0, r, px, false, pw1, pw2, ws, st);
+  const int64_t n = d.n_tokens * d.k;
+  Args A = base_args(d);
+  A.row = L.x, A.ld_row = L.ld_x, A.feat = L.w1, A.ld_feat = L.Hp * 2, A.feat_expert = 2 * L.Fp * L.Hp * 2;
+  A.K = (int)L.Hp, A.n_feat = d.inner, A.out = ws + r.act, A.ld_out = L.Fp, A.h = h;
+  hipError_t e = product<T, kUp>(A, n, st);
+  if (e != hipSuccess) return e;
+  A = base_args(d);
+  A.row = reinterpret_cast<const char *>(ws + r.act), A.ld_row = L.Fp * 2;
+  A.feat = L.w2, A.ld_feat = L.Fp * 2, A.feat_expert = (int64_t)d.hidden * L.Fp * 2;
+  A.K = (int)L.Fp, A.n_feat = d.hidden, A.out = ws + r.out, A.ld_out = L.Hp;
+  if ((e = product<T, kDown>(A, n, st)) != hipSuccess) return e;
+  return combine<T>(d, reinterpret_cast<const float *>(ws + r.out), d.weight, y, nullptr, 0, nullptr, st);
+}
+
+template <typename T>
+hipError_t backward(const cfp_experts_desc &d, const void *dy, int64_t dy_stride, const float *h, void *dx, void *dw1,
+                    void *dw2, float *dweight, uint8_t *ws, hipStream_t st) {
+  const bool some = d.n_tokens > 0;  // without tokens only the gradients of the weights are written, with zeros
+  const bool px = some && pads_x(d, d.x, d.x_stride), pdy = some && pads_x(d, dy, dy_stride);
+  const bool pw1 = some && pads_w1(d), pw2 = some && pads_w2(d);
+  const Region r = region(d, true, px, pdy, pw1, pw2);
+  const Laid L = lay_out(d, dy, dy_stride, r, px, pdy, pw1, pw2, ws, st);
+  const int64_t n = d.n_tokens * d.k;
+  Args A = base_args(d);
+  hipError_t e = hipSuccess;
+  if (n > 0) {
+  // p = dy W2, and what follows from it
+  A.row = L.dy, A.ld_row = L.ld_dy, A.feat = L.w2, A.ld_feat = L.Fp * 2, A.feat_expert = (int64_t)d.hidden * L.Fp * 2;
+  A.K = d.hidden, A.n_feat = (int)L.Fp, A.h = const_cast<float *>(h), A.out = ws + r.dgu, A.ld_out = 2 * L.Fp;
+  A.out2 = ws + r.act, A.dot = reinterpret_cast<float *>(ws + r.dot);
+  if ((e = product<T, kBackUp>(A, n, st)) != hipSuccess) return e;
+  // rows of dx
+  A = base_args(d);
+  A.row = reinterpret_cast<const char *>(ws + r.dgu), A.ld_row = 2 * L.Fp * 2;
+  A.feat = L.w1, A.ld_feat = L.Hp * 2, A.feat_expert = 2 * L.Fp * L.Hp * 2;
+  A.K = (int)(2 * L.Fp), A.n_feat = (int)L.Hp, A.out = ws + r.out, A.ld_out = L.Hp;
+  if ((e = product<T, kBackDown>(A, n, st)) != hipSuccess) return e;
+  }
+  // dW1 = [dg du]^T x
+  A = base_args(d);
+  A.row = reinterpret_cast<const char *>(ws + r.dgu), A.ld_row = 2 * L.Fp * 2, A.n_row = (int)(2 * L.Fp);
+  A.feat = L.x, A.ld_feat = L.ld_x, A.n_feat = d.hidden, A.out = dw1, A.ld_out = d.hidden;
+  if ((e = product<T, kGradW1>(A, n, st)) != hipSuccess) return e;
+  // dW2 = dy^T (w s)
+  A = base_args(d);
+  A.row = L.dy, A.ld_row = L.ld_dy, A.n_row = d.hidden;
+  A.feat = reinterpret_cast<const char *>(ws + r.act), A.ld_feat = L.Fp * 2, A.n_feat = d.inner, A.out = dw2,
+  A.ld_out = d.inner;
+  if ((e = product<T, kGradW2>(A, n, st)) != hipSuccess || n == 0) return e;
+  const int nt = (int)((L.Fp + kMinFeatTile - 1) / kMinFeatTile);
+  return combine<T>(d, reinterpret_cast<const float *>(ws + r.out), nullptr, dx,
+                    reinterpret_cast<const float *>(ws + r.dot), nt, dweight, st);
+}
+
+}  // namespace
+
+size_t experts_kept_bytes(const cfp_experts_desc &d) {
+  return (size_t)d.n_tokens * d.k * 2 * up(d.inner, 8) * 4;
+}
+
+size_t experts_bytes(const cfp_experts_desc &d, bool bwd) {
+  // dy is checked only when it is given: room for its copy is taken with x's
+  const bool px = pads_x(d, d.x, d.x_stride);
+  return region(d, bwd, px || bwd, bwd, pads_w1(d), pads_w2(d)).total;
+}
+
+hipError_t launch_experts(const cfp_experts_desc &d, void *y, float *h, uint8_t *ws, hipStream_t st) {
+  return d.dtype == CFP_DT_BF16 ? forward<bf16_t>(d, y, h, ws, st) : forward<f16_t>(d, y, h, ws, st);
+}
+
+hipError_t launch_experts_bwd(const cfp_experts_desc &d, const void *dy, int64_t dy_stride, const float *h, void *dx,
+                              void *dw1, void *dw2, float *dweight, uint8_t *ws, hipStream_t st) {
+  return d.dtype == CFP_DT_BF16 ? backward<bf16_t>(d, dy, dy_stride, h, dx, dw1, dw2, dweight, ws, st)
+                                : backward<f16_t>(d, dy, dy_stride, h, dx, dw1, dw2, dweight, ws, st);
+}
+
+}  // namespace cfp
