@@ -84,22 +84,72 @@ struct Along {
   }
 };
 
+// Pieces of 16 rows of the sum's axis repeat a thread's place in them, so its column is one for all its loads.
 template <int EXT, int THREADS>
-struct Across {
-  static constexpr int kPer = EXT / 8;
-  static constexpr int kLoads = EXT * 8 / THREADS;
-  // row(k): address of row k of the sum's axis, at the tile's first vector; in(c): vector c exists
-  template <typename R>
-  __device__ __forceinline__ void issue(char *lds, int wave, int k0, int K, int ext, R row) {
+struct AcrossPlace {
+  static constexpr int kPer = EXT / 8, kRows = THREADS / kPer, kLoads = kStep / kRows;
+  static_assert(kRows % 16 == 0 && kLoads * kRows == kStep, "");
+  int kr, col;  // row of the first load, first vector
+  __device__ __forceinline__ void init(int ext) {
+    kr = threadIdx.x / kPer;
+    const int c = across_place<EXT>(kr, threadIdx.x % kPer) * 8;
+    col = c < ext ? c : 0;  // vectors past the end repeat the first ones and are not written
+  }
+};
+
+// Rows at one distance.
+template <int EXT, int THREADS>
+struct Across : AcrossPlace<EXT, THREADS> {
+  using B = AcrossPlace<EXT, THREADS>;
+  const char *p;
+  int64_t ld;
+  __device__ __forceinline__ void init(const char *first, int64_t ld_, int ext) {
+    B::init(ext);
+    ld = ld_;
+    p = first + B::kr * ld + B::col * 2;
+  }
+  __device__ __forceinline__ void issue(char *lds, int wave, int k0, int K) {
     const char *zero = reinterpret_cast<const char *>(g_zero);
-    const int t = threadIdx.x;
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int kr = i * (THREADS / kPer) + t / kPer;
-      const int c = across_place<EXT>(kr, t % kPer) * 8;
-      const char *from = row(min(k0 + kr, K - 1)) + (c < ext ? c : 0) * 2;
-      copy16(k0 + kr < K ? from : zero, lds + (i * THREADS + wave * 64) * 16);
+    for (int i = 0; i < B::kLoads; ++i) {
+      const char *from = p + (int64_t)(i * B::kRows) * ld;
+      copy16(k0 + i * B::kRows + B::kr < K ? from : zero, lds + (i * THREADS + wave * 64) * 16);
     }
+    p += kStep * ld;
+  }
+};
+
+// Rows by a list, whose entries are read a stage ahead.
+template <int EXT, int THREADS>
+struct AcrossList : AcrossPlace<EXT, THREADS> {
+  using B = AcrossPlace<EXT, THREADS>;
+  const char *p;
+  int64_t ld;
+  const int32_t *list;
+  uint32_t magic, shift;
+  int32_t next[B::kLoads];
+  __device__ __forceinline__ void init(const char *base, int64_t ld_, int ext, const int32_t *list_, uint32_t m,
+                                       uint32_t sh, int K) {
+    B::init(ext);
+    ld = ld_, list = list_, magic = m, shift = sh;
+    p = base + B::col * 2;
+    fetch(0, K);
+  }
+  __device__ __forceinline__ void fetch(int k0, int K) {
+#pragma unroll
+    for (int i = 0; i < B::kLoads; ++i) {
+      const int k = k0 + i * B::kRows + B::kr;
+      next[i] = k < K ? list[k] : -1;
+    }
+  }
+  __device__ __forceinline__ void issue(char *lds, int wave, int k0, int K) {
+    const char *zero = reinterpret_cast<const char *>(g_zero);
+#pragma unroll
+    for (int i = 0; i < B::kLoads; ++i) {
+      const int64_t row = (uint64_t)(uint32_t)next[i] * magic >> shift;
+      copy16(next[i] >= 0 ? p + row * ld : zero, lds + (i * THREADS + wave * 64) * 16);
+    }
+    fetch(k0 + kStep, K);
   }
 };
 
@@ -134,7 +184,8 @@ struct Args {
   int64_t ld_row, ld_feat;     // bytes
   int64_t feat_expert;         // bytes between experts
   const int32_t *offsets, *rows;
-  int32_t experts, per_token;  // assignments of a token
+  int32_t experts;
+  uint32_t magic, shift;       // token of an assignment a: a * magic >> shift
   int32_t K;                   // length of the sum's axis (of the grouped rows: the products over assignments ignore it)
   int32_t n_row, n_feat;       // extents of the output (n_row: weight gradients)
   int32_t F, Fp;               // inner width, and as laid out
@@ -144,7 +195,8 @@ struct Args {
   float *h;                    // [A][2 Fp]
   const float *weight;         // [T * k]
   void *out2;                  // [A][Fp]: w s
-  float *dot;                  // [A][feature tiles]: s . p over a tile
+  float *dot;                  // [A][dot_tiles]: s . p over a feature tile
+  int32_t dot_tiles;
 };
 
 // Which expert and tile the workgroup takes: tiles of all experts in a row, dealt in
@@ -236,21 +288,34 @@ __global__ __launch_bounds__(WR *WF * 64) void product_kernel(Args A) {
   const int r0 = rt * BR, f0 = ft * kFeatTile;
   const int n_rows = kGrad ? A.n_row : pl.count;
 
-  auto token = [&](int i) { return (int64_t)(A.rows[pl.first + i] / A.per_token); };
-  Along<kRowAcross ? 64 : BR, THREADS> ra;
-  Along<kFeatAcross ? 64 : BF, THREADS> fa;
-  Across<BR, THREADS> rx;
-  Across<BF, THREADS> fx;
-  if constexpr (!kRowAcross) {
+  constexpr bool kRowList = P == kGradW2, kFeatList = P == kGradW1;
+  using RowLoad = std::conditional_t<!kRowAcross, Along<BR, THREADS>,
+                                     std::conditional_t<kRowList, AcrossList<BR, THREADS>, Across<BR, THREADS>>>;
+  using FeatLoad = std::conditional_t<!kFeatAcross, Along<BF, THREADS>,
+                                      std::conditional_t<kFeatList, AcrossList<BF, THREADS>, Across<BF, THREADS>>>;
+  RowLoad rl;
+  FeatLoad fl;
+  if constexpr (kRowList) {
+    rl.init(A.row + (int64_t)r0 * 2, A.ld_row, A.n_row - r0, A.rows + pl.first, A.magic, A.shift, K);
+  } else if constexpr (kRowAcross) {
+    rl.init(A.row + pl.first * A.ld_row + (int64_t)r0 * 2, A.ld_row, A.n_row - r0);
+  } else {
     constexpr bool kGather = P == kUp || P == kBackUp;
-    ra.init([&](int r) {
+    rl.init([&](int r) {
       const int i = min(r0 + r, n_rows - 1);  // rows past the end repeat the last one and are not written
-      return A.row + (kGather ? token(i) : (int64_t)(pl.first + i)) * A.ld_row;
+      int64_t row = pl.first + i;
+      if constexpr (kGather) row = (uint64_t)(uint32_t)A.rows[row] * A.magic >> A.shift;
+      return A.row + row * A.ld_row;
     });
   }
-  if constexpr (!kFeatAcross) {
+  if constexpr (kFeatList) {
+    fl.init(A.feat + (int64_t)f0 * 2, A.ld_feat, A.n_feat - f0, A.rows + pl.first, A.magic, A.shift, K);
+  } else if constexpr (kFeatAcross) {
+    fl.init(A.feat + (kGrad ? pl.first * A.ld_feat : pl.expert * A.feat_expert) + (int64_t)f0 * 2, A.ld_feat,
+            A.n_feat - f0);
+  } else {
     const char *base = A.feat + pl.expert * A.feat_expert;
-    fa.init([&](int n) {
+    fl.init([&](int n) {
       if constexpr (P == kUp) {
         const int w = n / TF, x = n % TF, f = min(f0 + w * (TF / 2) + x % (TF / 2), A.F - 1);
         return base + (int64_t)(f + (x < TF / 2 ? 0 : A.Fp)) * A.ld_feat;
@@ -262,23 +327,8 @@ __global__ __launch_bounds__(WR *WF * 64) void product_kernel(Args A) {
   auto issue = [&](int s) {
     char *at = smem + (s & 1) * kBytes;
     const int k0 = s * kStep;
-    if constexpr (kRowAcross) {
-      rx.issue(at, wave, k0, K, A.n_row - r0, [&](int k) {
-        return A.row + (P == kGradW2 ? token(k) : (int64_t)(pl.first + k)) * A.ld_row + (int64_t)r0 * 2;
-      });
-    } else {
-      ra.issue(at, wave, k0, K);
-    }
-    if constexpr (kFeatAcross) {
-      fx.issue(at + BR * kStep * 2, wave, k0, K, A.n_feat - f0, [&](int k) {
-        if constexpr (kGrad)
-          return A.feat + (P == kGradW1 ? token(k) : (int64_t)(pl.first + k)) * A.ld_feat + (int64_t)f0 * 2;
-        else
-          return A.feat + pl.expert * A.feat_expert + (int64_t)k * A.ld_feat + (int64_t)f0 * 2;
-      });
-    } else {
-      fa.issue(at + BR * kStep * 2, wave, k0, K);
-    }
+    rl.issue(at, wave, k0, K);
+    fl.issue(at + BR * kStep * 2, wave, k0, K);
   };
 
   f32x4 acc[FF][FR];
@@ -291,14 +341,14 @@ __global__ __launch_bounds__(WR *WF * 64) void product_kernel(Args A) {
   for (int s = 0; s < steps; ++s) {
     __syncthreads();  // stage s has landed, and the other one has been read
     if (s + 1 < steps) issue(s + 1);
-    const char *rl = smem + (s & 1) * kBytes, *fl = rl + BR * kStep * 2;
+    const char *rows = smem + (s & 1) * kBytes, *feats = rows + BR * kStep * 2;
 #pragma unroll
     for (int kk = 0; kk < kStep / 32; ++kk) {
       i16x8 fo[FF], ro[FR];
 #pragma unroll
-      for (int a = 0; a < FF; ++a) fo[a] = operand<BF, kFeatAcross>(fl, wf * TF + a * 16, kk);
+      for (int a = 0; a < FF; ++a) fo[a] = operand<BF, kFeatAcross>(feats, wf * TF + a * 16, kk);
 #pragma unroll
-      for (int b = 0; b < FR; ++b) ro[b] = operand<BR, kRowAcross>(rl, wr * TR + b * 16, kk);
+      for (int b = 0; b < FR; ++b) ro[b] = operand<BR, kRowAcross>(rows, wr * TR + b * 16, kk);
 #pragma unroll
       for (int a = 0; a < FF; ++a)
 #pragma unroll
@@ -386,7 +436,7 @@ __global__ __launch_bounds__(WR *WF * 64) void product_kernel(Args A) {
       if (g == 0) part[wf * BR + wr * TR + b * 16 + j] = v;
     }
     __syncthreads();
-    const int nt = (A.n_feat + BF - 1) / BF;
+    const int nt = A.dot_tiles;
     for (int r = threadIdx.x; r < BR; r += THREADS) {
       if (r0 + r >= n_rows) continue;
       float v = 0.f;
@@ -548,14 +598,22 @@ hipError_t run_product(const Args &A, int64_t n_assign, hipStream_t st) {
   return hipGetLastError();
 }
 
+bool large_tiles(int64_t n_assign, int experts) { return n_assign / experts >= 128; }
+
 template <typename T, int P>
 hipError_t product(const Args &A, int64_t n_assign, hipStream_t st) {
+  if (large_tiles(n_assign, A.experts)) return run_product<T, P, 256, 256, 2, 4>(A, n_assign, st);
   return run_product<T, P, 128, 128, 2, 2>(A, n_assign, st);
 }
 
 Args base_args(const cfp_experts_desc &d) {
   Args A{};
-  A.offsets = d.offsets, A.rows = d.rows, A.experts = d.n_experts, A.per_token = d.k;
+  A.offsets = d.offsets, A.rows = d.rows, A.experts = d.n_experts;
+  // a / k for 0 <= a < 2^31: with 2^c >= k, magic = ceil(2^(31 + c) / k) < 2^32 exceeds the quotient by less than
+  // k / 2^(31 + c) relative to 1 / k, and a times that is below 1 / k
+  int c = 0;
+  while ((1 << c) < d.k) ++c;
+  A.shift = 31 + c, A.magic = (uint32_t)((((uint64_t)1 << A.shift) + d.k - 1) / d.k);
   A.F = d.inner, A.Fp = (int)up(d.inner, 8), A.weight = d.weight;
   return A;
 }
@@ -632,11 +690,12 @@ hipError_t backward(const cfp_experts_desc &d, const void *dy, int64_t dy_stride
   const int64_t n = d.n_tokens * d.k;
   Args A = base_args(d);
   hipError_t e = hipSuccess;
+  const int dot_tile = large_tiles(n, d.n_experts) ? 256 : kMinFeatTile, dots = (int)((L.Fp + dot_tile - 1) / dot_tile);
   if (n > 0) {
   // p = dy W2, and what follows from it
   A.row = L.dy, A.ld_row = L.ld_dy, A.feat = L.w2, A.ld_feat = L.Fp * 2, A.feat_expert = (int64_t)d.hidden * L.Fp * 2;
   A.K = d.hidden, A.n_feat = (int)L.Fp, A.h = const_cast<float *>(h), A.out = ws + r.dgu, A.ld_out = 2 * L.Fp;
-  A.out2 = ws + r.act, A.dot = reinterpret_cast<float *>(ws + r.dot);
+  A.out2 = ws + r.act, A.dot = reinterpret_cast<float *>(ws + r.dot), A.dot_tiles = dots;
   if ((e = product<T, kBackUp>(A, n, st)) != hipSuccess) return e;
   // rows of dx
   A = base_args(d);
@@ -656,9 +715,8 @@ hipError_t backward(const cfp_experts_desc &d, const void *dy, int64_t dy_stride
   A.feat = reinterpret_cast<const char *>(ws + r.act), A.ld_feat = L.Fp * 2, A.n_feat = d.inner, A.out = dw2,
   A.ld_out = d.inner;
   if ((e = product<T, kGradW2>(A, n, st)) != hipSuccess || n == 0) return e;
-  const int nt = (int)((L.Fp + kMinFeatTile - 1) / kMinFeatTile);
   return combine<T>(d, reinterpret_cast<const float *>(ws + r.out), nullptr, dx,
-                    reinterpret_cast<const float *>(ws + r.dot), nt, dweight, st);
+                    reinterpret_cast<const float *>(ws + r.dot), dots, dweight, st);
 }
 
 }  // namespace
