@@ -107,8 +107,9 @@ typedef struct {
 
 /* Stable order of the assignments a = token * k + place by expert:
  *   offsets [n_experts + 1]   expert e has the positions offsets[e] .. offsets[e+1] - 1
- *   rows    [n_tokens * k]    assignment at each position, -1 behind the last one kept
+ *   rows    [n_tokens * k + CFP_PLAN_PAD]  assignment at each position, -1 behind the last one kept
  *   slot    [n_tokens * k]    position of each assignment, -1 where it is dropped */
+#define CFP_PLAN_PAD 16
 size_t cfp_expert_plan_workspace_bytes(const cfp_plan_desc *d);
 int cfp_expert_plan(const cfp_plan_desc *d, int32_t *offsets, int32_t *rows, int32_t *slot, void *ws, size_t ws_bytes,
                     void *stream);

@@ -25,6 +25,7 @@ LIB_PATH = os.path.join(HERE, "libcfp_block.so")
 
 CFP_DT_F32, CFP_DT_F16, CFP_DT_BF16 = 0, 1, 2
 SCORES = {"softmax": 0, "sigmoid": 1}
+CFP_PLAN_PAD = 16  # entries behind the last of a plan's rows
 GROUP_SCORES = {"max": 0, "top2": 1}
 
 EXPORTED = ("cfp_qk_norm_rope", "cfp_qk_workspace_bytes", "cfp_qk_norm_rope_bwd", "cfp_route", "cfp_route_bwd",
@@ -302,11 +303,12 @@ def expert_plan(index, n_experts, *, first=0, stream=None) -> ExpertPlan:
         d = cfp_plan_desc(T, k, int(n_experts), int(first), index.data_ptr())
         n, e = T * k, int(n_experts)
         need = int(lib().cfp_expert_plan_workspace_bytes(ctypes.byref(d)))
-        buf = torch.empty(max(e, 0) + 1 + 2 * n + need // 4, dtype=torch.int32, device=index.device)
-        plan = ExpertPlan(buf[:e + 1], buf[e + 1:e + 1 + n], buf[e + 1 + n:e + 1 + 2 * n], T, k, e, int(first))
+        r, s = max(e, 0) + 1, max(e, 0) + 1 + n + CFP_PLAN_PAD  # where rows and slot begin
+        buf = torch.empty(s + n + need // 4, dtype=torch.int32, device=index.device)
+        plan = ExpertPlan(buf[:r], buf[r:r + n], buf[s:s + n], T, k, e, int(first))
         at = buf.data_ptr()
         _check("cfp_expert_plan", lib().cfp_expert_plan(
-            ctypes.byref(d), at, at + 4 * (e + 1), at + 4 * (e + 1 + n), at + 4 * (e + 1 + 2 * n), need, _stream(stream)))
+            ctypes.byref(d), at, at + 4 * r, at + 4 * s, at + 4 * (s + n), need, _stream(stream)))
     return plan
 
 

@@ -110,7 +110,7 @@ size_t cfp_expert_plan_workspace_bytes(const cfp_plan_desc *d) {
 int cfp_expert_plan(const cfp_plan_desc *d, int32_t *offsets, int32_t *rows, int32_t *slot, void *ws, size_t ws_bytes,
                     void *stream) {
   if (int e = check_plan(d)) return e;
-  if (!offsets || (d->n_tokens > 0 && (!rows || !slot))) return CFP_ERR_ARG;
+  if (!offsets || !rows || (d->n_tokens > 0 && !slot)) return CFP_ERR_ARG;
   const size_t need = plan_bytes(d->n_tokens * d->k, d->n_experts);
   if (need && (!ws || ws_bytes < need)) return CFP_ERR_WORKSPACE;
   return status(launch_expert_plan(*d, offsets, rows, slot, (int32_t *)ws, (hipStream_t)stream));

@@ -32,139 +32,183 @@ typedef __attribute__((address_space(1))) const void global_void;
 
 __device__ const uint32_t g_zero[64] = {};  // what a load past the end of the sum's axis reads
 
+// c += a b on the matrix unit, the sums in accumulation registers.  Written as an
+// instruction because the register allocator, given 256 sums a lane, moves them between both
+// halves of the register file inside the loop; it neither knows nor has to know the
+// instruction's latency, as a sum is used again only FF * FR instructions later and
+// read after settle().
 template <typename T>
-__device__ __forceinline__ f32x4 mfma(i16x8 a, i16x8 b, f32x4 c) {
+__device__ __forceinline__ void mfma(i16x8 a, i16x8 b, f32x4 &c) {
   if constexpr (std::is_same<T, bf16_t>::value)
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
   else
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
 }
 
-constexpr int kStep = 64;  // of the sum's axis in a stage: 128 bytes
+// Waits until every matrix instruction has written its sums (at most 18 cycles).
+template <int M, int N>
+__device__ __forceinline__ void settle(f32x4 (&acc)[M][N]) {
+  asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+#pragma unroll
+  for (int a = 0; a < M; ++a)
+#pragma unroll
+    for (int b = 0; b < N; ++b) asm volatile("" : "+a"(acc[a][b]));
+}
+
+constexpr int kStep = 32;  // entries of the sum's axis in a stage: one matrix instruction's
 
 // ---------------------------------------------------------------- operands --
 //
-// A stage of an operand is EXT vectors of 64 entries of the sum's axis, 16-byte
+// A stage of an operand is EXT vectors of 32 entries of the sum's axis, 16-byte
 // pieces copied from memory straight into LDS.  An operand whose sum's axis is
-// contiguous in memory ("along") lies as [EXT][8 pieces], piece c of vector r at
-// place c ^ (r & 7); one whose vectors' axis is contiguous ("across") as
-// [64][EXT / 8 pieces] and is transposed by the read (ds_read_b64_tr_b16), with
-// the places permuted so that the 16 rows of one read meet different banks.
+// contiguous in memory ("along") lies as [EXT][4 pieces], piece c of vector r at
+// place c ^ (r >> 2 & 3), so that eight lanes that read one piece of eight vectors
+// meet all 64 banks; one whose vectors' axis is contiguous ("across") lies as
+// [32][EXT / 8 pieces] and is transposed by the read (ds_read_b64_tr_b16), with the
+// places permuted so that the 16 rows of one read meet different banks.  Each
+// wave copies kLoads pieces a lane; copy<I>() makes one of them.
 
 template <int EXT>
 __device__ __forceinline__ int across_place(int krow, int c) {
   return c ^ ((((krow & 3) | ((krow >> 3 & 1) << 2)) << 1) & (EXT / 8 - 1));
 }
 
-__device__ __forceinline__ void copy16(const char *from, char *to) {
-  __builtin_amdgcn_global_load_lds((global_void *)from, (lds_void *)to, 16, 0, 0);
+// 16 bytes a lane from `from` to LDS, at byte `to` for the wave's first lane and on from there.  An
+// instruction of its own, as the compiler would wait for every copy before each transposing
+// read; its only registers are read when it is issued.  The waits are product_kernel's.
+__device__ __forceinline__ void copy16(const char *from, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory");
 }
 
-template <int EXT, int THREADS>
+template <int N, typename F>
+__device__ __forceinline__ void each(F f) {  // f(0) .. f(N - 1), the index a constant
+  if constexpr (N > 0) {
+    each<N - 1>(f);
+    f(std::integral_constant<int, N - 1>{});
+  }
+}
+
+template <int EXT, int WAVES>
 struct Along {
-  static constexpr int kLoads = EXT * 8 / THREADS;
+  static constexpr int kLoads = EXT * 4 / (WAVES * 64);
   const char *p[kLoads];
-  int k;  // first entry of this thread's pieces
+  int k;  // first entry of this lane's pieces
+  bool in;
   // row(r): address of vector r
   template <typename F>
   __device__ __forceinline__ void init(F row) {
-    const int t = threadIdx.x;
-    k = ((t & 7) ^ (t >> 3 & 7)) * 8;
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    k = ((lane & 3) ^ (lane >> 4)) * 8;
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) p[i] = row(i * (THREADS / 8) + t / 8) + k * 2;
+    for (int i = 0; i < kLoads; ++i) p[i] = row((w * kLoads + i) * 16 + lane / 4) + k * 2;
   }
-  __device__ __forceinline__ void issue(char *lds, int wave, int k0, int K) {
-    const char *zero = reinterpret_cast<const char *>(g_zero);
-    const bool in = k0 + k < K;
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      copy16(in ? p[i] : zero, lds + (i * THREADS + wave * 64) * 16);
-      p[i] += kStep * 2;
-    }
+  __device__ __forceinline__ void begin(int k0, int K) { in = k0 + k < K; }
+  template <int I>
+  __device__ __forceinline__ void copy(uint32_t lds, int wave) {
+    copy16(in ? p[I] : reinterpret_cast<const char *>(g_zero), lds + (wave * kLoads + I) * 1024);
+    p[I] += kStep * 2;
   }
 };
 
-// Pieces of 16 rows of the sum's axis repeat a thread's place in them, so its column is one for all its loads.
-template <int EXT, int THREADS>
+template <int EXT, int WAVES>
 struct AcrossPlace {
-  static constexpr int kPer = EXT / 8, kRows = THREADS / kPer, kLoads = kStep / kRows;
-  static_assert(kRows % 16 == 0 && kLoads * kRows == kStep, "");
-  int kr, col;  // row of the first load, first vector
-  __device__ __forceinline__ void init(int ext) {
-    kr = threadIdx.x / kPer;
-    const int c = across_place<EXT>(kr, threadIdx.x % kPer) * 8;
-    col = c < ext ? c : 0;  // vectors past the end repeat the first ones and are not written
+  static constexpr int kPer = EXT / 8;              // pieces of a row
+  static constexpr int kRows = 64 / kPer;           // rows of a wave's load
+  static constexpr int kLoads = kStep / (WAVES * kRows);
+  static_assert(kLoads * WAVES * kRows == kStep, "");
+  __device__ __forceinline__ static int row(int wave, int i) {
+    return (wave * kLoads + i) * kRows + (int)(threadIdx.x & 63) / kPer;
+  }
+  // first vector of a load's piece; vectors past the end repeat the first ones and are not written
+  __device__ __forceinline__ static int col(int wave, int i, int ext) {
+    const int c = across_place<EXT>(row(wave, i), (int)(threadIdx.x & 63) % kPer) * 8;
+    return c < ext ? c : 0;
   }
 };
 
 // Rows at one distance.
-template <int EXT, int THREADS>
-struct Across : AcrossPlace<EXT, THREADS> {
-  using B = AcrossPlace<EXT, THREADS>;
-  const char *p;
-  int64_t ld;
-  __device__ __forceinline__ void init(const char *first, int64_t ld_, int ext) {
-    B::init(ext);
-    ld = ld_;
-    p = first + B::kr * ld + B::col * 2;
-  }
-  __device__ __forceinline__ void issue(char *lds, int wave, int k0, int K) {
-    const char *zero = reinterpret_cast<const char *>(g_zero);
+template <int EXT, int WAVES>
+struct Across : AcrossPlace<EXT, WAVES> {
+  using B = AcrossPlace<EXT, WAVES>;
+  const char *p[B::kLoads];
+  int64_t step;
+  int left;  // rows left of the sum's axis at the stage
+  __device__ __forceinline__ void init(const char *first, int64_t ld, int ext) {
+    const int wave = threadIdx.x >> 6;
 #pragma unroll
-    for (int i = 0; i < B::kLoads; ++i) {
-      const char *from = p + (int64_t)(i * B::kRows) * ld;
-      copy16(k0 + i * B::kRows + B::kr < K ? from : zero, lds + (i * THREADS + wave * 64) * 16);
-    }
-    p += kStep * ld;
+    for (int i = 0; i < B::kLoads; ++i) p[i] = first + B::row(wave, i) * ld + B::col(wave, i, ext) * 2;
+    step = kStep * ld;
+  }
+  __device__ __forceinline__ void begin(int k0, int K) { left = K - k0; }
+  template <int I>
+  __device__ __forceinline__ void copy(uint32_t lds, int wave) {
+    copy16(B::row(wave, I) < left ? p[I] : reinterpret_cast<const char *>(g_zero), lds + (wave * B::kLoads + I) * 1024);
+    p[I] += step;
   }
 };
 
-// Rows by a list, whose entries are read a stage ahead.
-template <int EXT, int THREADS>
-struct AcrossList : AcrossPlace<EXT, THREADS> {
-  using B = AcrossPlace<EXT, THREADS>;
-  const char *p;
+// Rows by a list of assignments, whose entries a wave reads a stage ahead in scalar loads.
+template <int EXT, int WAVES>
+struct AcrossList : AcrossPlace<EXT, WAVES> {
+  using B = AcrossPlace<EXT, WAVES>;
+  typedef __attribute__((address_space(4))) const int32_t scalar_int;
+  static constexpr int kEach = B::kLoads * B::kRows;  // rows of a wave
+  static_assert(kEach <= CFP_PLAN_PAD, "");
+  const char *p[B::kLoads];
   int64_t ld;
-  const int32_t *list;
+  scalar_int *list;
   uint32_t magic, shift;
-  int32_t next[B::kLoads];
+  int32_t now[kEach], next[kEach];
+  int left;
   __device__ __forceinline__ void init(const char *base, int64_t ld_, int ext, const int32_t *list_, uint32_t m,
-                                       uint32_t sh, int K) {
-    B::init(ext);
-    ld = ld_, list = list_, magic = m, shift = sh;
-    p = base + B::col * 2;
-    fetch(0, K);
-  }
-  __device__ __forceinline__ void fetch(int k0, int K) {
+                                       uint32_t sh, int wave, int K) {
 #pragma unroll
-    for (int i = 0; i < B::kLoads; ++i) {
-      const int k = k0 + i * B::kRows + B::kr;
-      next[i] = k < K ? list[k] : -1;
-    }
+    for (int i = 0; i < B::kLoads; ++i) p[i] = base + B::col(wave, i, ext) * 2;
+    ld = ld_, list = (scalar_int *)list_, magic = m, shift = sh;
+    fetch(wave * kEach, K);
   }
-  __device__ __forceinline__ void issue(char *lds, int wave, int k0, int K) {
-    const char *zero = reinterpret_cast<const char *>(g_zero);
+  // the list goes on for CFP_PLAN_PAD entries behind its last; those past the sum's end are not used
+  __device__ __forceinline__ void fetch(int k, int K) {
+    scalar_int *at = list + min(k, K);
 #pragma unroll
-    for (int i = 0; i < B::kLoads; ++i) {
-      const int64_t row = (uint64_t)(uint32_t)next[i] * magic >> shift;
-      copy16(next[i] >= 0 ? p + row * ld : zero, lds + (i * THREADS + wave * 64) * 16);
+    for (int i = 0; i < kEach; ++i) next[i] = at[i];
+  }
+  __device__ __forceinline__ void begin(int k0, int K) {
+    left = K - k0;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) now[i] = next[i];
+    fetch(k0 + kStep + wave * kEach, K);
+  }
+  __device__ __forceinline__ int64_t offset(int32_t a) const {
+    return (int64_t)((uint64_t)(uint32_t)a * magic >> shift) * ld;
+  }
+  template <int I>
+  __device__ __forceinline__ void copy(uint32_t lds, int wave) {
+    const int sub = (int)(threadIdx.x & 63) / B::kPer;
+    int64_t off = offset(now[I * B::kRows]);
+#pragma unroll
+    for (int x = 1; x < B::kRows; ++x) {
+      const int64_t o = offset(now[I * B::kRows + x]);
+      off = sub == x ? o : off;
     }
-    fetch(k0 + kStep, K);
+    const char *from = p[I] + off;
+    copy16(B::row(wave, I) < left ? from : reinterpret_cast<const char *>(g_zero), lds + (wave * B::kLoads + I) * 1024);
   }
 };
 
-// Operand of one matrix instruction: 16 vectors from r0, 32 entries from kk * 32.
+// Operand of one matrix instruction: 16 vectors from r0.
 template <int EXT, bool ACROSS>
-__device__ __forceinline__ i16x8 operand(const char *lds, int r0, int kk) {
+__device__ __forceinline__ i16x8 operand(const char *lds, int r0) {
   const int l = threadIdx.x & 63, j = l & 15, g = l >> 4;
   if constexpr (!ACROSS) {
     const int r = r0 + j;
-    return *reinterpret_cast<const i16x8 *>(lds + r * 128 + (((kk * 4 + g) ^ (r & 7)) << 4));
+    return *reinterpret_cast<const i16x8 *>(lds + r * 64 + ((g ^ (r >> 2 & 3)) << 4));
   } else {
     i16x8 v;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int kr = kk * 32 + g * 8 + h * 4 + (j >> 2), c = r0 + (j & 3) * 4;
+      const int kr = g * 8 + h * 4 + (j >> 2), c = r0 + (j & 3) * 4;
       const char *at = lds + kr * (EXT * 2) + (across_place<EXT>(kr, c >> 3) << 4) + (c & 7) * 2;
       const i16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)at);
 #pragma unroll
@@ -255,9 +299,15 @@ __device__ __forceinline__ float sigmoid(float x) { return 1.f / (1.f + __expf(-
 
 // BR rows x BF features by WR x WF waves.  The features are the matrix instruction's
 // first operand, so that a lane holds four consecutive features of one row.
-template <typename T, int P, int BR, int BF, int WR, int WF>
-__global__ __launch_bounds__(WR *WF * 64) void product_kernel(Args A) {
-  constexpr int THREADS = WR * WF * 64;
+//
+// STAGES stages of 32 entries of the sum's axis lie in LDS.  While the matrix units
+// work on the operands of stage s, which are in registers, the operands of stage s + 1 are
+// read from LDS, one pair before each run of FR instructions, and stage s + STAGES is copied
+// over stage s, which every wave has read: one barrier a stage, and copies have STAGES - 1
+// stages to land.  Copies past the end of the sum read zeros, so that their count is constant.
+template <typename T, int P, int BR, int BF, int WR, int WF, int STAGES, int PER_CU>
+__global__ __launch_bounds__(WR *WF * 64, PER_CU *WR *WF / 4) void product_kernel(Args A) {
+  constexpr int WAVES = WR * WF, THREADS = WAVES * 64;
   constexpr int TR = BR / WR, TF = BF / WF, FR = TR / 16, FF = TF / 16;
   constexpr bool kGrad = P == kGradW1 || P == kGradW2;
   constexpr bool kRowAcross = kGrad, kFeatAcross = kGrad || P == kBackUp || P == kBackDown;
@@ -289,14 +339,14 @@ __global__ __launch_bounds__(WR *WF * 64) void product_kernel(Args A) {
   const int n_rows = kGrad ? A.n_row : pl.count;
 
   constexpr bool kRowList = P == kGradW2, kFeatList = P == kGradW1;
-  using RowLoad = std::conditional_t<!kRowAcross, Along<BR, THREADS>,
-                                     std::conditional_t<kRowList, AcrossList<BR, THREADS>, Across<BR, THREADS>>>;
-  using FeatLoad = std::conditional_t<!kFeatAcross, Along<BF, THREADS>,
-                                      std::conditional_t<kFeatList, AcrossList<BF, THREADS>, Across<BF, THREADS>>>;
+  using RowLoad = std::conditional_t<!kRowAcross, Along<BR, WAVES>,
+                                     std::conditional_t<kRowList, AcrossList<BR, WAVES>, Across<BR, WAVES>>>;
+  using FeatLoad = std::conditional_t<!kFeatAcross, Along<BF, WAVES>,
+                                      std::conditional_t<kFeatList, AcrossList<BF, WAVES>, Across<BF, WAVES>>>;
   RowLoad rl;
   FeatLoad fl;
   if constexpr (kRowList) {
-    rl.init(A.row + (int64_t)r0 * 2, A.ld_row, A.n_row - r0, A.rows + pl.first, A.magic, A.shift, K);
+    rl.init(A.row + (int64_t)r0 * 2, A.ld_row, A.n_row - r0, A.rows + pl.first, A.magic, A.shift, wave, K);
   } else if constexpr (kRowAcross) {
     rl.init(A.row + pl.first * A.ld_row + (int64_t)r0 * 2, A.ld_row, A.n_row - r0);
   } else {
@@ -309,7 +359,7 @@ __global__ __launch_bounds__(WR *WF * 64) void product_kernel(Args A) {
     });
   }
   if constexpr (kFeatList) {
-    fl.init(A.feat + (int64_t)f0 * 2, A.ld_feat, A.n_feat - f0, A.rows + pl.first, A.magic, A.shift, K);
+    fl.init(A.feat + (int64_t)f0 * 2, A.ld_feat, A.n_feat - f0, A.rows + pl.first, A.magic, A.shift, wave, K);
   } else if constexpr (kFeatAcross) {
     fl.init(A.feat + (kGrad ? pl.first * A.ld_feat : pl.expert * A.feat_expert) + (int64_t)f0 * 2, A.ld_feat,
             A.n_feat - f0);
@@ -324,11 +374,13 @@ __global__ __launch_bounds__(WR *WF * 64) void product_kernel(Args A) {
       }
     });
   }
-  auto issue = [&](int s) {
-    char *at = smem + (s & 1) * kBytes;
-    const int k0 = s * kStep;
-    rl.issue(at, wave, k0, K);
-    fl.issue(at + BR * kStep * 2, wave, k0, K);
+  constexpr int kRowLoads = RowLoad::kLoads, kLoads = kRowLoads + FeatLoad::kLoads;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void *)smem;  // byte in LDS
+  auto copy = [&](auto i, uint32_t at) {
+    if constexpr (i.value < kRowLoads)
+      rl.template copy<i.value>(at, wave);
+    else
+      fl.template copy<i.value - kRowLoads>(at + BR * kStep * 2, wave);
   };
 
   f32x4 acc[FF][FR];
@@ -337,23 +389,57 @@ __global__ __launch_bounds__(WR *WF * 64) void product_kernel(Args A) {
 #pragma unroll
     for (int b = 0; b < FR; ++b) acc[a][b] = f32x4{0.f, 0.f, 0.f, 0.f};
   const int steps = (K + kStep - 1) / kStep;
-  if (steps > 0) issue(0);
-  for (int s = 0; s < steps; ++s) {
-    __syncthreads();  // stage s has landed, and the other one has been read
-    if (s + 1 < steps) issue(s + 1);
-    const char *rows = smem + (s & 1) * kBytes, *feats = rows + BR * kStep * 2;
+  if (steps > 0) {
 #pragma unroll
-    for (int kk = 0; kk < kStep / 32; ++kk) {
-      i16x8 fo[FF], ro[FR];
-#pragma unroll
-      for (int a = 0; a < FF; ++a) fo[a] = operand<BF, kFeatAcross>(feats, wf * TF + a * 16, kk);
-#pragma unroll
-      for (int b = 0; b < FR; ++b) ro[b] = operand<BR, kRowAcross>(rows, wr * TR + b * 16, kk);
-#pragma unroll
-      for (int a = 0; a < FF; ++a)
-#pragma unroll
-        for (int b = 0; b < FR; ++b) acc[a][b] = mfma<T>(fo[a], ro[b], acc[a][b]);
+    for (int s = 0; s < STAGES; ++s) {
+      rl.begin(s * kStep, K);
+      fl.begin(s * kStep, K);
+      each<kLoads>([&](auto i) { copy(i, lds0 + s * kBytes); });
     }
+    i16x8 fo[2][FF], ro[2][FR];
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((STAGES - 1) * kLoads) : "memory");
+    {
+      const char *rows = smem, *feats = smem + BR * kStep * 2;
+#pragma unroll
+      for (int a = 0; a < FF; ++a) fo[0][a] = operand<BF, kFeatAcross>(feats, wf * TF + a * 16);
+#pragma unroll
+      for (int b = 0; b < FR; ++b) ro[0][b] = operand<BR, kRowAcross>(rows, wr * TR + b * 16);
+    }
+    int slot = 0;
+    auto stage = [&](int s, auto now) {
+      constexpr int c = now.value, n = 1 - c;
+      // stage s + 1 has landed for every wave, and every wave has read stage s
+      __builtin_amdgcn_sched_barrier(0);
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((STAGES - 2) * kLoads) : "memory");
+      __builtin_amdgcn_sched_barrier(0);
+      const uint32_t old = lds0 + slot * kBytes;
+      slot = slot + 1 == STAGES ? 0 : slot + 1;
+      const char *rows = smem + slot * kBytes, *feats = rows + BR * kStep * 2;
+      rl.begin((s + STAGES) * kStep, K);
+      fl.begin((s + STAGES) * kStep, K);
+      each<FF>([&](auto ac) {
+        constexpr int a = ac.value;
+        // the next operands are asked for behind the first half of the run, so that the wait for the
+        // present ones, which have long arrived, does not wait for these
+#pragma unroll
+        for (int b = 0; b < FR / 2; ++b) mfma<T>(fo[c][a], ro[c][b], acc[a][b]);
+        each<(a + 1) * kLoads / FF - a * kLoads / FF>([&](auto i) {
+          copy(std::integral_constant<int, a * kLoads / FF + i.value>{}, old);
+        });
+        fo[n][a] = operand<BF, kFeatAcross>(feats, wf * TF + a * 16);
+#pragma unroll
+        for (int b = a * FR / FF; b < (a + 1) * FR / FF; ++b) ro[n][b] = operand<BR, kRowAcross>(rows, wr * TR + b * 16);
+#pragma unroll
+        for (int b = FR / 2; b < FR; ++b) mfma<T>(fo[c][a], ro[c][b], acc[a][b]);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+    };
+    for (int s = 0; s < steps; s += 2) {  // an odd count ends with a stage of zeros
+      stage(s, std::integral_constant<int, 0>{});
+      stage(s + 1, std::integral_constant<int, 1>{});
+    }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");  // copies still on their way end before the LDS is used again
+    settle(acc);
   }
 
   // ---- epilogues: lane (j, g) holds features 4 g .. 4 g + 3 of row j of each 16 x 16 block
@@ -577,10 +663,10 @@ void pad(const void *in, int64_t ld, int64_t rows, int cols, int halves, void *o
                                    static_cast<uint16_t *>(out), out_rows, out_cols, n);
 }
 
-template <typename T, int P, int BR, int BF, int WR, int WF>
+template <typename T, int P, int BR, int BF, int WR, int WF, int STAGES, int PER_CU>
 hipError_t run_product(const Args &A, int64_t n_assign, hipStream_t st) {
   constexpr int kFeatTile = P == kUp ? BF / 2 : BF;
-  constexpr size_t lds = 2 * (BR + BF) * kStep * 2;
+  constexpr size_t lds = STAGES * (BR + BF) * kStep * 2;
   const int64_t nt = ((P == kUp ? A.F : A.n_feat) + kFeatTile - 1) / kFeatTile;
   int64_t grid;
   if (P == kGradW1 || P == kGradW2)
@@ -588,7 +674,7 @@ hipError_t run_product(const Args &A, int64_t n_assign, hipStream_t st) {
   else
     grid = nt * (n_assign / BR + std::min<int64_t>(A.experts, n_assign));
   if (grid > 0x7FFFFFFF) return hipErrorInvalidValue;
-  auto *kernel = product_kernel<T, P, BR, BF, WR, WF>;
+  auto *kernel = product_kernel<T, P, BR, BF, WR, WF, STAGES, PER_CU>;
   if (lds > 65536) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
                                              hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
@@ -602,8 +688,8 @@ bool large_tiles(int64_t n_assign, int experts) { return n_assign / experts >= 1
 
 template <typename T, int P>
 hipError_t product(const Args &A, int64_t n_assign, hipStream_t st) {
-  if (large_tiles(n_assign, A.experts)) return run_product<T, P, 256, 256, 2, 4>(A, n_assign, st);
-  return run_product<T, P, 128, 128, 2, 2>(A, n_assign, st);
+  if (large_tiles(n_assign, A.experts)) return run_product<T, P, 256, 256, 2, 2, 4, 1>(A, n_assign, st);
+  return run_product<T, P, 128, 128, 2, 2, 4, 2>(A, n_assign, st);
 }
 
 Args base_args(const cfp_experts_desc &d) {

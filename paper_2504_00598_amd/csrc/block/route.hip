@@ -349,6 +349,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_count_kernel(PlanArgs A) {
 __global__ __launch_bounds__(kPlanThreads) void plan_place_kernel(PlanArgs A) {
   extern __shared__ int32_t next[];  // [waves][bins], then start [bins]
   const int bins = A.experts + 1;
+  if (blockIdx.x == 0 && threadIdx.x < CFP_PLAN_PAD) A.rows[A.n + threadIdx.x] = -1;
   int32_t *start = next + kPlanWaves * bins;
   const int wave = threadIdx.x / 64, lane = threadIdx.x % 64;
   const int64_t lo = (int64_t)blockIdx.x * kPlanPiece, hi = min(lo + kPlanPiece, A.n);
