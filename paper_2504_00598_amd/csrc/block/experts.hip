@@ -30,8 +30,6 @@ typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
 typedef __attribute__((address_space(1))) const void global_void;
 
-__device__ const uint32_t g_zero[64] = {};  // what a load past the end of the sum's axis reads
-
 // c += a b on the matrix unit, the sums in accumulation registers.  Written as an
 // instruction because the register allocator, given 256 sums a lane, moves them between both
 // halves of the register file inside the loop; it neither knows nor has to know the
@@ -73,12 +71,32 @@ __device__ __forceinline__ int across_place(int krow, int c) {
   return c ^ ((((krow & 3) | ((krow >> 3 & 1) << 2)) << 1) & (EXT / 8 - 1));
 }
 
-// 16 bytes a lane from `from` to LDS, at byte `to` for the wave's first lane and on from there.  An
-// instruction of its own, as the compiler would wait for every copy before each transposing
-// read; its only registers are read when it is issued.  The waits are product_kernel's.
-__device__ __forceinline__ void copy16(const char *from, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory");
+// Copies of 16 bytes a lane from memory to LDS: lane l's land at the byte set by copy_to, plus I KiB,
+// plus 16 l.  Instructions of their own, as the compiler would wait for every copy before each
+// transposing read; their only registers are read when they are issued, and nothing else in the
+// kernel uses m0.  The instruction adds I KiB to the memory address as well, so that the
+// addresses given are I KiB lower.  The waits are product_kernel's.
+__device__ __forceinline__ void copy_to(uint32_t at) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0" ::"s"(at) : "memory");
 }
+template <int I>
+__device__ __forceinline__ void copy16(const char *from) {
+  asm volatile("global_load_lds_dwordx4 %0, off offset:%1" ::"v"(from), "n"(I * 1024) : "memory");
+}
+template <int I>
+__device__ __forceinline__ void copy16(const char *base, uint32_t off) {  // base: of the wave
+  asm volatile("global_load_lds_dwordx4 %0, %1 offset:%2" ::"v"(off), "s"(base), "n"(I * 1024) : "memory");
+}
+// A value that is the same for all lanes, in scalar registers.
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x);
+  const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)((uint64_t)x >> 32));
+  return (int64_t)((uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ const char *uniform(const char *p) {
+  return reinterpret_cast<const char *>(uniform(reinterpret_cast<int64_t>(p)));
+}
+constexpr int kBack = 4096;  // what wave bases lie lower, so that lane offsets stay positive
 
 template <int N, typename F>
 __device__ __forceinline__ void each(F f) {  // f(0) .. f(N - 1), the index a constant
@@ -88,25 +106,47 @@ __device__ __forceinline__ void each(F f) {  // f(0) .. f(N - 1), the index a co
   }
 }
 
-template <int EXT, int WAVES>
+// Rows in a run, from a base that all lanes share ("run"), or each with an address of its own.
+template <int EXT, int WAVES, bool RUN>
 struct Along {
   static constexpr int kLoads = EXT * 4 / (WAVES * 64);
-  const char *p[kLoads];
-  int k;  // first entry of this lane's pieces
-  bool in;
-  // row(r): address of vector r
+  static_assert(kLoads <= 4, "");
+  const char *base, *start;                                 // run: of the next stage and of the first, kBack lower
+  std::conditional_t<RUN, uint32_t, const char *> p[kLoads];  // run: offset from base; each of the vector's first entry
+  int k;         // first entry of this lane's pieces
+  uint32_t off;  // what this lane adds for the stage
+  // row(r): offset of vector r from `from`, or its address; the offsets stay below 2^31
   template <typename F>
-  __device__ __forceinline__ void init(F row) {
+  __device__ __forceinline__ void init(const char *from, F row) {
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     k = ((lane & 3) ^ (lane >> 4)) * 8;
+    start = base = uniform(from) - kBack;
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) p[i] = row((w * kLoads + i) * 16 + lane / 4) + k * 2;
+    for (int i = 0; i < kLoads; ++i) {
+      if constexpr (RUN)
+        p[i] = (uint32_t)row((w * kLoads + i) * 16 + lane / 4) + kBack - i * 1024;
+      else
+        p[i] = row((w * kLoads + i) * 16 + lane / 4) - i * 1024;
+    }
   }
-  __device__ __forceinline__ void begin(int k0, int K) { in = k0 + k < K; }
+  // pieces past the end of the sum's axis are the vector's first ones, which the reader masks
+  __device__ __forceinline__ void begin(int k0, int K) {
+    if constexpr (RUN) {
+      off = k < K - k0 ? k * 2 : 0;
+      if (k0 >= K) base = start;
+    } else {
+      off = k < K - k0 ? (uint32_t)(k0 + k) * 2 : 0;
+    }
+  }
   template <int I>
-  __device__ __forceinline__ void copy(uint32_t lds, int wave) {
-    copy16(in ? p[I] : reinterpret_cast<const char *>(g_zero), lds + (wave * kLoads + I) * 1024);
-    p[I] += kStep * 2;
+  __device__ __forceinline__ void copy() {
+    if constexpr (RUN)
+      copy16<I>(base, p[I] + off);
+    else
+      copy16<I>(p[I] + off);
+  }
+  __device__ __forceinline__ void end() {
+    if constexpr (RUN) base += kStep * 2;
   }
 };
 
@@ -115,7 +155,7 @@ struct AcrossPlace {
   static constexpr int kPer = EXT / 8;              // pieces of a row
   static constexpr int kRows = 64 / kPer;           // rows of a wave's load
   static constexpr int kLoads = kStep / (WAVES * kRows);
-  static_assert(kLoads * WAVES * kRows == kStep, "");
+  static_assert(kLoads * WAVES * kRows == kStep && kLoads <= 4, "");
   __device__ __forceinline__ static int row(int wave, int i) {
     return (wave * kLoads + i) * kRows + (int)(threadIdx.x & 63) / kPer;
   }
@@ -126,25 +166,35 @@ struct AcrossPlace {
   }
 };
 
-// Rows at one distance.
+// Rows at one distance (32 of them within 2^31 bytes).  Rows past the end of the sum's axis are the
+// first one, which the reader masks.
 template <int EXT, int WAVES>
 struct Across : AcrossPlace<EXT, WAVES> {
   using B = AcrossPlace<EXT, WAVES>;
-  const char *p[B::kLoads];
+  const char *base, *start;
+  uint32_t p[B::kLoads], far[B::kLoads];  // offset of the column, and of the row
   int64_t step;
-  int left;  // rows left of the sum's axis at the stage
+  int left, row0;
   __device__ __forceinline__ void init(const char *first, int64_t ld, int ext) {
     const int wave = threadIdx.x >> 6;
+    start = base = uniform(first) - kBack;
 #pragma unroll
-    for (int i = 0; i < B::kLoads; ++i) p[i] = first + B::row(wave, i) * ld + B::col(wave, i, ext) * 2;
-    step = kStep * ld;
+    for (int i = 0; i < B::kLoads; ++i) {
+      p[i] = B::col(wave, i, ext) * 2 + kBack - i * 1024;
+      far[i] = p[i] + B::row(wave, i) * (uint32_t)ld;
+    }
+    row0 = B::row(wave, 0);
+    step = kStep * uniform(ld);
   }
-  __device__ __forceinline__ void begin(int k0, int K) { left = K - k0; }
+  __device__ __forceinline__ void begin(int k0, int K) {
+    left = K - k0;
+    if (left <= 0) base = start;
+  }
   template <int I>
-  __device__ __forceinline__ void copy(uint32_t lds, int wave) {
-    copy16(B::row(wave, I) < left ? p[I] : reinterpret_cast<const char *>(g_zero), lds + (wave * B::kLoads + I) * 1024);
-    p[I] += step;
+  __device__ __forceinline__ void copy() {
+    copy16<I>(base, row0 + I * B::kRows < left ? far[I] : p[I]);
   }
+  __device__ __forceinline__ void end() { base += step; }
 };
 
 // Rows by a list of assignments, whose entries a wave reads a stage ahead in scalar loads.
@@ -159,32 +209,32 @@ struct AcrossList : AcrossPlace<EXT, WAVES> {
   scalar_int *list;
   uint32_t magic, shift;
   int32_t now[kEach], next[kEach];
-  int left;
+  int first;
   __device__ __forceinline__ void init(const char *base, int64_t ld_, int ext, const int32_t *list_, uint32_t m,
                                        uint32_t sh, int wave, int K) {
 #pragma unroll
-    for (int i = 0; i < B::kLoads; ++i) p[i] = base + B::col(wave, i, ext) * 2;
-    ld = ld_, list = (scalar_int *)list_, magic = m, shift = sh;
-    fetch(wave * kEach, K);
+    for (int i = 0; i < B::kLoads; ++i) p[i] = base + B::col(wave, i, ext) * 2 - i * 1024;
+    ld = uniform(ld_), list = (scalar_int *)uniform(reinterpret_cast<const char *>(list_)), magic = m, shift = sh;
+    first = wave * kEach;
+    fetch(first, K);
   }
-  // the list goes on for CFP_PLAN_PAD entries behind its last; those past the sum's end are not used
+  // The list goes on for CFP_PLAN_PAD entries behind its last.  Those past the end of the sum's axis are
+  // another expert's or -1, taken as 0: rows that exist, which the reader masks.
   __device__ __forceinline__ void fetch(int k, int K) {
     scalar_int *at = list + min(k, K);
 #pragma unroll
     for (int i = 0; i < kEach; ++i) next[i] = at[i];
   }
   __device__ __forceinline__ void begin(int k0, int K) {
-    left = K - k0;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) now[i] = next[i];
-    fetch(k0 + kStep + wave * kEach, K);
+    for (int i = 0; i < kEach; ++i) now[i] = max(__builtin_amdgcn_readfirstlane(next[i]), 0);
+    fetch(k0 + kStep + first, K);
   }
   __device__ __forceinline__ int64_t offset(int32_t a) const {
     return (int64_t)((uint64_t)(uint32_t)a * magic >> shift) * ld;
   }
   template <int I>
-  __device__ __forceinline__ void copy(uint32_t lds, int wave) {
+  __device__ __forceinline__ void copy() {
     const int sub = (int)(threadIdx.x & 63) / B::kPer;
     int64_t off = offset(now[I * B::kRows]);
 #pragma unroll
@@ -192,31 +242,47 @@ struct AcrossList : AcrossPlace<EXT, WAVES> {
       const int64_t o = offset(now[I * B::kRows + x]);
       off = sub == x ? o : off;
     }
-    const char *from = p[I] + off;
-    copy16(B::row(wave, I) < left ? from : reinterpret_cast<const char *>(g_zero), lds + (wave * B::kLoads + I) * 1024);
+    copy16<I>(p[I] + off);
   }
+  __device__ __forceinline__ void end() {}
 };
 
-// Operand of one matrix instruction: 16 vectors from r0.
-template <int EXT, bool ACROSS>
-__device__ __forceinline__ i16x8 operand(const char *lds, int r0) {
-  const int l = threadIdx.x & 63, j = l & 15, g = l >> 4;
-  if constexpr (!ACROSS) {
-    const int r = r0 + j;
-    return *reinterpret_cast<const i16x8 *>(lds + r * 64 + ((g ^ (r >> 2 & 3)) << 4));
-  } else {
-    i16x8 v;
+// Zeros from entry `have` on.
+__device__ __forceinline__ void mask(i16x8 &v, int have) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int kr = g * 8 + h * 4 + (j >> 2), c = r0 + (j & 3) * 4;
-      const char *at = lds + kr * (EXT * 2) + (across_place<EXT>(kr, c >> 3) << 4) + (c & 7) * 2;
-      const i16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)at);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) v[h * 4 + i] = x[i];
-    }
-    return v;
-  }
+  for (int i = 0; i < 8; ++i) v[i] = i < have ? v[i] : (short)0;
 }
+
+// What the matrix instructions take from a stage: the vectors from r0 on, 16 an instruction.
+template <int EXT, bool ACROSS, int N>
+struct Reader {
+  uint32_t at[ACROSS ? N : 1];  // byte of this lane's entries in a stage, for each 16 vectors
+  static constexpr int kReads = ACROSS ? 2 : 1;
+  __device__ __forceinline__ void init(int r0) {
+    const int l = threadIdx.x & 63, j = l & 15, g = l >> 4;
+    if constexpr (!ACROSS) {
+      at[0] = (r0 + j) * 64 + ((g ^ (j >> 2)) << 4);
+    } else {
+      const int kr = g * 8 + (j >> 2);
+#pragma unroll
+      for (int b = 0; b < N; ++b) {
+        const int c = r0 + b * 16 + (j & 3) * 4;
+        at[b] = kr * (EXT * 2) + (across_place<EXT>(kr, c >> 3) << 4) + (c & 7) * 2;
+      }
+    }
+  }
+  // one of kReads parts of the operand of vectors r0 + 16 B on, from the stage at `lds`
+  template <int B, int PART>
+  __device__ __forceinline__ void read(const char *lds, i16x8 &v) const {
+    if constexpr (!ACROSS) {
+      v = *reinterpret_cast<const i16x8 *>(lds + at[0] + B * 1024);
+    } else {
+      const i16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(lds + at[B] + PART * 4 * EXT * 2));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[PART * 4 + i] = x[i];
+    }
+  }
+};
 
 // ------------------------------------------------------------------- tiles --
 
@@ -264,7 +330,7 @@ __device__ __forceinline__ bool find(const Args &A, int nt, Place &p, int &ft) {
     int c = e < A.experts ? (A.offsets[e + 1] - A.offsets[e] + BR - 1) / BR : 0;
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) c += __shfl_xor(c, off, 64);
-    total += c;
+    total += __builtin_amdgcn_readfirstlane(c);
   }
   if ((int64_t)blockIdx.x >= (int64_t)total * nt) return false;
   const int id = dealt(blockIdx.x, total * nt);
@@ -304,7 +370,7 @@ __device__ __forceinline__ float sigmoid(float x) { return 1.f / (1.f + __expf(-
 // work on the operands of stage s, which are in registers, the operands of stage s + 1 are
 // read from LDS, one pair before each run of FR instructions, and stage s + STAGES is copied
 // over stage s, which every wave has read: one barrier a stage, and copies have STAGES - 1
-// stages to land.  Copies past the end of the sum read zeros, so that their count is constant.
+// stages to land.  Copies go on past the end of the sum, so that their count is constant.
 template <typename T, int P, int BR, int BF, int WR, int WF, int STAGES, int PER_CU>
 __global__ __launch_bounds__(WR *WF * 64, PER_CU *WR *WF / 4) void product_kernel(Args A) {
   constexpr int WAVES = WR * WF, THREADS = WAVES * 64;
@@ -339,9 +405,10 @@ __global__ __launch_bounds__(WR *WF * 64, PER_CU *WR *WF / 4) void product_kerne
   const int n_rows = kGrad ? A.n_row : pl.count;
 
   constexpr bool kRowList = P == kGradW2, kFeatList = P == kGradW1;
-  using RowLoad = std::conditional_t<!kRowAcross, Along<BR, WAVES>,
+  constexpr bool kGather = P == kUp || P == kBackUp;
+  using RowLoad = std::conditional_t<!kRowAcross, Along<BR, WAVES, !kGather>,
                                      std::conditional_t<kRowList, AcrossList<BR, WAVES>, Across<BR, WAVES>>>;
-  using FeatLoad = std::conditional_t<!kFeatAcross, Along<BF, WAVES>,
+  using FeatLoad = std::conditional_t<!kFeatAcross, Along<BF, WAVES, true>,
                                       std::conditional_t<kFeatList, AcrossList<BF, WAVES>, Across<BF, WAVES>>>;
   RowLoad rl;
   FeatLoad fl;
@@ -350,13 +417,15 @@ __global__ __launch_bounds__(WR *WF * 64, PER_CU *WR *WF / 4) void product_kerne
   } else if constexpr (kRowAcross) {
     rl.init(A.row + pl.first * A.ld_row + (int64_t)r0 * 2, A.ld_row, A.n_row - r0);
   } else {
-    constexpr bool kGather = P == kUp || P == kBackUp;
-    rl.init([&](int r) {
-      const int i = min(r0 + r, n_rows - 1);  // rows past the end repeat the last one and are not written
-      int64_t row = pl.first + i;
-      if constexpr (kGather) row = (uint64_t)(uint32_t)A.rows[row] * A.magic >> A.shift;
-      return A.row + row * A.ld_row;
-    });
+    // rows past the end repeat the last one and are not written
+    if constexpr (kGather)
+      rl.init(nullptr, [&](int r) {
+        const int64_t a = A.rows[pl.first + min(r0 + r, n_rows - 1)];
+        return A.row + (int64_t)((uint64_t)a * A.magic >> A.shift) * A.ld_row;
+      });
+    else
+      rl.init(A.row + (int64_t)(pl.first + r0) * A.ld_row,
+              [&](int r) { return (uint32_t)min(r, n_rows - 1 - r0) * (uint32_t)A.ld_row; });
   }
   if constexpr (kFeatList) {
     fl.init(A.feat + (int64_t)f0 * 2, A.ld_feat, A.n_feat - f0, A.rows + pl.first, A.magic, A.shift, wave, K);
@@ -364,24 +433,32 @@ __global__ __launch_bounds__(WR *WF * 64, PER_CU *WR *WF / 4) void product_kerne
     fl.init(A.feat + (kGrad ? pl.first * A.ld_feat : pl.expert * A.feat_expert) + (int64_t)f0 * 2, A.ld_feat,
             A.n_feat - f0);
   } else {
-    const char *base = A.feat + pl.expert * A.feat_expert;
-    fl.init([&](int n) {
+    fl.init(A.feat + pl.expert * A.feat_expert + (int64_t)f0 * A.ld_feat, [&](int n) {
       if constexpr (P == kUp) {
-        const int w = n / TF, x = n % TF, f = min(f0 + w * (TF / 2) + x % (TF / 2), A.F - 1);
-        return base + (int64_t)(f + (x < TF / 2 ? 0 : A.Fp)) * A.ld_feat;
+        const int w = n / TF, x = n % TF, f = min(w * (TF / 2) + x % (TF / 2), A.F - 1 - f0);
+        return (uint32_t)(f + (x < TF / 2 ? 0 : A.Fp)) * (uint32_t)A.ld_feat;
       } else {
-        return base + (int64_t)min(f0 + n, A.n_feat - 1) * A.ld_feat;
+        return (uint32_t)min(n, A.n_feat - 1 - f0) * (uint32_t)A.ld_feat;
       }
     });
   }
-  constexpr int kRowLoads = RowLoad::kLoads, kLoads = kRowLoads + FeatLoad::kLoads;
-  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void *)smem;  // byte in LDS
+  constexpr int kRowLoads = RowLoad::kLoads, kFeatLoads = FeatLoad::kLoads, kLoads = kRowLoads + kFeatLoads;
+  // where this wave's copies of a stage begin
+  const uint32_t row_to = (uint32_t)(uintptr_t)(lds_void *)smem + wave * kRowLoads * 1024;
+  const uint32_t feat_to = (uint32_t)(uintptr_t)(lds_void *)smem + BR * kStep * 2 + wave * kFeatLoads * 1024;
+  // copy i of a stage that lies `at` bytes behind the first
   auto copy = [&](auto i, uint32_t at) {
+    if constexpr (i.value == 0) copy_to(row_to + at);
+    if constexpr (i.value == kRowLoads) copy_to(feat_to + at);
     if constexpr (i.value < kRowLoads)
-      rl.template copy<i.value>(at, wave);
+      rl.template copy<i.value>();
     else
-      fl.template copy<i.value - kRowLoads>(at + BR * kStep * 2, wave);
+      fl.template copy<i.value - kRowLoads>();
   };
+  Reader<BF, kFeatAcross, FF> fread;
+  Reader<BR, kRowAcross, FR> rread;
+  fread.init(wf * TF);
+  rread.init(wr * TR);
 
   f32x4 acc[FF][FR];
 #pragma unroll
@@ -394,49 +471,69 @@ __global__ __launch_bounds__(WR *WF * 64, PER_CU *WR *WF / 4) void product_kerne
     for (int s = 0; s < STAGES; ++s) {
       rl.begin(s * kStep, K);
       fl.begin(s * kStep, K);
-      each<kLoads>([&](auto i) { copy(i, lds0 + s * kBytes); });
+      each<kLoads>([&](auto i) { copy(i, s * kBytes); });
+      rl.end();
+      fl.end();
     }
     i16x8 fo[2][FF], ro[2][FR];
     asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((STAGES - 1) * kLoads) : "memory");
-    {
-      const char *rows = smem, *feats = smem + BR * kStep * 2;
-#pragma unroll
-      for (int a = 0; a < FF; ++a) fo[0][a] = operand<BF, kFeatAcross>(feats, wf * TF + a * 16);
-#pragma unroll
-      for (int b = 0; b < FR; ++b) ro[0][b] = operand<BR, kRowAcross>(rows, wr * TR + b * 16);
-    }
+    each<FF>([&](auto a) {
+      each<fread.kReads>([&](auto h) { fread.template read<a.value, h.value>(smem + BR * kStep * 2, fo[0][a.value]); });
+    });
+    each<FR>([&](auto b) {
+      each<rread.kReads>([&](auto h) { rread.template read<b.value, h.value>(smem, ro[0][b.value]); });
+    });
     int slot = 0;
+    // One stage: FF * FR matrix instructions with the copies and reads spread evenly between them.
     auto stage = [&](int s, auto now) {
       constexpr int c = now.value, n = 1 - c;
+      constexpr int kReads = FF * fread.kReads + FR * rread.kReads, kOps = kLoads + kReads, kMfma = FF * FR;
       // stage s + 1 has landed for every wave, and every wave has read stage s
       __builtin_amdgcn_sched_barrier(0);
       asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((STAGES - 2) * kLoads) : "memory");
       __builtin_amdgcn_sched_barrier(0);
-      const uint32_t old = lds0 + slot * kBytes;
+      const uint32_t old = slot * kBytes;
       slot = slot + 1 == STAGES ? 0 : slot + 1;
       const char *rows = smem + slot * kBytes, *feats = rows + BR * kStep * 2;
       rl.begin((s + STAGES) * kStep, K);
       fl.begin((s + STAGES) * kStep, K);
-      each<FF>([&](auto ac) {
-        constexpr int a = ac.value;
-        // the next operands are asked for behind the first half of the run, so that the wait for the
-        // present ones, which have long arrived, does not wait for these
-#pragma unroll
-        for (int b = 0; b < FR / 2; ++b) mfma<T>(fo[c][a], ro[c][b], acc[a][b]);
-        each<(a + 1) * kLoads / FF - a * kLoads / FF>([&](auto i) {
-          copy(std::integral_constant<int, a * kLoads / FF + i.value>{}, old);
+      if ((s + 1) * kStep > K) {  // the sum ends in this stage: entries behind its end count for nothing in either operand
+        const int have = K - s * kStep - g * 8;
+        each<FF>([&](auto a) { mask(fo[c][a.value], have); });
+        each<FR>([&](auto b) { mask(ro[c][b.value], have); });
+      }
+      each<kMfma>([&](auto mc) {
+        constexpr int m = mc.value, a = m / FR, b = m % FR;
+        mfma<T>(fo[c][a], ro[c][b], acc[a][b]);
+        // operations o0 .. o1 - 1 of the stage follow this instruction: reads first, one copy in every kOps / kLoads
+        constexpr int o0 = m * kOps / kMfma, o1 = (m + 1) * kOps / kMfma;
+        each<o1 - o0>([&](auto oc) {
+          constexpr int o = o0 + oc.value;
+          constexpr int copies = (o + 1) * kLoads / kOps;  // up to and with this operation
+          if constexpr (copies > o * kLoads / kOps) {
+            copy(std::integral_constant<int, copies - 1>{}, old);
+          } else {
+            constexpr int r = o - copies;  // a read
+            if constexpr (r < FF * fread.kReads) {
+              constexpr int x = r / fread.kReads, h = r % fread.kReads;
+              fread.template read<x, h>(feats, fo[n][x]);
+            } else {
+              constexpr int x = (r - FF * fread.kReads) / rread.kReads, h = (r - FF * fread.kReads) % rread.kReads;
+              rread.template read<x, h>(rows, ro[n][x]);
+            }
+          }
         });
-        fo[n][a] = operand<BF, kFeatAcross>(feats, wf * TF + a * 16);
-#pragma unroll
-        for (int b = a * FR / FF; b < (a + 1) * FR / FF; ++b) ro[n][b] = operand<BR, kRowAcross>(rows, wr * TR + b * 16);
-#pragma unroll
-        for (int b = FR / 2; b < FR; ++b) mfma<T>(fo[c][a], ro[c][b], acc[a][b]);
-        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (o1 > o0) __builtin_amdgcn_sched_barrier(0);
       });
+      rl.end();
+      fl.end();
     };
-    for (int s = 0; s < steps; s += 2) {  // an odd count ends with a stage of zeros
+    for (int s = 0; s < steps; s += 2) {  // an odd count ends with a stage that is masked whole
       stage(s, std::integral_constant<int, 0>{});
       stage(s + 1, std::integral_constant<int, 1>{});
+      // a copy of a sum that the register allocator might place here reads it written
+      asm volatile("s_nop 10");
+      __builtin_amdgcn_sched_barrier(0);
     }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");  // copies still on their way end before the LDS is used again
     settle(acc);
