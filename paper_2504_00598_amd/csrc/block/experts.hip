@@ -53,16 +53,16 @@ __device__ __forceinline__ void settle(f32x4 (&acc)[M][N]) {
     for (int b = 0; b < N; ++b) asm volatile("" : "+a"(acc[a][b]));
 }
 
-constexpr int kStep = 32;  // entries of the sum's axis in a stage: one matrix instruction's
+constexpr int kStep = 64;  // entries of the sum's axis in a stage, 128 bytes: whole lines of the caches
 
 // ---------------------------------------------------------------- operands --
 //
-// A stage of an operand is EXT vectors of 32 entries of the sum's axis, 16-byte
+// A stage of an operand is EXT vectors of 64 entries of the sum's axis, 16-byte
 // pieces copied from memory straight into LDS.  An operand whose sum's axis is
-// contiguous in memory ("along") lies as [EXT][4 pieces], piece c of vector r at
-// place c ^ (r >> 2 & 3), so that eight lanes that read one piece of eight vectors
+// contiguous in memory ("along") lies as [EXT][8 pieces], piece c of vector r at
+// place c ^ (r & 7), so that eight lanes that read one piece of eight vectors
 // meet all 64 banks; one whose vectors' axis is contiguous ("across") lies as
-// [32][EXT / 8 pieces] and is transposed by the read (ds_read_b64_tr_b16), with the
+// [64][EXT / 8 pieces] and is transposed by the read (ds_read_b64_tr_b16), with the
 // places permuted so that the 16 rows of one read meet different banks.  Each
 // wave copies kLoads pieces a lane; copy<I>() makes one of them.
 
@@ -71,21 +71,21 @@ __device__ __forceinline__ int across_place(int krow, int c) {
   return c ^ ((((krow & 3) | ((krow >> 3 & 1) << 2)) << 1) & (EXT / 8 - 1));
 }
 
-// Copies of 16 bytes a lane from memory to LDS: lane l's land at the byte set by copy_to, plus I KiB,
+// Copies of 16 bytes a lane from memory to LDS: lane l's land at the byte set by copy_to, plus (I mod 4) KiB,
 // plus 16 l.  Instructions of their own, as the compiler would wait for every copy before each
 // transposing read; their only registers are read when they are issued, and nothing else in the
-// kernel uses m0.  The instruction adds I KiB to the memory address as well, so that the
-// addresses given are I KiB lower.  The waits are product_kernel's.
+// kernel uses m0.  The instruction adds (I mod 4) KiB to the memory address as well, so
+// that the addresses given are that much lower.  The waits are product_kernel's.
 __device__ __forceinline__ void copy_to(uint32_t at) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0" ::"s"(at) : "memory");
 }
 template <int I>
 __device__ __forceinline__ void copy16(const char *from) {
-  asm volatile("global_load_lds_dwordx4 %0, off offset:%1" ::"v"(from), "n"(I * 1024) : "memory");
+  asm volatile("global_load_lds_dwordx4 %0, off offset:%1" ::"v"(from), "n"(I % 4 * 1024) : "memory");
 }
 template <int I>
 __device__ __forceinline__ void copy16(const char *base, uint32_t off) {  // base: of the wave
-  asm volatile("global_load_lds_dwordx4 %0, %1 offset:%2" ::"v"(off), "s"(base), "n"(I * 1024) : "memory");
+  asm volatile("global_load_lds_dwordx4 %0, %1 offset:%2" ::"v"(off), "s"(base), "n"(I % 4 * 1024) : "memory");
 }
 // A value that is the same for all lanes, in scalar registers.
 __device__ __forceinline__ int64_t uniform(int64_t x) {
@@ -109,8 +109,7 @@ __device__ __forceinline__ void each(F f) {  // f(0) .. f(N - 1), the index a co
 // Rows in a run, from a base that all lanes share ("run"), or each with an address of its own.
 template <int EXT, int WAVES, bool RUN>
 struct Along {
-  static constexpr int kLoads = EXT * 4 / (WAVES * 64);
-  static_assert(kLoads <= 4, "");
+  static constexpr int kLoads = EXT * 8 / (WAVES * 64);
   const char *base, *start;                                 // run: of the next stage and of the first, kBack lower
   std::conditional_t<RUN, uint32_t, const char *> p[kLoads];  // run: offset from base; each of the vector's first entry
   int k;         // first entry of this lane's pieces
@@ -119,14 +118,14 @@ struct Along {
   template <typename F>
   __device__ __forceinline__ void init(const char *from, F row) {
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    k = ((lane & 3) ^ (lane >> 4)) * 8;
+    k = ((lane & 7) ^ (lane >> 3)) * 8;
     start = base = uniform(from) - kBack;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       if constexpr (RUN)
-        p[i] = (uint32_t)row((w * kLoads + i) * 16 + lane / 4) + kBack - i * 1024;
+        p[i] = (uint32_t)row((w * kLoads + i) * 8 + lane / 8) + kBack - i % 4 * 1024;
       else
-        p[i] = row((w * kLoads + i) * 16 + lane / 4) - i * 1024;
+        p[i] = row((w * kLoads + i) * 8 + lane / 8) - i % 4 * 1024;
     }
   }
   // pieces past the end of the sum's axis are the vector's first ones, which the reader masks
@@ -155,7 +154,7 @@ struct AcrossPlace {
   static constexpr int kPer = EXT / 8;              // pieces of a row
   static constexpr int kRows = 64 / kPer;           // rows of a wave's load
   static constexpr int kLoads = kStep / (WAVES * kRows);
-  static_assert(kLoads * WAVES * kRows == kStep && kLoads <= 4, "");
+  static_assert(kLoads * WAVES * kRows == kStep, "");
   __device__ __forceinline__ static int row(int wave, int i) {
     return (wave * kLoads + i) * kRows + (int)(threadIdx.x & 63) / kPer;
   }
@@ -166,7 +165,7 @@ struct AcrossPlace {
   }
 };
 
-// Rows at one distance (32 of them within 2^31 bytes).  Rows past the end of the sum's axis are the
+// Rows at one distance (64 of them within 2^31 bytes).  Rows past the end of the sum's axis are the
 // first one, which the reader masks.
 template <int EXT, int WAVES>
 struct Across : AcrossPlace<EXT, WAVES> {
@@ -180,7 +179,7 @@ struct Across : AcrossPlace<EXT, WAVES> {
     start = base = uniform(first) - kBack;
 #pragma unroll
     for (int i = 0; i < B::kLoads; ++i) {
-      p[i] = B::col(wave, i, ext) * 2 + kBack - i * 1024;
+      p[i] = B::col(wave, i, ext) * 2 + kBack - i % 4 * 1024;
       far[i] = p[i] + B::row(wave, i) * (uint32_t)ld;
     }
     row0 = B::row(wave, 0);
@@ -197,7 +196,7 @@ struct Across : AcrossPlace<EXT, WAVES> {
   __device__ __forceinline__ void end() { base += step; }
 };
 
-// Rows by a list of assignments, whose entries a wave reads a stage ahead in scalar loads.
+// Rows by a list of assignments, whose entries a wave reads in scalar loads before it copies.
 template <int EXT, int WAVES>
 struct AcrossList : AcrossPlace<EXT, WAVES> {
   using B = AcrossPlace<EXT, WAVES>;
@@ -208,30 +207,24 @@ struct AcrossList : AcrossPlace<EXT, WAVES> {
   int64_t ld;
   scalar_int *list;
   uint32_t magic, shift;
-  int32_t now[kEach], next[kEach];
+  int32_t now[kEach];
   int first;
   __device__ __forceinline__ void init(const char *base, int64_t ld_, int ext, const int32_t *list_, uint32_t m,
-                                       uint32_t sh, int wave, int K) {
+                                       uint32_t sh, int wave) {
 #pragma unroll
-    for (int i = 0; i < B::kLoads; ++i) p[i] = base + B::col(wave, i, ext) * 2 - i * 1024;
+    for (int i = 0; i < B::kLoads; ++i) p[i] = base + B::col(wave, i, ext) * 2 - i % 4 * 1024;
     ld = uniform(ld_), list = (scalar_int *)uniform(reinterpret_cast<const char *>(list_)), magic = m, shift = sh;
     first = wave * kEach;
-    fetch(first, K);
   }
   // The list goes on for CFP_PLAN_PAD entries behind its last.  Those past the end of the sum's axis are
   // another expert's or -1, taken as 0: rows that exist, which the reader masks.
-  __device__ __forceinline__ void fetch(int k, int K) {
-    scalar_int *at = list + min(k, K);
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) next[i] = at[i];
-  }
   __device__ __forceinline__ void begin(int k0, int K) {
+    scalar_int *at = list + min(k0 + first, K);
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) now[i] = max(__builtin_amdgcn_readfirstlane(next[i]), 0);
-    fetch(k0 + kStep + first, K);
+    for (int i = 0; i < kEach; ++i) now[i] = at[i];
   }
   __device__ __forceinline__ int64_t offset(int32_t a) const {
-    return (int64_t)((uint64_t)(uint32_t)a * magic >> shift) * ld;
+    return (int64_t)((uint64_t)(uint32_t)max(__builtin_amdgcn_readfirstlane(a), 0) * magic >> shift) * ld;
   }
   template <int I>
   __device__ __forceinline__ void copy() {
@@ -256,12 +249,13 @@ __device__ __forceinline__ void mask(i16x8 &v, int have) {
 // What the matrix instructions take from a stage: the vectors from r0 on, 16 an instruction.
 template <int EXT, bool ACROSS, int N>
 struct Reader {
-  uint32_t at[ACROSS ? N : 1];  // byte of this lane's entries in a stage, for each 16 vectors
+  uint32_t at[ACROSS ? N : 2];  // byte of this lane's entries in a stage, for each 16 vectors (along: for each half)
   static constexpr int kReads = ACROSS ? 2 : 1;
   __device__ __forceinline__ void init(int r0) {
     const int l = threadIdx.x & 63, j = l & 15, g = l >> 4;
     if constexpr (!ACROSS) {
-      at[0] = (r0 + j) * 64 + ((g ^ (j >> 2)) << 4);
+      at[0] = (r0 + j) * 128 + ((g ^ (j & 7)) << 4);
+      at[1] = at[0] ^ 64;
     } else {
       const int kr = g * 8 + (j >> 2);
 #pragma unroll
@@ -271,13 +265,14 @@ struct Reader {
       }
     }
   }
-  // one of kReads parts of the operand of vectors r0 + 16 B on, from the stage at `lds`
-  template <int B, int PART>
+  // one of kReads parts of the operand of vectors r0 + 16 B on, entries 32 HALF on, from the stage at `lds`
+  template <int B, int HALF, int PART>
   __device__ __forceinline__ void read(const char *lds, i16x8 &v) const {
     if constexpr (!ACROSS) {
-      v = *reinterpret_cast<const i16x8 *>(lds + at[0] + B * 1024);
+      v = *reinterpret_cast<const i16x8 *>(lds + at[HALF] + B * 2048);
     } else {
-      const i16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(lds + at[B] + PART * 4 * EXT * 2));
+      const i16x4 x =
+          __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(lds + at[B] + (HALF * 32 + PART * 4) * EXT * 2));
 #pragma unroll
       for (int i = 0; i < 4; ++i) v[PART * 4 + i] = x[i];
     }
@@ -366,12 +361,13 @@ __device__ __forceinline__ float sigmoid(float x) { return 1.f / (1.f + __expf(-
 // BR rows x BF features by WR x WF waves.  The features are the matrix instruction's
 // first operand, so that a lane holds four consecutive features of one row.
 //
-// STAGES stages of 32 entries of the sum's axis lie in LDS.  While the matrix units
-// work on the operands of stage s, which are in registers, the operands of stage s + 1 are
-// read from LDS, one pair before each run of FR instructions, and stage s + STAGES is copied
-// over stage s, which every wave has read: one barrier a stage, and copies have STAGES - 1
-// stages to land.  Copies go on past the end of the sum, so that their count is constant.
-template <typename T, int P, int BR, int BF, int WR, int WF, int STAGES, int PER_CU>
+// Two stages of 64 entries of the sum's axis lie in LDS; a matrix instruction takes half of one.  While
+// the matrix units work on the first half of stage s, whose operands are in registers, those of its
+// second half are read from LDS; then one barrier, after which every wave has read stage s and stage
+// s + 1 has landed; while they work on the second half, the first operands of stage s + 1 are read and
+// stage s + 2 is copied over stage s.  Reads and copies are spread between the matrix instructions.
+// Copies go on past the end of the sum, over rows that exist.
+template <typename T, int P, int BR, int BF, int WR, int WF, int PER_CU>
 __global__ __launch_bounds__(WR *WF * 64, PER_CU *WR *WF / 4) void product_kernel(Args A) {
   constexpr int WAVES = WR * WF, THREADS = WAVES * 64;
   constexpr int TR = BR / WR, TF = BF / WF, FR = TR / 16, FF = TF / 16;
@@ -388,9 +384,11 @@ __global__ __launch_bounds__(WR *WF * 64, PER_CU *WR *WF / 4) void product_kerne
   int ft, rt = 0, K;
   if constexpr (kGrad) {
     const int nf = (A.n_feat + BF - 1) / BF, nr = (A.n_row + BR - 1) / BR;
-    const int id = dealt(blockIdx.x, gridDim.x);
-    pl.expert = id / (nf * nr);
-    rt = id / nf % nr;
+    // every die takes a run of each expert's tiles, as the experts' sums differ in length
+    const int x = blockIdx.x & 7, i = blockIdx.x >> 3, run = (nf * nr + 7) / 8, id = x * run + i % run;
+    pl.expert = i / run;
+    if (id >= nf * nr) return;
+    rt = id / nf;
     ft = id % nf;
     pl.first = A.offsets[pl.expert];
     pl.count = A.offsets[pl.expert + 1] - pl.first;
@@ -413,7 +411,7 @@ __global__ __launch_bounds__(WR *WF * 64, PER_CU *WR *WF / 4) void product_kerne
   RowLoad rl;
   FeatLoad fl;
   if constexpr (kRowList) {
-    rl.init(A.row + (int64_t)r0 * 2, A.ld_row, A.n_row - r0, A.rows + pl.first, A.magic, A.shift, wave, K);
+    rl.init(A.row + (int64_t)r0 * 2, A.ld_row, A.n_row - r0, A.rows + pl.first, A.magic, A.shift, wave);
   } else if constexpr (kRowAcross) {
     rl.init(A.row + pl.first * A.ld_row + (int64_t)r0 * 2, A.ld_row, A.n_row - r0);
   } else {
@@ -428,7 +426,7 @@ __global__ __launch_bounds__(WR *WF * 64, PER_CU *WR *WF / 4) void product_kerne
               [&](int r) { return (uint32_t)min(r, n_rows - 1 - r0) * (uint32_t)A.ld_row; });
   }
   if constexpr (kFeatList) {
-    fl.init(A.feat + (int64_t)f0 * 2, A.ld_feat, A.n_feat - f0, A.rows + pl.first, A.magic, A.shift, wave, K);
+    fl.init(A.feat + (int64_t)f0 * 2, A.ld_feat, A.n_feat - f0, A.rows + pl.first, A.magic, A.shift, wave);
   } else if constexpr (kFeatAcross) {
     fl.init(A.feat + (kGrad ? pl.first * A.ld_feat : pl.expert * A.feat_expert) + (int64_t)f0 * 2, A.ld_feat,
             A.n_feat - f0);
@@ -448,8 +446,9 @@ __global__ __launch_bounds__(WR *WF * 64, PER_CU *WR *WF / 4) void product_kerne
   const uint32_t feat_to = (uint32_t)(uintptr_t)(lds_void *)smem + BR * kStep * 2 + wave * kFeatLoads * 1024;
   // copy i of a stage that lies `at` bytes behind the first
   auto copy = [&](auto i, uint32_t at) {
-    if constexpr (i.value == 0) copy_to(row_to + at);
-    if constexpr (i.value == kRowLoads) copy_to(feat_to + at);
+    if constexpr (i.value < kRowLoads && i.value % 4 == 0) copy_to(row_to + at + i.value * 1024);
+    if constexpr (i.value >= kRowLoads && (i.value - kRowLoads) % 4 == 0)
+      copy_to(feat_to + at + (i.value - kRowLoads) * 1024);
     if constexpr (i.value < kRowLoads)
       rl.template copy<i.value>();
     else
@@ -468,7 +467,7 @@ __global__ __launch_bounds__(WR *WF * 64, PER_CU *WR *WF / 4) void product_kerne
   const int steps = (K + kStep - 1) / kStep;
   if (steps > 0) {
 #pragma unroll
-    for (int s = 0; s < STAGES; ++s) {
+    for (int s = 0; s < 2; ++s) {
       rl.begin(s * kStep, K);
       fl.begin(s * kStep, K);
       each<kLoads>([&](auto i) { copy(i, s * kBytes); });
@@ -476,61 +475,57 @@ __global__ __launch_bounds__(WR *WF * 64, PER_CU *WR *WF / 4) void product_kerne
       fl.end();
     }
     i16x8 fo[2][FF], ro[2][FR];
-    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((STAGES - 1) * kLoads) : "memory");
-    each<FF>([&](auto a) {
-      each<fread.kReads>([&](auto h) { fread.template read<a.value, h.value>(smem + BR * kStep * 2, fo[0][a.value]); });
-    });
-    each<FR>([&](auto b) {
-      each<rread.kReads>([&](auto h) { rread.template read<b.value, h.value>(smem, ro[0][b.value]); });
-    });
-    int slot = 0;
-    // One stage: FF * FR matrix instructions with the copies and reads spread evenly between them.
-    auto stage = [&](int s, auto now) {
-      constexpr int c = now.value, n = 1 - c;
-      constexpr int kReads = FF * fread.kReads + FR * rread.kReads, kOps = kLoads + kReads, kMfma = FF * FR;
-      // stage s + 1 has landed for every wave, and every wave has read stage s
-      __builtin_amdgcn_sched_barrier(0);
-      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((STAGES - 2) * kLoads) : "memory");
-      __builtin_amdgcn_sched_barrier(0);
-      const uint32_t old = slot * kBytes;
-      slot = slot + 1 == STAGES ? 0 : slot + 1;
-      const char *rows = smem + slot * kBytes, *feats = rows + BR * kStep * 2;
-      rl.begin((s + STAGES) * kStep, K);
-      fl.begin((s + STAGES) * kStep, K);
-      if ((s + 1) * kStep > K) {  // the sum ends in this stage: entries behind its end count for nothing in either operand
-        const int have = K - s * kStep - g * 8;
-        each<FF>([&](auto a) { mask(fo[c][a.value], have); });
-        each<FR>([&](auto b) { mask(ro[c][b.value], have); });
+    constexpr int kFeatReads = FF * fread.kReads, kReads = kFeatReads + FR * rread.kReads, kMfma = FF * FR;
+    // read number r of half h of the stage at `lds`
+    auto read = [&](auto r, auto h, const char *lds) {
+      if constexpr (r.value < kFeatReads) {
+        constexpr int x = r.value / fread.kReads;
+        fread.template read<x, h.value, r.value % fread.kReads>(lds + BR * kStep * 2, fo[h.value][x]);
+      } else {
+        constexpr int x = (r.value - kFeatReads) / rread.kReads;
+        rread.template read<x, h.value, (r.value - kFeatReads) % rread.kReads>(lds, ro[h.value][x]);
       }
-      each<kMfma>([&](auto mc) {
-        constexpr int m = mc.value, a = m / FR, b = m % FR;
-        mfma<T>(fo[c][a], ro[c][b], acc[a][b]);
-        // operations o0 .. o1 - 1 of the stage follow this instruction: reads first, one copy in every kOps / kLoads
-        constexpr int o0 = m * kOps / kMfma, o1 = (m + 1) * kOps / kMfma;
+    };
+    // The FF * FR instructions of half h, with the reads of the other half from `lds` and COPIES copies to `to` between them.
+    auto half = [&](auto h, const char *lds, auto n_copies, uint32_t to, int have) {
+      constexpr int kCopies = n_copies.value, kOps = kReads + kCopies;
+      if (have < 32) {  // the sum ends in this half: entries behind its end count for nothing in either operand
+        each<FF>([&](auto a) { mask(fo[h.value][a.value], have - g * 8); });
+        each<FR>([&](auto b) { mask(ro[h.value][b.value], have - g * 8); });
+      }
+      each<kMfma>([&](auto m) {
+        constexpr int a = m.value / FR, b = m.value % FR;
+        mfma<T>(fo[h.value][a], ro[h.value][b], acc[a][b]);
+        constexpr int o0 = m.value * kOps / kMfma, o1 = (m.value + 1) * kOps / kMfma;
         each<o1 - o0>([&](auto oc) {
-          constexpr int o = o0 + oc.value;
-          constexpr int copies = (o + 1) * kLoads / kOps;  // up to and with this operation
-          if constexpr (copies > o * kLoads / kOps) {
-            copy(std::integral_constant<int, copies - 1>{}, old);
-          } else {
-            constexpr int r = o - copies;  // a read
-            if constexpr (r < FF * fread.kReads) {
-              constexpr int x = r / fread.kReads, h = r % fread.kReads;
-              fread.template read<x, h>(feats, fo[n][x]);
-            } else {
-              constexpr int x = (r - FF * fread.kReads) / rread.kReads, h = (r - FF * fread.kReads) % rread.kReads;
-              rread.template read<x, h>(rows, ro[n][x]);
-            }
-          }
+          constexpr int o = o0 + oc.value, copies = (o + 1) * kCopies / kOps;  // up to and with this operation
+          if constexpr (copies > o * kCopies / kOps)
+            copy(std::integral_constant<int, copies - 1>{}, to);
+          else
+            read(std::integral_constant<int, o - copies>{}, std::integral_constant<int, 1 - h.value>{}, lds);
         });
         if constexpr (o1 > o0) __builtin_amdgcn_sched_barrier(0);
       });
+    };
+    const std::integral_constant<int, 0> zero;
+    const std::integral_constant<int, 1> one;
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(kLoads) : "memory");
+    each<kReads>([&](auto r) { read(r, zero, smem); });
+    uint32_t slot = 0;
+    for (int s = 0; s < steps; ++s) {
+      const int have = K - s * kStep;
+      __builtin_amdgcn_sched_barrier(0);
+      rl.begin((s + 2) * kStep, K);
+      fl.begin((s + 2) * kStep, K);
+      half(zero, smem + slot, zero, 0, have);
+      __builtin_amdgcn_sched_barrier(0);
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      __builtin_amdgcn_sched_barrier(0);
+      const uint32_t old = slot;
+      slot = kBytes - slot;
+      half(one, smem + slot, std::integral_constant<int, kLoads>{}, old, have - 32);
       rl.end();
       fl.end();
-    };
-    for (int s = 0; s < steps; s += 2) {  // an odd count ends with a stage that is masked whole
-      stage(s, std::integral_constant<int, 0>{});
-      stage(s + 1, std::integral_constant<int, 1>{});
       // a copy of a sum that the register allocator might place here reads it written
       asm volatile("s_nop 10");
       __builtin_amdgcn_sched_barrier(0);
@@ -760,18 +755,18 @@ void pad(const void *in, int64_t ld, int64_t rows, int cols, int halves, void *o
                                    static_cast<uint16_t *>(out), out_rows, out_cols, n);
 }
 
-template <typename T, int P, int BR, int BF, int WR, int WF, int STAGES, int PER_CU>
+template <typename T, int P, int BR, int BF, int WR, int WF, int PER_CU>
 hipError_t run_product(const Args &A, int64_t n_assign, hipStream_t st) {
   constexpr int kFeatTile = P == kUp ? BF / 2 : BF;
-  constexpr size_t lds = STAGES * (BR + BF) * kStep * 2;
+  constexpr size_t lds = 2 * (BR + BF) * kStep * 2;
   const int64_t nt = ((P == kUp ? A.F : A.n_feat) + kFeatTile - 1) / kFeatTile;
   int64_t grid;
   if (P == kGradW1 || P == kGradW2)
-    grid = nt * ((A.n_row + BR - 1) / BR) * A.experts;
+    grid = (nt * ((A.n_row + BR - 1) / BR) + 7) / 8 * 8 * A.experts;
   else
     grid = nt * (n_assign / BR + std::min<int64_t>(A.experts, n_assign));
   if (grid > 0x7FFFFFFF) return hipErrorInvalidValue;
-  auto *kernel = product_kernel<T, P, BR, BF, WR, WF, STAGES, PER_CU>;
+  auto *kernel = product_kernel<T, P, BR, BF, WR, WF, PER_CU>;
   if (lds > 65536) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
                                              hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
@@ -785,8 +780,8 @@ bool large_tiles(int64_t n_assign, int experts) { return n_assign / experts >= 1
 
 template <typename T, int P>
 hipError_t product(const Args &A, int64_t n_assign, hipStream_t st) {
-  if (large_tiles(n_assign, A.experts)) return run_product<T, P, 256, 256, 2, 2, 4, 1>(A, n_assign, st);
-  return run_product<T, P, 128, 128, 2, 2, 4, 2>(A, n_assign, st);
+  if (large_tiles(n_assign, A.experts)) return run_product<T, P, 256, 256, 2, 2, 1>(A, n_assign, st);
+  return run_product<T, P, 128, 128, 2, 2, 2>(A, n_assign, st);
 }
 
 Args base_args(const cfp_experts_desc &d) {
