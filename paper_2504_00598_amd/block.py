@@ -16,9 +16,9 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import os
-from dataclasses import dataclass
+import struct
 
-from ._lib import CFP_OK, CfpError, _stream
+from ._lib import CFP_OK, CfpError
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libcfp_block.so")
@@ -58,6 +58,12 @@ class cfp_experts_desc(ctypes.Structure):
                 ("slot", _P)]
 
 
+# The same layouts for struct.pack: filling a ctypes structure of 21 fields takes 3 us, packing it 0.6 (a small
+# launch takes 3).  A packed descriptor is passed by the address of its bytes.
+_CODES = {_I64: "q", _I32: "i", _F32: "f", _P: "P"}
+_QK, _ROUTE, _PLAN, _EXPERTS = (struct.Struct("@" + "".join(_CODES[t] for _, t in c._fields_)).pack
+                                for c in (cfp_qk_desc, cfp_route_desc, cfp_plan_desc, cfp_experts_desc))
+
 _lib = None
 
 
@@ -68,17 +74,16 @@ def lib() -> ctypes.CDLL:
         if not os.path.exists(LIB_PATH):
             raise OSError(f"{LIB_PATH} is missing: build it with `python -m paper_2504_00598_amd.build`")
         L = ctypes.CDLL(LIB_PATH)
-        Q, R, N, X = (ctypes.POINTER(t) for t in (cfp_qk_desc, cfp_route_desc, cfp_plan_desc, cfp_experts_desc))
         SZ = ctypes.c_size_t
-        for name, args in (("cfp_qk_workspace_bytes", [Q]), ("cfp_expert_plan_workspace_bytes", [N]),
-                           ("cfp_experts_kept_bytes", [X]), ("cfp_experts_workspace_bytes", [X, _I32])):
+        for name, args in (("cfp_qk_workspace_bytes", [_P]), ("cfp_expert_plan_workspace_bytes", [_P]),
+                           ("cfp_experts_kept_bytes", [_P]), ("cfp_experts_workspace_bytes", [_P, _I32])):
             getattr(L, name).argtypes, getattr(L, name).restype = args, SZ
-        for name, args in (("cfp_qk_norm_rope", [Q, _P, _P, _P]),
-                           ("cfp_qk_norm_rope_bwd", [Q, _P, _I64, _I64, _P, _I64, _I64, _P, _P, _P, _P, _P, SZ, _P]),
-                           ("cfp_route", [R, _P, _P, _P]), ("cfp_route_bwd", [R, _P, _P, _P, _P]),
-                           ("cfp_expert_plan", [N, _P, _P, _P, _P, SZ, _P]),
-                           ("cfp_experts", [X, _P, _P, _P, SZ, _P]),
-                           ("cfp_experts_bwd", [X, _P, _I64, _P, _P, _P, _P, _P, _P, SZ, _P])):
+        for name, args in (("cfp_qk_norm_rope", [_P, _P, _P, _P]),
+                           ("cfp_qk_norm_rope_bwd", [_P, _P, _I64, _I64, _P, _I64, _I64, _P, _P, _P, _P, _P, SZ, _P]),
+                           ("cfp_route", [_P, _P, _P, _P]), ("cfp_route_bwd", [_P, _P, _P, _P, _P]),
+                           ("cfp_expert_plan", [_P, _P, _P, _P, _P, SZ, _P]),
+                           ("cfp_experts", [_P, _P, _P, _P, SZ, _P]),
+                           ("cfp_experts_bwd", [_P, _P, _I64, _P, _P, _P, _P, _P, _P, SZ, _P])):
             getattr(L, name).argtypes, getattr(L, name).restype = args, ctypes.c_int
         _lib = L
     return _lib
@@ -94,6 +99,7 @@ def _torch():
 
     if not _DT:
         _DT.update({torch.float32: CFP_DT_F32, torch.float16: CFP_DT_F16, torch.bfloat16: CFP_DT_BF16})
+        lib()
     return torch
 
 
@@ -109,7 +115,6 @@ def _tensor(name, t, torch, dtypes=None, dim=None):
         raise TypeError(f"{name}: type {t.dtype} is not supported")
     if dim is not None and t.dim() != dim:
         raise ValueError(f"{name} must have {dim} dimensions")
-    return t
 
 
 def _same_device(first, *others):
@@ -118,13 +123,21 @@ def _same_device(first, *others):
             raise ValueError("all tensors must be on one device")
 
 
+_HERE = contextlib.nullcontext()
+
+
 def _on(torch, device, stream):
-    """Context whose allocations and current stream are the call's; none where both are current."""
+    """Context whose current device and stream, and so whose allocations, are the call's."""
     if stream is None:
-        return contextlib.nullcontext() if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+        return _HERE if device.index == torch._C._cuda_getDevice() else torch.cuda.device(device)
     if stream.device != device:
         raise ValueError("the stream is of another device than the tensors")
     return torch.cuda.stream(stream)
+
+
+def _raw(torch, device):
+    """The current stream's handle, inside _on."""
+    return torch._C._cuda_getCurrentRawStream(device.index)
 
 
 def _rows(name, t):
@@ -136,24 +149,29 @@ def _rows(name, t):
 
 def _ws(torch, nbytes, device, ws):
     if ws is None:
-        return torch.empty(max(int(nbytes), 1), dtype=torch.uint8, device=device)
+        return torch.empty(max(nbytes, 1), dtype=torch.uint8, device=device)
     if ws.dtype != torch.uint8 or not ws.is_contiguous() or ws.device != device:
         raise TypeError("ws must be a contiguous uint8 tensor on the tensors' device")
     return ws
 
 
+def _like(torch, t):
+    return torch.empty_like(t, memory_format=torch.contiguous_format)
+
+
+def _ptr(t):
+    return 0 if t is None else t.data_ptr()
+
+
 # -------------------------------------------------------- queries and keys --
 
-def _heads(name, t, torch):
-    _tensor(name, t, torch, dim=3)
-    if t.shape[2] > 1 and t.stride(2) != 1:
-        raise ValueError(f"{name}: the last dimension must be contiguous")
-    return t.stride(0), t.stride(1)
-
-
-def _qk_desc(q, k, wq, wk, cos, sin, positions, eps, interleaved, torch):
-    (qt, qh), (kt, kh) = _heads("q", q, torch), _heads("k", k, torch)
-    T, hq, D = q.shape
+def _qk_refuse(q, k, wq, wk, cos, sin, positions, torch):
+    """Raises what is wrong with the arguments."""
+    for name, t in (("q", q), ("k", k)):
+        _tensor(name, t, torch, dim=3)
+        if t.shape[2] > 1 and t.stride(2) != 1:
+            raise ValueError(f"{name}: the last dimension must be contiguous")
+    T, _, D = q.shape
     if k.shape[0] != T or k.shape[2] != D or k.dtype != q.dtype:
         raise ValueError("q is [T][heads][D] and k is [T][key heads][D], of one type")
     for name, w in (("wq", wq), ("wk", wk)):
@@ -174,12 +192,34 @@ def _qk_desc(q, k, wq, wk, cos, sin, positions, eps, interleaved, torch):
     elif cos.shape[1] and T > cos.shape[0]:
         raise ValueError("without positions the tables must hold a row for every token")
     _same_device(q, k, wq, wk, cos, sin, positions)
-    w = wq if wq is not None else wk
-    return cfp_qk_desc(T, hq, k.shape[1], D, 2 * cos.shape[1], int(bool(interleaved)), _DT[q.dtype],
-                       _DT[w.dtype] if w is not None else CFP_DT_F32, float(eps), cos.shape[0], q.data_ptr(),
-                       k.data_ptr(), qt, qh, kt, kh, wq.data_ptr() if wq is not None else None,
-                       wk.data_ptr() if wk is not None else None, cos.data_ptr(), sin.data_ptr(),
-                       positions.data_ptr() if positions is not None else None)
+
+
+def _qk_desc(q, k, wq, wk, cos, sin, positions, eps, interleaved, torch):
+    # one pass over what has to hold, on the way of every call; what does not hold is said by _qk_refuse
+    try:
+        at, half = q.get_device(), cos.shape[1]
+        (T, hq, D), (qt, qh, qd), (kt, kh, kd) = q.shape, q.stride(), k.stride()
+        ok = (at >= 0 and k.shape[0] == T and k.shape[2] == D and k.dtype is q.dtype and k.get_device() == at and
+              (D == 1 or (qd == 1 and kd == 1)) and cos.dtype is torch.float32 and sin.dtype is torch.float32 and
+              cos.is_contiguous() and sin.is_contiguous() and sin.shape == cos.shape and cos.get_device() == at and
+              sin.get_device() == at)
+        for w in (wq, wk):
+            ok = ok and (w is None or (w.numel() == D and w.dim() == 1 and w.get_device() == at and w.is_contiguous()))
+        ok = ok and (wq is None or wk is None or wq.dtype is wk.dtype)
+        if positions is None:
+            ok = ok and (T <= cos.shape[0] or half == 0)
+        else:
+            ok = ok and (positions.dtype is torch.int32 and positions.numel() == T and positions.dim() == 1 and
+                         positions.get_device() == at and positions.is_contiguous())
+        w = wq if wq is not None else wk
+        types = _DT[q.dtype], CFP_DT_F32 if w is None else _DT[w.dtype]
+    except (AttributeError, KeyError, IndexError, TypeError, ValueError):
+        ok = False
+    if not ok:
+        _qk_refuse(q, k, wq, wk, cos, sin, positions, torch)
+        raise ValueError("unsupported arguments")
+    return _QK(T, hq, k.shape[1], D, 2 * half, 1 if interleaved else 0, *types, eps, cos.shape[0], q.data_ptr(),
+               k.data_ptr(), qt, qh, kt, kh, _ptr(wq), _ptr(wk), cos.data_ptr(), sin.data_ptr(), _ptr(positions))
 
 
 def qk_norm_rope(q, k, wq, wk, cos, sin, positions=None, *, eps=1e-6, interleaved=False, stream=None):
@@ -194,8 +234,10 @@ def qk_norm_rope(q, k, wq, wk, cos, sin, positions=None, *, eps=1e-6, interleave
     torch = _torch()
     d = _qk_desc(q, k, wq, wk, cos, sin, positions, eps, interleaved, torch)
     with _on(torch, q.device, stream):
-        yq, yk = torch.empty(q.shape, dtype=q.dtype, device=q.device), torch.empty(k.shape, dtype=q.dtype, device=q.device)
-        _check("cfp_qk_norm_rope", lib().cfp_qk_norm_rope(ctypes.byref(d), yq.data_ptr(), yk.data_ptr(), _stream(stream)))
+        yq, yk = _like(torch, q), _like(torch, k)
+        rc = _lib.cfp_qk_norm_rope(d, yq.data_ptr(), yk.data_ptr(), _raw(torch, q.device))
+    if rc:
+        _check("cfp_qk_norm_rope", rc)
     return yq, yk
 
 
@@ -205,38 +247,39 @@ def qk_norm_rope_bwd(dyq, dyk, q, k, wq, wk, cos, sin, positions=None, *, eps=1e
     as they were given to it).  Returns (dq, dk, dwq, dwk); dwq and dwk are float32, None for a gain of None."""
     torch = _torch()
     d = _qk_desc(q, k, wq, wk, cos, sin, positions, eps, interleaved, torch)
-    (qt, qh), (kt, kh) = _heads("dyq", dyq, torch), _heads("dyk", dyk, torch)
-    if dyq.shape != q.shape or dyk.shape != k.shape or dyq.dtype != q.dtype or dyk.dtype != q.dtype:
-        raise ValueError("dyq and dyk must have the shapes and the type of q and k")
+    for name, t, of in (("dyq", dyq, q), ("dyk", dyk, k)):
+        _tensor(name, t, torch, (q.dtype,), 3)
+        if t.shape != of.shape or (t.shape[2] > 1 and t.stride(2) != 1):
+            raise ValueError(f"{name} must have the shape of its input, the last dimension contiguous")
     _same_device(q, dyq, dyk)
     with _on(torch, q.device, stream):
-        dq, dk = torch.empty(q.shape, dtype=q.dtype, device=q.device), torch.empty(k.shape, dtype=q.dtype, device=q.device)
+        dq, dk = _like(torch, q), _like(torch, k)
         dwq = torch.empty(q.shape[2], dtype=torch.float32, device=q.device) if wq is not None else None
         dwk = torch.empty(q.shape[2], dtype=torch.float32, device=q.device) if wk is not None else None
-        ws = _ws(torch, lib().cfp_qk_workspace_bytes(ctypes.byref(d)), q.device, ws)
-        _check("cfp_qk_norm_rope_bwd", lib().cfp_qk_norm_rope_bwd(
-            ctypes.byref(d), dyq.data_ptr(), qt, qh, dyk.data_ptr(), kt, kh, dq.data_ptr(), dk.data_ptr(),
-            dwq.data_ptr() if dwq is not None else None, dwk.data_ptr() if dwk is not None else None, ws.data_ptr(),
-            ws.numel(), _stream(stream)))
+        ws = _ws(torch, _lib.cfp_qk_workspace_bytes(d), q.device, ws)
+        _check("cfp_qk_norm_rope_bwd", _lib.cfp_qk_norm_rope_bwd(
+            d, dyq.data_ptr(), dyq.stride(0), dyq.stride(1), dyk.data_ptr(), dyk.stride(0), dyk.stride(1),
+            dq.data_ptr(), dk.data_ptr(), _ptr(dwq), _ptr(dwk), ws.data_ptr(), ws.numel(), _raw(torch, q.device)))
     return dq, dk, dwq, dwk
 
 
 # ----------------------------------------------------------------- routing --
 
 def _route_desc(logits, k, score, bias, groups, top_groups, group_score, renormalise, scale, torch):
-    _tensor("logits", logits, torch, dim=2)
+    if not (isinstance(logits, torch.Tensor) and logits.is_cuda and logits.dtype in _DT and logits.dim() == 2):
+        _tensor("logits", logits, torch, dim=2)
     if score not in SCORES:
         raise ValueError(f"score must be one of {sorted(SCORES)}")
     if group_score not in GROUP_SCORES:
         raise ValueError(f"group_score must be one of {sorted(GROUP_SCORES)}")
+    T, E = logits.shape
     if bias is not None:
         _tensor("bias", bias, torch, (torch.float32,), 1)
-        if bias.shape[0] != logits.shape[1] or not bias.is_contiguous():
+        if bias.shape[0] != E or not bias.is_contiguous():
             raise ValueError("bias must be contiguous [experts]")
         _same_device(logits, bias)
-    return cfp_route_desc(logits.shape[0], logits.shape[1], int(k), SCORES[score], int(groups), int(top_groups),
-                          GROUP_SCORES[group_score], int(bool(renormalise)), _DT[logits.dtype], float(scale),
-                          logits.data_ptr(), _rows("logits", logits), bias.data_ptr() if bias is not None else None)
+    return _ROUTE(T, E, k, SCORES[score], groups, top_groups, GROUP_SCORES[group_score], 1 if renormalise else 0,
+                  _DT[logits.dtype], scale, logits.data_ptr(), _rows("logits", logits), _ptr(bias))
 
 
 def route(logits, k, *, score="softmax", bias=None, groups=1, top_groups=1, group_score="max", renormalise=False,
@@ -252,44 +295,65 @@ def route(logits, k, *, score="softmax", bias=None, groups=1, top_groups=1, grou
     a place with no expert left has index -1 and weight 0."""
     torch = _torch()
     d = _route_desc(logits, k, score, bias, groups, top_groups, group_score, renormalise, scale, torch)
-    with _on(torch, logits.device, stream):
-        weight = torch.empty((logits.shape[0], int(k)), dtype=torch.float32, device=logits.device)
-        index = torch.empty((logits.shape[0], int(k)), dtype=torch.int32, device=logits.device)
-        _check("cfp_route", lib().cfp_route(ctypes.byref(d), weight.data_ptr(), index.data_ptr(), _stream(stream)))
+    device = logits.device
+    with _on(torch, device, stream):
+        weight = torch.empty((logits.shape[0], k), dtype=torch.float32, device=device)
+        index = torch.empty((logits.shape[0], k), dtype=torch.int32, device=device)
+        rc = _lib.cfp_route(d, weight.data_ptr(), index.data_ptr(), _raw(torch, device))
+    if rc:
+        _check("cfp_route", rc)
     return weight, index
 
 
 def route_bwd(dweight, logits, index, *, score="softmax", renormalise=False, scale=1.0, stream=None):
     """Gradient of route's weights in the logits [T][experts], from dweight [T][k] float32 and the index it returned."""
     torch = _torch()
-    k = index.shape[1] if index.dim() == 2 else 0
-    d = _route_desc(logits, k, score, None, 1, 1, "max", renormalise, scale, torch)
     _tensor("index", index, torch, (torch.int32,), 2)
     _tensor("dweight", dweight, torch, (torch.float32,), 2)
-    if tuple(index.shape) != (logits.shape[0], k) or index.shape != dweight.shape:
+    d = _route_desc(logits, index.shape[1], score, None, 1, 1, "max", renormalise, scale, torch)
+    if index.shape[0] != logits.shape[0] or index.shape != dweight.shape:
         raise ValueError("index and dweight are [T][k]")
     _same_device(logits, index, dweight)
     with _on(torch, logits.device, stream):
         index, dweight = index.contiguous(), dweight.contiguous()
-        dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
-        _check("cfp_route_bwd", lib().cfp_route_bwd(ctypes.byref(d), index.data_ptr(), dweight.data_ptr(),
-                                                    dlogits.data_ptr(), _stream(stream)))
+        dlogits = _like(torch, logits)
+        _check("cfp_route_bwd", _lib.cfp_route_bwd(d, index.data_ptr(), dweight.data_ptr(), dlogits.data_ptr(),
+                                                   _raw(torch, logits.device)))
     return dlogits
 
 
 # ----------------------------------------------------------------- experts --
 
-@dataclass
 class ExpertPlan:
-    """Order of the assignments a = token * k + place by expert."""
+    """Order of the assignments a = token * k + place by expert.
 
-    offsets: object   # [experts + 1] int32: the positions of each expert
-    rows: object      # [T * k] int32: the assignment at each position, -1 behind the last one kept
-    slot: object      # [T * k] int32: the position of each assignment, -1 where it is dropped
-    n_tokens: int
-    k: int
-    n_experts: int
-    first: int
+    offsets [experts + 1] int32: the positions of each expert; rows [T * k] int32: the assignment at
+    each position, -1 behind the last one kept; slot [T * k] int32: the position of each
+    assignment, -1 where it is dropped."""
+
+    __slots__ = ("_buf", "n_tokens", "k", "n_experts", "first")
+
+    def __init__(self, buf, n_tokens, k, n_experts, first):
+        self._buf, self.n_tokens, self.k, self.n_experts, self.first = buf, n_tokens, k, n_experts, first
+
+    # places in the buffer: offsets, rows and CFP_PLAN_PAD entries, slot
+    @property
+    def offsets(self):
+        return self._buf[:self.n_experts + 1]
+
+    @property
+    def rows(self):
+        return self._buf[self.n_experts + 1:self.n_experts + 1 + self.n_tokens * self.k]
+
+    @property
+    def slot(self):
+        at = self.n_experts + 1 + self.n_tokens * self.k + CFP_PLAN_PAD
+        return self._buf[at:at + self.n_tokens * self.k]
+
+    def _pointers(self):
+        at, n = self._buf.data_ptr(), self.n_tokens * self.k
+        rows = at + 4 * (self.n_experts + 1)
+        return at, rows, rows + 4 * (n + CFP_PLAN_PAD)
 
 
 def expert_plan(index, n_experts, *, first=0, stream=None) -> ExpertPlan:
@@ -298,17 +362,17 @@ def expert_plan(index, n_experts, *, first=0, stream=None) -> ExpertPlan:
     torch = _torch()
     _tensor("index", index, torch, (torch.int32,), 2)
     T, k = index.shape
-    with _on(torch, index.device, stream):
+    device = index.device
+    with _on(torch, device, stream):
         index = index.contiguous()
-        d = cfp_plan_desc(T, k, int(n_experts), int(first), index.data_ptr())
-        n, e = T * k, int(n_experts)
-        need = int(lib().cfp_expert_plan_workspace_bytes(ctypes.byref(d)))
-        r, s = max(e, 0) + 1, max(e, 0) + 1 + n + CFP_PLAN_PAD  # where rows and slot begin
-        buf = torch.empty(s + n + need // 4, dtype=torch.int32, device=index.device)
-        plan = ExpertPlan(buf[:r], buf[r:r + n], buf[s:s + n], T, k, e, int(first))
-        at = buf.data_ptr()
-        _check("cfp_expert_plan", lib().cfp_expert_plan(
-            ctypes.byref(d), at, at + 4 * r, at + 4 * s, at + 4 * (s + n), need, _stream(stream)))
+        d = _PLAN(T, k, n_experts, first, index.data_ptr())
+        need = _lib.cfp_expert_plan_workspace_bytes(d)
+        size = max(n_experts, 0) + 1 + 2 * T * k + CFP_PLAN_PAD
+        plan = ExpertPlan(torch.empty(size + need // 4, dtype=torch.int32, device=device), T, k, n_experts, first)
+        offsets, rows, slot = plan._pointers()
+        rc = _lib.cfp_expert_plan(d, offsets, rows, slot, offsets + 4 * size, need, _raw(torch, device))
+    if rc:
+        _check("cfp_expert_plan", rc)
     return plan
 
 
@@ -319,18 +383,18 @@ def _experts_desc(x, w1, w2, weight, plan, torch):
     _tensor("w2", w2, torch, half, 3)
     _tensor("weight", weight, torch, (torch.float32,), 2)
     T, H = x.shape
-    E, F = w2.shape[0], w2.shape[2]
-    if tuple(w1.shape) != (E, 2 * F, H) or w2.shape[1] != H:
+    E, _, F = w2.shape
+    if w1.shape != (E, 2 * F, H) or w2.shape[1] != H:
         raise ValueError("w1 is [experts][2 * inner][hidden] and w2 is [experts][hidden][inner]")
     if w1.dtype != x.dtype or w2.dtype != x.dtype:
         raise TypeError("x, w1 and w2 must be of one type")
     if not (w1.is_contiguous() and w2.is_contiguous() and weight.is_contiguous()):
         raise ValueError("w1, w2 and weight must be contiguous")
-    if not isinstance(plan, ExpertPlan) or (plan.n_tokens, plan.n_experts) != (T, E) or tuple(weight.shape) != (T, plan.k):
+    if not isinstance(plan, ExpertPlan) or (plan.n_tokens, plan.n_experts) != (T, E) or weight.shape != (T, plan.k):
         raise ValueError("the plan is of another number of tokens, experts or places than x, w1 and weight")
-    _same_device(x, w1, w2, weight, plan.offsets)
-    return cfp_experts_desc(T, plan.k, E, H, F, _DT[x.dtype], x.data_ptr(), _rows("x", x), w1.data_ptr(), w2.data_ptr(),
-                            weight.data_ptr(), plan.offsets.data_ptr(), plan.rows.data_ptr(), plan.slot.data_ptr())
+    _same_device(x, w1, w2, weight, plan._buf)
+    return _EXPERTS(T, plan.k, E, H, F, _DT[x.dtype], x.data_ptr(), _rows("x", x), w1.data_ptr(), w2.data_ptr(),
+                    weight.data_ptr(), *plan._pointers())
 
 
 def experts(x, w1, w2, weight, plan, *, keep=False, ws=None, stream=None):
@@ -342,13 +406,13 @@ def experts(x, w1, w2, weight, plan, *, keep=False, ws=None, stream=None):
     without assignments gets zeros.  With `keep` returns (y, kept): kept is what experts_bwd needs."""
     torch = _torch()
     d = _experts_desc(x, w1, w2, weight, plan, torch)
-    ref = ctypes.byref(d)
     with _on(torch, x.device, stream):
-        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        ws = _ws(torch, lib().cfp_experts_workspace_bytes(ref, 0), x.device, ws)
-        kept = _ws(torch, lib().cfp_experts_kept_bytes(ref), x.device, None) if keep else None
-        _check("cfp_experts", lib().cfp_experts(ref, y.data_ptr(), kept.data_ptr() if keep else None, ws.data_ptr(),
-                                                ws.numel(), _stream(stream)))
+        y = _like(torch, x)
+        ws = _ws(torch, _lib.cfp_experts_workspace_bytes(d, 0), x.device, ws)
+        kept = _ws(torch, _lib.cfp_experts_kept_bytes(d), x.device, None) if keep else None
+        rc = _lib.cfp_experts(d, y.data_ptr(), _ptr(kept), ws.data_ptr(), ws.numel(), _raw(torch, x.device))
+    if rc:
+        _check("cfp_experts", rc)
     return (y, kept) if keep else y
 
 
@@ -357,18 +421,17 @@ def experts_bwd(dy, x, w1, w2, weight, plan, kept, *, ws=None, stream=None):
     An expert without assignments gets zeros, and a dropped assignment's weight 0."""
     torch = _torch()
     d = _experts_desc(x, w1, w2, weight, plan, torch)
-    ref = ctypes.byref(d)
     _tensor("dy", dy, torch, (x.dtype,), 2)
     if dy.shape != x.shape:
         raise ValueError("dy must have the shape of x")
     _same_device(x, dy, kept)
-    if kept.dtype != torch.uint8 or kept.numel() < lib().cfp_experts_kept_bytes(ref) or not kept.is_contiguous():
+    if kept.dtype != torch.uint8 or kept.numel() < _lib.cfp_experts_kept_bytes(d) or not kept.is_contiguous():
         raise ValueError("kept is not what experts returned for these sizes")
     with _on(torch, x.device, stream):
-        dx, dw1, dw2 = torch.empty(x.shape, dtype=x.dtype, device=x.device), torch.empty_like(w1), torch.empty_like(w2)
+        dx, dw1, dw2 = _like(torch, x), torch.empty_like(w1), torch.empty_like(w2)
         dweight = torch.empty_like(weight)
-        ws = _ws(torch, lib().cfp_experts_workspace_bytes(ref, 1), x.device, ws)
-        _check("cfp_experts_bwd", lib().cfp_experts_bwd(
-            ref, dy.data_ptr(), _rows("dy", dy), kept.data_ptr(), dx.data_ptr(), dw1.data_ptr(), dw2.data_ptr(),
-            dweight.data_ptr(), ws.data_ptr(), ws.numel(), _stream(stream)))
+        ws = _ws(torch, _lib.cfp_experts_workspace_bytes(d, 1), x.device, ws)
+        _check("cfp_experts_bwd", _lib.cfp_experts_bwd(
+            d, dy.data_ptr(), _rows("dy", dy), kept.data_ptr(), dx.data_ptr(), dw1.data_ptr(), dw2.data_ptr(),
+            dweight.data_ptr(), ws.data_ptr(), ws.numel(), _raw(torch, x.device)))
     return dx, dw1, dw2, dweight

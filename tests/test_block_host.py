@@ -23,6 +23,14 @@ def test_header_binding_and_exports_agree():
     assert {ln.split()[-1] for ln in out.splitlines() if " T " in ln} == set(B.EXPORTED)
 
 
+def test_packed_descriptors_have_the_structures_layout():
+    for pack, c in ((B._QK, B.cfp_qk_desc), (B._ROUTE, B.cfp_route_desc), (B._PLAN, B.cfp_plan_desc),
+                    (B._EXPERTS, B.cfp_experts_desc)):
+        values = [i + 1 for i, _ in enumerate(c._fields_)]
+        got = c.from_buffer_copy(pack(*values).ljust(ctypes.sizeof(c), b"\0"))
+        assert [getattr(got, f) for f, _ in c._fields_] == values
+
+
 def qk(**kw):
     d = dict(n_tokens=4, n_q=2, n_k=1, dim=8, rot=8, interleaved=0, dtype=2, wdtype=2, eps=1e-6, n_pos=16, q=P, k=P,
              q_token_stride=24, q_head_stride=8, k_token_stride=24, k_head_stride=8, wq=P, wk=P, cos=P, sin=P, pos=P)
