@@ -668,6 +668,138 @@ __global__ __launch_bounds__(WR *WF * 64, PER_CU *WR *WF / 4) void product_kerne
   }
 }
 
+// ------------------------------------------------------------- few tokens --
+//
+// Where an expert has a few tokens the products are bound by reading its weights once.  A workgroup takes
+// 32 rows of them (16 gate rows and their 16 up rows, or 32 rows of W2) for 16 NT tokens, and its four
+// waves a quarter of the sum's axis each: the weights go from memory to the registers that the
+// matrix instructions take them from, kAhead steps of 2 KiB a wave ahead, and only the four partial
+// sums meet in LDS.  Rows need no alignment (a piece of 8 entries is one load of 16 bytes at any
+// address), so odd widths are read in place.
+
+constexpr int kFewWaves = 4;
+
+// Entries k .. k + 7 of a row of K, zeros behind its end.
+__device__ __forceinline__ i16x8 piece(const char *row, int k, int K) {
+  i16x8 v = {};
+  if (k + 8 <= K) {
+    __builtin_memcpy(&v, row + (int64_t)k * 2, 16);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (k + i < K) v[i] = reinterpret_cast<const short *>(row)[k + i];
+  }
+  return v;
+}
+
+template <typename T>
+__device__ __forceinline__ f32x4 mfma_v(i16x8 a, i16x8 b, f32x4 c) {  // with waits by the compiler
+  if constexpr (std::is_same<T, bf16_t>::value)
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+
+template <typename T, int P, int NT>
+__global__ __launch_bounds__(kFewWaves * 64) void few_kernel(Args A) {
+  constexpr int kAhead = NT == 1 ? 8 : 4;
+  constexpr int kTile = P == kUp ? 16 : 32;  // features of a workgroup
+  __shared__ f32x4 part[kFewWaves][NT * 2][64];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
+  const int n_feat = P == kUp ? A.F : A.n_feat;
+  Place pl;
+  int ft;
+  if (!find<16 * NT>(A, (n_feat + kTile - 1) / kTile, pl, ft)) return;
+  const int r0 = pl.tile * 16 * NT, f0 = ft * kTile, K = A.K;
+  const char *base = A.feat + pl.expert * A.feat_expert;
+  // rows past the end repeat the last one and are not written
+  const char *w0 = base + (int64_t)min(f0 + j, n_feat - 1) * A.ld_feat;
+  const char *w1 = P == kUp ? base + (int64_t)(min(f0 + j, n_feat - 1) + A.F) * A.ld_feat
+                            : base + (int64_t)min(f0 + 16 + j, n_feat - 1) * A.ld_feat;
+  const char *x[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    int64_t row = pl.first + min(r0 + t * 16 + j, pl.count - 1);
+    if constexpr (P == kUp) row = (uint64_t)(uint32_t)A.rows[row] * A.magic >> A.shift;
+    x[t] = A.row + row * A.ld_row;
+  }
+  const int steps = (K + 31) / 32, each = (steps + kFewWaves - 1) / kFewWaves;
+  const int from = wave * each, to = min(from + each, steps);
+  f32x4 acc[2][NT] = {};
+  auto run = [&](int s, auto whole) {
+    i16x8 a[2][kAhead], b[NT][kAhead];
+    auto load = [&](const char *row, int i) {
+      if constexpr (whole.value) {
+        i16x8 v;
+        __builtin_memcpy(&v, row + (int64_t)(s * 32 + g * 8) * 2 + i * 64, 16);
+        return v;
+      } else {
+        return piece(row, s + i < to ? (s + i) * 32 + g * 8 : K, K);  // past this wave's part: zeros
+      }
+    };
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      a[0][i] = load(w0, i);
+      a[1][i] = load(w1, i);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) b[t][i] = load(x[t], i);
+    }
+    __builtin_amdgcn_sched_barrier(0);  // every load is on its way before the first is waited for
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        acc[0][t] = mfma_v<T>(a[0][i], b[t][i], acc[0][t]);
+        acc[1][t] = mfma_v<T>(a[1][i], b[t][i], acc[1][t]);
+      }
+  };
+  int s = from;
+  for (; s + kAhead <= to && (s + kAhead) * 32 <= K; s += kAhead) run(s, std::true_type{});
+  for (; s < to; s += kAhead) run(s, std::false_type{});
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    part[wave][2 * t][lane] = acc[0][t];
+    part[wave][2 * t + 1][lane] = acc[1][t];
+  }
+  __syncthreads();
+  // lane (j, g) of the sum: features 4 g .. 4 g + 3 of token j
+  for (int t = wave; t < NT; t += kFewWaves) {
+    f32x4 v[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      v[h] = part[0][2 * t + h][lane];
+#pragma unroll
+      for (int w = 1; w < kFewWaves; ++w) v[h] += part[w][2 * t + h][lane];
+    }
+    const int i = r0 + t * 16 + j;
+    if (i >= pl.count) continue;
+    const int64_t at = pl.first + i;
+    if constexpr (P == kUp) {
+      const int f = f0 + g * 4;
+      if (f >= A.Fp) continue;
+      float s[4], ga[4], up[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const bool in = f + e < A.F;
+        ga[e] = in ? v[0][e] : 0.f;
+        up[e] = in ? v[1][e] : 0.f;
+        s[e] = ga[e] * sigmoid(ga[e]) * up[e];
+      }
+      store_vec<T, 4>(reinterpret_cast<T *>(A.out) + at * A.ld_out + f, s);
+      if (A.h != nullptr) {
+        store_vec<float, 4>(A.h + at * 2 * A.Fp + f, ga);
+        store_vec<float, 4>(A.h + at * 2 * A.Fp + A.Fp + f, up);
+      }
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int f = f0 + h * 16 + g * 4;
+        if (f < A.ld_out) *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(A.out) + at * A.ld_out + f) = v[h];
+      }
+    }
+  }
+}
+
 // ------------------------------------------------------ around the products --
 
 // y_t = sum over the token's assignments of w o (weight null: of o), and the gradient
@@ -702,15 +834,19 @@ __global__ __launch_bounds__(256) void combine_kernel(const float *o, int64_t ld
 }
 
 // Copy of [n][rows][cols] with both inner extents padded by zeros (16-bit elements).  `halves`: the rows
-// are two runs of rows / halves that are padded each.
-__global__ __launch_bounds__(256) void pad_kernel(const uint16_t *in, int64_t ld, int64_t rows, int cols, int halves,
-                                                  uint16_t *out, int64_t out_rows, int out_cols, int64_t n) {
-  const int64_t total = n * out_rows * out_cols;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-    const int c = (int)(i % out_cols);
-    const int64_t r = i / out_cols % out_rows, e = i / out_cols / out_rows;
-    const int64_t per = out_rows / halves, half = r / per, x = r - half * per, src = rows / halves;
-    out[i] = c < cols && x < src ? in[(e * rows + half * src + x) * ld + c] : (uint16_t)0;
+// are two runs of rows / halves that are padded each.  A workgroup copies one row of the copy at a time.
+__global__ __launch_bounds__(256) void pad_kernel(const uint16_t *in, int64_t ld, int rows, int cols, int halves,
+                                                  uint16_t *out, int out_rows, int out_cols, int64_t n) {
+  const int per = out_rows / halves, src = rows / halves;
+  for (int64_t r = blockIdx.x; r < n * out_rows; r += gridDim.x) {
+    const int64_t e = r / out_rows;
+    const int y = (int)(r - e * out_rows), half = y / per, x = y - half * per;
+    const uint16_t *from = in + (e * rows + half * src + min(x, src - 1)) * ld;
+    uint16_t *to = out + r * out_cols;
+    for (int c = threadIdx.x * 2; c < out_cols; c += 512) {  // out_cols is a multiple of 8
+      const uint32_t a = x < src && c < cols ? from[c] : 0, b = x < src && c + 1 < cols ? from[c + 1] : 0;
+      *reinterpret_cast<uint32_t *>(to + c) = a | b << 16;
+    }
   }
 }
 
@@ -762,10 +898,9 @@ bool pads_w2(const cfp_experts_desc &d) { return d.inner % 8 != 0 || !on16(d.w2)
 
 void pad(const void *in, int64_t ld, int64_t rows, int cols, int halves, void *out, int64_t out_rows, int out_cols,
          int64_t n, hipStream_t st) {
-  const int64_t total = n * out_rows * out_cols;
-  const unsigned grid = (unsigned)std::min<int64_t>((total + 255) / 256, 16384);
-  pad_kernel<<<grid, 256, 0, st>>>(static_cast<const uint16_t *>(in), ld, rows, cols, halves,
-                                   static_cast<uint16_t *>(out), out_rows, out_cols, n);
+  const unsigned grid = (unsigned)std::min<int64_t>(n * out_rows, 8192);
+  pad_kernel<<<grid, 256, 0, st>>>(static_cast<const uint16_t *>(in), ld, (int)rows, cols, halves,
+                                   static_cast<uint16_t *>(out), (int)out_rows, out_cols, n);
 }
 
 template <typename T, int P, int BR, int BF, int WR, int WF, int PER_CU>
@@ -794,6 +929,22 @@ hipError_t run_product(Args A, int64_t n_assign, hipStream_t st) {
   }
   kernel<<<(unsigned)grid, WR * WF * 64, lds, st>>>(A);
   return hipGetLastError();
+}
+
+// Few tokens an expert: the products are bound by the weights' bytes.
+bool few_tokens(int64_t n_assign, int experts) { return n_assign <= (int64_t)experts * 32 || n_assign <= 64; }
+
+template <typename T, int P>
+hipError_t few(const Args &A, int64_t n_assign, hipStream_t st) {
+  const auto go = [&](auto nt) {
+    constexpr int kTile = P == kUp ? 16 : 32;
+    const int64_t tiles = ((P == kUp ? A.F : A.n_feat) + kTile - 1) / kTile;
+    const int64_t grid = tiles * (n_assign / (16 * nt.value) + std::min<int64_t>(A.experts, n_assign));
+    if (grid > 0x7FFFFFFF) return hipErrorInvalidValue;
+    few_kernel<T, P, nt.value><<<(unsigned)grid, kFewWaves * 64, 0, st>>>(A);
+    return hipGetLastError();
+  };
+  return n_assign <= (int64_t)A.experts * 8 ? go(std::integral_constant<int, 1>{}) : go(std::integral_constant<int, 4>{});
 }
 
 bool large_tiles(int64_t n_assign, int experts) { return n_assign / experts >= 128; }
@@ -860,20 +1011,22 @@ Laid lay_out(const cfp_experts_desc &d, const void *dy, int64_t dy_stride, const
 
 template <typename T>
 hipError_t forward(const cfp_experts_desc &d, void *y, float *h, uint8_t *ws, hipStream_t st) {
-  const bool px = pads_x(d, d.x, d.x_stride), pw1 = pads_w1(d), pw2 = pads_w2(d);
+  const int64_t n = d.n_tokens * d.k;
+  const bool small = few_tokens(n, d.n_experts);  // reads rows of any alignment in place
+  const bool px = !small && pads_x(d, d.x, d.x_stride), pw1 = !small && pads_w1(d), pw2 = !small && pads_w2(d);
   const Region r = region(d, false, px, false, pw1, pw2);
   const Laid L = lay_out(d, nullptr, 0, r, px, false, pw1, pw2, ws, st);
-  const int64_t n = d.n_tokens * d.k;
+  const int64_t H = small ? d.hidden : L.Hp, F = small ? d.inner : L.Fp;  // widths of the weights' rows
   Args A = base_args(d);
-  A.row = L.x, A.ld_row = L.ld_x, A.feat = L.w1, A.ld_feat = L.Hp * 2, A.feat_expert = 2 * L.Fp * L.Hp * 2;
-  A.K = (int)L.Hp, A.n_feat = d.inner, A.out = ws + r.act, A.ld_out = L.Fp, A.h = h;
-  hipError_t e = product<T, kUp>(A, n, st);
+  A.row = L.x, A.ld_row = L.ld_x, A.feat = L.w1, A.ld_feat = H * 2, A.feat_expert = 2 * F * H * 2;
+  A.K = (int)H, A.n_feat = d.inner, A.out = ws + r.act, A.ld_out = L.Fp, A.h = h;
+  hipError_t e = small ? few<T, kUp>(A, n, st) : product<T, kUp>(A, n, st);
   if (e != hipSuccess) return e;
   A = base_args(d);
   A.row = reinterpret_cast<const char *>(ws + r.act), A.ld_row = L.Fp * 2;
-  A.feat = L.w2, A.ld_feat = L.Fp * 2, A.feat_expert = (int64_t)d.hidden * L.Fp * 2;
-  A.K = (int)L.Fp, A.n_feat = d.hidden, A.out = ws + r.out, A.ld_out = L.Hp;
-  if ((e = product<T, kDown>(A, n, st)) != hipSuccess) return e;
+  A.feat = L.w2, A.ld_feat = F * 2, A.feat_expert = (int64_t)d.hidden * F * 2;
+  A.K = (int)F, A.n_feat = d.hidden, A.out = ws + r.out, A.ld_out = L.Hp;
+  if ((e = small ? few<T, kDown>(A, n, st) : product<T, kDown>(A, n, st)) != hipSuccess) return e;
   return combine<T>(d, reinterpret_cast<const float *>(ws + r.out), d.weight, y, nullptr, 0, nullptr, st);
 }
 
@@ -925,8 +1078,8 @@ size_t experts_kept_bytes(const cfp_experts_desc &d) {
 
 size_t experts_bytes(const cfp_experts_desc &d, bool bwd) {
   // dy is checked only when it is given: room for its copy is taken with x's
-  const bool px = pads_x(d, d.x, d.x_stride);
-  return region(d, bwd, px || bwd, bwd, pads_w1(d), pads_w2(d)).total;
+  const bool small = !bwd && few_tokens(d.n_tokens * d.k, d.n_experts), px = !small && pads_x(d, d.x, d.x_stride);
+  return region(d, bwd, px || bwd, bwd, !small && pads_w1(d), !small && pads_w2(d)).total;
 }
 
 hipError_t launch_experts(const cfp_experts_desc &d, void *y, float *h, uint8_t *ws, hipStream_t st) {
