@@ -10,7 +10,9 @@
 // All six products run on the matrix units with 32-bit sums.  Rounded to 16 bits
 // between products: s, [dg du] and w s, which the next product takes as operands.
 // Kept in 32 bits: g and u for the backward pass (the gradients and dw are computed
-// from them) and the experts' outputs before the weighted sum over a token's experts.
+// from them).  The experts' outputs wait for the weighted sum over a token's experts
+// as 16-bit floats with one exponent for 32 of them: 11 bits, an eighth of a bfloat16's
+// rounding, at any magnitude, for half the bytes of 32-bit sums.
 // Nothing is added through memory in an order that could change: a token's rows are
 // gathered and summed by the token.
 #include <algorithm>
@@ -283,6 +285,13 @@ struct Reader {
 
 enum Product { kUp, kDown, kBackUp, kBackDown, kGradW1, kGradW2 };
 
+// 16-bit floats with an exponent for 32 of them (store_shared).
+struct Shared16 {
+  f16_t *out;       // [rows][ld]
+  uint8_t *exps;    // [rows][ld_exp]
+  int64_t ld, ld_exp;
+};
+
 struct Args {
   // operands: rows of the tile (assignments, or output rows of a weight gradient), and features
   const char *row, *feat;
@@ -296,11 +305,12 @@ struct Args {
   int32_t F, Fp;               // inner width, and as laid out
   int32_t deal_rows;           // weight gradients: blocks of row tiles that eight dies divide, 1, 2, 4 or 8
   // epilogues
-  void *out;                   // 16-bit or 32-bit rows
+  void *out;                   // 16-bit rows
   int64_t ld_out;              // elements
   float *h;                    // [A][2 Fp]
   const float *weight;         // [T * k]
   void *out2;                  // [A][Fp]: w s
+  Shared16 shared;             // kDown, kBackDown
   float *dot;                  // [A][dot_tiles]: s . p over a feature tile
   int32_t dot_tiles;
 };
@@ -363,6 +373,32 @@ __device__ __forceinline__ bool find(const Args &A, int nt, Place &p, int &ft) {
     before += __builtin_amdgcn_readfirstlane(__shfl(c, 63, 64));
   }
   return false;
+}
+
+// 32 features of a row, 8 of them in each of the four lanes of equal j (two runs of four, 16 apart), as 16-bit
+// floats under one exponent: the largest finite one, m, in [2^e, 2^(e + 1)), goes to [2^14, 2^15), and the
+// byte stored is e's in a float.  Entries that are not finite stay so.
+__device__ __forceinline__ void store_shared(const Shared16 &S, int64_t row, int f, int g, f32x4 a, f32x4 b) {
+  float m = 0.f;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float x = fabsf(a[e]), y = fabsf(b[e]);
+    m = fmaxf(m, x < INFINITY ? x : 0.f);
+    m = fmaxf(m, y < INFINITY ? y : 0.f);
+  }
+  m = fmaxf(m, __shfl_xor(m, 16, 64));
+  m = fmaxf(m, __shfl_xor(m, 32, 64));
+  const int e = (int)(__float_as_uint(m) >> 23), by = 141 - e;
+  vec<f16_t, 4> u, v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    u[i] = (f16_t)ldexpf(a[i], by);
+    v[i] = (f16_t)ldexpf(b[i], by);
+  }
+  f16_t *to = S.out + row * S.ld + f + g * 4;
+  if (f + g * 4 < S.ld) *reinterpret_cast<vec<f16_t, 4> *>(to) = u;
+  if (f + 16 + g * 4 < S.ld) *reinterpret_cast<vec<f16_t, 4> *>(to + 16) = v;
+  if (g == 0 && f < S.ld) S.exps[row * S.ld_exp + f / 32] = (uint8_t)e;
 }
 
 __device__ __forceinline__ float sigmoid(float x) { return 1.f / (1.f + __expf(-x)); }
@@ -578,12 +614,9 @@ __global__ __launch_bounds__(WR *WF * 64, PER_CU *WR *WF / 4) void product_kerne
     for (int b = 0; b < FR; ++b) {
       const int i = r0 + wr * TR + b * 16 + j;
       if (i >= n_rows) continue;
-      float *o = reinterpret_cast<float *>(A.out) + (int64_t)(pl.first + i) * A.ld_out;
 #pragma unroll
-      for (int q = 0; q < FF; ++q) {
-        const int f = f0 + wf * TF + q * 16 + g * 4;
-        if (f < A.ld_out) *reinterpret_cast<f32x4 *>(o + f) = acc[q][b];
-      }
+      for (int q = 0; q < FF; q += 2)
+        store_shared(A.shared, pl.first + i, f0 + wf * TF + q * 16, g, acc[q][b], acc[q + 1][b]);
     }
   } else if constexpr (P == kBackUp) {
     float dots[FR];
@@ -791,11 +824,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(Args A) {
         store_vec<float, 4>(A.h + at * 2 * A.Fp + A.Fp + f, up);
       }
     } else {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int f = f0 + h * 16 + g * 4;
-        if (f < A.ld_out) *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(A.out) + at * A.ld_out + f) = v[h];
-      }
+      store_shared(A.shared, at, f0, g, v[0], v[1]);
     }
   }
 }
@@ -803,10 +832,10 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(Args A) {
 // ------------------------------------------------------ around the products --
 
 // y_t = sum over the token's assignments of w o (weight null: of o), and the gradient
-// of the weights from the feature tiles' sums.
+// of the weights from the feature tiles' sums.  Bound by the bytes of o: 8 entries a load.
 template <typename T, int V>
-__global__ __launch_bounds__(256) void combine_kernel(const float *o, int64_t ld, const float *weight, const int32_t *slot,
-                                                      int per_token, int H, T *y, const float *dot, int nt, float *dweight) {
+__global__ __launch_bounds__(256) void combine_kernel(Shared16 o, const float *weight, const int32_t *slot, int per_token,
+                                                      int H, T *y, const float *dot, int nt, float *dweight) {
   const int64_t t = blockIdx.x;
   const int32_t *sl = slot + t * per_token;
   if (dweight != nullptr && blockIdx.y == 0)
@@ -816,20 +845,27 @@ __global__ __launch_bounds__(256) void combine_kernel(const float *o, int64_t ld
         for (int i = 0; i < nt; ++i) v += dot[(int64_t)sl[q] * nt + i];
       dweight[t * per_token + q] = v;
     }
-  for (int c = (blockIdx.y * 256 + threadIdx.x) * V; c < H; c += gridDim.y * 256 * V) {
-    float v[V];
+  const int c = (blockIdx.y * 256 + threadIdx.x) * 8;
+  if (c >= H) return;
+  float v[8];
 #pragma unroll
-    for (int i = 0; i < V; ++i) v[i] = 0.f;
-    for (int q = 0; q < per_token; ++q) {
-      const int a = sl[q];
-      if (a < 0) continue;
-      const float w = weight ? weight[t * per_token + q] : 1.f;
-      float x[V];
-      load_vec<float, V>(o + a * ld + c, x);
+  for (int i = 0; i < 8; ++i) v[i] = 0.f;
+  for (int q = 0; q < per_token; ++q) {
+    const int64_t a = sl[q];
+    if (a < 0) continue;
+    const float w = weight ? weight[t * per_token + q] : 1.f;
+    const int by = (int)o.exps[a * o.ld_exp + c / 32] - 141;
+    float x[8];
+    load_vec<f16_t, 8>(o.out + a * o.ld + c, x);
 #pragma unroll
-      for (int i = 0; i < V; ++i) v[i] += w * x[i];
-    }
-    store_vec<T, V>(y + t * H + c, v);
+    for (int i = 0; i < 8; ++i) v[i] += w * ldexpf(x[i], by);
+  }
+  if constexpr (V == 8) {
+    store_vec<T, 8>(y + t * H + c, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (c + i < H) y[t * H + c + i] = (T)v[i];
   }
 }
 
@@ -857,7 +893,7 @@ inline int64_t up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
 struct Region {
   size_t x = 0, dy = 0, w1 = 0, w2 = 0;  // copies
   size_t act = 0;                         // s, or w s backwards [A][Fp]
-  size_t out = 0;                         // o, or the rows of dx [A][Hp] 32-bit
+  size_t out = 0, exps = 0;               // o, or the rows of dx [A][Hp], and their exponents
   size_t dgu = 0;                         // [A][2 Fp]
   size_t dot = 0;                         // [A][feature tiles]
   size_t total = 0;
@@ -881,7 +917,8 @@ Region region(const cfp_experts_desc &d, bool bwd, bool pad_x, bool pad_dy, bool
   if (pad_w1) r.w1 = take(E * 2 * Fp * Hp * 2);
   if (pad_w2) r.w2 = take(E * d.hidden * Fp * 2);
   r.act = take(A * Fp * 2);
-  r.out = take(A * Hp * 4);
+  r.out = take(A * Hp * 2);
+  r.exps = take(A * ((d.hidden + 31) / 32));
   if (bwd) {
     r.dgu = take(A * 2 * Fp * 2);
     r.dot = take(A * ((d.inner + kMinFeatTile - 1) / kMinFeatTile) * 4);
@@ -947,12 +984,29 @@ hipError_t few(const Args &A, int64_t n_assign, hipStream_t st) {
   return n_assign <= (int64_t)A.experts * 8 ? go(std::integral_constant<int, 1>{}) : go(std::integral_constant<int, 4>{});
 }
 
-bool large_tiles(int64_t n_assign, int experts) { return n_assign / experts >= 128; }
+// The tile of a product, rows x features: the largest that gives most compute units one.  (256 x 256 against
+// 128 x 128 and 64 x 128: training step of 4096 tokens, 480 tiles, up 148, 192 and 222 us, and 240 tiles,
+// p = dy W2 131, 145 and 155 us; a window of 7 experts, 30 tiles, 39, 20 and 16 us.)
+struct Tile {
+  int rows, feats;
+};
+Tile tile_of(int p, const Args &A, int64_t n_assign) {
+  const auto tiles = [&](int br, int bf) {  // expected: an expert's last tile is half full
+    const int64_t nt = p == kUp ? (2 * (int64_t)A.F + bf - 1) / bf : ((int64_t)A.n_feat + bf - 1) / bf;
+    if (p == kGradW1 || p == kGradW2) return nt * ((A.n_row + br - 1) / br) * A.experts;
+    return nt * (n_assign / br + std::min<int64_t>(A.experts, n_assign) / 2);
+  };
+  if (tiles(256, 256) >= 160) return {256, 256};
+  if (tiles(128, 128) >= 256) return {128, 128};
+  return {64, 128};
+}
 
 template <typename T, int P>
 hipError_t product(const Args &A, int64_t n_assign, hipStream_t st) {
-  if (large_tiles(n_assign, A.experts)) return run_product<T, P, 256, 256, 2, 2, 1>(A, n_assign, st);
-  return run_product<T, P, 128, 128, 2, 2, 2>(A, n_assign, st);
+  const Tile t = tile_of(P, A, n_assign);
+  if (t.rows == 256) return run_product<T, P, 256, 256, 2, 2, 1>(A, n_assign, st);
+  if (t.rows == 128) return run_product<T, P, 128, 128, 2, 2, 2>(A, n_assign, st);
+  return run_product<T, P, 64, 128, 2, 2, 3>(A, n_assign, st);
 }
 
 Args base_args(const cfp_experts_desc &d) {
@@ -967,16 +1021,18 @@ Args base_args(const cfp_experts_desc &d) {
   return A;
 }
 
+Shared16 shared_of(const cfp_experts_desc &d, const Region &r, uint8_t *ws) {
+  return {reinterpret_cast<f16_t *>(ws + r.out), ws + r.exps, up(d.hidden, 8), (d.hidden + 31) / 32};
+}
+
 template <typename T>
-hipError_t combine(const cfp_experts_desc &d, const float *o, const float *weight, void *y, const float *dot, int nt,
+hipError_t combine(const cfp_experts_desc &d, const Shared16 &o, const float *weight, void *y, const float *dot, int nt,
                    float *dweight, hipStream_t st) {
-  const int64_t ld = up(d.hidden, 8);
-  if (d.hidden % 4 == 0 && reinterpret_cast<uintptr_t>(y) % 8 == 0)
-    combine_kernel<T, 4><<<dim3((unsigned)d.n_tokens, (d.hidden + 1023) / 1024), 256, 0, st>>>(
-        o, ld, weight, d.slot, d.k, d.hidden, static_cast<T *>(y), dot, nt, dweight);
+  const dim3 grid((unsigned)d.n_tokens, (d.hidden + 2047) / 2048);
+  if (d.hidden % 8 == 0 && reinterpret_cast<uintptr_t>(y) % 16 == 0)
+    combine_kernel<T, 8><<<grid, 256, 0, st>>>(o, weight, d.slot, d.k, d.hidden, static_cast<T *>(y), dot, nt, dweight);
   else
-    combine_kernel<T, 1><<<dim3((unsigned)d.n_tokens, (d.hidden + 1023) / 1024), 256, 0, st>>>(
-        o, ld, weight, d.slot, d.k, d.hidden, static_cast<T *>(y), dot, nt, dweight);
+    combine_kernel<T, 1><<<grid, 256, 0, st>>>(o, weight, d.slot, d.k, d.hidden, static_cast<T *>(y), dot, nt, dweight);
   return hipGetLastError();
 }
 
@@ -1025,9 +1081,9 @@ hipError_t forward(const cfp_experts_desc &d, void *y, float *h, uint8_t *ws, hi
   A = base_args(d);
   A.row = reinterpret_cast<const char *>(ws + r.act), A.ld_row = L.Fp * 2;
   A.feat = L.w2, A.ld_feat = F * 2, A.feat_expert = (int64_t)d.hidden * F * 2;
-  A.K = (int)F, A.n_feat = d.hidden, A.out = ws + r.out, A.ld_out = L.Hp;
+  A.K = (int)F, A.n_feat = d.hidden, A.shared = shared_of(d, r, ws);
   if ((e = small ? few<T, kDown>(A, n, st) : product<T, kDown>(A, n, st)) != hipSuccess) return e;
-  return combine<T>(d, reinterpret_cast<const float *>(ws + r.out), d.weight, y, nullptr, 0, nullptr, st);
+  return combine<T>(d, A.shared, d.weight, y, nullptr, 0, nullptr, st);
 }
 
 template <typename T>
@@ -1041,19 +1097,21 @@ hipError_t backward(const cfp_experts_desc &d, const void *dy, int64_t dy_stride
   const int64_t n = d.n_tokens * d.k;
   Args A = base_args(d);
   hipError_t e = hipSuccess;
-  const int dot_tile = large_tiles(n, d.n_experts) ? 256 : kMinFeatTile, dots = (int)((L.Fp + dot_tile - 1) / dot_tile);
+  int dots = 0;
   if (n > 0) {
-  // p = dy W2, and what follows from it
-  A.row = L.dy, A.ld_row = L.ld_dy, A.feat = L.w2, A.ld_feat = L.Fp * 2, A.feat_expert = (int64_t)d.hidden * L.Fp * 2;
-  A.K = d.hidden, A.n_feat = (int)L.Fp, A.h = const_cast<float *>(h), A.out = ws + r.dgu, A.ld_out = 2 * L.Fp;
-  A.out2 = ws + r.act, A.dot = reinterpret_cast<float *>(ws + r.dot), A.dot_tiles = dots;
-  if ((e = product<T, kBackUp>(A, n, st)) != hipSuccess) return e;
-  // rows of dx
-  A = base_args(d);
-  A.row = reinterpret_cast<const char *>(ws + r.dgu), A.ld_row = 2 * L.Fp * 2;
-  A.feat = L.w1, A.ld_feat = L.Hp * 2, A.feat_expert = 2 * L.Fp * L.Hp * 2;
-  A.K = (int)(2 * L.Fp), A.n_feat = (int)L.Hp, A.out = ws + r.out, A.ld_out = L.Hp;
-  if ((e = product<T, kBackDown>(A, n, st)) != hipSuccess) return e;
+    // p = dy W2, and what follows from it
+    A.row = L.dy, A.ld_row = L.ld_dy, A.feat = L.w2, A.ld_feat = L.Fp * 2, A.feat_expert = (int64_t)d.hidden * L.Fp * 2;
+    A.K = d.hidden, A.n_feat = (int)L.Fp, A.h = const_cast<float *>(h), A.out = ws + r.dgu, A.ld_out = 2 * L.Fp;
+    A.out2 = ws + r.act, A.dot = reinterpret_cast<float *>(ws + r.dot);
+    const int dot_tile = tile_of(kBackUp, A, n).feats;
+    A.dot_tiles = dots = (int)((L.Fp + dot_tile - 1) / dot_tile);
+    if ((e = product<T, kBackUp>(A, n, st)) != hipSuccess) return e;
+    // rows of dx
+    A = base_args(d);
+    A.row = reinterpret_cast<const char *>(ws + r.dgu), A.ld_row = 2 * L.Fp * 2;
+    A.feat = L.w1, A.ld_feat = L.Hp * 2, A.feat_expert = 2 * L.Fp * L.Hp * 2;
+    A.K = (int)(2 * L.Fp), A.n_feat = (int)L.Hp, A.shared = shared_of(d, r, ws);
+    if ((e = product<T, kBackDown>(A, n, st)) != hipSuccess) return e;
   }
   // dW1 = [dg du]^T x
   A = base_args(d);
@@ -1066,7 +1124,7 @@ hipError_t backward(const cfp_experts_desc &d, const void *dy, int64_t dy_stride
   A.feat = reinterpret_cast<const char *>(ws + r.act), A.ld_feat = L.Fp * 2, A.n_feat = d.inner, A.out = dw2,
   A.ld_out = d.inner;
   if ((e = product<T, kGradW2>(A, n, st)) != hipSuccess || n == 0) return e;
-  return combine<T>(d, reinterpret_cast<const float *>(ws + r.out), nullptr, dx,
+  return combine<T>(d, shared_of(d, r, ws), nullptr, dx,
                     reinterpret_cast<const float *>(ws + r.dot), dots, dweight, st);
 }
 
