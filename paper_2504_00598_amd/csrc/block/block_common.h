@@ -40,19 +40,47 @@ __device__ __forceinline__ void store_vec(T *p, const float (&v)[N]) {
   }
 }
 
-// Sum and maximum over aligned groups of G lanes; every lane gets the result.
-template <int G>
-__device__ __forceinline__ float group_sum(float v) {
-#pragma unroll
-  for (int off = G / 2; off >= 1; off >>= 1) v += __shfl_xor(v, off, 64);
+// op over aligned groups of G lanes; every lane gets the result.  Inside a row of 16 the
+// other operand comes by data-parallel moves (quads, then mirrored halves and rows of what is
+// already equal in them), beyond it by row swaps.
+template <int CTRL>
+__device__ __forceinline__ uint32_t moved(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, CTRL, 0xf, 0xf, false);
+}
+template <int G, typename Op>
+__device__ __forceinline__ uint32_t group_reduce(uint32_t v, Op op) {
+  if constexpr (G > 1) v = op(v, moved<0xB1>(v));   // quad_perm [1, 0, 3, 2]
+  if constexpr (G > 2) v = op(v, moved<0x4E>(v));   // quad_perm [2, 3, 0, 1]
+  if constexpr (G > 4) v = op(v, moved<0x141>(v));  // row_half_mirror
+  if constexpr (G > 8) v = op(v, moved<0x140>(v));  // row_mirror
+  if constexpr (G > 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = op(r[0], r[1]);
+  }
+  if constexpr (G > 32) {
+    const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    v = op(r[0], r[1]);
+  }
   return v;
 }
 
 template <int G>
+__device__ __forceinline__ float group_sum(float v) {
+  return __uint_as_float(group_reduce<G>(__float_as_uint(v), [](uint32_t a, uint32_t b) {
+    return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
+  }));
+}
+
+template <int G>
 __device__ __forceinline__ float group_max(float v) {
-#pragma unroll
-  for (int off = G / 2; off >= 1; off >>= 1) v = fmaxf(v, __shfl_xor(v, off, 64));
-  return v;
+  return __uint_as_float(group_reduce<G>(__float_as_uint(v), [](uint32_t a, uint32_t b) {
+    return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+  }));
+}
+
+template <int G>
+__device__ __forceinline__ uint32_t group_umax(uint32_t v) {
+  return group_reduce<G>(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
 }
 
 inline int elem_bytes(int dtype) { return dtype == CFP_DT_F32 ? 4 : 2; }

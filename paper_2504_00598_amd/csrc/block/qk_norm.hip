@@ -256,24 +256,26 @@ __global__ __launch_bounds__(kQkThreads) void qk_bwd_kernel(QkArgs A) {
   }
 }
 
-// dg: the sum of the workgroups' rows.  One workgroup of 256 threads for each 16
-// entries; 16 threads share an entry's rows.
-__global__ __launch_bounds__(256) void qk_gain_kernel(const float *part, int blocks_q, int blocks_k, int dim, float *dwq,
-                                                      float *dwk) {
-  __shared__ float s[16][17];
-  const int which = blockIdx.y, e = blockIdx.x * 16 + threadIdx.x % 16, lane = threadIdx.x / 16;
+// dg: the sum of the workgroups' rows.  A workgroup takes 16 entries, 64 threads an entry.
+__global__ __launch_bounds__(1024) void qk_gain_kernel(const float *part, int blocks_q, int blocks_k, int dim, float *dwq,
+                                                       float *dwk) {
+  __shared__ float s[64][17];
+  const int which = blockIdx.y, c = threadIdx.x % 16, e = blockIdx.x * 16 + c, lane = threadIdx.x / 16;
   const int n = which ? blocks_k : blocks_q;
   const float *p = part + (which ? (int64_t)blocks_q * dim : 0);
   float v = 0.f;
-  if (e < dim)
-    for (int b = lane; b < n; b += 16) v += p[(int64_t)b * dim + e];
-  s[lane][threadIdx.x % 16] = v;
-  __syncthreads();
-  float *out = which ? dwk : dwq;
-  if (lane == 0 && e < dim && out != nullptr) {
-    for (int i = 1; i < 16; ++i) v += s[i][threadIdx.x % 16];
-    out[e] = v;
+  if (e < dim) {
+#pragma unroll 4
+    for (int b = lane; b < n; b += 64) v += p[(int64_t)b * dim + e];
   }
+  s[lane][c] = v;
+  __syncthreads();
+  for (int half = 32; half >= 1; half >>= 1) {
+    if (lane < half) s[lane][c] += s[lane + half][c];
+    __syncthreads();
+  }
+  float *out = which ? dwk : dwq;
+  if (lane == 0 && e < dim && out != nullptr) out[e] = s[0][c];
 }
 
 bool aligned(const void *p, const HeadStrides &s, int heads, int64_t tokens, int v, int bytes) {
@@ -414,7 +416,7 @@ hipError_t launch_qk_bwd(const cfp_qk_desc &d, const void *dyq, const void *dyk,
     return hipGetLastError();
   });
   if (e != hipSuccess) return e;
-  qk_gain_kernel<<<dim3((d.dim + 15) / 16, 2), 256, 0, st>>>(part, bq, bk, d.dim, dwq, dwk);
+  qk_gain_kernel<<<dim3((d.dim + 15) / 16, 2), 1024, 0, st>>>(part, bq, bk, d.dim, dwq, dwk);
   return hipGetLastError();
 }
 

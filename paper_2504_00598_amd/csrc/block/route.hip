@@ -38,16 +38,6 @@ __device__ __forceinline__ uint32_t key_of(float v, bool gone) {
   return k < 2u ? 2u : k;
 }
 
-template <int G>
-__device__ __forceinline__ uint32_t group_umax(uint32_t v) {
-#pragma unroll
-  for (int off = G / 2; off >= 1; off >>= 1) {
-    const uint32_t o = (uint32_t)__shfl_xor((int)v, off, 64);
-    v = v > o ? v : o;
-  }
-  return v;
-}
-
 template <typename T, int NPL, bool ALIGNED>
 __device__ __forceinline__ void load_logits(const T *row, int e0, int n, float (&l)[NPL]) {
   constexpr int V = NPL * (int)sizeof(T) >= 16 ? 16 / (int)sizeof(T) : NPL;
@@ -98,10 +88,20 @@ struct RouteArgs {
   float scale;
 };
 
-template <typename T, int NPL, int G, bool ALIGNED, bool GROUPED>
+// Two largest of two descending pairs, into the first.
+__device__ __forceinline__ void merge_two(float &a, float &b, float c, float d) {
+  b = fmaxf(fminf(a, c), fmaxf(b, d));
+  a = fmaxf(a, c);
+}
+
+enum Grouping { kNoGroups, kLaneGroups, kAnyGroups };
+
+template <typename T, int NPL, int G, bool ALIGNED, int GROUPS>
 __global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs A) {
   constexpr int kTok = kRouteThreads / G;
-  extern __shared__ float values[];  // groups only: [kTok][n + groups]
+  __shared__ int32_t chosen[kTok][CFP_ROUTE_MAX_K];
+  __shared__ float logit[kTok][CFP_ROUTE_MAX_K];
+  extern __shared__ float values[];  // kAnyGroups: [kTok][n + groups]
   const int lane = threadIdx.x % G, sub = threadIdx.x / G;
   const int base = (threadIdx.x % 64) / G * G;  // first lane of the group in its wave
   const int64_t t = (int64_t)blockIdx.x * kTok + sub;
@@ -118,54 +118,79 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs A) {
     if (A.bias != nullptr && e0 + i < n) v[i] = score_of(l[i], A.softmax, top, sum) + A.bias[e0 + i];
     key[i] = key_of(v[i], e0 + i >= n || l[i] == -INFINITY);
   }
-  if constexpr (GROUPED) {
+  if constexpr (GROUPS != kNoGroups) {
     const int per = n / A.groups;
-    float *val = values + sub * (n + A.groups);
-    float *gv = val + n;
+    float gval[NPL];  // what counts for a group: masked experts count for nothing
 #pragma unroll
     for (int i = 0; i < NPL; ++i)
-      if (e0 + i < n)  // what counts for a group: masked experts count for nothing
-        val[e0 + i] = key[i] == 0u ? -INFINITY
-                      : A.top2 && A.bias == nullptr ? score_of(l[i], A.softmax, top, sum) : v[i];
-    __syncthreads();
-    for (int g = lane; g < A.groups; g += G) {
+      gval[i] = key[i] == 0u                ? -INFINITY
+                : A.top2 && A.bias == nullptr ? score_of(l[i], A.softmax, top, sum)
+                                              : v[i];
+    if constexpr (GROUPS == kLaneGroups) {  // a group is a power of two of whole lanes
+      const int wide = per / NPL;
       float a = -INFINITY, b = -INFINITY;
-      for (int i = 0; i < per; ++i) {
-        const float x = val[g * per + i];
-        if (x != x) {
-          a = b = x;
-          break;
-        }
-        b = fmaxf(b, fminf(a, x));
-        a = fmaxf(a, x);
-      }
-      gv[g] = A.top2 ? a + b : a;
-    }
-    __syncthreads();
-    // a group stays if fewer than top_groups come before it
-    int held = -1;
-    bool stays = true;
+      uint32_t bad = 0u;
 #pragma unroll
-    for (int i = 0; i < NPL; ++i) {
-      if (e0 + i >= n) continue;
-      const int g = (e0 + i) / per;
-      if (g != held) {
-        held = g;
-        const uint32_t mine = key_of(gv[g], gv[g] == -INFINITY);
-        int before = 0;
-        for (int o = 0; o < A.groups; ++o) {
-          const uint32_t other = key_of(gv[o], gv[o] == -INFINITY);
-          before += other > mine || (other == mine && o < g);
-        }
-        stays = before < A.top_groups;
+      for (int i = 0; i < NPL; ++i) {
+        bad |= gval[i] != gval[i];
+        merge_two(a, b, gval[i], -INFINITY);
       }
-      if (!stays) key[i] = 0u;
+      for (int off = 1; off < wide; off <<= 1) {
+        merge_two(a, b, __shfl_xor(a, off, 64), __shfl_xor(b, off, 64));
+        bad |= (uint32_t)__shfl_xor((int)bad, off, 64);
+      }
+      const float gv = bad ? __builtin_nanf("") : A.top2 ? a + b : a;
+      const uint32_t mine = key_of(gv, gv == -INFINITY);
+      int before = 0;
+      for (int o = 0; o < A.groups; ++o) {
+        const uint32_t other = (uint32_t)__shfl((int)mine, base + o * wide, 64);
+        before += other > mine || (other == mine && o < lane / wide);
+      }
+#pragma unroll
+      for (int i = 0; i < NPL; ++i)
+        if (before >= A.top_groups) key[i] = 0u;
+    } else {
+      float *val = values + sub * (n + A.groups);
+      float *gv = val + n;
+#pragma unroll
+      for (int i = 0; i < NPL; ++i)
+        if (e0 + i < n) val[e0 + i] = gval[i];
+      __syncthreads();
+      for (int g = lane; g < A.groups; g += G) {
+        float a = -INFINITY, b = -INFINITY;
+        for (int i = 0; i < per; ++i) {
+          const float x = val[g * per + i];
+          if (x != x) {
+            a = b = x;
+            break;
+          }
+          merge_two(a, b, x, -INFINITY);
+        }
+        gv[g] = A.top2 ? a + b : a;
+      }
+      __syncthreads();
+      // a group stays if fewer than top_groups come before it
+      int held = -1;
+      bool stays = true;
+#pragma unroll
+      for (int i = 0; i < NPL; ++i) {
+        if (e0 + i >= n) continue;
+        const int g = (e0 + i) / per;
+        if (g != held) {
+          held = g;
+          const uint32_t mine = key_of(gv[g], gv[g] == -INFINITY);
+          int before = 0;
+          for (int o = 0; o < A.groups; ++o) {
+            const uint32_t other = key_of(gv[o], gv[o] == -INFINITY);
+            before += other > mine || (other == mine && o < g);
+          }
+          stays = before < A.top_groups;
+        }
+        if (!stays) key[i] = 0u;
+      }
     }
   }
   // k rounds: the first lane with the largest key gives it up
-  float w[2] = {0.f, 0.f};
-  int32_t at[2] = {-1, -1};
-  float total = 0.f;
   const uint64_t mask = (~0ull >> (64 - G)) << base;
   for (int j = 0; j < A.k; ++j) {
     uint32_t best = 0u;
@@ -173,43 +198,42 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs A) {
     for (int i = 0; i < NPL; ++i) best = best > key[i] ? best : key[i];
     const uint32_t all = group_umax<G>(best);
     const uint64_t who = __ballot(best == all) & mask;
-    const int src = __ffsll((unsigned long long)who) - 1;
-    const bool mine = (int)(threadIdx.x % 64) == src && all != 0u;
-    int e = -1;
-    float lv = 0.f;
-    if (mine) {
-      bool done = false;
+    if ((int)(threadIdx.x % 64) == __ffsll((unsigned long long)who) - 1) {
+      int e = -1;
+      float lv = 0.f;
+      if (all != 0u) {
 #pragma unroll
-      for (int i = 0; i < NPL; ++i) {
-        const bool hit = !done && key[i] == all;
-        if (hit) {
-          e = e0 + i;
-          lv = l[i];
-          key[i] = 0u;
+        for (int i = NPL - 1; i >= 0; --i) {  // the lowest index with this key is the last that is met
+          e = key[i] == all ? i : e;
+          lv = key[i] == all ? l[i] : lv;
         }
-        done = done || hit;
+#pragma unroll
+        for (int i = 0; i < NPL; ++i) key[i] = i == e ? 0u : key[i];
+        e += e0;
       }
-    }
-    e = __shfl(e, src, 64);
-    lv = __shfl(lv, src, 64);
-    const float s = e < 0 ? 0.f : score_of(lv, A.softmax, top, sum);
-    total += s;
-    if (lane == j % G) {
-      if (j < G) {
-        w[0] = s, at[0] = e;
-      } else {
-        w[1] = s, at[1] = e;
-      }
+      chosen[sub][j] = e;
+      logit[sub][j] = lv;
     }
   }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // a group's results are written and read by its own wave
+  __builtin_amdgcn_wave_barrier();
+  float w[2] = {0.f, 0.f};
+  int32_t at[2] = {-1, -1};
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int j = lane + h * G;
+    if (j >= A.k) continue;
+    at[h] = chosen[sub][j];
+    w[h] = at[h] < 0 ? 0.f : score_of(logit[sub][j], A.softmax, top, sum);
+  }
+  const float total = group_sum<G>(w[0] + w[1]);
   if (!live) return;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const int j = lane + h * G;
     if (j >= A.k) continue;
-    float x = w[h];
-    if (A.renorm) x = total == 0.f ? 0.f : x / total;
-    A.weight[t * A.k + j] = x * A.scale;
+    if (A.renorm) w[h] = total == 0.f ? 0.f : w[h] / total;
+    A.weight[t * A.k + j] = w[h] * A.scale;
     A.index[t * A.k + j] = at[h];
   }
 }
@@ -318,13 +342,15 @@ bool rows_aligned(const cfp_route_desc &d, int npl, const void *out) {
 
 constexpr int kPlanWaves = 8;
 constexpr int kPlanThreads = kPlanWaves * 64;
-constexpr int kPlanPiece = 4096;  // assignments of a workgroup
+constexpr int kPlanParts = 8;      // threads that share a bin's counts of the pieces
+// Assignments of a workgroup: one takes up to 4096, which saves the counting launch.
+inline int plan_piece(int64_t n) { return n <= 4096 ? 4096 : 2048; }
 
 struct PlanArgs {
   const int32_t *index;
   int32_t *offsets, *rows, *slot, *count;
   int64_t n;
-  int32_t experts, first;
+  int32_t experts, first, piece;
 };
 
 __device__ __forceinline__ int bin_of(const PlanArgs &A, int64_t i) {
@@ -338,7 +364,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_count_kernel(PlanArgs A) {
   const int bins = A.experts + 1;
   for (int b = threadIdx.x; b < bins; b += kPlanThreads) hist[b] = 0;
   __syncthreads();
-  const int64_t lo = (int64_t)blockIdx.x * kPlanPiece, hi = min(lo + kPlanPiece, A.n);
+  const int64_t lo = (int64_t)blockIdx.x * A.piece, hi = min(lo + A.piece, A.n);
   for (int64_t i = lo + threadIdx.x; i < hi; i += kPlanThreads) atomicAdd(&hist[bin_of(A, i)], 1);
   __syncthreads();
   for (int b = threadIdx.x; b < bins; b += kPlanThreads) A.count[(int64_t)blockIdx.x * bins + b] = hist[b];
@@ -347,12 +373,12 @@ __global__ __launch_bounds__(kPlanThreads) void plan_count_kernel(PlanArgs A) {
 // Wave w of a workgroup places the w-th part of its piece, 64 assignments at a time:
 // a lane's rank among the lanes of its bin is a ballot's population count.
 __global__ __launch_bounds__(kPlanThreads) void plan_place_kernel(PlanArgs A) {
-  extern __shared__ int32_t next[];  // [waves][bins], then start [bins]
+  extern __shared__ int32_t next[];  // [waves][bins], then start [bins] and base [bins]
   const int bins = A.experts + 1;
   if (blockIdx.x == 0 && threadIdx.x < CFP_PLAN_PAD) A.rows[A.n + threadIdx.x] = -1;
   int32_t *start = next + kPlanWaves * bins;
   const int wave = threadIdx.x / 64, lane = threadIdx.x % 64;
-  const int64_t lo = (int64_t)blockIdx.x * kPlanPiece, hi = min(lo + kPlanPiece, A.n);
+  const int64_t lo = (int64_t)blockIdx.x * A.piece, hi = min(lo + A.piece, A.n);
   const int each = (int)(((hi - lo) + kPlanWaves * 64 - 1) / (kPlanWaves * 64)) * 64;
   const int64_t from = min(lo + (int64_t)wave * each, hi), to = min(from + each, hi);
   for (int b = threadIdx.x; b < kPlanWaves * bins; b += kPlanThreads) next[b] = 0;
@@ -360,23 +386,33 @@ __global__ __launch_bounds__(kPlanThreads) void plan_place_kernel(PlanArgs A) {
   for (int64_t i = from + lane; i < to; i += 64) atomicAdd(&next[wave * bins + bin_of(A, i)], 1);
   __syncthreads();
   // bins' totals and what earlier pieces hold of them
-  for (int b = threadIdx.x; b < bins; b += kPlanThreads) {
-    int32_t before = 0, all = 0;
-    if (gridDim.x == 1) {
-      for (int w = 0; w < kPlanWaves; ++w) all += next[w * bins + b];
-    } else {
-      for (unsigned p = 0; p < gridDim.x; ++p) {
+  int32_t *base = start + bins;
+  if (gridDim.x > 1) {
+    for (int b = threadIdx.x; b < bins; b += kPlanThreads) start[b] = base[b] = 0;
+    __syncthreads();
+    const int pieces = gridDim.x, each = (pieces + kPlanParts - 1) / kPlanParts;
+    for (int x = threadIdx.x; x < bins * kPlanParts; x += kPlanThreads) {
+      const int part = x / bins, b = x - part * bins, to = min((part + 1) * each, pieces);
+      int32_t before = 0, all = 0;
+#pragma unroll 8
+      for (int p = part * each; p < to; ++p) {
         const int32_t c = A.count[(int64_t)p * bins + b];
-        before += p < blockIdx.x ? c : 0;
+        before += p < (int)blockIdx.x ? c : 0;
         all += c;
       }
+      atomicAdd(&start[b], all);
+      atomicAdd(&base[b], before);
     }
-    start[b] = all;
+    __syncthreads();
+  }
+  for (int b = threadIdx.x; b < bins; b += kPlanThreads) {
+    int32_t before = gridDim.x > 1 ? base[b] : 0, own = 0;
     for (int w = 0; w < kPlanWaves; ++w) {
       const int32_t c = next[w * bins + b];
-      next[w * bins + b] = before;
-      before += c;
+      next[w * bins + b] = before + own;
+      own += c;
     }
+    if (gridDim.x == 1) start[b] = own;
   }
   __syncthreads();
   if (wave == 0) {  // exclusive prefix sums of the totals
@@ -431,15 +467,18 @@ hipError_t launch_route(const cfp_route_desc &d, float *weight, int32_t *index, 
     return with_shape(d.n_experts, [&](auto npl, auto g) {
       constexpr int kTok = kRouteThreads / g.value;
       const unsigned grid = (unsigned)((d.n_tokens + kTok - 1) / kTok);
-      const bool al = rows_aligned(d, npl.value, nullptr), grouped = d.top_groups < d.groups;
-      const size_t lds = grouped ? (size_t)kTok * (d.n_experts + d.groups) * 4 : 0;
-      auto go = [&](auto a, auto q) {
-        route_kernel<T, npl.value, g.value, a.value, q.value><<<grid, kRouteThreads, lds, st>>>(A);
+      const int per = d.n_experts / d.groups, wide = per / npl.value;
+      const bool lanes = per % npl.value == 0 && (wide & (wide - 1)) == 0;
+      auto go = [&](auto a) {
+        if (d.top_groups == d.groups)
+          route_kernel<T, npl.value, g.value, a.value, kNoGroups><<<grid, kRouteThreads, 0, st>>>(A);
+        else if (lanes)
+          route_kernel<T, npl.value, g.value, a.value, kLaneGroups><<<grid, kRouteThreads, 0, st>>>(A);
+        else
+          route_kernel<T, npl.value, g.value, a.value, kAnyGroups>
+              <<<grid, kRouteThreads, (size_t)kTok * (d.n_experts + d.groups) * 4, st>>>(A);
       };
-      if (grouped)
-        al ? go(std::true_type{}, std::true_type{}) : go(std::false_type{}, std::true_type{});
-      else
-        al ? go(std::true_type{}, std::false_type{}) : go(std::false_type{}, std::false_type{});
+      rows_aligned(d, npl.value, nullptr) ? go(std::true_type{}) : go(std::false_type{});
       return hipGetLastError();
     });
   });
@@ -464,17 +503,18 @@ hipError_t launch_route_bwd(const cfp_route_desc &d, const int32_t *index, const
 }
 
 size_t plan_bytes(int64_t n_assign, int n_experts) {
-  const int64_t pieces = (n_assign + kPlanPiece - 1) / kPlanPiece;
+  const int64_t pieces = (n_assign + plan_piece(n_assign) - 1) / plan_piece(n_assign);
   return pieces <= 1 ? 0 : (size_t)pieces * (n_experts + 1) * 4;
 }
 
 hipError_t launch_expert_plan(const cfp_plan_desc &d, int32_t *offsets, int32_t *rows, int32_t *slot, int32_t *scratch,
                               hipStream_t st) {
-  PlanArgs A{d.index, offsets, rows, slot, scratch, d.n_tokens * d.k, d.n_experts, d.first};
+  PlanArgs A{d.index, offsets, rows, slot, scratch, d.n_tokens * d.k, d.n_experts, d.first, 0};
+  A.piece = plan_piece(A.n);
   const int bins = d.n_experts + 1;
-  const unsigned pieces = (unsigned)std::max<int64_t>(1, (A.n + kPlanPiece - 1) / kPlanPiece);
+  const unsigned pieces = (unsigned)std::max<int64_t>(1, (A.n + A.piece - 1) / A.piece);
   if (pieces > 1) plan_count_kernel<<<pieces, kPlanThreads, (size_t)bins * 4, st>>>(A);
-  plan_place_kernel<<<pieces, kPlanThreads, (size_t)(kPlanWaves + 1) * bins * 4, st>>>(A);
+  plan_place_kernel<<<pieces, kPlanThreads, (size_t)(kPlanWaves + 2) * bins * 4, st>>>(A);
   return hipGetLastError();
 }
 
