@@ -45,6 +45,13 @@ __device__ __forceinline__ void mfma(i16x8 a, i16x8 b, f32x4 &c) {
     asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
 }
 
+// Between vector instructions that write operands or sums and the matrix instructions that read them.
+__device__ __forceinline__ void written() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_nop 7" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
 // Waits until every matrix instruction has written its sums (at most 18 cycles).
 template <int M, int N>
 __device__ __forceinline__ void settle(f32x4 (&acc)[M][N]) {
@@ -511,6 +518,7 @@ __global__ __launch_bounds__(WR *WF * 64, PER_CU *WR *WF / 4) void product_kerne
   for (int a = 0; a < FF; ++a)
 #pragma unroll
     for (int b = 0; b < FR; ++b) acc[a][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+  written();
   const int steps = (K + kStep - 1) / kStep;
   if (steps > 0) {
 #pragma unroll
@@ -539,6 +547,7 @@ __global__ __launch_bounds__(WR *WF * 64, PER_CU *WR *WF / 4) void product_kerne
       if (have < 32) {  // the sum ends in this half: entries behind its end count for nothing in either operand
         each<FF>([&](auto a) { mask(fo[h.value][a.value], have - g * 8); });
         each<FR>([&](auto b) { mask(ro[h.value][b.value], have - g * 8); });
+        written();
       }
       each<kMfma>([&](auto m) {
         constexpr int a = m.value / FR, b = m.value % FR;
