@@ -376,7 +376,8 @@ def expert_plan(index, n_experts, *, first=0, stream=None) -> ExpertPlan:
     return plan
 
 
-def _experts_desc(x, w1, w2, weight, plan, torch):
+def _experts_refuse(x, w1, w2, weight, plan, torch):
+    """Raises what is wrong with the arguments."""
     half = (torch.float16, torch.bfloat16)
     _tensor("x", x, torch, half, 2)
     _tensor("w1", w1, torch, half, 3)
@@ -393,7 +394,26 @@ def _experts_desc(x, w1, w2, weight, plan, torch):
     if not isinstance(plan, ExpertPlan) or (plan.n_tokens, plan.n_experts) != (T, E) or weight.shape != (T, plan.k):
         raise ValueError("the plan is of another number of tokens, experts or places than x, w1 and weight")
     _same_device(x, w1, w2, weight, plan._buf)
-    return _EXPERTS(T, plan.k, E, H, F, _DT[x.dtype], x.data_ptr(), _rows("x", x), w1.data_ptr(), w2.data_ptr(),
+    _rows("x", x)
+
+
+def _experts_desc(x, w1, w2, weight, plan, torch):
+    # one pass over what has to hold, on the way of every call; what does not hold is said by _experts_refuse
+    try:
+        at, dt = x.get_device(), x.dtype
+        (T, H), (E, H2, F), (ld, one) = x.shape, w2.shape, x.stride()
+        ok = (at >= 0 and dt is not torch.float32 and w1.dtype is dt and w2.dtype is dt and weight.dtype is torch.float32 and
+              w1.shape == (E, 2 * F, H) and H2 == H and weight.shape == (T, plan.k) and plan.n_tokens == T and
+              plan.n_experts == E and w1.get_device() == at and w2.get_device() == at and weight.get_device() == at and
+              plan._buf.get_device() == at and w1.is_contiguous() and w2.is_contiguous() and weight.is_contiguous() and
+              (one == 1 or H == 1))
+        kind = _DT[dt]
+    except (AttributeError, KeyError, TypeError, ValueError):
+        ok = False
+    if not ok:
+        _experts_refuse(x, w1, w2, weight, plan, torch)
+        raise ValueError("unsupported arguments")
+    return _EXPERTS(T, plan.k, E, H, F, kind, x.data_ptr(), ld if T > 1 else H, w1.data_ptr(), w2.data_ptr(),
                     weight.data_ptr(), *plan._pointers())
 
 

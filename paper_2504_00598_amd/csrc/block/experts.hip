@@ -10,9 +10,10 @@
 // All six products run on the matrix units with 32-bit sums.  Rounded to 16 bits
 // between products: s, [dg du] and w s, which the next product takes as operands.
 // Kept in 32 bits: g and u for the backward pass (the gradients and dw are computed
-// from them).  The experts' outputs wait for the weighted sum over a token's experts
-// as 16-bit floats with one exponent for 32 of them: 11 bits, an eighth of a bfloat16's
-// rounding, at any magnitude, for half the bytes of 32-bit sums.
+// from them).  For bfloat16 the experts' outputs wait for the weighted sum over a token's
+// experts as 16-bit floats with one exponent for 32 of them: 11 bits, an eighth of a
+// bfloat16's rounding, at any magnitude, for half the bytes of 32-bit sums; for float16,
+// whose own rounding this would double, they wait in 32 bits.
 // Nothing is added through memory in an order that could change: a token's rows are
 // gathered and summed by the token.
 #include <algorithm>
@@ -292,12 +293,15 @@ struct Reader {
 
 enum Product { kUp, kDown, kBackUp, kBackDown, kGradW1, kGradW2 };
 
-// 16-bit floats with an exponent for 32 of them (store_shared).
-struct Shared16 {
-  f16_t *out;       // [rows][ld]
+// The experts' outputs before the weighted sum: 16-bit floats with an exponent for 32 of them (store_outputs),
+// or 32 bits for results in float16.
+struct Outputs {
+  void *out;        // [rows][ld] f16_t or float
   uint8_t *exps;    // [rows][ld_exp]
   int64_t ld, ld_exp;
 };
+template <typename T>
+constexpr bool kWideOutputs = std::is_same<T, f16_t>::value;
 
 struct Args {
   // operands: rows of the tile (assignments, or output rows of a weight gradient), and features
@@ -317,7 +321,7 @@ struct Args {
   float *h;                    // [A][2 Fp]
   const float *weight;         // [T * k]
   void *out2;                  // [A][Fp]: w s
-  Shared16 shared;             // kDown, kBackDown
+  Outputs outputs;             // kDown, kBackDown
   float *dot;                  // [A][dot_tiles]: s . p over a feature tile
   int32_t dot_tiles;
 };
@@ -385,7 +389,14 @@ __device__ __forceinline__ bool find(const Args &A, int nt, Place &p, int &ft) {
 // 32 features of a row, 8 of them in each of the four lanes of equal j (two runs of four, 16 apart), as 16-bit
 // floats under one exponent: the largest finite one, m, in [2^e, 2^(e + 1)), goes to [2^14, 2^15), and the
 // byte stored is e's in a float.  Entries that are not finite stay so.
-__device__ __forceinline__ void store_shared(const Shared16 &S, int64_t row, int f, int g, f32x4 a, f32x4 b) {
+template <typename T>
+__device__ __forceinline__ void store_outputs(const Outputs &S, int64_t row, int f, int g, f32x4 a, f32x4 b) {
+  if constexpr (kWideOutputs<T>) {
+    float *to = reinterpret_cast<float *>(S.out) + row * S.ld + f + g * 4;
+    if (f + g * 4 < S.ld) *reinterpret_cast<f32x4 *>(to) = a;
+    if (f + 16 + g * 4 < S.ld) *reinterpret_cast<f32x4 *>(to + 16) = b;
+    return;
+  }
   float m = 0.f;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
@@ -402,7 +413,7 @@ __device__ __forceinline__ void store_shared(const Shared16 &S, int64_t row, int
     u[i] = (f16_t)ldexpf(a[i], by);
     v[i] = (f16_t)ldexpf(b[i], by);
   }
-  f16_t *to = S.out + row * S.ld + f + g * 4;
+  f16_t *to = reinterpret_cast<f16_t *>(S.out) + row * S.ld + f + g * 4;
   if (f + g * 4 < S.ld) *reinterpret_cast<vec<f16_t, 4> *>(to) = u;
   if (f + 16 + g * 4 < S.ld) *reinterpret_cast<vec<f16_t, 4> *>(to + 16) = v;
   if (g == 0 && f < S.ld) S.exps[row * S.ld_exp + f / 32] = (uint8_t)e;
@@ -625,7 +636,7 @@ __global__ __launch_bounds__(WR *WF * 64, PER_CU *WR *WF / 4) void product_kerne
       if (i >= n_rows) continue;
 #pragma unroll
       for (int q = 0; q < FF; q += 2)
-        store_shared(A.shared, pl.first + i, f0 + wf * TF + q * 16, g, acc[q][b], acc[q + 1][b]);
+        store_outputs<T>(A.outputs, pl.first + i, f0 + wf * TF + q * 16, g, acc[q][b], acc[q + 1][b]);
     }
   } else if constexpr (P == kBackUp) {
     float dots[FR];
@@ -698,8 +709,9 @@ __global__ __launch_bounds__(WR *WF * 64, PER_CU *WR *WF / 4) void product_kerne
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = acc[q][b][e];
         const int width = (int)A.ld_out;
-        if (f + 4 <= width && width % 4 == 0) {
-          store_vec<T, 4>(o + f, v);
+        if (f + 4 <= width) {  // at any address: rows of an odd width
+          const vec<T, 4> w = {(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
+          __builtin_memcpy(o + f, &w, 8);
         } else {
 #pragma unroll
           for (int e = 0; e < 4; ++e)
@@ -833,7 +845,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(Args A) {
         store_vec<float, 4>(A.h + at * 2 * A.Fp + A.Fp + f, up);
       }
     } else {
-      store_shared(A.shared, at, f0, g, v[0], v[1]);
+      store_outputs<T>(A.outputs, at, f0, g, v[0], v[1]);
     }
   }
 }
@@ -842,8 +854,8 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(Args A) {
 
 // y_t = sum over the token's assignments of w o (weight null: of o), and the gradient
 // of the weights from the feature tiles' sums.  Bound by the bytes of o: 8 entries a load.
-template <typename T, int V>
-__global__ __launch_bounds__(256) void combine_kernel(Shared16 o, const float *weight, const int32_t *slot, int per_token,
+template <typename T>
+__global__ __launch_bounds__(256) void combine_kernel(Outputs o, const float *weight, const int32_t *slot, int per_token,
                                                       int H, T *y, const float *dot, int nt, float *dweight) {
   const int64_t t = blockIdx.x;
   const int32_t *sl = slot + t * per_token;
@@ -863,18 +875,28 @@ __global__ __launch_bounds__(256) void combine_kernel(Shared16 o, const float *w
     const int64_t a = sl[q];
     if (a < 0) continue;
     const float w = weight ? weight[t * per_token + q] : 1.f;
-    const int by = (int)o.exps[a * o.ld_exp + c / 32] - 141;
     float x[8];
-    load_vec<f16_t, 8>(o.out + a * o.ld + c, x);
+    if constexpr (kWideOutputs<T>) {
+      load_vec<float, 8>(reinterpret_cast<const float *>(o.out) + a * o.ld + c, x);
+    } else {
+      const int by = (int)o.exps[a * o.ld_exp + c / 32] - 141;
+      load_vec<f16_t, 8>(reinterpret_cast<const f16_t *>(o.out) + a * o.ld + c, x);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] += w * ldexpf(x[i], by);
+      for (int i = 0; i < 8; ++i) x[i] = ldexpf(x[i], by);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += w * x[i];
   }
-  if constexpr (V == 8) {
-    store_vec<T, 8>(y + t * H + c, v);
+  T *to = y + t * H + c;
+  if (c + 8 <= H) {  // at any address: rows of an odd width
+    vec<T, 8> w;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = (T)v[i];
+    __builtin_memcpy(to, &w, 16);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      if (c + i < H) y[t * H + c + i] = (T)v[i];
+      if (c + i < H) to[i] = (T)v[i];
   }
 }
 
@@ -888,10 +910,9 @@ __global__ __launch_bounds__(256) void pad_kernel(const uint16_t *in, int64_t ld
     const int y = (int)(r - e * out_rows), half = y / per, x = y - half * per;
     const uint16_t *from = in + (e * rows + half * src + min(x, src - 1)) * ld;
     uint16_t *to = out + r * out_cols;
-    for (int c = threadIdx.x * 2; c < out_cols; c += 512) {  // out_cols is a multiple of 8
-      const uint32_t a = x < src && c < cols ? from[c] : 0, b = x < src && c + 1 < cols ? from[c + 1] : 0;
-      *reinterpret_cast<uint32_t *>(to + c) = a | b << 16;
-    }
+    // out_cols is a multiple of 8
+    for (int c = threadIdx.x * 8; c < out_cols; c += 2048)
+      *reinterpret_cast<i16x8 *>(to + c) = x < src ? piece(reinterpret_cast<const char *>(from), c, cols) : i16x8{};
   }
 }
 
@@ -926,7 +947,7 @@ Region region(const cfp_experts_desc &d, bool bwd, bool pad_x, bool pad_dy, bool
   if (pad_w1) r.w1 = take(E * 2 * Fp * Hp * 2);
   if (pad_w2) r.w2 = take(E * d.hidden * Fp * 2);
   r.act = take(A * Fp * 2);
-  r.out = take(A * Hp * 2);
+  r.out = take(A * Hp * (d.dtype == CFP_DT_F16 ? 4 : 2));
   r.exps = take(A * ((d.hidden + 31) / 32));
   if (bwd) {
     r.dgu = take(A * 2 * Fp * 2);
@@ -1030,18 +1051,15 @@ Args base_args(const cfp_experts_desc &d) {
   return A;
 }
 
-Shared16 shared_of(const cfp_experts_desc &d, const Region &r, uint8_t *ws) {
-  return {reinterpret_cast<f16_t *>(ws + r.out), ws + r.exps, up(d.hidden, 8), (d.hidden + 31) / 32};
+Outputs outputs_of(const cfp_experts_desc &d, const Region &r, uint8_t *ws) {
+  return {ws + r.out, ws + r.exps, up(d.hidden, 8), (d.hidden + 31) / 32};
 }
 
 template <typename T>
-hipError_t combine(const cfp_experts_desc &d, const Shared16 &o, const float *weight, void *y, const float *dot, int nt,
+hipError_t combine(const cfp_experts_desc &d, const Outputs &o, const float *weight, void *y, const float *dot, int nt,
                    float *dweight, hipStream_t st) {
   const dim3 grid((unsigned)d.n_tokens, (d.hidden + 2047) / 2048);
-  if (d.hidden % 8 == 0 && reinterpret_cast<uintptr_t>(y) % 16 == 0)
-    combine_kernel<T, 8><<<grid, 256, 0, st>>>(o, weight, d.slot, d.k, d.hidden, static_cast<T *>(y), dot, nt, dweight);
-  else
-    combine_kernel<T, 1><<<grid, 256, 0, st>>>(o, weight, d.slot, d.k, d.hidden, static_cast<T *>(y), dot, nt, dweight);
+  combine_kernel<T><<<grid, 256, 0, st>>>(o, weight, d.slot, d.k, d.hidden, static_cast<T *>(y), dot, nt, dweight);
   return hipGetLastError();
 }
 
@@ -1090,9 +1108,9 @@ hipError_t forward(const cfp_experts_desc &d, void *y, float *h, uint8_t *ws, hi
   A = base_args(d);
   A.row = reinterpret_cast<const char *>(ws + r.act), A.ld_row = L.Fp * 2;
   A.feat = L.w2, A.ld_feat = F * 2, A.feat_expert = (int64_t)d.hidden * F * 2;
-  A.K = (int)F, A.n_feat = d.hidden, A.shared = shared_of(d, r, ws);
+  A.K = (int)F, A.n_feat = d.hidden, A.outputs = outputs_of(d, r, ws);
   if ((e = small ? few<T, kDown>(A, n, st) : product<T, kDown>(A, n, st)) != hipSuccess) return e;
-  return combine<T>(d, A.shared, d.weight, y, nullptr, 0, nullptr, st);
+  return combine<T>(d, A.outputs, d.weight, y, nullptr, 0, nullptr, st);
 }
 
 template <typename T>
@@ -1119,7 +1137,7 @@ hipError_t backward(const cfp_experts_desc &d, const void *dy, int64_t dy_stride
     A = base_args(d);
     A.row = reinterpret_cast<const char *>(ws + r.dgu), A.ld_row = 2 * L.Fp * 2;
     A.feat = L.w1, A.ld_feat = L.Hp * 2, A.feat_expert = 2 * L.Fp * L.Hp * 2;
-    A.K = (int)(2 * L.Fp), A.n_feat = (int)L.Hp, A.shared = shared_of(d, r, ws);
+    A.K = (int)(2 * L.Fp), A.n_feat = (int)L.Hp, A.outputs = outputs_of(d, r, ws);
     if ((e = product<T, kBackDown>(A, n, st)) != hipSuccess) return e;
   }
   // dW1 = [dg du]^T x
@@ -1133,7 +1151,7 @@ hipError_t backward(const cfp_experts_desc &d, const void *dy, int64_t dy_stride
   A.feat = reinterpret_cast<const char *>(ws + r.act), A.ld_feat = L.Fp * 2, A.n_feat = d.inner, A.out = dw2,
   A.ld_out = d.inner;
   if ((e = product<T, kGradW2>(A, n, st)) != hipSuccess || n == 0) return e;
-  return combine<T>(d, shared_of(d, r, ws), nullptr, dx,
+  return combine<T>(d, outputs_of(d, r, ws), nullptr, dx,
                     reinterpret_cast<const float *>(ws + r.dot), dots, dweight, st);
 }
 
