@@ -93,9 +93,11 @@ template <int I>
 __device__ __forceinline__ void copy16(const char *from) {
   asm volatile("global_load_lds_dwordx4 %0, off offset:%1" ::"v"(from), "n"(I % 4 * 1024) : "memory");
 }
+// base: of the wave.  A memory instruction reads a scalar register that a vector instruction has written five wait
+// states later at the earliest; the compiler, which keeps that distance for its own, does not know this one.
 template <int I>
-__device__ __forceinline__ void copy16(const char *base, uint32_t off) {  // base: of the wave
-  asm volatile("global_load_lds_dwordx4 %0, %1 offset:%2" ::"v"(off), "s"(base), "n"(I % 4 * 1024) : "memory");
+__device__ __forceinline__ void copy16(const char *base, uint32_t off) {
+  asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %0, %1 offset:%2" ::"v"(off), "s"(base), "n"(I % 4 * 1024) : "memory");
 }
 // A value that is the same for all lanes, in scalar registers.
 __device__ __forceinline__ int64_t uniform(int64_t x) {
@@ -389,12 +391,12 @@ __device__ __forceinline__ bool find(const Args &A, int nt, Place &p, int &ft) {
 // 32 features of a row, 8 of them in each of the four lanes of equal j (two runs of four, 16 apart), as 16-bit
 // floats under one exponent: the largest finite one, m, in [2^e, 2^(e + 1)), goes to [2^14, 2^15), and the
 // byte stored is e's in a float.  Entries that are not finite stay so.
-template <typename T>
+template <typename T, bool WHOLE>
 __device__ __forceinline__ void store_outputs(const Outputs &S, int64_t row, int f, int g, f32x4 a, f32x4 b) {
   if constexpr (kWideOutputs<T>) {
     float *to = reinterpret_cast<float *>(S.out) + row * S.ld + f + g * 4;
-    if (f + g * 4 < S.ld) *reinterpret_cast<f32x4 *>(to) = a;
-    if (f + 16 + g * 4 < S.ld) *reinterpret_cast<f32x4 *>(to + 16) = b;
+    if (WHOLE || f + g * 4 < S.ld) *reinterpret_cast<f32x4 *>(to) = a;
+    if (WHOLE || f + 16 + g * 4 < S.ld) *reinterpret_cast<f32x4 *>(to + 16) = b;
     return;
   }
   float m = 0.f;
@@ -414,12 +416,12 @@ __device__ __forceinline__ void store_outputs(const Outputs &S, int64_t row, int
     v[i] = (f16_t)ldexpf(b[i], by);
   }
   f16_t *to = reinterpret_cast<f16_t *>(S.out) + row * S.ld + f + g * 4;
-  if (f + g * 4 < S.ld) *reinterpret_cast<vec<f16_t, 4> *>(to) = u;
-  if (f + 16 + g * 4 < S.ld) *reinterpret_cast<vec<f16_t, 4> *>(to + 16) = v;
-  if (g == 0 && f < S.ld) S.exps[row * S.ld_exp + f / 32] = (uint8_t)e;
+  if (WHOLE || f + g * 4 < S.ld) *reinterpret_cast<vec<f16_t, 4> *>(to) = u;
+  if (WHOLE || f + 16 + g * 4 < S.ld) *reinterpret_cast<vec<f16_t, 4> *>(to + 16) = v;
+  if (g == 0 && (WHOLE || f < S.ld)) S.exps[row * S.ld_exp + f / 32] = (uint8_t)e;
 }
 
-__device__ __forceinline__ float sigmoid(float x) { return 1.f / (1.f + __expf(-x)); }
+__device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.f + __expf(-x)); }  // to 1e-7 or so
 
 // BR rows x BF features by WR x WF waves.  The features are the matrix instruction's
 // first operand, so that a lane holds four consecutive features of one row.
@@ -603,123 +605,127 @@ __global__ __launch_bounds__(WR *WF * 64, PER_CU *WR *WF / 4) void product_kerne
     settle(acc);
   }
 
-  // ---- epilogues: lane (j, g) holds features 4 g .. 4 g + 3 of row j of each 16 x 16 block
-  if constexpr (P == kUp) {
+  // ---- epilogues: lane (j, g) holds features 4 g .. 4 g + 3 of row j of each 16 x 16 block.  A tile that lies inside
+  // its matrix is written without a test and with addresses at fixed distances: with the tests and products
+  // of addresses the epilogue of a weight gradient's tile took 8 us, without them 2.
+  const int width = P == kUp || P == kBackUp ? A.F : P == kDown || P == kBackDown ? (int)A.outputs.ld : (int)A.ld_out;
+  const bool inside = f0 + kFeatTile <= width && r0 + BR <= n_rows && (P != kGradW1 || A.F == A.Fp);
+  auto finish = [&](auto whole) {
+    constexpr bool kWhole = whole.value;
+    const int i0 = r0 + wr * TR + j;                                              // this lane's first row
+    const int c0 = f0 + wf * (P == kUp ? TF / 2 : TF) + g * 4;                     // and first feature
+    if constexpr (P == kUp) {
+      T *s0 = reinterpret_cast<T *>(A.out) + (int64_t)(pl.first + i0) * A.ld_out + c0;
+      float *h0 = A.h == nullptr ? nullptr : A.h + (int64_t)(pl.first + i0) * 2 * A.Fp + c0;
 #pragma unroll
-    for (int b = 0; b < FR; ++b) {
-      const int i = r0 + wr * TR + b * 16 + j;
-      if (i >= n_rows) continue;
-      const int64_t a = pl.first + i;
+      for (int b = 0; b < FR; ++b) {
+        if (!kWhole && i0 + b * 16 >= n_rows) continue;
+        T *to = s0 + b * 16 * A.ld_out;
+        float *h = h0 + (int64_t)b * 32 * A.Fp;
 #pragma unroll
-      for (int q = 0; q < FF / 2; ++q) {
-        const int f = f0 + wf * (TF / 2) + q * 16 + g * 4;
-        if (f >= A.Fp) continue;
-        float s[4], ga[4], up[4];
+        for (int q = 0; q < FF / 2; ++q) {
+          if (!kWhole && c0 + q * 16 >= A.Fp) continue;
+          float s[4], ga[4], up[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const bool in = f + e < A.F;
-          ga[e] = in ? acc[q][b][e] : 0.f;
-          up[e] = in ? acc[q + FF / 2][b][e] : 0.f;
-          s[e] = ga[e] * sigmoid(ga[e]) * up[e];
+          for (int e = 0; e < 4; ++e) {
+            const bool in = kWhole || c0 + q * 16 + e < A.F;
+            ga[e] = in ? acc[q][b][e] : 0.f;
+            up[e] = in ? acc[q + FF / 2][b][e] : 0.f;
+            s[e] = ga[e] * sigmoid(ga[e]) * up[e];
+          }
+          store_vec<T, 4>(to + q * 16, s);
+          if (h0 != nullptr) {
+            store_vec<float, 4>(h + q * 16, ga);
+            store_vec<float, 4>(h + A.Fp + q * 16, up);
+          }
         }
-        store_vec<T, 4>(reinterpret_cast<T *>(A.out) + a * A.ld_out + f, s);
-        if (A.h != nullptr) {
-          store_vec<float, 4>(A.h + a * 2 * A.Fp + f, ga);
-          store_vec<float, 4>(A.h + a * 2 * A.Fp + A.Fp + f, up);
+      }
+    } else if constexpr (P == kDown || P == kBackDown) {
+#pragma unroll
+      for (int b = 0; b < FR; ++b) {
+        if (!kWhole && i0 + b * 16 >= n_rows) continue;
+#pragma unroll
+        for (int q = 0; q < FF; q += 2)
+          store_outputs<T, kWhole>(A.outputs, pl.first + i0 + b * 16, f0 + wf * TF + q * 16, g, acc[q][b], acc[q + 1][b]);
+      }
+    } else if constexpr (P == kBackUp) {
+      float dots[FR];
+      const int64_t a0 = pl.first + i0;
+#pragma unroll
+      for (int b = 0; b < FR; ++b) {
+        dots[b] = 0.f;
+        if (!kWhole && i0 + b * 16 >= n_rows) continue;
+        const float *h = A.h + (a0 + b * 16) * 2 * A.Fp + c0;
+        T *d = reinterpret_cast<T *>(A.out) + (a0 + b * 16) * A.ld_out + c0;
+        T *s0 = reinterpret_cast<T *>(A.out2) + (a0 + b * 16) * A.Fp + c0;
+        const float w = A.weight[A.rows[a0 + b * 16]];
+#pragma unroll
+        for (int q = 0; q < FF; ++q) {
+          if (!kWhole && c0 + q * 16 >= A.Fp) continue;
+          float ga[4], up[4], dg[4], du[4], ws[4];
+          load_vec<float, 4>(h + q * 16, ga);
+          load_vec<float, 4>(h + A.Fp + q * 16, up);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const bool in = kWhole || c0 + q * 16 + e < A.F;
+            const float p = in ? acc[q][b][e] : 0.f;
+            const float sg = sigmoid(ga[e]), si = ga[e] * sg, s = si * up[e];
+            dots[b] += in ? s * p : 0.f;
+            dg[e] = w * p * up[e] * sg * (1.f + ga[e] * (1.f - sg));
+            du[e] = w * p * si;
+            ws[e] = w * s;
+          }
+          store_vec<T, 4>(d + q * 16, dg);
+          store_vec<T, 4>(d + A.Fp + q * 16, du);
+          store_vec<T, 4>(s0 + q * 16, ws);
+        }
+      }
+      float *part = reinterpret_cast<float *>(smem);  // [WF][BR]
+      __syncthreads();
+#pragma unroll
+      for (int b = 0; b < FR; ++b) {
+        float v = dots[b];
+        v += __shfl_xor(v, 16, 64);
+        v += __shfl_xor(v, 32, 64);
+        if (g == 0) part[wf * BR + wr * TR + b * 16 + j] = v;
+      }
+      __syncthreads();
+      for (int r = threadIdx.x; r < BR; r += THREADS) {
+        if (!kWhole && r0 + r >= n_rows) continue;
+        float v = 0.f;
+#pragma unroll
+        for (int w = 0; w < WF; ++w) v += part[w * BR + r];
+        A.dot[(int64_t)(pl.first + r0 + r) * A.dot_tiles + ft] = v;
+      }
+    } else {  // gradients of the weights; stores of 8 bytes at any address, for rows of an odd width
+      const int64_t per = P == kGradW1 ? 2 * A.F : A.n_row;
+      T *o0 = reinterpret_cast<T *>(A.out) + (pl.expert * per + i0) * A.ld_out + c0;
+#pragma unroll
+      for (int b = 0; b < FR; ++b) {
+        T *o = o0 + b * 16 * A.ld_out;
+        if constexpr (!kWhole) {
+          const int i = i0 + b * 16, half = P == kGradW1 && i >= A.Fp;  // gate and up rows, each Fp as laid out
+          if (i >= n_rows || (P == kGradW1 && i - half * A.Fp >= A.F)) continue;
+          if (half) o -= (int64_t)(A.Fp - A.F) * A.ld_out;
+        }
+#pragma unroll
+        for (int q = 0; q < FF; ++q) {
+          const vec<T, 4> v = {(T)acc[q][b][0], (T)acc[q][b][1], (T)acc[q][b][2], (T)acc[q][b][3]};
+          if (kWhole || c0 + q * 16 + 4 <= width) {
+            __builtin_memcpy(o + q * 16, &v, 8);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (c0 + q * 16 + e < width) o[q * 16 + e] = v[e];
+          }
         }
       }
     }
-  } else if constexpr (P == kDown || P == kBackDown) {
-#pragma unroll
-    for (int b = 0; b < FR; ++b) {
-      const int i = r0 + wr * TR + b * 16 + j;
-      if (i >= n_rows) continue;
-#pragma unroll
-      for (int q = 0; q < FF; q += 2)
-        store_outputs<T>(A.outputs, pl.first + i, f0 + wf * TF + q * 16, g, acc[q][b], acc[q + 1][b]);
-    }
-  } else if constexpr (P == kBackUp) {
-    float dots[FR];
-#pragma unroll
-    for (int b = 0; b < FR; ++b) {
-      dots[b] = 0.f;
-      const int i = r0 + wr * TR + b * 16 + j;
-      if (i >= n_rows) continue;
-      const int64_t a = pl.first + i;
-      const float w = A.weight[A.rows[a]];
-#pragma unroll
-      for (int q = 0; q < FF; ++q) {
-        const int f = f0 + wf * TF + q * 16 + g * 4;
-        if (f >= A.Fp) continue;
-        float ga[4], up[4], dg[4], du[4], ws[4];
-        load_vec<float, 4>(A.h + a * 2 * A.Fp + f, ga);
-        load_vec<float, 4>(A.h + a * 2 * A.Fp + A.Fp + f, up);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const bool in = f + e < A.F;
-          const float p = in ? acc[q][b][e] : 0.f;
-          const float sg = sigmoid(ga[e]), si = ga[e] * sg, s = si * up[e];
-          dots[b] += in ? s * p : 0.f;
-          dg[e] = w * p * up[e] * sg * (1.f + ga[e] * (1.f - sg));
-          du[e] = w * p * si;
-          ws[e] = w * s;
-        }
-        T *d = reinterpret_cast<T *>(A.out) + a * A.ld_out;
-        store_vec<T, 4>(d + f, dg);
-        store_vec<T, 4>(d + A.Fp + f, du);
-        store_vec<T, 4>(reinterpret_cast<T *>(A.out2) + a * A.Fp + f, ws);
-      }
-    }
-    float *part = reinterpret_cast<float *>(smem);  // [WF][BR]
-    __syncthreads();
-#pragma unroll
-    for (int b = 0; b < FR; ++b) {
-      float v = dots[b];
-      v += __shfl_xor(v, 16, 64);
-      v += __shfl_xor(v, 32, 64);
-      if (g == 0) part[wf * BR + wr * TR + b * 16 + j] = v;
-    }
-    __syncthreads();
-    const int nt = A.dot_tiles;
-    for (int r = threadIdx.x; r < BR; r += THREADS) {
-      if (r0 + r >= n_rows) continue;
-      float v = 0.f;
-#pragma unroll
-      for (int w = 0; w < WF; ++w) v += part[w * BR + r];
-      A.dot[(int64_t)(pl.first + r0 + r) * nt + ft] = v;
-    }
-  } else {  // gradients of the weights: rows of the output, whole or scalar stores by its width
-#pragma unroll
-    for (int b = 0; b < FR; ++b) {
-      int i = r0 + wr * TR + b * 16 + j;
-      if (i >= A.n_row) continue;
-      int64_t orow = i;
-      int64_t per = A.n_row;
-      if constexpr (P == kGradW1) {  // gate and up rows, each Fp as laid out
-        const int half = i >= A.Fp, x = i - half * A.Fp;
-        if (x >= A.F) continue;
-        orow = x + (half ? A.F : 0);
-        per = 2 * A.F;
-      }
-      T *o = reinterpret_cast<T *>(A.out) + (pl.expert * per + orow) * A.ld_out;
-#pragma unroll
-      for (int q = 0; q < FF; ++q) {
-        const int f = f0 + wf * TF + q * 16 + g * 4;
-        float v[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = acc[q][b][e];
-        const int width = (int)A.ld_out;
-        if (f + 4 <= width) {  // at any address: rows of an odd width
-          const vec<T, 4> w = {(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
-          __builtin_memcpy(o + f, &w, 8);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (f + e < width) o[f + e] = (T)v[e];
-        }
-      }
-    }
-  }
+  };
+  if (inside)
+    finish(std::true_type{});
+  else
+    finish(std::false_type{});
 }
 
 // ------------------------------------------------------------- few tokens --
@@ -845,7 +851,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(Args A) {
         store_vec<float, 4>(A.h + at * 2 * A.Fp + A.Fp + f, up);
       }
     } else {
-      store_outputs<T>(A.outputs, at, f0, g, v[0], v[1]);
+      store_outputs<T, false>(A.outputs, at, f0, g, v[0], v[1]);
     }
   }
 }
