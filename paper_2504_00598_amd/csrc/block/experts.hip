@@ -29,6 +29,9 @@ typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef short i16x8 __attribute__((ext_vector_type(8)));
 typedef bf16_t bf16x8 __attribute__((ext_vector_type(8)));
 typedef f16_t f16x8 __attribute__((ext_vector_type(8)));
+typedef f16_t f16x4 __attribute__((ext_vector_type(4)));
+template <typename T>
+using vec4 = vec<T, 4>;
 typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
 typedef __attribute__((address_space(1))) const void global_void;
@@ -295,7 +298,7 @@ struct Reader {
 
 enum Product { kUp, kDown, kBackUp, kBackDown, kGradW1, kGradW2 };
 
-// The experts' outputs before the weighted sum: 16-bit floats with an exponent for 32 of them (store_outputs),
+// The experts' outputs before the weighted sum: 16-bit floats with an exponent for 32 of them (shared16),
 // or 32 bits for results in float16.
 struct Outputs {
   void *out;        // [rows][ld] f16_t or float
@@ -320,7 +323,8 @@ struct Args {
   // epilogues
   void *out;                   // 16-bit rows
   int64_t ld_out;              // elements
-  float *h;                    // [A][2 Fp]
+  float *h;                    // g and u in blocks of 16 assignments of an expert x 16 features, gate block then up block, each
+                               // in the order of the lanes that make and take it; expert e's from block row first / 16 + e on
   const float *weight;         // [T * k]
   void *out2;                  // [A][Fp]: w s
   Outputs outputs;             // kDown, kBackDown
@@ -389,16 +393,9 @@ __device__ __forceinline__ bool find(const Args &A, int nt, Place &p, int &ft) {
 }
 
 // 32 features of a row, 8 of them in each of the four lanes of equal j (two runs of four, 16 apart), as 16-bit
-// floats under one exponent: the largest finite one, m, in [2^e, 2^(e + 1)), goes to [2^14, 2^15), and the
-// byte stored is e's in a float.  Entries that are not finite stay so.
-template <typename T, bool WHOLE>
-__device__ __forceinline__ void store_outputs(const Outputs &S, int64_t row, int f, int g, f32x4 a, f32x4 b) {
-  if constexpr (kWideOutputs<T>) {
-    float *to = reinterpret_cast<float *>(S.out) + row * S.ld + f + g * 4;
-    if (WHOLE || f + g * 4 < S.ld) *reinterpret_cast<f32x4 *>(to) = a;
-    if (WHOLE || f + 16 + g * 4 < S.ld) *reinterpret_cast<f32x4 *>(to + 16) = b;
-    return;
-  }
+// floats under one exponent: the largest finite one, m, in [2^e, 2^(e + 1)), goes to [2^14, 2^15), and e as in a
+// float is returned.  Entries that are not finite stay so.
+__device__ __forceinline__ int shared16(f32x4 a, f32x4 b, f16x4 &u, f16x4 &v) {
   float m = 0.f;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
@@ -409,16 +406,12 @@ __device__ __forceinline__ void store_outputs(const Outputs &S, int64_t row, int
   m = fmaxf(m, __shfl_xor(m, 16, 64));
   m = fmaxf(m, __shfl_xor(m, 32, 64));
   const int e = (int)(__float_as_uint(m) >> 23), by = 141 - e;
-  vec<f16_t, 4> u, v;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     u[i] = (f16_t)ldexpf(a[i], by);
     v[i] = (f16_t)ldexpf(b[i], by);
   }
-  f16_t *to = reinterpret_cast<f16_t *>(S.out) + row * S.ld + f + g * 4;
-  if (WHOLE || f + g * 4 < S.ld) *reinterpret_cast<vec<f16_t, 4> *>(to) = u;
-  if (WHOLE || f + 16 + g * 4 < S.ld) *reinterpret_cast<vec<f16_t, 4> *>(to + 16) = v;
-  if (g == 0 && (WHOLE || f < S.ld)) S.exps[row * S.ld_exp + f / 32] = (uint8_t)e;
+  return e;
 }
 
 __device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.f + __expf(-x)); }  // to 1e-7 or so
@@ -605,81 +598,162 @@ __global__ __launch_bounds__(WR *WF * 64, PER_CU *WR *WF / 4) void product_kerne
     settle(acc);
   }
 
-  // ---- epilogues: lane (j, g) holds features 4 g .. 4 g + 3 of row j of each 16 x 16 block.  A tile that lies inside
-  // its matrix is written without a test and with addresses at fixed distances: with the tests and products
-  // of addresses the epilogue of a weight gradient's tile took 8 us, without them 2.
+  // ---- epilogues: lane (j, g) holds features 4 g .. 4 g + 3 of row j of each 16 x 16 block.  Stores of
+  // such pieces touch 16 lines each and took 60 cycles apiece, half of the 31 thousand cycles of a weight gradient's
+  // tile of two stages.  So 16-bit results pass through LDS, a part of its own for each wave, and leave in whole
+  // rows of that; what is kept in 32 bits is laid out by blocks in the lanes' order.  (4096 tokens to 2 of 16
+  // experts, 2048 wide, 1408 inside, tiles of 256 x 256: dW1 from 185 to 170 us, dW2 from 105 to 97 us.)
   const int width = P == kUp || P == kBackUp ? A.F : P == kDown || P == kBackDown ? (int)A.outputs.ld : (int)A.ld_out;
   const bool inside = f0 + kFeatTile <= width && r0 + BR <= n_rows && (P != kGradW1 || A.F == A.Fp);
+  constexpr int kCols = P == kUp ? TF / 2 : TF, kPieces = kCols / 8;  // a wave's results of a row
+  constexpr int kHold = P == kBackUp ? 48 : TR;               // rows of its part
+  static_assert(kHold * kCols * 2 * WAVES <= 2 * kBytes && 16 * kPieces % 64 == 0, "");
+  char *mine = smem + wave * kHold * kCols * 2;
+  auto put = [&](int row, int col, const vec<T, 4> &v) {
+    *reinterpret_cast<vec<T, 4> *>(mine + row * kCols * 2 + ((col >> 3 ^ (row & (kPieces - 1))) << 4) + (col & 4) * 2) = v;
+  };
+  // `rows` rows from row `from` of the wave's part, to to(row): where the wave's first result of that row of the part
+  // goes, or null; `limit` results of a row exist
+  auto flush = [&](auto rows, int from, auto to, int limit) {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+    for (int i = 0; i < rows.value * kPieces / 64; ++i) {
+      const int row = i * (64 / kPieces) + lane / kPieces, c = lane % kPieces;
+      const vec<T, 8> v =
+          *reinterpret_cast<const vec<T, 8> *>(mine + (from + row) * kCols * 2 + ((c ^ (row & (kPieces - 1))) << 4));
+      T *at = to(row);
+      if (at == nullptr || c * 8 >= limit) continue;
+      if (!kGrad || c * 8 + 8 <= limit) {  // the others have a multiple of 8 results in a row
+        __builtin_memcpy(at + c * 8, &v, 16);  // at any address: rows of an odd width
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (c * 8 + e < limit) at[c * 8 + e] = v[e];
+      }
+    }
+  };
+  constexpr std::integral_constant<int, TR> kAll{};
+  __syncthreads();  // every wave has read its last stage
   auto finish = [&](auto whole) {
     constexpr bool kWhole = whole.value;
-    const int i0 = r0 + wr * TR + j;                                              // this lane's first row
-    const int c0 = f0 + wf * (P == kUp ? TF / 2 : TF) + g * 4;                     // and first feature
+    const int i0 = r0 + wr * TR;       // the wave's first row
+    const int c0 = f0 + wf * kCols;    // and first feature
+    const int64_t a0 = pl.first + i0;  // its assignment, where rows are assignments
+    // the row's place in `base`, ld results a row
+    auto rows_of = [&](void *base, int64_t ld) {
+      return [=](int row) -> T * {
+        return kWhole || i0 + row < n_rows ? reinterpret_cast<T *>(base) + (a0 + row) * ld + c0 : nullptr;
+      };
+    };
+    const int Fb = (A.F + 15) / 16;
+    // this lane's part of the block of rows b and features q of what is kept: gate, and 256 entries on, up
+    auto kept = [&](int b, int q) {
+      return A.h + ((int64_t)(pl.first / 16 + pl.expert + i0 / 16 + b) * Fb + c0 / 16 + q) * 512 + lane * 4;
+    };
     if constexpr (P == kUp) {
-      T *s0 = reinterpret_cast<T *>(A.out) + (int64_t)(pl.first + i0) * A.ld_out + c0;
-      float *h0 = A.h == nullptr ? nullptr : A.h + (int64_t)(pl.first + i0) * 2 * A.Fp + c0;
 #pragma unroll
       for (int b = 0; b < FR; ++b) {
         if (!kWhole && i0 + b * 16 >= n_rows) continue;
-        T *to = s0 + b * 16 * A.ld_out;
-        float *h = h0 + (int64_t)b * 32 * A.Fp;
 #pragma unroll
         for (int q = 0; q < FF / 2; ++q) {
-          if (!kWhole && c0 + q * 16 >= A.Fp) continue;
-          float s[4], ga[4], up[4];
+          if (!kWhole && c0 + q * 16 >= A.F) continue;
+          f32x4 ga, up;
+          vec<T, 4> s;
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const bool in = kWhole || c0 + q * 16 + e < A.F;
+            const bool in = kWhole || c0 + q * 16 + g * 4 + e < A.F;
             ga[e] = in ? acc[q][b][e] : 0.f;
             up[e] = in ? acc[q + FF / 2][b][e] : 0.f;
-            s[e] = ga[e] * sigmoid(ga[e]) * up[e];
+            s[e] = (T)(ga[e] * sigmoid(ga[e]) * up[e]);
           }
-          store_vec<T, 4>(to + q * 16, s);
-          if (h0 != nullptr) {
-            store_vec<float, 4>(h + q * 16, ga);
-            store_vec<float, 4>(h + A.Fp + q * 16, up);
+          put(b * 16 + j, q * 16 + g * 4, s);
+          if (A.h != nullptr) {
+            *reinterpret_cast<f32x4 *>(kept(b, q)) = ga;
+            *reinterpret_cast<f32x4 *>(kept(b, q) + 256) = up;
           }
         }
       }
+      flush(kAll, 0, rows_of(A.out, A.ld_out), A.Fp - c0);
     } else if constexpr (P == kDown || P == kBackDown) {
+      if constexpr (kWideOutputs<T>) {
 #pragma unroll
-      for (int b = 0; b < FR; ++b) {
-        if (!kWhole && i0 + b * 16 >= n_rows) continue;
+        for (int b = 0; b < FR; ++b) {
+          if (!kWhole && i0 + b * 16 + j >= n_rows) continue;
+          float *to = reinterpret_cast<float *>(A.outputs.out) + (a0 + b * 16 + j) * A.outputs.ld + c0 + g * 4;
 #pragma unroll
-        for (int q = 0; q < FF; q += 2)
-          store_outputs<T, kWhole>(A.outputs, pl.first + i0 + b * 16, f0 + wf * TF + q * 16, g, acc[q][b], acc[q + 1][b]);
+          for (int q = 0; q < FF; ++q)
+            if (kWhole || c0 + q * 16 + g * 4 < width) *reinterpret_cast<f32x4 *>(to + q * 16) = acc[q][b];
+        }
+      } else {
+#pragma unroll
+        for (int b = 0; b < FR; ++b) {
+          uint8_t *exps = A.outputs.exps + (a0 + b * 16 + j) * A.outputs.ld_exp + c0 / 32;
+#pragma unroll
+          for (int q = 0; q < FF; q += 2) {
+            f16x4 u, v;
+            const int e = shared16(acc[q][b], acc[q + 1][b], u, v);
+            put(b * 16 + j, q * 16 + g * 4, __builtin_bit_cast(vec4<T>, u));
+            put(b * 16 + j, q * 16 + 16 + g * 4, __builtin_bit_cast(vec4<T>, v));
+            if (g == q / 2 % 4 && (kWhole || (i0 + b * 16 + j < n_rows && c0 + q * 16 < width))) exps[q / 2] = (uint8_t)e;
+          }
+        }
+        flush(kAll, 0, rows_of(A.outputs.out, A.outputs.ld), width - c0);
       }
     } else if constexpr (P == kBackUp) {
       float dots[FR];
-      const int64_t a0 = pl.first + i0;
-#pragma unroll
-      for (int b = 0; b < FR; ++b) {
-        dots[b] = 0.f;
-        if (!kWhole && i0 + b * 16 >= n_rows) continue;
-        const float *h = A.h + (a0 + b * 16) * 2 * A.Fp + c0;
-        T *d = reinterpret_cast<T *>(A.out) + (a0 + b * 16) * A.ld_out + c0;
-        T *s0 = reinterpret_cast<T *>(A.out2) + (a0 + b * 16) * A.Fp + c0;
-        const float w = A.weight[A.rows[a0 + b * 16]];
+      constexpr std::integral_constant<int, 16> kBlock{};
+      float weight[2];
+      f32x4 gate[2][FF], value[2][FF];
+      auto fetch = [&](auto at) {  // what a block of 16 rows takes, on its way while the block before is worked on
+        constexpr int b = at.value;
+        if (!kWhole && i0 + b * 16 >= n_rows) return;
+        weight[b & 1] = kWhole || i0 + b * 16 + j < n_rows ? A.weight[A.rows[a0 + b * 16 + j]] : 0.f;
 #pragma unroll
         for (int q = 0; q < FF; ++q) {
-          if (!kWhole && c0 + q * 16 >= A.Fp) continue;
-          float ga[4], up[4], dg[4], du[4], ws[4];
-          load_vec<float, 4>(h + q * 16, ga);
-          load_vec<float, 4>(h + A.Fp + q * 16, up);
+          if (!kWhole && c0 + q * 16 >= A.F) continue;
+          gate[b & 1][q] = *reinterpret_cast<const f32x4 *>(kept(b, q));
+          value[b & 1][q] = *reinterpret_cast<const f32x4 *>(kept(b, q) + 256);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      };
+      fetch(std::integral_constant<int, 0>{});
+      each<FR>([&](auto at) {  // 16 rows at a time: dg, du and w s
+        constexpr int b = at.value;
+        dots[b] = 0.f;
+        if constexpr (b + 1 < FR) fetch(std::integral_constant<int, b + 1>{});
+        if (!kWhole && i0 + b * 16 >= n_rows) return;
+        const float w = weight[b & 1];
+#pragma unroll
+        for (int q = 0; q < FF; ++q) {
+          if (!kWhole && c0 + q * 16 >= A.F) continue;
+          const f32x4 ga = gate[b & 1][q], up = value[b & 1][q];
+          vec<T, 4> dg, du, ws;
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const bool in = kWhole || c0 + q * 16 + e < A.F;
+            const bool in = kWhole || c0 + q * 16 + g * 4 + e < A.F;
             const float p = in ? acc[q][b][e] : 0.f;
             const float sg = sigmoid(ga[e]), si = ga[e] * sg, s = si * up[e];
             dots[b] += in ? s * p : 0.f;
-            dg[e] = w * p * up[e] * sg * (1.f + ga[e] * (1.f - sg));
-            du[e] = w * p * si;
-            ws[e] = w * s;
+            dg[e] = (T)(w * p * up[e] * sg * (1.f + ga[e] * (1.f - sg)));
+            du[e] = (T)(w * p * si);
+            ws[e] = (T)(in ? w * s : 0.f);
           }
-          store_vec<T, 4>(d + q * 16, dg);
-          store_vec<T, 4>(d + A.Fp + q * 16, du);
-          store_vec<T, 4>(s0 + q * 16, ws);
+          put(j, q * 16 + g * 4, dg);
+          put(16 + j, q * 16 + g * 4, du);
+          put(32 + j, q * 16 + g * 4, ws);
         }
-      }
+        auto rows_of = [&](void *base, int64_t ld) {
+          return [=](int row) -> T * {
+            const int i = i0 + b * 16 + row;
+            return kWhole || i < n_rows ? reinterpret_cast<T *>(base) + (pl.first + (int64_t)i) * ld + c0 : nullptr;
+          };
+        };
+        flush(kBlock, 0, rows_of(A.out, A.ld_out), A.Fp - c0);
+        flush(kBlock, 16, rows_of(reinterpret_cast<T *>(A.out) + A.Fp, A.ld_out), A.Fp - c0);
+        flush(kBlock, 32, rows_of(A.out2, A.Fp), A.Fp - c0);
+      });
       float *part = reinterpret_cast<float *>(smem);  // [WF][BR]
       __syncthreads();
 #pragma unroll
@@ -697,29 +771,24 @@ __global__ __launch_bounds__(WR *WF * 64, PER_CU *WR *WF / 4) void product_kerne
         for (int w = 0; w < WF; ++w) v += part[w * BR + r];
         A.dot[(int64_t)(pl.first + r0 + r) * A.dot_tiles + ft] = v;
       }
-    } else {  // gradients of the weights; stores of 8 bytes at any address, for rows of an odd width
+    } else {  // gradients of the weights
+#pragma unroll
+      for (int b = 0; b < FR; ++b)
+#pragma unroll
+        for (int q = 0; q < FF; ++q)
+          put(b * 16 + j, q * 16 + g * 4,
+              vec<T, 4>{(T)acc[q][b][0], (T)acc[q][b][1], (T)acc[q][b][2], (T)acc[q][b][3]});
       const int64_t per = P == kGradW1 ? 2 * A.F : A.n_row;
       T *o0 = reinterpret_cast<T *>(A.out) + (pl.expert * per + i0) * A.ld_out + c0;
-#pragma unroll
-      for (int b = 0; b < FR; ++b) {
-        T *o = o0 + b * 16 * A.ld_out;
-        if constexpr (!kWhole) {
-          const int i = i0 + b * 16, half = P == kGradW1 && i >= A.Fp;  // gate and up rows, each Fp as laid out
-          if (i >= n_rows || (P == kGradW1 && i - half * A.Fp >= A.F)) continue;
-          if (half) o -= (int64_t)(A.Fp - A.F) * A.ld_out;
-        }
-#pragma unroll
-        for (int q = 0; q < FF; ++q) {
-          const vec<T, 4> v = {(T)acc[q][b][0], (T)acc[q][b][1], (T)acc[q][b][2], (T)acc[q][b][3]};
-          if (kWhole || c0 + q * 16 + 4 <= width) {
-            __builtin_memcpy(o + q * 16, &v, 8);
-          } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (c0 + q * 16 + e < width) o[q * 16 + e] = v[e];
-          }
-        }
-      }
+      flush(
+          kAll, 0,
+          [&](int row) -> T * {
+            if constexpr (kWhole) return o0 + row * A.ld_out;
+            const int i = i0 + row, half = P == kGradW1 && i >= A.Fp;  // gate and up rows, each Fp as laid out
+            if (i >= n_rows || (P == kGradW1 && i - half * A.Fp >= A.F)) return nullptr;
+            return o0 + (row - half * (int64_t)(A.Fp - A.F)) * A.ld_out;
+          },
+          width - c0);
     }
   };
   if (inside)
@@ -846,12 +915,26 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(Args A) {
         s[e] = ga[e] * sigmoid(ga[e]) * up[e];
       }
       store_vec<T, 4>(reinterpret_cast<T *>(A.out) + at * A.ld_out + f, s);
-      if (A.h != nullptr) {
-        store_vec<float, 4>(A.h + at * 2 * A.Fp + f, ga);
-        store_vec<float, 4>(A.h + at * 2 * A.Fp + A.Fp + f, up);
+      if (A.h != nullptr) {  // the block of what is kept, in the lanes' order
+        float *h = A.h + ((int64_t)(pl.first / 16 + pl.expert + r0 / 16 + t) * ((A.F + 15) / 16) + ft) * 512 + lane * 4;
+        store_vec<float, 4>(h, ga);
+        store_vec<float, 4>(h + 256, up);
       }
     } else {
-      store_outputs<T, false>(A.outputs, at, f0, g, v[0], v[1]);
+      const Outputs &S = A.outputs;
+      const int f = f0 + g * 4;
+      if constexpr (kWideOutputs<T>) {
+        float *to = reinterpret_cast<float *>(S.out) + at * S.ld + f;
+        if (f < S.ld) *reinterpret_cast<f32x4 *>(to) = v[0];
+        if (f + 16 < S.ld) *reinterpret_cast<f32x4 *>(to + 16) = v[1];
+      } else {
+        f16x4 x, y;
+        const int e = shared16(v[0], v[1], x, y);
+        f16_t *to = reinterpret_cast<f16_t *>(S.out) + at * S.ld + f;
+        if (f < S.ld) *reinterpret_cast<f16x4 *>(to) = x;
+        if (f + 16 < S.ld) *reinterpret_cast<f16x4 *>(to + 16) = y;
+        if (g == 0) S.exps[at * S.ld_exp + ft] = (uint8_t)e;
+      }
     }
   }
 }
@@ -1020,27 +1103,35 @@ hipError_t few(const Args &A, int64_t n_assign, hipStream_t st) {
   return n_assign <= (int64_t)A.experts * 8 ? go(std::integral_constant<int, 1>{}) : go(std::integral_constant<int, 4>{});
 }
 
-// The tile of a product, rows x features: the largest that gives most compute units one.  (256 x 256 against
-// 128 x 128 and 64 x 128: training step of 4096 tokens, 480 tiles, up 148, 192 and 222 us, and 240 tiles,
-// p = dy W2 131, 145 and 155 us; a window of 7 experts, 30 tiles, 39, 20 and 16 us.)
+// The tile of a product, rows x features: the one of least time by a model of it, as the tiles that a compute unit
+// works through, and half of one more for the end, times a tile's fixed part and its stages.  Fitted to eleven
+// training steps of 180 to 81 thousand assignments; the tile it picks takes 1.02 times the best one's time in the mean.
+// (256 x 256 against 128 x 128 and 64 x 128: 32768 assignments of 8 experts, 2048 wide, 1408 inside, up 418, 536 and
+// 610 us; 16384 of 32, 1024 wide, 512 inside, up 87, 72 and 74 us; 1860 of 16, 536 wide, 1184 inside, down 41, 21 and
+// 18 us.)  p = dy W2 has no tile of 256 x 256, as its epilogue needs more registers than that leaves: 485, 340 and
+// 378 us in the first of these.
 struct Tile {
   int rows, feats;
 };
 Tile tile_of(int p, const Args &A, int64_t n_assign) {
-  const auto tiles = [&](int br, int bf) {  // expected: an expert's last tile is half full
-    const int64_t nt = p == kUp ? (2 * (int64_t)A.F + bf - 1) / bf : ((int64_t)A.n_feat + bf - 1) / bf;
-    if (p == kGradW1 || p == kGradW2) return nt * ((A.n_row + br - 1) / br) * A.experts;
-    return nt * (n_assign / br + std::min<int64_t>(A.experts, n_assign) / 2);
+  const bool grad = p == kGradW1 || p == kGradW2;
+  const double stages = (double)((grad ? n_assign / A.experts : A.K) + kStep - 1) / kStep;
+  const auto time = [&](int br, int bf, int per_cu, double fixed, double stage) {
+    const double nt = ((p == kUp ? 2 * (int64_t)A.F : (int64_t)A.n_feat) + bf - 1) / bf;
+    const double nr = grad ? (double)((A.n_row + br - 1) / br) * A.experts  // else an expert's last tile is half full
+                           : (double)n_assign / br + std::min<int64_t>(A.experts, n_assign) / 2;
+    return std::max(1., nt * nr / (256 * per_cu) + .5) * (fixed + stages * stage);
   };
-  if (tiles(256, 256) >= 160) return {256, 256};
-  if (tiles(128, 128) >= 256) return {128, 128};
-  return {64, 128};
+  const double t256 = p == kBackUp ? INFINITY : time(256, 256, 1, 18, 1.75), t128 = time(128, 128, 2, 5, 1.3),
+               t64 = time(64, 128, 3, 4, 1.2);
+  return t256 < std::min(t128, t64) ? Tile{256, 256} : t128 < t64 ? Tile{128, 128} : Tile{64, 128};
 }
 
 template <typename T, int P>
 hipError_t product(const Args &A, int64_t n_assign, hipStream_t st) {
   const Tile t = tile_of(P, A, n_assign);
-  if (t.rows == 256) return run_product<T, P, 256, 256, 2, 2, 1>(A, n_assign, st);
+  if constexpr (P != kBackUp)
+    if (t.rows == 256) return run_product<T, P, 256, 256, 2, 2, 1>(A, n_assign, st);
   if (t.rows == 128) return run_product<T, P, 128, 128, 2, 2, 2>(A, n_assign, st);
   return run_product<T, P, 64, 128, 2, 2, 3>(A, n_assign, st);
 }
@@ -1164,7 +1255,8 @@ hipError_t backward(const cfp_experts_desc &d, const void *dy, int64_t dy_stride
 }  // namespace
 
 size_t experts_kept_bytes(const cfp_experts_desc &d) {
-  return (size_t)d.n_tokens * d.k * 2 * up(d.inner, 8) * 4;
+  // floor(first / 16) + e leaves each expert room for its last, partial block
+  return ((size_t)d.n_tokens * d.k / 16 + d.n_experts) * ((d.inner + 15) / 16) * 512 * 4;
 }
 
 size_t experts_bytes(const cfp_experts_desc &d, bool bwd) {
