@@ -808,17 +808,24 @@ __global__ __launch_bounds__(WR *WF * 64, PER_CU *WR *WF / 4) void product_kerne
 
 constexpr int kFewWaves = 4;
 
-// Entries k .. k + 7 of a row of K, zeros behind its end.
-__device__ __forceinline__ i16x8 piece(const char *row, int k, int K) {
+// Entries k .. k + 7 of a row of K, zeros behind its end, in two steps: one load of 16 bytes that ends with the
+// row at the latest, then a shift by what it began too early.  (Entries tested one by one cost a wait each.)
+__device__ __forceinline__ i16x8 piece_load(const char *row, int k, int K) {
   i16x8 v = {};
-  if (k + 8 <= K) {
-    __builtin_memcpy(&v, row + (int64_t)k * 2, 16);
+  if (K >= 8) {
+    __builtin_memcpy(&v, row + (int64_t)min(k, K - 8) * 2, 16);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
       if (k + i < K) v[i] = reinterpret_cast<const short *>(row)[k + i];
   }
   return v;
+}
+__device__ __forceinline__ i16x8 piece_shift(i16x8 v, int k, int K) {
+  const int by = K >= 8 ? k - min(k, K - 8) : 0;
+  unsigned __int128 x = __builtin_bit_cast(unsigned __int128, v);
+  x = by < 8 ? x >> (by * 16) : 0;
+  return __builtin_bit_cast(i16x8, x);
 }
 
 template <typename T>
@@ -857,13 +864,14 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(Args A) {
   f32x4 acc[2][NT] = {};
   auto run = [&](int s, auto whole) {
     i16x8 a[2][kAhead], b[NT][kAhead];
+    auto place = [&](int i) { return s + i < to ? (s + i) * 32 + g * 8 : K; };  // past this wave's part: zeros
     auto load = [&](const char *row, int i) {
       if constexpr (whole.value) {
         i16x8 v;
         __builtin_memcpy(&v, row + (int64_t)(s * 32 + g * 8) * 2 + i * 64, 16);
         return v;
       } else {
-        return piece(row, s + i < to ? (s + i) * 32 + g * 8 : K, K);  // past this wave's part: zeros
+        return piece_load(row, place(i), K);
       }
     };
 #pragma unroll
@@ -874,6 +882,15 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(Args A) {
       for (int t = 0; t < NT; ++t) b[t][i] = load(x[t], i);
     }
     __builtin_amdgcn_sched_barrier(0);  // every load is on its way before the first is waited for
+    if constexpr (!whole.value) {
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        a[0][i] = piece_shift(a[0][i], place(i), K);
+        a[1][i] = piece_shift(a[1][i], place(i), K);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) b[t][i] = piece_shift(b[t][i], place(i), K);
+      }
+    }
 #pragma unroll
     for (int i = 0; i < kAhead; ++i)
 #pragma unroll
@@ -990,18 +1007,29 @@ __global__ __launch_bounds__(256) void combine_kernel(Outputs o, const float *we
 }
 
 // Copy of [n][rows][cols] with both inner extents padded by zeros (16-bit elements).  `halves`: the rows
-// are two runs of rows / halves that are padded each.  A workgroup copies one row of the copy at a time.
+// are two runs of rows / halves that are padded each.  Bound by its bytes: a workgroup makes kPadPieces pieces of
+// 16 bytes of the copy in a row, whatever the width, four loads a thread on their way at once.
+constexpr int kPadPieces = 1024;
 __global__ __launch_bounds__(256) void pad_kernel(const uint16_t *in, int64_t ld, int rows, int cols, int halves,
                                                   uint16_t *out, int out_rows, int out_cols, int64_t n) {
-  const int per = out_rows / halves, src = rows / halves;
-  for (int64_t r = blockIdx.x; r < n * out_rows; r += gridDim.x) {
-    const int64_t e = r / out_rows;
-    const int y = (int)(r - e * out_rows), half = y / per, x = y - half * per;
-    const uint16_t *from = in + (e * rows + half * src + min(x, src - 1)) * ld;
-    uint16_t *to = out + r * out_cols;
-    // out_cols is a multiple of 8
-    for (int c = threadIdx.x * 8; c < out_cols; c += 2048)
-      *reinterpret_cast<i16x8 *>(to + c) = x < src ? piece(reinterpret_cast<const char *>(from), c, cols) : i16x8{};
+  const int per = out_rows / halves, src = rows / halves, width = out_cols / 8;  // out_cols is a multiple of 8
+  const int64_t pieces = n * out_rows * width, from = blockIdx.x * (int64_t)kPadPieces;
+  const int64_t r0 = from / width, e0 = r0 / out_rows;
+  const int y0 = (int)(r0 - e0 * out_rows), c0 = (int)(from - r0 * width);
+  i16x8 v[4];
+  int k[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t at = c0 + i * 256 + threadIdx.x, dr = at / (uint32_t)width, y = y0 + dr, de = y / (uint32_t)out_rows;
+    const int row = (int)(y - de * out_rows), half = row >= per, x = row - half * per;
+    k[i] = x < src ? (int)(at - dr * width) * 8 : cols;
+    const int64_t e = min(e0 + (int64_t)de, n - 1);
+    v[i] = piece_load(reinterpret_cast<const char *>(in + (e * rows + half * src + min(x, src - 1)) * ld), k[i], cols);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int64_t at = from + i * 256 + threadIdx.x;
+    if (at < pieces) *reinterpret_cast<i16x8 *>(out + at * 8) = piece_shift(v[i], k[i], cols);
   }
 }
 
@@ -1054,8 +1082,8 @@ bool pads_w2(const cfp_experts_desc &d) { return d.inner % 8 != 0 || !on16(d.w2)
 
 void pad(const void *in, int64_t ld, int64_t rows, int cols, int halves, void *out, int64_t out_rows, int out_cols,
          int64_t n, hipStream_t st) {
-  const unsigned grid = (unsigned)std::min<int64_t>(n * out_rows, 8192);
-  pad_kernel<<<grid, 256, 0, st>>>(static_cast<const uint16_t *>(in), ld, (int)rows, cols, halves,
+  const int64_t grid = (n * out_rows * (out_cols / 8) + kPadPieces - 1) / kPadPieces;
+  pad_kernel<<<(unsigned)grid, 256, 0, st>>>(static_cast<const uint16_t *>(in), ld, (int)rows, cols, halves,
                                    static_cast<uint16_t *>(out), (int)out_rows, out_cols, n);
 }
 
