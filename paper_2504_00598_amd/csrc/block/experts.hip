@@ -350,7 +350,7 @@ __device__ __forceinline__ int dealt(int i, int total) {
 constexpr int kGroup = 8;
 
 template <int BR>
-__device__ __forceinline__ bool find(const Args &A, int nt, Place &p, int &ft) {
+__device__ __forceinline__ bool find(const Args &A, uint32_t block, int nt, Place &p, int &ft) {
   const int lane = threadIdx.x & 63;
   int total = 0;
   for (int e0 = 0; e0 < A.experts; e0 += 64) {
@@ -360,8 +360,8 @@ __device__ __forceinline__ bool find(const Args &A, int nt, Place &p, int &ft) {
     for (int off = 32; off >= 1; off >>= 1) c += __shfl_xor(c, off, 64);
     total += __builtin_amdgcn_readfirstlane(c);
   }
-  if ((int64_t)blockIdx.x >= (int64_t)total * nt) return false;
-  const int id = dealt(blockIdx.x, total * nt);
+  if ((int64_t)block >= (int64_t)total * nt) return false;
+  const int id = dealt(block, total * nt);
   const int tile = id / nt;
   int before = 0;
   for (int e0 = 0; e0 < A.experts; e0 += 64) {
@@ -425,8 +425,8 @@ __device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf
 // s + 1 has landed; while they work on the second half, the first operands of stage s + 1 are read and
 // stage s + 2 is copied over stage s.  Reads and copies are spread between the matrix instructions.
 // Copies go on past the end of the sum, over rows that exist.
-template <typename T, int P, int BR, int BF, int WR, int WF, int PER_CU>
-__global__ __launch_bounds__(WR *WF * 64, PER_CU *WR *WF / 4) void product_kernel(Args A) {
+template <typename T, int P, int BR, int BF, int WR, int WF>
+__device__ __forceinline__ void product_tile(const Args &A, uint32_t block) {
   constexpr int WAVES = WR * WF, THREADS = WAVES * 64;
   constexpr int TR = BR / WR, TF = BF / WF, FR = TR / 16, FF = TF / 16;
   constexpr bool kGrad = P == kGradW1 || P == kGradW2;
@@ -443,19 +443,19 @@ __global__ __launch_bounds__(WR *WF * 64, PER_CU *WR *WF / 4) void product_kerne
   if constexpr (kGrad) {
     const int nf = (A.n_feat + BF - 1) / BF, nr = (A.n_row + BR - 1) / BR;
     // every die takes a block of each expert's tiles, as the experts' sums differ in length
-    const int x = blockIdx.x & 7, i = blockIdx.x >> 3, br = (nr + A.deal_rows - 1) / A.deal_rows,
+    const int x = block & 7, i = block >> 3, br = (nr + A.deal_rows - 1) / A.deal_rows,
               bf = (nf * A.deal_rows + 7) / 8;
     pl.expert = i / (br * bf);
     const int in = i - pl.expert * br * bf;
     rt = x % A.deal_rows * br + in % br;
     ft = x / A.deal_rows * bf + in / br;
     if (rt >= nr || ft >= nf) return;
-    pl.first = A.offsets[pl.expert];
-    pl.count = A.offsets[pl.expert + 1] - pl.first;
+    pl.first = __builtin_amdgcn_readfirstlane(A.offsets[pl.expert]);
+    pl.count = __builtin_amdgcn_readfirstlane(A.offsets[pl.expert + 1]) - pl.first;
     K = pl.count;
   } else {
     const int nt = ((P == kUp ? A.F : A.n_feat) + kFeatTile - 1) / kFeatTile;
-    if (!find<BR>(A, nt, pl, ft)) return;
+    if (!find<BR>(A, block, nt, pl, ft)) return;
     rt = pl.tile;
     K = A.K;
   }
@@ -602,7 +602,7 @@ __global__ __launch_bounds__(WR *WF * 64, PER_CU *WR *WF / 4) void product_kerne
   // such pieces touch 16 lines each and took 60 cycles apiece, half of the 31 thousand cycles of a weight gradient's
   // tile of two stages.  So 16-bit results pass through LDS, a part of its own for each wave, and leave in whole
   // rows of that; what is kept in 32 bits is laid out by blocks in the lanes' order.  (4096 tokens to 2 of 16
-  // experts, 2048 wide, 1408 inside, tiles of 256 x 256: dW1 from 185 to 170 us, dW2 from 105 to 97 us.)
+  // experts, 2048 wide, 1536 inside, tiles of 256 x 256: dW1 from 185 to 170 us, dW2 from 105 to 97 us.)
   const int width = P == kUp || P == kBackUp ? A.F : P == kDown || P == kBackDown ? (int)A.outputs.ld : (int)A.ld_out;
   const bool inside = f0 + kFeatTile <= width && r0 + BR <= n_rows && (P != kGradW1 || A.F == A.Fp);
   constexpr int kCols = P == kUp ? TF / 2 : TF, kPieces = kCols / 8;  // a wave's results of a row
@@ -797,6 +797,23 @@ __global__ __launch_bounds__(WR *WF * 64, PER_CU *WR *WF / 4) void product_kerne
     finish(std::false_type{});
 }
 
+template <typename T, int P, int BR, int BF, int WR, int WF, int PER_CU>
+__global__ __launch_bounds__(WR *WF * 64, PER_CU *WR *WF / 4) void product_kernel(Args A) {
+  product_tile<T, P, BR, BF, WR, WF>(A, blockIdx.x);
+}
+
+// What follows from p = dy W2 in one launch: rows of dx, dW1 and dW2.  For steps whose products do not fill the
+// chip one by one.
+template <typename T>
+__global__ __launch_bounds__(256, 3) void gradients_kernel(Args dx, Args dw1, Args dw2, uint32_t from1, uint32_t from2) {
+  if (blockIdx.x < from1)
+    product_tile<T, kBackDown, 64, 128, 2, 2>(dx, blockIdx.x);
+  else if (blockIdx.x < from2)
+    product_tile<T, kGradW1, 64, 128, 2, 2>(dw1, blockIdx.x - from1);
+  else
+    product_tile<T, kGradW2, 64, 128, 2, 2>(dw2, blockIdx.x - from2);
+}
+
 // ------------------------------------------------------------- few tokens --
 //
 // Where an expert has a few tokens the products are bound by reading its weights once.  A workgroup takes
@@ -845,7 +862,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(Args A) {
   const int n_feat = P == kUp ? A.F : A.n_feat;
   Place pl;
   int ft;
-  if (!find<16 * NT>(A, (n_feat + kTile - 1) / kTile, pl, ft)) return;
+  if (!find<16 * NT>(A, blockIdx.x, (n_feat + kTile - 1) / kTile, pl, ft)) return;
   const int r0 = pl.tile * 16 * NT, f0 = ft * kTile, K = A.K;
   const char *base = A.feat + pl.expert * A.feat_expert;
   // rows past the end repeat the last one and are not written
@@ -1087,23 +1104,25 @@ void pad(const void *in, int64_t ld, int64_t rows, int cols, int halves, void *o
                                    static_cast<uint16_t *>(out), (int)out_rows, out_cols, n);
 }
 
+// Workgroups of a product; for gradients of weights also how the dies share an expert's tiles (A.deal_rows).
+template <int P, int BR, int BF>
+int64_t workgroups(Args &A, int64_t n_assign) {
+  constexpr int kFeatTile = P == kUp ? BF / 2 : BF;
+  const int64_t nt = ((P == kUp ? A.F : A.n_feat) + kFeatTile - 1) / kFeatTile;
+  if (P != kGradW1 && P != kGradW2) return nt * (n_assign / BR + std::min<int64_t>(A.experts, n_assign));
+  int64_t grid = 0, best = 0;
+  const int64_t nr = (A.n_row + BR - 1) / BR;
+  for (int r = 1; r <= 8; r *= 2) {  // the fewest idle workgroups, then the squarest blocks
+    const int64_t br = (nr + r - 1) / r, bf = (nt * r + 7) / 8, cost = br * bf * 1024 + br + bf;
+    if (grid == 0 || cost < best) best = cost, A.deal_rows = r, grid = 8 * br * bf * A.experts;
+  }
+  return grid;
+}
+
 template <typename T, int P, int BR, int BF, int WR, int WF, int PER_CU>
 hipError_t run_product(Args A, int64_t n_assign, hipStream_t st) {
-  constexpr int kFeatTile = P == kUp ? BF / 2 : BF;
   constexpr size_t lds = 2 * (BR + BF) * kStep * 2;
-  const int64_t nt = ((P == kUp ? A.F : A.n_feat) + kFeatTile - 1) / kFeatTile;
-  int64_t grid;
-  if (P == kGradW1 || P == kGradW2) {
-    grid = 0;
-    const int64_t nr = (A.n_row + BR - 1) / BR;
-    int64_t best = 0;
-    for (int r = 1; r <= 8; r *= 2) {  // the fewest idle workgroups, then the squarest blocks
-      const int64_t br = (nr + r - 1) / r, bf = (nt * r + 7) / 8, cost = br * bf * 1024 + br + bf;
-      if (grid == 0 || cost < best) best = cost, A.deal_rows = r, grid = 8 * br * bf * A.experts;
-    }
-  } else {
-    grid = nt * (n_assign / BR + std::min<int64_t>(A.experts, n_assign));
-  }
+  const int64_t grid = workgroups<P, BR, BF>(A, n_assign);
   if (grid > 0x7FFFFFFF) return hipErrorInvalidValue;
   auto *kernel = product_kernel<T, P, BR, BF, WR, WF, PER_CU>;
   if (lds > 65536) {
@@ -1162,6 +1181,27 @@ hipError_t product(const Args &A, int64_t n_assign, hipStream_t st) {
     if (t.rows == 256) return run_product<T, P, 256, 256, 2, 2, 1>(A, n_assign, st);
   if (t.rows == 128) return run_product<T, P, 128, 128, 2, 2, 2>(A, n_assign, st);
   return run_product<T, P, 64, 128, 2, 2, 3>(A, n_assign, st);
+}
+
+// The three products that follow from p = dy W2: in one launch of 64 x 128 tiles up to kTogether workgroups of it,
+// else one by one in the tiles of each.  (Sum of the three against the one: 777 tokens to 7 of 12 experts, 1000 wide,
+// 364 inside, 1352 workgroups, 43 and 23 us; 6000 to 2 of 8, 1024 wide, 512 inside, 3096, 126 and 108 us; 1024 to 2 of
+// 16, 2048 wide, 512 inside, 6912, 74 and 68 us.  Above, tiles of 256 x 256 are worth more.)
+constexpr int64_t kTogether = 8192;
+template <typename T>
+hipError_t gradients(Args dx, Args dw1, Args dw2, int64_t n_assign, hipStream_t st) {
+  // a multiple of 8 each, as eight dies take workgroups in turn
+  const int64_t n0 = n_assign > 0 ? up(workgroups<kBackDown, 64, 128>(dx, n_assign), 8) : 0;
+  const int64_t n1 = workgroups<kGradW1, 64, 128>(dw1, n_assign), n2 = workgroups<kGradW2, 64, 128>(dw2, n_assign);
+  if (n0 + n1 + n2 <= kTogether) {
+    gradients_kernel<T><<<(unsigned)(n0 + n1 + n2), 256, 2 * (64 + 128) * kStep * 2, st>>>(dx, dw1, dw2, (uint32_t)n0,
+                                                                                         (uint32_t)(n0 + n1));
+    return hipGetLastError();
+  }
+  hipError_t e = hipSuccess;
+  if (n_assign > 0) e = product<T, kBackDown>(dx, n_assign, st);
+  if (e == hipSuccess) e = product<T, kGradW1>(dw1, n_assign, st);
+  return e == hipSuccess ? product<T, kGradW2>(dw2, n_assign, st) : e;
 }
 
 Args base_args(const cfp_experts_desc &d) {
@@ -1258,24 +1298,19 @@ hipError_t backward(const cfp_experts_desc &d, const void *dy, int64_t dy_stride
     const int dot_tile = tile_of(kBackUp, A, n).feats;
     A.dot_tiles = dots = (int)((L.Fp + dot_tile - 1) / dot_tile);
     if ((e = product<T, kBackUp>(A, n, st)) != hipSuccess) return e;
-    // rows of dx
-    A = base_args(d);
-    A.row = reinterpret_cast<const char *>(ws + r.dgu), A.ld_row = 2 * L.Fp * 2;
-    A.feat = L.w1, A.ld_feat = L.Hp * 2, A.feat_expert = 2 * L.Fp * L.Hp * 2;
-    A.K = (int)(2 * L.Fp), A.n_feat = (int)L.Hp, A.outputs = outputs_of(d, r, ws);
-    if ((e = product<T, kBackDown>(A, n, st)) != hipSuccess) return e;
   }
-  // dW1 = [dg du]^T x
-  A = base_args(d);
-  A.row = reinterpret_cast<const char *>(ws + r.dgu), A.ld_row = 2 * L.Fp * 2, A.n_row = (int)(2 * L.Fp);
-  A.feat = L.x, A.ld_feat = L.ld_x, A.n_feat = d.hidden, A.out = dw1, A.ld_out = d.hidden;
-  if ((e = product<T, kGradW1>(A, n, st)) != hipSuccess) return e;
-  // dW2 = dy^T (w s)
-  A = base_args(d);
-  A.row = L.dy, A.ld_row = L.ld_dy, A.n_row = d.hidden;
-  A.feat = reinterpret_cast<const char *>(ws + r.act), A.ld_feat = L.Fp * 2, A.n_feat = d.inner, A.out = dw2,
-  A.ld_out = d.inner;
-  if ((e = product<T, kGradW2>(A, n, st)) != hipSuccess || n == 0) return e;
+  Args X = base_args(d);  // rows of dx
+  X.row = reinterpret_cast<const char *>(ws + r.dgu), X.ld_row = 2 * L.Fp * 2;
+  X.feat = L.w1, X.ld_feat = L.Hp * 2, X.feat_expert = 2 * L.Fp * L.Hp * 2;
+  X.K = (int)(2 * L.Fp), X.n_feat = (int)L.Hp, X.outputs = outputs_of(d, r, ws);
+  Args W1 = base_args(d);  // dW1 = [dg du]^T x
+  W1.row = reinterpret_cast<const char *>(ws + r.dgu), W1.ld_row = 2 * L.Fp * 2, W1.n_row = (int)(2 * L.Fp);
+  W1.feat = L.x, W1.ld_feat = L.ld_x, W1.n_feat = d.hidden, W1.out = dw1, W1.ld_out = d.hidden;
+  Args W2 = base_args(d);  // dW2 = dy^T (w s)
+  W2.row = L.dy, W2.ld_row = L.ld_dy, W2.n_row = d.hidden;
+  W2.feat = reinterpret_cast<const char *>(ws + r.act), W2.ld_feat = L.Fp * 2, W2.n_feat = d.inner, W2.out = dw2;
+  W2.ld_out = d.inner;
+  if ((e = gradients<T>(X, W1, W2, n, st)) != hipSuccess || n == 0) return e;
   return combine<T>(d, outputs_of(d, r, ws), nullptr, dx,
                     reinterpret_cast<const float *>(ws + r.dot), dots, dweight, st);
 }
