@@ -819,7 +819,7 @@ __global__ __launch_bounds__(256, 3) void gradients_kernel(Args dx, Args dw1, Ar
 // Where an expert has a few tokens the products are bound by reading its weights once.  A workgroup takes
 // 32 rows of them (16 gate rows and their 16 up rows, or 32 rows of W2) for 16 NT tokens, and its four
 // waves a quarter of the sum's axis each: the weights go from memory to the registers that the
-// matrix instructions take them from, kAhead steps of 2 KiB a wave ahead, and only the four partial
+// matrix instructions take them from, kMost steps of 2 KiB a wave ahead, and only the four partial
 // sums meet in LDS.  Rows need no alignment (a piece of 8 entries is one load of 16 bytes at any
 // address), so odd widths are read in place.
 
@@ -855,7 +855,7 @@ __device__ __forceinline__ f32x4 mfma_v(i16x8 a, i16x8 b, f32x4 c) {  // with wa
 
 template <typename T, int P, int NT>
 __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(Args A) {
-  constexpr int kAhead = NT == 1 ? 8 : 4;
+  constexpr int kMost = NT == 1 ? 8 : 4;  // steps of a wave on their way at once
   constexpr int kTile = P == kUp ? 16 : 32;  // features of a workgroup
   __shared__ f32x4 part[kFewWaves][NT * 2][64];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
@@ -880,6 +880,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(Args A) {
   const int from = wave * each, to = min(from + each, steps);
   f32x4 acc[2][NT] = {};
   auto run = [&](int s, auto whole) {
+    constexpr int kAhead = whole.value ? kMost : kMost / 2;  // the shifts at the end need registers of their own
     i16x8 a[2][kAhead], b[NT][kAhead];
     auto place = [&](int i) { return s + i < to ? (s + i) * 32 + g * 8 : K; };  // past this wave's part: zeros
     auto load = [&](const char *row, int i) {
@@ -917,8 +918,8 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(Args A) {
       }
   };
   int s = from;
-  for (; s + kAhead <= to && (s + kAhead) * 32 <= K; s += kAhead) run(s, std::true_type{});
-  for (; s < to; s += kAhead) run(s, std::false_type{});
+  for (; s + kMost <= to && (s + kMost) * 32 <= K; s += kMost) run(s, std::true_type{});
+  for (; s < to; s += kMost / 2) run(s, std::false_type{});
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     part[wave][2 * t][lane] = acc[0][t];
