@@ -10,10 +10,7 @@
 // All six products run on the matrix units with 32-bit sums.  Rounded to 16 bits
 // between products: s, [dg du] and w s, which the next product takes as operands.
 // Kept in 32 bits: g and u for the backward pass (the gradients and dw are computed
-// from them).  For bfloat16 the experts' outputs wait for the weighted sum over a token's
-// experts as 16-bit floats with one exponent for 32 of them: 11 bits, an eighth of a
-// bfloat16's rounding, at any magnitude, for half the bytes of 32-bit sums; for float16,
-// whose own rounding this would double, they wait in 32 bits.
+// from them), and the experts' outputs and the rows of dx, which wait for the sum over a token's experts.
 // Nothing is added through memory in an order that could change: a token's rows are
 // gathered and summed by the token.
 //
@@ -39,9 +36,6 @@ typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef short i16x8 __attribute__((ext_vector_type(8)));
 typedef bf16_t bf16x8 __attribute__((ext_vector_type(8)));
 typedef f16_t f16x8 __attribute__((ext_vector_type(8)));
-typedef f16_t f16x4 __attribute__((ext_vector_type(4)));
-template <typename T>
-using vec4 = vec<T, 4>;
 typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
 typedef __attribute__((address_space(1))) const void global_void;
@@ -308,15 +302,11 @@ struct Reader {
 
 enum Product { kUp, kDown, kBackUp, kBackDown, kGradW1, kGradW2 };
 
-// The experts' outputs before the weighted sum: 16-bit floats with an exponent for 32 of them (shared16),
-// or 32 bits for results in float16.
+// The experts' outputs before the weighted sum.
 struct Outputs {
-  void *out;        // [rows][ld] f16_t or float
-  uint8_t *exps;    // [rows][ld_exp]
-  int64_t ld, ld_exp;
+  float *out;  // [rows][ld]
+  int64_t ld;
 };
-template <typename T>
-constexpr bool kWideOutputs = std::is_same<T, f16_t>::value;
 
 struct Args {
   // operands: rows of the tile (assignments, or output rows of a weight gradient), and features
@@ -400,28 +390,6 @@ __device__ __forceinline__ bool find(const Args &A, uint32_t block, int nt, Plac
     before += __builtin_amdgcn_readfirstlane(__shfl(c, 63, 64));
   }
   return false;
-}
-
-// 32 features of a row, 8 of them in each of the four lanes of equal j (two runs of four, 16 apart), as 16-bit
-// floats under one exponent: the largest finite one, m, in [2^e, 2^(e + 1)), goes to [2^14, 2^15), and e as in a
-// float is returned.  Entries that are not finite stay so.
-__device__ __forceinline__ int shared16(f32x4 a, f32x4 b, f16x4 &u, f16x4 &v) {
-  float m = 0.f;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const float x = fabsf(a[e]), y = fabsf(b[e]);
-    m = fmaxf(m, x < INFINITY ? x : 0.f);
-    m = fmaxf(m, y < INFINITY ? y : 0.f);
-  }
-  m = fmaxf(m, __shfl_xor(m, 16, 64));
-  m = fmaxf(m, __shfl_xor(m, 32, 64));
-  const int e = (int)(__float_as_uint(m) >> 23), by = 141 - e;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    u[i] = (f16_t)ldexpf(a[i], by);
-    v[i] = (f16_t)ldexpf(b[i], by);
-  }
-  return e;
 }
 
 __device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.f + __expf(-x)); }  // to 1e-7 or so
@@ -691,29 +659,13 @@ __device__ __forceinline__ void product_tile(const Args &A, uint32_t block) {
       }
       flush(kAll, 0, rows_of(A.out, A.ld_out), A.Fp - c0);
     } else if constexpr (P == kDown || P == kBackDown) {
-      if constexpr (kWideOutputs<T>) {
 #pragma unroll
-        for (int b = 0; b < FR; ++b) {
-          if (!kWhole && i0 + b * 16 + j >= n_rows) continue;
-          float *to = reinterpret_cast<float *>(A.outputs.out) + (a0 + b * 16 + j) * A.outputs.ld + c0 + g * 4;
+      for (int b = 0; b < FR; ++b) {
+        if (!kWhole && i0 + b * 16 + j >= n_rows) continue;
+        float *to = A.outputs.out + (a0 + b * 16 + j) * A.outputs.ld + c0 + g * 4;
 #pragma unroll
-          for (int q = 0; q < FF; ++q)
-            if (kWhole || c0 + q * 16 + g * 4 < width) *reinterpret_cast<f32x4 *>(to + q * 16) = acc[q][b];
-        }
-      } else {
-#pragma unroll
-        for (int b = 0; b < FR; ++b) {
-          uint8_t *exps = A.outputs.exps + (a0 + b * 16 + j) * A.outputs.ld_exp + c0 / 32;
-#pragma unroll
-          for (int q = 0; q < FF; q += 2) {
-            f16x4 u, v;
-            const int e = shared16(acc[q][b], acc[q + 1][b], u, v);
-            put(b * 16 + j, q * 16 + g * 4, __builtin_bit_cast(vec4<T>, u));
-            put(b * 16 + j, q * 16 + 16 + g * 4, __builtin_bit_cast(vec4<T>, v));
-            if (g == q / 2 % 4 && (kWhole || (i0 + b * 16 + j < n_rows && c0 + q * 16 < width))) exps[q / 2] = (uint8_t)e;
-          }
-        }
-        flush(kAll, 0, rows_of(A.outputs.out, A.outputs.ld), width - c0);
+        for (int q = 0; q < FF; ++q)
+          if (kWhole || c0 + q * 16 + g * 4 < width) *reinterpret_cast<f32x4 *>(to + q * 16) = acc[q][b];
       }
     } else if constexpr (P == kBackUp) {
       float dots[FR];
@@ -975,18 +927,9 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(Args A) {
     } else {
       const Outputs &S = A.outputs;
       const int f = f0 + g * 4;
-      if constexpr (kWideOutputs<T>) {
-        float *to = reinterpret_cast<float *>(S.out) + at * S.ld + f;
-        if (f < S.ld) *reinterpret_cast<f32x4 *>(to) = v[0];
-        if (f + 16 < S.ld) *reinterpret_cast<f32x4 *>(to + 16) = v[1];
-      } else {
-        f16x4 x, y;
-        const int e = shared16(v[0], v[1], x, y);
-        f16_t *to = reinterpret_cast<f16_t *>(S.out) + at * S.ld + f;
-        if (f < S.ld) *reinterpret_cast<f16x4 *>(to) = x;
-        if (f + 16 < S.ld) *reinterpret_cast<f16x4 *>(to + 16) = y;
-        if (g == 0) S.exps[at * S.ld_exp + ft] = (uint8_t)e;
-      }
+      float *to = S.out + at * S.ld + f;
+      if (f < S.ld) *reinterpret_cast<f32x4 *>(to) = v[0];
+      if (f + 16 < S.ld) *reinterpret_cast<f32x4 *>(to + 16) = v[1];
     }
   }
 }
@@ -995,7 +938,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(Args A) {
 
 // y_t = sum over the token's assignments of w o (weight null: of o), and the gradient
 // of the weights from the feature tiles' sums.  Bound by the bytes of o: 8 entries a load.
-// (65536 outputs of 4096: 131 us, 5.1 TB/s.)
+// (65536 outputs of 4096: 247 us, 4.9 TB/s.)
 template <typename T>
 __global__ __launch_bounds__(256) void combine_kernel(Outputs o, const float *weight, const int32_t *slot, int per_token,
                                                       int H, T *y, const float *dot, int nt, float *dweight) {
@@ -1018,14 +961,7 @@ __global__ __launch_bounds__(256) void combine_kernel(Outputs o, const float *we
     if (a < 0) continue;
     const float w = weight ? weight[t * per_token + q] : 1.f;
     float x[8];
-    if constexpr (kWideOutputs<T>) {
-      load_vec<float, 8>(reinterpret_cast<const float *>(o.out) + a * o.ld + c, x);
-    } else {
-      const int by = (int)o.exps[a * o.ld_exp + c / 32] - 141;
-      load_vec<f16_t, 8>(reinterpret_cast<const f16_t *>(o.out) + a * o.ld + c, x);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = ldexpf(x[i], by);
-    }
+    load_vec<float, 8>(o.out + a * o.ld + c, x);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] += w * x[i];
   }
@@ -1076,7 +1012,7 @@ inline int64_t up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
 struct Region {
   size_t x = 0, dy = 0, w1 = 0, w2 = 0;  // copies
   size_t act = 0;                         // s, or w s backwards [A][Fp]
-  size_t out = 0, exps = 0;               // o, or the rows of dx [A][Hp], and their exponents
+  size_t out = 0;                         // o, or the rows of dx [A][Hp] float
   size_t dgu = 0;                         // [A][2 Fp]
   size_t dot = 0;                         // [A][feature tiles]
   size_t total = 0;
@@ -1100,8 +1036,7 @@ Region region(const cfp_experts_desc &d, bool bwd, bool pad_x, bool pad_dy, bool
   if (pad_w1) r.w1 = take(E * 2 * Fp * Hp * 2);
   if (pad_w2) r.w2 = take(E * d.hidden * Fp * 2);
   r.act = take(A * Fp * 2);
-  r.out = take(A * Hp * (d.dtype == CFP_DT_F16 ? 4 : 2));
-  r.exps = take(A * ((d.hidden + 31) / 32));
+  r.out = take(A * Hp * 4);
   if (bwd) {
     r.dgu = take(A * 2 * Fp * 2);
     r.dot = take(A * ((d.inner + kMinFeatTile - 1) / kMinFeatTile) * 4);
@@ -1236,7 +1171,7 @@ Args base_args(const cfp_experts_desc &d) {
 }
 
 Outputs outputs_of(const cfp_experts_desc &d, const Region &r, uint8_t *ws) {
-  return {ws + r.out, ws + r.exps, up(d.hidden, 8), (d.hidden + 31) / 32};
+  return {reinterpret_cast<float *>(ws + r.out), up(d.hidden, 8)};
 }
 
 template <typename T>
