@@ -83,6 +83,14 @@ __device__ __forceinline__ uint32_t group_umax(uint32_t v) {
   return group_reduce<G>(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
 }
 
+// n workgroups (below 2^31), numbered by block_id().  A launch of 2^32 threads or more in one dimension starts only
+// some of them and reports no error, so they lie in rows of kGridRow; those behind the n-th have nothing to do.
+constexpr int64_t kGridRow = 1 << 20;
+inline dim3 grid_of(int64_t n) {
+  return n <= kGridRow ? dim3((unsigned)n) : dim3((unsigned)kGridRow, (unsigned)((n + kGridRow - 1) / kGridRow));
+}
+__device__ __forceinline__ uint32_t block_id() { return blockIdx.y * gridDim.x + blockIdx.x; }
+
 inline int elem_bytes(int dtype) { return dtype == CFP_DT_F32 ? 4 : 2; }
 
 // Strides in elements of a [tokens][heads][dim] array whose last dimension is contiguous.

@@ -428,6 +428,7 @@ __device__ __forceinline__ void product_tile(const Args &A, uint32_t block) {
     const int x = block & 7, i = block >> 3, br = (nr + A.deal_rows - 1) / A.deal_rows,
               bf = (nf * A.deal_rows + 7) / 8;
     pl.expert = i / (br * bf);
+    if (pl.expert >= A.experts) return;
     const int in = i - pl.expert * br * bf;
     rt = x % A.deal_rows * br + in % br;
     ft = x / A.deal_rows * bf + in / br;
@@ -765,7 +766,7 @@ __device__ __forceinline__ void product_tile(const Args &A, uint32_t block) {
 
 template <typename T, int P, int BR, int BF, int WR, int WF, int PER_CU>
 __global__ __launch_bounds__(WR *WF * 64, PER_CU *WR *WF / 4) void product_kernel(Args A) {
-  product_tile<T, P, BR, BF, WR, WF>(A, blockIdx.x);
+  product_tile<T, P, BR, BF, WR, WF>(A, block_id());
 }
 
 // What follows from p = dy W2 in one launch: rows of dx, dW1 and dW2.  For steps whose products do not fill the
@@ -831,7 +832,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(Args A) {
   const int n_feat = P == kUp ? A.F : A.n_feat;
   Place pl;
   int ft;
-  if (!find<16 * NT>(A, blockIdx.x, (n_feat + kTile - 1) / kTile, pl, ft)) return;
+  if (!find<16 * NT>(A, block_id(), (n_feat + kTile - 1) / kTile, pl, ft)) return;
   const int r0 = pl.tile * 16 * NT, f0 = ft * kTile, K = A.K;
   const char *base = A.feat + pl.expert * A.feat_expert;
   // rows past the end repeat the last one and are not written
@@ -940,18 +941,19 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(Args A) {
 // of the weights from the feature tiles' sums.  Bound by the bytes of o: 8 entries a load.
 // (65536 outputs of 4096: 247 us, 4.9 TB/s.)
 template <typename T>
-__global__ __launch_bounds__(256) void combine_kernel(Outputs o, const float *weight, const int32_t *slot, int per_token,
-                                                      int H, T *y, const float *dot, int nt, float *dweight) {
-  const int64_t t = blockIdx.x;
+__global__ __launch_bounds__(256) void combine_kernel(Outputs o, const float *weight, const int32_t *slot, int64_t n_tokens,
+                                                      int per_token, int H, T *y, const float *dot, int nt, float *dweight) {
+  const int64_t t = block_id();
+  if (t >= n_tokens) return;
   const int32_t *sl = slot + t * per_token;
-  if (dweight != nullptr && blockIdx.y == 0)
+  if (dweight != nullptr && blockIdx.z == 0)
     for (int q = threadIdx.x; q < per_token; q += 256) {
       float v = 0.f;
       if (sl[q] >= 0)
         for (int i = 0; i < nt; ++i) v += dot[(int64_t)sl[q] * nt + i];
       dweight[t * per_token + q] = v;
     }
-  const int c = (blockIdx.y * 256 + threadIdx.x) * 8;
+  const int c = (blockIdx.z * 256 + threadIdx.x) * 8;
   if (c >= H) return;
   float v[8];
 #pragma unroll
@@ -985,7 +987,8 @@ constexpr int kPadPieces = 1024;
 __global__ __launch_bounds__(256) void pad_kernel(const uint16_t *in, int64_t ld, int rows, int cols, int halves,
                                                   uint16_t *out, int out_rows, int out_cols, int64_t n) {
   const int per = out_rows / halves, src = rows / halves, width = out_cols / 8;  // out_cols is a multiple of 8
-  const int64_t pieces = n * out_rows * width, from = blockIdx.x * (int64_t)kPadPieces;
+  const int64_t pieces = n * out_rows * width, from = block_id() * (int64_t)kPadPieces;
+  if (from >= pieces) return;
   const int64_t r0 = from / width, e0 = r0 / out_rows;
   const int y0 = (int)(r0 - e0 * out_rows), c0 = (int)(from - r0 * width);
   i16x8 v[4];
@@ -1054,7 +1057,7 @@ bool pads_w2(const cfp_experts_desc &d) { return d.inner % 8 != 0 || !on16(d.w2)
 void pad(const void *in, int64_t ld, int64_t rows, int cols, int halves, void *out, int64_t out_rows, int out_cols,
          int64_t n, hipStream_t st) {
   const int64_t grid = (n * out_rows * (out_cols / 8) + kPadPieces - 1) / kPadPieces;
-  pad_kernel<<<(unsigned)grid, 256, 0, st>>>(static_cast<const uint16_t *>(in), ld, (int)rows, cols, halves,
+  pad_kernel<<<grid_of(grid), 256, 0, st>>>(static_cast<const uint16_t *>(in), ld, (int)rows, cols, halves,
                                    static_cast<uint16_t *>(out), (int)out_rows, out_cols, n);
 }
 
@@ -1084,7 +1087,7 @@ hipError_t run_product(Args A, int64_t n_assign, hipStream_t st) {
                                              hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;
   }
-  kernel<<<(unsigned)grid, WR * WF * 64, lds, st>>>(A);
+  kernel<<<grid_of(grid), WR * WF * 64, lds, st>>>(A);
   return hipGetLastError();
 }
 
@@ -1098,7 +1101,7 @@ hipError_t few(const Args &A, int64_t n_assign, hipStream_t st) {
     const int64_t tiles = ((P == kUp ? A.F : A.n_feat) + kTile - 1) / kTile;
     const int64_t grid = tiles * (n_assign / (16 * nt.value) + std::min<int64_t>(A.experts, n_assign));
     if (grid > 0x7FFFFFFF) return hipErrorInvalidValue;
-    few_kernel<T, P, nt.value><<<(unsigned)grid, kFewWaves * 64, 0, st>>>(A);
+    few_kernel<T, P, nt.value><<<grid_of(grid), kFewWaves * 64, 0, st>>>(A);
     return hipGetLastError();
   };
   return n_assign <= (int64_t)A.experts * 8 ? go(std::integral_constant<int, 1>{}) : go(std::integral_constant<int, 4>{});
@@ -1177,8 +1180,9 @@ Outputs outputs_of(const cfp_experts_desc &d, const Region &r, uint8_t *ws) {
 template <typename T>
 hipError_t combine(const cfp_experts_desc &d, const Outputs &o, const float *weight, void *y, const float *dot, int nt,
                    float *dweight, hipStream_t st) {
-  const dim3 grid((unsigned)d.n_tokens, (d.hidden + 2047) / 2048);
-  combine_kernel<T><<<grid, 256, 0, st>>>(o, weight, d.slot, d.k, d.hidden, static_cast<T *>(y), dot, nt, dweight);
+  dim3 grid = grid_of(d.n_tokens);
+  grid.z = (d.hidden + 2047) / 2048;
+  combine_kernel<T><<<grid, 256, 0, st>>>(o, weight, d.slot, d.n_tokens, d.k, d.hidden, static_cast<T *>(y), dot, nt, dweight);
   return hipGetLastError();
 }
 

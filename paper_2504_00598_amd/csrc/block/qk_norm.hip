@@ -110,7 +110,7 @@ __global__ __launch_bounds__(kQkThreads) void qk_fwd_kernel(QkArgs A) {
   const int lane = threadIdx.x % G;
   const int heads = A.heads[0] + A.heads[1];
   const int64_t rows = A.n_tokens * heads;
-  const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / G;
+  const int64_t row = (int64_t)block_id() * kRows + threadIdx.x / G;
   if (row >= rows) return;  // whole groups leave; the others' shuffles stay inside their group
   const int64_t t = row / heads;
   const int hh = (int)(row - t * heads);
@@ -393,7 +393,7 @@ hipError_t launch_qk_fwd(const cfp_qk_desc &d, void *yq, void *yk, hipStream_t s
     using T = decltype(t);
     const int64_t rows = d.n_tokens * (d.n_q + d.n_k);
     const int64_t per = kQkThreads / g.value;
-    qk_fwd_kernel<T, v.value, g.value, u.value><<<(unsigned)((rows + per - 1) / per), kQkThreads, 0, st>>>(A);
+    qk_fwd_kernel<T, v.value, g.value, u.value><<<grid_of((rows + per - 1) / per), kQkThreads, 0, st>>>(A);
     return hipGetLastError();
   });
 }

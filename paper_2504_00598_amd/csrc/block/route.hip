@@ -107,7 +107,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs A) {
   extern __shared__ float values[];  // kAnyGroups: [kTok][n + groups]
   const int lane = threadIdx.x % G, sub = threadIdx.x / G;
   const int base = (threadIdx.x % 64) / G * G;  // first lane of the group in its wave
-  const int64_t t = (int64_t)blockIdx.x * kTok + sub;
+  const int64_t t = (int64_t)block_id() * kTok + sub;
   const bool live = t < A.n_tokens;
   const int n = A.n, e0 = lane * NPL;
   float l[NPL], v[NPL];
@@ -246,7 +246,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_bwd_kernel(RouteArgs A) {
   constexpr int kTok = kRouteThreads / G;
   const int lane = threadIdx.x % G;
   const int base = (threadIdx.x % 64) / G * G;
-  const int64_t t = (int64_t)blockIdx.x * kTok + threadIdx.x / G;
+  const int64_t t = (int64_t)block_id() * kTok + threadIdx.x / G;
   if (t >= A.n_tokens) return;  // whole groups: the others' shuffles stay inside their group
   const int n = A.n, e0 = lane * NPL;
   const T *row = reinterpret_cast<const T *>(A.logits) + t * A.stride;
@@ -469,7 +469,7 @@ hipError_t launch_route(const cfp_route_desc &d, float *weight, int32_t *index, 
     using T = decltype(t);
     return with_shape(d.n_experts, [&](auto npl, auto g) {
       constexpr int kTok = kRouteThreads / g.value;
-      const unsigned grid = (unsigned)((d.n_tokens + kTok - 1) / kTok);
+      const dim3 grid = grid_of((d.n_tokens + kTok - 1) / kTok);
       const int per = d.n_experts / d.groups, wide = per / npl.value;
       const bool lanes = per % npl.value == 0 && (wide & (wide - 1)) == 0;
       auto go = [&](auto a) {
@@ -495,7 +495,7 @@ hipError_t launch_route_bwd(const cfp_route_desc &d, const int32_t *index, const
     using T = decltype(t);
     return with_shape(d.n_experts, [&](auto npl, auto g) {
       constexpr int kTok = kRouteThreads / g.value;
-      const unsigned grid = (unsigned)((d.n_tokens + kTok - 1) / kTok);
+      const dim3 grid = grid_of((d.n_tokens + kTok - 1) / kTok);
       if (rows_aligned(d, npl.value, dlogits))
         route_bwd_kernel<T, npl.value, g.value, true><<<grid, kRouteThreads, 0, st>>>(A);
       else
