@@ -392,7 +392,15 @@ __device__ __forceinline__ bool find(const Args &A, uint32_t block, int nt, Plac
   return false;
 }
 
-__device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.f + __expf(-x)); }  // to 1e-7 or so
+// 1 / (1 + 2^t), t = -x log2(e), within four units of the last place.  The rounding of the product t alone would be
+// |x| units of 2^t: its rest r, in two parts of log2(e), is taken up as 2^(t + r) = 2^t (1 + r ln 2).  Past |x| = 100
+// the value is 1 or, below 2^-126 already at x = -88, 0.
+__device__ __forceinline__ float sigmoid(float x) {
+  constexpr float kHigh = -1.44269502f, kLow = -1.92596299e-8f, kLn2 = 0.693147181f;
+  x = fminf(fmaxf(x, -100.f), 100.f);
+  const float t = x * kHigh, r = fmaf(x, kLow, fmaf(x, kHigh, -t));
+  return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(t) * fmaf(r, kLn2, 1.f));
+}
 
 // BR rows x BF features by WR x WF waves.  The features are the matrix instruction's
 // first operand, so that a lane holds four consecutive features of one row.

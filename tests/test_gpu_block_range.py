@@ -59,3 +59,23 @@ def test_features_of_other_magnitudes(T, H, F, E, k):
     back = (got[0].double() / s, got[1].double() / s, got[2].double() * s, got[3].double() * s[:, None], got[4])
     for name, a, b in zip(("y", "dx", "dw1", "dw2", "dweight"), back, want):
         near_product(a, b.cpu(), U[torch.bfloat16] if name != "dweight" else 2.0 ** -16, name)
+
+
+@pytest.mark.parametrize("T", [60, 349])
+def test_activation_at_any_gate(T):
+    """dweight = s . p with one term: silu of the gate, in 32 bits, within eight roundings of it (below 2^-116: 0)."""
+    say("gate", T)
+    far = torch.tensor([-2.0 ** 127, -2.0 ** 14, -256, -96, 256, 2.0 ** 14, 2.0 ** 127], device="cuda")
+    gate = torch.cat((torch.arange(T, device="cuda") * 0.5 - 87, far))
+    T = len(gate)
+    x = torch.zeros(T, 8, device="cuda")
+    x[:, 0], x[:, 1] = gate, 1
+    w1, w2, dy = torch.zeros(1, 16, 8, device="cuda"), torch.zeros(1, 8, 8, device="cuda"), torch.zeros(T, 8, device="cuda")
+    w1[0, 0, 0] = w1[0, 8, 1] = w2[0, 0, 0] = 1
+    dy[:, 0] = 1
+    idx, weight = torch.zeros(T, 1, dtype=torch.int32, device="cuda"), torch.ones(T, 1, device="cuda")
+    x16 = x.bfloat16()
+    assert torch.equal(x16.float(), x)
+    dweight = results(x16, w1.bfloat16(), w2.bfloat16(), weight, idx, dy.bfloat16())[4][:, 0].double()
+    want = gate.double() * torch.sigmoid(gate.double())
+    assert bool(((dweight - want).abs() <= 2.0 ** -21 * want.abs() + 2.0 ** -116).all()), float(((dweight - want) / want).abs().nan_to_num().max())
