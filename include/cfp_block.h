@@ -15,7 +15,8 @@
  * Conventions (as in cfp.h): the caller owns all memory; nothing is allocated, kept or
  * synchronised; work is enqueued on `stream` and may be captured into a graph; argument
  * errors are returned as CFP_ERR_* before any HIP call.  16-bit and 32-bit element
- * types are CFP_DT_*; sums are held in 32 bits; a result is rounded to its type once.
+ * types are CFP_DT_*; sums are held in 32 bits; a result is rounded to its type once.  The
+ * experts' products round operands between them as well, see there.
  * Results do not depend on the order in which workgroups run.  A call with no tokens
  * writes what does not depend on them (the plan's offsets, gradients of zero) and returns CFP_OK.
  */
@@ -113,6 +114,12 @@ typedef struct {
 size_t cfp_expert_plan_workspace_bytes(const cfp_plan_desc *d);
 int cfp_expert_plan(const cfp_plan_desc *d, int32_t *offsets, int32_t *rows, int32_t *slot, void *ws, size_t ws_bytes,
                     void *stream);
+
+/* Rounding between the products: silu(gate) * up, its gradient in gate and up, and weight * silu(gate) * up are the
+ * next product's operands and are rounded to 8 bits (bfloat16) or 11 (float16) once; gate, up, dweight, the
+ * experts' outputs before the sum over a token's experts and the rows of dx are in 32 bits.  Magnitudes between the
+ * products are those of 32-bit floats for both types: float16 operands are rounded under a power of two for each
+ * vector that a product sums over, so that entries within 2^28 of the vector's largest keep their 11 bits. */
 
 #define CFP_EXPERTS_MAX_K 64
 #define CFP_EXPERTS_MAX_DIM 32768

@@ -11,6 +11,9 @@
 // between products: s, [dg du] and w s, which the next product takes as operands.
 // Kept in 32 bits: g and u for the backward pass (the gradients and dw are computed
 // from them), and the experts' outputs and the rows of dx, which wait for the sum over a token's experts.
+// float16 holds too few magnitudes for what lies between the products (s is a product of two sums, gradients are often
+// below 2^-14 where its bits run out), so there s, [dg du] and w s are first written in 32 bits and then rounded
+// under a power of two for every vector that a product sums over, which the product's result is multiplied by.
 // Nothing is added through memory in an order that could change: a token's rows are
 // gathered and summed by the token.
 //
@@ -308,6 +311,16 @@ struct Outputs {
   int64_t ld;
 };
 
+// Whether operands between the products are rounded under powers of two (see above).
+template <typename T>
+constexpr bool kScaled = std::is_same<T, f16_t>::value;
+// The power of two of a vector whose largest finite magnitude is m, as the exponent that m has as a float: m in
+// [2^e, 2^(e + 1)) goes to [2^14, 2^15).  Entries that are not finite stay so; those 2^28 below m begin to lose bits.
+__device__ __forceinline__ float finite(float x) { return fabsf(x) < INFINITY ? fabsf(x) : 0.f; }
+__device__ __forceinline__ int exponent(float m) { return (int)(__float_as_uint(m) >> 23); }
+__device__ __forceinline__ float scale_down(float x, int e) { return ldexpf(x, 141 - e); }
+__device__ __forceinline__ float scale_up(float x, int e) { return ldexpf(x, e - 141); }
+
 struct Args {
   // operands: rows of the tile (assignments, or output rows of a weight gradient), and features
   const char *row, *feat;
@@ -321,12 +334,14 @@ struct Args {
   int32_t F, Fp;               // inner width, and as laid out
   int32_t deal_rows;           // weight gradients: blocks of row tiles that eight dies divide, 1, 2, 4 or 8
   // epilogues
-  void *out;                   // 16-bit rows
+  void *out;                   // 16-bit rows; float rows of operands to be scaled
   int64_t ld_out;              // elements
   float *h;                    // g and u in blocks of 16 assignments of an expert x 16 features, gate block then up block, each
                                // in the order of the lanes that make and take it; expert e's from block row first / 16 + e on
   const float *weight;         // [T * k]
-  void *out2;                  // [A][Fp]: w s
+  void *out2;                  // w s, rows like those of out, ld_out2 elements apart
+  int64_t ld_out2;
+  const uint8_t *exps;         // weight gradients from scaled operands: exponents of an expert's Fp + Fp + Fp columns
   Outputs outputs;             // kDown, kBackDown
   float *dot;                  // [A][dot_tiles]: s . p over a feature tile
   int32_t dot_tiles;
@@ -638,6 +653,11 @@ __device__ __forceinline__ void product_tile(const Args &A, uint32_t block) {
         return kWhole || i0 + row < n_rows ? reinterpret_cast<T *>(base) + (a0 + row) * ld + c0 : nullptr;
       };
     };
+    using Between = std::conditional_t<kScaled<T>, float, T>;
+    // this lane's four entries of the block of rows b and features q in rows of floats
+    auto wide = [&](void *base, int64_t ld, int b, int q) {
+      return reinterpret_cast<float *>(base) + (a0 + b * 16 + j) * ld + c0 + q * 16 + g * 4;
+    };
     const int Fb = (A.F + 15) / 16;
     // this lane's part of the block of rows b and features q of what is kept: gate, and 256 entries on, up
     auto kept = [&](int b, int q) {
@@ -651,22 +671,25 @@ __device__ __forceinline__ void product_tile(const Args &A, uint32_t block) {
         for (int q = 0; q < FF / 2; ++q) {
           if (!kWhole && c0 + q * 16 >= A.F) continue;
           f32x4 ga, up;
-          vec<T, 4> s;
+          vec<Between, 4> s;
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const bool in = kWhole || c0 + q * 16 + g * 4 + e < A.F;
             ga[e] = in ? acc[q][b][e] : 0.f;
             up[e] = in ? acc[q + FF / 2][b][e] : 0.f;
-            s[e] = (T)(ga[e] * sigmoid(ga[e]) * up[e]);
+            s[e] = (Between)(ga[e] * sigmoid(ga[e]) * up[e]);
           }
-          put(b * 16 + j, q * 16 + g * 4, s);
+          if constexpr (!kScaled<T>)
+            put(b * 16 + j, q * 16 + g * 4, s);
+          else if (kWhole || (i0 + b * 16 + j < n_rows && c0 + q * 16 + g * 4 < A.Fp))
+            *reinterpret_cast<f32x4 *>(wide(A.out, A.ld_out, b, q)) = s;
           if (A.h != nullptr) {
             *reinterpret_cast<f32x4 *>(kept(b, q)) = ga;
             *reinterpret_cast<f32x4 *>(kept(b, q) + 256) = up;
           }
         }
       }
-      flush(kAll, 0, rows_of(A.out, A.ld_out), A.Fp - c0);
+      if constexpr (!kScaled<T>) flush(kAll, 0, rows_of(A.out, A.ld_out), A.Fp - c0);
     } else if constexpr (P == kDown || P == kBackDown) {
 #pragma unroll
       for (int b = 0; b < FR; ++b) {
@@ -704,21 +727,29 @@ __device__ __forceinline__ void product_tile(const Args &A, uint32_t block) {
         for (int q = 0; q < FF; ++q) {
           if (!kWhole && c0 + q * 16 >= A.F) continue;
           const f32x4 ga = gate[b & 1][q], up = value[b & 1][q];
-          vec<T, 4> dg, du, ws;
+          vec<Between, 4> dg, du, ws;
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const bool in = kWhole || c0 + q * 16 + g * 4 + e < A.F;
             const float p = in ? acc[q][b][e] : 0.f;
             const float sg = sigmoid(ga[e]), si = ga[e] * sg, s = si * up[e];
             dots[b] += in ? s * p : 0.f;
-            dg[e] = (T)(w * p * up[e] * sg * (1.f + ga[e] * (1.f - sg)));
-            du[e] = (T)(w * p * si);
-            ws[e] = (T)(in ? w * s : 0.f);
+            dg[e] = (Between)(w * p * up[e] * sg * (1.f + ga[e] * (1.f - sg)));
+            du[e] = (Between)(w * p * si);
+            ws[e] = (Between)(in ? w * s : 0.f);
           }
-          put(j, q * 16 + g * 4, dg);
-          put(16 + j, q * 16 + g * 4, du);
-          put(32 + j, q * 16 + g * 4, ws);
+          if constexpr (!kScaled<T>) {
+            put(j, q * 16 + g * 4, dg);
+            put(16 + j, q * 16 + g * 4, du);
+            put(32 + j, q * 16 + g * 4, ws);
+          } else if (kWhole || (i0 + b * 16 + j < n_rows && c0 + q * 16 + g * 4 < A.Fp)) {
+            float *to = wide(A.out, A.ld_out, b, q);
+            *reinterpret_cast<f32x4 *>(to) = dg;
+            *reinterpret_cast<f32x4 *>(to + A.Fp) = du;
+            *reinterpret_cast<f32x4 *>(wide(A.out2, A.ld_out2, b, q)) = ws;
+          }
         }
+        if constexpr (kScaled<T>) return;
         auto rows_of = [&](void *base, int64_t ld) {
           return [=](int row) -> T * {
             const int i = i0 + b * 16 + row;
@@ -727,7 +758,7 @@ __device__ __forceinline__ void product_tile(const Args &A, uint32_t block) {
         };
         flush(kBlock, 0, rows_of(A.out, A.ld_out), A.Fp - c0);
         flush(kBlock, 16, rows_of(reinterpret_cast<T *>(A.out) + A.Fp, A.ld_out), A.Fp - c0);
-        flush(kBlock, 32, rows_of(A.out2, A.Fp), A.Fp - c0);
+        flush(kBlock, 32, rows_of(A.out2, A.ld_out2), A.Fp - c0);
       });
       float *part = reinterpret_cast<float *>(smem);  // [WF][BR]
       __syncthreads();
@@ -750,9 +781,21 @@ __device__ __forceinline__ void product_tile(const Args &A, uint32_t block) {
 #pragma unroll
       for (int b = 0; b < FR; ++b)
 #pragma unroll
-        for (int q = 0; q < FF; ++q)
-          put(b * 16 + j, q * 16 + g * 4,
-              vec<T, 4>{(T)acc[q][b][0], (T)acc[q][b][1], (T)acc[q][b][2], (T)acc[q][b][3]});
+        for (int q = 0; q < FF; ++q) {
+          f32x4 v = acc[q][b];
+          if (kScaled<T> && pl.count > 0) {  // an expert's exponents: of gate, up and w s (not there without any row)
+            const uint8_t *exps = A.exps + pl.expert * (int64_t)(3 * A.Fp);
+            if constexpr (P == kGradW1) {
+              const int by = exps[min(i0 + b * 16 + j, A.n_row - 1)];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) v[e] = scale_up(v[e], by);
+            } else {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) v[e] = scale_up(v[e], exps[2 * A.Fp + min(c0 + q * 16 + g * 4 + e, A.Fp - 1)]);
+            }
+          }
+          put(b * 16 + j, q * 16 + g * 4, vec<T, 4>{(T)v[0], (T)v[1], (T)v[2], (T)v[3]});
+        }
       const int64_t per = P == kGradW1 ? 2 * A.F : A.n_row;
       T *o0 = reinterpret_cast<T *>(A.out) + (pl.expert * per + i0) * A.ld_out + c0;
       flush(
@@ -927,7 +970,8 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(Args A) {
         up[e] = in ? v[1][e] : 0.f;
         s[e] = ga[e] * sigmoid(ga[e]) * up[e];
       }
-      store_vec<T, 4>(reinterpret_cast<T *>(A.out) + at * A.ld_out + f, s);
+      using Between = std::conditional_t<kScaled<T>, float, T>;
+      store_vec<Between, 4>(reinterpret_cast<Between *>(A.out) + at * A.ld_out + f, s);
       if (A.h != nullptr) {  // the block of what is kept, in the lanes' order
         float *h = A.h + ((int64_t)(pl.first / 16 + pl.expert + r0 / 16 + t) * ((A.F + 15) / 16) + ft) * 512 + lane * 4;
         store_vec<float, 4>(h, ga);
@@ -945,11 +989,99 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(Args A) {
 
 // ------------------------------------------------------ around the products --
 
-// y_t = sum over the token's assignments of w o (weight null: of o), and the gradient
+// Rows of `in` [rows][ld_in], `cols` (a multiple of 4) of each, rounded under a power of two for each row: a wave a
+// row, read twice (the second time from the caches).  Positions behind the last one kept are left out.  Bound by its
+// bytes; 1166 rows of 368: 4 us, the launch.
+__global__ __launch_bounds__(256) void scale_rows_kernel(const float *in, int64_t ld_in, int cols, f16_t *out,
+                                                         uint8_t *exps, const int32_t *offsets, int experts) {
+  const int64_t row = (int64_t)block_id() * 4 + (threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  if (row >= offsets[experts]) return;
+  const float *from = in + row * ld_in;
+  float m = 0.f;
+  for (int c = lane * 4; c < cols; c += 256) {
+    float x[4];
+    load_vec<float, 4>(from + c, x);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m = fmaxf(m, finite(x[i]));
+  }
+  const int e = exponent(group_max<64>(m));
+  for (int c = lane * 4; c < cols; c += 256) {
+    float x[4];
+    load_vec<float, 4>(from + c, x);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = scale_down(x[i], e);
+    store_vec<f16_t, 4>(out + row * cols + c, x);
+  }
+  if (lane == 0) exps[row] = (uint8_t)e;
+}
+
+// The same for each column of an expert's rows.  A workgroup takes 64 columns (blockIdx.x) of an expert
+// (blockIdx.y) and the blockIdx.z-th part of its rows; with more than one part their largest magnitudes come from a
+// launch before (ROUND false), part [parts][experts][cols].  Bound by its bytes, where there are few rows by two
+// rounds of loads (7 experts of about 170 rows, 1104 columns: 10 us, 256 threads 16).
+constexpr int kColThreads = 1024;
+template <bool ROUND>
+__global__ __launch_bounds__(kColThreads) void scale_cols_kernel(const float *in, int cols, f16_t *out, uint8_t *exps, float *part,
+                                                         const int32_t *offsets) {
+  constexpr int kRows = kColThreads / 16;
+  __shared__ float most[kColThreads / 64][64];
+  const int x = threadIdx.x & 15, y = threadIdx.x >> 4, c = blockIdx.x * 64 + x * 4, e = blockIdx.y;
+  const int lo = offsets[e], hi = offsets[e + 1], parts = gridDim.z, each = (hi - lo + parts - 1) / parts;
+  const int64_t from = lo + (int64_t)blockIdx.z * each, to = min(from + each, (int64_t)hi);
+  float m[4] = {0.f, 0.f, 0.f, 0.f};
+  if (!ROUND || parts == 1) {
+    if (c < cols)
+#pragma unroll 4
+      for (int64_t r = from + y; r < to; r += kRows) {
+        float v[4];
+        load_vec<float, 4>(in + r * cols + c, v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m[i] = fmaxf(m[i], finite(v[i]));
+      }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {  // a wave holds four rows of threads
+      m[i] = fmaxf(m[i], __shfl_xor(m[i], 16, 64));
+      most[y >> 2][x * 4 + i] = fmaxf(m[i], __shfl_xor(m[i], 32, 64));
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      for (int k = 0; k < kColThreads / 64; ++k) m[i] = fmaxf(m[i], most[k][x * 4 + i]);
+  } else if (c < cols) {
+    for (int z = 0; z < parts; ++z) {
+      float v[4];
+      load_vec<float, 4>(part + ((int64_t)z * gridDim.y + e) * cols + c, v);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) m[i] = fmaxf(m[i], v[i]);
+    }
+  }
+  if (c >= cols) return;
+  if constexpr (!ROUND) {
+    if (y == 0) store_vec<float, 4>(part + ((int64_t)blockIdx.z * gridDim.y + e) * cols + c, m);
+  } else {
+    int by[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) by[i] = exponent(m[i]);
+    if (y == 0 && blockIdx.z == 0)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) exps[(int64_t)e * cols + c + i] = (uint8_t)by[i];
+#pragma unroll 4
+    for (int64_t r = from + y; r < to; r += kRows) {
+      float v[4];
+      load_vec<float, 4>(in + r * cols + c, v);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = scale_down(v[i], by[i]);
+      store_vec<f16_t, 4>(out + r * cols + c, v);
+    }
+  }
+}
+
+// y_t = sum over the token's assignments of w o (weight null: of o; exps: of the operand's rows, where it was scaled), and the gradient
 // of the weights from the feature tiles' sums.  Bound by the bytes of o: 8 entries a load.
 // (65536 outputs of 4096: 247 us, 4.9 TB/s.)
 template <typename T>
-__global__ __launch_bounds__(256) void combine_kernel(Outputs o, const float *weight, const int32_t *slot, int64_t n_tokens,
+__global__ __launch_bounds__(256) void combine_kernel(Outputs o, const uint8_t *exps, const float *weight, const int32_t *slot, int64_t n_tokens,
                                                       int per_token, int H, T *y, const float *dot, int nt, float *dweight) {
   const int64_t t = block_id();
   if (t >= n_tokens) return;
@@ -972,6 +1104,11 @@ __global__ __launch_bounds__(256) void combine_kernel(Outputs o, const float *we
     const float w = weight ? weight[t * per_token + q] : 1.f;
     float x[8];
     load_vec<float, 8>(o.out + a * o.ld + c, x);
+    if constexpr (kScaled<T>) {
+      const int e = exps[a];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = scale_up(x[i], e);
+    }
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] += w * x[i];
   }
@@ -1022,9 +1159,12 @@ inline int64_t up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
 // 16 bytes are made for the call.
 struct Region {
   size_t x = 0, dy = 0, w1 = 0, w2 = 0;  // copies
-  size_t act = 0;                         // s, or w s backwards [A][Fp]
+  size_t act = 0;                         // s, or w s backwards [A][Fp]; scaled, backwards: [dg du w s] by columns [A][3 Fp]
   size_t out = 0;                         // o, or the rows of dx [A][Hp] float
   size_t dgu = 0;                         // [A][2 Fp]
+  size_t wide = 0;                        // scaled: s, or [dg du w s], float [A][Fp] or [A][3 Fp]
+  size_t exps = 0, col_exps = 0;          // and the exponents of rows [A] and of columns [E][3 Fp]
+  size_t part = 0;                        // [parts][E][3 Fp] float
   size_t dot = 0;                         // [A][feature tiles]
   size_t total = 0;
 };
@@ -1032,6 +1172,11 @@ struct Region {
 bool on16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
 constexpr int kMinFeatTile = 128;
+
+// Parts that an expert's rows are taken in by scale_cols_kernel, of 512 in the mean.
+int column_parts(const cfp_experts_desc &d) {
+  return (int)std::min<int64_t>(64, std::max<int64_t>(1, d.n_tokens * d.k / (d.n_experts * (int64_t)512)));
+}
 
 Region region(const cfp_experts_desc &d, bool bwd, bool pad_x, bool pad_dy, bool pad_w1, bool pad_w2) {
   const size_t A = (size_t)d.n_tokens * d.k, Hp = up(d.hidden, 8), Fp = up(d.inner, 8), E = d.n_experts;
@@ -1046,7 +1191,13 @@ Region region(const cfp_experts_desc &d, bool bwd, bool pad_x, bool pad_dy, bool
   if (pad_dy) r.dy = take((size_t)d.n_tokens * Hp * 2);
   if (pad_w1) r.w1 = take(E * 2 * Fp * Hp * 2);
   if (pad_w2) r.w2 = take(E * d.hidden * Fp * 2);
-  r.act = take(A * Fp * 2);
+  const bool scaled = d.dtype == CFP_DT_F16;
+  r.act = take(A * Fp * (scaled && bwd ? 6 : 2));
+  if (scaled) r.wide = take(A * Fp * (bwd ? 12 : 4)), r.exps = take(A);
+  if (scaled && bwd) {
+    r.col_exps = take(E * 3 * Fp);
+    if (column_parts(d) > 1) r.part = take((size_t)column_parts(d) * E * 3 * Fp * 4);
+  }
   r.out = take(A * Hp * 4);
   if (bwd) {
     r.dgu = take(A * 2 * Fp * 2);
@@ -1186,11 +1337,11 @@ Outputs outputs_of(const cfp_experts_desc &d, const Region &r, uint8_t *ws) {
 }
 
 template <typename T>
-hipError_t combine(const cfp_experts_desc &d, const Outputs &o, const float *weight, void *y, const float *dot, int nt,
+hipError_t combine(const cfp_experts_desc &d, const Outputs &o, const uint8_t *exps, const float *weight, void *y, const float *dot, int nt,
                    float *dweight, hipStream_t st) {
   dim3 grid = grid_of(d.n_tokens);
   grid.z = (d.hidden + 2047) / 2048;
-  combine_kernel<T><<<grid, 256, 0, st>>>(o, weight, d.slot, d.n_tokens, d.k, d.hidden, static_cast<T *>(y), dot, nt, dweight);
+  combine_kernel<T><<<grid, 256, 0, st>>>(o, exps, weight, d.slot, d.n_tokens, d.k, d.hidden, static_cast<T *>(y), dot, nt, dweight);
   return hipGetLastError();
 }
 
@@ -1223,6 +1374,26 @@ Laid lay_out(const cfp_experts_desc &d, const void *dy, int64_t dy_stride, const
   return L;
 }
 
+// The first `cols` of the ld entries of the wide rows, under a power of two for each row, to `out` [A][cols].
+hipError_t scale_rows(const cfp_experts_desc &d, const Region &r, uint8_t *ws, int64_t ld, int64_t cols, void *out,
+                      hipStream_t st) {
+  scale_rows_kernel<<<grid_of((d.n_tokens * d.k + 3) / 4), 256, 0, st>>>(
+      reinterpret_cast<const float *>(ws + r.wide), ld, (int)cols, static_cast<f16_t *>(out), ws + r.exps, d.offsets,
+      d.n_experts);
+  return hipGetLastError();
+}
+
+// All 3 Fp columns of the wide rows, under a power of two for each column of an expert, to r.act.
+hipError_t scale_cols(const cfp_experts_desc &d, const Region &r, uint8_t *ws, int64_t cols, hipStream_t st) {
+  const dim3 grid((unsigned)((cols + 63) / 64), d.n_experts, column_parts(d));
+  const float *in = reinterpret_cast<const float *>(ws + r.wide);
+  f16_t *out = reinterpret_cast<f16_t *>(ws + r.act);
+  float *part = reinterpret_cast<float *>(ws + r.part);
+  if (grid.z > 1) scale_cols_kernel<false><<<grid, kColThreads, 0, st>>>(in, (int)cols, out, ws + r.col_exps, part, d.offsets);
+  scale_cols_kernel<true><<<grid, kColThreads, 0, st>>>(in, (int)cols, out, ws + r.col_exps, part, d.offsets);
+  return hipGetLastError();
+}
+
 template <typename T>
 hipError_t forward(const cfp_experts_desc &d, void *y, float *h, uint8_t *ws, hipStream_t st) {
   const int64_t n = d.n_tokens * d.k;
@@ -1233,15 +1404,16 @@ hipError_t forward(const cfp_experts_desc &d, void *y, float *h, uint8_t *ws, hi
   const int64_t H = small ? d.hidden : L.Hp, F = small ? d.inner : L.Fp;  // widths of the weights' rows
   Args A = base_args(d);
   A.row = L.x, A.ld_row = L.ld_x, A.feat = L.w1, A.ld_feat = H * 2, A.feat_expert = 2 * F * H * 2;
-  A.K = (int)H, A.n_feat = d.inner, A.out = ws + r.act, A.ld_out = L.Fp, A.h = h;
+  A.K = (int)H, A.n_feat = d.inner, A.out = ws + (kScaled<T> ? r.wide : r.act), A.ld_out = L.Fp, A.h = h;
   hipError_t e = small ? few<T, kUp>(A, n, st) : product<T, kUp>(A, n, st);
+  if (e == hipSuccess && kScaled<T>) e = scale_rows(d, r, ws, L.Fp, L.Fp, ws + r.act, st);
   if (e != hipSuccess) return e;
   A = base_args(d);
   A.row = reinterpret_cast<const char *>(ws + r.act), A.ld_row = L.Fp * 2;
   A.feat = L.w2, A.ld_feat = F * 2, A.feat_expert = (int64_t)d.hidden * F * 2;
   A.K = (int)F, A.n_feat = d.hidden, A.outputs = outputs_of(d, r, ws);
   if ((e = small ? few<T, kDown>(A, n, st) : product<T, kDown>(A, n, st)) != hipSuccess) return e;
-  return combine<T>(d, A.outputs, d.weight, y, nullptr, 0, nullptr, st);
+  return combine<T>(d, A.outputs, ws + r.exps, d.weight, y, nullptr, 0, nullptr, st);
 }
 
 template <typename T>
@@ -1259,25 +1431,36 @@ hipError_t backward(const cfp_experts_desc &d, const void *dy, int64_t dy_stride
   if (n > 0) {
     // p = dy W2, and what follows from it
     A.row = L.dy, A.ld_row = L.ld_dy, A.feat = L.w2, A.ld_feat = L.Fp * 2, A.feat_expert = (int64_t)d.hidden * L.Fp * 2;
-    A.K = d.hidden, A.n_feat = (int)L.Fp, A.h = const_cast<float *>(h), A.out = ws + r.dgu, A.ld_out = 2 * L.Fp;
-    A.out2 = ws + r.act, A.dot = reinterpret_cast<float *>(ws + r.dot);
+    A.K = d.hidden, A.n_feat = (int)L.Fp, A.h = const_cast<float *>(h);
+    if constexpr (kScaled<T>) {
+      A.out = ws + r.wide, A.ld_out = A.ld_out2 = 3 * L.Fp, A.out2 = ws + r.wide + 2 * L.Fp * sizeof(float);
+    } else {
+      A.out = ws + r.dgu, A.ld_out = 2 * L.Fp, A.out2 = ws + r.act, A.ld_out2 = L.Fp;
+    }
+    A.dot = reinterpret_cast<float *>(ws + r.dot);
     const int dot_tile = tile_of(kBackUp, A, n).feats;
     A.dot_tiles = dots = (int)((L.Fp + dot_tile - 1) / dot_tile);
     if ((e = product<T, kBackUp>(A, n, st)) != hipSuccess) return e;
+    if constexpr (kScaled<T>) {
+      if ((e = scale_rows(d, r, ws, 3 * L.Fp, 2 * L.Fp, ws + r.dgu, st)) != hipSuccess) return e;
+      if ((e = scale_cols(d, r, ws, 3 * L.Fp, st)) != hipSuccess) return e;
+    }
   }
   Args X = base_args(d);  // rows of dx
   X.row = reinterpret_cast<const char *>(ws + r.dgu), X.ld_row = 2 * L.Fp * 2;
   X.feat = L.w1, X.ld_feat = L.Hp * 2, X.feat_expert = 2 * L.Fp * L.Hp * 2;
   X.K = (int)(2 * L.Fp), X.n_feat = (int)L.Hp, X.outputs = outputs_of(d, r, ws);
-  Args W1 = base_args(d);  // dW1 = [dg du]^T x
-  W1.row = reinterpret_cast<const char *>(ws + r.dgu), W1.ld_row = 2 * L.Fp * 2, W1.n_row = (int)(2 * L.Fp);
+  Args W1 = base_args(d), W2 = W1;  // dW1 = [dg du]^T x
+  W1.row = reinterpret_cast<const char *>(ws + (kScaled<T> ? r.act : r.dgu)), W1.ld_row = (kScaled<T> ? 3 : 2) * L.Fp * 2;
+  W1.exps = W2.exps = ws + r.col_exps, W1.n_row = (int)(2 * L.Fp);
   W1.feat = L.x, W1.ld_feat = L.ld_x, W1.n_feat = d.hidden, W1.out = dw1, W1.ld_out = d.hidden;
-  Args W2 = base_args(d);  // dW2 = dy^T (w s)
+  // dW2 = dy^T (w s)
   W2.row = L.dy, W2.ld_row = L.ld_dy, W2.n_row = d.hidden;
-  W2.feat = reinterpret_cast<const char *>(ws + r.act), W2.ld_feat = L.Fp * 2, W2.n_feat = d.inner, W2.out = dw2;
+  W2.feat = reinterpret_cast<const char *>(ws + r.act + (kScaled<T> ? 2 * L.Fp * 2 : 0));
+  W2.ld_feat = (kScaled<T> ? 3 : 1) * L.Fp * 2, W2.n_feat = d.inner, W2.out = dw2;
   W2.ld_out = d.inner;
   if ((e = gradients<T>(X, W1, W2, n, st)) != hipSuccess || n == 0) return e;
-  return combine<T>(d, outputs_of(d, r, ws), nullptr, dx,
+  return combine<T>(d, outputs_of(d, r, ws), ws + r.exps, nullptr, dx,
                     reinterpret_cast<const float *>(ws + r.dot), dots, dweight, st);
 }
 

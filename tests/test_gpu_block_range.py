@@ -79,3 +79,49 @@ def test_activation_at_any_gate(T):
     dweight = results(x16, w1.bfloat16(), w2.bfloat16(), weight, idx, dy.bfloat16())[4][:, 0].double()
     want = gate.double() * torch.sigmoid(gate.double())
     assert bool(((dweight - want).abs() <= 2.0 ** -21 * want.abs() + 2.0 ** -116).all()), float(((dweight - want) / want).abs().nan_to_num().max())
+
+
+HALF = [  # scales of x, w1, w2, dy and the weights
+    dict(x=2.0 ** 4, w1=2.0 ** 4, w2=2.0 ** -8, dy=2.0 ** -10),                        # s above 65504
+    dict(x=2.0 ** -8, w2=2.0 ** 8),                                                    # s below 2^-14
+    dict(x=2.0 ** 10, w1=2.0 ** -4, w2=2.0 ** -3, dy=2.0 ** 12),                       # the gradients of gate and up above 65504
+    dict(x=2.0 ** -9, w1=2.0 ** 9, dy=2.0 ** -9, weight=2.0 ** -12),                   # and below 2^-14
+    dict(x=2.0 ** -4, w1=2.0 ** -1, w2=2.0 ** -4, dy=2.0 ** 6, weight=2.0 ** -14),     # w s below 2^-14
+]
+
+
+@pytest.mark.parametrize("scales", range(len(HALF)))
+@pytest.mark.parametrize("T,H,F,E,k", SIZES)
+def test_float16_between_the_products(T, H, F, E, k, scales):
+    """float16 inputs and results in range, what lies between them not."""
+    say("float16", T, H, F, E, k, HALF[scales])
+    args = inputs(T, H, F, E, k, torch.float16, **HALF[scales])
+    want = formulas(*(t.double() for t in args[:4]), args[4], args[5].double())
+    u = U[torch.float16]
+    for name, a, b in zip(("y", "dx", "dw1", "dw2", "dweight"), results(*args), want):
+        if name == "dweight":
+            near_product(a, b.cpu(), 2.0 ** -16, name)
+            continue
+        step, rms = 2.0 ** -25, b.square().mean().sqrt()
+        entry = 20 * u * torch.maximum(b.abs(), rms) + step
+        # a result of float16 ends at 65504: infinite where it is past it by more than the bound
+        fits, past = b.abs() + entry < 65504, b.abs() - entry > 65520
+        assert bool(a[past].isinf().all()), name
+        off = (a.double() - b).abs()
+        assert bool((off <= entry)[fits].all()), (name, float(off[fits].max()), float(rms))
+        assert name not in ("y", "dx") or bool(fits.all()), name
+        if bool(fits.all()):
+            assert float(off.norm()) <= 1.5 * u * float(b.norm()) + step * math.sqrt(b.numel()), (name, float(off.norm() / b.norm()))
+
+
+def test_float16_tokens_of_other_magnitudes():
+    """A token's results do not depend on how large the other tokens of its expert are."""
+    args = list(inputs(150, 96, 72, 2, 1, torch.float16, x=2.0 ** -6, w1=2.0 ** 6))
+    small = results(*args)
+    large = torch.arange(150, device="cuda") % 3 == 0
+    args[0], args[5] = args[0].clone(), args[5].clone()
+    args[0][large] *= 2.0 ** 9
+    args[5][large] *= 2.0 ** 6
+    both = results(*args)
+    for a, b in zip((small[0], small[1], small[4]), (both[0], both[1], both[4])):
+        assert torch.equal(a[~large], b[~large])
