@@ -346,8 +346,12 @@ bool rows_aligned(const cfp_route_desc &d, int npl, const void *out) {
 constexpr int kPlanWaves = 8;
 constexpr int kPlanThreads = kPlanWaves * 64;
 constexpr int kPlanParts = 8;      // threads that share a bin's counts of the pieces
-// Assignments of a workgroup: one takes up to 4096, which saves the counting launch.
-inline int plan_piece(int64_t n) { return n <= 4096 ? 4096 : 2048; }
+// Assignments of a workgroup: one takes up to 4096, which saves the counting launch.  Every workgroup reads all
+// pieces' counts, so above kPlanPieces of 2048 the pieces grow and not their number.
+constexpr int kPlanPieces = 512;
+inline int plan_piece(int64_t n) {
+  return n <= 4096 ? 4096 : (int)std::max<int64_t>(2048, (n + kPlanPieces - 1) / kPlanPieces);
+}
 
 struct PlanArgs {
   const int32_t *index;
