@@ -147,11 +147,13 @@ def _rows(name, t):
     return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
-def _ws(torch, nbytes, device, ws):
+def _ws(torch, nbytes, device, ws, align=16):
     if ws is None:
         return torch.empty(max(nbytes, 1), dtype=torch.uint8, device=device)
-    if ws.dtype != torch.uint8 or not ws.is_contiguous() or ws.device != device:
+    if not isinstance(ws, torch.Tensor) or ws.dtype != torch.uint8 or not ws.is_contiguous() or ws.device != device:
         raise TypeError("ws must be a contiguous uint8 tensor on the tensors' device")
+    if ws.data_ptr() % align:
+        raise ValueError(f"ws must start on {align} bytes")
     return ws
 
 
@@ -256,7 +258,7 @@ def qk_norm_rope_bwd(dyq, dyk, q, k, wq, wk, cos, sin, positions=None, *, eps=1e
         dq, dk = _like(torch, q), _like(torch, k)
         dwq = torch.empty(q.shape[2], dtype=torch.float32, device=q.device) if wq is not None else None
         dwk = torch.empty(q.shape[2], dtype=torch.float32, device=q.device) if wk is not None else None
-        ws = _ws(torch, _lib.cfp_qk_workspace_bytes(d), q.device, ws)
+        ws = _ws(torch, _lib.cfp_qk_workspace_bytes(d), q.device, ws, 4)
         _check("cfp_qk_norm_rope_bwd", _lib.cfp_qk_norm_rope_bwd(
             d, dyq.data_ptr(), dyq.stride(0), dyq.stride(1), dyk.data_ptr(), dyk.stride(0), dyk.stride(1),
             dq.data_ptr(), dk.data_ptr(), _ptr(dwq), _ptr(dwk), ws.data_ptr(), ws.numel(), _raw(torch, q.device)))
@@ -444,9 +446,13 @@ def experts_bwd(dy, x, w1, w2, weight, plan, kept, *, ws=None, stream=None):
     _tensor("dy", dy, torch, (x.dtype,), 2)
     if dy.shape != x.shape:
         raise ValueError("dy must have the shape of x")
-    _same_device(x, dy, kept)
-    if kept.dtype != torch.uint8 or kept.numel() < _lib.cfp_experts_kept_bytes(d) or not kept.is_contiguous():
+    _same_device(x, dy)
+    if not isinstance(kept, torch.Tensor) or kept.dtype != torch.uint8:
+        raise TypeError("kept must be what experts returned")
+    if kept.device != x.device or not kept.is_contiguous() or kept.numel() < _lib.cfp_experts_kept_bytes(d):
         raise ValueError("kept is not what experts returned for these sizes")
+    if kept.data_ptr() % 16:
+        raise ValueError("kept must start on 16 bytes")
     with _on(torch, x.device, stream):
         dx, dw1, dw2 = _like(torch, x), torch.empty_like(w1), torch.empty_like(w2)
         dweight = torch.empty_like(weight)

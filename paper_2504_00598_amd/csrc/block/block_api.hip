@@ -9,6 +9,8 @@ constexpr int64_t kMaxTokens = (int64_t)1 << 31;  // counts of rows and of assig
 
 bool dtype_ok(int t) { return t == CFP_DT_F32 || t == CFP_DT_F16 || t == CFP_DT_BF16; }
 
+bool on(const void *p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+
 int status(hipError_t e) { return e == hipSuccess ? CFP_OK : CFP_ERR_HIP; }
 
 int check_qk(const cfp_qk_desc *d) {
@@ -85,6 +87,7 @@ int cfp_qk_norm_rope_bwd(const cfp_qk_desc *d, const void *dyq, int64_t dyq_toke
   if (!none && ((d->n_q && (!dyq || !dq)) || (d->n_k && (!dyk || !dk)))) return CFP_ERR_ARG;
   const size_t need = cfp_qk_workspace_bytes(d);
   if (need && (!ws || ws_bytes < need)) return CFP_ERR_WORKSPACE;
+  if (need && !on(ws, 4)) return CFP_ERR_ARG;
   return status(launch_qk_bwd(*d, dyq, dyk, {dyq_token_stride, dyq_head_stride}, {dyk_token_stride, dyk_head_stride}, dq,
                               dk, dwq, dwk, (float *)ws, (hipStream_t)stream));
 }
@@ -113,6 +116,7 @@ int cfp_expert_plan(const cfp_plan_desc *d, int32_t *offsets, int32_t *rows, int
   if (!offsets || !rows || (d->n_tokens > 0 && !slot)) return CFP_ERR_ARG;
   const size_t need = plan_bytes(d->n_tokens * d->k, d->n_experts);
   if (need && (!ws || ws_bytes < need)) return CFP_ERR_WORKSPACE;
+  if (need && !on(ws, 4)) return CFP_ERR_ARG;
   return status(launch_expert_plan(*d, offsets, rows, slot, (int32_t *)ws, (hipStream_t)stream));
 }
 
@@ -129,6 +133,7 @@ int cfp_experts(const cfp_experts_desc *d, void *y, void *kept, void *ws, size_t
   if (d->n_tokens == 0) return CFP_OK;
   if (!y) return CFP_ERR_ARG;
   if (!ws || ws_bytes < experts_bytes(*d, false)) return CFP_ERR_WORKSPACE;
+  if (!on(ws, 16) || !on(kept, 16)) return CFP_ERR_ARG;
   return status(launch_experts(*d, y, (float *)kept, (uint8_t *)ws, (hipStream_t)stream));
 }
 
@@ -139,6 +144,7 @@ int cfp_experts_bwd(const cfp_experts_desc *d, const void *dy, int64_t dy_stride
   if (d->n_tokens > 0) {
     if (!dy || !kept || !dx || !dweight || (d->n_tokens > 1 && dy_stride < d->hidden)) return CFP_ERR_ARG;
     if (!ws || ws_bytes < experts_bytes(*d, true)) return CFP_ERR_WORKSPACE;
+    if (!on(ws, 16) || !on(kept, 16)) return CFP_ERR_ARG;
   }
   return status(launch_experts_bwd(*d, dy, dy_stride, (const float *)kept, dx, dw1, dw2, dweight, (uint8_t *)ws,
                                    (hipStream_t)stream));
