@@ -6,7 +6,8 @@
     plan = block.expert_plan(index, n_experts)
     y = block.experts(x, w1, w2, weight, plan)
 
-Each has its gradient beside it (`*_bwd`).  Argument marshalling only: the work is
+Each has its gradient beside it (`*_bwd`), and where gradients are recorded and an input requires one, backward()
+reaches it through that (block_grad).  What a `*_bwd` returns has no gradient of its own.  Argument marshalling only: the work is
 the HIP kernels' behind the C ABI of include/cfp_block.h, enqueued on the current
 stream or on `stream`; nothing synchronises.  Results and workspaces are allocated
 for the stream that the work runs on.
@@ -161,6 +162,15 @@ def _like(torch, t):
     return torch.empty_like(t, memory_format=torch.contiguous_format)
 
 
+def _recorded(torch, *inputs):
+    """Whether backward() has to reach one of the inputs through this call."""
+    if torch.is_grad_enabled():
+        for t in inputs:
+            if t is not None and t.requires_grad:
+                return True
+    return False
+
+
 def _ptr(t):
     return 0 if t is None else t.data_ptr()
 
@@ -235,6 +245,10 @@ def qk_norm_rope(q, k, wq, wk, cos, sin, positions=None, *, eps=1e-6, interleave
     the tables makes its rotated entries NaN.  Returns contiguous (q, k) of q's type."""
     torch = _torch()
     d = _qk_desc(q, k, wq, wk, cos, sin, positions, eps, interleaved, torch)
+    if _recorded(torch, q, k, wq, wk, cos, sin):
+        from . import block_grad
+        with _on(torch, q.device, stream):
+            return block_grad.qk_norm_rope(q, k, wq, wk, cos, sin, positions, eps, interleaved)
     with _on(torch, q.device, stream):
         yq, yk = _like(torch, q), _like(torch, k)
         rc = _lib.cfp_qk_norm_rope(d, yq.data_ptr(), yk.data_ptr(), _raw(torch, q.device))
@@ -298,6 +312,12 @@ def route(logits, k, *, score="softmax", bias=None, groups=1, top_groups=1, grou
     torch = _torch()
     d = _route_desc(logits, k, score, bias, groups, top_groups, group_score, renormalise, scale, torch)
     device = logits.device
+    if _recorded(torch, logits):
+        from . import block_grad
+        with _on(torch, device, stream):
+            return block_grad.route(logits, k, {"bias": bias, "groups": groups, "top_groups": top_groups,
+                                                "group_score": group_score},
+                                    {"score": score, "renormalise": renormalise, "scale": scale})
     with _on(torch, device, stream):
         weight = torch.empty((logits.shape[0], k), dtype=torch.float32, device=device)
         index = torch.empty((logits.shape[0], k), dtype=torch.int32, device=device)
@@ -425,9 +445,14 @@ def experts(x, w1, w2, weight, plan, *, keep=False, ws=None, stream=None):
 
     x [T][hidden] (rows may lie apart), w1 [experts][2 * inner][hidden] (gate rows, then
     up rows), w2 [experts][hidden][inner], float16 or bfloat16; weight [T][k] float32.  A token
-    without assignments gets zeros.  With `keep` returns (y, kept): kept is what experts_bwd needs."""
+    without assignments gets zeros.  With `keep` returns (y, kept): kept is what experts_bwd needs, and is kept as well
+    where gradients are recorded."""
     torch = _torch()
     d = _experts_desc(x, w1, w2, weight, plan, torch)
+    if _recorded(torch, x, w1, w2, weight):
+        from . import block_grad
+        with _on(torch, x.device, stream):
+            return block_grad.experts(x, w1, w2, weight, plan, keep, ws)
     with _on(torch, x.device, stream):
         y = _like(torch, x)
         ws = _ws(torch, _lib.cfp_experts_workspace_bytes(d, 0), x.device, ws)
