@@ -78,7 +78,7 @@ typedef struct {
   int32_t k;                  /* experts of a token, 1 .. min(n_experts, CFP_ROUTE_MAX_K) */
   int32_t score;              /* CFP_SCORE_* */
   int32_t groups, top_groups; /* equal consecutive groups, of which top_groups stay (1, 1: none) */
-  int32_t group_score;        /* CFP_GROUP_*: a group's largest value, or the sum of its two largest */
+  int32_t group_score;        /* CFP_GROUP_*: a group's largest value, or the sum of the two largest of its scores + bias */
   int32_t renormalise;        /* weights over their sum */
   int32_t dtype;              /* of the logits */
   float scale;                /* of the weights */

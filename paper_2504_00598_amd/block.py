@@ -305,7 +305,7 @@ def route(logits, k, *, score="softmax", bias=None, groups=1, top_groups=1, grou
     logits [T][experts] (rows may lie apart).  score "softmax" or "sigmoid"; `bias`
     [experts] float32 is added to the scores for the choice alone.  With groups > top_groups
     only the experts of the `top_groups` best of `groups` equal runs take part (a run's largest
-    value, or with group_score "top2" the sum of its two largest).  Weights are the scores, over
+    value, or with group_score "top2" the sum of its two largest scores, each with its bias).  Weights are the scores, over
     their sum with `renormalise`, times `scale`.  Returns (weight [T][k] float32, index [T][k]
     int32), best first, equal values by the lowest index.  A logit of -inf masks its expert;
     a place with no expert left has index -1 and weight 0."""

@@ -4,9 +4,9 @@
 // Routing.  For a token's logits l: scores s = softmax(l) or 1 / (1 + exp(-l)),
 // selection values v = s + bias, or l itself without a bias (scores grow with
 // their logit, so the order is the same and no rounding of s takes part in it).
-// With groups, the values of the consecutive groups (their largest v, or the sum
-// of their two largest) pick the groups that stay.  The k largest v are taken,
-// equal ones by the lowest index; w = s of each, over their sum if asked, times
+// With groups, the values of the consecutive groups (their largest v, or the sum of their
+// two largest s + bias, of the scores themselves without a bias: sums of logits would be in another
+// order) pick the groups that stay.  The k largest v are taken, equal ones by the lowest index; w = s of each, over their sum if asked, times
 // the scale.  An expert whose logit is -inf is never taken; a place with none left
 // holds index -1 and weight 0.
 // A group of G lanes holds a token's values in registers, NPL consecutive ones
