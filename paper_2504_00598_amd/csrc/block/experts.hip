@@ -19,13 +19,13 @@
 //
 // Measured, bfloat16, rates of the products alone (the card's library reaches 1.5 to 1.6 PFLOP/s on one large
 // product of rows by rows, 1.0 to 1.4 where an operand is transposed):
-//     16384 tokens to 4 of 32 experts, 4096 wide, 1536 inside: up 1520 us (1.08 PFLOP/s), down 880 (0.94),
-//     p = dy W2 1080 (0.76), rows of dx 1559 (1.06), dW1 1588 (1.04), dW2 838 us (0.98);
-//     16384 tokens to 8 of 64, 2048 wide, 768 inside: up 720 us (1.15), down 568 (0.73);
-//     4096 tokens to 2 of 16, 2048 wide, 1536 inside: 148, 100, 109, 185, 179 and 100 us (0.5 to 0.7).
-// The large ones are bound by the copies into LDS: those of the first up alone, without its matrix instructions, took
-// 1508 us (9.1 TB/s from the caches), the matrix instructions alone 1145.  The small ones have fewer tiles than
-// the chip takes at a time, or not many more.
+//     16384 tokens to 4 of 32 experts, 4096 wide, 1536 inside: up 1580 us (1.04 PFLOP/s), down 973 (0.85),
+//     p = dy W2 1089 (0.76), rows of dx 1629 (1.01), dW1 1645 (1.00), dW2 853 us (0.97);
+//     16384 tokens to 8 of 64, 2048 wide, 768 inside: up 820 us (1.01), down 626 (0.66);
+//     4096 tokens to 2 of 16, 2048 wide, 1536 inside: 159, 105, 115, 193, 193 and 106 us (0.4 to 0.6).
+// The large ones wait for the copies of a stage, which are issued when the stage before has landed; how much of that
+// more copies on their way would hide has not been measured.  Down and the rows of dx also write their sums in 32
+// bits.  The small ones have fewer tiles than the chip takes at a time, or not many more.
 #include <algorithm>
 #include <type_traits>
 
@@ -607,8 +607,9 @@ __device__ __forceinline__ void product_tile(const Args &A, uint32_t block) {
   // ---- epilogues: lane (j, g) holds features 4 g .. 4 g + 3 of row j of each 16 x 16 block.  Stores of
   // such pieces touch 16 lines each and took 60 cycles apiece, half of the 31 thousand cycles of a weight gradient's
   // tile of two stages.  So 16-bit results pass through LDS, a part of its own for each wave, and leave in whole
-  // rows of that; what is kept in 32 bits is laid out by blocks in the lanes' order.  (4096 tokens to 2 of 16
-  // experts, 2048 wide, 1536 inside, tiles of 256 x 256: dW1 from 185 to 170 us, dW2 from 105 to 97 us.)
+  // rows of that (4096 tokens to 2 of 16 experts, 2048 wide, 1536 inside, tiles of 256 x 256: dW1 from 185 to 170 us,
+  // dW2 from 105 to 97 us); what is kept in 32 bits is laid out by blocks in the lanes' order, and other results in 32
+  // bits go out as 64 bytes of each row.
   const int width = P == kUp || P == kBackUp ? A.F : P == kDown || P == kBackDown ? (int)A.outputs.ld : (int)A.ld_out;
   const bool inside = f0 + kFeatTile <= width && r0 + BR <= n_rows && (P != kGradW1 || A.F == A.Fp);
   constexpr int kCols = P == kUp ? TF / 2 : TF, kPieces = kCols / 8;  // a wave's results of a row
@@ -840,7 +841,7 @@ __global__ __launch_bounds__(256, 3) void gradients_kernel(Args dx, Args dw1, Ar
 // matrix instructions take them from, kMost steps of 2 KiB a wave ahead, and only the four partial
 // sums meet in LDS.  Rows need no alignment (a piece of 8 entries is one load of 16 bytes at any
 // address), so odd widths are read in place.
-// 384 assignments to 64 experts, 2048 wide, 1024 inside: up 104 us (5.2 TB/s), down 60 us (4.5 TB/s); one token to 6:
+// 384 assignments to 64 experts, 2048 wide, 1024 inside: up 100 us (5.4 TB/s), down 57 us (4.7 TB/s); one token to 6:
 // 14 and 8 us, bound by the latency of a launch and two or three rounds of loads.  Twice the steps on their way
 // leaves half the waves: 110 and 68 us.
 
@@ -1022,8 +1023,8 @@ __global__ __launch_bounds__(256) void scale_rows_kernel(const float *in, int64_
 // rounds of loads (7 experts of about 170 rows, 1104 columns: 10 us, 256 threads 16).
 constexpr int kColThreads = 1024;
 template <bool ROUND>
-__global__ __launch_bounds__(kColThreads) void scale_cols_kernel(const float *in, int cols, f16_t *out, uint8_t *exps, float *part,
-                                                         const int32_t *offsets) {
+__global__ __launch_bounds__(kColThreads) void scale_cols_kernel(const float *in, int cols, f16_t *out, uint8_t *exps,
+                                                                 float *part, const int32_t *offsets) {
   constexpr int kRows = kColThreads / 16;
   __shared__ float most[kColThreads / 64][64];
   const int x = threadIdx.x & 15, y = threadIdx.x >> 4, c = blockIdx.x * 64 + x * 4, e = blockIdx.y;
@@ -1077,12 +1078,13 @@ __global__ __launch_bounds__(kColThreads) void scale_cols_kernel(const float *in
   }
 }
 
-// y_t = sum over the token's assignments of w o (weight null: of o; exps: of the operand's rows, where it was scaled), and the gradient
-// of the weights from the feature tiles' sums.  Bound by the bytes of o: 8 entries a load.
+// y_t = sum over the token's assignments of w o (weight null: of o; exps: of the rows that o was made from, where they
+// were scaled), and the gradient of the weights from the feature tiles' sums.  Bound by the bytes of o: 8 entries a load.
 // (65536 outputs of 4096: 247 us, 4.9 TB/s.)
 template <typename T>
-__global__ __launch_bounds__(256) void combine_kernel(Outputs o, const uint8_t *exps, const float *weight, const int32_t *slot, int64_t n_tokens,
-                                                      int per_token, int H, T *y, const float *dot, int nt, float *dweight) {
+__global__ __launch_bounds__(256) void combine_kernel(Outputs o, const uint8_t *exps, const float *weight,
+                                                      const int32_t *slot, int64_t n_tokens, int per_token, int H, T *y,
+                                                      const float *dot, int nt, float *dweight) {
   const int64_t t = block_id();
   if (t >= n_tokens) return;
   const int32_t *sl = slot + t * per_token;
@@ -1269,10 +1271,10 @@ hipError_t few(const Args &A, int64_t n_assign, hipStream_t st) {
 // The tile of a product, rows x features: the one of least time by a model of it, as the tiles that a compute unit
 // works through, and half of one more for the end, times a tile's fixed part and its stages.  Fitted to eleven
 // training steps of 180 to 81 thousand assignments; the tile it picks takes 1.02 times the best one's time in the mean.
-// (256 x 256 against 128 x 128 and 64 x 128: 32768 assignments of 8 experts, 2048 wide, 1408 inside, up 418, 536 and
-// 610 us; 16384 of 32, 1024 wide, 512 inside, up 87, 72 and 74 us; 1860 of 16, 536 wide, 1184 inside, down 41, 21 and
-// 18 us.)  p = dy W2 has no tile of 256 x 256, as its epilogue needs more registers than that leaves: 485, 340 and
-// 378 us in the first of these.
+// (256 x 256 against 128 x 128 and 64 x 128: 32768 assignments of 8 experts, 2048 wide, 1408 inside, up 456, 522 and
+// 577 us; 16384 of 32, 1024 wide, 512 inside, up 92, 75 and 74 us; 1860 of 16, 536 wide, 1184 inside, down 31, 20 and
+// 17 us.)  p = dy W2 has no tile of 256 x 256, as its epilogue needs more registers than that leaves: 485 us where 128 x
+// 128 took 340 in the first of these.
 struct Tile {
   int rows, feats;
 };
@@ -1301,8 +1303,8 @@ hipError_t product(const Args &A, int64_t n_assign, hipStream_t st) {
 
 // The three products that follow from p = dy W2: in one launch of 64 x 128 tiles up to kTogether workgroups of it,
 // else one by one in the tiles of each.  (Sum of the three against the one: 777 tokens to 7 of 12 experts, 1000 wide,
-// 364 inside, 1352 workgroups, 43 and 23 us; 6000 to 2 of 8, 1024 wide, 512 inside, 3096, 126 and 108 us; 1024 to 2 of
-// 16, 2048 wide, 512 inside, 6912, 74 and 68 us.  Above, tiles of 256 x 256 are worth more.)
+// 364 inside, 1352 workgroups, 48 and 28 us; 6000 to 2 of 8, 1024 wide, 512 inside, 3096, 129 and 111 us; 1024 to 2 of
+// 16, 2048 wide, 512 inside, 6912, 75 and 69 us.  Above, tiles of 256 x 256 are worth more.)
 constexpr int64_t kTogether = 8192;
 template <typename T>
 hipError_t gradients(Args dx, Args dw1, Args dw2, int64_t n_assign, hipStream_t st) {
@@ -1337,11 +1339,12 @@ Outputs outputs_of(const cfp_experts_desc &d, const Region &r, uint8_t *ws) {
 }
 
 template <typename T>
-hipError_t combine(const cfp_experts_desc &d, const Outputs &o, const uint8_t *exps, const float *weight, void *y, const float *dot, int nt,
-                   float *dweight, hipStream_t st) {
+hipError_t combine(const cfp_experts_desc &d, const Outputs &o, const uint8_t *exps, const float *weight, void *y,
+                   const float *dot, int nt, float *dweight, hipStream_t st) {
   dim3 grid = grid_of(d.n_tokens);
   grid.z = (d.hidden + 2047) / 2048;
-  combine_kernel<T><<<grid, 256, 0, st>>>(o, exps, weight, d.slot, d.n_tokens, d.k, d.hidden, static_cast<T *>(y), dot, nt, dweight);
+  combine_kernel<T><<<grid, 256, 0, st>>>(o, exps, weight, d.slot, d.n_tokens, d.k, d.hidden, static_cast<T *>(y), dot,
+                                          nt, dweight);
   return hipGetLastError();
 }
 
@@ -1389,8 +1392,9 @@ hipError_t scale_cols(const cfp_experts_desc &d, const Region &r, uint8_t *ws, i
   const float *in = reinterpret_cast<const float *>(ws + r.wide);
   f16_t *out = reinterpret_cast<f16_t *>(ws + r.act);
   float *part = reinterpret_cast<float *>(ws + r.part);
-  if (grid.z > 1) scale_cols_kernel<false><<<grid, kColThreads, 0, st>>>(in, (int)cols, out, ws + r.col_exps, part, d.offsets);
-  scale_cols_kernel<true><<<grid, kColThreads, 0, st>>>(in, (int)cols, out, ws + r.col_exps, part, d.offsets);
+  uint8_t *exps = ws + r.col_exps;
+  if (grid.z > 1) scale_cols_kernel<false><<<grid, kColThreads, 0, st>>>(in, (int)cols, out, exps, part, d.offsets);
+  scale_cols_kernel<true><<<grid, kColThreads, 0, st>>>(in, (int)cols, out, exps, part, d.offsets);
   return hipGetLastError();
 }
 

@@ -16,8 +16,8 @@
 // rotation stays inside a lane and only the sum of squares crosses lanes.  V is
 // the widest load that divides the halves and fits the alignment.
 //
-// Measured, bfloat16, 16384 tokens of 40 + 8 heads of 128: forward 86 us for 403 MB (4.7 TB/s; a copy reaches 5.2),
-// backward 129 us for 604 MB (4.7 TB/s) and 5 us for the sums of dg.  Four tokens: 4 us, the launch.
+// Measured, bfloat16, 16384 tokens of 40 + 8 heads of 128: forward 87 us for 403 MB (4.6 TB/s; a copy reaches 5.2),
+// backward 131 us for 604 MB (4.6 TB/s) and 5 us for the sums of dg.  Four tokens: 4 us, the launch.
 #include <algorithm>
 
 #include "block_common.h"
