@@ -248,7 +248,7 @@ def qk_norm_rope(q, k, wq, wk, cos, sin, positions=None, *, eps=1e-6, interleave
     if _recorded(torch, q, k, wq, wk, cos, sin):
         from . import block_grad
         with _on(torch, q.device, stream):
-            return block_grad.qk_norm_rope(q, k, wq, wk, cos, sin, positions, eps, interleaved)
+            return block_grad.qk_norm_rope(q, k, wq, wk, cos, sin, positions, eps, interleaved, stream)
     with _on(torch, q.device, stream):
         yq, yk = _like(torch, q), _like(torch, k)
         rc = _lib.cfp_qk_norm_rope(d, yq.data_ptr(), yk.data_ptr(), _raw(torch, q.device))
@@ -317,7 +317,7 @@ def route(logits, k, *, score="softmax", bias=None, groups=1, top_groups=1, grou
         with _on(torch, device, stream):
             return block_grad.route(logits, k, {"bias": bias, "groups": groups, "top_groups": top_groups,
                                                 "group_score": group_score},
-                                    {"score": score, "renormalise": renormalise, "scale": scale})
+                                    {"score": score, "renormalise": renormalise, "scale": scale}, stream)
     with _on(torch, device, stream):
         weight = torch.empty((logits.shape[0], k), dtype=torch.float32, device=device)
         index = torch.empty((logits.shape[0], k), dtype=torch.int32, device=device)
@@ -452,7 +452,7 @@ def experts(x, w1, w2, weight, plan, *, keep=False, ws=None, stream=None):
     if _recorded(torch, x, w1, w2, weight):
         from . import block_grad
         with _on(torch, x.device, stream):
-            return block_grad.experts(x, w1, w2, weight, plan, keep, ws)
+            return block_grad.experts(x, w1, w2, weight, plan, keep, ws, stream)
     with _on(torch, x.device, stream):
         y = _like(torch, x)
         ws = _ws(torch, _lib.cfp_experts_workspace_bytes(d, 0), x.device, ws)

@@ -3,7 +3,8 @@
 `block` calls these where gradients are recorded and one of the inputs requires one: the forward call and its
 `*_bwd`, tied together for backward().  A gradient that is asked for reaches q, k, wq and wk; logits; x, w1, w2
 and weight.  It has none of its own (a second derivative is refused).  Backward runs on the stream of the forward
-call, as torch does for its own functions.
+call, as torch does for its own functions.  The recorded program may hold the last reference to an input and drops it
+while that stream still reads it, so inputs of a call that names a stream are marked as used on it.
 """
 from __future__ import annotations
 
@@ -68,16 +69,26 @@ class Experts(Function):
         return (*block.experts_bwd(dy, *args, ctx.plan, kept), None, None)
 
 
-def qk_norm_rope(q, k, wq, wk, cos, sin, positions, eps, interleaved):
+def _used_on(stream, *tensors):
+    if stream is not None:
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+
+
+def qk_norm_rope(q, k, wq, wk, cos, sin, positions, eps, interleaved, stream):
     if cos.requires_grad or sin.requires_grad:
         raise ValueError("cos and sin have no gradient")
+    _used_on(stream, q, k, wq, wk, cos, sin, positions)
     return QkNormRope.apply(q, k, wq, wk, cos, sin, positions, eps, interleaved)
 
 
-def route(logits, k, choice, weights):
+def route(logits, k, choice, weights, stream):
+    _used_on(stream, logits, choice["bias"])
     return Route.apply(logits, k, choice, weights)
 
 
-def experts(x, w1, w2, weight, plan, keep, ws):
+def experts(x, w1, w2, weight, plan, keep, ws, stream):
+    _used_on(stream, x, w1, w2, weight, plan._buf, ws)
     y, kept = Experts.apply(x, w1, w2, weight, plan, ws)
     return (y, kept) if keep else y

@@ -86,3 +86,25 @@ def test_only_what_is_asked_for():
     assert torch.equal(dev[3].grad, want[3]) and dev[0].grad is None and dev[1].grad is None
     # an explicit call still takes inputs that require a gradient
     assert torch.equal(block.experts_bwd(ones, *dev, plan, kept)[1], want[1])
+
+
+def test_inputs_outlive_their_stream():
+    """What only the recorded program holds is not handed out again while the call's stream still reads it."""
+    from paper_2504_00598_amd import block
+    idx, _, dy, w1, w2, weight = expert_inputs(4096, 64, 48, 5, 0, 5, 2, torch.bfloat16)
+    w1, w2, dy, weight, idx = leaf(w1), leaf(w2), dy.cuda(), weight.cuda(), idx.cuda()
+    side = torch.cuda.Stream()
+    x = torch.randn(4096, 64, device="cuda").bfloat16()
+    at, size = x.data_ptr(), x.shape
+    side.wait_stream(torch.cuda.current_stream())
+    plan = block.expert_plan(idx, 5, stream=side)
+    y = block.experts(x, w1, w2, weight, plan, stream=side)
+    del x
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(100_000_000)  # cycles of a kernel that only waits
+        y.backward(dy)
+    del y
+    others = [torch.empty(size, dtype=torch.bfloat16, device="cuda") for _ in range(64)]
+    assert at not in [t.data_ptr() for t in others]
+    torch.cuda.synchronize()
+    assert bool(w1.grad.isfinite().all())
