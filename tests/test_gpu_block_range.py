@@ -125,3 +125,18 @@ def test_float16_tokens_of_other_magnitudes():
     both = results(*args)
     for a, b in zip((small[0], small[1], small[4]), (both[0], both[1], both[4])):
         assert torch.equal(a[~large], b[~large])
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("T", [0, 40, 700])
+def test_nothing_kept(T, dtype):
+    """No tokens, or a window that drops every assignment: zeros, whatever the workspace held."""
+    from paper_2504_00598_amd import block
+    say("nothing kept", T, dtype)
+    x, w1, w2, weight, idx, dy = inputs(T, 96, 72, 4, 2, dtype)
+    plan = block.expert_plan(idx, 4, first=7)
+    ws = torch.full((1 << 24,), 255, dtype=torch.uint8, device="cuda")
+    y, kept = block.experts(x, w1, w2, weight, plan, keep=True, ws=ws)
+    ws.fill_(255)
+    for t in (y,) + block.experts_bwd(dy, x, w1, w2, weight, plan, kept, ws=ws):
+        assert not t.any()
