@@ -1,0 +1,487 @@
+"""Measured cases of the decoder block's attention: a paged cache of keys and values that is written (and
+quantised) and read back, the attention of new tokens over it, and the norm and rotation of queries
+and keys by positions of several axes.
+
+run() computes a case in its plain form, elementary torch operations in 32 bits, where `own` is false, and calls
+the framework where it is true; exact() computes it in 64 bits.
+
+A cache holds keys [pages][heads][page][dim] and values [pages][heads][dim][page], in 16 bits or in e4m3 with a
+power of two 2^(scale - 127) for each token and head.  Row b of `table` lists the pages of sequence b; its
+new tokens are rows starts[b] .. starts[b+1] - 1 of the call, and are the last of its lengths[b] tokens.
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+
+DEVICE = "cuda"
+DTYPE = {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32, "e4m3": torch.float8_e4m3fn}
+SIZE = {"bf16": 2, "f16": 2, "f32": 4, "e4m3": 1}
+EPS = 1e-6
+P_TABLE = 32768  # rows of the rotation tables
+
+
+def listed():
+    return [
+        # Four sequences take one token each and are read back: launches and their latency.
+        {"name": "cache tokens", "op": "cache", "B": 4, "low": 60, "high": 130, "new": 1, "hk": 8, "d": 128, "page": 16,
+         "dtype": "bf16", "held": "e4m3"},
+        # A prompt of odd length behind an odd prefix, heads of 80, half precision held as it is.
+        {"name": "cache prompt odd", "op": "cache", "B": 3, "low": 1700, "high": 2100, "new": 1537, "hk": 5, "d": 80,
+         "page": 32, "dtype": "f16", "held": "f16"},
+        # Chunks of 16 long sequences, quantised as they are written.
+        {"name": "cache chunks large", "op": "cache", "B": 16, "low": 6000, "high": 9000, "new": 2048, "hk": 8, "d": 128,
+         "page": 64, "dtype": "bf16", "held": "e4m3"},
+        # One decoded token over a short context: latency.
+        {"name": "attend token", "op": "attend", "B": 1, "low": 777, "high": 777, "new": 1, "chunks": 1, "hq": 32, "hk": 8,
+         "d": 128, "page": 16, "window": 0, "causal": True, "dtype": "bf16", "held": "bf16"},
+        # A serving batch of uneven contexts, one token each.
+        {"name": "attend decode", "op": "attend", "B": 64, "low": 16, "high": 16384, "new": 1, "chunks": 64, "hq": 32,
+         "hk": 8, "d": 128, "page": 16, "window": 0, "causal": True, "dtype": "bf16", "held": "bf16"},
+        # The same over a quantised cache, five queries to a key head.
+        {"name": "attend decode e4m3", "op": "attend", "B": 32, "low": 4000, "high": 12000, "new": 1, "chunks": 32,
+         "hq": 40, "hk": 8, "d": 128, "page": 64, "window": 0, "causal": True, "dtype": "bf16", "held": "e4m3"},
+        # Five proposed tokens a sequence are verified under a sliding window, half precision, small heads.
+        {"name": "attend verify window", "op": "attend", "B": 16, "low": 300, "high": 5000, "new": 5, "chunks": 16,
+         "hq": 16, "hk": 16, "d": 64, "page": 32, "window": 1024, "causal": True, "dtype": "f16", "held": "f16"},
+        # A chunk of odd length behind an odd prefix, heads of 80, pages that end inside every tile.
+        {"name": "attend chunk odd", "op": "attend", "B": 2, "low": 1301, "high": 2477, "new": 333, "chunks": 2, "hq": 20,
+         "hk": 5, "d": 80, "page": 16, "window": 0, "causal": True, "dtype": "f16", "held": "f16"},
+        # A serving step: one prompt's chunk together with 32 decoded tokens, over a quantised cache.
+        {"name": "attend mixed e4m3", "op": "attend", "B": 33, "low": 2048, "high": 8192, "new": 2048, "chunks": 1,
+         "hq": 32, "hk": 8, "d": 128, "page": 64, "window": 0, "causal": True, "dtype": "bf16", "held": "e4m3"},
+        # A long prompt's chunk over a long context.
+        {"name": "attend chunk large", "op": "attend", "B": 1, "low": 32768, "high": 32768, "new": 8192, "chunks": 1,
+         "hq": 32, "hk": 8, "d": 128, "page": 64, "window": 0, "causal": True, "dtype": "bf16", "held": "bf16"},
+        # Queries and keys of four image tokens, positions of three axes in turn.
+        {"name": "axes tokens", "op": "axes", "T": 4, "hq": 32, "hk": 8, "d": 128, "r": 128, "pairs": "halves", "axes": 3,
+         "turns": True, "dtype": "bf16", "train": False},
+        # A training step over 16 sequences of 1024, time, height and width in sections.
+        {"name": "axes train", "op": "axes", "T": 16384, "hq": 40, "hk": 8, "d": 128, "r": 128, "pairs": "halves", "axes": 3,
+         "turns": False, "dtype": "bf16", "train": True},
+    ]
+
+
+def _spread(rng, low, high, step=1):
+    """A multiple of `step` in [low, high], spread over the logarithm."""
+    v = int(round(math.exp(rng.uniform(math.log(low), math.log(high))) / step)) * step
+    return min(max(v, low), high)
+
+
+def draw(rng):
+    op = rng.choice(["cache", "attend", "attend", "attend", "axes"])
+    if op == "axes":
+        hk = rng.choice([1, 2, 5, 8])
+        d = rng.choice([64, 80, 96, 128, 192, 256])
+        return {"op": op, "T": _spread(rng, 1, 16384), "hq": hk * rng.choice([1, 2, 4, 5]), "hk": hk, "d": d,
+                "r": rng.choice([d, d, d // 2]), "pairs": rng.choice(["halves", "neighbours"]), "axes": rng.choice([2, 3, 3, 4]),
+                "turns": rng.random() < 0.5, "dtype": rng.choice(["bf16", "bf16", "f16", "f32"]) if d <= 128 else "bf16",
+                "train": rng.random() < 0.5}
+    d = rng.choice([64, 80, 96, 128, 128, 128, 192, 256])
+    hk = rng.choice([1, 2, 5, 8, 8, 16])
+    dtype = rng.choice(["bf16", "bf16", "f16"])
+    c = {"op": op, "B": _spread(rng, 1, 64), "hk": hk, "d": d, "page": rng.choice([16, 16, 32, 64, 128]), "dtype": dtype,
+         "held": rng.choice([dtype, dtype, "e4m3"])}
+    c["high"] = _spread(rng, 16, 16384)
+    c["low"] = _spread(rng, 1, c["high"])
+    if op == "cache":
+        c["new"] = _spread(rng, 1, max(1, min(2048, c["low"])))
+        while c["B"] > 1 and c["B"] * c["high"] * hk * d > 1.0e8:
+            c["B"] //= 2
+        return c
+    c["hq"] = hk * rng.choice([1, 2, 4, 5, 7, 8] if hk < 16 else [1, 2])
+    kind = rng.choice(["tokens", "few", "chunks", "mixed"])
+    c["new"] = 1 if kind == "tokens" else rng.randint(2, 8) if kind == "few" else _spread(rng, 16, 4096)
+    c["chunks"] = rng.randint(1, max(1, c["B"] // 4)) if kind == "mixed" else c["B"]
+    c["window"] = rng.choice([0, 0, 0, _spread(rng, 16, 4096)])
+    c["causal"] = c["window"] > 0 or rng.random() < 0.85
+    while work(c)["bytes"] > 1.5e9 or work(c)["flops"] > 1.5e12:
+        c["B"] = max(1, c["B"] // 2)
+        c["chunks"] = min(c["chunks"], c["B"])
+        c["new"] = max(1, c["new"] // 2)
+    return c
+
+
+def _lengths(c):
+    """Tokens and new tokens of each sequence: lengths evenly from high down to low, the first `chunks` with `new` new
+    tokens (or all they have), the others with one."""
+    B = c["B"]
+    lengths = [c["high"] - (c["high"] - c["low"]) * b // max(B - 1, 1) for b in range(B)]
+    return lengths, [min(c["new"] if b < c.get("chunks", B) else 1, lengths[b]) for b in range(B)]
+
+
+def _axis_of_pairs(c):
+    """The axis of each rotated pair: in sections, the first half as long as the others, or in turns."""
+    half, n = c["r"] // 2, c["axes"]
+    if c["turns"]:
+        return [i % n for i in range(half)]
+    return [0 if i < half // (2 * n) else 1 + (i - half // (2 * n)) * (n - 1) // (half - half // (2 * n)) for i in range(half)]
+
+
+# ---------------------------------------------------------------- inputs --
+
+def _power(e):
+    """2^e in 32 bits, -126 <= e <= 127, by its bits."""
+    return (e.int() + 127 << 23).view(torch.float32)
+
+
+def _held(x):
+    """(e4m3 values, exponent + 127) of x [..., d]: the least power of two under which no entry passes 448."""
+    x = x.float()
+    m, e = torch.frexp(x.abs().amax(-1))  # m 2^e with m in [1/2, 1)
+    e = (e - 9 + (m > 0.875).int()).clamp_min(-126)
+    return (x * _power(-e)[..., None]).to(torch.float8_e4m3fn), (e + 127).to(torch.uint8)
+
+
+def _prepare_paged(c, g):
+    hk, d, page, dt, held = c["hk"], c["d"], c["page"], DTYPE[c["dtype"]], DTYPE[c["held"]]
+    lengths, new = _lengths(c)
+    B, T = c["B"], sum(new)
+    rand = lambda *s: torch.randn(*s, generator=g, device=DEVICE)  # noqa: E731
+    used = [-(-n // page) for n in lengths]
+    pages, width = sum(used) + 3, max(used)
+    order = torch.randperm(pages, generator=g, device=DEVICE).int()
+    table = torch.full((B, width), -1, dtype=torch.int32, device=DEVICE)
+    at = 0
+    for b in range(B):
+        table[b, :used[b]] = order[at:at + used[b]]
+        at += used[b]
+    mix = torch.randperm(B, generator=g, device=DEVICE).tolist()  # sequences in any order
+    lengths, new = [lengths[b] for b in mix], [new[b] for b in mix]
+    table = table[mix].contiguous()
+    starts = [0]
+    for n in new:
+        starts.append(starts[-1] + n)
+    s = {"table": table, "lengths": torch.tensor(lengths, dtype=torch.int32, device=DEVICE),
+         "starts": torch.tensor(starts, dtype=torch.int32, device=DEVICE), "host": (lengths, new, starts)}
+    k = rand(pages, hk, page, d)
+    k = (k * (0.5 + rand(pages, hk, page, 1).abs())).to(dt) if held == torch.float8_e4m3fn else k.to(dt)
+    v = rand(pages, hk, page, d).to(dt)
+    if held == torch.float8_e4m3fn:
+        k, s["k_scale"] = _held(k)
+        v, s["v_scale"] = _held(v)
+    s["k"] = k
+    s["v"] = v.view(torch.uint8 if v.element_size() == 1 else torch.int16).transpose(2, 3).contiguous().view(v.dtype)
+    # one product makes queries, keys and values
+    hq = c.get("hq", 0)
+    qkv = rand(T, (hq + 2 * hk) * d).to(dt)
+    s["new_q"] = qkv[:, :hq * d].view(T, hq, d)
+    s["new_k"] = qkv[:, hq * d:(hq + hk) * d].view(T, hk, d)
+    s["new_v"] = qkv[:, (hq + hk) * d:].view(T, hk, d)
+    if c["op"] == "cache":
+        rows = [0]
+        for n in lengths:
+            rows.append(rows[-1] + n)
+        s["rows"], s["total"] = torch.tensor(rows, dtype=torch.int32, device=DEVICE), rows[-1]
+    return s
+
+
+def _prepare_axes(c, g):
+    T, hq, hk, d, r, dt = c["T"], c["hq"], c["hk"], c["d"], c["r"], DTYPE[c["dtype"]]
+    rand = lambda *s: torch.randn(*s, generator=g, device=DEVICE)  # noqa: E731
+    qkv = (rand(T, (hq + 2 * hk) * d) * (0.5 + rand(T, 1).abs())).to(dt)
+    s = {"q": qkv[:, :hq * d].view(T, hq, d), "k": qkv[:, hq * d:(hq + hk) * d].view(T, hk, d)}
+    s["wq"], s["wk"] = (1 + 0.2 * rand(d)).to(dt), (1 + 0.2 * rand(d)).to(dt)
+    i = torch.arange(r // 2, device=DEVICE, dtype=torch.float64)
+    a = torch.arange(P_TABLE, device=DEVICE, dtype=torch.float64)[:, None] * torch.pow(10000.0, -2.0 * i / r)
+    s["cos"], s["sin"] = a.cos().float(), a.sin().float()
+    t = torch.arange(T, device=DEVICE)
+    first = int(torch.randint(0, P_TABLE // 2, (1,), generator=g, device=DEVICE))
+    grid = [first + t // 256, t % 256 // 16, t % 16, first + t % 1024]  # time, height, width; text
+    s["pos"] = torch.stack(grid[:c["axes"]]).to(torch.int32)
+    if c["train"]:
+        s["dq"], s["dk"] = rand(T, hq, d).to(dt), rand(T, hk, d).to(dt)
+    return s
+
+
+def prepare(case, seed):
+    g = torch.Generator(device=DEVICE)
+    g.manual_seed(seed)
+    s = _prepare_axes(case, g) if case["op"] == "axes" else _prepare_paged(case, g)
+    s["case"] = case
+    if own and case["op"] != "axes":
+        from paper_2504_00598_amd import block
+
+        s["cache"] = block.KVCache(s["k"], s["v"], s.get("k_scale"), s.get("v_scale"))
+        s["seqs"] = block.Sequences(s["table"], s["starts"], s["lengths"], max_new=max(s["host"][1]))
+    return s
+
+
+# ------------------------------------------------------------ plain forms --
+
+def _places(s):
+    """Page and place in it of every new token."""
+    page = s["case"]["page"]
+    starts, lengths = s["starts"].long(), s["lengths"].long()
+    b = torch.repeat_interleave(torch.arange(lengths.numel(), device=DEVICE), starts[1:] - starts[:-1],
+                                output_size=s["host"][2][-1])
+    p = lengths[b] - starts[b + 1] + torch.arange(b.numel(), device=DEVICE)
+    return s["table"][b, p // page].long(), p % page
+
+
+def _values(held, scale):
+    """What is held, in 32 bits; scale [...][1]."""
+    x = held.float()
+    return x if scale is None else x * _power(scale.int() - 127)
+
+
+def _plain_cache(s):
+    c = s["case"]
+    dt = DTYPE[c["dtype"]]
+    at, place = _places(s)
+    k, v = s["new_k"], s["new_v"]
+    if c["held"] == "e4m3":
+        (k, ks), (v, vs) = _held(k), _held(v)
+        s["k_scale"][at, :, place] = ks
+        s["v_scale"][at, :, place] = vs
+    bits = torch.uint8 if c["held"] == "e4m3" else torch.int16
+    s["k"].view(bits)[at, :, place, :] = k.view(bits) if k.is_contiguous() else k.contiguous().view(bits)
+    s["v"].view(bits)[at, :, :, place] = v.view(bits) if v.is_contiguous() else v.contiguous().view(bits)
+    rows, total, page = s["rows"].long(), s["total"], c["page"]
+    b = torch.repeat_interleave(torch.arange(rows.numel() - 1, device=DEVICE), rows[1:] - rows[:-1], output_size=total)
+    p = torch.arange(total, device=DEVICE) - rows[b]
+    at, place = s["table"][b, p // page].long(), p % page
+    k = s["k"].view(bits)[at, :, place, :].view(s["k"].dtype)
+    v = s["v"].view(bits)[at, :, :, place].view(s["v"].dtype)
+    if c["held"] != "e4m3":
+        return [k, v, s["k"], s["v"]]
+    return [_values(k, s["k_scale"][at, :, place][..., None]).to(dt), _values(v, s["v_scale"][at, :, place][..., None]).to(dt)]
+
+
+def _plain_attend(s):
+    c = s["case"]
+    hk, d, page, dt = c["hk"], c["d"], c["page"], DTYPE[c["dtype"]]
+    g = c["hq"] // hk
+    bits = torch.uint8 if c["held"] == "e4m3" else torch.int16
+    lengths, new, starts = s["host"]
+    out, lse = [], []
+    for b, (L, n) in enumerate(zip(lengths, new)):
+        at = s["table"][b, :-(-L // page)].long()
+        ks = s["k_scale"][at][..., None] if c["held"] == "e4m3" else None
+        vs = s["v_scale"][at][:, :, None] if c["held"] == "e4m3" else None
+        k = _values(s["k"].view(bits)[at].view(s["k"].dtype), ks).permute(1, 0, 2, 3).reshape(hk, -1, d)[:, :L]
+        v = _values(s["v"].view(bits)[at].view(s["v"].dtype), vs).permute(1, 0, 3, 2).reshape(hk, -1, d)[:, :L]
+        q = s["new_q"][starts[b]:starts[b + 1]].float().view(n, hk, g, d).permute(1, 0, 2, 3).reshape(hk, n * g, d)
+        i, j = torch.arange(n, device=DEVICE)[:, None] + (L - n), torch.arange(L, device=DEVICE)[None]
+        off = torch.zeros(n, L, dtype=torch.bool, device=DEVICE)
+        if c["causal"]:
+            off |= j > i
+        if c["window"]:
+            off |= j <= i - c["window"]
+        off = off.repeat_interleave(g, 0)
+        o, ls = [], []
+        few = n * g * L < 1 << 24
+        for h in ([slice(0, hk)] if few else [slice(h, h + 1) for h in range(hk)]):
+            x = torch.matmul(q[h], k[h].transpose(1, 2)).mul_(1 / math.sqrt(d)).masked_fill_(off, -math.inf)
+            m = x.amax(2, keepdim=True)
+            x = x.sub_(m).exp_()
+            l = x.sum(2, keepdim=True)
+            o.append(torch.matmul(x, v[h]) / l)
+            ls.append((m + torch.log(l))[..., 0])
+        out.append(torch.cat(o).view(hk, n, g, d).transpose(0, 1).reshape(n, c["hq"], d))
+        lse.append(torch.cat(ls).view(hk, n, g).transpose(0, 1).reshape(n, c["hq"]))
+    return [torch.cat(out).to(dt), torch.cat(lse)]
+
+
+def _turn(z, cos, sin, r, pairs):
+    if pairs == "halves":
+        a, b, rest = z[..., :r // 2], z[..., r // 2:r], z[..., r:]
+        return torch.cat((a * cos - b * sin, b * cos + a * sin, rest), -1)
+    a, b, rest = z[..., 0:r:2], z[..., 1:r:2], z[..., r:]
+    return torch.cat((torch.stack((a * cos - b * sin, b * cos + a * sin), -1).flatten(-2), rest), -1)
+
+
+def _plain_axes(s):
+    c = s["case"]
+    dt, r, pairs = s["q"].dtype, c["r"], c["pairs"]
+    axis = torch.tensor(_axis_of_pairs(c), device=DEVICE)
+    row = s["pos"].long()[axis].t()  # [T][pairs]
+    cos, sin = s["cos"].gather(0, row)[:, None], s["sin"].gather(0, row)[:, None]
+    out, grads, gains = [], [], []
+    for x, w, dy in ((s["q"], s["wq"], s.get("dq")), (s["k"], s["wk"], s.get("dk"))):
+        x, w = x.float(), w.float()
+        scale = torch.rsqrt((x * x).mean(-1, keepdim=True) + EPS)
+        n = x * scale
+        out.append(_turn(n * w, cos, sin, r, pairs).to(dt))
+        if dy is not None:
+            dz = _turn(dy.float(), cos, -sin, r, pairs)  # by the opposite angles
+            dn = dz * w
+            grads.append((scale * (dn - n * (dn * n).mean(-1, keepdim=True))).to(dt))
+            gains.append((dz * n).sum((0, 1)))
+    return out + grads + gains
+
+
+# ------------------------------------------------------- the framework's --
+
+def _own_cache(s):
+    from paper_2504_00598_amd import block
+
+    block.cache_write(s["cache"], s["new_k"], s["new_v"], s["seqs"])
+    k, v = block.cache_read(s["cache"], s["table"], s["rows"], s["total"], dtype=DTYPE[s["case"]["dtype"]])
+    return [k, v] if s["case"]["held"] == "e4m3" else [k, v, s["cache"].k, s["cache"].v]
+
+
+def _own_attend(s):
+    from paper_2504_00598_amd import block
+
+    return list(block.attend(s["new_q"], s["cache"], s["seqs"], causal=s["case"]["causal"], window=s["case"]["window"],
+                             with_lse=True))
+
+
+def _own_axes(s):
+    from paper_2504_00598_amd import block
+
+    c = s["case"]
+    how = {"eps": EPS, "interleaved": c["pairs"] == "neighbours", "axes": _axis_of_pairs(c)}
+    args = (s["q"], s["k"], s["wq"], s["wk"], s["cos"], s["sin"], s["pos"])
+    out = list(block.qk_norm_rope(*args, **how))
+    if c["train"]:
+        out += block.qk_norm_rope_bwd(s["dq"], s["dk"], *args, **how)
+    return out
+
+
+def run(state):
+    if own:
+        return {"cache": _own_cache, "attend": _own_attend, "axes": _own_axes}[state["case"]["op"]](state)
+    return {"cache": _plain_cache, "attend": _plain_attend, "axes": _plain_axes}[state["case"]["op"]](state)
+
+
+# ------------------------------------------------------------------ work --
+
+def work(case):
+    """Inputs read once, outputs written once, and the products' operations.  Of the cache what some row sees is read."""
+    c = case
+    size = SIZE[c["dtype"]]
+    if c["op"] == "axes":
+        rows = c["T"] * (c["hq"] + c["hk"]) * c["d"]
+        return {"bytes": rows * size * (5 if c["train"] else 2) + c["T"] * (c["r"] * 4 + 4 * c["axes"]),
+                "flops": rows * (24 if c["train"] else 8)}
+    lengths, new = _lengths(c)
+    held = SIZE[c["held"]] + (1 / c["d"] if c["held"] == "e4m3" else 0)
+    token = 2 * c["hk"] * c["d"]  # entries of a token's keys and values
+    if c["op"] == "cache":
+        return {"bytes": token * (sum(new) + sum(lengths)) * (size + held), "flops": token * 2 * (sum(new) + sum(lengths))}
+    seen, pairs = 0, 0
+    for L, n in zip(lengths, new):
+        w = c["window"]
+        seen += min(L, w + n - 1) if w else L
+        if not c["causal"] and not w:
+            pairs += L * n
+        else:
+            pairs += sum(min(p + 1, w or p + 1) for p in range(L - n, L))
+    rows = sum(new) * c["hq"]
+    return {"bytes": token * seen * held + rows * (2 * c["d"] * size + 4), "flops": 4 * c["d"] * pairs * c["hq"]}
+
+
+# ----------------------------------------------------------- in 64 bits --
+
+def _two(e):
+    """2^e of whole numbers e, by its bits."""
+    return (e.long() + 1023 << 52).view(torch.float64)
+
+
+def _round_e4m3(x):
+    """x to 4 significant bits, below 2^-6 to multiples of 2^-9; ties to even."""
+    e = (torch.frexp(x)[1] - 1).clamp_min(-6)
+    step = _two(e - 3)
+    return torch.round(x / step) * step
+
+
+def _exact_held(x):
+    x = x.double()
+    top = x.abs().amax(-1, keepdim=True)
+    e = torch.ceil(torch.log2(top.clamp_min(2.0 ** -140) / 448)).clamp_min(-126.0)
+    e = torch.where(_two(e) * 448 < top, e + 1, e)
+    e = torch.where((_two(e - 1) * 448 >= top) & (e > -126), e - 1, e)
+    return _round_e4m3(x / _two(e)) * _two(e)
+
+
+def _decoded(s, b, L):
+    """Keys and values [L][heads][d] of sequence b in 64 bits."""
+    page = s["case"]["page"]
+    at = s["table"][b, :-(-L // page)].long().tolist()
+    raw = lambda t, i: t[i].double()  # noqa: E731
+    k = torch.cat([raw(s["k"], i).transpose(0, 1) for i in at])[:L]
+    v = torch.cat([raw(s["v"], i).permute(2, 0, 1) for i in at])[:L]
+    if "k_scale" in s:
+        ks = torch.cat([s["k_scale"][i].t() for i in at])[:L].double()
+        vs = torch.cat([s["v_scale"][i].t() for i in at])[:L].double()
+        k, v = k * _two(ks - 127)[..., None], v * _two(vs - 127)[..., None]
+    return k, v
+
+
+def _exact_cache(c, s):
+    lengths, new, starts = s["host"]
+    ks, vs = [], []
+    for b, (L, n) in enumerate(zip(lengths, new)):
+        k, v = _decoded(s, b, L)
+        nk, nv = s["new_k"][starts[b]:starts[b + 1]], s["new_v"][starts[b]:starts[b + 1]]
+        if c["held"] == "e4m3":
+            nk, nv = _exact_held(nk), _exact_held(nv)
+        k[L - n:], v[L - n:] = nk.double(), nv.double()
+        ks.append(k)
+        vs.append(v)
+    out = [torch.cat(ks), torch.cat(vs)]
+    return out if c["held"] == "e4m3" else out + [None, None]
+
+
+def _exact_attend(c, s):
+    lengths, new, starts = s["host"]
+    out = torch.empty(starts[-1], c["hq"], c["d"], dtype=torch.float64, device=DEVICE)
+    lse = torch.empty(starts[-1], c["hq"], dtype=torch.float64, device=DEVICE)
+    g = c["hq"] // c["hk"]
+    for b, (L, n) in enumerate(zip(lengths, new)):
+        k, v = _decoded(s, b, L)
+        for first in range(0, n, 1024):
+            some = min(1024, n - first)
+            p = L - n + first + torch.arange(some, device=DEVICE)
+            sees = torch.ones(some, L, dtype=torch.bool, device=DEVICE)
+            t = torch.arange(L, device=DEVICE)
+            if c["causal"]:
+                sees &= t <= p[:, None]
+            if c["window"]:
+                sees &= t > p[:, None] - c["window"]
+            rows = slice(starts[b] + first, starts[b] + first + some)
+            for h in range(c["hq"]):
+                x = (s["new_q"][rows, h].double() @ k[:, h // g].T.contiguous()) / math.sqrt(c["d"])
+                x = x.masked_fill(~sees, -math.inf)
+                lse[rows, h] = torch.logsumexp(x, 1)
+                out[rows, h] = torch.softmax(x, 1) @ v[:, h // g].contiguous()
+    return [out, lse]
+
+
+def _exact_axes(c, s):
+    half = c["r"] // 2
+    first, second = (torch.arange(half), torch.arange(half) + half) if c["pairs"] == "halves" else (
+        2 * torch.arange(half), 2 * torch.arange(half) + 1)
+    axis = _axis_of_pairs(c)
+    cos = torch.stack([s["cos"].double()[s["pos"][axis[i]].long(), i] for i in range(half)], 1)[:, None]
+    sin = torch.stack([s["sin"].double()[s["pos"][axis[i]].long(), i] for i in range(half)], 1)[:, None]
+
+    def one(x, w, dy):
+        x, w = x.double(), w.double()
+        r1 = 1 / torch.sqrt(x.pow(2).sum(2, keepdim=True) / c["d"] + EPS)
+        z = x * r1 * w
+        y = z.clone()
+        y[:, :, first] = z[:, :, first] * cos - z[:, :, second] * sin
+        y[:, :, second] = z[:, :, second] * cos + z[:, :, first] * sin
+        if dy is None:
+            return y, None, None
+        dz = dy.double().clone()
+        dz[:, :, first] = dy.double()[:, :, first] * cos + dy.double()[:, :, second] * sin
+        dz[:, :, second] = dy.double()[:, :, second] * cos - dy.double()[:, :, first] * sin
+        dw = (dz * x * r1).reshape(-1, c["d"]).sum(0)
+        dn = dz * w
+        return y, dn * r1 - x * ((dn * x).sum(2, keepdim=True) * r1.pow(3) / c["d"]), dw
+
+    yq, dq, dwq = one(s["q"], s["wq"], s.get("dq"))
+    yk, dk, dwk = one(s["k"], s["wk"], s.get("dk"))
+    return [yq, yk, dq, dk, dwq, dwk] if c["train"] else [yq, yk]
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    return {"cache": _exact_cache, "attend": _exact_attend, "axes": _exact_axes}[case["op"]](case, s)
