@@ -207,6 +207,8 @@ def prepare(case, seed):
 
         s["cache"] = block.KVCache(s["k"], s["v"], s.get("k_scale"), s.get("v_scale"))
         s["seqs"] = block.Sequences(s["table"], s["starts"], s["lengths"], max_new=max(s["host"][1]))
+        if case["op"] == "cache":  # read back, all tokens are a sequence's last
+            s["all"] = block.Sequences(s["table"], s["rows"], s["lengths"])
     return s
 
 
@@ -320,7 +322,7 @@ def _own_cache(s):
     from paper_2504_00598_amd import block
 
     block.cache_write(s["cache"], s["new_k"], s["new_v"], s["seqs"])
-    k, v = block.cache_read(s["cache"], s["table"], s["rows"], s["total"], dtype=DTYPE[s["case"]["dtype"]])
+    k, v = block.cache_read(s["cache"], s["all"], s["total"], dtype=DTYPE[s["case"]["dtype"]])
     return [k, v] if s["case"]["held"] == "e4m3" else [k, v, s["cache"].k, s["cache"].v]
 
 
