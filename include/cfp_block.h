@@ -11,6 +11,9 @@
  *   cfp_route           routing of tokens to experts; and its gradient
  *   cfp_expert_plan     order of the assignments by expert
  *   cfp_experts         the experts' products over that order; and their gradient
+ *   cfp_cache_write     keys and values of new tokens into a paged cache, quantised as they are written
+ *   cfp_cache_read      the tokens of sequences back from it
+ *   cfp_attend          attention of new tokens over it
  *
  * Conventions (as in cfp.h): the caller owns all memory; nothing is allocated, kept or
  * synchronised; work is enqueued on `stream` and may be captured into a graph; argument
@@ -63,6 +66,16 @@ size_t cfp_qk_workspace_bytes(const cfp_qk_desc *d);
 int cfp_qk_norm_rope_bwd(const cfp_qk_desc *d, const void *dyq, int64_t dyq_token_stride, int64_t dyq_head_stride,
                          const void *dyk, int64_t dyk_token_stride, int64_t dyk_head_stride, void *dq, void *dk,
                          float *dwq, float *dwk, void *ws, size_t ws_bytes, void *stream);
+
+/* The same with positions of several axes (of an image: its row and its column): d->pos is [n_axes][n_tokens], and pair i of
+ * the rotated entries takes its angle from the tables' row pos[axis[i]][t].  axis: host [rot / 2], values below
+ * n_axes, read before the call returns.  A position outside the tables turns the entries of its axis into NaN. */
+#define CFP_QK_MAX_AXES 4
+int cfp_qk_norm_rope_axes(const cfp_qk_desc *d, const uint8_t *axis, int32_t n_axes, void *yq, void *yk, void *stream);
+int cfp_qk_norm_rope_axes_bwd(const cfp_qk_desc *d, const uint8_t *axis, int32_t n_axes, const void *dyq,
+                              int64_t dyq_token_stride, int64_t dyq_head_stride, const void *dyk, int64_t dyk_token_stride,
+                              int64_t dyk_head_stride, void *dq, void *dk, float *dwq, float *dwk, void *ws,
+                              size_t ws_bytes, void *stream);
 
 /* ---- routing ---- */
 
@@ -148,6 +161,79 @@ int cfp_experts(const cfp_experts_desc *d, void *y, void *kept, void *ws, size_t
  * dw1 and dw2 as w1 and w2 (zeros for an expert without assignments), dweight [n_tokens][k] (0 where dropped). */
 int cfp_experts_bwd(const cfp_experts_desc *d, const void *dy, int64_t dy_stride, const void *kept, void *dx, void *dw1,
                     void *dw2, float *dweight, void *ws, size_t ws_bytes, void *stream);
+
+/* ---- keys and values of past tokens ---- */
+
+/* Floats of 8 bits with 4 exponent bits, no infinities (OCP E4M3): of a cache only. */
+#define CFP_DT_E4M3 3
+#define CFP_CACHE_MAX_DIM 256
+#define CFP_CACHE_MAX_PAGE 256
+
+/* Keys [n_pages][heads][page][dim] and values [n_pages][heads][dim][page]: a value's tokens lie behind each other, as
+ * the product over tokens takes them.  Entries of CFP_DT_E4M3 stand for themselves times 2^(scale - 127) with a scale
+ * for each token and head, [n_pages][heads][page].  Pages may lie apart; the inner dimensions are contiguous. */
+typedef struct {
+  int64_t n_pages;                            /* 1 .. 2^31 - 1 */
+  int32_t page;                               /* tokens in a page: 16, 32, 64, 128 or 256 */
+  int32_t heads, dim;                         /* dim: a multiple of 16 up to CFP_CACHE_MAX_DIM */
+  int32_t dtype;                              /* CFP_DT_F16, CFP_DT_BF16 or CFP_DT_E4M3 */
+  void *k, *v;                                /* device, on 16 bytes */
+  uint8_t *k_scale, *v_scale;                 /* device, on 16 bytes, for CFP_DT_E4M3; else NULL */
+  int64_t k_page_stride, v_page_stride;       /* elements between pages, multiples of 16 */
+  int64_t k_scale_page_stride, v_scale_page_stride;
+} cfp_cache_desc;
+
+/* Sequences of a call: rows starts[b] .. starts[b+1] - 1 of its tensors are the last tokens of sequence b, which has
+ * lengths[b] tokens with them, so that row starts[b+1] - 1 is token lengths[b] - 1; token p lies in page
+ * table[b][p / page] at p % page.  starts ascends within the call's rows; rows outside it are neither read nor written.
+ * Several rows of the table may name one page to read it. */
+typedef struct {
+  int32_t n_seqs, width;   /* width: entries of a row of the table; width * page stays below 2^30 */
+  const int32_t *table;    /* device [n_seqs][width], rows table_stride entries apart */
+  int64_t table_stride;
+  const int32_t *starts;   /* device [n_seqs + 1] */
+  const int32_t *lengths;  /* device [n_seqs] */
+  int32_t max_new;         /* the most rows that a sequence has, or more */
+} cfp_sequences_desc;
+
+/* Writes the keys and values of n_tokens rows (k, v [n_tokens][heads][dim] in CFP_DT_F16 or CFP_DT_BF16, strides in
+ * elements, last dimension contiguous) to their places.  A cache of 16 bits is of the rows' type.  One of
+ * CFP_DT_E4M3 gets for each token and head the least power of two 2^e, e >= -126, for which no finite entry passes
+ * 448 2^e, and each entry over it rounded to the nearest value that is also one of the rows' type; infinities and NaN are
+ * held as NaN.  A token whose place is before the first, behind the table's width or in a page outside the cache is not
+ * written.  Where two rows have one place, what is held there afterwards is unspecified. */
+int cfp_cache_write(const cfp_cache_desc *c, const cfp_sequences_desc *s, int64_t n_tokens, int32_t dtype, const void *k,
+                    int64_t k_token_stride, int64_t k_head_stride, const void *v, int64_t v_token_stride,
+                    int64_t v_head_stride, void *stream);
+
+/* The tokens of the rows back, as the values that they stand for: k, v [n_tokens][heads][dim] contiguous, of the cache's type
+ * or, from CFP_DT_E4M3, in `dtype`.  A token before the first reads as zeros, one behind the table's width or in a page
+ * outside the cache as NaN. */
+int cfp_cache_read(const cfp_cache_desc *c, const cfp_sequences_desc *s, int64_t n_tokens, int32_t dtype, void *k, void *v,
+                   void *stream);
+
+/* ---- attention ---- */
+
+typedef struct {
+  int64_t n_tokens;
+  int32_t n_q;            /* heads, a multiple of the cache's; head h reads the cache's head h / (n_q / heads) */
+  int32_t dtype;          /* CFP_DT_F16 or CFP_DT_BF16: of q and out, and of a cache of 16 bits */
+  const void *q;          /* device [n_tokens][n_q][dim], last dimension contiguous */
+  int64_t q_token_stride, q_head_stride; /* in elements */
+  float scale;            /* of the scores, > 0 */
+  int32_t causal;         /* a row of token p sees the tokens up to p; else all of its sequence's */
+  int32_t window;         /* and with window > 0 none before p - window + 1 */
+} cfp_attend_desc;
+
+/* out [n_tokens][n_q][dim]: for every row the mean of the values that it sees, weighted by exp(scale q . k); lse
+ * [n_tokens][n_q] float (or NULL): the logarithm of the sum of the weights.  A row that sees nothing gets zeros and -inf.
+ * What a row does not see has no effect on it, whatever it holds.  A row that sees a token of a page outside the
+ * cache, and all rows of a sequence longer than its table or with more rows than max_new, become NaN.
+ * The weights are rounded to `dtype` as operands of the product with the values, relative to the largest so far;
+ * sums, maxima and what is held between parts of a long sequence are in 32 bits. */
+size_t cfp_attend_workspace_bytes(const cfp_attend_desc *a, const cfp_cache_desc *c, const cfp_sequences_desc *s);
+int cfp_attend(const cfp_attend_desc *a, const cfp_cache_desc *c, const cfp_sequences_desc *s, void *out, float *lse, void *ws,
+               size_t ws_bytes, void *stream);
 
 #ifdef __cplusplus
 }

@@ -6,7 +6,12 @@
     plan = block.expert_plan(index, n_experts)
     y = block.experts(x, w1, w2, weight, plan)
 
-Each has its gradient beside it (`*_bwd`), and where gradients are recorded and an input requires one, backward()
+    cache = block.KVCache.empty(pages, 64, key_heads, dim, torch.float8_e4m3fn)
+    seqs = block.Sequences(table, starts, lengths, max_new=1)
+    block.cache_write(cache, k, v, seqs)
+    y = block.attend(q, cache, seqs)
+
+The first three have their gradient beside them (`*_bwd`), and where gradients are recorded and an input requires one, backward()
 reaches it through that (block_grad).  What a `*_bwd` returns has no gradient of its own.  Argument marshalling only: the work is
 the HIP kernels' behind the C ABI of include/cfp_block.h, enqueued on the current
 stream or on `stream`; nothing synchronises.  Results and workspaces are allocated
@@ -24,14 +29,16 @@ from ._lib import CFP_OK, CfpError
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libcfp_block.so")
 
-CFP_DT_F32, CFP_DT_F16, CFP_DT_BF16 = 0, 1, 2
+CFP_DT_F32, CFP_DT_F16, CFP_DT_BF16, CFP_DT_E4M3 = 0, 1, 2, 3
+CFP_QK_MAX_AXES = 4
 SCORES = {"softmax": 0, "sigmoid": 1}
 CFP_PLAN_PAD = 16  # entries behind the last of a plan's rows
 GROUP_SCORES = {"max": 0, "top2": 1}
 
 EXPORTED = ("cfp_qk_norm_rope", "cfp_qk_workspace_bytes", "cfp_qk_norm_rope_bwd", "cfp_route", "cfp_route_bwd",
             "cfp_expert_plan_workspace_bytes", "cfp_expert_plan", "cfp_experts_kept_bytes",
-            "cfp_experts_workspace_bytes", "cfp_experts", "cfp_experts_bwd")
+            "cfp_experts_workspace_bytes", "cfp_experts", "cfp_experts_bwd", "cfp_qk_norm_rope_axes",
+            "cfp_qk_norm_rope_axes_bwd", "cfp_cache_write", "cfp_cache_read", "cfp_attend_workspace_bytes", "cfp_attend")
 
 _P, _I32, _I64, _F32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
 
@@ -59,11 +66,29 @@ class cfp_experts_desc(ctypes.Structure):
                 ("slot", _P)]
 
 
+class cfp_cache_desc(ctypes.Structure):
+    _fields_ = [("n_pages", _I64), ("page", _I32), ("heads", _I32), ("dim", _I32), ("dtype", _I32), ("k", _P), ("v", _P),
+                ("k_scale", _P), ("v_scale", _P), ("k_page_stride", _I64), ("v_page_stride", _I64),
+                ("k_scale_page_stride", _I64), ("v_scale_page_stride", _I64)]
+
+
+class cfp_sequences_desc(ctypes.Structure):
+    _fields_ = [("n_seqs", _I32), ("width", _I32), ("table", _P), ("table_stride", _I64), ("starts", _P), ("lengths", _P),
+                ("max_new", _I32)]
+
+
+class cfp_attend_desc(ctypes.Structure):
+    _fields_ = [("n_tokens", _I64), ("n_q", _I32), ("dtype", _I32), ("q", _P), ("q_token_stride", _I64),
+                ("q_head_stride", _I64), ("scale", _F32), ("causal", _I32), ("window", _I32)]
+
+
 # The same layouts for struct.pack: filling a ctypes structure of 21 fields takes 3 us, packing it 0.6 (a small
 # launch takes 3).  A packed descriptor is passed by the address of its bytes.
 _CODES = {_I64: "q", _I32: "i", _F32: "f", _P: "P"}
-_QK, _ROUTE, _PLAN, _EXPERTS = (struct.Struct("@" + "".join(_CODES[t] for _, t in c._fields_)).pack
-                                for c in (cfp_qk_desc, cfp_route_desc, cfp_plan_desc, cfp_experts_desc))
+_QK, _ROUTE, _PLAN, _EXPERTS, _CACHE, _SEQUENCES, _ATTEND = (
+    struct.Struct("@" + "".join(_CODES[t] for _, t in c._fields_) + "0q").pack
+    for c in (cfp_qk_desc, cfp_route_desc, cfp_plan_desc, cfp_experts_desc, cfp_cache_desc, cfp_sequences_desc,
+              cfp_attend_desc))
 
 _lib = None
 
@@ -77,14 +102,21 @@ def lib() -> ctypes.CDLL:
         L = ctypes.CDLL(LIB_PATH)
         SZ = ctypes.c_size_t
         for name, args in (("cfp_qk_workspace_bytes", [_P]), ("cfp_expert_plan_workspace_bytes", [_P]),
-                           ("cfp_experts_kept_bytes", [_P]), ("cfp_experts_workspace_bytes", [_P, _I32])):
+                           ("cfp_experts_kept_bytes", [_P]), ("cfp_experts_workspace_bytes", [_P, _I32]),
+                           ("cfp_attend_workspace_bytes", [_P, _P, _P])):
             getattr(L, name).argtypes, getattr(L, name).restype = args, SZ
         for name, args in (("cfp_qk_norm_rope", [_P, _P, _P, _P]),
                            ("cfp_qk_norm_rope_bwd", [_P, _P, _I64, _I64, _P, _I64, _I64, _P, _P, _P, _P, _P, SZ, _P]),
                            ("cfp_route", [_P, _P, _P, _P]), ("cfp_route_bwd", [_P, _P, _P, _P, _P]),
                            ("cfp_expert_plan", [_P, _P, _P, _P, _P, SZ, _P]),
                            ("cfp_experts", [_P, _P, _P, _P, SZ, _P]),
-                           ("cfp_experts_bwd", [_P, _P, _I64, _P, _P, _P, _P, _P, _P, SZ, _P])):
+                           ("cfp_experts_bwd", [_P, _P, _I64, _P, _P, _P, _P, _P, _P, SZ, _P]),
+                           ("cfp_qk_norm_rope_axes", [_P, _P, _I32, _P, _P, _P]),
+                           ("cfp_qk_norm_rope_axes_bwd", [_P, _P, _I32, _P, _I64, _I64, _P, _I64, _I64, _P, _P, _P, _P, _P,
+                                                          SZ, _P]),
+                           ("cfp_cache_write", [_P, _P, _I64, _I32, _P, _I64, _I64, _P, _I64, _I64, _P]),
+                           ("cfp_cache_read", [_P, _P, _I64, _I32, _P, _P, _P]),
+                           ("cfp_attend", [_P, _P, _P, _P, _P, _P, SZ, _P])):
             getattr(L, name).argtypes, getattr(L, name).restype = args, ctypes.c_int
         _lib = L
     return _lib
@@ -177,7 +209,7 @@ def _ptr(t):
 
 # -------------------------------------------------------- queries and keys --
 
-def _qk_refuse(q, k, wq, wk, cos, sin, positions, torch):
+def _qk_refuse(q, k, wq, wk, cos, sin, positions, axes, torch):
     """Raises what is wrong with the arguments."""
     for name, t in (("q", q), ("k", k)):
         _tensor(name, t, torch, dim=3)
@@ -197,7 +229,15 @@ def _qk_refuse(q, k, wq, wk, cos, sin, positions, torch):
         _tensor(name, t, torch, (torch.float32,), 2)
         if not t.is_contiguous() or t.shape != cos.shape:
             raise ValueError("cos and sin must be contiguous [positions][rotated / 2]")
-    if positions is not None:
+    if axes is not None:
+        if positions is None:
+            raise ValueError("axes need positions of each axis")
+        _tensor("positions", positions, torch, (torch.int32,), 2)
+        if positions.shape[1] != T or not positions.is_contiguous() or not 1 <= positions.shape[0] <= CFP_QK_MAX_AXES:
+            raise ValueError(f"positions must be contiguous [axes][T], of at most {CFP_QK_MAX_AXES} axes")
+        if len(axes) != cos.shape[1] or any(a not in range(positions.shape[0]) for a in axes):
+            raise ValueError("axes must name an axis of positions for each rotated pair")
+    elif positions is not None:
         _tensor("positions", positions, torch, (torch.int32,), 1)
         if positions.shape[0] != T or not positions.is_contiguous():
             raise ValueError("positions must be contiguous [T]")
@@ -206,7 +246,8 @@ def _qk_refuse(q, k, wq, wk, cos, sin, positions, torch):
     _same_device(q, k, wq, wk, cos, sin, positions)
 
 
-def _qk_desc(q, k, wq, wk, cos, sin, positions, eps, interleaved, torch):
+def _qk_desc(q, k, wq, wk, cos, sin, positions, eps, interleaved, axes, torch):
+    """The packed descriptor, and with axes that of each pair in a byte."""
     # one pass over what has to hold, on the way of every call; what does not hold is said by _qk_refuse
     try:
         at, half = q.get_device(), cos.shape[1]
@@ -218,8 +259,14 @@ def _qk_desc(q, k, wq, wk, cos, sin, positions, eps, interleaved, torch):
         for w in (wq, wk):
             ok = ok and (w is None or (w.numel() == D and w.dim() == 1 and w.get_device() == at and w.is_contiguous()))
         ok = ok and (wq is None or wk is None or wq.dtype is wk.dtype)
+        pairs = None
         if positions is None:
-            ok = ok and (T <= cos.shape[0] or half == 0)
+            ok = ok and axes is None and (T <= cos.shape[0] or half == 0)
+        elif axes is not None:
+            pairs = bytes([*axes])
+            ok = ok and (positions.dtype is torch.int32 and positions.dim() == 2 and positions.shape[1] == T and
+                         positions.get_device() == at and positions.is_contiguous() and len(pairs) == half and
+                         1 <= positions.shape[0] <= CFP_QK_MAX_AXES and max(pairs, default=0) < positions.shape[0])
         else:
             ok = ok and (positions.dtype is torch.int32 and positions.numel() == T and positions.dim() == 1 and
                          positions.get_device() == at and positions.is_contiguous())
@@ -228,41 +275,46 @@ def _qk_desc(q, k, wq, wk, cos, sin, positions, eps, interleaved, torch):
     except (AttributeError, KeyError, IndexError, TypeError, ValueError):
         ok = False
     if not ok:
-        _qk_refuse(q, k, wq, wk, cos, sin, positions, torch)
+        _qk_refuse(q, k, wq, wk, cos, sin, positions, axes, torch)
         raise ValueError("unsupported arguments")
     return _QK(T, hq, k.shape[1], D, 2 * half, 1 if interleaved else 0, *types, eps, cos.shape[0], q.data_ptr(),
-               k.data_ptr(), qt, qh, kt, kh, _ptr(wq), _ptr(wk), cos.data_ptr(), sin.data_ptr(), _ptr(positions))
+               k.data_ptr(), qt, qh, kt, kh, _ptr(wq), _ptr(wk), cos.data_ptr(), sin.data_ptr(), _ptr(positions)), pairs
 
 
-def qk_norm_rope(q, k, wq, wk, cos, sin, positions=None, *, eps=1e-6, interleaved=False, stream=None):
+def qk_norm_rope(q, k, wq, wk, cos, sin, positions=None, *, eps=1e-6, interleaved=False, axes=None, stream=None):
     """Norm and rotation of queries and keys in one pass.
 
     q [T][heads][D] and k [T][key heads][D] may be views of a larger product (last
     dimension contiguous).  Each head is divided by sqrt(mean(x^2) + eps), times its
     gain wq or wk [D] (None: ones), and its first 2 * cos.shape[1] entries are rotated by
     the angles of row positions[t] of the tables cos, sin [positions][rotated / 2]
-    (None: row t): pairs (i, i + rotated / 2), or with `interleaved` (2i, 2i + 1).  A position outside
-    the tables makes its rotated entries NaN.  Returns contiguous (q, k) of q's type."""
+    (None: row t): pairs (i, i + rotated / 2), or with `interleaved` (2i, 2i + 1).  With `axes`, the axis of each pair
+    (a sequence of rotated / 2 numbers), pair i turns by row positions[axes[i]][t], positions [axes][T].  A position outside
+    the tables makes the entries that it rotates NaN.  Returns contiguous (q, k) of q's type."""
     torch = _torch()
-    d = _qk_desc(q, k, wq, wk, cos, sin, positions, eps, interleaved, torch)
+    d, pairs = _qk_desc(q, k, wq, wk, cos, sin, positions, eps, interleaved, axes, torch)
     if _recorded(torch, q, k, wq, wk, cos, sin):
         from . import block_grad
         with _on(torch, q.device, stream):
-            return block_grad.qk_norm_rope(q, k, wq, wk, cos, sin, positions, eps, interleaved, stream)
+            return block_grad.qk_norm_rope(q, k, wq, wk, cos, sin, positions, eps, interleaved, stream, axes)
     with _on(torch, q.device, stream):
         yq, yk = _like(torch, q), _like(torch, k)
-        rc = _lib.cfp_qk_norm_rope(d, yq.data_ptr(), yk.data_ptr(), _raw(torch, q.device))
+        if pairs is None:
+            rc = _lib.cfp_qk_norm_rope(d, yq.data_ptr(), yk.data_ptr(), _raw(torch, q.device))
+        else:
+            rc = _lib.cfp_qk_norm_rope_axes(d, pairs, positions.shape[0], yq.data_ptr(), yk.data_ptr(),
+                                            _raw(torch, q.device))
     if rc:
         _check("cfp_qk_norm_rope", rc)
     return yq, yk
 
 
-def qk_norm_rope_bwd(dyq, dyk, q, k, wq, wk, cos, sin, positions=None, *, eps=1e-6, interleaved=False, ws=None,
-                     stream=None):
+def qk_norm_rope_bwd(dyq, dyk, q, k, wq, wk, cos, sin, positions=None, *, eps=1e-6, interleaved=False, axes=None,
+                     ws=None, stream=None):
     """Gradients of qk_norm_rope in q, k, wq and wk from those of its results (the inputs
     as they were given to it).  Returns (dq, dk, dwq, dwk); dwq and dwk are float32, None for a gain of None."""
     torch = _torch()
-    d = _qk_desc(q, k, wq, wk, cos, sin, positions, eps, interleaved, torch)
+    d, pairs = _qk_desc(q, k, wq, wk, cos, sin, positions, eps, interleaved, axes, torch)
     for name, t, of in (("dyq", dyq, q), ("dyk", dyk, k)):
         _tensor(name, t, torch, (q.dtype,), 3)
         if t.shape != of.shape or (t.shape[2] > 1 and t.stride(2) != 1):
@@ -273,9 +325,10 @@ def qk_norm_rope_bwd(dyq, dyk, q, k, wq, wk, cos, sin, positions=None, *, eps=1e
         dwq = torch.empty(q.shape[2], dtype=torch.float32, device=q.device) if wq is not None else None
         dwk = torch.empty(q.shape[2], dtype=torch.float32, device=q.device) if wk is not None else None
         ws = _ws(torch, _lib.cfp_qk_workspace_bytes(d), q.device, ws, 4)
-        _check("cfp_qk_norm_rope_bwd", _lib.cfp_qk_norm_rope_bwd(
-            d, dyq.data_ptr(), dyq.stride(0), dyq.stride(1), dyk.data_ptr(), dyk.stride(0), dyk.stride(1),
-            dq.data_ptr(), dk.data_ptr(), _ptr(dwq), _ptr(dwk), ws.data_ptr(), ws.numel(), _raw(torch, q.device)))
+        rest = (dyq.data_ptr(), dyq.stride(0), dyq.stride(1), dyk.data_ptr(), dyk.stride(0), dyk.stride(1),
+                dq.data_ptr(), dk.data_ptr(), _ptr(dwq), _ptr(dwk), ws.data_ptr(), ws.numel(), _raw(torch, q.device))
+        _check("cfp_qk_norm_rope_bwd", _lib.cfp_qk_norm_rope_bwd(d, *rest) if pairs is None else
+               _lib.cfp_qk_norm_rope_axes_bwd(d, pairs, positions.shape[0], *rest))
     return dq, dk, dwq, dwk
 
 
@@ -486,3 +539,222 @@ def experts_bwd(dy, x, w1, w2, weight, plan, kept, *, ws=None, stream=None):
             d, dy.data_ptr(), _rows("dy", dy), kept.data_ptr(), dx.data_ptr(), dw1.data_ptr(), dw2.data_ptr(),
             dweight.data_ptr(), ws.data_ptr(), ws.numel(), _raw(torch, x.device)))
     return dx, dw1, dw2, dweight
+
+
+# --------------------------------------------- past tokens and attention --
+
+class KVCache:
+    """Keys and values of past tokens in pages.
+
+    k [pages][heads][page][dim] and v [pages][heads][dim][page], float16, bfloat16 or float8_e4m3fn; the last with
+    k_scale, v_scale [pages][heads][page] uint8: an entry stands for itself times 2^(scale - 127).  Pages may lie apart (a
+    view of a larger tensor), what is in one is contiguous.  page is 16, 32, 64, 128 or 256, dim a multiple of 16 up to 256."""
+
+    __slots__ = ("k", "v", "k_scale", "v_scale", "_desc")
+
+    def __init__(self, k, v, k_scale=None, v_scale=None):
+        torch = _torch()
+        byte = getattr(k, "dtype", None) is torch.float8_e4m3fn
+        held = {torch.float16: CFP_DT_F16, torch.bfloat16: CFP_DT_BF16, torch.float8_e4m3fn: CFP_DT_E4M3}
+        for name, t in (("k", k), ("v", v)):
+            _tensor(name, t, torch, held, 4)
+        (n, h, page, d), device = k.shape, k.device
+        if v.dtype != k.dtype or v.shape != (n, h, d, page):
+            raise ValueError("k is [pages][heads][page][dim] and v is [pages][heads][dim][page], of one type")
+        if byte != (k_scale is not None) or byte != (v_scale is not None):
+            raise ValueError("k_scale and v_scale go with float8_e4m3fn")
+        strides = []
+        for name, t in (("k", k), ("v", v)) + ((("k_scale", k_scale), ("v_scale", v_scale)) if byte else ()):
+            if name in ("k_scale", "v_scale"):
+                _tensor(name, t, torch, (torch.uint8,), 3)
+                if t.shape != (n, h, page):
+                    raise ValueError(f"{name} must be [pages][heads][page]")
+            if n and not t[0].is_contiguous():
+                raise ValueError(f"{name}: what is in a page must be contiguous")
+            strides.append(t.stride(0) if n > 1 else t[0].numel() if n else 0)
+        _same_device(k, v, k_scale, v_scale)
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self._desc = _CACHE(n, page, h, d, held[k.dtype], k.data_ptr(), v.data_ptr(), _ptr(k_scale), _ptr(v_scale),
+                            *(strides + [0, 0])[:4])
+
+    @classmethod
+    def empty(cls, pages, page, heads, dim, dtype, device="cuda"):
+        """A cache of its own; what its pages hold is unspecified until it is written."""
+        import torch
+
+        k = torch.empty((pages, heads, page, dim), dtype=dtype, device=device)
+        v = torch.empty((pages, heads, dim, page), dtype=dtype, device=device)
+        if dtype is not torch.float8_e4m3fn:
+            return cls(k, v)
+        return cls(k, v, *(torch.empty((pages, heads, page), dtype=torch.uint8, device=device) for _ in range(2)))
+
+    def _tensors(self):
+        return self.k, self.v, self.k_scale, self.v_scale
+
+
+class Sequences:
+    """Which rows of a call are which tokens of which sequence, and where these lie in a cache.
+
+    Rows starts[b] .. starts[b + 1] - 1 are the last tokens of sequence b, which has lengths[b] with them; its token p is in
+    page table[b][p // page].  table [sequences][width], starts [sequences + 1] and lengths [sequences] are
+    int32 on the GPU and are read when the kernels run: a captured call follows what a program writes into them.  starts
+    ascends; rows outside it belong to no sequence.  max_new: the most rows that a sequence has, or
+    more (None: any number); attend lays its work out for it, and for table's width."""
+
+    __slots__ = ("table", "starts", "lengths", "max_new", "_desc")
+
+    def __init__(self, table, starts, lengths, *, max_new=None):
+        torch = _torch()
+        _tensor("table", table, torch, (torch.int32,), 2)
+        _tensor("starts", starts, torch, (torch.int32,), 1)
+        _tensor("lengths", lengths, torch, (torch.int32,), 1)
+        n, width = table.shape
+        if starts.shape[0] != n + 1 or lengths.shape[0] != n:
+            raise ValueError("table is [sequences][width], starts [sequences + 1] and lengths [sequences]")
+        if not starts.is_contiguous() or not lengths.is_contiguous():
+            raise ValueError("starts and lengths must be contiguous")
+        _same_device(table, starts, lengths)
+        if max_new is not None and max_new < 0:
+            raise ValueError("max_new must not be negative")
+        self.table, self.starts, self.lengths, self.max_new = table, starts, lengths, max_new
+        most = 0x7FFFFFFF if max_new is None else min(max_new, 0x7FFFFFFF)
+        self._desc = _SEQUENCES(n, width, table.data_ptr(), _rows("table", table), starts.data_ptr(), lengths.data_ptr(), most)
+
+    def _tensors(self):
+        return self.table, self.starts, self.lengths
+
+
+def _paged(torch, cache, seqs, *others):
+    """Checks what the operators over a cache share; returns its device."""
+    if not isinstance(cache, KVCache):
+        raise TypeError("cache must be a KVCache")
+    if not isinstance(seqs, Sequences):
+        raise TypeError("seqs must be Sequences")
+    at = cache.k.get_device()
+    if seqs.table.get_device() != at or any(t is not None and t.get_device() != at for t in others):
+        raise ValueError("all tensors must be on one device")
+    return cache.k.device
+
+
+def _heads(name, t, torch, dim, held):
+    """Checks rows of heads of a cache's dim; `held`: its type."""
+    _tensor(name, t, torch, (torch.float16, torch.bfloat16), 3)
+    if t.shape[2] != dim or (dim > 1 and t.stride(2) != 1):
+        raise ValueError(f"{name} must be [T][heads][dim] with the cache's dim, the last dimension contiguous")
+    if held is not torch.float8_e4m3fn and t.dtype is not held:
+        raise TypeError(f"{name} must be of the cache's type")
+
+
+def _no_gradient(torch, name, *inputs):
+    if _recorded(torch, *inputs):
+        raise RuntimeError(f"{name} has no gradient: call it under torch.no_grad()")
+
+
+def _used_on(stream, *tensors):
+    """The caching allocator hands memory out again in the order of the stream it was allocated on."""
+    if stream is not None:
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+
+
+def cache_write(cache, k, v, seqs, *, stream=None):
+    """Writes k and v [T][heads][dim] (views with a contiguous last dimension) to their sequences' places in the cache.
+
+    A cache of 16 bits is of their type.  One of float8_e4m3fn gets for each token and head the least power of two under
+    which no finite entry passes 448, and every entry over it rounded to the nearest; infinities and NaN become NaN.  A token
+    whose page is not one of the cache's is not written.  Two rows must not have one place."""
+    torch = _torch()
+    device = _paged(torch, cache, seqs, k, v) if isinstance(k, torch.Tensor) and isinstance(v, torch.Tensor) else None
+    held, (_, heads, _, dim) = cache.k.dtype, cache.k.shape
+    _heads("k", k, torch, dim, held)
+    _heads("v", v, torch, dim, held)
+    if k.shape != v.shape or k.shape[1] != heads or k.dtype is not v.dtype:
+        raise ValueError("k and v are [T][the cache's heads][dim], of one type")
+    _no_gradient(torch, "cache_write", k, v)
+    _used_on(stream, k, v, *cache._tensors(), *seqs._tensors())
+    with _on(torch, device, stream):
+        rc = _lib.cfp_cache_write(cache._desc, seqs._desc, k.shape[0], _DT[k.dtype], k.data_ptr(), k.stride(0), k.stride(1),
+                                  v.data_ptr(), v.stride(0), v.stride(1), _raw(torch, device))
+    if rc:
+        _check("cfp_cache_write", rc)
+
+
+def cache_read(cache, seqs, n_tokens, *, dtype=None, out=None, stream=None):
+    """The tokens of `seqs` back from the cache, as the values that they stand for: (k, v) [n_tokens][heads][dim] of the
+    cache's type, or of `dtype` (float8_e4m3fn: bfloat16, or float16).  With starts as the sums of lengths these are
+    whole sequences.  A token whose page is not one of the cache's reads as NaN.  Rows of no sequence are left as they
+    are: unspecified, or with out=(k, v) what these held."""
+    torch = _torch()
+    device = _paged(torch, cache, seqs)
+    held, (_, heads, _, dim) = cache.k.dtype, cache.k.shape
+    if dtype is None:
+        dtype = torch.bfloat16 if held is torch.float8_e4m3fn else held
+    if dtype not in (torch.float16, torch.bfloat16) or (held is not torch.float8_e4m3fn and dtype is not held):
+        raise TypeError("dtype must be the cache's, or float16 or bfloat16 of float8_e4m3fn")
+    if n_tokens < 0:
+        raise ValueError("n_tokens must not be negative")
+    shape = (n_tokens, heads, dim)
+    if out is not None:
+        for name, t in zip(("k", "v"), out, strict=True):
+            _tensor(name, t, torch, (dtype,), 3)
+            if t.shape != shape or not t.is_contiguous():
+                raise ValueError("out must be contiguous [n_tokens][heads][dim]")
+        _same_device(cache.k, *out)
+        _used_on(stream, *out)
+    _used_on(stream, *cache._tensors(), *seqs._tensors())
+    with _on(torch, device, stream):
+        k, v = out if out is not None else (torch.empty(shape, dtype=dtype, device=device) for _ in range(2))
+        rc = _lib.cfp_cache_read(cache._desc, seqs._desc, n_tokens, _DT[dtype], k.data_ptr(), v.data_ptr(), _raw(torch, device))
+    if rc:
+        _check("cfp_cache_read", rc)
+    return k, v
+
+
+def attend(q, cache, seqs, *, scale=None, causal=True, window=0, with_lse=False, out=None, ws=None, stream=None):
+    """Attention of new tokens over a cache that holds them and those before them.
+
+    q [T][heads][dim] (a view with a contiguous last dimension), heads a multiple of the cache's: head h reads head
+    h // (heads / cache heads).  A row that is token p of its sequence sees the tokens up to p, or all without `causal`, and with a
+    window > 0 none before p - window + 1.  Its result is the mean of their values weighted by exp(scale q . k)
+    (scale > 0; None: 1 / sqrt(dim)).  Returns [T][heads][dim] of q's type, or with `with_lse` also the logarithm of the
+    sum of the weights, [T][heads] float32, by which results over parts of a context are joined.  A row that sees nothing gets
+    zeros and -inf; what it does not see has no effect on it.  A row that sees a page outside the cache, a sequence
+    longer than its table and one with more rows than max_new get NaN.  Rows of no sequence are left as they are: unspecified,
+    or what `out` (or out=(y, lse) with `with_lse`) held."""
+    torch = _torch()
+    device = _paged(torch, cache, seqs, q) if isinstance(q, torch.Tensor) else None
+    held, (_, heads, _, dim) = cache.k.dtype, cache.k.shape
+    _heads("q", q, torch, dim, held)
+    if heads == 0 or q.shape[1] == 0 or q.shape[1] % heads:
+        raise ValueError("q's heads must be a multiple of the cache's")
+    if scale is None:
+        scale = dim ** -0.5
+    _no_gradient(torch, "attend", q)
+    T, hq = q.shape[:2]
+    y, lse = out if with_lse and out is not None else (out, None)
+    if out is not None:
+        _tensor("out", y, torch, (q.dtype,), 3)
+        if y.shape != q.shape or not y.is_contiguous():
+            raise ValueError("out must be contiguous, of q's shape")
+        if with_lse:
+            _tensor("lse", lse, torch, (torch.float32,), 2)
+            if lse.shape != (T, hq) or not lse.is_contiguous():
+                raise ValueError("lse must be contiguous [T][heads]")
+        _same_device(q, y, lse)
+        _used_on(stream, y, lse)
+    d = _ATTEND(T, hq, _DT[q.dtype], q.data_ptr(), q.stride(0), q.stride(1), scale, 1 if causal else 0,
+                window if 0 <= window < 1 << 31 else -1 if window < 0 else 0x7FFFFFFF)
+    _used_on(stream, q, ws, *cache._tensors(), *seqs._tensors())
+    with _on(torch, device, stream):
+        if out is None:
+            y = torch.empty(q.shape, dtype=q.dtype, device=device)
+            lse = torch.empty((T, hq), dtype=torch.float32, device=device) if with_lse else None
+        need = _lib.cfp_attend_workspace_bytes(d, cache._desc, seqs._desc)
+        if need or ws is not None:
+            ws = _ws(torch, need, device, ws)
+        rc = _lib.cfp_attend(d, cache._desc, seqs._desc, y.data_ptr(), _ptr(lse), _ptr(ws), 0 if ws is None else ws.numel(),
+                             _raw(torch, device))
+    if rc:
+        _check("cfp_attend", rc)
+    return (y, lse) if with_lse else y

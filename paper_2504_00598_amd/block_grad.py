@@ -22,9 +22,9 @@ def _last(t):
 
 class QkNormRope(Function):
     @staticmethod
-    def forward(ctx, q, k, wq, wk, cos, sin, positions, eps, interleaved):
+    def forward(ctx, q, k, wq, wk, cos, sin, positions, eps, interleaved, axes=None):
         ctx.save_for_backward(q, k, wq, wk, cos, sin, positions)
-        ctx.how = {"eps": eps, "interleaved": interleaved}
+        ctx.how = {"eps": eps, "interleaved": interleaved, "axes": None if axes is None else tuple(axes)}
         return block.qk_norm_rope(q, k, wq, wk, cos, sin, positions, **ctx.how)
 
     @staticmethod
@@ -33,7 +33,7 @@ class QkNormRope(Function):
         wq, wk = ctx.saved_tensors[2:4]
         dq, dk, dwq, dwk = block.qk_norm_rope_bwd(_last(dyq), _last(dyk), *ctx.saved_tensors, **ctx.how)
         return (dq, dk, None if wq is None else dwq.to(wq.dtype), None if wk is None else dwk.to(wk.dtype),
-                None, None, None, None, None)
+                None, None, None, None, None, None)
 
 
 class Route(Function):
@@ -76,11 +76,11 @@ def _used_on(stream, *tensors):
                 t.record_stream(stream)
 
 
-def qk_norm_rope(q, k, wq, wk, cos, sin, positions, eps, interleaved, stream):
+def qk_norm_rope(q, k, wq, wk, cos, sin, positions, eps, interleaved, stream, axes=None):
     if cos.requires_grad or sin.requires_grad:
         raise ValueError("cos and sin have no gradient")
     _used_on(stream, q, k, wq, wk, cos, sin, positions)
-    return QkNormRope.apply(q, k, wq, wk, cos, sin, positions, eps, interleaved)
+    return QkNormRope.apply(q, k, wq, wk, cos, sin, positions, eps, interleaved, axes)
 
 
 def route(logits, k, choice, weights, stream):

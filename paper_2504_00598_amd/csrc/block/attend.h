@@ -1,0 +1,780 @@
+// Attention of new tokens over a paged cache.
+//
+// A row is one head of one new token: query q, token p of its sequence.  Over the tokens j that it sees, with
+// s_j = scale q . k_j:  m = max s_j,  l = sum exp(s_j - m),  o = sum exp(s_j - m) v_j / l,  lse = m + ln l.
+// One pass over the tokens: m and l run along, and what is summed so far is multiplied by exp(m_old - m_new)
+// where m grows.  It grows only when the new maximum is over it by more than 2^kSlack, which leaves every ratio as it is.
+//
+// The heads that share a key head, and the tokens of a chunk, are rows of one product.  Scores are made transposed,
+// S^T = K Q^T by 32x32x16 products of 32 tokens and 32 rows: a lane holds one row's scores of 16 tokens, so that
+// maxima and sums stay in a lane but for one exchange with the lane's partner, and the weights are the next
+// product's operand as they lie: O^T += V^T P^T, whose other operand has its tokens behind each other, as the cache
+// holds values.  The product's row i is token 16 (i / 4 % 2) + 4 (i / 8) + i % 4 of the 32: then lane l holds the scores of
+// tokens 16 (l / 32) .. + 15 in order, which is what the second product takes from it (8 at a time), and both
+// halves of a wave read whole 16-token runs of one page each.
+//
+// What is masked is left out by a choice, not by arithmetic: scores become -inf, and where a tile that some row sees in part
+// holds values that are not finite, these are taken out of the product and added to the rows that see them.
+#pragma once
+
+#include <algorithm>
+#include <type_traits>
+
+#include "cache_common.h"
+
+namespace cfp {
+
+constexpr int kFewRows = 32;    // rows of a sequence and key head that the kernel for few takes
+constexpr int kManyRows = 128;  // rows of a workgroup of the kernel for many
+constexpr int kFewStep = 32, kManyStep = 64;     // tokens of a tile
+constexpr int kFewLeast = 128, kManyLeast = 256;  // tokens of a part, at least
+
+struct AttendArgs {
+  SeqArgs s;
+  const void *q, *k, *v;
+  const uint8_t *ks, *vs;
+  int64_t kp, vp, ksp, vsp;  // strides of pages
+  int64_t qt, qh;            // strides of tokens and heads
+  void *out;
+  float *lse;
+  float *few_o, *few_ml, *many_o, *many_ml;  // parts: sums over exp(s - m), and m (in powers of two) and l
+  int32_t heads, group, dim, max_new;
+  int32_t causal, window, wide;  // wide: queries lie on 16 bytes
+  int32_t few_parts, many_parts, few_rows;
+  uint32_t tiles;  // of kManyRows rows, at most
+  float scale;     // times log2(e)
+};
+
+hipError_t attend_bf16(const AttendArgs &A, bool bytes, hipStream_t st);
+hipError_t attend_f16(const AttendArgs &A, bool bytes, hipStream_t st);
+
+#ifdef __HIPCC__
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr float kSlack = 6.f;
+constexpr float kLn2F = 0.693147180559945309f;
+
+template <typename T>
+__device__ __forceinline__ f32x16 mfma32(vec<T, 8> a, vec<T, 8> b, f32x16 c) {
+  if constexpr (std::is_same<T, bf16_t>::value)
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+
+// The other half's value.
+__device__ __forceinline__ float partner(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
+}
+
+// 8 entries of 8 bits times a power of two.
+template <typename T>
+__device__ __forceinline__ vec<T, 8> widen(u32x2 w, float s) {
+  vec<T, 8> r;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    if constexpr (std::is_same<T, bf16_t>::value) {
+      const auto a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], s, false);
+      const auto b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], s, true);
+      r[4 * i] = a[0], r[4 * i + 1] = a[1], r[4 * i + 2] = b[0], r[4 * i + 3] = b[1];
+    } else {
+      const auto a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[i], s, false);
+      const auto b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[i], s, true);
+      r[4 * i] = a[0], r[4 * i + 1] = a[1], r[4 * i + 2] = b[0], r[4 * i + 3] = b[1];
+    }
+  }
+  return r;
+}
+
+// 8 entries of 8 bits, each times a power of two of its own (scale bytes).
+template <typename T>
+__device__ __forceinline__ vec<T, 8> widen(u32x2 w, u32x2 s) {
+  vec<T, 8> r;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const auto a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i], false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i], true);
+    const float x[4] = {a[0], a[1], b[0], b[1]};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) r[4 * i + j] = (T)(x[j] * scale_of(s[i] >> (8 * j) & 0xff));
+  }
+  return r;
+}
+
+// What rows with first and last token p0 <= p1 of a sequence of `len` see, cut into parts.
+struct Span {
+  int32_t begin, end, per, parts;
+};
+template <int STEP, int LEAST>
+__device__ __forceinline__ Span span_of(const AttendArgs &A, int p0, int p1, int len, int most) {
+  Span r;
+  r.end = A.causal ? p1 + 1 : len;
+  r.begin = (A.window > 0 ? max(p0 - A.window + 1, 0) : 0) & ~(STEP - 1);
+  const int n = r.end - r.begin;
+  r.per = max(((n + most - 1) / most + STEP - 1) & ~(STEP - 1), LEAST);
+  r.parts = n > 0 ? (n + r.per - 1) / r.per : 0;
+  return r;
+}
+
+// Query of a row as the second operand: entries of its d-th piece of 8.
+template <typename T>
+__device__ __forceinline__ vec<T, 8> load_q(const T *q, int d, int dim, bool there, bool wide) {
+  vec<T, 8> r;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) r[i] = (T)0.f;
+  if (there && d < dim) {
+    if (wide) {
+      r = *reinterpret_cast<const vec<T, 8> *>(q + d);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) r[i] = q[d + i];
+    }
+  }
+  return r;
+}
+
+// What is infinite or not a number among a word's entries of type H (the first in the lowest bits): cleared in the word, and
+// its bits by sign in `up` and `down` (what is not a number is both).
+template <typename T, typename H>
+__device__ __forceinline__ uint32_t take_odd(uint32_t w, uint32_t &up, uint32_t &down) {
+  up = down = 0;
+  if constexpr (sizeof(H) == 1) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if ((w >> (8 * i) & 0x7f) == 0x7f) up |= 1u << i, down |= 1u << i, w &= ~(0xffu << (8 * i));
+  } else {
+    constexpr uint32_t kInf = std::is_same<T, bf16_t>::value ? 0x7f80 : 0x7c00;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t x = w >> (16 * i) & 0xffff;
+      if ((x & kInf) != kInf) continue;
+      if ((x & 0x7fff) != kInf || !(x & 0x8000)) up |= 1u << i;
+      if ((x & 0x7fff) != kInf || (x & 0x8000)) down |= 1u << i;
+      w &= ~(0xffffu << (16 * i));
+    }
+  }
+  return w;
+}
+// The same of 16 bytes.
+template <typename T, typename H>
+__device__ __forceinline__ void take_odd(u32x4 &w, uint32_t &up, uint32_t &down) {
+  up = down = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t u, d;
+    w[i] = take_odd<T, H>(w[i], u, d);
+    up |= u << (4 / (int)sizeof(H) * i), down |= d << (4 / (int)sizeof(H) * i);
+  }
+}
+
+// One row's running state and its scores of a tile of 16 N tokens a lane.
+template <typename T, int DP>
+struct Rows {
+  float m, l;            // l: of this lane's tokens
+  f32x16 o[DP / 32];
+  uint32_t odd[DP / 32];  // infinities to be added to an entry of o: two bits each, of either sign
+
+  __device__ __forceinline__ void clear() {
+    m = -__builtin_inff(), l = 0.f;
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i) {
+      odd[i] = 0;
+#pragma unroll
+      for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
+    }
+  }
+
+  // The tokens (a bit each) that this lane's row sees hold infinities of either sign in its entry j of o[i].
+  __device__ __forceinline__ void add_odd(int i, int j, bool up, bool down) {
+    odd[i] |= (up ? 1u : 0u) << (2 * j) | (down ? 2u : 0u) << (2 * j);
+  }
+  __device__ __forceinline__ void finish() {
+    l += partner(l);
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i)
+      if (__any(odd[i] != 0)) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          o[i][j] += odd[i] >> (2 * j) & 1 ? __builtin_inff() : 0.f;
+          o[i][j] -= odd[i] >> (2 * j) & 2 ? __builtin_inff() : 0.f;
+        }
+      }
+  }
+
+  // Scores to weights exp2(c s - m), as the next product's operands.  float16 has no bits below 2^-24, so m stays 8 below
+  // the maximum there and weights go up to 2^14.
+  template <int N>
+  __device__ __forceinline__ void weigh(f32x16 (&s)[N], float c, vec<T, 8> (&p)[2 * N]) {
+    float top = s[0][0];
+#pragma unroll
+    for (int u = 0; u < N; ++u)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[u][i]);
+    top = fmaxf(top, partner(top)) * c;
+    constexpr float kBelow = std::is_same<T, f16_t>::value ? 8.f : 0.f;
+    if (__any(top > m + (kSlack + kBelow))) {
+      const float to = top > m + (kSlack + kBelow) ? top - kBelow : m;
+      const float by = to == m ? 1.f : __builtin_amdgcn_exp2f(m - to);
+      m = to;
+      l *= by;
+#pragma unroll
+      for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) o[i][j] *= by;
+    }
+    const float from = m == -__builtin_inff() ? 0.f : m;
+    float sum = 0.f;
+#pragma unroll
+    for (int u = 0; u < N; ++u)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float e = __builtin_amdgcn_exp2f(fmaf(s[u][i], c, -from));
+        s[u][i] = e;
+        sum += e;
+      }
+    l += sum;
+#pragma unroll
+    for (int u = 0; u < N; ++u)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) p[2 * u + i / 8][i % 8] = (T)s[u][i];
+  }
+};
+
+// The lowest n of 32 bits, all for n >= 32 and none for n <= 0.
+__device__ __forceinline__ uint32_t bits_of(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1; }
+
+// Scores that a lane's row does not see; `bad`: the lane's 16 tokens have no page.
+__device__ __forceinline__ void mask16(f32x16 &s, int first, int lo, int hi, bool bad) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const float x = bad ? __builtin_nanf("") : s[i];
+    s[i] = first + i >= lo && first + i <= hi ? x : -__builtin_inff();
+  }
+}
+
+// ---- few rows: a workgroup takes a part of one sequence's tokens for one key head and up to 32 rows.  Each of its
+// four waves takes every fourth tile of 32 tokens, operands from memory straight to the matrix instructions'
+// registers (16 bytes a lane, the next tile's keys loaded while this one's scores become weights, its values
+// while the next scores are made), and a state of its own; the four meet in LDS.
+template <typename T, bool BYTES, int DP>
+__global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_few_kernel(AttendArgs A) {
+  typedef std::conditional_t<BYTES, uint8_t, T> H;
+  typedef vec<T, 8> Vec8;
+  constexpr int kK = BYTES ? DP / 32 : DP / 16, kLd = DP + 4;
+  extern __shared__ __align__(16) float shared[];
+  __shared__ float ml[2][4][kFewRows];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 31, h = lane >> 5;
+  uint32_t id = block_id();
+  const int part = (int)(id % A.few_parts);
+  id /= A.few_parts;
+  const int head = (int)(id % A.heads), b = (int)(id / A.heads);
+  if (b >= A.s.n_seqs) return;
+  const Seq sq = seq_of(A.s, b);
+  const int64_t rows64 = (int64_t)sq.n * A.group;
+  const bool lost = sq.n > A.max_new || (sq.pos + sq.n) > (A.s.width << A.s.page_shift);
+  const int g = A.group, hq = A.heads * g, D = A.dim;
+  T *out = reinterpret_cast<T *>(A.out);
+  if (lost) {  // too long for its table, or more rows than the call was laid out for
+    if (part == 0)
+      for (int64_t e = threadIdx.x; e < rows64 * D; e += 256) {
+        const int64_t r = e / D;
+        const int64_t row = (sq.row + r / g) * hq + head * g + r % g;
+        out[row * D + e % D] = (T)__builtin_nanf("");
+        if (e % D == 0 && A.lse) A.lse[row] = __builtin_nanf("");
+      }
+    return;
+  }
+  if (rows64 == 0 || rows64 > kFewRows) return;
+  const int rows = (int)rows64, len = sq.pos + sq.n;
+  const Span sp = span_of<kFewStep, kFewLeast>(A, sq.pos, len - 1, len, A.few_parts);
+  if (part >= max(sp.parts, 1)) return;
+  const int i = col / g;
+  const int p = sq.pos + i;
+  const bool mine = col < rows;
+  const int hi = mine ? (A.causal ? p : len - 1) : -1, lo = A.window > 0 ? p - A.window + 1 : 0;
+  const int all_hi = A.causal ? sq.pos : len - 1, all_lo = A.window > 0 ? len - A.window : 0;  // seen by all rows
+
+  vec<T, 8> q[DP / 16];
+  const T *qp = reinterpret_cast<const T *>(A.q) + (int64_t)(sq.row + i) * A.qt + (int64_t)(head * g + col % g) * A.qh;
+#pragma unroll
+  for (int c = 0; c < DP / 16; ++c)
+    q[c] = load_q<T>(qp, BYTES ? 32 * (c / 2) + 16 * h + 8 * (c % 2) : 16 * c + 8 * h, D, mine, A.wide != 0);
+
+  const int page = 1 << A.s.page_shift, inner = page - 1;
+  const int ki = 16 * (col >> 2 & 1) + 4 * (col >> 3) + (col & 3);  // token of this lane's key
+  u32x4 kr[kK], vr[DP / 32][BYTES ? 1 : 2], vsr;
+  uint32_t ksr = 0;
+  const int end = min(sp.end, sp.begin + (part + 1) * sp.per);
+
+  struct Pages {
+    uint32_t at[2];
+    bool ok[2];
+  };
+  auto pages = [&](int t) {
+    Pages r;
+    r.at[0] = page_of(A.s, b, t, r.ok[0]);
+    r.at[1] = page_of(A.s, b, t + 16, r.ok[1]);
+    return r;
+  };
+  auto load_k = [&](int t, const Pages &pg) {
+    const uint32_t at = col & 4 ? pg.at[1] : pg.at[0];
+    const int place = (t + ki) & inner;
+    const H *kp = reinterpret_cast<const H *>(A.k) + at * A.kp + (int64_t)(head * page + place) * D;
+#pragma unroll
+    for (int c = 0; c < kK; ++c) {
+      const int d = BYTES ? 32 * c + 16 * h : 16 * c + 8 * h;
+      u32x4 w = {0, 0, 0, 0};
+      if (d < D) w = *reinterpret_cast<const u32x4 *>(kp + d);
+      kr[c] = w;
+    }
+    if constexpr (BYTES) ksr = A.ks[at * A.ksp + head * page + place];
+  };
+  auto load_v = [&](int t, const Pages &pg) {
+    const uint32_t at = h ? pg.at[1] : pg.at[0];
+    const int place = (t + 16 * h) & inner;
+    const H *vp = reinterpret_cast<const H *>(A.v) + at * A.vp + (int64_t)head * D * page + place;
+#pragma unroll
+    for (int mt = 0; mt < DP / 32; ++mt) {
+      const int d = 32 * mt + col;
+#pragma unroll
+      for (int j = 0; j < (BYTES ? 1 : 2); ++j) {
+        u32x4 w = {0, 0, 0, 0};
+        if (d < D) w = *reinterpret_cast<const u32x4 *>(vp + (int64_t)d * page + 8 * j);
+        vr[mt][j] = w;
+      }
+    }
+    if constexpr (BYTES) vsr = *reinterpret_cast<const u32x4 *>(A.vs + at * A.vsp + head * page + place);
+  };
+
+  Rows<T, DP> st;
+  st.clear();
+  uint32_t *odds = reinterpret_cast<uint32_t *>(shared) + wave * 2 * DP;
+  int t = sp.begin + part * sp.per + 32 * wave;
+  if (t < end) {
+    Pages now = pages(t), next = now;
+    load_k(t, now);
+    load_v(t, now);
+    if (t + 128 < end) next = pages(t + 128);
+    for (; t < end; t += 128) {
+      Pages later = next;
+      if (t + 256 < end) later = pages(t + 256);
+      f32x16 s[1];
+#pragma unroll
+      for (int j = 0; j < 16; ++j) s[0][j] = 0.f;
+      if constexpr (BYTES) {
+        const float by = scale_of(ksr);
+#pragma unroll
+        for (int c = 0; c < kK; ++c) {
+          s[0] = mfma32<T>(widen<T>(u32x2{kr[c][0], kr[c][1]}, by), q[2 * c], s[0]);
+          s[0] = mfma32<T>(widen<T>(u32x2{kr[c][2], kr[c][3]}, by), q[2 * c + 1], s[0]);
+        }
+      } else {
+#pragma unroll
+        for (int c = 0; c < kK; ++c) s[0] = mfma32<T>(__builtin_bit_cast(Vec8, kr[c]), q[c], s[0]);
+      }
+      if (t + 128 < end) load_k(t + 128, next);
+      const bool edge = t + 31 > all_hi || t < all_lo || !now.ok[0] || !now.ok[1];
+      const int first = t + 16 * h;
+      if (edge) mask16(s[0], first, lo, hi, !(h ? now.ok[1] : now.ok[0]));
+      vec<T, 8> w[2];
+      st.weigh(s, A.scale, w);
+      if (edge) {
+        bool any = false;
+#pragma unroll
+        for (int mt = 0; mt < DP / 32; ++mt) {
+          uint32_t up, down;
+          if constexpr (BYTES) {
+            take_odd<T, H>(vr[mt][0], up, down);
+          } else {
+            uint32_t up1, down1;
+            take_odd<T, H>(vr[mt][0], up, down);
+            take_odd<T, H>(vr[mt][1], up1, down1);
+            up |= up1 << 8, down |= down1 << 8;
+          }
+          odds[h * DP + 32 * mt + col] = up | down << 16;
+          any = any || up != 0 || down != 0;
+        }
+        if (__any(any)) {
+          __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+          __builtin_amdgcn_wave_barrier();
+          __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+          const uint32_t sees = bits_of(hi + 1 - t) & ~bits_of(lo - t);
+#pragma unroll
+          for (int mt = 0; mt < DP / 32; ++mt)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+              const int d = 32 * mt + 8 * (j / 4) + 4 * h + j % 4;
+              const uint32_t a = odds[d], b = odds[DP + d];
+              st.add_odd(mt, j, ((a & 0xffff) | b << 16) & sees, (a >> 16 | (b & 0xffff0000)) & sees);
+            }
+        }
+      }
+#pragma unroll
+      for (int mt = 0; mt < DP / 32; ++mt)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          vec<T, 8> v;
+          if constexpr (BYTES)
+            v = widen<T>(u32x2{vr[mt][0][2 * j], vr[mt][0][2 * j + 1]}, u32x2{vsr[2 * j], vsr[2 * j + 1]});
+          else
+            v = __builtin_bit_cast(Vec8, vr[mt][j]);
+          st.o[mt] = mfma32<T>(v, w[j], st.o[mt]);
+        }
+      if (t + 128 < end) load_v(t + 128, next);
+      now = next, next = later;
+    }
+  }
+
+  // the waves' states together
+  st.finish();
+  if (h == 0) ml[0][wave][col] = st.m, ml[1][wave][col] = st.l;
+  __syncthreads();
+  float top = ml[0][0][col];
+#pragma unroll
+  for (int w = 1; w < 4; ++w) top = fmaxf(top, ml[0][w][col]);
+  const float by = st.m == top ? 1.f : __builtin_amdgcn_exp2f(st.m - top);
+  if (mine) {
+    float *to = shared + (wave * A.few_rows + col) * kLd + 4 * h;
+#pragma unroll
+    for (int mt = 0; mt < DP / 32; ++mt)
+#pragma unroll
+      for (int a = 0; a < 4; ++a) {
+        vec<float, 4> x;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = st.o[mt][4 * a + j] * by;
+        *reinterpret_cast<vec<float, 4> *>(to + 32 * mt + 8 * a) = x;
+      }
+  }
+  __syncthreads();
+  const int quads = D / 4;
+  const bool whole = sp.parts <= 1;
+  const int64_t slot = ((int64_t)(b * A.heads + head) * A.few_parts + part) * A.few_rows;
+  for (int e = threadIdx.x; e < rows * quads; e += 256) {
+    const int r = e / quads, d = e % quads * 4;
+    float top = ml[0][0][r];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) top = fmaxf(top, ml[0][w][r]);
+    float l = 0.f;
+    vec<float, 4> o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      l += ml[1][w][r] * (ml[0][w][r] == top ? 1.f : __builtin_amdgcn_exp2f(ml[0][w][r] - top));
+      o += *reinterpret_cast<const vec<float, 4> *>(shared + (w * A.few_rows + r) * kLd + d);
+    }
+    if (whole) {
+      const int64_t row = (int64_t)(sq.row + r / g) * hq + head * g + r % g;
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      const float y[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+      store_vec<T, 4>(out + row * D + d, y);
+      if (d == 0 && A.lse) A.lse[row] = (top + __builtin_amdgcn_logf(l)) * kLn2F;
+    } else {
+      *reinterpret_cast<vec<float, 4> *>(A.few_o + (slot + r) * D + d) = o;
+      if (d == 0) A.few_ml[2 * (slot + r)] = top, A.few_ml[2 * (slot + r) + 1] = l;
+    }
+  }
+}
+
+// ---- many rows: a workgroup takes 128 rows of one sequence and key head, 32 a wave, over tiles of 64 tokens whose keys
+// and values lie in LDS (two tiles, so that the next one's lands while this one is worked on).
+template <typename T, bool BYTES, int DP>
+__global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many_kernel(AttendArgs A) {
+  typedef std::conditional_t<BYTES, uint8_t, T> H;
+  // rows of LDS are 16 bytes longer than their entries: then 16 lanes that read one piece of 16 rows meet all banks
+  constexpr int kKLd = DP + 8, kVLd = kManyStep + 8;
+  constexpr int kTile = kManyStep * kKLd + DP * kVLd;
+  constexpr int kPer = BYTES ? 16 : 8;                       // entries of a piece of 16 bytes in memory
+  constexpr int kAll = kManyStep * DP / kPer, kPieces = (kAll + 255) / 256;  // pieces of a tile's keys, of a thread
+  extern __shared__ __align__(16) char shared_bytes[];
+  T *lds = reinterpret_cast<T *>(shared_bytes);
+  // of a tile that some row sees in part: the tokens whose values are not finite, a bit each, [2][DP][sign][8 bytes], and
+  // in odd_at the tile (its first token + 1) that last had any
+  uint8_t *odds = reinterpret_cast<uint8_t *>(lds + 2 * kTile);
+  volatile int *odd_at = reinterpret_cast<volatile int *>(odds + 2 * DP * 16);
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, h = lane >> 5;
+  uint32_t id = block_id();
+  const int head = (int)(id % A.heads);
+  id /= A.heads;
+  const int part = (int)(id % A.many_parts);
+  id /= A.many_parts;
+  if (id >= A.tiles) return;
+  int b;
+  uint32_t tile;
+  const int g = A.group, hq = A.heads * g, D = A.dim;
+  if (!find_unit(A.s.n_seqs, A.tiles - 1 - id, [&](int i) {
+        const Seq s = seq_of(A.s, i);
+        const int64_t r = (int64_t)s.n * g;
+        return r > kFewRows && s.n <= A.max_new ? (uint32_t)((r + kManyRows - 1) / kManyRows) : 0u;
+      }, b, tile))
+    return;
+  b = __builtin_amdgcn_readfirstlane(b);
+  const Seq sq = seq_of(A.s, b);
+  const int len = sq.pos + sq.n, rows = sq.n * g;
+  if (len > (A.s.width << A.s.page_shift)) return;  // the kernel for few writes what such rows become
+  const int r0 = (int)tile * kManyRows, r1 = min(r0 + kManyRows, rows);
+  const int p0 = sq.pos + r0 / g, p1 = sq.pos + (r1 - 1) / g;
+  const Span sp = span_of<kManyStep, kManyLeast>(A, p0, p1, len, A.many_parts);
+  if (part >= max(sp.parts, 1)) return;
+  const int r = r0 + wave * 32 + col;
+  const bool mine = r < rows;
+  const int i = r / g, p = sq.pos + i;
+  const int hi = mine ? (A.causal ? p : len - 1) : -1, lo = A.window > 0 ? p - A.window + 1 : 0;
+  const int all_hi = A.causal ? p0 : len - 1, all_lo = A.window > 0 ? p1 - A.window + 1 : 0;
+
+  vec<T, 8> q[DP / 16];
+  const T *qp = reinterpret_cast<const T *>(A.q) + (int64_t)(sq.row + i) * A.qt + (int64_t)(head * g + r % g) * A.qh;
+#pragma unroll
+  for (int c = 0; c < DP / 16; ++c) q[c] = load_q<T>(qp, 16 * c + 8 * h, D, mine, A.wide != 0);
+
+  const int page = 1 << A.s.page_shift, inner = page - 1;
+  u32x4 kr[kPieces], vr[kPieces], vsr = {0, 0, 0, 0};
+  uint32_t ksr[BYTES ? kPieces : 1];
+  struct Pages {
+    uint32_t at[4];
+    bool ok[4];
+  };
+  auto pages = [&](int t) {
+    Pages r;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) r.at[j] = page_of(A.s, b, t + 16 * j, r.ok[j]);
+    return r;
+  };
+  auto pick = [&](const Pages &pg, int j) { return j & 2 ? (j & 1 ? pg.at[3] : pg.at[2]) : (j & 1 ? pg.at[1] : pg.at[0]); };
+  constexpr int kKRow = DP / kPer, kVRow = kManyStep / kPer;  // pieces of a row
+  auto load = [&](int t, const Pages &pg) {
+#pragma unroll
+    for (int e = 0; e < kPieces; ++e) {
+      const int n = e * 256 + tid;
+      {
+        const int row = n / kKRow, d = n % kKRow * kPer;
+        const int64_t at = pick(pg, row >> 4 & 3);
+        const int place = (t + row) & inner;
+        if (n < kAll && d < D) kr[e] = *reinterpret_cast<const u32x4 *>(reinterpret_cast<const H *>(A.k) + at * A.kp + (int64_t)(head * page + place) * D + d);
+        if constexpr (BYTES) ksr[e] = A.ks[at * A.ksp + head * page + place];  // n >= kAll: of another row, not used
+      }
+      {
+        const int d = n / kVRow, tok = n % kVRow * kPer;
+        const int64_t at = pick(pg, tok >> 4);
+        const int place = (t + tok) & inner;
+        if (n < kAll && d < D) vr[e] = *reinterpret_cast<const u32x4 *>(reinterpret_cast<const H *>(A.v) + at * A.vp + (int64_t)(head * D + d) * page + place);
+        if constexpr (BYTES)
+          if (e == 0) vsr = *reinterpret_cast<const u32x4 *>(A.vs + at * A.vsp + head * page + place);
+      }
+    }
+  };
+  // whether some row does not see all of the tokens from t on
+  auto partly = [&](int t) { return t + kManyStep - 1 > all_hi || t < all_lo; };
+  auto store = [&](int buf, int t) {
+    T *k = lds + buf * kTile, *v = k + kManyStep * kKLd;
+    const bool edge = partly(t);
+#pragma unroll
+    for (int e = 0; e < kPieces; ++e) {
+      const int n = e * 256 + tid;
+      {
+        const int row = n / kKRow, d = n % kKRow * kPer;
+        T *to = k + row * kKLd + d;
+        if (n < kAll && d < D) {
+          if constexpr (BYTES) {
+            const float by = scale_of(ksr[e]);
+            *reinterpret_cast<vec<T, 8> *>(to) = widen<T>(u32x2{kr[e][0], kr[e][1]}, by);
+            *reinterpret_cast<vec<T, 8> *>(to + 8) = widen<T>(u32x2{kr[e][2], kr[e][3]}, by);
+          } else {
+            *reinterpret_cast<u32x4 *>(to) = kr[e];
+          }
+        }
+      }
+      {
+        const int d = n / kVRow, tok = n % kVRow * kPer;
+        T *to = v + d * kVLd + tok;
+        if (n < kAll && d < D) {
+          if (edge) {
+            uint32_t up, down;
+            take_odd<T, H>(vr[e], up, down);
+            uint8_t *at = odds + (buf * DP + d) * 16 + tok / 8;
+            at[0] = (uint8_t)up, at[8] = (uint8_t)down;
+            if constexpr (BYTES) at[1] = (uint8_t)(up >> 8), at[9] = (uint8_t)(down >> 8);
+            if (up | down) odd_at[buf] = t + 1;
+          }
+          if constexpr (BYTES) {
+            *reinterpret_cast<vec<T, 8> *>(to) = widen<T>(u32x2{vr[e][0], vr[e][1]}, u32x2{vsr[0], vsr[1]});
+            *reinterpret_cast<vec<T, 8> *>(to + 8) = widen<T>(u32x2{vr[e][2], vr[e][3]}, u32x2{vsr[2], vsr[3]});
+          } else {
+            *reinterpret_cast<u32x4 *>(to) = vr[e];
+          }
+        }
+      }
+    }
+  };
+
+  Rows<T, DP> st;
+  st.clear();
+  int t = sp.begin + part * sp.per;
+  const int end = min(sp.end, t + sp.per);
+  if (t < end) {
+    if (tid < 2) odd_at[tid] = 0;
+    if (D < DP)  // what no entry is written to is zero
+      for (int e = tid; e < 2 * kTile / 8; e += 256) reinterpret_cast<u32x4 *>(lds)[e] = u32x4{0, 0, 0, 0};
+    __syncthreads();
+    Pages now = pages(t), next = now;
+    load(t, now);
+    if (t + kManyStep < end) next = pages(t + kManyStep);
+    store(0, t);
+    int buf = 0;
+    for (; t < end; t += kManyStep) {
+      const bool more = t + kManyStep < end;
+      Pages later = next;
+      if (t + 2 * kManyStep < end) later = pages(t + 2 * kManyStep);
+      if (more) load(t + kManyStep, next);
+      __syncthreads();
+      const T *k = lds + buf * kTile, *v = k + kManyStep * kKLd;
+      f32x16 s[2];
+      const int ki = 16 * (col >> 2 & 1) + 4 * (col >> 3) + (col & 3);
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) s[u][j] = 0.f;
+#pragma unroll
+      for (int c = 0; c < DP / 16; ++c)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+          s[u] = mfma32<T>(*reinterpret_cast<const vec<T, 8> *>(k + (32 * u + ki) * kKLd + 16 * c + 8 * h), q[c], s[u]);
+      const bool edge = partly(t) || !(now.ok[0] && now.ok[1] && now.ok[2] && now.ok[3]);
+      const int first = t + 16 * h;
+      if (edge) {
+        mask16(s[0], first, lo, hi, !(h ? now.ok[1] : now.ok[0]));
+        mask16(s[1], first + 32, lo, hi, !(h ? now.ok[3] : now.ok[2]));
+      }
+      vec<T, 8> w[4];
+      st.weigh(s, A.scale, w);
+      if (partly(t) && odd_at[buf] == t + 1) {
+        const uint32_t sees[2] = {bits_of(hi + 1 - t) & ~bits_of(lo - t), bits_of(hi + 1 - t - 32) & ~bits_of(lo - t - 32)};
+#pragma unroll
+        for (int mt = 0; mt < DP / 32; ++mt)
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            const u32x4 x = *reinterpret_cast<const u32x4 *>(odds + (buf * DP + 32 * mt + 8 * (j / 4) + 4 * h + j % 4) * 16);
+            st.add_odd(mt, j, (x[0] & sees[0]) | (x[1] & sees[1]), (x[2] & sees[0]) | (x[3] & sees[1]));
+          }
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int mt = 0; mt < DP / 32; ++mt)
+          st.o[mt] = mfma32<T>(*reinterpret_cast<const vec<T, 8> *>(v + (32 * mt + col) * kVLd + 32 * (j / 2) + 8 * (j % 2) + 16 * h),
+                               w[j], st.o[mt]);
+      buf ^= 1;
+      if (more) store(buf, t + kManyStep);
+      now = next, next = later;
+    }
+  }
+  st.finish();
+  if (!mine) return;
+  const int64_t row = (int64_t)(sq.row + i) * hq + head * g + r % g;
+  const bool whole = sp.parts <= 1;
+  if (whole) {
+    const float inv = st.l == 0.f ? 0.f : 1.f / st.l;
+    T *to = reinterpret_cast<T *>(A.out) + row * D + 4 * h;
+#pragma unroll
+    for (int mt = 0; mt < DP / 32; ++mt)
+#pragma unroll
+      for (int a = 0; a < 4; ++a) {
+        const float y[4] = {st.o[mt][4 * a] * inv, st.o[mt][4 * a + 1] * inv, st.o[mt][4 * a + 2] * inv, st.o[mt][4 * a + 3] * inv};
+        if (32 * mt + 8 * a + 4 * h < D) store_vec<T, 4>(to + 32 * mt + 8 * a, y);
+      }
+    if (h == 0 && A.lse) A.lse[row] = (st.m + __builtin_amdgcn_logf(st.l)) * kLn2F;
+  } else {
+    const int64_t at = part * A.s.n_tokens * hq + row;
+    float *to = A.many_o + at * D + 4 * h;
+#pragma unroll
+    for (int mt = 0; mt < DP / 32; ++mt)
+#pragma unroll
+      for (int a = 0; a < 4; ++a) {
+        const float y[4] = {st.o[mt][4 * a], st.o[mt][4 * a + 1], st.o[mt][4 * a + 2], st.o[mt][4 * a + 3]};
+        if (32 * mt + 8 * a + 4 * h < D) store_vec<float, 4>(to + 32 * mt + 8 * a, y);
+      }
+    if (h == 0) A.many_ml[2 * at] = st.m, A.many_ml[2 * at + 1] = st.l;
+  }
+}
+
+// ---- the parts of a row together, in their order: a thread takes four entries of one row.
+template <typename T>
+__global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs A) {
+  const int hq = A.heads * A.group, g = A.group, D = A.dim, quads = D / 4;
+  const uint32_t blocks = (uint32_t)((int64_t)hq * quads + 255) / 256;
+  const uint32_t id = block_id();
+  const int64_t row = id / blocks;  // token
+  if (row >= A.s.n_tokens) return;
+  int b;
+  uint32_t k;
+  if (row < A.s.starts[0] || !find_unit(A.s.n_seqs, (uint32_t)(row - A.s.starts[0]), [&](int i) { return (uint32_t)seq_of(A.s, i).n; }, b, k)) return;
+  const Seq sq = seq_of(A.s, b);
+  const int len = sq.pos + sq.n, e = (int)(id % blocks) * 256 + threadIdx.x;
+  if (sq.n > A.max_new || len > (A.s.width << A.s.page_shift) || e >= hq * quads) return;
+  const int head = e / quads, d = e % quads * 4;
+  const int i = (int)k, r = i * g + head % g, rows = sq.n * g;
+  const bool few = rows <= kFewRows;
+  if (few ? A.few_parts == 1 : A.many_parts == 1) return;
+  Span sp;
+  int64_t at, step;
+  if (few) {
+    sp = span_of<kFewStep, kFewLeast>(A, sq.pos, len - 1, len, A.few_parts);
+    at = (int64_t)(b * A.heads + head / g) * A.few_parts * A.few_rows + r, step = A.few_rows;
+  } else {
+    const int r0 = r / kManyRows * kManyRows, r1 = min(r0 + kManyRows, rows);
+    sp = span_of<kManyStep, kManyLeast>(A, sq.pos + r0 / g, sq.pos + (r1 - 1) / g, len, A.many_parts);
+    at = (int64_t)(sq.row + i) * hq + head, step = A.s.n_tokens * hq;
+  }
+  if (sp.parts <= 1) return;
+  const float *po = few ? A.few_o : A.many_o, *pm = few ? A.few_ml : A.many_ml;
+  float top = -__builtin_inff();
+  for (int s = 0; s < sp.parts; ++s) top = fmaxf(top, pm[2 * (at + s * step)]);
+  float l = 0.f;
+  vec<float, 4> o = {0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < sp.parts; ++s) {
+    const int64_t a = at + s * step;
+    const float m = pm[2 * a], by = m == top ? 1.f : __builtin_amdgcn_exp2f(m - top);
+    l += pm[2 * a + 1] * by;
+    o += *reinterpret_cast<const vec<float, 4> *>(po + a * D + d) * by;
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const float y[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+  const int64_t to = ((int64_t)(sq.row + i) * hq + head);
+  store_vec<T, 4>(reinterpret_cast<T *>(A.out) + to * D + d, y);
+  if (d == 0 && A.lse) A.lse[to] = (top + __builtin_amdgcn_logf(l)) * kLn2F;
+}
+
+template <typename T, bool BYTES, int DP>
+hipError_t attend_run(const AttendArgs &A, hipStream_t st) {
+  const size_t few = (size_t)4 * 4 * std::max(A.few_rows * (DP + 4), 2 * DP);
+  const size_t many = (size_t)2 * (kManyStep * (DP + 8) + DP * (kManyStep + 8)) * 2 + 2 * DP * 16 + 16;
+  auto *few_kernel = attend_few_kernel<T, BYTES, DP>;
+  auto *many_kernel = attend_many_kernel<T, BYTES, DP>;
+  for (int i = 0; i < 2; ++i)  // LDS beyond 64 KiB is asked for
+    if ((i ? many : few) > 65536 && (i == 0 || A.tiles)) {
+      const hipError_t e = hipFuncSetAttribute(i ? reinterpret_cast<const void *>(many_kernel) : reinterpret_cast<const void *>(few_kernel),
+                                               hipFuncAttributeMaxDynamicSharedMemorySize, (int)(i ? many : few));
+      if (e != hipSuccess) return e;
+    }
+  few_kernel<<<grid_of((int64_t)A.s.n_seqs * A.heads * A.few_parts), 256, few, st>>>(A);
+  if (A.tiles) many_kernel<<<grid_of((int64_t)A.tiles * A.heads * A.many_parts), 256, many, st>>>(A);
+  if (A.few_parts > 1 || A.many_parts > 1) {
+    const int64_t blocks = ((int64_t)A.heads * A.group * (A.dim / 4) + 255) / 256;
+    attend_join_kernel<T><<<grid_of(A.s.n_tokens * blocks), 256, 0, st>>>(A);
+  }
+  return hipGetLastError();
+}
+
+template <typename T, bool BYTES>
+hipError_t attend_dim(const AttendArgs &A, hipStream_t st) {
+  if (A.dim <= 64) return attend_run<T, BYTES, 64>(A, st);
+  if (A.dim <= 96) return attend_run<T, BYTES, 96>(A, st);
+  if (A.dim <= 128) return attend_run<T, BYTES, 128>(A, st);
+  if (A.dim <= 192) return attend_run<T, BYTES, 192>(A, st);
+  return attend_run<T, BYTES, 256>(A, st);
+}
+
+#endif  // __HIPCC__
+
+}  // namespace cfp

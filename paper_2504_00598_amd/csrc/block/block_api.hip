@@ -1,6 +1,8 @@
 // Exported C ABI of libcfp_block: argument checks and launches.  Every check is
 // made on the host before the first HIP call.
-#include "block_common.h"
+#include <cmath>
+
+#include "cache_common.h"
 
 namespace cfp {
 namespace {
@@ -23,6 +25,32 @@ int check_qk(const cfp_qk_desc *d) {
   if ((d->n_q && !d->q) || (d->n_k && !d->k)) return CFP_ERR_ARG;
   if (d->rot && (!d->cos || !d->sin || (!d->pos && d->n_tokens > d->n_pos))) return CFP_ERR_ARG;
   return CFP_OK;
+}
+
+int check_axes(const cfp_qk_desc *d, const uint8_t *axis, int n_axes) {
+  if (int e = check_qk(d)) return e;
+  if (n_axes < 1 || (d->rot && !axis) || (d->n_tokens > 0 && d->rot && !d->pos)) return CFP_ERR_ARG;
+  if (n_axes > CFP_QK_MAX_AXES) return CFP_ERR_UNSUPPORTED;
+  for (int i = 0; i < d->rot / 2; ++i)
+    if (axis[i] >= n_axes) return CFP_ERR_ARG;
+  return CFP_OK;
+}
+
+int qk_fwd(const cfp_qk_desc &d, const uint8_t *axis, int n_axes, void *yq, void *yk, void *stream) {
+  if (d.n_tokens == 0 || d.n_q + d.n_k == 0) return CFP_OK;
+  if ((d.n_q && !yq) || (d.n_k && !yk)) return CFP_ERR_ARG;
+  return status(launch_qk_fwd(d, d.rot ? axis : nullptr, n_axes, yq, yk, (hipStream_t)stream));
+}
+
+int qk_bwd(const cfp_qk_desc &d, const uint8_t *axis, int n_axes, const void *dyq, HeadStrides sq, const void *dyk,
+           HeadStrides sk, void *dq, void *dk, float *dwq, float *dwk, void *ws, size_t ws_bytes, void *stream) {
+  const bool none = d.n_tokens == 0;
+  if (!none && ((d.n_q && (!dyq || !dq)) || (d.n_k && (!dyk || !dk)))) return CFP_ERR_ARG;
+  const size_t need = none || d.n_q + d.n_k == 0 ? 0 : qk_bwd_bytes(d);
+  if (need && (!ws || ws_bytes < need)) return CFP_ERR_WORKSPACE;
+  if (need && !on(ws, 4)) return CFP_ERR_ARG;
+  return status(launch_qk_bwd(d, d.rot ? axis : nullptr, n_axes, dyq, dyk, sq, sk, dq, dk, dwq, dwk, (float *)ws,
+                              (hipStream_t)stream));
 }
 
 int check_route(const cfp_route_desc *d) {
@@ -59,6 +87,59 @@ int check_experts(const cfp_experts_desc *d) {
   return CFP_OK;
 }
 
+bool half_type(int t) { return t == CFP_DT_F16 || t == CFP_DT_BF16; }
+
+int check_cache(const cfp_cache_desc *c) {
+  if (!c || c->n_pages < 1 || c->page < 1 || c->heads < 1 || c->dim < 1 || !c->k || !c->v ||
+      (!half_type(c->dtype) && c->dtype != CFP_DT_E4M3))
+    return CFP_ERR_ARG;
+  if (c->n_pages > 0x7fffffff || c->page < 16 || c->page > CFP_CACHE_MAX_PAGE || (c->page & (c->page - 1)) ||
+      c->dim > CFP_CACHE_MAX_DIM || c->dim % 16 || (int64_t)c->heads * c->dim * c->page >= kMaxTokens)
+    return CFP_ERR_UNSUPPORTED;
+  const int64_t inner = (int64_t)c->heads * c->page * c->dim, scales = (int64_t)c->heads * c->page;
+  const bool several = c->n_pages > 1;
+  if (!on(c->k, 16) || !on(c->v, 16) || (several && (c->k_page_stride < inner || c->v_page_stride < inner ||
+                                                      c->k_page_stride % 16 || c->v_page_stride % 16)))
+    return CFP_ERR_ARG;
+  if (c->dtype == CFP_DT_E4M3 &&
+      (!c->k_scale || !c->v_scale || !on(c->k_scale, 16) || !on(c->v_scale, 16) ||
+       (several && (c->k_scale_page_stride < scales || c->v_scale_page_stride < scales || c->k_scale_page_stride % 16 ||
+                    c->v_scale_page_stride % 16))))
+    return CFP_ERR_ARG;
+  return CFP_OK;
+}
+
+int check_sequences(const cfp_sequences_desc *s, const cfp_cache_desc &c, int64_t n_tokens) {
+  if (!s || s->n_seqs < 0 || s->width < 0 || n_tokens < 0 || s->max_new < 0) return CFP_ERR_ARG;
+  if (n_tokens >= kMaxTokens || n_tokens * c.heads >= kMaxTokens || (int64_t)s->n_seqs * c.heads >= kMaxTokens / 4 ||
+      (int64_t)s->width * c.page >= (int64_t)1 << 30)
+    return CFP_ERR_UNSUPPORTED;
+  if (s->n_seqs > 0 && n_tokens > 0 &&
+      (!s->starts || !s->lengths || (s->width && !s->table) || (s->n_seqs > 1 && s->table_stride < s->width)))
+    return CFP_ERR_ARG;
+  return CFP_OK;
+}
+
+int check_rows(const cfp_cache_desc *c, const cfp_sequences_desc *s, int64_t n_tokens, int dtype) {
+  if (int e = check_cache(c)) return e;
+  if (int e = check_sequences(s, *c, n_tokens)) return e;
+  if (!half_type(dtype)) return CFP_ERR_ARG;
+  return c->dtype != CFP_DT_E4M3 && c->dtype != dtype ? CFP_ERR_UNSUPPORTED : CFP_OK;
+}
+
+int check_attend(const cfp_attend_desc *a, const cfp_cache_desc *c, const cfp_sequences_desc *s) {
+  if (!a) return CFP_ERR_ARG;
+  if (int e = check_rows(c, s, a->n_tokens, a->dtype)) return e;
+  if (a->n_q < 1 || a->n_q % c->heads || !(a->scale > 0.f) || !std::isfinite(a->scale) || a->window < 0) return CFP_ERR_ARG;
+  // a row's entries are counted in 32 bits where a workgroup's are
+  if (a->n_tokens * a->n_q >= kMaxTokens || (int64_t)a->n_q * c->dim >= kMaxTokens ||
+      a->n_tokens * (((int64_t)a->n_q * c->dim / 4 + 255) / 256) >= kMaxTokens)
+    return CFP_ERR_UNSUPPORTED;
+  return a->n_tokens > 0 && !a->q ? CFP_ERR_ARG : CFP_OK;
+}
+
+bool nothing(const cfp_sequences_desc &s, int64_t n_tokens) { return n_tokens == 0 || s.n_seqs == 0; }
+
 }  // namespace
 }  // namespace cfp
 
@@ -69,9 +150,7 @@ extern "C" {
 
 int cfp_qk_norm_rope(const cfp_qk_desc *d, void *yq, void *yk, void *stream) {
   if (int e = check_qk(d)) return e;
-  if (d->n_tokens == 0 || d->n_q + d->n_k == 0) return CFP_OK;
-  if ((d->n_q && !yq) || (d->n_k && !yk)) return CFP_ERR_ARG;
-  return status(launch_qk_fwd(*d, yq, yk, (hipStream_t)stream));
+  return qk_fwd(*d, nullptr, 0, yq, yk, stream);
 }
 
 size_t cfp_qk_workspace_bytes(const cfp_qk_desc *d) {
@@ -83,13 +162,22 @@ int cfp_qk_norm_rope_bwd(const cfp_qk_desc *d, const void *dyq, int64_t dyq_toke
                          const void *dyk, int64_t dyk_token_stride, int64_t dyk_head_stride, void *dq, void *dk,
                          float *dwq, float *dwk, void *ws, size_t ws_bytes, void *stream) {
   if (int e = check_qk(d)) return e;
-  const bool none = d->n_tokens == 0;
-  if (!none && ((d->n_q && (!dyq || !dq)) || (d->n_k && (!dyk || !dk)))) return CFP_ERR_ARG;
-  const size_t need = cfp_qk_workspace_bytes(d);
-  if (need && (!ws || ws_bytes < need)) return CFP_ERR_WORKSPACE;
-  if (need && !on(ws, 4)) return CFP_ERR_ARG;
-  return status(launch_qk_bwd(*d, dyq, dyk, {dyq_token_stride, dyq_head_stride}, {dyk_token_stride, dyk_head_stride}, dq,
-                              dk, dwq, dwk, (float *)ws, (hipStream_t)stream));
+  return qk_bwd(*d, nullptr, 0, dyq, {dyq_token_stride, dyq_head_stride}, dyk, {dyk_token_stride, dyk_head_stride}, dq, dk,
+                dwq, dwk, ws, ws_bytes, stream);
+}
+
+int cfp_qk_norm_rope_axes(const cfp_qk_desc *d, const uint8_t *axis, int32_t n_axes, void *yq, void *yk, void *stream) {
+  if (int e = check_axes(d, axis, n_axes)) return e;
+  return qk_fwd(*d, axis, n_axes, yq, yk, stream);
+}
+
+int cfp_qk_norm_rope_axes_bwd(const cfp_qk_desc *d, const uint8_t *axis, int32_t n_axes, const void *dyq,
+                              int64_t dyq_token_stride, int64_t dyq_head_stride, const void *dyk, int64_t dyk_token_stride,
+                              int64_t dyk_head_stride, void *dq, void *dk, float *dwq, float *dwk, void *ws,
+                              size_t ws_bytes, void *stream) {
+  if (int e = check_axes(d, axis, n_axes)) return e;
+  return qk_bwd(*d, axis, n_axes, dyq, {dyq_token_stride, dyq_head_stride}, dyk, {dyk_token_stride, dyk_head_stride}, dq, dk,
+                dwq, dwk, ws, ws_bytes, stream);
 }
 
 int cfp_route(const cfp_route_desc *d, float *weight, int32_t *index, void *stream) {
@@ -148,6 +236,39 @@ int cfp_experts_bwd(const cfp_experts_desc *d, const void *dy, int64_t dy_stride
   }
   return status(launch_experts_bwd(*d, dy, dy_stride, (const float *)kept, dx, dw1, dw2, dweight, (uint8_t *)ws,
                                    (hipStream_t)stream));
+}
+
+int cfp_cache_write(const cfp_cache_desc *c, const cfp_sequences_desc *s, int64_t n_tokens, int32_t dtype, const void *k,
+                    int64_t k_token_stride, int64_t k_head_stride, const void *v, int64_t v_token_stride,
+                    int64_t v_head_stride, void *stream) {
+  if (int e = check_rows(c, s, n_tokens, dtype)) return e;
+  if (nothing(*s, n_tokens)) return CFP_OK;
+  if (!k || !v) return CFP_ERR_ARG;
+  return status(launch_cache_write(*c, *s, n_tokens, dtype, k, {k_token_stride, k_head_stride}, v,
+                                   {v_token_stride, v_head_stride}, (hipStream_t)stream));
+}
+
+int cfp_cache_read(const cfp_cache_desc *c, const cfp_sequences_desc *s, int64_t n_tokens, int32_t dtype, void *k, void *v,
+                   void *stream) {
+  if (int e = check_rows(c, s, n_tokens, dtype)) return e;
+  if (nothing(*s, n_tokens)) return CFP_OK;
+  if (!k || !v || !on(k, 16) || !on(v, 16)) return CFP_ERR_ARG;
+  return status(launch_cache_read(*c, *s, n_tokens, dtype, k, v, (hipStream_t)stream));
+}
+
+size_t cfp_attend_workspace_bytes(const cfp_attend_desc *a, const cfp_cache_desc *c, const cfp_sequences_desc *s) {
+  return check_attend(a, c, s) || nothing(*s, a->n_tokens) ? 0 : attend_bytes(*a, *c, *s);
+}
+
+int cfp_attend(const cfp_attend_desc *a, const cfp_cache_desc *c, const cfp_sequences_desc *s, void *out, float *lse, void *ws,
+               size_t ws_bytes, void *stream) {
+  if (int e = check_attend(a, c, s)) return e;
+  if (nothing(*s, a->n_tokens)) return CFP_OK;
+  if (!out || !on(out, 16)) return CFP_ERR_ARG;
+  const size_t need = attend_bytes(*a, *c, *s);
+  if (need && (!ws || ws_bytes < need)) return CFP_ERR_WORKSPACE;
+  if (need && !on(ws, 16)) return CFP_ERR_ARG;
+  return status(launch_attend(*a, *c, *s, out, lse, ws, (hipStream_t)stream));
 }
 
 }  // extern "C"

@@ -1,0 +1,85 @@
+// What the operators over a paged cache share: sequences, pages and the 8-bit floats.
+#pragma once
+
+#include "block_common.h"
+
+namespace cfp {
+
+struct SeqArgs {
+  const int32_t *table, *starts, *lengths;
+  int64_t table_stride, n_tokens;  // n_tokens: rows of the call
+  int32_t n_seqs, width, page_shift;
+  uint32_t n_pages;
+};
+
+inline SeqArgs seq_args(const cfp_cache_desc &c, const cfp_sequences_desc &s, int64_t n_tokens) {
+  SeqArgs a{};
+  a.table = s.table, a.starts = s.starts, a.lengths = s.lengths;
+  a.table_stride = s.table_stride, a.n_tokens = n_tokens;
+  a.n_seqs = s.n_seqs, a.width = s.width, a.n_pages = (uint32_t)c.n_pages;
+  while ((1 << a.page_shift) < c.page) ++a.page_shift;
+  return a;
+}
+
+// Rows of sequence b: first row, how many, and the token that the first one is.  What lies outside the call's rows
+// is no sequence's.
+struct Seq {
+  int32_t row, n, pos;
+};
+__device__ __forceinline__ Seq seq_of(const SeqArgs &S, int b) {
+  const int64_t from = S.starts[b], to = S.starts[b + 1];
+  Seq q;
+  q.row = (int32_t)from;
+  q.n = from >= 0 && to > from && to <= S.n_tokens ? (int32_t)(to - from) : 0;
+  q.pos = max(S.lengths[b], 0) - q.n;
+  return q;
+}
+
+// The page of token p >= 0 of sequence b, and whether it is one of the cache's (else page 0).
+__device__ __forceinline__ uint32_t page_of(const SeqArgs &S, int b, int p, bool &ok) {
+  const int at = p >> S.page_shift;
+  ok = at < S.width;
+  const uint32_t pg = ok ? (uint32_t)S.table[b * S.table_stride + at] : 0u;
+  ok = ok && pg < S.n_pages;
+  return ok ? pg : 0u;
+}
+
+// Which sequence the unit `id` belongs to, and the how-manieth of its units it is, where sequence b has units(b) of
+// them in a row.  All 64 lanes of a wave call it; false where there is no such unit.
+template <typename F>
+__device__ __forceinline__ bool find_unit(int n_seqs, uint32_t id, F units, int &b, uint32_t &k) {
+  const int lane = threadIdx.x & 63;
+  uint32_t before = 0;
+  for (int first = 0; first < n_seqs; first += 64) {
+    const uint32_t own = first + lane < n_seqs ? units(first + lane) : 0u;
+    uint32_t sum = own;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const uint32_t o = __shfl_up(sum, d, 64);
+      sum += lane >= d ? o : 0u;
+    }
+    const uint64_t past = __ballot(before + sum > id);
+    if (past) {
+      const int l = __builtin_ctzll(past);
+      b = first + l;
+      k = id - before - (__builtin_amdgcn_readfirstlane(__shfl(sum, l, 64)) - __builtin_amdgcn_readfirstlane(__shfl(own, l, 64)));
+      return true;
+    }
+    before += __builtin_amdgcn_readfirstlane(__shfl(sum, 63, 64));
+  }
+  return false;
+}
+
+// 2^(scale - 127)
+__device__ __forceinline__ float scale_of(uint32_t s) { return s ? __uint_as_float(s << 23) : 0x1p-127f; }
+
+hipError_t launch_cache_write(const cfp_cache_desc &c, const cfp_sequences_desc &s, int64_t n_tokens, int dtype, const void *k,
+                              HeadStrides sk, const void *v, HeadStrides sv, hipStream_t st);
+hipError_t launch_cache_read(const cfp_cache_desc &c, const cfp_sequences_desc &s, int64_t n_tokens, int dtype, void *k,
+                             void *v, hipStream_t st);
+
+size_t attend_bytes(const cfp_attend_desc &a, const cfp_cache_desc &c, const cfp_sequences_desc &s);
+hipError_t launch_attend(const cfp_attend_desc &a, const cfp_cache_desc &c, const cfp_sequences_desc &s, void *out, float *lse,
+                         void *ws, hipStream_t st);
+
+}  // namespace cfp

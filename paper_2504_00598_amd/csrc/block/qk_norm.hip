@@ -16,6 +16,9 @@
 // rotation stays inside a lane and only the sum of squares crosses lanes.  V is
 // the widest load that divides the halves and fits the alignment.
 //
+// With several axes a pair's position is that of its axis, two bits a pair in the arguments: a unit whose pairs share an axis
+// loads its angles as without, another one loads each by itself.
+//
 // Measured, bfloat16, 16384 tokens of 40 + 8 heads of 128: forward 87 us for 403 MB (4.6 TB/s; a copy reaches 5.2),
 // backward 131 us for 604 MB (4.6 TB/s) and 5 us for the sums of dg.  Four tokens: 4 us, the launch.
 #include <algorithm>
@@ -42,6 +45,8 @@ struct QkArgs {
   int32_t blocks_q;          // backwards: workgroups that take queries; the others take keys
   int32_t dim, rot, interleaved, wdtype;
   float eps;
+  uint32_t axis[CFP_QK_MAX_DIM / 32];  // axes: that of each pair, two bits
+  int32_t n_axes;
 };
 
 template <int V>
@@ -72,13 +77,51 @@ __device__ __forceinline__ Unit<V> unit_of(int u, int rot, int interleaved) {
   return Unit<V>{c, c + V, false};
 }
 
-// The angles' cos and sin of a unit's pairs at position p; interleaved pairs lie
+// The angles' cos and sin of a unit's pairs at position p of the tables; interleaved pairs lie
 // (0,1)(2,3).. over both chunks, so chunk a holds the first V/2 pairs.
 template <int V>
 __device__ __forceinline__ void angles(const QkArgs &A, int64_t p, int u, float (&c)[V], float (&s)[V]) {
   const int64_t o = p * (A.rot / 2) + (int64_t)u * V;
   load_vec<float, V>(A.cos + o, c);
   load_vec<float, V>(A.sin + o, s);
+}
+
+// The same of a unit of token t, in NaN where a position is outside the tables: the rotated part is not a number then.
+template <int V, bool AXES>
+__device__ __forceinline__ void angles_of(const QkArgs &A, int64_t t, int u, float (&c)[V], float (&s)[V]) {
+  if constexpr (!AXES) {
+    const int64_t p = A.pos ? A.pos[t] : t;
+    if (p >= 0 && p < A.n_pos) {
+      angles<V>(A, p, u, c, s);
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i) c[i] = s[i] = __builtin_nanf("");
+    }
+  } else {
+    int64_t at[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) at[i] = i < A.n_axes ? A.pos[i * A.n_tokens + t] : 0;
+    const uint32_t two = A.axis[u * V / 16] >> (2 * (u * V % 16)) & ((1u << 2 * V) - 1);
+    auto row = [&](uint32_t a) { return a & 2 ? (a & 1 ? at[3] : at[2]) : (a & 1 ? at[1] : at[0]); };
+    if (two == (two & 3) * (((1u << 2 * V) - 1) / 3)) {  // one axis
+      const int64_t p = row(two);
+      if (p >= 0 && p < A.n_pos) {
+        angles<V>(A, p, u, c, s);
+      } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) c[i] = s[i] = __builtin_nanf("");
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const int64_t p = row(two >> (2 * i));
+        const bool ok = p >= 0 && p < A.n_pos;
+        const int64_t o = (ok ? p : 0) * (A.rot / 2) + u * V + i;  // a rotated pair has tables of a row at least
+        c[i] = ok ? A.cos[o] : __builtin_nanf("");
+        s[i] = ok ? A.sin[o] : __builtin_nanf("");
+      }
+    }
+  }
 }
 
 // Turns the V pairs of a unit by their angles (back: by the opposite ones).
@@ -104,7 +147,7 @@ __device__ __forceinline__ void turn(float (&a)[V], float (&b)[V], const float (
   }
 }
 
-template <typename T, int V, int G, int UPL>
+template <typename T, int V, int G, int UPL, bool AXES>
 __global__ __launch_bounds__(kQkThreads) void qk_fwd_kernel(QkArgs A) {
   constexpr int kRows = kQkThreads / G;
   const int lane = threadIdx.x % G;
@@ -119,8 +162,6 @@ __global__ __launch_bounds__(kQkThreads) void qk_fwd_kernel(QkArgs A) {
   const T *x = reinterpret_cast<const T *>(A.x[which]) + t * A.sx[which].tok + head * A.sx[which].head;
   T *y = reinterpret_cast<T *>(A.out[which]) + (t * A.heads[which] + head) * A.dim;
   const int D = A.dim;
-  const int64_t p = A.pos ? A.pos[t] : t;
-  const bool ok = p >= 0 && p < A.n_pos;
   float a[UPL][V], b[UPL][V];
   float ss = 0.f;
 #pragma unroll
@@ -148,12 +189,7 @@ __global__ __launch_bounds__(kQkThreads) void qk_fwd_kernel(QkArgs A) {
     for (int i = 0; i < V; ++i) b[j][i] *= r * g[i];
     if (u.pair) {
       float c[V], s[V];
-      if (ok) {
-        angles<V>(A, p, un, c, s);
-      } else {  // a position outside the tables: the row's rotated part is not a number
-#pragma unroll
-        for (int i = 0; i < V; ++i) c[i] = s[i] = __builtin_nanf("");
-      }
+      angles_of<V, AXES>(A, t, un, c, s);
       turn<V, false>(a[j], b[j], c, s, A.interleaved != 0);
     }
     store_vec<T, V>(y + u.a, a[j]);
@@ -164,7 +200,7 @@ __global__ __launch_bounds__(kQkThreads) void qk_fwd_kernel(QkArgs A) {
 // A workgroup takes rows of the queries or of the keys, one stride of the grid
 // after the other, and keeps the sums for dg in registers; they meet in LDS and
 // leave as one row of `part`, so that the order of the sum is the launch's alone.
-template <typename T, int V, int G, int UPL>
+template <typename T, int V, int G, int UPL, bool AXES>
 __global__ __launch_bounds__(kQkThreads) void qk_bwd_kernel(QkArgs A) {
   constexpr int kRows = kQkThreads / G;
   __shared__ float sums[kQkThreads * 2 * V * UPL];
@@ -189,8 +225,6 @@ __global__ __launch_bounds__(kQkThreads) void qk_bwd_kernel(QkArgs A) {
     const T *x = reinterpret_cast<const T *>(A.x[which]) + t * A.sx[which].tok + head * A.sx[which].head;
     const T *dy = reinterpret_cast<const T *>(A.dy[which]) + t * A.sdy[which].tok + head * A.sdy[which].head;
     T *dx = reinterpret_cast<T *>(A.out[which]) + row * D;
-    const int64_t p = A.pos ? A.pos[t] : t;
-    const bool ok = p >= 0 && p < A.n_pos;
     float a[UPL][V], b[UPL][V], ya[UPL][V], yb[UPL][V];
     float ss = 0.f, dot = 0.f;
 #pragma unroll
@@ -209,12 +243,7 @@ __global__ __launch_bounds__(kQkThreads) void qk_bwd_kernel(QkArgs A) {
       }
       if (u.pair) {
         float c[V], s[V];
-        if (ok) {
-          angles<V>(A, p, un, c, s);
-        } else {
-#pragma unroll
-          for (int i = 0; i < V; ++i) c[i] = s[i] = __builtin_nanf("");
-        }
+        angles_of<V, AXES>(A, t, un, c, s);
         turn<V, true>(ya[j], yb[j], c, s, A.interleaved != 0);
       }
 #pragma unroll
@@ -358,8 +387,10 @@ hipError_t with_form(const QkArgs &A, int dtype, bool bwd, F f) {
   });
 }
 
-QkArgs args_of(const cfp_qk_desc &d) {
+QkArgs args_of(const cfp_qk_desc &d, const uint8_t *axis, int n_axes) {
   QkArgs A{};
+  A.n_axes = n_axes;
+  for (int i = 0; axis && i < d.rot / 2; ++i) A.axis[i / 16] |= (uint32_t)axis[i] << (2 * (i % 16));
   A.x[0] = d.q, A.x[1] = d.k;
   A.sx[0] = {d.q_token_stride, d.q_head_stride};
   A.sx[1] = {d.k_token_stride, d.k_head_stride};
@@ -386,14 +417,18 @@ void bwd_blocks(const cfp_qk_desc &d, int &bq, int &bk) {
 
 }  // namespace
 
-hipError_t launch_qk_fwd(const cfp_qk_desc &d, void *yq, void *yk, hipStream_t st) {
-  QkArgs A = args_of(d);
+hipError_t launch_qk_fwd(const cfp_qk_desc &d, const uint8_t *axis, int n_axes, void *yq, void *yk, hipStream_t st) {
+  QkArgs A = args_of(d, axis, n_axes);
   A.out[0] = yq, A.out[1] = yk;
   return with_form(A, d.dtype, false, [&](auto t, auto v, auto g, auto u) {
     using T = decltype(t);
     const int64_t rows = d.n_tokens * (d.n_q + d.n_k);
     const int64_t per = kQkThreads / g.value;
-    qk_fwd_kernel<T, v.value, g.value, u.value><<<grid_of((rows + per - 1) / per), kQkThreads, 0, st>>>(A);
+    const dim3 grid = grid_of((rows + per - 1) / per);
+    if (axis)
+      qk_fwd_kernel<T, v.value, g.value, u.value, true><<<grid, kQkThreads, 0, st>>>(A);
+    else
+      qk_fwd_kernel<T, v.value, g.value, u.value, false><<<grid, kQkThreads, 0, st>>>(A);
     return hipGetLastError();
   });
 }
@@ -404,9 +439,10 @@ size_t qk_bwd_bytes(const cfp_qk_desc &d) {
   return (size_t)(bq + bk) * d.dim * 4;
 }
 
-hipError_t launch_qk_bwd(const cfp_qk_desc &d, const void *dyq, const void *dyk, HeadStrides sq, HeadStrides sk, void *dq,
-                         void *dk, float *dwq, float *dwk, float *part, hipStream_t st) {
-  QkArgs A = args_of(d);
+hipError_t launch_qk_bwd(const cfp_qk_desc &d, const uint8_t *axis, int n_axes, const void *dyq, const void *dyk,
+                         HeadStrides sq, HeadStrides sk, void *dq, void *dk, float *dwq, float *dwk, float *part,
+                         hipStream_t st) {
+  QkArgs A = args_of(d, axis, n_axes);
   A.dy[0] = dyq, A.dy[1] = dyk, A.sdy[0] = sq, A.sdy[1] = sk;
   A.out[0] = dq, A.out[1] = dk, A.part = part;
   int bq, bk;
@@ -415,7 +451,10 @@ hipError_t launch_qk_bwd(const cfp_qk_desc &d, const void *dyq, const void *dyk,
   if (d.n_tokens == 0) bq = bk = 0;  // the gains' gradients are zeros
   hipError_t e = bq + bk == 0 ? hipSuccess : with_form(A, d.dtype, true, [&](auto t, auto v, auto g, auto u) {
     using T = decltype(t);
-    qk_bwd_kernel<T, v.value, g.value, u.value><<<bq + bk, kQkThreads, 0, st>>>(A);
+    if (axis)
+      qk_bwd_kernel<T, v.value, g.value, u.value, true><<<bq + bk, kQkThreads, 0, st>>>(A);
+    else
+      qk_bwd_kernel<T, v.value, g.value, u.value, false><<<bq + bk, kQkThreads, 0, st>>>(A);
     return hipGetLastError();
   });
   if (e != hipSuccess) return e;
