@@ -25,7 +25,9 @@
 namespace cfp {
 
 constexpr int kFewRows = 32;    // rows of a sequence and key head that the kernel for few takes
-constexpr int kManyRows = 128;  // rows of a workgroup of the kernel for many
+constexpr int kManyRows = 128;  // rows of a workgroup of the kernel for many, and of the one for heads up to 128
+constexpr int kWideRows = 256, kWideDim = 128;
+constexpr int kFewParts = 1536;
 constexpr int kFewStep = 32, kManyStep = 64;     // tokens of a tile
 constexpr int kFewLeast = 128, kManyLeast = 256;  // tokens of a part, at least
 
@@ -40,8 +42,10 @@ struct AttendArgs {
   float *few_o, *few_ml, *many_o, *many_ml;  // parts: sums over exp(s - m), and m (in powers of two) and l
   int32_t heads, group, dim, max_new;
   int32_t causal, window, wide;  // wide: queries lie on 16 bytes
-  int32_t few_parts, many_parts, few_rows;
-  uint32_t tiles;  // of kManyRows rows, at most
+  int32_t few_units, few_target;  // parts of all sequences with few rows: at most, and for their tokens alone
+  int32_t few_rows, joined;       // joined: there may be parts
+  int32_t many_parts, many_rows;  // many_rows: of a workgroup
+  uint32_t tiles;                 // of many_rows rows, at most
   float scale;     // times log2(e)
 };
 
@@ -117,6 +121,38 @@ __device__ __forceinline__ Span span_of(const AttendArgs &A, int p0, int p1, int
   r.per = max(((n + most - 1) / most + STEP - 1) & ~(STEP - 1), LEAST);
   r.parts = n > 0 ? (n + r.per - 1) / r.per : 0;
   return r;
+}
+
+// Sequences with few rows are cut into parts of `per` tokens, the same for all, so that workgroups have equal work.
+struct Few {
+  bool lost;     // longer than its table, or more rows than the call was laid out for
+  bool few;
+  int32_t tokens;  // that some row sees, from a multiple of kFewStep on
+};
+__device__ __forceinline__ Few few_of(const AttendArgs &A, int b) {
+  const Seq q = seq_of(A.s, b);
+  const int len = q.pos + q.n;
+  Few f;
+  f.lost = q.n > 0 && (q.n > A.max_new || len > (A.s.width << A.s.page_shift));
+  f.few = q.n > 0 && !f.lost && (int64_t)q.n * A.group <= kFewRows;
+  const int begin = (A.window > 0 ? max(q.pos - A.window + 1, 0) : 0) & ~(kFewStep - 1);
+  f.tokens = f.few ? max(len - begin, 0) : 0;
+  return f;
+}
+__device__ __forceinline__ uint32_t few_parts(const AttendArgs &A, int b, int per) {
+  const Few f = few_of(A, b);
+  return f.lost ? 1u : f.few ? max((uint32_t)((f.tokens + per - 1) / per), 1u) : 0u;
+}
+// All 64 lanes of a wave call it.  The sum is in 32-bit floats: the share is taken a little larger than it says, so that there
+// are never more than few_target parts beside each sequence's last.
+__device__ __forceinline__ int few_per(const AttendArgs &A) {
+  float sum = 0.f;
+  for (int first = 0; first < A.s.n_seqs; first += 64) {
+    const int b = first + (threadIdx.x & 63);
+    sum += group_sum<64>(b < A.s.n_seqs ? (float)few_of(A, b).tokens : 0.f);
+  }
+  const int per = (int)ceilf(sum * 1.001f / (float)A.few_target);
+  return __builtin_amdgcn_readfirstlane(max((per + kFewStep - 1) & ~(kFewStep - 1), kFewLeast));
 }
 
 // Query of a row as the second operand: entries of its d-th piece of 8.
@@ -204,10 +240,19 @@ struct Rows {
       }
   }
 
-  // Scores to weights exp2(c s - m), as the next product's operands.  float16 has no bits below 2^-24, so m stays 8 below
+  // The weights as the next product's operands.
+  template <int N>
+  __device__ __forceinline__ void pack(const f32x16 (&s)[N], vec<T, 8> (&p)[2 * N]) {
+#pragma unroll
+    for (int u = 0; u < N; ++u)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) p[2 * u + i / 8][i % 8] = (T)s[u][i];
+  }
+
+  // Scores to weights exp2(c s - m).  float16 has no bits below 2^-24, so m stays 8 below
   // the maximum there and weights go up to 2^14.
   template <int N>
-  __device__ __forceinline__ void weigh(f32x16 (&s)[N], float c, vec<T, 8> (&p)[2 * N]) {
+  __device__ __forceinline__ void weigh(f32x16 (&s)[N], float c) {
     float top = s[0][0];
 #pragma unroll
     for (int u = 0; u < N; ++u)
@@ -236,12 +281,19 @@ struct Rows {
         sum += e;
       }
     l += sum;
-#pragma unroll
-    for (int u = 0; u < N; ++u)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) p[2 * u + i / 8][i % 8] = (T)s[u][i];
   }
 };
+
+// Where values of 8 bits are times their tokens' powers of two: bfloat16 has the range of 32 bits, so there the weights
+// take them (16 products a lane and 32 tokens); float16's weights could not hold them, and the values do.
+template <typename T, bool BYTES>
+constexpr bool kWeightsScaled = BYTES && std::is_same<T, bf16_t>::value;
+
+// s times the 16 scales whose bytes are w.
+__device__ __forceinline__ void times_scales(f32x16 &s, u32x4 w) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) s[i] *= scale_of(w[i / 4] >> (8 * (i % 4)) & 0xff);
+}
 
 // The lowest n of 32 bits, all for n >= 32 and none for n <= 0.
 __device__ __forceinline__ uint32_t bits_of(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1; }
@@ -267,30 +319,29 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_few_kernel(Atte
   extern __shared__ __align__(16) float shared[];
   __shared__ float ml[2][4][kFewRows];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 31, h = lane >> 5;
-  uint32_t id = block_id();
-  const int part = (int)(id % A.few_parts);
-  id /= A.few_parts;
-  const int head = (int)(id % A.heads), b = (int)(id / A.heads);
-  if (b >= A.s.n_seqs) return;
+  const uint32_t id = block_id(), unit = id / A.heads;
+  const int head = (int)(id % A.heads);
+  const int per = few_per(A);
+  int b;
+  uint32_t part;
+  if (unit >= (uint32_t)A.few_units || !find_unit(A.s.n_seqs, unit, [&](int i) { return few_parts(A, i, per); }, b, part)) return;
+  b = __builtin_amdgcn_readfirstlane(b);
   const Seq sq = seq_of(A.s, b);
-  const int64_t rows64 = (int64_t)sq.n * A.group;
-  const bool lost = sq.n > A.max_new || (sq.pos + sq.n) > (A.s.width << A.s.page_shift);
+  const Few few = few_of(A, b);
   const int g = A.group, hq = A.heads * g, D = A.dim;
   T *out = reinterpret_cast<T *>(A.out);
-  if (lost) {  // too long for its table, or more rows than the call was laid out for
-    if (part == 0)
-      for (int64_t e = threadIdx.x; e < rows64 * D; e += 256) {
-        const int64_t r = e / D;
-        const int64_t row = (sq.row + r / g) * hq + head * g + r % g;
-        out[row * D + e % D] = (T)__builtin_nanf("");
-        if (e % D == 0 && A.lse) A.lse[row] = __builtin_nanf("");
-      }
+  if (few.lost) {
+    for (int64_t e = threadIdx.x; e < (int64_t)sq.n * g * D; e += 256) {
+      const int64_t r = e / D;
+      const int64_t row = (sq.row + r / g) * hq + head * g + r % g;
+      out[row * D + e % D] = (T)__builtin_nanf("");
+      if (e % D == 0 && A.lse) A.lse[row] = __builtin_nanf("");
+    }
     return;
   }
-  if (rows64 == 0 || rows64 > kFewRows) return;
-  const int rows = (int)rows64, len = sq.pos + sq.n;
-  const Span sp = span_of<kFewStep, kFewLeast>(A, sq.pos, len - 1, len, A.few_parts);
-  if (part >= max(sp.parts, 1)) return;
+  const int rows = sq.n * g, len = sq.pos + sq.n;
+  const bool whole = few.tokens <= per;
+  const int begin = len - few.tokens + (int)part * per, end = min(len, begin + per);
   const int i = col / g;
   const int p = sq.pos + i;
   const bool mine = col < rows;
@@ -307,20 +358,15 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_few_kernel(Atte
   const int ki = 16 * (col >> 2 & 1) + 4 * (col >> 3) + (col & 3);  // token of this lane's key
   u32x4 kr[kK], vr[DP / 32][BYTES ? 1 : 2], vsr;
   uint32_t ksr = 0;
-  const int end = min(sp.end, sp.begin + (part + 1) * sp.per);
 
   struct Pages {
-    uint32_t at[2];
-    bool ok[2];
+    uint32_t at[2];  // as the table has them
   };
-  auto pages = [&](int t) {
-    Pages r;
-    r.at[0] = page_of(A.s, b, t, r.ok[0]);
-    r.at[1] = page_of(A.s, b, t + 16, r.ok[1]);
-    return r;
-  };
+  const TableRow table = table_row(A.s, b);
+  auto pages = [&](int t) { return Pages{{table.entry(t), table.entry(t + 16)}}; };
+  auto inside = [&](uint32_t page) { return page < A.s.n_pages; };
   auto load_k = [&](int t, const Pages &pg) {
-    const uint32_t at = col & 4 ? pg.at[1] : pg.at[0];
+    const uint32_t entry = col & 4 ? pg.at[1] : pg.at[0], at = inside(entry) ? entry : 0u;
     const int place = (t + ki) & inner;
     const H *kp = reinterpret_cast<const H *>(A.k) + at * A.kp + (int64_t)(head * page + place) * D;
 #pragma unroll
@@ -333,7 +379,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_few_kernel(Atte
     if constexpr (BYTES) ksr = A.ks[at * A.ksp + head * page + place];
   };
   auto load_v = [&](int t, const Pages &pg) {
-    const uint32_t at = h ? pg.at[1] : pg.at[0];
+    const uint32_t entry = h ? pg.at[1] : pg.at[0], at = inside(entry) ? entry : 0u;
     const int place = (t + 16 * h) & inner;
     const H *vp = reinterpret_cast<const H *>(A.v) + at * A.vp + (int64_t)head * D * page + place;
 #pragma unroll
@@ -352,7 +398,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_few_kernel(Atte
   Rows<T, DP> st;
   st.clear();
   uint32_t *odds = reinterpret_cast<uint32_t *>(shared) + wave * 2 * DP;
-  int t = sp.begin + part * sp.per + 32 * wave;
+  int t = begin + 32 * wave;
   if (t < end) {
     Pages now = pages(t), next = now;
     load_k(t, now);
@@ -376,11 +422,13 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_few_kernel(Atte
         for (int c = 0; c < kK; ++c) s[0] = mfma32<T>(__builtin_bit_cast(Vec8, kr[c]), q[c], s[0]);
       }
       if (t + 128 < end) load_k(t + 128, next);
-      const bool edge = t + 31 > all_hi || t < all_lo || !now.ok[0] || !now.ok[1];
+      const bool edge = t + 31 > all_hi || t < all_lo || !inside(now.at[0]) || !inside(now.at[1]);
       const int first = t + 16 * h;
-      if (edge) mask16(s[0], first, lo, hi, !(h ? now.ok[1] : now.ok[0]));
+      if (edge) mask16(s[0], first, lo, hi, !inside(h ? now.at[1] : now.at[0]));
       vec<T, 8> w[2];
-      st.weigh(s, A.scale, w);
+      st.weigh(s, A.scale);
+      if constexpr (kWeightsScaled<T, BYTES>) times_scales(s[0], vsr);
+      st.pack(s, w);
       if (edge) {
         bool any = false;
 #pragma unroll
@@ -417,7 +465,9 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_few_kernel(Atte
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           vec<T, 8> v;
-          if constexpr (BYTES)
+          if constexpr (kWeightsScaled<T, BYTES>)
+            v = widen<T>(u32x2{vr[mt][0][2 * j], vr[mt][0][2 * j + 1]}, 1.f);
+          else if constexpr (BYTES)
             v = widen<T>(u32x2{vr[mt][0][2 * j], vr[mt][0][2 * j + 1]}, u32x2{vsr[2 * j], vsr[2 * j + 1]});
           else
             v = __builtin_bit_cast(Vec8, vr[mt][j]);
@@ -450,8 +500,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_few_kernel(Atte
   }
   __syncthreads();
   const int quads = D / 4;
-  const bool whole = sp.parts <= 1;
-  const int64_t slot = ((int64_t)(b * A.heads + head) * A.few_parts + part) * A.few_rows;
+  const int64_t slot = (int64_t)id * A.few_rows;
   for (int e = threadIdx.x; e < rows * quads; e += 256) {
     const int r = e / quads, d = e % quads * 4;
     float top = ml[0][0][r];
@@ -532,16 +581,15 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many_kernel(Att
   u32x4 kr[kPieces], vr[kPieces], vsr = {0, 0, 0, 0};
   uint32_t ksr[BYTES ? kPieces : 1];
   struct Pages {
-    uint32_t at[4];
-    bool ok[4];
+    uint32_t at[4];  // as the table has them
   };
-  auto pages = [&](int t) {
-    Pages r;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) r.at[j] = page_of(A.s, b, t + 16 * j, r.ok[j]);
-    return r;
+  const TableRow table = table_row(A.s, b);
+  auto pages = [&](int t) { return Pages{{table.entry(t), table.entry(t + 16), table.entry(t + 32), table.entry(t + 48)}}; };
+  auto inside = [&](uint32_t page) { return page < A.s.n_pages; };
+  auto pick = [&](const Pages &pg, int j) {
+    const uint32_t e = j & 2 ? (j & 1 ? pg.at[3] : pg.at[2]) : (j & 1 ? pg.at[1] : pg.at[0]);
+    return inside(e) ? e : 0u;
   };
-  auto pick = [&](const Pages &pg, int j) { return j & 2 ? (j & 1 ? pg.at[3] : pg.at[2]) : (j & 1 ? pg.at[1] : pg.at[0]); };
   constexpr int kKRow = DP / kPer, kVRow = kManyStep / kPer;  // pieces of a row
   auto load = [&](int t, const Pages &pg) {
 #pragma unroll
@@ -640,14 +688,15 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many_kernel(Att
 #pragma unroll
         for (int u = 0; u < 2; ++u)
           s[u] = mfma32<T>(*reinterpret_cast<const vec<T, 8> *>(k + (32 * u + ki) * kKLd + 16 * c + 8 * h), q[c], s[u]);
-      const bool edge = partly(t) || !(now.ok[0] && now.ok[1] && now.ok[2] && now.ok[3]);
+      const bool edge = partly(t) || !(inside(now.at[0]) && inside(now.at[1]) && inside(now.at[2]) && inside(now.at[3]));
       const int first = t + 16 * h;
       if (edge) {
-        mask16(s[0], first, lo, hi, !(h ? now.ok[1] : now.ok[0]));
-        mask16(s[1], first + 32, lo, hi, !(h ? now.ok[3] : now.ok[2]));
+        mask16(s[0], first, lo, hi, !inside(h ? now.at[1] : now.at[0]));
+        mask16(s[1], first + 32, lo, hi, !inside(h ? now.at[3] : now.at[2]));
       }
       vec<T, 8> w[4];
-      st.weigh(s, A.scale, w);
+      st.weigh(s, A.scale);
+      st.pack(s, w);
       if (partly(t) && odd_at[buf] == t + 1) {
         const uint32_t sees[2] = {bits_of(hi + 1 - t) & ~bits_of(lo - t), bits_of(hi + 1 - t - 32) & ~bits_of(lo - t - 32)};
 #pragma unroll
@@ -698,71 +747,548 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many_kernel(Att
   }
 }
 
-// ---- the parts of a row together, in their order: a thread takes four entries of one row.
+// ---- many rows of heads up to 128: a workgroup takes 256 rows, 64 a wave in two columns of 32, so that every operand read
+// from LDS serves two products; one wave a SIMD, with its 512 registers.  Tiles of 64 tokens lie in rings of three
+// for keys and for values, copied straight into LDS (8 bits: widened on the way).  The work on a half tile i is three
+// stages of three halves at a time, which do not wait for each other: scores of i + 1, weights of i, the product of i - 1
+// with its values; so the matrix unit works while the vector unit takes exponentials.
+
+// Copies 16 bytes a lane from memory to LDS: lane l's land at `to` + 16 l, `to` the same for all lanes.  Nothing else in the
+// kernel uses m0.
+__device__ __forceinline__ void copy_piece(const void *from, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory");
+}
+__device__ __forceinline__ void copies_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// c += a b with the sums in accumulation registers.  Written as an instruction because the allocator, left the choice,
+// moves them between both halves of the register file around every use of a score.  It does not know the
+// instruction's latency: sums are used again four products later, and read or written by others only after settle_products
+// (at most 18 cycles) and before before_products.
 template <typename T>
-__global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs A) {
-  const int hq = A.heads * A.group, g = A.group, D = A.dim, quads = D / 4;
-  const uint32_t blocks = (uint32_t)((int64_t)hq * quads + 255) / 256;
-  const uint32_t id = block_id();
-  const int64_t row = id / blocks;  // token
-  if (row >= A.s.n_tokens) return;
-  int b;
-  uint32_t k;
-  if (row < A.s.starts[0] || !find_unit(A.s.n_seqs, (uint32_t)(row - A.s.starts[0]), [&](int i) { return (uint32_t)seq_of(A.s, i).n; }, b, k)) return;
-  const Seq sq = seq_of(A.s, b);
-  const int len = sq.pos + sq.n, e = (int)(id % blocks) * 256 + threadIdx.x;
-  if (sq.n > A.max_new || len > (A.s.width << A.s.page_shift) || e >= hq * quads) return;
-  const int head = e / quads, d = e % quads * 4;
-  const int i = (int)k, r = i * g + head % g, rows = sq.n * g;
-  const bool few = rows <= kFewRows;
-  if (few ? A.few_parts == 1 : A.many_parts == 1) return;
-  Span sp;
-  int64_t at, step;
-  if (few) {
-    sp = span_of<kFewStep, kFewLeast>(A, sq.pos, len - 1, len, A.few_parts);
-    at = (int64_t)(b * A.heads + head / g) * A.few_parts * A.few_rows + r, step = A.few_rows;
+__device__ __forceinline__ void add_product(f32x16 &c, vec<T, 8> a, vec<T, 8> b) {
+  if constexpr (std::is_same<T, bf16_t>::value)
+    asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+  else
+    asm volatile("v_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+}
+// Scores: s = a q, or with the products before them.  They are read by the vector unit after two more products of 8 passes
+// each (11 are asked for).
+template <typename T>
+__device__ __forceinline__ void score_product(f32x16 &s, vec<T, 8> a, vec<T, 8> q, bool first) {
+  if constexpr (std::is_same<T, bf16_t>::value) {
+    if (first)
+      asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(s) : "v"(a), "a"(q));
+    else
+      asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(s) : "v"(a), "a"(q));
   } else {
-    const int r0 = r / kManyRows * kManyRows, r1 = min(r0 + kManyRows, rows);
-    sp = span_of<kManyStep, kManyLeast>(A, sq.pos + r0 / g, sq.pos + (r1 - 1) / g, len, A.many_parts);
-    at = (int64_t)(sq.row + i) * hq + head, step = A.s.n_tokens * hq;
+    if (first)
+      asm volatile("v_mfma_f32_32x32x16_f16 %0, %1, %2, 0" : "=&v"(s) : "v"(a), "a"(q));
+    else
+      asm volatile("v_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+v"(s) : "v"(a), "a"(q));
   }
-  if (sp.parts <= 1) return;
-  const float *po = few ? A.few_o : A.many_o, *pm = few ? A.few_ml : A.many_ml;
+}
+template <int N>
+__device__ __forceinline__ void settle_products(f32x16 (&o)[N]) {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+a"(o[i]));
+}
+template <int N>
+__device__ __forceinline__ void before_products(f32x16 (&o)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+a"(o[i]));
+  asm volatile("s_nop 7" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// Sums times a factor where they are: a use by an ordinary instruction would move all of them at every branch's end.
+__device__ __forceinline__ void times_sums(f32x16 &o, float by) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    float x = o[i], y;
+    asm volatile("v_accvgpr_read_b32 %1, %0\n\ts_nop 1\n\tv_mul_f32 %1, %1, %2\n\ts_nop 1\n\tv_accvgpr_write_b32 %0, %1"
+                 : "+a"(x), "=&v"(y) : "v"(by));
+    o[i] = x;
+  }
+}
+
+// Place of piece c (8 entries) of a row in LDS: 16 lanes that read one piece of rows 0-3, 16-19, 4-7, 20-23 (or these + 8) of
+// keys, or of 16 rows of values in order, meet all banks.
+template <int DP>
+__device__ __forceinline__ int key_place(int row, int c) {
+  if constexpr (DP == 128) return c ^ ((row & 7) | (row >> 4 & 1) << 3);
+  if constexpr (DP == 64) return c ^ ((row >> 1 & 3) | (row >> 4 & 1) << 2);
+  const int p = c + ((row >> 2 & 1) | (row >> 4 & 1) << 1);
+  return p >= DP / 8 ? p - DP / 8 : p;
+}
+template <int DP>
+__device__ __forceinline__ int key_piece(int row, int place) {  // which piece lies there
+  if constexpr (DP != 96) return key_place<DP>(row, place);
+  const int c = place - ((row >> 2 & 1) | (row >> 4 & 1) << 1);
+  return c < 0 ? c + DP / 8 : c;
+}
+__device__ __forceinline__ int value_place(int d, int c) { return c ^ (d >> 1 & 7); }
+
+template <typename T, bool BYTES, int DP>
+__global__ __launch_bounds__(256, 1) void attend_wide_kernel(AttendArgs A) {
+  typedef std::conditional_t<BYTES, uint8_t, T> H;
+  typedef vec<T, 8> Vec8;
+  constexpr int kTile = 64 * DP;  // entries of a tile of keys, and of values
+  constexpr int kMt = DP / 32, kC = DP / 16;
+  extern __shared__ __align__(1024) char shared_bytes[];
+  T *keys = reinterpret_cast<T *>(shared_bytes), *values = keys + 3 * kTile;
+  uint8_t *odds = reinterpret_cast<uint8_t *>(values + 3 * kTile);  // as in the kernel above, of one tile
+  volatile int *odd_at = reinterpret_cast<volatile int *>(odds + DP * 16);
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, h = lane >> 5;
+  uint32_t id = block_id();
+  const int head = (int)(id % A.heads);
+  id /= A.heads;
+  const int part = (int)(id % A.many_parts);
+  id /= A.many_parts;
+  if (id >= A.tiles) return;
+  int b;
+  uint32_t tile;
+  const int g = A.group, hq = A.heads * g, D = A.dim;
+  if (!find_unit(A.s.n_seqs, A.tiles - 1 - id, [&](int i) {
+        const Seq s = seq_of(A.s, i);
+        const int64_t r = (int64_t)s.n * g;
+        return r > kFewRows && s.n <= A.max_new ? (uint32_t)((r + kWideRows - 1) / kWideRows) : 0u;
+      }, b, tile))
+    return;
+  b = __builtin_amdgcn_readfirstlane(b);
+  const Seq sq = seq_of(A.s, b);
+  const int len = sq.pos + sq.n, rows = sq.n * g;
+  if (len > (A.s.width << A.s.page_shift)) return;  // the kernel for few writes what such rows become
+  const int r0 = (int)tile * kWideRows, r1 = min(r0 + kWideRows, rows);
+  const int p0 = sq.pos + r0 / g, p1 = sq.pos + (r1 - 1) / g;
+  const Span sp = span_of<kManyStep, kManyLeast>(A, p0, p1, len, A.many_parts);
+  if (part >= max(sp.parts, 1)) return;
+  const int begin = sp.begin + part * sp.per, end = min(sp.end, begin + sp.per);
+  const int n = end > begin ? (end - begin + 63) / 64 : 0;  // tiles
+  const int all_hi = A.causal ? p0 : len - 1, all_lo = A.window > 0 ? p1 - A.window + 1 : 0;
+  const bool active = r0 + wave * 64 < rows;  // of the wave
+
+  Vec8 q[2][kC];
+  int hi[2], lo[2];
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    const int r = r0 + wave * 64 + 32 * x + col, i = r / g;
+    const bool mine = r < rows;
+    hi[x] = mine ? (A.causal ? sq.pos + i : len - 1) : -1, lo[x] = A.window > 0 ? sq.pos + i - A.window + 1 : 0;
+    const T *qp = reinterpret_cast<const T *>(A.q) + (int64_t)(sq.row + i) * A.qt + (int64_t)(head * g + r % g) * A.qh;
+#pragma unroll
+    for (int c = 0; c < kC; ++c) q[x][c] = load_q<T>(qp, 16 * c + 8 * h, D, mine, A.wide != 0);
+  }
+
+  const int page = 1 << A.s.page_shift, inner = page - 1;
+  struct Pages {
+    uint32_t at[4];  // as the table has them
+  };
+  const TableRow table = table_row(A.s, b);
+  auto pages = [&](int j) {
+    const int t = begin + 64 * j;
+    return Pages{{table.entry(t), table.entry(t + 16), table.entry(t + 32), table.entry(t + 48)}};
+  };
+  auto inside = [&](uint32_t page) { return page < A.s.n_pages; };
+  auto pick = [&](const Pages &pg, int j) {
+    const uint32_t e = j & 2 ? (j & 1 ? pg.at[3] : pg.at[2]) : (j & 1 ? pg.at[1] : pg.at[0]);
+    return inside(e) ? e : 0u;
+  };
+  const H *kbase = reinterpret_cast<const H *>(A.k) + (int64_t)head * page * D;
+  const H *vbase = reinterpret_cast<const H *>(A.v) + (int64_t)head * page * D;
+  constexpr int kPer = 16 / (int)sizeof(H);                         // entries of a piece in memory
+  constexpr int kAll = kTile / kPer, kPieces = (kAll + 255) / 256;  // pieces of a tile, of a thread
+  constexpr int kKRow = DP / kPer, kVRow = 64 / kPer;
+  auto key_from = [&](int m, int t, const Pages &pg, int &row, int &d) {  // piece m of the tile, its row and first entry
+    row = m / kKRow;
+    d = BYTES ? m % kKRow * 16 : 8 * key_piece<DP>(row, m % kKRow);
+    return kbase + (int64_t)pick(pg, row >> 4 & 3) * A.kp + ((t + row) & inner) * D + d;
+  };
+  auto value_from = [&](int m, int t, const Pages &pg, int &d, int &tok) {
+    d = m / kVRow;
+    tok = BYTES ? m % kVRow * 16 : 8 * value_place(d, m % kVRow);
+    return vbase + (int64_t)pick(pg, tok >> 4) * A.vp + (int64_t)d * page + ((t + tok) & inner);
+  };
+  // 16 bits: copies; 8 bits: into registers, from where put_* writes them
+  u32x4 kr[BYTES ? kPieces : 1], vr[BYTES ? kPieces : 1], vsr = {0, 0, 0, 0};
+  uint32_t ksr[BYTES ? kPieces : 1];
+  auto get_keys = [&](int j, const Pages &pg) {
+#pragma unroll
+    for (int e = 0; e < kPieces; ++e) {
+      const int m = (BYTES ? e * 256 : (e * 4 + wave) * 64) + (BYTES ? tid : lane);
+      int row, d;
+      const H *from = key_from(m, begin + 64 * j, pg, row, d);
+      if constexpr (BYTES) {
+        if (m < kAll && d < D) kr[e] = *reinterpret_cast<const u32x4 *>(from);
+        ksr[e] = A.ks[(int64_t)pick(pg, row >> 4 & 3) * A.ksp + head * page + ((begin + 64 * j + row) & inner)];
+      } else if (d < D) {
+        copy_piece(from, (uint32_t)((j % 3) * kTile * 2 + (e * 4 + wave) * 1024));
+      }
+    }
+  };
+  auto get_values = [&](int j, const Pages &pg) {
+#pragma unroll
+    for (int e = 0; e < kPieces; ++e) {
+      const int m = (BYTES ? e * 256 : (e * 4 + wave) * 64) + (BYTES ? tid : lane);
+      int d, tok;
+      const H *from = value_from(m, begin + 64 * j, pg, d, tok);
+      if constexpr (BYTES) {
+        if (m < kAll && d < D) vr[e] = *reinterpret_cast<const u32x4 *>(from);
+        if (e == 0) vsr = *reinterpret_cast<const u32x4 *>(A.vs + (int64_t)pick(pg, tok >> 4) * A.vsp + head * page + ((begin + 64 * j + tok) & inner));
+      } else if (d < D) {
+        copy_piece(from, (uint32_t)((3 + j % 3) * kTile * 2 + (e * 4 + wave) * 1024));
+      }
+    }
+  };
+  auto put_keys = [&](int j) {
+    if constexpr (BYTES) {
+#pragma unroll
+      for (int e = 0; e < kPieces; ++e) {
+        const int m = e * 256 + tid, row = m / kKRow, c = m % kKRow * 2;
+        if (m >= kAll || 8 * c >= D) continue;
+        const float by = scale_of(ksr[e]);
+        T *to = keys + (j % 3) * kTile + row * DP;
+        *reinterpret_cast<Vec8 *>(to + 8 * key_place<DP>(row, c)) = widen<T>(u32x2{kr[e][0], kr[e][1]}, by);
+        *reinterpret_cast<Vec8 *>(to + 8 * key_place<DP>(row, c + 1)) = widen<T>(u32x2{kr[e][2], kr[e][3]}, by);
+      }
+    }
+  };
+  auto put_values = [&](int j) {
+    if constexpr (BYTES) {
+#pragma unroll
+      for (int e = 0; e < kPieces; ++e) {
+        const int m = e * 256 + tid, d = m / kVRow, c = m % kVRow * 2;
+        if (m >= kAll || d >= D) continue;
+        T *to = values + (j % 3) * kTile + d * 64;
+        *reinterpret_cast<Vec8 *>(to + 8 * value_place(d, c)) = widen<T>(u32x2{vr[e][0], vr[e][1]}, u32x2{vsr[0], vsr[1]});
+        *reinterpret_cast<Vec8 *>(to + 8 * value_place(d, c + 1)) = widen<T>(u32x2{vr[e][2], vr[e][3]}, u32x2{vsr[2], vsr[3]});
+      }
+    }
+  };
+
+  Rows<T, DP> st[2];
+  st[0].clear(), st[1].clear();
+  const int ki = 16 * (col >> 2 & 1) + 4 * (col >> 3) + (col & 3);
+  int koff[kC], voff[4];
+#pragma unroll
+  for (int c = 0; c < kC; ++c) koff[c] = ki * DP + 8 * key_place<DP>(ki, 2 * c + h);
+#pragma unroll
+  for (int c = 0; c < 4; ++c) voff[c] = col * 64 + 8 * value_place(col, 4 * (c / 2) + 2 * h + c % 2);
+  auto scores = [&](f32x16 (&s)[2], const T *k, int u) {
+#pragma unroll
+    for (int c = 0; c < kC; ++c) {
+      const Vec8 a = *reinterpret_cast<const Vec8 *>(k + 32 * u * DP + koff[c]);
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        if (c == 0) {
+          f32x16 zero;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) zero[i] = 0.f;
+          s[x] = mfma32<T>(a, q[x][c], zero);
+        } else {
+          s[x] = mfma32<T>(a, q[x][c], s[x]);
+        }
+      }
+    }
+  };
+  auto value_piece = [&](const T *v, int u, int m) {  // of the half's kC products' first operands
+    return *reinterpret_cast<const Vec8 *>(v + m / 2 * 32 * 64 + voff[2 * u + m % 2]);
+  };
+  constexpr float kBelow = std::is_same<T, f16_t>::value ? 8.f : 0.f;  // as in Rows::weigh
+  // One half's stage: weights of s to p, scores of half ku of tile k to next, and half vu of the values v times pp.
+  // Every product is followed by its share of the vector instructions, and nothing is moved across.
+  auto stage = [&](f32x16 (&s)[2], Vec8 (&p)[2][2], f32x16 (&next)[2], const T *k, int ku, const T *v, int vu, const Vec8 (&pp)[2][2]) {
+    constexpr int kSlots = 4 * kC, kFirst = 4;  // products; the first kFirst share the maxima
+    Vec8 ka[2], va[2];
+    ka[0] = *reinterpret_cast<const Vec8 *>(k + 32 * ku * DP + koff[0]);
+    va[0] = value_piece(v, vu, 0);
+    float top[2], to[2], by[2], from[2], sum[2] = {0.f, 0.f}, w[32];
+    bool grows = false;
+    auto vector_share = [&](int slot) {
+      if (slot < 2) {
+        top[slot] = fmaxf(s[slot][0], s[slot][1]);
+#pragma unroll
+        for (int i = 2; i < 16; ++i) top[slot] = fmaxf(top[slot], s[slot][i]);
+      } else if (slot == 2) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          top[x] = fmaxf(top[x], partner(top[x])) * A.scale;
+          const bool more = top[x] > st[x].m + (kSlack + kBelow);
+          grows = grows || more;
+          to[x] = more ? top[x] - kBelow : st[x].m;
+          from[x] = to[x] == -__builtin_inff() ? 0.f : to[x];
+        }
+      } else if (slot == 3) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          by[x] = to[x] == st[x].m ? 1.f : __builtin_amdgcn_exp2f(st[x].m - to[x]);
+          st[x].m = to[x];
+        }
+      } else {
+        const int lo = (slot - kFirst) * 32 / (kSlots - kFirst), hi = (slot + 1 - kFirst) * 32 / (kSlots - kFirst);
+#pragma unroll
+        for (int e = lo; e < hi; ++e) {
+          const int x = e / 16, i = e % 16;
+          w[e] = __builtin_amdgcn_exp2f(fmaf(s[x][i], A.scale, -from[x]));
+          asm volatile("" : "+v"(w[e]));  // here, not behind the branch at the stage's end
+          sum[x] += w[e];
+          if (i % 2) p[x][i / 8][i % 8 - 1] = (T)w[e - 1], p[x][i / 8][i % 8] = (T)w[e];
+        }
+      }
+    };
+#pragma unroll
+    for (int c = 0; c < kC; ++c) {
+      if (c + 1 < kC) {
+        ka[(c + 1) % 2] = *reinterpret_cast<const Vec8 *>(k + 32 * ku * DP + koff[c + 1]);
+        va[(c + 1) % 2] = value_piece(v, vu, c + 1);
+      }
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        score_product<T>(next[x], ka[c % 2], q[x][c], c == 0);
+        vector_share(4 * c + x);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        add_product<T>(st[x].o[c / 2], va[c % 2], pp[x][c % 2]);
+        vector_share(4 * c + 2 + x);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+#pragma unroll
+    for (int x = 0; x < 2; ++x) st[x].l = st[x].l * by[x] + sum[x];
+    if (__any(grows)) {
+      settle_products(st[0].o), settle_products(st[1].o);
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int mt = 0; mt < kMt; ++mt) times_sums(st[x].o[mt], by[x]);
+      before_products(st[0].o), before_products(st[1].o);
+    }
+  };
+
+  before_products(st[0].o), before_products(st[1].o);
+#pragma unroll
+  for (int x = 0; x < 2; ++x)
+#pragma unroll
+    for (int c = 0; c < kC; ++c) asm volatile("" : "+a"(q[x][c]));  // queries stay in accumulation registers too
+  if (n > 0) {
+    // zeros where no entry is written to, and in the tile that stands before the first
+    for (int e = tid; e < (D < DP ? 6 : 0) * kTile / 8; e += 256) reinterpret_cast<u32x4 *>(keys)[e] = u32x4{0, 0, 0, 0};
+    if (D == DP)
+      for (int e = tid; e < kTile / 8; e += 256) reinterpret_cast<u32x4 *>(values + 2 * kTile)[e] = u32x4{0, 0, 0, 0};
+    if (tid == 0) *odd_at = 0;
+    if (D < DP) __syncthreads();
+    Pages now = pages(0), next = now, later = now;
+    if (n > 1) next = pages(1);
+    get_keys(0, now);
+    put_keys(0);
+    get_values(0, now);
+    put_values(0);
+    if (n > 1) {
+      get_keys(1, next);
+      put_keys(1);
+      if (n > 2) later = pages(2);
+    }
+    copies_done();
+    __syncthreads();
+    f32x16 s0[2], s1[2];
+    Vec8 pa[2][2], pb[2][2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) pb[x][j][i] = (T)0.f;
+    if (active) scores(s0, keys, 0);
+    for (int j = 0; j < n; ++j) {
+      const int t = begin + 64 * j;
+      copies_done();
+      __syncthreads();  // tiles j + 1 of keys and j of values are there, and what is overwritten now has been read
+      Pages after = later;
+      if (j + 3 < n) after = pages(j + 3);
+      if (j + 2 < n) get_keys(j + 2, later);
+      if (j + 1 < n) get_values(j + 1, next);
+      const T *k1 = keys + (j + 1) % 3 * kTile, *k0 = keys + j % 3 * kTile;
+      T *v0 = values + j % 3 * kTile;
+      const T *v1 = values + (j + 2) % 3 * kTile;  // tile j - 1
+      const bool partly = t + 63 > all_hi || t < all_lo;  // some row does not see all tokens
+      if (partly) {
+        for (int m = tid; m < D * 8; m += 256) {
+          const int d = m / 8, c = value_place(d, m % 8);
+          u32x4 w = reinterpret_cast<const u32x4 *>(v0)[m];
+          uint32_t up, down;
+          take_odd<T, T>(w, up, down);
+          odds[d * 16 + c] = (uint8_t)up, odds[d * 16 + 8 + c] = (uint8_t)down;
+          if (up | down) {
+            reinterpret_cast<u32x4 *>(v0)[m] = w;
+            *odd_at = t + 1;
+          }
+        }
+        __syncthreads();
+        if (*odd_at == t + 1) {
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            const uint32_t sees[2] = {bits_of(hi[x] + 1 - t) & ~bits_of(lo[x] - t), bits_of(hi[x] + 1 - t - 32) & ~bits_of(lo[x] - t - 32)};
+#pragma unroll
+            for (int mt = 0; mt < kMt; ++mt)
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                const int d = 32 * mt + 8 * (i / 4) + 4 * h + i % 4;
+                const u32x4 w = *reinterpret_cast<const u32x4 *>(odds + d * 16);
+                st[x].add_odd(mt, i, d < D && ((w[0] & sees[0]) | (w[1] & sees[1])), d < D && ((w[2] & sees[0]) | (w[3] & sees[1])));
+                __builtin_amdgcn_sched_barrier(0);  // one after the other: seldom run, and not worth registers
+              }
+          }
+        }
+      }
+      if (active) {
+        const bool edge = partly || !(inside(now.at[0]) && inside(now.at[1]) && inside(now.at[2]) && inside(now.at[3]));
+        const int first = t + 16 * h;
+        if (edge)
+#pragma unroll
+          for (int x = 0; x < 2; ++x) mask16(s0[x], first, lo[x], hi[x], !inside(h ? now.at[1] : now.at[0]));
+        stage(s0, pa, s1, k0, 1, v1, 1, pb);
+        if (edge)
+#pragma unroll
+          for (int x = 0; x < 2; ++x) mask16(s1[x], first + 32, lo[x], hi[x], !inside(h ? now.at[3] : now.at[2]));
+        stage(s1, pb, s0, k1, 0, v0, 0, pa);
+      }
+      if (j + 2 < n) put_keys(j + 2);
+      if (j + 1 < n) put_values(j + 1);
+      now = next, next = later, later = after;
+    }
+    if (active) {
+      const T *v = values + (n - 1) % 3 * kTile;
+#pragma unroll
+      for (int m = 0; m < kC; ++m)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) add_product<T>(st[x].o[m / 2], value_piece(v, 1, m), pb[x][m % 2]);
+    }
+  }
+  if (!active) return;
+  settle_products(st[0].o), settle_products(st[1].o);
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    st[x].finish();
+    const int r = r0 + wave * 64 + 32 * x + col;
+    if (r >= rows) continue;
+    const int64_t row = (int64_t)(sq.row + r / g) * hq + head * g + r % g;
+    if (sp.parts <= 1) {
+      const float inv = st[x].l == 0.f ? 0.f : 1.f / st[x].l;
+      T *to = reinterpret_cast<T *>(A.out) + row * D + 4 * h;
+#pragma unroll
+      for (int mt = 0; mt < kMt; ++mt)
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+          const float y[4] = {st[x].o[mt][4 * a] * inv, st[x].o[mt][4 * a + 1] * inv, st[x].o[mt][4 * a + 2] * inv, st[x].o[mt][4 * a + 3] * inv};
+          if (32 * mt + 8 * a + 4 * h < D) store_vec<T, 4>(to + 32 * mt + 8 * a, y);
+        }
+      if (h == 0 && A.lse) A.lse[row] = (st[x].m + __builtin_amdgcn_logf(st[x].l)) * kLn2F;
+    } else {
+      const int64_t at = part * A.s.n_tokens * hq + row;
+      float *to = A.many_o + at * D + 4 * h;
+#pragma unroll
+      for (int mt = 0; mt < kMt; ++mt)
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+          const float y[4] = {st[x].o[mt][4 * a], st[x].o[mt][4 * a + 1], st[x].o[mt][4 * a + 2], st[x].o[mt][4 * a + 3]};
+          if (32 * mt + 8 * a + 4 * h < D) store_vec<float, 4>(to + 32 * mt + 8 * a, y);
+        }
+      if (h == 0) A.many_ml[2 * at] = st[x].m, A.many_ml[2 * at + 1] = st[x].l;
+    }
+  }
+}
+
+// ---- the parts of a row together, in their order: a thread takes four entries of one row.  The first workgroups take the
+// sequences with few rows, the others the tokens of the others.
+template <typename T>
+__device__ __forceinline__ void join_row(const AttendArgs &A, const float *po, const float *pm, int64_t at, int64_t step, int parts,
+                                         int64_t row, int d) {
   float top = -__builtin_inff();
-  for (int s = 0; s < sp.parts; ++s) top = fmaxf(top, pm[2 * (at + s * step)]);
+  for (int s = 0; s < parts; ++s) top = fmaxf(top, pm[2 * (at + s * step)]);
   float l = 0.f;
   vec<float, 4> o = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < sp.parts; ++s) {
+#pragma unroll 4
+  for (int s = 0; s < parts; ++s) {
     const int64_t a = at + s * step;
     const float m = pm[2 * a], by = m == top ? 1.f : __builtin_amdgcn_exp2f(m - top);
     l += pm[2 * a + 1] * by;
-    o += *reinterpret_cast<const vec<float, 4> *>(po + a * D + d) * by;
+    o += *reinterpret_cast<const vec<float, 4> *>(po + a * A.dim + d) * by;
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
   const float y[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
-  const int64_t to = ((int64_t)(sq.row + i) * hq + head);
-  store_vec<T, 4>(reinterpret_cast<T *>(A.out) + to * D + d, y);
-  if (d == 0 && A.lse) A.lse[to] = (top + __builtin_amdgcn_logf(l)) * kLn2F;
+  store_vec<T, 4>(reinterpret_cast<T *>(A.out) + row * A.dim + d, y);
+  if (d == 0 && A.lse) A.lse[row] = (top + __builtin_amdgcn_logf(l)) * kLn2F;
+}
+
+// Workgroups of a sequence with few rows, and of a token.
+inline __host__ __device__ uint32_t few_joins(const AttendArgs &A) {
+  return (uint32_t)(((int64_t)A.heads * A.few_rows * (A.dim / 4) + 255) / 256);
+}
+inline __host__ __device__ uint32_t many_joins(const AttendArgs &A) {
+  return (uint32_t)(((int64_t)A.heads * A.group * (A.dim / 4) + 255) / 256);
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs A) {
+  const int g = A.group, hq = A.heads * g, quads = A.dim / 4;
+  uint32_t id = block_id();
+  const uint32_t few = few_joins(A), few_all = A.joined ? few * A.s.n_seqs : 0u;
+  int b;
+  if (id < few_all) {
+    b = (int)(id / few);
+    const Few f = few_of(A, b);
+    if (!f.few || f.tokens <= kFewLeast) return;
+    const int per = few_per(A), parts = (f.tokens + per - 1) / per;
+    if (parts <= 1) return;
+    const uint32_t unit = units_before(b, [&](int i) { return few_parts(A, i, per); });
+    const Seq sq = seq_of(A.s, b);
+    const int rows = sq.n * g, e = (int)(id % few) * 256 + threadIdx.x, r = e / quads % rows, head = e / quads / rows;
+    if (head >= A.heads) return;
+    join_row<T>(A, A.few_o, A.few_ml, ((int64_t)unit * A.heads + head) * A.few_rows + r, (int64_t)A.heads * A.few_rows, parts,
+                (int64_t)(sq.row + r / g) * hq + head * g + r % g, e % quads * 4);
+    return;
+  }
+  id -= few_all;
+  const uint32_t many = many_joins(A);
+  const int64_t token = id / many;
+  if (A.many_parts == 1 || token >= A.s.n_tokens) return;
+  uint32_t k;
+  if (token < A.s.starts[0] || !find_unit(A.s.n_seqs, (uint32_t)(token - A.s.starts[0]), [&](int i) { return (uint32_t)seq_of(A.s, i).n; }, b, k)) return;
+  const Seq sq = seq_of(A.s, b);
+  const int len = sq.pos + sq.n, rows = sq.n * g, e = (int)(id % many) * 256 + threadIdx.x;
+  if (sq.n > A.max_new || len > (A.s.width << A.s.page_shift) || rows <= kFewRows || e >= hq * quads) return;
+  const int head = e / quads, i = (int)k, r = i * g + head % g;
+  const int r0 = r / A.many_rows * A.many_rows, r1 = min(r0 + A.many_rows, rows);
+  const Span sp = span_of<kManyStep, kManyLeast>(A, sq.pos + r0 / g, sq.pos + (r1 - 1) / g, len, A.many_parts);
+  if (sp.parts <= 1) return;
+  const int64_t row = (int64_t)(sq.row + i) * hq + head;
+  join_row<T>(A, A.many_o, A.many_ml, row, A.s.n_tokens * hq, sp.parts, row, e % quads * 4);
 }
 
 template <typename T, bool BYTES, int DP>
 hipError_t attend_run(const AttendArgs &A, hipStream_t st) {
   const size_t few = (size_t)4 * 4 * std::max(A.few_rows * (DP + 4), 2 * DP);
-  const size_t many = (size_t)2 * (kManyStep * (DP + 8) + DP * (kManyStep + 8)) * 2 + 2 * DP * 16 + 16;
+  const size_t many = DP <= kWideDim ? (size_t)6 * 64 * DP * 2 + DP * 16 + 16
+                                     : (size_t)2 * (kManyStep * (DP + 8) + DP * (kManyStep + 8)) * 2 + 2 * DP * 16 + 16;
   auto *few_kernel = attend_few_kernel<T, BYTES, DP>;
-  auto *many_kernel = attend_many_kernel<T, BYTES, DP>;
+  void (*many_kernel)(AttendArgs);
+  if constexpr (DP <= kWideDim)
+    many_kernel = attend_wide_kernel<T, BYTES, DP>;
+  else
+    many_kernel = attend_many_kernel<T, BYTES, DP>;
   for (int i = 0; i < 2; ++i)  // LDS beyond 64 KiB is asked for
     if ((i ? many : few) > 65536 && (i == 0 || A.tiles)) {
       const hipError_t e = hipFuncSetAttribute(i ? reinterpret_cast<const void *>(many_kernel) : reinterpret_cast<const void *>(few_kernel),
                                                hipFuncAttributeMaxDynamicSharedMemorySize, (int)(i ? many : few));
       if (e != hipSuccess) return e;
     }
-  few_kernel<<<grid_of((int64_t)A.s.n_seqs * A.heads * A.few_parts), 256, few, st>>>(A);
+  few_kernel<<<grid_of((int64_t)A.few_units * A.heads), 256, few, st>>>(A);
   if (A.tiles) many_kernel<<<grid_of((int64_t)A.tiles * A.heads * A.many_parts), 256, many, st>>>(A);
-  if (A.few_parts > 1 || A.many_parts > 1) {
-    const int64_t blocks = ((int64_t)A.heads * A.group * (A.dim / 4) + 255) / 256;
-    attend_join_kernel<T><<<grid_of(A.s.n_tokens * blocks), 256, 0, st>>>(A);
-  }
+  const int64_t joins = (A.joined ? (int64_t)few_joins(A) * A.s.n_seqs : 0) + (A.many_parts > 1 ? A.s.n_tokens * many_joins(A) : 0);
+  if (joins) attend_join_kernel<T><<<grid_of(joins), 256, 0, st>>>(A);
   return hipGetLastError();
 }
 

@@ -6,25 +6,28 @@
 namespace cfp {
 namespace {
 
-// Parts that the tokens of a sequence are cut into at most (a short one is cut into fewer on the device).
+// How the work is laid out: bounds from what the host knows; the device cuts by the lengths that it finds.  Sequences with few
+// rows are cut into about kFewParts equal parts over all (six for every workgroup that the chip holds at a time).
 void parts_of(const cfp_attend_desc &a, const cfp_cache_desc &c, const cfp_sequences_desc &s, AttendArgs &A) {
   const int64_t g = a.n_q / c.heads, most_len = (int64_t)s.width * c.page;
   const int64_t new_rows = std::min<int64_t>(s.max_new, a.n_tokens) * g;
-  const int64_t pairs = (int64_t)s.n_seqs * c.heads;
   A.few_rows = (int32_t)std::min<int64_t>(kFewRows, new_rows);
-  A.few_parts = (int32_t)std::clamp<int64_t>(std::min<int64_t>(2048 / pairs, most_len / kFewLeast), 1, 64);
+  A.joined = most_len > kFewLeast;
+  A.few_target = (int32_t)std::max<int64_t>(kFewParts / c.heads, 1);
+  A.few_units = s.n_seqs + (A.joined ? (int32_t)std::min<int64_t>(A.few_target, most_len / kFewLeast * s.n_seqs) : 0);
+  A.many_rows = c.dim <= kWideDim ? kWideRows : kManyRows;
   A.tiles = 0, A.many_parts = 1;
   if (new_rows > kFewRows) {
-    A.tiles = (uint32_t)std::min<int64_t>(a.n_tokens * g / kManyRows + s.n_seqs, (a.n_tokens * g + kFewRows) / (kFewRows + 1));
+    A.tiles = (uint32_t)std::min<int64_t>(a.n_tokens * g / A.many_rows + s.n_seqs, (a.n_tokens * g + kFewRows) / (kFewRows + 1));
     const int64_t groups = (int64_t)A.tiles * c.heads;
     if (groups < 512) A.many_parts = (int32_t)std::clamp<int64_t>(std::min<int64_t>(1024 / groups, most_len / kManyLeast), 1, 16);
   }
 }
 
-size_t few_floats(const cfp_cache_desc &c, const cfp_sequences_desc &s, const AttendArgs &A) {
-  return A.few_parts > 1 ? (size_t)s.n_seqs * c.heads * A.few_parts * A.few_rows : 0;
+size_t few_slots(const cfp_cache_desc &c, const AttendArgs &A) {
+  return A.joined ? (size_t)A.few_units * c.heads * A.few_rows : 0;
 }
-size_t many_floats(const cfp_attend_desc &a, const AttendArgs &A) {
+size_t many_slots(const cfp_attend_desc &a, const AttendArgs &A) {
   return A.many_parts > 1 ? (size_t)a.n_tokens * a.n_q * A.many_parts : 0;
 }
 
@@ -33,7 +36,7 @@ size_t many_floats(const cfp_attend_desc &a, const AttendArgs &A) {
 size_t attend_bytes(const cfp_attend_desc &a, const cfp_cache_desc &c, const cfp_sequences_desc &s) {
   AttendArgs A{};
   parts_of(a, c, s, A);
-  return (few_floats(c, s, A) + many_floats(a, A)) * (c.dim + 2) * 4;
+  return (few_slots(c, A) + many_slots(a, A)) * (c.dim + 2) * 4;
 }
 
 hipError_t launch_attend(const cfp_attend_desc &a, const cfp_cache_desc &c, const cfp_sequences_desc &s, void *out, float *lse,
@@ -45,7 +48,7 @@ hipError_t launch_attend(const cfp_attend_desc &a, const cfp_cache_desc &c, cons
   A.kp = c.k_page_stride, A.vp = c.v_page_stride, A.ksp = c.k_scale_page_stride, A.vsp = c.v_scale_page_stride;
   A.qt = a.q_token_stride, A.qh = a.q_head_stride;
   A.out = out, A.lse = lse;
-  const size_t few = few_floats(c, s, A), many = many_floats(a, A);
+  const size_t few = few_slots(c, A), many = many_slots(a, A);
   A.few_o = (float *)ws, A.many_o = A.few_o + few * c.dim;
   A.few_ml = A.many_o + many * c.dim, A.many_ml = A.few_ml + 2 * few;
   A.heads = c.heads, A.group = a.n_q / c.heads, A.dim = c.dim, A.max_new = s.max_new;

@@ -44,6 +44,30 @@ __device__ __forceinline__ uint32_t page_of(const SeqArgs &S, int b, int p, bool
   return ok ? pg : 0u;
 }
 
+// Entries of a sequence's row of the table, read as constants (by scalar loads: the index is the same for all lanes).  They
+// are loaded a tile or two before they are looked at.
+typedef const __attribute__((address_space(4))) int32_t const_i32;
+struct TableRow {
+  const_i32 *row;
+  int32_t last, shift;
+  // Of the page that token p >= 0 lies in; of the last one for tokens behind the table, which no row sees.
+  __device__ __forceinline__ uint32_t entry(int p) const { return (uint32_t)row[min(p >> shift, last)]; }
+};
+__device__ __forceinline__ TableRow table_row(const SeqArgs &S, int b) {  // of a sequence with tokens that fit its row
+  return {reinterpret_cast<const_i32 *>(reinterpret_cast<uintptr_t>(S.table + b * S.table_stride)), S.width - 1, S.page_shift};
+}
+
+// Sums over the lanes up to this one.
+__device__ __forceinline__ uint32_t lanes_before(uint32_t v) {
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, false);  // row_shr: 1, 2, 4, 8
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xf, 0xf, false);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xf, 0xf, false);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, false);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xa, 0xf, false);  // row_bcast: 15 to rows 1 and 3
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false);  // 31 to rows 2 and 3
+  return v;
+}
+
 // Which sequence the unit `id` belongs to, and the how-manieth of its units it is, where sequence b has units(b) of
 // them in a row.  All 64 lanes of a wave call it; false where there is no such unit.
 template <typename F>
@@ -52,22 +76,27 @@ __device__ __forceinline__ bool find_unit(int n_seqs, uint32_t id, F units, int 
   uint32_t before = 0;
   for (int first = 0; first < n_seqs; first += 64) {
     const uint32_t own = first + lane < n_seqs ? units(first + lane) : 0u;
-    uint32_t sum = own;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const uint32_t o = __shfl_up(sum, d, 64);
-      sum += lane >= d ? o : 0u;
-    }
+    const uint32_t sum = lanes_before(own);
     const uint64_t past = __ballot(before + sum > id);
     if (past) {
       const int l = __builtin_ctzll(past);
       b = first + l;
-      k = id - before - (__builtin_amdgcn_readfirstlane(__shfl(sum, l, 64)) - __builtin_amdgcn_readfirstlane(__shfl(own, l, 64)));
+      k = id - before - (uint32_t)__builtin_amdgcn_readlane((int)(sum - own), l);
       return true;
     }
-    before += __builtin_amdgcn_readfirstlane(__shfl(sum, 63, 64));
+    before += (uint32_t)__builtin_amdgcn_readlane((int)sum, 63);
   }
   return false;
+}
+
+// Units of the sequences before b.  All 64 lanes call it.
+template <typename F>
+__device__ __forceinline__ uint32_t units_before(int b, F units) {
+  const int lane = threadIdx.x & 63;
+  uint32_t before = 0;
+  for (int first = 0; first < b; first += 64)
+    before += (uint32_t)__builtin_amdgcn_readlane((int)lanes_before(first + lane < b ? units(first + lane) : 0u), 63);
+  return before;
 }
 
 // 2^(scale - 127)
