@@ -326,7 +326,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_few_kernel(Atte
   uint32_t part;
   if (unit >= (uint32_t)A.few_units || !find_unit(A.s.n_seqs, unit, [&](int i) { return few_parts(A, i, per); }, b, part)) return;
   b = __builtin_amdgcn_readfirstlane(b);
-  const Seq sq = seq_of(A.s, b);
+  const Seq sq = uniform_seq_of(A.s, b);
   const Few few = few_of(A, b);
   const int g = A.group, hq = A.heads * g, D = A.dim;
   T *out = reinterpret_cast<T *>(A.out);
@@ -559,7 +559,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many_kernel(Att
       }, b, tile))
     return;
   b = __builtin_amdgcn_readfirstlane(b);
-  const Seq sq = seq_of(A.s, b);
+  const Seq sq = uniform_seq_of(A.s, b);
   const int len = sq.pos + sq.n, rows = sq.n * g;
   if (len > (A.s.width << A.s.page_shift)) return;  // the kernel for few writes what such rows become
   const int r0 = (int)tile * kManyRows, r1 = min(r0 + kManyRows, rows);
@@ -748,17 +748,32 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many_kernel(Att
 }
 
 // ---- many rows of heads up to 128: a workgroup takes 256 rows, 64 a wave in two columns of 32, so that every operand read
-// from LDS serves two products; one wave a SIMD, with its 512 registers.  Tiles of 64 tokens lie in rings of three
-// for keys and for values, copied straight into LDS (8 bits: widened on the way).  The work on a half tile i is three
-// stages of three halves at a time, which do not wait for each other: scores of i + 1, weights of i, the product of i - 1
-// with its values; so the matrix unit works while the vector unit takes exponentials.
+// from LDS serves two products; one wave a SIMD, with its 512 registers.  Tiles of 64 tokens are copied straight into
+// rings in LDS, two tiles ahead of their use (8 bits: as they are, and widened from there into rings of T).  The work
+// on a half tile i is three stages of three halves at a time, which do not wait for each other: scores of i + 1, weights of i,
+// the product of i - 1 with its values; so the matrix unit works while the vector unit takes exponentials.
 
-// Copies 16 bytes a lane from memory to LDS: lane l's land at `to` + 16 l, `to` the same for all lanes.  Nothing else in the
-// kernel uses m0.
+// Copies of 16 bytes a lane from memory to LDS: lane l's land at `to` + 16 l, `to` the same for all lanes.  Instructions of
+// their own, as the compiler would wait for every copy before each read of LDS; nothing else in the kernel uses
+// m0.  A scalar base is read five wait states after the instruction that wrote it at the earliest.
 __device__ __forceinline__ void copy_piece(const void *from, uint32_t to) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory");
 }
-__device__ __forceinline__ void copies_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ void copy_piece(const void *base, uint32_t off, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory");
+}
+template <typename H>
+__device__ __forceinline__ const H *uniform_pointer(const H *p) {  // one for all lanes, in scalar registers
+  const uint64_t x = reinterpret_cast<uint64_t>(p);
+  return reinterpret_cast<const H *>((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 |
+                                     (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
+}
+// Waits until at most N of this wave's copies are on their way.
+template <int N>
+__device__ __forceinline__ void copies_left() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+static __device__ const u32x4 kZeros = {0, 0, 0, 0};  // what rows of values behind the last entry are copied from
 
 // c += a b with the sums in accumulation registers.  Written as an instruction because the allocator, left the choice,
 // moves them between both halves of the register file around every use of a score.  It does not know the
@@ -793,6 +808,12 @@ __device__ __forceinline__ void settle_products(f32x16 (&o)[N]) {
   asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
 #pragma unroll
   for (int i = 0; i < N; ++i) asm volatile("" : "+a"(o[i]));
+}
+template <int N>
+__device__ __forceinline__ void settle_scores(f32x16 (&s)[N]) {
+  asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+v"(s[i]));
 }
 template <int N>
 __device__ __forceinline__ void before_products(f32x16 (&o)[N]) {
@@ -830,16 +851,30 @@ __device__ __forceinline__ int key_piece(int row, int place) {  // which piece l
 }
 __device__ __forceinline__ int value_place(int d, int c) { return c ^ (d >> 1 & 7); }
 
+// LDS of the kernel: rings of kRing tiles of keys and of values; 8 bits: three tiles of either as they are in memory and their
+// scales; the bits of take_odd.
+template <typename T, bool BYTES, int DP>
+struct Wide {
+  static constexpr int kRing = BYTES ? 3 : 4, kLead = BYTES ? 4 : 3;  // tiles; how far ahead of its use a tile of keys is copied
+  static constexpr int kTile = 64 * DP;                               // entries
+  static constexpr int kRaw = BYTES ? (DP + 63) / 64 : 0;             // copies of a wave for a tile as it is, of keys and of values
+  static constexpr int kCopies = BYTES ? 2 * kRaw + 1 : DP / 16;      // of a wave for a tile of keys and one of values
+  static constexpr uint32_t kKeys = 0, kValues = kRing * kTile * 2, kRawKeys = 2 * kValues, kRawValues = kRawKeys + 3 * kRaw * 4096,
+                            kScales = kRawValues + 3 * kRaw * 4096, kOdds = kScales + (BYTES ? 3 * 1024 : 0),
+                            kOddAt = kOdds + DP * 16, kBytes = kOddAt + 16;
+};
+
 template <typename T, bool BYTES, int DP>
 __global__ __launch_bounds__(256, 1) void attend_wide_kernel(AttendArgs A) {
   typedef std::conditional_t<BYTES, uint8_t, T> H;
   typedef vec<T, 8> Vec8;
-  constexpr int kTile = 64 * DP;  // entries of a tile of keys, and of values
-  constexpr int kMt = DP / 32, kC = DP / 16;
+  typedef Wide<T, BYTES, DP> W;
+  constexpr int kMt = DP / 32, kC = DP / 16, kTile = W::kTile, kLead = W::kLead;
   extern __shared__ __align__(1024) char shared_bytes[];
-  T *keys = reinterpret_cast<T *>(shared_bytes), *values = keys + 3 * kTile;
-  uint8_t *odds = reinterpret_cast<uint8_t *>(values + 3 * kTile);  // as in the kernel above, of one tile
-  volatile int *odd_at = reinterpret_cast<volatile int *>(odds + DP * 16);
+  const T *keys = reinterpret_cast<const T *>(shared_bytes + W::kKeys);
+  T *values = reinterpret_cast<T *>(shared_bytes + W::kValues);
+  uint8_t *odds = reinterpret_cast<uint8_t *>(shared_bytes + W::kOdds);  // as in the kernel above, of one tile
+  volatile int *odd_at = reinterpret_cast<volatile int *>(shared_bytes + W::kOddAt);
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, h = lane >> 5;
   uint32_t id = block_id();
   const int head = (int)(id % A.heads);
@@ -857,7 +892,8 @@ __global__ __launch_bounds__(256, 1) void attend_wide_kernel(AttendArgs A) {
       }, b, tile))
     return;
   b = __builtin_amdgcn_readfirstlane(b);
-  const Seq sq = seq_of(A.s, b);
+  tile = __builtin_amdgcn_readfirstlane(tile);
+  const Seq sq = uniform_seq_of(A.s, b);
   const int len = sq.pos + sq.n, rows = sq.n * g;
   if (len > (A.s.width << A.s.page_shift)) return;  // the kernel for few writes what such rows become
   const int r0 = (int)tile * kWideRows, r1 = min(r0 + kWideRows, rows);
@@ -881,88 +917,91 @@ __global__ __launch_bounds__(256, 1) void attend_wide_kernel(AttendArgs A) {
     for (int c = 0; c < kC; ++c) q[x][c] = load_q<T>(qp, 16 * c + 8 * h, D, mine, A.wide != 0);
   }
 
+  // ---- copies.  Keys: wave w copies tokens 16 w .. + 15, which lie in one page; values: a lane's 16 bytes of every row
+  // that it copies are of the same tokens.
   const int page = 1 << A.s.page_shift, inner = page - 1;
   struct Pages {
-    uint32_t at[4];  // as the table has them
+    uint32_t at[4];  // of 16 tokens each, as the table has them
   };
   const TableRow table = table_row(A.s, b);
   auto pages = [&](int j) {
     const int t = begin + 64 * j;
     return Pages{{table.entry(t), table.entry(t + 16), table.entry(t + 32), table.entry(t + 48)}};
   };
-  auto inside = [&](uint32_t page) { return page < A.s.n_pages; };
-  auto pick = [&](const Pages &pg, int j) {
+  auto inside = [&](uint32_t e) { return e < A.s.n_pages; };
+  auto outside4 = [&](const Pages &pg) {
+    return (inside(pg.at[0]) ? 0u : 1u) | (inside(pg.at[1]) ? 0u : 2u) | (inside(pg.at[2]) ? 0u : 4u) | (inside(pg.at[3]) ? 0u : 8u);
+  };
+  auto pick = [&](const Pages &pg, int j) -> int64_t {
     const uint32_t e = j & 2 ? (j & 1 ? pg.at[3] : pg.at[2]) : (j & 1 ? pg.at[1] : pg.at[0]);
     return inside(e) ? e : 0u;
   };
+  auto slot = [&](int j) { return W::kRing == 4 ? j & 3 : j % 3; };
   const H *kbase = reinterpret_cast<const H *>(A.k) + (int64_t)head * page * D;
   const H *vbase = reinterpret_cast<const H *>(A.v) + (int64_t)head * page * D;
-  constexpr int kPer = 16 / (int)sizeof(H);                         // entries of a piece in memory
-  constexpr int kAll = kTile / kPer, kPieces = (kAll + 255) / 256;  // pieces of a tile, of a thread
-  constexpr int kKRow = DP / kPer, kVRow = 64 / kPer;
-  auto key_from = [&](int m, int t, const Pages &pg, int &row, int &d) {  // piece m of the tile, its row and first entry
-    row = m / kKRow;
-    d = BYTES ? m % kKRow * 16 : 8 * key_piece<DP>(row, m % kKRow);
-    return kbase + (int64_t)pick(pg, row >> 4 & 3) * A.kp + ((t + row) & inner) * D + d;
-  };
-  auto value_from = [&](int m, int t, const Pages &pg, int &d, int &tok) {
-    d = m / kVRow;
-    tok = BYTES ? m % kVRow * 16 : 8 * value_place(d, m % kVRow);
-    return vbase + (int64_t)pick(pg, tok >> 4) * A.vp + (int64_t)d * page + ((t + tok) & inner);
-  };
-  // 16 bits: copies; 8 bits: into registers, from where put_* writes them
-  u32x4 kr[BYTES ? kPieces : 1], vr[BYTES ? kPieces : 1], vsr = {0, 0, 0, 0};
-  uint32_t ksr[BYTES ? kPieces : 1];
-  auto get_keys = [&](int j, const Pages &pg) {
+  constexpr int kRowPieces = DP / (16 / (int)sizeof(H));  // of 16 bytes, of a row of keys in LDS
+  constexpr int kKeyCopies = BYTES ? W::kRaw : DP / 32, kValueCopies = kKeyCopies;
+  uint32_t key_off[kKeyCopies];  // bytes from the wave's first token's key; ~0: nothing
 #pragma unroll
-    for (int e = 0; e < kPieces; ++e) {
-      const int m = (BYTES ? e * 256 : (e * 4 + wave) * 64) + (BYTES ? tid : lane);
-      int row, d;
-      const H *from = key_from(m, begin + 64 * j, pg, row, d);
-      if constexpr (BYTES) {
-        if (m < kAll && d < D) kr[e] = *reinterpret_cast<const u32x4 *>(from);
-        ksr[e] = A.ks[(int64_t)pick(pg, row >> 4 & 3) * A.ksp + head * page + ((begin + 64 * j + row) & inner)];
-      } else if (d < D) {
-        copy_piece(from, (uint32_t)((j % 3) * kTile * 2 + (e * 4 + wave) * 1024));
-      }
+  for (int e = 0; e < kKeyCopies; ++e) {
+    const int m = e * 64 + lane, row = m / kRowPieces;
+    const int d = BYTES ? m % kRowPieces * 16 : 8 * key_piece<DP>(16 * wave + row, m % kRowPieces);
+    key_off[e] = row < 16 && d < D ? (uint32_t)((row * D + d) * sizeof(H)) : ~0u;
+  }
+  // first row of this lane's copies of values and its tokens in the tile
+  const int value_row = BYTES ? wave * 16 + lane / 4 : wave * 8 + lane / 8;
+  const int value_tok = BYTES ? lane % 4 * 16 : 8 * value_place(value_row, lane % 8);
+  constexpr int kValueRows = BYTES ? 64 : 32;  // that all waves' copies of one number take
+  auto copy_keys = [&](int j, const Pages &pg) {
+    const int t = begin + 64 * j + 16 * wave;
+    const H *base = uniform_pointer(kbase + pick(pg, wave) * A.kp + (t & inner) * D);
+    const uint32_t to = BYTES ? W::kRawKeys + (j % 3) * W::kRaw * 4096 + wave * W::kRaw * 1024 : W::kKeys + slot(j) * kTile * 2 + wave * 32 * DP;
+#pragma unroll
+    for (int e = 0; e < kKeyCopies; ++e)
+      if (key_off[e] != ~0u) copy_piece(base, key_off[e], to + e * 1024);
+  };
+  auto copy_values = [&](int j, const Pages &pg) {
+    const H *from = vbase + pick(pg, value_tok >> 4) * A.vp + ((begin + 64 * j + value_tok) & inner) + value_row * page;
+    const uint32_t to = BYTES ? W::kRawValues + (j % 3) * W::kRaw * 4096 + wave * 1024 : W::kValues + slot(j) * kTile * 2 + wave * 1024;
+#pragma unroll
+    for (int e = 0; e < kValueCopies; ++e) {
+      copy_piece(value_row + e * kValueRows < D ? (const void *)from : (const void *)&kZeros, to + e * 4096);
+      from += kValueRows * page;
     }
   };
-  auto get_values = [&](int j, const Pages &pg) {
-#pragma unroll
-    for (int e = 0; e < kPieces; ++e) {
-      const int m = (BYTES ? e * 256 : (e * 4 + wave) * 64) + (BYTES ? tid : lane);
-      int d, tok;
-      const H *from = value_from(m, begin + 64 * j, pg, d, tok);
-      if constexpr (BYTES) {
-        if (m < kAll && d < D) vr[e] = *reinterpret_cast<const u32x4 *>(from);
-        if (e == 0) vsr = *reinterpret_cast<const u32x4 *>(A.vs + (int64_t)pick(pg, tok >> 4) * A.vsp + head * page + ((begin + 64 * j + tok) & inner));
-      } else if (d < D) {
-        copy_piece(from, (uint32_t)((3 + j % 3) * kTile * 2 + (e * 4 + wave) * 1024));
-      }
-    }
+  // 8 bits: scales of the keys of a tile and of the values of the one before it, 64 bytes each (every wave copies all)
+  auto copy_scales = [&](int j, const Pages &pk, const Pages &pv) {
+    const int gr = lane & 3;
+    const int64_t in = head * page + ((begin + 64 * j + 16 * gr) & inner), before = head * page + ((begin + 64 * (j - 1) + 16 * gr) & inner);
+    const uint8_t *from = lane & 4 ? A.vs + pick(pv, gr) * A.vsp + before : A.ks + pick(pk, gr) * A.ksp + in;
+    copy_piece(from, W::kScales + (j % 3) * 1024);
   };
-  auto put_keys = [&](int j) {
+  // 8 bits: a copied tile to the rings
+  auto widen_keys = [&](int j) {
     if constexpr (BYTES) {
 #pragma unroll
-      for (int e = 0; e < kPieces; ++e) {
-        const int m = e * 256 + tid, row = m / kKRow, c = m % kKRow * 2;
-        if (m >= kAll || 8 * c >= D) continue;
-        const float by = scale_of(ksr[e]);
-        T *to = keys + (j % 3) * kTile + row * DP;
-        *reinterpret_cast<Vec8 *>(to + 8 * key_place<DP>(row, c)) = widen<T>(u32x2{kr[e][0], kr[e][1]}, by);
-        *reinterpret_cast<Vec8 *>(to + 8 * key_place<DP>(row, c + 1)) = widen<T>(u32x2{kr[e][2], kr[e][3]}, by);
+      for (int e = 0; e < W::kRaw; ++e) {
+        const int m = e * 256 + tid, w = m / (W::kRaw * 64), i = m % (W::kRaw * 64), row = 16 * w + i / kRowPieces, c = i % kRowPieces * 2;
+        if (i >= 16 * kRowPieces || 8 * c >= D) continue;
+        const u32x4 x = *reinterpret_cast<const u32x4 *>(shared_bytes + W::kRawKeys + (j % 3) * W::kRaw * 4096 + m * 16);
+        const float by = scale_of((uint8_t)shared_bytes[W::kScales + (j % 3) * 1024 + row]);
+        T *to = const_cast<T *>(keys) + slot(j) * kTile + row * DP;
+        *reinterpret_cast<Vec8 *>(to + 8 * key_place<DP>(row, c)) = widen<T>(u32x2{x[0], x[1]}, by);
+        *reinterpret_cast<Vec8 *>(to + 8 * key_place<DP>(row, c + 1)) = widen<T>(u32x2{x[2], x[3]}, by);
       }
     }
   };
-  auto put_values = [&](int j) {
+  auto widen_values = [&](int j) {
     if constexpr (BYTES) {
+      const u32x4 by = *reinterpret_cast<const u32x4 *>(shared_bytes + W::kScales + ((j + 1) % 3) * 1024 + 64 + tid % 4 * 16);
 #pragma unroll
-      for (int e = 0; e < kPieces; ++e) {
-        const int m = e * 256 + tid, d = m / kVRow, c = m % kVRow * 2;
-        if (m >= kAll || d >= D) continue;
-        T *to = values + (j % 3) * kTile + d * 64;
-        *reinterpret_cast<Vec8 *>(to + 8 * value_place(d, c)) = widen<T>(u32x2{vr[e][0], vr[e][1]}, u32x2{vsr[0], vsr[1]});
-        *reinterpret_cast<Vec8 *>(to + 8 * value_place(d, c + 1)) = widen<T>(u32x2{vr[e][2], vr[e][3]}, u32x2{vsr[2], vsr[3]});
+      for (int e = 0; e < W::kRaw; ++e) {
+        const int m = e * 256 + tid, d = m / 4, c = m % 4 * 2;
+        if (d >= DP) continue;
+        const u32x4 x = *reinterpret_cast<const u32x4 *>(shared_bytes + W::kRawValues + (j % 3) * W::kRaw * 4096 + m * 16);
+        T *to = values + slot(j) * kTile + d * 64;
+        *reinterpret_cast<Vec8 *>(to + 8 * value_place(d, c)) = widen<T>(u32x2{x[0], x[1]}, u32x2{by[0], by[1]});
+        *reinterpret_cast<Vec8 *>(to + 8 * value_place(d, c + 1)) = widen<T>(u32x2{x[2], x[3]}, u32x2{by[2], by[3]});
       }
     }
   };
@@ -975,48 +1014,38 @@ __global__ __launch_bounds__(256, 1) void attend_wide_kernel(AttendArgs A) {
   for (int c = 0; c < kC; ++c) koff[c] = ki * DP + 8 * key_place<DP>(ki, 2 * c + h);
 #pragma unroll
   for (int c = 0; c < 4; ++c) voff[c] = col * 64 + 8 * value_place(col, 4 * (c / 2) + 2 * h + c % 2);
-  auto scores = [&](f32x16 (&s)[2], const T *k, int u) {
-#pragma unroll
-    for (int c = 0; c < kC; ++c) {
-      const Vec8 a = *reinterpret_cast<const Vec8 *>(k + 32 * u * DP + koff[c]);
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        if (c == 0) {
-          f32x16 zero;
-#pragma unroll
-          for (int i = 0; i < 16; ++i) zero[i] = 0.f;
-          s[x] = mfma32<T>(a, q[x][c], zero);
-        } else {
-          s[x] = mfma32<T>(a, q[x][c], s[x]);
-        }
-      }
-    }
-  };
-  auto value_piece = [&](const T *v, int u, int m) {  // of the half's kC products' first operands
+  auto key_piece_of = [&](const T *k, int u, int c) { return *reinterpret_cast<const Vec8 *>(k + 32 * u * DP + koff[c]); };
+  auto value_piece_of = [&](const T *v, int u, int m) {  // of the half's kC products' first operands
     return *reinterpret_cast<const Vec8 *>(v + m / 2 * 32 * 64 + voff[2 * u + m % 2]);
   };
   constexpr float kBelow = std::is_same<T, f16_t>::value ? 8.f : 0.f;  // as in Rows::weigh
   // One half's stage: weights of s to p, scores of half ku of tile k to next, and half vu of the values v times pp.
-  // Every product is followed by its share of the vector instructions, and nothing is moved across.
+  // Every product is followed by its share of the vector instructions, and nothing is moved across: of an entry the
+  // argument of the exponential, the exponential, and what uses it behind three products in a row.
   auto stage = [&](f32x16 (&s)[2], Vec8 (&p)[2][2], f32x16 (&next)[2], const T *k, int ku, const T *v, int vu, const Vec8 (&pp)[2][2]) {
-    constexpr int kSlots = 4 * kC, kFirst = 4;  // products; the first kFirst share the maxima
-    Vec8 ka[2], va[2];
-    ka[0] = *reinterpret_cast<const Vec8 *>(k + 32 * ku * DP + koff[0]);
-    va[0] = value_piece(v, vu, 0);
-    float top[2], to[2], by[2], from[2], sum[2] = {0.f, 0.f}, w[32];
+    constexpr int kSlots = 4 * kC, kFirst = 4, kOver = kSlots - kFirst - 2;  // products; the first kFirst share the maxima
+    constexpr int kAhead = 2, kHeld = kAhead + 1;                            // operands on their way from LDS
+    Vec8 ka[kHeld], va[kHeld];
+#pragma unroll
+    for (int c = 0; c < kAhead; ++c) ka[c] = key_piece_of(k, ku, c), va[c] = value_piece_of(v, vu, c);
+    float top[2][4], to[2], by[2], from[2], sum[2] = {0.f, 0.f}, w[32];
     bool grows = false;
     auto vector_share = [&](int slot) {
-      if (slot < 2) {
-        top[slot] = fmaxf(s[slot][0], s[slot][1]);
+      if (slot == 0) {
 #pragma unroll
-        for (int i = 2; i < 16; ++i) top[slot] = fmaxf(top[slot], s[slot][i]);
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) top[x][i] = fmaxf(fmaxf(s[x][4 * i], s[x][4 * i + 1]), fmaxf(s[x][4 * i + 2], s[x][4 * i + 3]));
+      } else if (slot == 1) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) top[x][0] = fmaxf(fmaxf(top[x][0], top[x][1]), fmaxf(top[x][2], top[x][3]));
       } else if (slot == 2) {
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-          top[x] = fmaxf(top[x], partner(top[x])) * A.scale;
-          const bool more = top[x] > st[x].m + (kSlack + kBelow);
+          const float t = fmaxf(top[x][0], partner(top[x][0])) * A.scale;
+          const bool more = t > st[x].m + (kSlack + kBelow);
           grows = grows || more;
-          to[x] = more ? top[x] - kBelow : st[x].m;
+          to[x] = more ? t - kBelow : st[x].m;
           from[x] = to[x] == -__builtin_inff() ? 0.f : to[x];
         }
       } else if (slot == 3) {
@@ -1025,33 +1054,34 @@ __global__ __launch_bounds__(256, 1) void attend_wide_kernel(AttendArgs A) {
           by[x] = to[x] == st[x].m ? 1.f : __builtin_amdgcn_exp2f(st[x].m - to[x]);
           st[x].m = to[x];
         }
-      } else {
-        const int lo = (slot - kFirst) * 32 / (kSlots - kFirst), hi = (slot + 1 - kFirst) * 32 / (kSlots - kFirst);
+      }
 #pragma unroll
-        for (int e = lo; e < hi; ++e) {
-          const int x = e / 16, i = e % 16;
-          w[e] = __builtin_amdgcn_exp2f(fmaf(s[x][i], A.scale, -from[x]));
+      for (int e = 0; e < 32; ++e) {
+        const int x = e / 16, i = e % 16, at = kFirst + e * kOver / 32;
+        if (slot == at + 2) {
           asm volatile("" : "+v"(w[e]));  // here, not behind the branch at the stage's end
           sum[x] += w[e];
           if (i % 2) p[x][i / 8][i % 8 - 1] = (T)w[e - 1], p[x][i / 8][i % 8] = (T)w[e];
         }
+        if (slot == at + 1) w[e] = __builtin_amdgcn_exp2f(w[e]);
+        if (slot == at) w[e] = fmaf(s[x][i], A.scale, -from[x]);
       }
     };
 #pragma unroll
     for (int c = 0; c < kC; ++c) {
-      if (c + 1 < kC) {
-        ka[(c + 1) % 2] = *reinterpret_cast<const Vec8 *>(k + 32 * ku * DP + koff[c + 1]);
-        va[(c + 1) % 2] = value_piece(v, vu, c + 1);
+      if (c + kAhead < kC) {
+        ka[(c + kAhead) % kHeld] = key_piece_of(k, ku, c + kAhead);
+        va[(c + kAhead) % kHeld] = value_piece_of(v, vu, c + kAhead);
       }
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        score_product<T>(next[x], ka[c % 2], q[x][c], c == 0);
+        score_product<T>(next[x], ka[c % kHeld], q[x][c], c == 0);
         vector_share(4 * c + x);
         __builtin_amdgcn_sched_barrier(0);
       }
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        add_product<T>(st[x].o[c / 2], va[c % 2], pp[x][c % 2]);
+        add_product<T>(st[x].o[c / 2], va[c % kHeld], pp[x][c % 2]);
         vector_share(4 * c + 2 + x);
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -1074,25 +1104,43 @@ __global__ __launch_bounds__(256, 1) void attend_wide_kernel(AttendArgs A) {
 #pragma unroll
     for (int c = 0; c < kC; ++c) asm volatile("" : "+a"(q[x][c]));  // queries stay in accumulation registers too
   if (n > 0) {
-    // zeros where no entry is written to, and in the tile that stands before the first
-    for (int e = tid; e < (D < DP ? 6 : 0) * kTile / 8; e += 256) reinterpret_cast<u32x4 *>(keys)[e] = u32x4{0, 0, 0, 0};
-    if (D == DP)
-      for (int e = tid; e < kTile / 8; e += 256) reinterpret_cast<u32x4 *>(values + 2 * kTile)[e] = u32x4{0, 0, 0, 0};
+    // zeros where no key's entry is written to, and in the tile of values that stands before the first
+    constexpr uint32_t kBefore = W::kValues + (W::kRing - 1) * kTile * 2;
+    for (uint32_t e = tid * 16; e < (D < DP ? W::kValues : 0u); e += 4096) *reinterpret_cast<u32x4 *>(shared_bytes + e) = u32x4{0, 0, 0, 0};
+    for (uint32_t e = tid * 16; e < kTile * 2; e += 4096) *reinterpret_cast<u32x4 *>(shared_bytes + kBefore + e) = u32x4{0, 0, 0, 0};
     if (tid == 0) *odd_at = 0;
-    if (D < DP) __syncthreads();
-    Pages now = pages(0), next = now, later = now;
-    if (n > 1) next = pages(1);
-    get_keys(0, now);
-    put_keys(0);
-    get_values(0, now);
-    put_values(0);
-    if (n > 1) {
-      get_keys(1, next);
-      put_keys(1);
-      if (n > 2) later = pages(2);
-    }
-    copies_done();
     __syncthreads();
+    uint32_t bad = 0;  // bits of 16 tokens each without a page, of this tile and those after it
+    Pages pk = pages(0), pv = pk;  // of the tiles of keys and of values that are copied next
+    auto copy_next = [&](int j) {  // keys of tile j and values of j - 1, whose pages are pk and pv
+      if (j < n) {
+        copy_keys(j, pk);
+        bad |= outside4(pk) << (4 * kLead);
+      }
+      if constexpr (BYTES) {
+        if (j - 1 < n) copy_scales(j, pk, pv);
+      }
+      if (j > 0 && j - 1 < n) copy_values(j - 1, pv);
+    };
+#pragma unroll
+    for (int j = 0; j < 3; ++j) {
+      const Pages after = j + 1 < n ? pages(j + 1) : pk;
+      copy_next(j);
+      pv = pk, pk = after;
+      bad >>= 4;
+    }
+    copies_left<0>();
+    __syncthreads();
+    if constexpr (BYTES) {  // tiles 0 and 1 of keys and 0 of values; then the next into their places
+      widen_keys(0);
+      if (n > 1) widen_keys(1);
+      widen_values(0);
+      __syncthreads();
+      const Pages after = 4 < n ? pages(4) : pk;
+      copy_next(3);
+      pv = pk, pk = after;
+      bad >>= 4;
+    }
     f32x16 s0[2], s1[2];
     Vec8 pa[2][2], pb[2][2];
 #pragma unroll
@@ -1101,18 +1149,25 @@ __global__ __launch_bounds__(256, 1) void attend_wide_kernel(AttendArgs A) {
       for (int j = 0; j < 2; ++j)
 #pragma unroll
         for (int i = 0; i < 8; ++i) pb[x][j][i] = (T)0.f;
-    if (active) scores(s0, keys, 0);
+    if (active)
+#pragma unroll
+      for (int c = 0; c < kC; ++c)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) score_product<T>(s0[x], key_piece_of(keys, 0, c), q[x][c], c == 0);
+    settle_scores(s0);
     for (int j = 0; j < n; ++j) {
       const int t = begin + 64 * j;
-      copies_done();
-      __syncthreads();  // tiles j + 1 of keys and j of values are there, and what is overwritten now has been read
-      Pages after = later;
-      if (j + 3 < n) after = pages(j + 3);
-      if (j + 2 < n) get_keys(j + 2, later);
-      if (j + 1 < n) get_values(j + 1, next);
-      const T *k1 = keys + (j + 1) % 3 * kTile, *k0 = keys + j % 3 * kTile;
-      T *v0 = values + j % 3 * kTile;
-      const T *v1 = values + (j + 2) % 3 * kTile;  // tile j - 1
+      // of the copies only those of the iteration before may be on their way
+      if (j + kLead - 1 < n)
+        copies_left<W::kCopies>();
+      else
+        copies_left<0>();
+      __syncthreads();  // and what is overwritten now has been read
+      const Pages after = j + kLead + 1 < n ? pages(j + kLead + 1) : pk;
+      copy_next(j + kLead);
+      const T *k1 = keys + slot(j + 1) * kTile, *k0 = keys + slot(j) * kTile;
+      T *v0 = values + slot(j) * kTile;
+      const T *v1 = values + slot(j + W::kRing - 1) * kTile;  // tile j - 1
       const bool partly = t + 63 > all_hi || t < all_lo;  // some row does not see all tokens
       if (partly) {
         for (int m = tid; m < D * 8; m += 256) {
@@ -1144,27 +1199,30 @@ __global__ __launch_bounds__(256, 1) void attend_wide_kernel(AttendArgs A) {
         }
       }
       if (active) {
-        const bool edge = partly || !(inside(now.at[0]) && inside(now.at[1]) && inside(now.at[2]) && inside(now.at[3]));
+        const bool edge = partly || (bad & 15);
         const int first = t + 16 * h;
         if (edge)
 #pragma unroll
-          for (int x = 0; x < 2; ++x) mask16(s0[x], first, lo[x], hi[x], !inside(h ? now.at[1] : now.at[0]));
+          for (int x = 0; x < 2; ++x) mask16(s0[x], first, lo[x], hi[x], bad >> h & 1);
         stage(s0, pa, s1, k0, 1, v1, 1, pb);
         if (edge)
 #pragma unroll
-          for (int x = 0; x < 2; ++x) mask16(s1[x], first + 32, lo[x], hi[x], !inside(h ? now.at[3] : now.at[2]));
+          for (int x = 0; x < 2; ++x) mask16(s1[x], first + 32, lo[x], hi[x], bad >> (2 + h) & 1);
         stage(s1, pb, s0, k1, 0, v0, 0, pa);
       }
-      if (j + 2 < n) put_keys(j + 2);
-      if (j + 1 < n) put_values(j + 1);
-      now = next, next = later, later = after;
+      if constexpr (BYTES) {
+        if (j + 2 < n) widen_keys(j + 2);
+        if (j + 1 < n) widen_values(j + 1);
+      }
+      pv = pk, pk = after;
+      bad >>= 4;
     }
     if (active) {
-      const T *v = values + (n - 1) % 3 * kTile;
+      const T *v = values + slot(n - 1) * kTile;
 #pragma unroll
       for (int m = 0; m < kC; ++m)
 #pragma unroll
-        for (int x = 0; x < 2; ++x) add_product<T>(st[x].o[m / 2], value_piece(v, 1, m), pb[x][m % 2]);
+        for (int x = 0; x < 2; ++x) add_product<T>(st[x].o[m / 2], value_piece_of(v, 1, m), pb[x][m % 2]);
     }
   }
   if (!active) return;
@@ -1271,7 +1329,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs A) {
 template <typename T, bool BYTES, int DP>
 hipError_t attend_run(const AttendArgs &A, hipStream_t st) {
   const size_t few = (size_t)4 * 4 * std::max(A.few_rows * (DP + 4), 2 * DP);
-  const size_t many = DP <= kWideDim ? (size_t)6 * 64 * DP * 2 + DP * 16 + 16
+  const size_t many = DP <= kWideDim ? (size_t)Wide<T, BYTES, DP>::kBytes
                                      : (size_t)2 * (kManyStep * (DP + 8) + DP * (kManyStep + 8)) * 2 + 2 * DP * 16 + 16;
   auto *few_kernel = attend_few_kernel<T, BYTES, DP>;
   void (*many_kernel)(AttendArgs);

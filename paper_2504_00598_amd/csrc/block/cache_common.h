@@ -35,6 +35,12 @@ __device__ __forceinline__ Seq seq_of(const SeqArgs &S, int b) {
   return q;
 }
 
+// The same of a sequence that is one for all lanes, in scalar registers.
+__device__ __forceinline__ Seq uniform_seq_of(const SeqArgs &S, int b) {
+  const Seq q = seq_of(S, b);
+  return {__builtin_amdgcn_readfirstlane(q.row), __builtin_amdgcn_readfirstlane(q.n), __builtin_amdgcn_readfirstlane(q.pos)};
+}
+
 // The page of token p >= 0 of sequence b, and whether it is one of the cache's (else page 0).
 __device__ __forceinline__ uint32_t page_of(const SeqArgs &S, int b, int p, bool &ok) {
   const int at = p >> S.page_shift;
