@@ -295,6 +295,16 @@ __device__ __forceinline__ void times_scales(f32x16 &s, u32x4 w) {
   for (int i = 0; i < 16; ++i) s[i] *= scale_of(w[i / 4] >> (8 * (i % 4)) & 0xff);
 }
 
+// Pages of four runs of 16 tokens, as the table has them, and one of them: by masks, as the compiler would make an array in
+// memory of what is chosen by an index.
+struct Pages4 {
+  uint32_t a, b, c, d;
+};
+__device__ __forceinline__ uint32_t one_of(const Pages4 &p, int i) {
+  const uint32_t low = 0u - (uint32_t)(i & 1), high = 0u - (uint32_t)(i >> 1 & 1);
+  return (((p.a & ~low) | (p.b & low)) & ~high) | (((p.c & ~low) | (p.d & low)) & high);
+}
+
 // The lowest n of 32 bits, all for n >= 32 and none for n <= 0.
 __device__ __forceinline__ uint32_t bits_of(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1; }
 
@@ -580,14 +590,12 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many_kernel(Att
   const int page = 1 << A.s.page_shift, inner = page - 1;
   u32x4 kr[kPieces], vr[kPieces], vsr = {0, 0, 0, 0};
   uint32_t ksr[BYTES ? kPieces : 1];
-  struct Pages {
-    uint32_t at[4];  // as the table has them
-  };
+  typedef Pages4 Pages;
   const TableRow table = table_row(A.s, b);
-  auto pages = [&](int t) { return Pages{{table.entry(t), table.entry(t + 16), table.entry(t + 32), table.entry(t + 48)}}; };
+  auto pages = [&](int t) { return Pages{table.entry(t), table.entry(t + 16), table.entry(t + 32), table.entry(t + 48)}; };
   auto inside = [&](uint32_t page) { return page < A.s.n_pages; };
   auto pick = [&](const Pages &pg, int j) {
-    const uint32_t e = j & 2 ? (j & 1 ? pg.at[3] : pg.at[2]) : (j & 1 ? pg.at[1] : pg.at[0]);
+    const uint32_t e = one_of(pg, j);
     return inside(e) ? e : 0u;
   };
   constexpr int kKRow = DP / kPer, kVRow = kManyStep / kPer;  // pieces of a row
@@ -688,11 +696,11 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many_kernel(Att
 #pragma unroll
         for (int u = 0; u < 2; ++u)
           s[u] = mfma32<T>(*reinterpret_cast<const vec<T, 8> *>(k + (32 * u + ki) * kKLd + 16 * c + 8 * h), q[c], s[u]);
-      const bool edge = partly(t) || !(inside(now.at[0]) && inside(now.at[1]) && inside(now.at[2]) && inside(now.at[3]));
+      const bool edge = partly(t) || !(inside(now.a) && inside(now.b) && inside(now.c) && inside(now.d));
       const int first = t + 16 * h;
       if (edge) {
-        mask16(s[0], first, lo, hi, !inside(h ? now.at[1] : now.at[0]));
-        mask16(s[1], first + 32, lo, hi, !inside(h ? now.at[3] : now.at[2]));
+        mask16(s[0], first, lo, hi, !inside(h ? now.b : now.a));
+        mask16(s[1], first + 32, lo, hi, !inside(h ? now.d : now.c));
       }
       vec<T, 8> w[4];
       st.weigh(s, A.scale);
@@ -920,20 +928,18 @@ __global__ __launch_bounds__(256, 1) void attend_wide_kernel(AttendArgs A) {
   // ---- copies.  Keys: wave w copies tokens 16 w .. + 15, which lie in one page; values: a lane's 16 bytes of every row
   // that it copies are of the same tokens.
   const int page = 1 << A.s.page_shift, inner = page - 1;
-  struct Pages {
-    uint32_t at[4];  // of 16 tokens each, as the table has them
-  };
+  typedef Pages4 Pages;
   const TableRow table = table_row(A.s, b);
   auto pages = [&](int j) {
     const int t = begin + 64 * j;
-    return Pages{{table.entry(t), table.entry(t + 16), table.entry(t + 32), table.entry(t + 48)}};
+    return Pages{table.entry(t), table.entry(t + 16), table.entry(t + 32), table.entry(t + 48)};
   };
   auto inside = [&](uint32_t e) { return e < A.s.n_pages; };
   auto outside4 = [&](const Pages &pg) {
-    return (inside(pg.at[0]) ? 0u : 1u) | (inside(pg.at[1]) ? 0u : 2u) | (inside(pg.at[2]) ? 0u : 4u) | (inside(pg.at[3]) ? 0u : 8u);
+    return (inside(pg.a) ? 0u : 1u) | (inside(pg.b) ? 0u : 2u) | (inside(pg.c) ? 0u : 4u) | (inside(pg.d) ? 0u : 8u);
   };
   auto pick = [&](const Pages &pg, int j) -> int64_t {
-    const uint32_t e = j & 2 ? (j & 1 ? pg.at[3] : pg.at[2]) : (j & 1 ? pg.at[1] : pg.at[0]);
+    const uint32_t e = one_of(pg, j);
     return inside(e) ? e : 0u;
   };
   auto slot = [&](int j) { return W::kRing == 4 ? j & 3 : j % 3; };
