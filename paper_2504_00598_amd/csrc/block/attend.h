@@ -295,6 +295,13 @@ __device__ __forceinline__ void times_scales(f32x16 &s, u32x4 w) {
   for (int i = 0; i < 16; ++i) s[i] *= scale_of(w[i / 4] >> (8 * (i % 4)) & 0xff);
 }
 
+// The largest of three, without a step for each operand that makes signalling NaN quiet.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+
 // Pages of four runs of 16 tokens, as the table has them, and one of them: by masks, as the compiler would make an array in
 // memory of what is chosen by an index.
 struct Pages4 {
@@ -1028,12 +1035,18 @@ __global__ __launch_bounds__(256, 1) void attend_wide_kernel(AttendArgs A) {
   // One half's stage: weights of s to p, scores of half ku of tile k to next, and half vu of the values v times pp.
   // Every product is followed by its share of the vector instructions, and nothing is moved across: of an entry the
   // argument of the exponential, the exponential, and what uses it behind three products in a row.
-  auto stage = [&](f32x16 (&s)[2], Vec8 (&p)[2][2], f32x16 (&next)[2], const T *k, int ku, const T *v, int vu, const Vec8 (&pp)[2][2]) {
+  constexpr int kAhead = 2, kHeld = kAhead + 1;  // operands on their way from LDS
+  Vec8 first_k[kAhead], first_v[kAhead];         // of the next stage
+  auto first_pieces = [&](const T *k, int ku, const T *v, int vu) {
+#pragma unroll
+    for (int c = 0; c < kAhead; ++c) first_k[c] = key_piece_of(k, ku, c), first_v[c] = value_piece_of(v, vu, c);
+  };
+  auto stage = [&](f32x16 (&s)[2], Vec8 (&p)[2][2], f32x16 (&next)[2], const T *k, int ku, const T *v, int vu, const Vec8 (&pp)[2][2],
+                   const T *then_k, int then_ku, const T *then_v, int then_vu) {
     constexpr int kSlots = 4 * kC, kFirst = 4, kOver = kSlots - kFirst - 2;  // products; the first kFirst share the maxima
-    constexpr int kAhead = 2, kHeld = kAhead + 1;                            // operands on their way from LDS
     Vec8 ka[kHeld], va[kHeld];
 #pragma unroll
-    for (int c = 0; c < kAhead; ++c) ka[c] = key_piece_of(k, ku, c), va[c] = value_piece_of(v, vu, c);
+    for (int c = 0; c < kAhead; ++c) ka[c] = first_k[c], va[c] = first_v[c];
     float top[2][4], to[2], by[2], from[2], sum[2] = {0.f, 0.f}, w[32];
     bool grows = false;
     auto vector_share = [&](int slot) {
@@ -1041,14 +1054,17 @@ __global__ __launch_bounds__(256, 1) void attend_wide_kernel(AttendArgs A) {
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) top[x][i] = fmaxf(fmaxf(s[x][4 * i], s[x][4 * i + 1]), fmaxf(s[x][4 * i + 2], s[x][4 * i + 3]));
+          for (int i = 0; i < 4; ++i) top[x][i] = max3(s[x][4 * i], s[x][4 * i + 1], s[x][4 * i + 2]);
       } else if (slot == 1) {
 #pragma unroll
-        for (int x = 0; x < 2; ++x) top[x][0] = fmaxf(fmaxf(top[x][0], top[x][1]), fmaxf(top[x][2], top[x][3]));
+        for (int x = 0; x < 2; ++x) {
+          top[x][0] = max3(top[x][0], s[x][3], s[x][7]), top[x][1] = max3(top[x][1], s[x][11], s[x][15]);
+          top[x][0] = max3(top[x][0], top[x][2], top[x][3]);
+        }
       } else if (slot == 2) {
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-          const float t = fmaxf(top[x][0], partner(top[x][0])) * A.scale;
+          const float t = max3(top[x][0], top[x][1], partner(max3(top[x][0], top[x][1], top[x][1]))) * A.scale;
           const bool more = t > st[x].m + (kSlack + kBelow);
           grows = grows || more;
           to[x] = more ? t - kBelow : st[x].m;
@@ -1065,9 +1081,9 @@ __global__ __launch_bounds__(256, 1) void attend_wide_kernel(AttendArgs A) {
       for (int e = 0; e < 32; ++e) {
         const int x = e / 16, i = e % 16, at = kFirst + e * kOver / 32;
         if (slot == at + 2) {
-          asm volatile("" : "+v"(w[e]));  // here, not behind the branch at the stage's end
           sum[x] += w[e];
           if (i % 2) p[x][i / 8][i % 8 - 1] = (T)w[e - 1], p[x][i / 8][i % 8] = (T)w[e];
+          if (i % 8 == 7) asm volatile("" : "+v"(p[x][i / 8]), "+v"(sum[x]));  // here, not behind the branch at the stage's end
         }
         if (slot == at + 1) w[e] = __builtin_amdgcn_exp2f(w[e]);
         if (slot == at) w[e] = fmaf(s[x][i], A.scale, -from[x]);
@@ -1078,6 +1094,9 @@ __global__ __launch_bounds__(256, 1) void attend_wide_kernel(AttendArgs A) {
       if (c + kAhead < kC) {
         ka[(c + kAhead) % kHeld] = key_piece_of(k, ku, c + kAhead);
         va[(c + kAhead) % kHeld] = value_piece_of(v, vu, c + kAhead);
+      } else {
+        first_k[c + kAhead - kC] = key_piece_of(then_k, then_ku, c + kAhead - kC);
+        first_v[c + kAhead - kC] = value_piece_of(then_v, then_vu, c + kAhead - kC);
       }
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
@@ -1161,6 +1180,7 @@ __global__ __launch_bounds__(256, 1) void attend_wide_kernel(AttendArgs A) {
 #pragma unroll
         for (int x = 0; x < 2; ++x) score_product<T>(s0[x], key_piece_of(keys, 0, c), q[x][c], c == 0);
     settle_scores(s0);
+    first_pieces(keys, 1, values + (W::kRing - 1) * kTile, 1);
     for (int j = 0; j < n; ++j) {
       const int t = begin + 64 * j;
       // of the copies only those of the iteration before may be on their way
@@ -1210,11 +1230,11 @@ __global__ __launch_bounds__(256, 1) void attend_wide_kernel(AttendArgs A) {
         if (edge)
 #pragma unroll
           for (int x = 0; x < 2; ++x) mask16(s0[x], first, lo[x], hi[x], bad >> h & 1);
-        stage(s0, pa, s1, k0, 1, v1, 1, pb);
+        stage(s0, pa, s1, k0, 1, v1, 1, pb, k1, 0, v0, 0);
         if (edge)
 #pragma unroll
           for (int x = 0; x < 2; ++x) mask16(s1[x], first + 32, lo[x], hi[x], bad >> (2 + h) & 1);
-        stage(s1, pb, s0, k1, 0, v0, 0, pa);
+        stage(s1, pb, s0, k1, 0, v0, 0, pa, k1, 1, v0, 1);
       }
       if constexpr (BYTES) {
         if (j + 2 < n) widen_keys(j + 2);
