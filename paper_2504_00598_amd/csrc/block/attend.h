@@ -3,7 +3,7 @@
 // A row is one head of one new token: query q, token p of its sequence.  Over the tokens j that it sees, with
 // s_j = scale q . k_j:  m = max s_j,  l = sum exp(s_j - m),  o = sum exp(s_j - m) v_j / l,  lse = m + ln l.
 // One pass over the tokens: m and l run along, and what is summed so far is multiplied by exp(m_old - m_new)
-// where m grows.  It grows only when the new maximum is over it by more than 2^kSlack, which leaves every ratio as it is.
+// where m grows.  It follows the maximum only when that is far over it, which leaves every ratio as it is.
 //
 // The heads that share a key head, and the tokens of a chunk, are rows of one product.  Scores are made transposed,
 // S^T = K Q^T by 32x32x16 products of 32 tokens and 32 rows: a lane holds one row's scores of 16 tokens, so that
@@ -58,7 +58,14 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr float kSlack = 6.f;
+// How far below the running maximum (in powers of two) m is set, and how far the maximum may grow above that before m
+// follows.  The range of the weights' type is used: bfloat16 has that of 32 bits, so weights up to 2^20 lose nothing, and
+// multiplying what is summed so far, which a wave does when one of its rows asks for it, stays rare.  float16 has no bits below
+// 2^-24 and ends at 2^16: m stays 8 below the maximum, and weights go up to 2^14.
+template <typename T>
+constexpr float kBelow = std::is_same<T, f16_t>::value ? 8.f : 0.f;
+template <typename T>
+constexpr float kGrowth = std::is_same<T, f16_t>::value ? 14.f : 20.f;
 constexpr float kLn2F = 0.693147180559945309f;
 
 template <typename T>
@@ -249,8 +256,7 @@ struct Rows {
       for (int i = 0; i < 16; ++i) p[2 * u + i / 8][i % 8] = (T)s[u][i];
   }
 
-  // Scores to weights exp2(c s - m).  float16 has no bits below 2^-24, so m stays 8 below
-  // the maximum there and weights go up to 2^14.
+  // Scores to weights exp2(c s - m).
   template <int N>
   __device__ __forceinline__ void weigh(f32x16 (&s)[N], float c) {
     float top = s[0][0];
@@ -259,9 +265,8 @@ struct Rows {
 #pragma unroll
       for (int i = 0; i < 16; ++i) top = fmaxf(top, s[u][i]);
     top = fmaxf(top, partner(top)) * c;
-    constexpr float kBelow = std::is_same<T, f16_t>::value ? 8.f : 0.f;
-    if (__any(top > m + (kSlack + kBelow))) {
-      const float to = top > m + (kSlack + kBelow) ? top - kBelow : m;
+    if (__any(top > m + kGrowth<T>)) {
+      const float to = top > m + kGrowth<T> ? top - kBelow<T> : m;
       const float by = to == m ? 1.f : __builtin_amdgcn_exp2f(m - to);
       m = to;
       l *= by;
@@ -843,7 +848,7 @@ __device__ __forceinline__ void times_sums(f32x16 &o, float by) {
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     float x = o[i], y;
-    asm volatile("v_accvgpr_read_b32 %1, %0\n\ts_nop 1\n\tv_mul_f32 %1, %1, %2\n\ts_nop 1\n\tv_accvgpr_write_b32 %0, %1"
+    asm volatile("v_accvgpr_read_b32 %1, %0\n\tv_mul_f32 %1, %1, %2\n\tv_accvgpr_write_b32 %0, %1"
                  : "+a"(x), "=&v"(y) : "v"(by));
     o[i] = x;
   }
@@ -1031,7 +1036,6 @@ __global__ __launch_bounds__(256, 1) void attend_wide_kernel(AttendArgs A) {
   auto value_piece_of = [&](const T *v, int u, int m) {  // of the half's kC products' first operands
     return *reinterpret_cast<const Vec8 *>(v + m / 2 * 32 * 64 + voff[2 * u + m % 2]);
   };
-  constexpr float kBelow = std::is_same<T, f16_t>::value ? 8.f : 0.f;  // as in Rows::weigh
   // One half's stage: weights of s to p, scores of half ku of tile k to next, and half vu of the values v times pp.
   // Every product is followed by its share of the vector instructions, and nothing is moved across: of an entry the
   // argument of the exponential, the exponential, and what uses it behind three products in a row.
@@ -1065,9 +1069,9 @@ __global__ __launch_bounds__(256, 1) void attend_wide_kernel(AttendArgs A) {
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
           const float t = max3(top[x][0], top[x][1], partner(max3(top[x][0], top[x][1], top[x][1]))) * A.scale;
-          const bool more = t > st[x].m + (kSlack + kBelow);
+          const bool more = t > st[x].m + kGrowth<T>;
           grows = grows || more;
-          to[x] = more ? t - kBelow : st[x].m;
+          to[x] = more ? t - kBelow<T> : st[x].m;
           from[x] = to[x] == -__builtin_inff() ? 0.f : to[x];
         }
       } else if (slot == 3) {
