@@ -171,7 +171,7 @@ int cfp_experts_bwd(const cfp_experts_desc *d, const void *dy, int64_t dy_stride
 
 /* Keys [n_pages][heads][page][dim] and values [n_pages][heads][dim][page]: a value's tokens lie behind each other, as
  * the product over tokens takes them.  Entries of CFP_DT_E4M3 stand for themselves times 2^(scale - 127) with a scale
- * for each token and head, [n_pages][heads][page].  Pages may lie apart; the inner dimensions are contiguous. */
+ * from 1 to 254 for each token and head, [n_pages][heads][page].  Pages may lie apart; the inner dimensions are contiguous. */
 typedef struct {
   int64_t n_pages;                            /* 1 .. 2^31 - 1 */
   int32_t page;                               /* tokens in a page: 16, 32, 64, 128 or 256 */

@@ -547,7 +547,7 @@ class KVCache:
     """Keys and values of past tokens in pages.
 
     k [pages][heads][page][dim] and v [pages][heads][dim][page], float16, bfloat16 or float8_e4m3fn; the last with
-    k_scale, v_scale [pages][heads][page] uint8: an entry stands for itself times 2^(scale - 127).  Pages may lie apart (a
+    k_scale, v_scale [pages][heads][page] uint8: an entry stands for itself times 2^(scale - 127), scales from 1 to 254.  Pages may lie apart (a
     view of a larger tensor), what is in one is contiguous.  page is 16, 32, 64, 128 or 256, dim a multiple of 16 up to 256."""
 
     __slots__ = ("k", "v", "k_scale", "v_scale", "_desc")

@@ -24,12 +24,12 @@
 
 namespace cfp {
 
-constexpr int kFewRows = 32;    // rows of a sequence and key head that the kernel for few takes
+constexpr int kTokenRows = 16, kFewRows = 32;  // rows of a sequence and key head that the kernels for few take
 constexpr int kManyRows = 128;  // rows of a workgroup of the kernel for many, and of the one for heads up to 128
 constexpr int kWideRows = 256, kWideDim = 128;
 constexpr int kFewParts = 1536;
-constexpr int kFewStep = 32, kManyStep = 64;     // tokens of a tile
-constexpr int kFewLeast = 128, kManyLeast = 256;  // tokens of a part, at least
+constexpr int kFewStep = 64, kManyStep = 64;     // parts start and end on these
+constexpr int kFewLeast = 256, kManyLeast = 256;  // tokens of a part, at least
 
 struct AttendArgs {
   SeqArgs s;
@@ -43,7 +43,7 @@ struct AttendArgs {
   int32_t heads, group, dim, max_new;
   int32_t causal, window, wide;  // wide: queries lie on 16 bytes
   int32_t few_units, few_target;  // parts of all sequences with few rows: at most, and for their tokens alone
-  int32_t few_rows, joined;       // joined: there may be parts
+  int32_t few_rows, joined;       // few_rows: of a sequence and key head, at most; joined: there may be parts
   int32_t many_parts, many_rows;  // many_rows: of a workgroup
   uint32_t tiles;                 // of many_rows rows, at most
   float scale;     // times log2(e)
@@ -141,7 +141,7 @@ __device__ __forceinline__ Few few_of(const AttendArgs &A, int b) {
   const int len = q.pos + q.n;
   Few f;
   f.lost = q.n > 0 && (q.n > A.max_new || len > (A.s.width << A.s.page_shift));
-  f.few = q.n > 0 && !f.lost && (int64_t)q.n * A.group <= kFewRows;
+  f.few = q.n > 0 && !f.lost && (int64_t)q.n * A.group <= A.few_rows;
   const int begin = (A.window > 0 ? max(q.pos - A.window + 1, 0) : 0) & ~(kFewStep - 1);
   f.tokens = f.few ? max(len - begin, 0) : 0;
   return f;
@@ -329,6 +329,295 @@ __device__ __forceinline__ void mask16(f32x16 &s, int first, int lo, int hi, boo
   }
 }
 
+// What the rows of a sequence become that is too long for its table, or has more rows than the call was laid out for.
+template <typename T>
+__device__ __forceinline__ void write_lost(const AttendArgs &A, const Seq &sq, int head) {
+  const int g = A.group, hq = A.heads * g, D = A.dim;
+  for (int64_t e = threadIdx.x; e < (int64_t)sq.n * g * D; e += 256) {
+    const int64_t r = e / D;
+    const int64_t row = (sq.row + r / g) * hq + head * g + r % g;
+    reinterpret_cast<T *>(A.out)[row * D + e % D] = (T)__builtin_nanf("");
+    if (e % D == 0 && A.lse) A.lse[row] = __builtin_nanf("");
+  }
+}
+
+// The sums of four waves, laid out in LDS [wave][few_rows][LD] relative to the largest m, to their rows or as a part.
+template <typename T, int ROWS, int LD>
+__device__ __forceinline__ void write_few(const AttendArgs &A, const float *shared, const float (&ml)[2][4][ROWS], const Seq &sq,
+                                          int head, int rows, bool whole, int64_t slot) {
+  const int g = A.group, hq = A.heads * g, D = A.dim, quads = D / 4;
+  for (int e = threadIdx.x; e < rows * quads; e += 256) {
+    const int r = e / quads, d = e % quads * 4;
+    float top = ml[0][0][r];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) top = fmaxf(top, ml[0][w][r]);
+    float l = 0.f;
+    vec<float, 4> o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      l += ml[1][w][r] * (ml[0][w][r] == top ? 1.f : __builtin_amdgcn_exp2f(ml[0][w][r] - top));
+      o += *reinterpret_cast<const vec<float, 4> *>(shared + (w * A.few_rows + r) * LD + d);
+    }
+    if (whole) {
+      const int64_t row = (int64_t)(sq.row + r / g) * hq + head * g + r % g;
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      const float y[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+      store_vec<T, 4>(reinterpret_cast<T *>(A.out) + row * D + d, y);
+      if (d == 0 && A.lse) A.lse[row] = (top + __builtin_amdgcn_logf(l)) * kLn2F;
+    } else {
+      *reinterpret_cast<vec<float, 4> *>(A.few_o + (slot + r) * D + d) = o;
+      if (d == 0) A.few_ml[2 * (slot + r)] = top, A.few_ml[2 * (slot + r) + 1] = l;
+    }
+  }
+}
+
+// ---- up to 16 rows, as a token's heads that share a key head are: like the kernel for up to 32 below, with 16x16x32 products of
+// 16 tokens and 16 rows and 64 tokens a wave at a time.  Row i of product u is token 16 (i / 4) + 4 u + i % 4, so lane l has
+// scores of tokens 16 (l / 16) .. + 15 of row l % 16, which are its share of the two products with the values.  Half the
+// registers of the wider products, so twice the bytes are on their way, and half the exponentials.
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+template <typename T>
+__device__ __forceinline__ f32x4 mfma16(vec<T, 8> a, vec<T, 8> b, f32x4 c) {
+  if constexpr (std::is_same<T, bf16_t>::value)
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+// op over the four lanes of a row
+__device__ __forceinline__ float row_max(float x) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float row_sum(float x) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+template <typename T, bool BYTES, int DP>
+__global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_token_kernel(AttendArgs A) {
+  typedef std::conditional_t<BYTES, uint8_t, T> H;
+  typedef vec<T, 8> Vec8;
+  constexpr int kC = DP / 32, kMt = DP / 16, kLd = DP + 4;
+  constexpr int kK = BYTES ? DP / 64 : DP / 32;  // loads of a key
+  static_assert(!BYTES || DP % 64 == 0, "keys of 8 bits are read 64 entries at a time");
+  extern __shared__ __align__(16) float shared[];
+  __shared__ float ml[2][4][kTokenRows];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 15, h = lane >> 4;
+  const uint32_t id = block_id(), unit = id / A.heads;
+  const int head = (int)(id % A.heads);
+  const int per = few_per(A);
+  int b;
+  uint32_t part;
+  if (unit >= (uint32_t)A.few_units || !find_unit(A.s.n_seqs, unit, [&](int i) { return few_parts(A, i, per); }, b, part)) return;
+  b = __builtin_amdgcn_readfirstlane(b);
+  const Seq sq = uniform_seq_of(A.s, b);
+  const Few few = few_of(A, b);
+  const int g = A.group, hq = A.heads * g, D = A.dim;
+  if (few.lost) return write_lost<T>(A, sq, head);
+  const int rows = sq.n * g, len = sq.pos + sq.n;
+  const bool whole = few.tokens <= per;
+  const int begin = len - few.tokens + (int)part * per, end = min(len, begin + per);
+  const int i = col / g, p = sq.pos + i;
+  const bool mine = col < rows;
+  const int hi = mine ? (A.causal ? p : len - 1) : -1, lo = A.window > 0 ? p - A.window + 1 : 0;
+  const int all_hi = A.causal ? sq.pos : len - 1, all_lo = A.window > 0 ? len - A.window : 0;  // seen by all rows
+
+  Vec8 q[kC];
+  const T *qp = reinterpret_cast<const T *>(A.q) + (int64_t)(sq.row + i) * A.qt + (int64_t)(head * g + col % g) * A.qh;
+#pragma unroll
+  for (int c = 0; c < kC; ++c)
+    q[c] = load_q<T>(qp, BYTES ? 64 * (c / 2) + 16 * h + 8 * (c % 2) : 32 * c + 8 * h, D, mine, A.wide != 0);
+
+  const int page = 1 << A.s.page_shift, inner = page - 1;
+  const TableRow table = table_row(A.s, b);
+  auto pages = [&](int t) { return Pages4{table.entry(t), table.entry(t + 16), table.entry(t + 32), table.entry(t + 48)}; };
+  auto inside = [&](uint32_t e) { return e < A.s.n_pages; };
+  auto pick = [&](const Pages4 &pg, int j) -> int64_t {
+    const uint32_t e = one_of(pg, j);
+    return inside(e) ? e : 0u;
+  };
+  const int kq = col >> 2;  // the 16 tokens that this lane's keys are of: 16 kq + 4 u + col % 4
+  const H *kbase = reinterpret_cast<const H *>(A.k) + (int64_t)(head * page + (col & 3)) * D + (BYTES ? 16 : 8) * h;
+  const H *vbase = reinterpret_cast<const H *>(A.v) + (int64_t)(head * D + col) * page;
+  u32x4 kr[4][kK], vr[kMt][BYTES ? 1 : 2], ksr, vsr;
+  auto load_k = [&](int t, const Pages4 &pg) {
+    const int64_t at = pick(pg, kq);
+    const int place = (t + 16 * kq) & inner;
+    const H *kp = kbase + at * A.kp + place * D;
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int c = 0; c < kK; ++c) {
+        const int d = BYTES ? 64 * c : 32 * c;
+        u32x4 w = {0, 0, 0, 0};
+        if (d + (BYTES ? 16 : 8) * h < D) w = *reinterpret_cast<const u32x4 *>(kp + 4 * u * D + d);
+        kr[u][c] = w;
+      }
+    if constexpr (BYTES) ksr = *reinterpret_cast<const u32x4 *>(A.ks + at * A.ksp + head * page + place);
+  };
+  auto load_v = [&](int t, const Pages4 &pg) {
+    const int64_t at = pick(pg, h);
+    const int place = (t + 16 * h) & inner;
+    const H *vp = vbase + at * A.vp + place;
+#pragma unroll
+    for (int mt = 0; mt < kMt; ++mt)
+#pragma unroll
+      for (int j = 0; j < (BYTES ? 1 : 2); ++j) {
+        u32x4 w = {0, 0, 0, 0};
+        if (16 * mt < D) w = *reinterpret_cast<const u32x4 *>(vp + 16 * mt * page + 8 * j);
+        vr[mt][j] = w;
+      }
+    if constexpr (BYTES) vsr = *reinterpret_cast<const u32x4 *>(A.vs + at * A.vsp + head * page + place);
+  };
+
+  float m = -__builtin_inff(), l = 0.f;
+  f32x4 o[kMt];
+  uint64_t odd[(DP + 127) / 128];  // as in Rows, two bits for each of the 4 kMt entries
+#pragma unroll
+  for (int x = 0; x < (DP + 127) / 128; ++x) odd[x] = 0;
+#pragma unroll
+  for (int mt = 0; mt < kMt; ++mt) o[mt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  uint32_t *odds = reinterpret_cast<uint32_t *>(shared) + wave * 4 * DP;  // [16 tokens][entry]: bits of either sign
+  int t = begin + 64 * wave;
+  if (t < end) {
+    Pages4 now = pages(t), next = now;
+    load_k(t, now);
+    load_v(t, now);
+    if (t + 256 < end) next = pages(t + 256);
+    for (; t < end; t += 256) {
+      Pages4 later = next;
+      if (t + 512 < end) later = pages(t + 512);
+      f32x4 s[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        s[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if constexpr (BYTES) {
+          const float by = scale_of(ksr[u] >> (8 * (col & 3)) & 0xff);
+#pragma unroll
+          for (int c = 0; c < kK; ++c) {
+            s[u] = mfma16<T>(widen<T>(u32x2{kr[u][c][0], kr[u][c][1]}, by), q[2 * c], s[u]);
+            s[u] = mfma16<T>(widen<T>(u32x2{kr[u][c][2], kr[u][c][3]}, by), q[2 * c + 1], s[u]);
+          }
+        } else {
+#pragma unroll
+          for (int c = 0; c < kK; ++c) s[u] = mfma16<T>(__builtin_bit_cast(Vec8, kr[u][c]), q[c], s[u]);
+        }
+      }
+      if (t + 256 < end) load_k(t + 256, next);
+      const int first = t + 16 * h;
+      const bool edge = t + 63 > all_hi || t < all_lo || !(inside(now.a) && inside(now.b) && inside(now.c) && inside(now.d));
+      if (edge) {
+        const bool bad = !inside(one_of(now, h));
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const float x = bad ? __builtin_nanf("") : s[e / 4][e % 4];
+          s[e / 4][e % 4] = first + e >= lo && first + e <= hi ? x : -__builtin_inff();
+        }
+      }
+      float top = s[0][0];
+#pragma unroll
+      for (int e = 1; e < 16; ++e) top = fmaxf(top, s[e / 4][e % 4]);
+      top = row_max(top) * A.scale;
+      if (__any(top > m + kGrowth<T>)) {
+        const float to = top > m + kGrowth<T> ? top - kBelow<T> : m;
+        const float by = to == m ? 1.f : __builtin_amdgcn_exp2f(m - to);
+        m = to;
+        l *= by;
+#pragma unroll
+        for (int mt = 0; mt < kMt; ++mt)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) o[mt][r] *= by;
+      }
+      const float from = m == -__builtin_inff() ? 0.f : m;
+      Vec8 w[2];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        float x = __builtin_amdgcn_exp2f(fmaf(s[e / 4][e % 4], A.scale, -from));
+        l += x;
+        if constexpr (kWeightsScaled<T, BYTES>) x *= scale_of(vsr[e / 4] >> (8 * (e % 4)) & 0xff);
+        w[e / 8][e % 8] = (T)x;
+      }
+      if (edge) {
+        bool any = false;
+#pragma unroll
+        for (int mt = 0; mt < kMt; ++mt) {
+          uint32_t up, down;
+          if constexpr (BYTES) {
+            take_odd<T, H>(vr[mt][0], up, down);
+          } else {
+            uint32_t up1, down1;
+            take_odd<T, H>(vr[mt][0], up, down);
+            take_odd<T, H>(vr[mt][1], up1, down1);
+            up |= up1 << 8, down |= down1 << 8;
+          }
+          odds[h * DP + 16 * mt + col] = up | down << 16;
+          any = any || up != 0 || down != 0;
+        }
+        if (__any(any)) {
+          __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+          __builtin_amdgcn_wave_barrier();
+          __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const uint32_t sees = bits_of(hi + 1 - t - 16 * x) & ~bits_of(lo - t - 16 * x);
+#pragma unroll
+            for (int e = 0; e < 4 * kMt; ++e) {
+              const uint32_t a = odds[x * DP + 16 * (e / 4) + 4 * h + e % 4];
+              odd[e / 32] |= (uint64_t)((a & sees & 0xffff ? 1u : 0u) | (a >> 16 & sees ? 2u : 0u)) << (2 * (e % 32));
+              __builtin_amdgcn_sched_barrier(0);  // one after the other: seldom run, and not worth registers
+            }
+          }
+        }
+      }
+#pragma unroll
+      for (int mt = 0; mt < kMt; ++mt)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          Vec8 v;
+          if constexpr (kWeightsScaled<T, BYTES>)
+            v = widen<T>(u32x2{vr[mt][0][2 * j], vr[mt][0][2 * j + 1]}, 1.f);
+          else if constexpr (BYTES)
+            v = widen<T>(u32x2{vr[mt][0][2 * j], vr[mt][0][2 * j + 1]}, u32x2{vsr[2 * j], vsr[2 * j + 1]});
+          else
+            v = __builtin_bit_cast(Vec8, vr[mt][j]);
+          o[mt] = mfma16<T>(v, w[j], o[mt]);
+        }
+      if (t + 256 < end) load_v(t + 256, next);
+      now = next, next = later;
+    }
+  }
+
+  // the waves' states together
+  l = row_sum(l);
+#pragma unroll
+  for (int x = 0; x < (DP + 127) / 128; ++x)
+    if (__any(odd[x] != 0)) {
+#pragma unroll
+      for (int e = 0; e < 32 && 32 * x + e < 4 * kMt; ++e) {
+        const int mt = (32 * x + e) / 4;
+        o[mt][e % 4] += odd[x] >> (2 * e) & 1 ? __builtin_inff() : 0.f;
+        o[mt][e % 4] -= odd[x] >> (2 * e) & 2 ? __builtin_inff() : 0.f;
+      }
+    }
+  if (h == 0) ml[0][wave][col] = m, ml[1][wave][col] = l;
+  __syncthreads();
+  float top = ml[0][0][col];
+#pragma unroll
+  for (int w = 1; w < 4; ++w) top = fmaxf(top, ml[0][w][col]);
+  const float by = m == top ? 1.f : __builtin_amdgcn_exp2f(m - top);
+  if (mine) {
+    float *to = shared + (wave * A.few_rows + col) * kLd + 4 * h;
+#pragma unroll
+    for (int mt = 0; mt < kMt; ++mt) *reinterpret_cast<f32x4 *>(to + 16 * mt) = o[mt] * by;
+  }
+  __syncthreads();
+  write_few<T, kTokenRows, kLd>(A, shared, ml, sq, head, rows, whole, (int64_t)id * A.few_rows);
+}
+
 // ---- few rows: a workgroup takes a part of one sequence's tokens for one key head and up to 32 rows.  Each of its
 // four waves takes every fourth tile of 32 tokens, operands from memory straight to the matrix instructions'
 // registers (16 bytes a lane, the next tile's keys loaded while this one's scores become weights, its values
@@ -351,16 +640,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_few_kernel(Atte
   const Seq sq = uniform_seq_of(A.s, b);
   const Few few = few_of(A, b);
   const int g = A.group, hq = A.heads * g, D = A.dim;
-  T *out = reinterpret_cast<T *>(A.out);
-  if (few.lost) {
-    for (int64_t e = threadIdx.x; e < (int64_t)sq.n * g * D; e += 256) {
-      const int64_t r = e / D;
-      const int64_t row = (sq.row + r / g) * hq + head * g + r % g;
-      out[row * D + e % D] = (T)__builtin_nanf("");
-      if (e % D == 0 && A.lse) A.lse[row] = __builtin_nanf("");
-    }
-    return;
-  }
+  if (few.lost) return write_lost<T>(A, sq, head);
   const int rows = sq.n * g, len = sq.pos + sq.n;
   const bool whole = few.tokens <= per;
   const int begin = len - few.tokens + (int)part * per, end = min(len, begin + per);
@@ -521,31 +801,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_few_kernel(Atte
       }
   }
   __syncthreads();
-  const int quads = D / 4;
-  const int64_t slot = (int64_t)id * A.few_rows;
-  for (int e = threadIdx.x; e < rows * quads; e += 256) {
-    const int r = e / quads, d = e % quads * 4;
-    float top = ml[0][0][r];
-#pragma unroll
-    for (int w = 1; w < 4; ++w) top = fmaxf(top, ml[0][w][r]);
-    float l = 0.f;
-    vec<float, 4> o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      l += ml[1][w][r] * (ml[0][w][r] == top ? 1.f : __builtin_amdgcn_exp2f(ml[0][w][r] - top));
-      o += *reinterpret_cast<const vec<float, 4> *>(shared + (w * A.few_rows + r) * kLd + d);
-    }
-    if (whole) {
-      const int64_t row = (int64_t)(sq.row + r / g) * hq + head * g + r % g;
-      const float inv = l == 0.f ? 0.f : 1.f / l;
-      const float y[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
-      store_vec<T, 4>(out + row * D + d, y);
-      if (d == 0 && A.lse) A.lse[row] = (top + __builtin_amdgcn_logf(l)) * kLn2F;
-    } else {
-      *reinterpret_cast<vec<float, 4> *>(A.few_o + (slot + r) * D + d) = o;
-      if (d == 0) A.few_ml[2 * (slot + r)] = top, A.few_ml[2 * (slot + r) + 1] = l;
-    }
-  }
+  write_few<T, kFewRows, kLd>(A, shared, ml, sq, head, rows, whole, (int64_t)id * A.few_rows);
 }
 
 // ---- many rows: a workgroup takes 128 rows of one sequence and key head, 32 a wave, over tiles of 64 tokens whose keys
@@ -577,7 +833,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many_kernel(Att
   if (!find_unit(A.s.n_seqs, A.tiles - 1 - id, [&](int i) {
         const Seq s = seq_of(A.s, i);
         const int64_t r = (int64_t)s.n * g;
-        return r > kFewRows && s.n <= A.max_new ? (uint32_t)((r + kManyRows - 1) / kManyRows) : 0u;
+        return r > A.few_rows && s.n <= A.max_new ? (uint32_t)((r + kManyRows - 1) / kManyRows) : 0u;
       }, b, tile))
     return;
   b = __builtin_amdgcn_readfirstlane(b);
@@ -908,7 +1164,7 @@ __global__ __launch_bounds__(256, 1) void attend_wide_kernel(AttendArgs A) {
   if (!find_unit(A.s.n_seqs, A.tiles - 1 - id, [&](int i) {
         const Seq s = seq_of(A.s, i);
         const int64_t r = (int64_t)s.n * g;
-        return r > kFewRows && s.n <= A.max_new ? (uint32_t)((r + kWideRows - 1) / kWideRows) : 0u;
+        return r > A.few_rows && s.n <= A.max_new ? (uint32_t)((r + kWideRows - 1) / kWideRows) : 0u;
       }, b, tile))
     return;
   b = __builtin_amdgcn_readfirstlane(b);
@@ -1347,7 +1603,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs A) {
   if (token < A.s.starts[0] || !find_unit(A.s.n_seqs, (uint32_t)(token - A.s.starts[0]), [&](int i) { return (uint32_t)seq_of(A.s, i).n; }, b, k)) return;
   const Seq sq = seq_of(A.s, b);
   const int len = sq.pos + sq.n, rows = sq.n * g, e = (int)(id % many) * 256 + threadIdx.x;
-  if (sq.n > A.max_new || len > (A.s.width << A.s.page_shift) || rows <= kFewRows || e >= hq * quads) return;
+  if (sq.n > A.max_new || len > (A.s.width << A.s.page_shift) || rows <= A.few_rows || e >= hq * quads) return;
   const int head = e / quads, i = (int)k, r = i * g + head % g;
   const int r0 = r / A.many_rows * A.many_rows, r1 = min(r0 + A.many_rows, rows);
   const Span sp = span_of<kManyStep, kManyLeast>(A, sq.pos + r0 / g, sq.pos + (r1 - 1) / g, len, A.many_parts);
@@ -1358,10 +1614,12 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs A) {
 
 template <typename T, bool BYTES, int DP>
 hipError_t attend_run(const AttendArgs &A, hipStream_t st) {
-  const size_t few = (size_t)4 * 4 * std::max(A.few_rows * (DP + 4), 2 * DP);
+  constexpr int kFewDim = BYTES && DP == 96 ? 128 : DP;
+  const size_t few = (size_t)4 * 4 * std::max(A.few_rows * (kFewDim + 4), 4 * kFewDim);  // keys of 8 bits are read 64 entries at a time
   const size_t many = DP <= kWideDim ? (size_t)Wide<T, BYTES, DP>::kBytes
                                      : (size_t)2 * (kManyStep * (DP + 8) + DP * (kManyStep + 8)) * 2 + 2 * DP * 16 + 16;
-  auto *few_kernel = attend_few_kernel<T, BYTES, DP>;
+  void (*few_kernel)(AttendArgs) = attend_few_kernel<T, BYTES, DP>;
+  if (A.few_rows <= kTokenRows) few_kernel = attend_token_kernel<T, BYTES, kFewDim>;
   void (*many_kernel)(AttendArgs);
   if constexpr (DP <= kWideDim)
     many_kernel = attend_wide_kernel<T, BYTES, DP>;

@@ -11,14 +11,15 @@ namespace {
 void parts_of(const cfp_attend_desc &a, const cfp_cache_desc &c, const cfp_sequences_desc &s, AttendArgs &A) {
   const int64_t g = a.n_q / c.heads, most_len = (int64_t)s.width * c.page;
   const int64_t new_rows = std::min<int64_t>(s.max_new, a.n_tokens) * g;
-  A.few_rows = (int32_t)std::min<int64_t>(kFewRows, new_rows);
+  // all sequences have few rows, or those that have go with the narrow kernel and the others with the one for many
+  A.few_rows = (int32_t)(new_rows <= kFewRows ? new_rows : g <= kTokenRows ? kTokenRows : kFewRows);
   A.joined = most_len > kFewLeast;
   A.few_target = (int32_t)std::max<int64_t>(kFewParts / c.heads, 1);
   A.few_units = s.n_seqs + (A.joined ? (int32_t)std::min<int64_t>(A.few_target, most_len / kFewLeast * s.n_seqs) : 0);
   A.many_rows = c.dim <= kWideDim ? kWideRows : kManyRows;
   A.tiles = 0, A.many_parts = 1;
-  if (new_rows > kFewRows) {
-    A.tiles = (uint32_t)std::min<int64_t>(a.n_tokens * g / A.many_rows + s.n_seqs, (a.n_tokens * g + kFewRows) / (kFewRows + 1));
+  if (new_rows > A.few_rows) {
+    A.tiles = (uint32_t)std::min<int64_t>(a.n_tokens * g / A.many_rows + s.n_seqs, (a.n_tokens * g + A.few_rows) / (A.few_rows + 1));
     const int64_t groups = (int64_t)A.tiles * c.heads;
     if (groups < 512) A.many_parts = (int32_t)std::clamp<int64_t>(std::min<int64_t>(1024 / groups, most_len / kManyLeast), 1, 16);
   }

@@ -105,8 +105,8 @@ __device__ __forceinline__ uint32_t units_before(int b, F units) {
   return before;
 }
 
-// 2^(scale - 127)
-__device__ __forceinline__ float scale_of(uint32_t s) { return s ? __uint_as_float(s << 23) : 0x1p-127f; }
+// 2^(scale - 127) of a scale from 1 to 254
+__device__ __forceinline__ float scale_of(uint32_t s) { return __uint_as_float(s << 23); }
 
 hipError_t launch_cache_write(const cfp_cache_desc &c, const cfp_sequences_desc &s, int64_t n_tokens, int dtype, const void *k,
                               HeadStrides sk, const void *v, HeadStrides sv, hipStream_t st);
