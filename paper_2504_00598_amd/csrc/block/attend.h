@@ -27,9 +27,9 @@ namespace cfp {
 constexpr int kTokenRows = 16, kFewRows = 32;  // rows of a sequence and key head that the kernels for few take
 constexpr int kManyRows = 128;  // rows of a workgroup of the kernel for many, and of the one for heads up to 128
 constexpr int kWideRows = 256, kWideDim = 128;
-constexpr int kFewParts = 1536;
+constexpr int kFewParts = 768;
 constexpr int kFewStep = 64, kManyStep = 64;     // parts start and end on these
-constexpr int kFewLeast = 256, kManyLeast = 256;  // tokens of a part, at least
+constexpr int kFewLeast = 256, kTokenLeast = 512, kManyLeast = 256;  // tokens of a part, at least
 
 struct AttendArgs {
   SeqArgs s;
@@ -43,6 +43,7 @@ struct AttendArgs {
   int32_t heads, group, dim, max_new;
   int32_t causal, window, wide;  // wide: queries lie on 16 bytes
   int32_t few_units, few_target;  // parts of all sequences with few rows: at most, and for their tokens alone
+  int32_t few_least;              // tokens of a part, at least
   int32_t few_rows, joined;       // few_rows: of a sequence and key head, at most; joined: there may be parts
   int32_t many_parts, many_rows;  // many_rows: of a workgroup
   uint32_t tiles;                 // of many_rows rows, at most
@@ -136,8 +137,7 @@ struct Few {
   bool few;
   int32_t tokens;  // that some row sees, from a multiple of kFewStep on
 };
-__device__ __forceinline__ Few few_of(const AttendArgs &A, int b) {
-  const Seq q = seq_of(A.s, b);
+__device__ __forceinline__ Few few_of(const AttendArgs &A, const Seq &q) {
   const int len = q.pos + q.n;
   Few f;
   f.lost = q.n > 0 && (q.n > A.max_new || len > (A.s.width << A.s.page_shift));
@@ -146,9 +146,13 @@ __device__ __forceinline__ Few few_of(const AttendArgs &A, int b) {
   f.tokens = f.few ? max(len - begin, 0) : 0;
   return f;
 }
-__device__ __forceinline__ uint32_t few_parts(const AttendArgs &A, int b, int per) {
-  const Few f = few_of(A, b);
+__device__ __forceinline__ uint32_t few_parts(const AttendArgs &A, const Seq &q, int per) {
+  const Few f = few_of(A, q);
   return f.lost ? 1u : f.few ? max((uint32_t)((f.tokens + per - 1) / per), 1u) : 0u;
+}
+__device__ __forceinline__ int few_share(const AttendArgs &A, float tokens) {
+  const int per = (int)ceilf(tokens * 1.001f / (float)A.few_target);
+  return __builtin_amdgcn_readfirstlane(max((per + kFewStep - 1) & ~(kFewStep - 1), A.few_least));
 }
 // All 64 lanes of a wave call it.  The sum is in 32-bit floats: the share is taken a little larger than it says, so that there
 // are never more than few_target parts beside each sequence's last.
@@ -156,10 +160,27 @@ __device__ __forceinline__ int few_per(const AttendArgs &A) {
   float sum = 0.f;
   for (int first = 0; first < A.s.n_seqs; first += 64) {
     const int b = first + (threadIdx.x & 63);
-    sum += group_sum<64>(b < A.s.n_seqs ? (float)few_of(A, b).tokens : 0.f);
+    sum += group_sum<64>(b < A.s.n_seqs ? (float)few_of(A, seq_of(A.s, b)).tokens : 0.f);
   }
-  const int per = (int)ceilf(sum * 1.001f / (float)A.few_target);
-  return __builtin_amdgcn_readfirstlane(max((per + kFewStep - 1) & ~(kFewStep - 1), kFewLeast));
+  return few_share(A, sum);
+}
+// Sequence, part and tokens of a part of a workgroup `unit`; false: there is none.  Up to 64 sequences are looked at once.
+__device__ __forceinline__ bool find_few(const AttendArgs &A, uint32_t unit, int &b, uint32_t &part, Seq &q, int &per) {
+  if (A.s.n_seqs > 64) {
+    per = few_per(A);
+    return find_unit(A.s, unit, [&](const Seq &s) { return few_parts(A, s, per); }, b, part, q);
+  }
+  const int lane = threadIdx.x & 63;
+  Seq s = {0, 0, 0};
+  if (lane < A.s.n_seqs) s = seq_of(A.s, lane);
+  per = few_share(A, group_sum<64>((float)few_of(A, s).tokens));
+  const uint32_t own = few_parts(A, s, per), sum = lanes_before(own);
+  const uint64_t past = __ballot(sum > unit);
+  if (past == 0) return false;
+  b = __builtin_ctzll(past);
+  q = seq_of_lane(s, b);
+  part = unit - (uint32_t)__builtin_amdgcn_readlane((int)(sum - own), b);
+  return true;
 }
 
 // Query of a row as the second operand: entries of its d-th piece of 8.
@@ -330,10 +351,10 @@ __device__ __forceinline__ void mask16(f32x16 &s, int first, int lo, int hi, boo
 }
 
 // What the rows of a sequence become that is too long for its table, or has more rows than the call was laid out for.
-template <typename T>
+template <typename T, int THREADS>
 __device__ __forceinline__ void write_lost(const AttendArgs &A, const Seq &sq, int head) {
   const int g = A.group, hq = A.heads * g, D = A.dim;
-  for (int64_t e = threadIdx.x; e < (int64_t)sq.n * g * D; e += 256) {
+  for (int64_t e = threadIdx.x; e < (int64_t)sq.n * g * D; e += THREADS) {
     const int64_t r = e / D;
     const int64_t row = (sq.row + r / g) * hq + head * g + r % g;
     reinterpret_cast<T *>(A.out)[row * D + e % D] = (T)__builtin_nanf("");
@@ -341,20 +362,20 @@ __device__ __forceinline__ void write_lost(const AttendArgs &A, const Seq &sq, i
   }
 }
 
-// The sums of four waves, laid out in LDS [wave][few_rows][LD] relative to the largest m, to their rows or as a part.
-template <typename T, int ROWS, int LD>
-__device__ __forceinline__ void write_few(const AttendArgs &A, const float *shared, const float (&ml)[2][4][ROWS], const Seq &sq,
+// The sums of the waves, laid out in LDS [wave][few_rows][LD] relative to the largest m, to their rows or as a part.
+template <typename T, int WAVES, int ROWS, int LD>
+__device__ __forceinline__ void write_few(const AttendArgs &A, const float *shared, const float (&ml)[2][WAVES][ROWS], const Seq &sq,
                                           int head, int rows, bool whole, int64_t slot) {
   const int g = A.group, hq = A.heads * g, D = A.dim, quads = D / 4;
-  for (int e = threadIdx.x; e < rows * quads; e += 256) {
+  for (int e = threadIdx.x; e < rows * quads; e += 64 * WAVES) {
     const int r = e / quads, d = e % quads * 4;
     float top = ml[0][0][r];
 #pragma unroll
-    for (int w = 1; w < 4; ++w) top = fmaxf(top, ml[0][w][r]);
+    for (int w = 1; w < WAVES; ++w) top = fmaxf(top, ml[0][w][r]);
     float l = 0.f;
     vec<float, 4> o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < WAVES; ++w) {
       l += ml[1][w][r] * (ml[0][w][r] == top ? 1.f : __builtin_amdgcn_exp2f(ml[0][w][r] - top));
       o += *reinterpret_cast<const vec<float, 4> *>(shared + (w * A.few_rows + r) * LD + d);
     }
@@ -383,6 +404,7 @@ __device__ __forceinline__ f32x4 mfma16(vec<T, 8> a, vec<T, 8> b, f32x4 c) {
   else
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
+constexpr int kTokenWaves = 4;  // of a workgroup
 // op over the four lanes of a row
 __device__ __forceinline__ float row_max(float x) {
   const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -398,26 +420,24 @@ __device__ __forceinline__ float row_sum(float x) {
 }
 
 template <typename T, bool BYTES, int DP>
-__global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_token_kernel(AttendArgs A) {
+__global__ __launch_bounds__(64 * kTokenWaves, DP <= 128 ? 2 : 1) void attend_token_kernel(AttendArgs A) {
   typedef std::conditional_t<BYTES, uint8_t, T> H;
   typedef vec<T, 8> Vec8;
-  constexpr int kC = DP / 32, kMt = DP / 16, kLd = DP + 4;
+  constexpr int kC = DP / 32, kMt = DP / 16, kLd = DP + 4, kWaves = kTokenWaves, kStep = 64 * kWaves;
   constexpr int kK = BYTES ? DP / 64 : DP / 32;  // loads of a key
   static_assert(!BYTES || DP % 64 == 0, "keys of 8 bits are read 64 entries at a time");
   extern __shared__ __align__(16) float shared[];
-  __shared__ float ml[2][4][kTokenRows];
+  __shared__ float ml[2][kWaves][kTokenRows];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 15, h = lane >> 4;
   const uint32_t id = block_id(), unit = id / A.heads;
   const int head = (int)(id % A.heads);
-  const int per = few_per(A);
-  int b;
+  int b, per;
   uint32_t part;
-  if (unit >= (uint32_t)A.few_units || !find_unit(A.s.n_seqs, unit, [&](int i) { return few_parts(A, i, per); }, b, part)) return;
-  b = __builtin_amdgcn_readfirstlane(b);
-  const Seq sq = uniform_seq_of(A.s, b);
-  const Few few = few_of(A, b);
+  Seq sq;
+  if (unit >= (uint32_t)A.few_units || !find_few(A, unit, b, part, sq, per)) return;
+  const Few few = few_of(A, sq);
   const int g = A.group, hq = A.heads * g, D = A.dim;
-  if (few.lost) return write_lost<T>(A, sq, head);
+  if (few.lost) return write_lost<T, kStep>(A, sq, head);
   const int rows = sq.n * g, len = sq.pos + sq.n;
   const bool whole = few.tokens <= per;
   const int begin = len - few.tokens + (int)part * per, end = min(len, begin + per);
@@ -487,10 +507,10 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_token_kernel(At
     Pages4 now = pages(t), next = now;
     load_k(t, now);
     load_v(t, now);
-    if (t + 256 < end) next = pages(t + 256);
-    for (; t < end; t += 256) {
+    if (t + kStep < end) next = pages(t + kStep);
+    for (; t < end; t += kStep) {
       Pages4 later = next;
-      if (t + 512 < end) later = pages(t + 512);
+      if (t + 2 * kStep < end) later = pages(t + 2 * kStep);
       f32x4 s[4];
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
@@ -507,7 +527,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_token_kernel(At
           for (int c = 0; c < kK; ++c) s[u] = mfma16<T>(__builtin_bit_cast(Vec8, kr[u][c]), q[c], s[u]);
         }
       }
-      if (t + 256 < end) load_k(t + 256, next);
+      if (t + kStep < end) load_k(t + kStep, next);
       const int first = t + 16 * h;
       const bool edge = t + 63 > all_hi || t < all_lo || !(inside(now.a) && inside(now.b) && inside(now.c) && inside(now.d));
       if (edge) {
@@ -586,7 +606,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_token_kernel(At
             v = __builtin_bit_cast(Vec8, vr[mt][j]);
           o[mt] = mfma16<T>(v, w[j], o[mt]);
         }
-      if (t + 256 < end) load_v(t + 256, next);
+      if (t + kStep < end) load_v(t + kStep, next);
       now = next, next = later;
     }
   }
@@ -607,7 +627,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_token_kernel(At
   __syncthreads();
   float top = ml[0][0][col];
 #pragma unroll
-  for (int w = 1; w < 4; ++w) top = fmaxf(top, ml[0][w][col]);
+  for (int w = 1; w < kWaves; ++w) top = fmaxf(top, ml[0][w][col]);
   const float by = m == top ? 1.f : __builtin_amdgcn_exp2f(m - top);
   if (mine) {
     float *to = shared + (wave * A.few_rows + col) * kLd + 4 * h;
@@ -615,7 +635,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_token_kernel(At
     for (int mt = 0; mt < kMt; ++mt) *reinterpret_cast<f32x4 *>(to + 16 * mt) = o[mt] * by;
   }
   __syncthreads();
-  write_few<T, kTokenRows, kLd>(A, shared, ml, sq, head, rows, whole, (int64_t)id * A.few_rows);
+  write_few<T, kWaves, kTokenRows, kLd>(A, shared, ml, sq, head, rows, whole, (int64_t)id * A.few_rows);
 }
 
 // ---- few rows: a workgroup takes a part of one sequence's tokens for one key head and up to 32 rows.  Each of its
@@ -632,15 +652,13 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_few_kernel(Atte
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 31, h = lane >> 5;
   const uint32_t id = block_id(), unit = id / A.heads;
   const int head = (int)(id % A.heads);
-  const int per = few_per(A);
-  int b;
+  int b, per;
   uint32_t part;
-  if (unit >= (uint32_t)A.few_units || !find_unit(A.s.n_seqs, unit, [&](int i) { return few_parts(A, i, per); }, b, part)) return;
-  b = __builtin_amdgcn_readfirstlane(b);
-  const Seq sq = uniform_seq_of(A.s, b);
-  const Few few = few_of(A, b);
+  Seq sq;
+  if (unit >= (uint32_t)A.few_units || !find_few(A, unit, b, part, sq, per)) return;
+  const Few few = few_of(A, sq);
   const int g = A.group, hq = A.heads * g, D = A.dim;
-  if (few.lost) return write_lost<T>(A, sq, head);
+  if (few.lost) return write_lost<T, 256>(A, sq, head);
   const int rows = sq.n * g, len = sq.pos + sq.n;
   const bool whole = few.tokens <= per;
   const int begin = len - few.tokens + (int)part * per, end = min(len, begin + per);
@@ -801,7 +819,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_few_kernel(Atte
       }
   }
   __syncthreads();
-  write_few<T, kFewRows, kLd>(A, shared, ml, sq, head, rows, whole, (int64_t)id * A.few_rows);
+  write_few<T, 4, kFewRows, kLd>(A, shared, ml, sq, head, rows, whole, (int64_t)id * A.few_rows);
 }
 
 // ---- many rows: a workgroup takes 128 rows of one sequence and key head, 32 a wave, over tiles of 64 tokens whose keys
@@ -829,15 +847,13 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many_kernel(Att
   if (id >= A.tiles) return;
   int b;
   uint32_t tile;
+  Seq sq;
   const int g = A.group, hq = A.heads * g, D = A.dim;
-  if (!find_unit(A.s.n_seqs, A.tiles - 1 - id, [&](int i) {
-        const Seq s = seq_of(A.s, i);
+  if (!find_unit(A.s, A.tiles - 1 - id, [&](const Seq &s) {
         const int64_t r = (int64_t)s.n * g;
         return r > A.few_rows && s.n <= A.max_new ? (uint32_t)((r + kManyRows - 1) / kManyRows) : 0u;
-      }, b, tile))
+      }, b, tile, sq))
     return;
-  b = __builtin_amdgcn_readfirstlane(b);
-  const Seq sq = uniform_seq_of(A.s, b);
   const int len = sq.pos + sq.n, rows = sq.n * g;
   if (len > (A.s.width << A.s.page_shift)) return;  // the kernel for few writes what such rows become
   const int r0 = (int)tile * kManyRows, r1 = min(r0 + kManyRows, rows);
@@ -1160,16 +1176,13 @@ __global__ __launch_bounds__(256, 1) void attend_wide_kernel(AttendArgs A) {
   if (id >= A.tiles) return;
   int b;
   uint32_t tile;
+  Seq sq;
   const int g = A.group, hq = A.heads * g, D = A.dim;
-  if (!find_unit(A.s.n_seqs, A.tiles - 1 - id, [&](int i) {
-        const Seq s = seq_of(A.s, i);
+  if (!find_unit(A.s, A.tiles - 1 - id, [&](const Seq &s) {
         const int64_t r = (int64_t)s.n * g;
         return r > A.few_rows && s.n <= A.max_new ? (uint32_t)((r + kWideRows - 1) / kWideRows) : 0u;
-      }, b, tile))
+      }, b, tile, sq))
     return;
-  b = __builtin_amdgcn_readfirstlane(b);
-  tile = __builtin_amdgcn_readfirstlane(tile);
-  const Seq sq = uniform_seq_of(A.s, b);
   const int len = sq.pos + sq.n, rows = sq.n * g;
   if (len > (A.s.width << A.s.page_shift)) return;  // the kernel for few writes what such rows become
   const int r0 = (int)tile * kWideRows, r1 = min(r0 + kWideRows, rows);
@@ -1545,21 +1558,39 @@ __global__ __launch_bounds__(256, 1) void attend_wide_kernel(AttendArgs A) {
   }
 }
 
-// ---- the parts of a row together, in their order: a thread takes four entries of one row.  The first workgroups take the
-// sequences with few rows, the others the tokens of the others.
+// ---- the parts of a row together: a workgroup takes 32 times four entries of rows, and of each eight threads every eighth
+// part; their sums meet in LDS, in order.  The first workgroups take the sequences with few rows, the others the tokens
+// of the others.
+constexpr int kJoinQuads = 32, kJoinThreads = 8 * kJoinQuads;
+
+// All threads of a workgroup call it; `there`: this thread's entries are some row's.
 template <typename T>
 __device__ __forceinline__ void join_row(const AttendArgs &A, const float *po, const float *pm, int64_t at, int64_t step, int parts,
-                                         int64_t row, int d) {
-  float top = -__builtin_inff();
-  for (int s = 0; s < parts; ++s) top = fmaxf(top, pm[2 * (at + s * step)]);
-  float l = 0.f;
+                                         int64_t row, int d, bool there) {
+  __shared__ vec<float, 4> sums[8][kJoinQuads];
+  __shared__ float ml[2][8][kJoinQuads];
+  const int k = threadIdx.x / kJoinQuads, e = threadIdx.x % kJoinQuads;
+  float top = -__builtin_inff(), l = 0.f;
   vec<float, 4> o = {0.f, 0.f, 0.f, 0.f};
+  if (there) {
+    for (int s = k; s < parts; s += 8) top = fmaxf(top, pm[2 * (at + s * step)]);
 #pragma unroll 4
-  for (int s = 0; s < parts; ++s) {
-    const int64_t a = at + s * step;
-    const float m = pm[2 * a], by = m == top ? 1.f : __builtin_amdgcn_exp2f(m - top);
-    l += pm[2 * a + 1] * by;
-    o += *reinterpret_cast<const vec<float, 4> *>(po + a * A.dim + d) * by;
+    for (int s = k; s < parts; s += 8) {
+      const int64_t a = at + s * step;
+      const float m = pm[2 * a], by = m == top ? 1.f : __builtin_amdgcn_exp2f(m - top);
+      l += pm[2 * a + 1] * by;
+      o += *reinterpret_cast<const vec<float, 4> *>(po + a * A.dim + d) * by;
+    }
+  }
+  sums[k][e] = o, ml[0][k][e] = top, ml[1][k][e] = l;
+  __syncthreads();
+  if (k != 0 || !there) return;
+  for (int w = 1; w < 8; ++w) top = fmaxf(top, ml[0][w][e]);
+  l = 0.f, o = vec<float, 4>{0.f, 0.f, 0.f, 0.f};
+  for (int w = 0; w < 8; ++w) {
+    const float m = ml[0][w][e], by = m == top ? 1.f : __builtin_amdgcn_exp2f(m - top);
+    l += ml[1][w][e] * by;
+    o += sums[w][e] * by;
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
   const float y[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
@@ -1569,30 +1600,30 @@ __device__ __forceinline__ void join_row(const AttendArgs &A, const float *po, c
 
 // Workgroups of a sequence with few rows, and of a token.
 inline __host__ __device__ uint32_t few_joins(const AttendArgs &A) {
-  return (uint32_t)(((int64_t)A.heads * A.few_rows * (A.dim / 4) + 255) / 256);
+  return (uint32_t)(((int64_t)A.heads * A.few_rows * (A.dim / 4) + kJoinQuads - 1) / kJoinQuads);
 }
 inline __host__ __device__ uint32_t many_joins(const AttendArgs &A) {
-  return (uint32_t)(((int64_t)A.heads * A.group * (A.dim / 4) + 255) / 256);
+  return (uint32_t)(((int64_t)A.heads * A.group * (A.dim / 4) + kJoinQuads - 1) / kJoinQuads);
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs A) {
+__global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendArgs A) {
   const int g = A.group, hq = A.heads * g, quads = A.dim / 4;
   uint32_t id = block_id();
   const uint32_t few = few_joins(A), few_all = A.joined ? few * A.s.n_seqs : 0u;
   int b;
   if (id < few_all) {
     b = (int)(id / few);
-    const Few f = few_of(A, b);
-    if (!f.few || f.tokens <= kFewLeast) return;
+    const Seq sq = seq_of(A.s, b);
+    const Few f = few_of(A, sq);
+    if (!f.few || f.tokens <= A.few_least) return;
     const int per = few_per(A), parts = (f.tokens + per - 1) / per;
     if (parts <= 1) return;
-    const uint32_t unit = units_before(b, [&](int i) { return few_parts(A, i, per); });
-    const Seq sq = seq_of(A.s, b);
-    const int rows = sq.n * g, e = (int)(id % few) * 256 + threadIdx.x, r = e / quads % rows, head = e / quads / rows;
-    if (head >= A.heads) return;
+    const uint32_t unit = units_before(A.s, b, [&](const Seq &s) { return few_parts(A, s, per); });
+    const int rows = sq.n * g, e = (int)(id % few) * kJoinQuads + threadIdx.x % kJoinQuads;
+    const int r = e / quads % rows, head = e / quads / rows;
     join_row<T>(A, A.few_o, A.few_ml, ((int64_t)unit * A.heads + head) * A.few_rows + r, (int64_t)A.heads * A.few_rows, parts,
-                (int64_t)(sq.row + r / g) * hq + head * g + r % g, e % quads * 4);
+                (int64_t)(sq.row + r / g) * hq + head * g + r % g, e % quads * 4, head < A.heads);
     return;
   }
   id -= few_all;
@@ -1600,26 +1631,27 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs A) {
   const int64_t token = id / many;
   if (A.many_parts == 1 || token >= A.s.n_tokens) return;
   uint32_t k;
-  if (token < A.s.starts[0] || !find_unit(A.s.n_seqs, (uint32_t)(token - A.s.starts[0]), [&](int i) { return (uint32_t)seq_of(A.s, i).n; }, b, k)) return;
-  const Seq sq = seq_of(A.s, b);
-  const int len = sq.pos + sq.n, rows = sq.n * g, e = (int)(id % many) * 256 + threadIdx.x;
-  if (sq.n > A.max_new || len > (A.s.width << A.s.page_shift) || rows <= A.few_rows || e >= hq * quads) return;
-  const int head = e / quads, i = (int)k, r = i * g + head % g;
+  Seq sq;
+  if (token < A.s.starts[0] || !find_unit(A.s, (uint32_t)(token - A.s.starts[0]), [](const Seq &s) { return (uint32_t)s.n; }, b, k, sq)) return;
+  const int len = sq.pos + sq.n, rows = sq.n * g, e = (int)(id % many) * kJoinQuads + threadIdx.x % kJoinQuads;
+  if (sq.n > A.max_new || len > (A.s.width << A.s.page_shift) || rows <= A.few_rows) return;
+  const int head = min(e / quads, hq - 1), i = (int)k, r = i * g + head % g;
   const int r0 = r / A.many_rows * A.many_rows, r1 = min(r0 + A.many_rows, rows);
   const Span sp = span_of<kManyStep, kManyLeast>(A, sq.pos + r0 / g, sq.pos + (r1 - 1) / g, len, A.many_parts);
-  if (sp.parts <= 1) return;
   const int64_t row = (int64_t)(sq.row + i) * hq + head;
-  join_row<T>(A, A.many_o, A.many_ml, row, A.s.n_tokens * hq, sp.parts, row, e % quads * 4);
+  join_row<T>(A, A.many_o, A.many_ml, row, A.s.n_tokens * hq, sp.parts, row, e % quads * 4, sp.parts > 1 && e < hq * quads);
 }
 
 template <typename T, bool BYTES, int DP>
 hipError_t attend_run(const AttendArgs &A, hipStream_t st) {
-  constexpr int kFewDim = BYTES && DP == 96 ? 128 : DP;
-  const size_t few = (size_t)4 * 4 * std::max(A.few_rows * (kFewDim + 4), 4 * kFewDim);  // keys of 8 bits are read 64 entries at a time
+  constexpr int kTokenDim = BYTES && DP == 96 ? 128 : DP;  // keys of 8 bits are read 64 entries at a time
+  const bool token = A.few_rows <= kTokenRows;
+  const int waves = token ? kTokenWaves : 4;
+  const size_t few = (size_t)waves * 4 * (token ? std::max(A.few_rows * (kTokenDim + 4), 4 * kTokenDim) : std::max(A.few_rows * (DP + 4), 2 * DP));
   const size_t many = DP <= kWideDim ? (size_t)Wide<T, BYTES, DP>::kBytes
                                      : (size_t)2 * (kManyStep * (DP + 8) + DP * (kManyStep + 8)) * 2 + 2 * DP * 16 + 16;
   void (*few_kernel)(AttendArgs) = attend_few_kernel<T, BYTES, DP>;
-  if (A.few_rows <= kTokenRows) few_kernel = attend_token_kernel<T, BYTES, kFewDim>;
+  if (token) few_kernel = attend_token_kernel<T, BYTES, kTokenDim>;
   void (*many_kernel)(AttendArgs);
   if constexpr (DP <= kWideDim)
     many_kernel = attend_wide_kernel<T, BYTES, DP>;
@@ -1631,10 +1663,10 @@ hipError_t attend_run(const AttendArgs &A, hipStream_t st) {
                                                hipFuncAttributeMaxDynamicSharedMemorySize, (int)(i ? many : few));
       if (e != hipSuccess) return e;
     }
-  few_kernel<<<grid_of((int64_t)A.few_units * A.heads), 256, few, st>>>(A);
+  few_kernel<<<grid_of((int64_t)A.few_units * A.heads), 64 * waves, few, st>>>(A);
   if (A.tiles) many_kernel<<<grid_of((int64_t)A.tiles * A.heads * A.many_parts), 256, many, st>>>(A);
   const int64_t joins = (A.joined ? (int64_t)few_joins(A) * A.s.n_seqs : 0) + (A.many_parts > 1 ? A.s.n_tokens * many_joins(A) : 0);
-  if (joins) attend_join_kernel<T><<<grid_of(joins), 256, 0, st>>>(A);
+  if (joins) attend_join_kernel<T><<<grid_of(joins), kJoinThreads, 0, st>>>(A);
   return hipGetLastError();
 }
 

@@ -7,15 +7,16 @@ namespace cfp {
 namespace {
 
 // How the work is laid out: bounds from what the host knows; the device cuts by the lengths that it finds.  Sequences with few
-// rows are cut into about kFewParts equal parts over all (six for every workgroup that the chip holds at a time).
+// rows are cut into about kFewParts equal parts over all (512 workgroups are at work at a time).
 void parts_of(const cfp_attend_desc &a, const cfp_cache_desc &c, const cfp_sequences_desc &s, AttendArgs &A) {
   const int64_t g = a.n_q / c.heads, most_len = (int64_t)s.width * c.page;
   const int64_t new_rows = std::min<int64_t>(s.max_new, a.n_tokens) * g;
   // all sequences have few rows, or those that have go with the narrow kernel and the others with the one for many
   A.few_rows = (int32_t)(new_rows <= kFewRows ? new_rows : g <= kTokenRows ? kTokenRows : kFewRows);
-  A.joined = most_len > kFewLeast;
+  A.few_least = A.few_rows <= kTokenRows ? kTokenLeast : kFewLeast;
+  A.joined = most_len > A.few_least;
   A.few_target = (int32_t)std::max<int64_t>(kFewParts / c.heads, 1);
-  A.few_units = s.n_seqs + (A.joined ? (int32_t)std::min<int64_t>(A.few_target, most_len / kFewLeast * s.n_seqs) : 0);
+  A.few_units = s.n_seqs + (A.joined ? (int32_t)std::min<int64_t>(A.few_target, most_len / A.few_least * s.n_seqs) : 0);
   A.many_rows = c.dim <= kWideDim ? kWideRows : kManyRows;
   A.tiles = 0, A.many_parts = 1;
   if (new_rows > A.few_rows) {

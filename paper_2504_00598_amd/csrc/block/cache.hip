@@ -30,9 +30,8 @@ struct CacheArgs {
 
 // Units of sequence b: its tokens by aligned runs of kUnit, the first of which holds token max(pos, 0)
 // (rows before the first token count as that many units more when they are read).
-__device__ __forceinline__ uint32_t units_of(const SeqArgs &S, int b) {
-  const Seq q = seq_of(S, b);
-  const int lo = (int)((q.pos & ~(kUnit - 1)));
+__device__ __forceinline__ uint32_t units_of(const Seq &q) {
+  const int lo = q.pos & ~(kUnit - 1);
   return q.n ? (uint32_t)(q.pos + q.n - lo + kUnit - 1) / kUnit : 0u;
 }
 int64_t most_units(int64_t n_tokens, int64_t n_seqs) { return std::min(n_tokens, n_tokens / kUnit + 2 * n_seqs); }
@@ -47,9 +46,8 @@ struct UnitAt {
 __device__ __forceinline__ bool unit_at(const SeqArgs &S, uint32_t id, UnitAt &u) {
   uint32_t k;
   int b;
-  if (!find_unit(S.n_seqs, id, [&](int i) { return units_of(S, i); }, b, k)) return false;
+  if (!find_unit(S, id, [](const Seq &q) { return units_of(q); }, b, k, u.q)) return false;
   u.b = b;
-  u.q = seq_of(S, b);
   u.first = (u.q.pos & ~(kUnit - 1)) + (int)k * kUnit;
   u.lo = max(u.q.pos - u.first, 0);
   u.hi = min(u.q.pos + u.q.n - u.first, kUnit);

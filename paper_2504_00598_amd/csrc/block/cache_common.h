@@ -28,17 +28,15 @@ struct Seq {
 };
 __device__ __forceinline__ Seq seq_of(const SeqArgs &S, int b) {
   const int64_t from = S.starts[b], to = S.starts[b + 1];
+  const int32_t length = S.lengths[b];
   Seq q;
   q.row = (int32_t)from;
   q.n = from >= 0 && to > from && to <= S.n_tokens ? (int32_t)(to - from) : 0;
-  q.pos = max(S.lengths[b], 0) - q.n;
+  q.pos = max(length, 0) - q.n;
   return q;
 }
-
-// The same of a sequence that is one for all lanes, in scalar registers.
-__device__ __forceinline__ Seq uniform_seq_of(const SeqArgs &S, int b) {
-  const Seq q = seq_of(S, b);
-  return {__builtin_amdgcn_readfirstlane(q.row), __builtin_amdgcn_readfirstlane(q.n), __builtin_amdgcn_readfirstlane(q.pos)};
+__device__ __forceinline__ Seq seq_of_lane(const Seq &q, int lane) {
+  return {__builtin_amdgcn_readlane(q.row, lane), __builtin_amdgcn_readlane(q.n, lane), __builtin_amdgcn_readlane(q.pos, lane)};
 }
 
 // The page of token p >= 0 of sequence b, and whether it is one of the cache's (else page 0).
@@ -74,19 +72,22 @@ __device__ __forceinline__ uint32_t lanes_before(uint32_t v) {
   return v;
 }
 
-// Which sequence the unit `id` belongs to, and the how-manieth of its units it is, where sequence b has units(b) of
+// Which sequence the unit `id` belongs to, and the how-manieth of its units it is, where a sequence q has units(q) of
 // them in a row.  All 64 lanes of a wave call it; false where there is no such unit.
 template <typename F>
-__device__ __forceinline__ bool find_unit(int n_seqs, uint32_t id, F units, int &b, uint32_t &k) {
+__device__ __forceinline__ bool find_unit(const SeqArgs &S, uint32_t id, F units, int &b, uint32_t &k, Seq &q) {
   const int lane = threadIdx.x & 63;
   uint32_t before = 0;
-  for (int first = 0; first < n_seqs; first += 64) {
-    const uint32_t own = first + lane < n_seqs ? units(first + lane) : 0u;
+  for (int first = 0; first < S.n_seqs; first += 64) {
+    Seq s = {0, 0, 0};
+    if (first + lane < S.n_seqs) s = seq_of(S, first + lane);
+    const uint32_t own = first + lane < S.n_seqs ? units(s) : 0u;
     const uint32_t sum = lanes_before(own);
     const uint64_t past = __ballot(before + sum > id);
     if (past) {
       const int l = __builtin_ctzll(past);
       b = first + l;
+      q = seq_of_lane(s, l);
       k = id - before - (uint32_t)__builtin_amdgcn_readlane((int)(sum - own), l);
       return true;
     }
@@ -97,11 +98,11 @@ __device__ __forceinline__ bool find_unit(int n_seqs, uint32_t id, F units, int 
 
 // Units of the sequences before b.  All 64 lanes call it.
 template <typename F>
-__device__ __forceinline__ uint32_t units_before(int b, F units) {
+__device__ __forceinline__ uint32_t units_before(const SeqArgs &S, int b, F units) {
   const int lane = threadIdx.x & 63;
   uint32_t before = 0;
   for (int first = 0; first < b; first += 64)
-    before += (uint32_t)__builtin_amdgcn_readlane((int)lanes_before(first + lane < b ? units(first + lane) : 0u), 63);
+    before += (uint32_t)__builtin_amdgcn_readlane((int)lanes_before(first + lane < b ? units(seq_of(S, first + lane)) : 0u), 63);
   return before;
 }
 
