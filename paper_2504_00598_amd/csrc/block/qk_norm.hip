@@ -16,12 +16,13 @@
 // rotation stays inside a lane and only the sum of squares crosses lanes.  V is
 // the widest load that divides the halves and fits the alignment.
 //
-// With several axes a pair's position is that of its axis, two bits a pair in the arguments: a unit whose pairs share an axis
-// loads its angles as without, another one loads each by itself.
+// With several axes a pair's position is that of its axis, two bits a pair in the arguments; the rows of a workgroup are heads of
+// few tokens, whose angles are gathered into LDS once.
 //
 // Measured, bfloat16, 16384 tokens of 40 + 8 heads of 128: forward 87 us for 403 MB (4.6 TB/s; a copy reaches 5.2),
 // backward 131 us for 604 MB (4.6 TB/s) and 5 us for the sums of dg.  Four tokens: 4 us, the launch.
 #include <algorithm>
+#include <type_traits>
 
 #include "block_common.h"
 
@@ -86,43 +87,47 @@ __device__ __forceinline__ void angles(const QkArgs &A, int64_t p, int u, float 
   load_vec<float, V>(A.sin + o, s);
 }
 
-// The same of a unit of token t, in NaN where a position is outside the tables: the rotated part is not a number then.
-template <int V, bool AXES>
+// The same of a unit of token t, in NaN where the position is outside the tables: the rotated part is not a number then.
+template <int V>
 __device__ __forceinline__ void angles_of(const QkArgs &A, int64_t t, int u, float (&c)[V], float (&s)[V]) {
-  if constexpr (!AXES) {
-    const int64_t p = A.pos ? A.pos[t] : t;
-    if (p >= 0 && p < A.n_pos) {
-      angles<V>(A, p, u, c, s);
-    } else {
-#pragma unroll
-      for (int i = 0; i < V; ++i) c[i] = s[i] = __builtin_nanf("");
-    }
+  const int64_t p = A.pos ? A.pos[t] : t;
+  if (p >= 0 && p < A.n_pos) {
+    angles<V>(A, p, u, c, s);
   } else {
-    int64_t at[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) at[i] = i < A.n_axes ? A.pos[i * A.n_tokens + t] : 0;
-    const uint32_t two = A.axis[u * V / 16] >> (2 * (u * V % 16)) & ((1u << 2 * V) - 1);
-    auto row = [&](uint32_t a) { return a & 2 ? (a & 1 ? at[3] : at[2]) : (a & 1 ? at[1] : at[0]); };
-    if (two == (two & 3) * (((1u << 2 * V) - 1) / 3)) {  // one axis
-      const int64_t p = row(two);
-      if (p >= 0 && p < A.n_pos) {
-        angles<V>(A, p, u, c, s);
-      } else {
-#pragma unroll
-        for (int i = 0; i < V; ++i) c[i] = s[i] = __builtin_nanf("");
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        const int64_t p = row(two >> (2 * i));
-        const bool ok = p >= 0 && p < A.n_pos;
-        const int64_t o = (ok ? p : 0) * (A.rot / 2) + u * V + i;  // a rotated pair has tables of a row at least
-        c[i] = ok ? A.cos[o] : __builtin_nanf("");
-        s[i] = ok ? A.sin[o] : __builtin_nanf("");
-      }
-    }
+    for (int i = 0; i < V; ++i) c[i] = s[i] = __builtin_nanf("");
   }
 }
+
+// Several axes: the angles of a workgroup's rows, which are a few tokens', gathered pair by pair into LDS once.
+// cos, then sin, of up to N pairs: rows of the workgroup times their pairs.
+template <int N>
+struct Gathered {
+  float cs[2][N];
+  // the tokens of rows first .. last
+  __device__ __forceinline__ void gather(const QkArgs &A, int64_t first, int64_t last, int heads) {
+    const int half = A.rot / 2;
+    const int64_t t0 = first / heads;
+    const int n = ((int)(last / heads - t0) + 1) * half;
+    for (int e = threadIdx.x; e < n; e += kQkThreads) {
+      const int i = e % half;
+      const int64_t t = t0 + e / half;
+      const int64_t p = A.pos[(A.axis[i / 16] >> (2 * (i % 16)) & 3) * A.n_tokens + t];
+      const bool ok = p >= 0 && p < A.n_pos;
+      const int64_t o = ok ? p * half + i : 0;
+      cs[0][e] = ok ? A.cos[o] : __builtin_nanf("");
+      cs[1][e] = ok ? A.sin[o] : __builtin_nanf("");
+    }
+  }
+  template <int V>
+  __device__ __forceinline__ void angles(const QkArgs &A, int64_t token, int u, float (&c)[V], float (&s)[V]) const {
+    const int at = (int)token * (A.rot / 2) + u * V;
+    load_vec<float, V>(cs[0] + at, c);
+    load_vec<float, V>(cs[1] + at, s);
+  }
+};
+template <int V, int UPL>
+constexpr int kGathered = kQkThreads * V * UPL;  // G lanes hold a row of up to G V UPL pairs
 
 // Turns the V pairs of a unit by their angles (back: by the opposite ones).
 template <int V, bool BACK>
@@ -152,8 +157,14 @@ __global__ __launch_bounds__(kQkThreads) void qk_fwd_kernel(QkArgs A) {
   constexpr int kRows = kQkThreads / G;
   const int lane = threadIdx.x % G;
   const int heads = A.heads[0] + A.heads[1];
-  const int64_t rows = A.n_tokens * heads;
-  const int64_t row = (int64_t)block_id() * kRows + threadIdx.x / G;
+  const int64_t rows = A.n_tokens * heads, first = (int64_t)block_id() * kRows;
+  const int64_t row = first + threadIdx.x / G;
+  __shared__ std::conditional_t<AXES, Gathered<kGathered<V, UPL>>, int> table;
+  if constexpr (AXES) {
+    if (first >= rows) return;
+    table.gather(A, first, min(first + kRows, rows) - 1, heads);
+    __syncthreads();
+  }
   if (row >= rows) return;  // whole groups leave; the others' shuffles stay inside their group
   const int64_t t = row / heads;
   const int hh = (int)(row - t * heads);
@@ -189,7 +200,10 @@ __global__ __launch_bounds__(kQkThreads) void qk_fwd_kernel(QkArgs A) {
     for (int i = 0; i < V; ++i) b[j][i] *= r * g[i];
     if (u.pair) {
       float c[V], s[V];
-      angles_of<V, AXES>(A, t, un, c, s);
+      if constexpr (AXES)
+        table.template angles<V>(A, t - first / heads, un, c, s);
+      else
+        angles_of<V>(A, t, un, c, s);
       turn<V, false>(a[j], b[j], c, s, A.interleaved != 0);
     }
     store_vec<T, V>(y + u.a, a[j]);
@@ -219,7 +233,15 @@ __global__ __launch_bounds__(kQkThreads) void qk_bwd_kernel(QkArgs A) {
     if (u.a < D) load_gain<V>(A.w[which], A.wdtype, u.a, ga[j]);
     if (u.b < D) load_gain<V>(A.w[which], A.wdtype, u.b, gb[j]);
   }
-  for (int64_t row = first * kRows + threadIdx.x / G; row < rows; row += blocks * kRows) {
+  __shared__ std::conditional_t<AXES, Gathered<kGathered<V, UPL>>, int> table;
+  for (int64_t from = first * kRows; from < rows; from += blocks * kRows) {
+    const int64_t row = from + threadIdx.x / G;
+    if constexpr (AXES) {
+      __syncthreads();  // the angles of the rows before have been read
+      table.gather(A, from, min(from + kRows, rows) - 1, heads);
+      __syncthreads();
+    }
+    if (row >= rows) continue;
     const int64_t t = row / heads;
     const int head = (int)(row - t * heads);
     const T *x = reinterpret_cast<const T *>(A.x[which]) + t * A.sx[which].tok + head * A.sx[which].head;
@@ -243,7 +265,10 @@ __global__ __launch_bounds__(kQkThreads) void qk_bwd_kernel(QkArgs A) {
       }
       if (u.pair) {
         float c[V], s[V];
-        angles_of<V, AXES>(A, t, un, c, s);
+        if constexpr (AXES)
+          table.template angles<V>(A, t - from / heads, un, c, s);
+        else
+          angles_of<V>(A, t, un, c, s);
         turn<V, true>(ya[j], yb[j], c, s, A.interleaved != 0);
       }
 #pragma unroll
