@@ -1065,7 +1065,6 @@ template <int N>
 __device__ __forceinline__ void copies_left() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
-static __device__ const u32x4 kZeros = {0, 0, 0, 0};  // what rows of values behind the last entry are copied from
 
 // c += a b with the sums in accumulation registers.  Written as an instruction because the allocator, left the choice,
 // moves them between both halves of the register file around every use of a score.  It does not know the
@@ -1101,6 +1100,8 @@ __device__ __forceinline__ void settle_products(f32x16 (&o)[N]) {
 #pragma unroll
   for (int i = 0; i < N; ++i) asm volatile("" : "+a"(o[i]));
 }
+// Between a product and one that adds to its result, or (behind one more product) what reads it.
+__device__ __forceinline__ void apart() { asm volatile("s_nop 7" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void settle_scores(f32x16 (&s)[N]) {
   asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
@@ -1147,21 +1148,22 @@ __device__ __forceinline__ int value_place(int d, int c) { return c ^ (d >> 1 & 
 // scales; the bits of take_odd.
 template <typename T, bool BYTES, int DP>
 struct Wide {
+  static constexpr int kCols = 1, kWaves = 8 / kCols;                 // columns of 32 rows of a wave; waves
   static constexpr int kRing = BYTES ? 3 : 4, kLead = BYTES ? 4 : 3;  // tiles; how far ahead of its use a tile of keys is copied
   static constexpr int kTile = 64 * DP;                               // entries
   static constexpr int kRaw = BYTES ? (DP + 63) / 64 : 0;             // copies of a wave for a tile as it is, of keys and of values
-  static constexpr int kCopies = BYTES ? 2 * kRaw + 1 : DP / 16;      // of a wave for a tile of keys and one of values
+  static constexpr int kCopies = (BYTES ? kRaw : DP / 32) * (kWaves == 8 ? 1 : 2) + (BYTES ? 1 : 0);  // of a wave for a tile of keys and one of values
   static constexpr uint32_t kKeys = 0, kValues = kRing * kTile * 2, kRawKeys = 2 * kValues, kRawValues = kRawKeys + 3 * kRaw * 4096,
                             kScales = kRawValues + 3 * kRaw * 4096, kOdds = kScales + (BYTES ? 3 * 1024 : 0),
                             kOddAt = kOdds + DP * 16, kBytes = kOddAt + 16;
 };
 
 template <typename T, bool BYTES, int DP>
-__global__ __launch_bounds__(256, 1) void attend_wide_kernel(AttendArgs A) {
+__global__ __launch_bounds__(64 * (Wide<T, BYTES, DP>::kWaves), (Wide<T, BYTES, DP>::kWaves) / 4) void attend_wide_kernel(AttendArgs A) {
   typedef std::conditional_t<BYTES, uint8_t, T> H;
   typedef vec<T, 8> Vec8;
   typedef Wide<T, BYTES, DP> W;
-  constexpr int kMt = DP / 32, kC = DP / 16, kTile = W::kTile, kLead = W::kLead;
+  constexpr int kMt = DP / 32, kC = DP / 16, kTile = W::kTile, kLead = W::kLead, kX = W::kCols, kThreads = 64 * W::kWaves;
   extern __shared__ __align__(1024) char shared_bytes[];
   const T *keys = reinterpret_cast<const T *>(shared_bytes + W::kKeys);
   T *values = reinterpret_cast<T *>(shared_bytes + W::kValues);
@@ -1192,13 +1194,13 @@ __global__ __launch_bounds__(256, 1) void attend_wide_kernel(AttendArgs A) {
   const int begin = sp.begin + part * sp.per, end = min(sp.end, begin + sp.per);
   const int n = end > begin ? (end - begin + 63) / 64 : 0;  // tiles
   const int all_hi = A.causal ? p0 : len - 1, all_lo = A.window > 0 ? p1 - A.window + 1 : 0;
-  const bool active = r0 + wave * 64 < rows;  // of the wave
+  const bool active = r0 + wave * 32 * kX < rows;  // of the wave
 
-  Vec8 q[2][kC];
-  int hi[2], lo[2];
+  Vec8 q[kX][kC];
+  int hi[kX], lo[kX];
 #pragma unroll
-  for (int x = 0; x < 2; ++x) {
-    const int r = r0 + wave * 64 + 32 * x + col, i = r / g;
+  for (int x = 0; x < kX; ++x) {
+    const int r = r0 + (wave * kX + x) * 32 + col, i = r / g;
     const bool mine = r < rows;
     hi[x] = mine ? (A.causal ? sq.pos + i : len - 1) : -1, lo[x] = A.window > 0 ? sq.pos + i - A.window + 1 : 0;
     const T *qp = reinterpret_cast<const T *>(A.q) + (int64_t)(sq.row + i) * A.qt + (int64_t)(head * g + r % g) * A.qh;
@@ -1206,21 +1208,27 @@ __global__ __launch_bounds__(256, 1) void attend_wide_kernel(AttendArgs A) {
     for (int c = 0; c < kC; ++c) q[x][c] = load_q<T>(qp, 16 * c + 8 * h, D, mine, A.wide != 0);
   }
 
-  // ---- copies.  Keys: wave w copies tokens 16 w .. + 15, which lie in one page; values: a lane's 16 bytes of every row
-  // that it copies are of the same tokens.
+  // ---- copies.  Of eight waves four copy keys and four values.  Keys: wave w copies tokens 16 w .. + 15, which lie in one page; values: a lane's 16 bytes of every row
+  // that it copies are of the same tokens.  In pages of 64 and more a tile lies in one, and all bases are scalars.
+  const int quarter = wave & 3;
+  const bool for_keys = W::kWaves == 4 || wave < 4, for_values = W::kWaves == 4 || wave >= 4;
   const int page = 1 << A.s.page_shift, inner = page - 1;
+  const bool single = page >= 64;
   typedef Pages4 Pages;
   const TableRow table = table_row(A.s, b);
   auto pages = [&](int j) {
     const int t = begin + 64 * j;
-    return Pages{table.entry(t), table.entry(t + 16), table.entry(t + 32), table.entry(t + 48)};
+    const uint32_t e = table.entry(t);
+    if (single) return Pages{e, e, e, e};
+    return Pages{e, table.entry(t + 16), table.entry(t + 32), table.entry(t + 48)};
   };
   auto inside = [&](uint32_t e) { return e < A.s.n_pages; };
   auto outside4 = [&](const Pages &pg) {
+    if (single) return inside(pg.a) ? 0u : 15u;
     return (inside(pg.a) ? 0u : 1u) | (inside(pg.b) ? 0u : 2u) | (inside(pg.c) ? 0u : 4u) | (inside(pg.d) ? 0u : 8u);
   };
   auto pick = [&](const Pages &pg, int j) -> int64_t {
-    const uint32_t e = one_of(pg, j);
+    const uint32_t e = single ? pg.a : one_of(pg, j);
     return inside(e) ? e : 0u;
   };
   auto slot = [&](int j) { return W::kRing == 4 ? j & 3 : j % 3; };
@@ -1228,32 +1236,43 @@ __global__ __launch_bounds__(256, 1) void attend_wide_kernel(AttendArgs A) {
   const H *vbase = reinterpret_cast<const H *>(A.v) + (int64_t)head * page * D;
   constexpr int kRowPieces = DP / (16 / (int)sizeof(H));  // of 16 bytes, of a row of keys in LDS
   constexpr int kKeyCopies = BYTES ? W::kRaw : DP / 32, kValueCopies = kKeyCopies;
-  uint32_t key_off[kKeyCopies];  // bytes from the wave's first token's key; ~0: nothing
+  constexpr bool kRagged = BYTES && DP == 96;             // a wave's keys do not fill its copies
+  uint32_t key_off[kKeyCopies], value_off[kValueCopies];  // bytes from the wave's first token's key (~0: nothing); from the tokens
+  const int value_row = BYTES ? quarter * 16 + lane / 4 : quarter * 8 + lane / 8;
+  const int value_tok = BYTES ? lane % 4 * 16 : 8 * value_place(value_row, lane % 8);
 #pragma unroll
   for (int e = 0; e < kKeyCopies; ++e) {
     const int m = e * 64 + lane, row = m / kRowPieces;
-    const int d = BYTES ? m % kRowPieces * 16 : 8 * key_piece<DP>(16 * wave + row, m % kRowPieces);
+    const int d = BYTES ? m % kRowPieces * 16 : 8 * key_piece<DP>(16 * quarter + row, m % kRowPieces);
     key_off[e] = row < 16 && d < D ? (uint32_t)((row * D + d) * sizeof(H)) : ~0u;
+    // rows of values behind the last entry are copies of it: what comes of them is not stored
+    value_off[e] = (uint32_t)(((int64_t)min(value_row + e * (BYTES ? 64 : 32), D - 1) * page + value_tok) * sizeof(H));
   }
-  // first row of this lane's copies of values and its tokens in the tile
-  const int value_row = BYTES ? wave * 16 + lane / 4 : wave * 8 + lane / 8;
-  const int value_tok = BYTES ? lane % 4 * 16 : 8 * value_place(value_row, lane % 8);
-  constexpr int kValueRows = BYTES ? 64 : 32;  // that all waves' copies of one number take
   auto copy_keys = [&](int j, const Pages &pg) {
-    const int t = begin + 64 * j + 16 * wave;
-    const H *base = uniform_pointer(kbase + pick(pg, wave) * A.kp + (t & inner) * D);
-    const uint32_t to = BYTES ? W::kRawKeys + (j % 3) * W::kRaw * 4096 + wave * W::kRaw * 1024 : W::kKeys + slot(j) * kTile * 2 + wave * 32 * DP;
+    const int t = begin + 64 * j + 16 * quarter;
+    const H *base = uniform_pointer(kbase + pick(pg, quarter) * A.kp + (t & inner) * D);
+    const uint32_t to = BYTES ? W::kRawKeys + (j % 3) * W::kRaw * 4096 + quarter * W::kRaw * 1024 : W::kKeys + slot(j) * kTile * 2 + quarter * 32 * DP;
+    if (D == DP && !kRagged) {
 #pragma unroll
-    for (int e = 0; e < kKeyCopies; ++e)
-      if (key_off[e] != ~0u) copy_piece(base, key_off[e], to + e * 1024);
+      for (int e = 0; e < kKeyCopies; ++e) copy_piece(base, key_off[e], to + e * 1024);
+    } else {
+#pragma unroll
+      for (int e = 0; e < kKeyCopies; ++e)
+        if (key_off[e] != ~0u) copy_piece(base, key_off[e], to + e * 1024);
+    }
   };
   auto copy_values = [&](int j, const Pages &pg) {
-    const H *from = vbase + pick(pg, value_tok >> 4) * A.vp + ((begin + 64 * j + value_tok) & inner) + value_row * page;
-    const uint32_t to = BYTES ? W::kRawValues + (j % 3) * W::kRaw * 4096 + wave * 1024 : W::kValues + slot(j) * kTile * 2 + wave * 1024;
+    const int t = begin + 64 * j;
+    const uint32_t to = BYTES ? W::kRawValues + (j % 3) * W::kRaw * 4096 + quarter * 1024 : W::kValues + slot(j) * kTile * 2 + quarter * 1024;
+    if (single) {
+      const H *base = uniform_pointer(vbase + pick(pg, 0) * A.vp + (t & inner));
 #pragma unroll
-    for (int e = 0; e < kValueCopies; ++e) {
-      copy_piece(value_row + e * kValueRows < D ? (const void *)from : (const void *)&kZeros, to + e * 4096);
-      from += kValueRows * page;
+      for (int e = 0; e < kValueCopies; ++e) copy_piece(base, value_off[e], to + e * 4096);
+    } else {
+      const int at = value_tok & ~15;  // value_off counts from the tile's first token
+      const char *from = reinterpret_cast<const char *>(vbase + pick(pg, at >> 4) * A.vp + (((t + at) & inner) - at));
+#pragma unroll
+      for (int e = 0; e < kValueCopies; ++e) copy_piece(from + value_off[e], to + e * 4096);
     }
   };
   // 8 bits: scales of the keys of a tile and of the values of the one before it, 64 bytes each (every wave copies all)
@@ -1267,8 +1286,8 @@ __global__ __launch_bounds__(256, 1) void attend_wide_kernel(AttendArgs A) {
   auto widen_keys = [&](int j) {
     if constexpr (BYTES) {
 #pragma unroll
-      for (int e = 0; e < W::kRaw; ++e) {
-        const int m = e * 256 + tid, w = m / (W::kRaw * 64), i = m % (W::kRaw * 64), row = 16 * w + i / kRowPieces, c = i % kRowPieces * 2;
+      for (int m = tid; m < W::kRaw * 256; m += kThreads) {
+        const int w = m / (W::kRaw * 64), i = m % (W::kRaw * 64), row = 16 * w + i / kRowPieces, c = i % kRowPieces * 2;
         if (i >= 16 * kRowPieces || 8 * c >= D) continue;
         const u32x4 x = *reinterpret_cast<const u32x4 *>(shared_bytes + W::kRawKeys + (j % 3) * W::kRaw * 4096 + m * 16);
         const float by = scale_of((uint8_t)shared_bytes[W::kScales + (j % 3) * 1024 + row]);
@@ -1282,8 +1301,8 @@ __global__ __launch_bounds__(256, 1) void attend_wide_kernel(AttendArgs A) {
     if constexpr (BYTES) {
       const u32x4 by = *reinterpret_cast<const u32x4 *>(shared_bytes + W::kScales + ((j + 1) % 3) * 1024 + 64 + tid % 4 * 16);
 #pragma unroll
-      for (int e = 0; e < W::kRaw; ++e) {
-        const int m = e * 256 + tid, d = m / 4, c = m % 4 * 2;
+      for (int m = tid; m < W::kRaw * 256; m += kThreads) {
+        const int d = m / 4, c = m % 4 * 2;
         if (d >= DP) continue;
         const u32x4 x = *reinterpret_cast<const u32x4 *>(shared_bytes + W::kRawValues + (j % 3) * W::kRaw * 4096 + m * 16);
         T *to = values + slot(j) * kTile + d * 64;
@@ -1293,8 +1312,9 @@ __global__ __launch_bounds__(256, 1) void attend_wide_kernel(AttendArgs A) {
     }
   };
 
-  Rows<T, DP> st[2];
-  st[0].clear(), st[1].clear();
+  Rows<T, DP> st[kX];
+#pragma unroll
+  for (int x = 0; x < kX; ++x) st[x].clear();
   const int ki = 16 * (col >> 2 & 1) + 4 * (col >> 3) + (col & 3);
   int koff[kC], voff[4];
 #pragma unroll
@@ -1314,29 +1334,29 @@ __global__ __launch_bounds__(256, 1) void attend_wide_kernel(AttendArgs A) {
 #pragma unroll
     for (int c = 0; c < kAhead; ++c) first_k[c] = key_piece_of(k, ku, c), first_v[c] = value_piece_of(v, vu, c);
   };
-  auto stage = [&](f32x16 (&s)[2], Vec8 (&p)[2][2], f32x16 (&next)[2], const T *k, int ku, const T *v, int vu, const Vec8 (&pp)[2][2],
+  auto stage = [&](f32x16 (&s)[kX], Vec8 (&p)[kX][2], f32x16 (&next)[kX], const T *k, int ku, const T *v, int vu, const Vec8 (&pp)[kX][2],
                    const T *then_k, int then_ku, const T *then_v, int then_vu) {
-    constexpr int kSlots = 4 * kC, kFirst = 4, kOver = kSlots - kFirst - 2;  // products; the first kFirst share the maxima
+    constexpr int kSlots = 2 * kX * kC, kFirst = 4, kOver = kSlots - kFirst - 2;  // products; the first kFirst share the maxima
     Vec8 ka[kHeld], va[kHeld];
 #pragma unroll
     for (int c = 0; c < kAhead; ++c) ka[c] = first_k[c], va[c] = first_v[c];
-    float top[2][4], to[2], by[2], from[2], sum[2] = {0.f, 0.f}, w[32];
+    float top[kX][4], to[kX], by[kX], from[kX], sum[kX] = {}, w[16 * kX];
     bool grows = false;
     auto vector_share = [&](int slot) {
       if (slot == 0) {
 #pragma unroll
-        for (int x = 0; x < 2; ++x)
+        for (int x = 0; x < kX; ++x)
 #pragma unroll
           for (int i = 0; i < 4; ++i) top[x][i] = max3(s[x][4 * i], s[x][4 * i + 1], s[x][4 * i + 2]);
       } else if (slot == 1) {
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
+        for (int x = 0; x < kX; ++x) {
           top[x][0] = max3(top[x][0], s[x][3], s[x][7]), top[x][1] = max3(top[x][1], s[x][11], s[x][15]);
           top[x][0] = max3(top[x][0], top[x][2], top[x][3]);
         }
       } else if (slot == 2) {
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
+        for (int x = 0; x < kX; ++x) {
           const float t = max3(top[x][0], top[x][1], partner(max3(top[x][0], top[x][1], top[x][1]))) * A.scale;
           const bool more = t > st[x].m + kGrowth<T>;
           grows = grows || more;
@@ -1345,14 +1365,14 @@ __global__ __launch_bounds__(256, 1) void attend_wide_kernel(AttendArgs A) {
         }
       } else if (slot == 3) {
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
+        for (int x = 0; x < kX; ++x) {
           by[x] = to[x] == st[x].m ? 1.f : __builtin_amdgcn_exp2f(st[x].m - to[x]);
           st[x].m = to[x];
         }
       }
 #pragma unroll
-      for (int e = 0; e < 32; ++e) {
-        const int x = e / 16, i = e % 16, at = kFirst + e * kOver / 32;
+      for (int e = 0; e < 16 * kX; ++e) {
+        const int x = e / 16, i = e % 16, at = kFirst + e * kOver / (16 * kX);
         if (slot == at + 2) {
           sum[x] += w[e];
           if (i % 2) p[x][i / 8][i % 8 - 1] = (T)w[e - 1], p[x][i / 8][i % 8] = (T)w[e];
@@ -1372,59 +1392,62 @@ __global__ __launch_bounds__(256, 1) void attend_wide_kernel(AttendArgs A) {
         first_v[c + kAhead - kC] = value_piece_of(then_v, then_vu, c + kAhead - kC);
       }
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
+      for (int x = 0; x < kX; ++x) {
         score_product<T>(next[x], ka[c % kHeld], q[x][c], c == 0);
-        vector_share(4 * c + x);
+        vector_share(2 * kX * c + x);
         __builtin_amdgcn_sched_barrier(0);
       }
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
+      for (int x = 0; x < kX; ++x) {
         add_product<T>(st[x].o[c / 2], va[c % kHeld], pp[x][c % 2]);
-        vector_share(4 * c + 2 + x);
+        vector_share(2 * kX * c + kX + x);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
 #pragma unroll
-    for (int x = 0; x < 2; ++x) st[x].l = st[x].l * by[x] + sum[x];
+    for (int x = 0; x < kX; ++x) st[x].l = st[x].l * by[x] + sum[x];
+    if constexpr (kX == 1) apart();  // one product has followed the last score
     if (__any(grows)) {
-      settle_products(st[0].o), settle_products(st[1].o);
 #pragma unroll
-      for (int x = 0; x < 2; ++x)
+      for (int x = 0; x < kX; ++x) {
+        settle_products(st[x].o);
 #pragma unroll
         for (int mt = 0; mt < kMt; ++mt) times_sums(st[x].o[mt], by[x]);
-      before_products(st[0].o), before_products(st[1].o);
+        before_products(st[x].o);
+      }
     }
   };
 
-  before_products(st[0].o), before_products(st[1].o);
 #pragma unroll
-  for (int x = 0; x < 2; ++x)
+  for (int x = 0; x < kX; ++x) before_products(st[x].o);
+#pragma unroll
+  for (int x = 0; x < kX; ++x)
 #pragma unroll
     for (int c = 0; c < kC; ++c) asm volatile("" : "+a"(q[x][c]));  // queries stay in accumulation registers too
   if (n > 0) {
     // zeros where no key's entry is written to, and in the tile of values that stands before the first
     constexpr uint32_t kBefore = W::kValues + (W::kRing - 1) * kTile * 2;
-    for (uint32_t e = tid * 16; e < (D < DP ? W::kValues : 0u); e += 4096) *reinterpret_cast<u32x4 *>(shared_bytes + e) = u32x4{0, 0, 0, 0};
-    for (uint32_t e = tid * 16; e < kTile * 2; e += 4096) *reinterpret_cast<u32x4 *>(shared_bytes + kBefore + e) = u32x4{0, 0, 0, 0};
+    for (uint32_t e = tid * 16; e < (D < DP ? W::kValues : 0u); e += 16 * kThreads) *reinterpret_cast<u32x4 *>(shared_bytes + e) = u32x4{0, 0, 0, 0};
+    for (uint32_t e = tid * 16; e < kTile * 2; e += 16 * kThreads) *reinterpret_cast<u32x4 *>(shared_bytes + kBefore + e) = u32x4{0, 0, 0, 0};
     if (tid == 0) *odd_at = 0;
     __syncthreads();
     uint32_t bad = 0;  // bits of 16 tokens each without a page, of this tile and those after it
-    Pages pk = pages(0), pv = pk;  // of the tiles of keys and of values that are copied next
+    Pages pk = pages(0), pv = pk, pn = 1 < n ? pages(1) : pk;  // of the tiles of keys and of values copied next, and after
     auto copy_next = [&](int j) {  // keys of tile j and values of j - 1, whose pages are pk and pv
       if (j < n) {
-        copy_keys(j, pk);
+        if (for_keys) copy_keys(j, pk);
         bad |= outside4(pk) << (4 * kLead);
       }
       if constexpr (BYTES) {
         if (j - 1 < n) copy_scales(j, pk, pv);
       }
-      if (j > 0 && j - 1 < n) copy_values(j - 1, pv);
+      if (for_values && j > 0 && j - 1 < n) copy_values(j - 1, pv);
     };
 #pragma unroll
     for (int j = 0; j < 3; ++j) {
-      const Pages after = j + 1 < n ? pages(j + 1) : pk;
       copy_next(j);
-      pv = pk, pk = after;
+      pv = pk, pk = pn;
+      if (j + 2 < n) pn = pages(j + 2);
       bad >>= 4;
     }
     copies_left<0>();
@@ -1434,15 +1457,15 @@ __global__ __launch_bounds__(256, 1) void attend_wide_kernel(AttendArgs A) {
       if (n > 1) widen_keys(1);
       widen_values(0);
       __syncthreads();
-      const Pages after = 4 < n ? pages(4) : pk;
       copy_next(3);
-      pv = pk, pk = after;
+      pv = pk, pk = pn;
+      if (5 < n) pn = pages(5);
       bad >>= 4;
     }
-    f32x16 s0[2], s1[2];
-    Vec8 pa[2][2], pb[2][2];
+    f32x16 s0[kX], s1[kX];
+    Vec8 pa[kX][2], pb[kX][2];
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
+    for (int x = 0; x < kX; ++x)
 #pragma unroll
       for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -1451,7 +1474,10 @@ __global__ __launch_bounds__(256, 1) void attend_wide_kernel(AttendArgs A) {
 #pragma unroll
       for (int c = 0; c < kC; ++c)
 #pragma unroll
-        for (int x = 0; x < 2; ++x) score_product<T>(s0[x], key_piece_of(keys, 0, c), q[x][c], c == 0);
+        for (int x = 0; x < kX; ++x) {
+          score_product<T>(s0[x], key_piece_of(keys, 0, c), q[x][c], c == 0);
+          apart();
+        }
     settle_scores(s0);
     first_pieces(keys, 1, values + (W::kRing - 1) * kTile, 1);
     for (int j = 0; j < n; ++j) {
@@ -1462,14 +1488,13 @@ __global__ __launch_bounds__(256, 1) void attend_wide_kernel(AttendArgs A) {
       else
         copies_left<0>();
       __syncthreads();  // and what is overwritten now has been read
-      const Pages after = j + kLead + 1 < n ? pages(j + kLead + 1) : pk;
       copy_next(j + kLead);
       const T *k1 = keys + slot(j + 1) * kTile, *k0 = keys + slot(j) * kTile;
       T *v0 = values + slot(j) * kTile;
       const T *v1 = values + slot(j + W::kRing - 1) * kTile;  // tile j - 1
       const bool partly = t + 63 > all_hi || t < all_lo;  // some row does not see all tokens
       if (partly) {
-        for (int m = tid; m < D * 8; m += 256) {
+        for (int m = tid; m < D * 8; m += kThreads) {
           const int d = m / 8, c = value_place(d, m % 8);
           u32x4 w = reinterpret_cast<const u32x4 *>(v0)[m];
           uint32_t up, down;
@@ -1483,7 +1508,7 @@ __global__ __launch_bounds__(256, 1) void attend_wide_kernel(AttendArgs A) {
         __syncthreads();
         if (*odd_at == t + 1) {
 #pragma unroll
-          for (int x = 0; x < 2; ++x) {
+          for (int x = 0; x < kX; ++x) {
             const uint32_t sees[2] = {bits_of(hi[x] + 1 - t) & ~bits_of(lo[x] - t), bits_of(hi[x] + 1 - t - 32) & ~bits_of(lo[x] - t - 32)};
 #pragma unroll
             for (int mt = 0; mt < kMt; ++mt)
@@ -1502,18 +1527,19 @@ __global__ __launch_bounds__(256, 1) void attend_wide_kernel(AttendArgs A) {
         const int first = t + 16 * h;
         if (edge)
 #pragma unroll
-          for (int x = 0; x < 2; ++x) mask16(s0[x], first, lo[x], hi[x], bad >> h & 1);
+          for (int x = 0; x < kX; ++x) mask16(s0[x], first, lo[x], hi[x], bad >> h & 1);
         stage(s0, pa, s1, k0, 1, v1, 1, pb, k1, 0, v0, 0);
         if (edge)
 #pragma unroll
-          for (int x = 0; x < 2; ++x) mask16(s1[x], first + 32, lo[x], hi[x], bad >> (2 + h) & 1);
+          for (int x = 0; x < kX; ++x) mask16(s1[x], first + 32, lo[x], hi[x], bad >> (2 + h) & 1);
         stage(s1, pb, s0, k1, 0, v0, 0, pa, k1, 1, v0, 1);
       }
       if constexpr (BYTES) {
         if (j + 2 < n) widen_keys(j + 2);
         if (j + 1 < n) widen_values(j + 1);
       }
-      pv = pk, pk = after;
+      pv = pk, pk = pn;
+      if (j + kLead + 2 < n) pn = pages(j + kLead + 2);  // looked at behind the barrier after next
       bad >>= 4;
     }
     if (active) {
@@ -1521,15 +1547,19 @@ __global__ __launch_bounds__(256, 1) void attend_wide_kernel(AttendArgs A) {
 #pragma unroll
       for (int m = 0; m < kC; ++m)
 #pragma unroll
-        for (int x = 0; x < 2; ++x) add_product<T>(st[x].o[m / 2], value_piece_of(v, 1, m), pb[x][m % 2]);
+        for (int x = 0; x < kX; ++x) {
+          add_product<T>(st[x].o[m / 2], value_piece_of(v, 1, m), pb[x][m % 2]);
+          apart();
+        }
     }
   }
   if (!active) return;
-  settle_products(st[0].o), settle_products(st[1].o);
 #pragma unroll
-  for (int x = 0; x < 2; ++x) {
+  for (int x = 0; x < kX; ++x) settle_products(st[x].o);
+#pragma unroll
+  for (int x = 0; x < kX; ++x) {
     st[x].finish();
-    const int r = r0 + wave * 64 + 32 * x + col;
+    const int r = r0 + (wave * kX + x) * 32 + col;
     if (r >= rows) continue;
     const int64_t row = (int64_t)(sq.row + r / g) * hq + head * g + r % g;
     if (sp.parts <= 1) {
@@ -1558,40 +1588,43 @@ __global__ __launch_bounds__(256, 1) void attend_wide_kernel(AttendArgs A) {
   }
 }
 
-// ---- the parts of a row together: a workgroup takes 32 times four entries of rows, and of each eight threads every eighth
-// part; their sums meet in LDS, in order.  The first workgroups take the sequences with few rows, the others the tokens
-// of the others.
-constexpr int kJoinQuads = 32, kJoinThreads = 8 * kJoinQuads;
+// ---- the parts of a row together, in their order.  The first workgroups take sequences with few rows: 32 times four entries,
+// and of each eight threads every eighth part, whose sums meet in LDS.  The others take the tokens of the other
+// sequences, whose parts are few: a thread four entries.
+constexpr int kJoinThreads = 256, kJoinQuads = kJoinThreads / 8;
 
 // All threads of a workgroup call it; `there`: this thread's entries are some row's.
-template <typename T>
+template <typename T, int SPLIT>
 __device__ __forceinline__ void join_row(const AttendArgs &A, const float *po, const float *pm, int64_t at, int64_t step, int parts,
                                          int64_t row, int d, bool there) {
-  __shared__ vec<float, 4> sums[8][kJoinQuads];
-  __shared__ float ml[2][8][kJoinQuads];
-  const int k = threadIdx.x / kJoinQuads, e = threadIdx.x % kJoinQuads;
+  constexpr int kQuads = kJoinThreads / SPLIT;
+  const int k = threadIdx.x / kQuads, e = threadIdx.x % kQuads;
   float top = -__builtin_inff(), l = 0.f;
   vec<float, 4> o = {0.f, 0.f, 0.f, 0.f};
   if (there) {
-    for (int s = k; s < parts; s += 8) top = fmaxf(top, pm[2 * (at + s * step)]);
+    for (int s = k; s < parts; s += SPLIT) top = fmaxf(top, pm[2 * (at + s * step)]);
 #pragma unroll 4
-    for (int s = k; s < parts; s += 8) {
+    for (int s = k; s < parts; s += SPLIT) {
       const int64_t a = at + s * step;
       const float m = pm[2 * a], by = m == top ? 1.f : __builtin_amdgcn_exp2f(m - top);
       l += pm[2 * a + 1] * by;
       o += *reinterpret_cast<const vec<float, 4> *>(po + a * A.dim + d) * by;
     }
   }
-  sums[k][e] = o, ml[0][k][e] = top, ml[1][k][e] = l;
-  __syncthreads();
-  if (k != 0 || !there) return;
-  for (int w = 1; w < 8; ++w) top = fmaxf(top, ml[0][w][e]);
-  l = 0.f, o = vec<float, 4>{0.f, 0.f, 0.f, 0.f};
-  for (int w = 0; w < 8; ++w) {
-    const float m = ml[0][w][e], by = m == top ? 1.f : __builtin_amdgcn_exp2f(m - top);
-    l += ml[1][w][e] * by;
-    o += sums[w][e] * by;
+  if constexpr (SPLIT > 1) {
+    __shared__ vec<float, 4> sums[SPLIT][kQuads];
+    __shared__ float ml[2][SPLIT][kQuads];
+    sums[k][e] = o, ml[0][k][e] = top, ml[1][k][e] = l;
+    __syncthreads();
+    for (int w = 1; w < SPLIT; ++w) top = fmaxf(top, ml[0][w][e]);
+    l = 0.f, o = vec<float, 4>{0.f, 0.f, 0.f, 0.f};
+    for (int w = 0; w < SPLIT; ++w) {
+      const float m = ml[0][w][e], by = m == top ? 1.f : __builtin_amdgcn_exp2f(m - top);
+      l += ml[1][w][e] * by;
+      o += sums[w][e] * by;
+    }
   }
+  if (k != 0 || !there) return;
   const float inv = l == 0.f ? 0.f : 1.f / l;
   const float y[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
   store_vec<T, 4>(reinterpret_cast<T *>(A.out) + row * A.dim + d, y);
@@ -1603,7 +1636,7 @@ inline __host__ __device__ uint32_t few_joins(const AttendArgs &A) {
   return (uint32_t)(((int64_t)A.heads * A.few_rows * (A.dim / 4) + kJoinQuads - 1) / kJoinQuads);
 }
 inline __host__ __device__ uint32_t many_joins(const AttendArgs &A) {
-  return (uint32_t)(((int64_t)A.heads * A.group * (A.dim / 4) + kJoinQuads - 1) / kJoinQuads);
+  return (uint32_t)(((int64_t)A.heads * A.group * (A.dim / 4) + kJoinThreads - 1) / kJoinThreads);
 }
 
 template <typename T>
@@ -1622,7 +1655,7 @@ __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendArgs A)
     const uint32_t unit = units_before(A.s, b, [&](const Seq &s) { return few_parts(A, s, per); });
     const int rows = sq.n * g, e = (int)(id % few) * kJoinQuads + threadIdx.x % kJoinQuads;
     const int r = e / quads % rows, head = e / quads / rows;
-    join_row<T>(A, A.few_o, A.few_ml, ((int64_t)unit * A.heads + head) * A.few_rows + r, (int64_t)A.heads * A.few_rows, parts,
+    join_row<T, 8>(A, A.few_o, A.few_ml, ((int64_t)unit * A.heads + head) * A.few_rows + r, (int64_t)A.heads * A.few_rows, parts,
                 (int64_t)(sq.row + r / g) * hq + head * g + r % g, e % quads * 4, head < A.heads);
     return;
   }
@@ -1633,13 +1666,13 @@ __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendArgs A)
   uint32_t k;
   Seq sq;
   if (token < A.s.starts[0] || !find_unit(A.s, (uint32_t)(token - A.s.starts[0]), [](const Seq &s) { return (uint32_t)s.n; }, b, k, sq)) return;
-  const int len = sq.pos + sq.n, rows = sq.n * g, e = (int)(id % many) * kJoinQuads + threadIdx.x % kJoinQuads;
+  const int len = sq.pos + sq.n, rows = sq.n * g, e = (int)(id % many) * kJoinThreads + threadIdx.x;
   if (sq.n > A.max_new || len > (A.s.width << A.s.page_shift) || rows <= A.few_rows) return;
   const int head = min(e / quads, hq - 1), i = (int)k, r = i * g + head % g;
   const int r0 = r / A.many_rows * A.many_rows, r1 = min(r0 + A.many_rows, rows);
   const Span sp = span_of<kManyStep, kManyLeast>(A, sq.pos + r0 / g, sq.pos + (r1 - 1) / g, len, A.many_parts);
   const int64_t row = (int64_t)(sq.row + i) * hq + head;
-  join_row<T>(A, A.many_o, A.many_ml, row, A.s.n_tokens * hq, sp.parts, row, e % quads * 4, sp.parts > 1 && e < hq * quads);
+  join_row<T, 1>(A, A.many_o, A.many_ml, row, A.s.n_tokens * hq, sp.parts, row, e % quads * 4, sp.parts > 1 && e < hq * quads);
 }
 
 template <typename T, bool BYTES, int DP>
@@ -1653,8 +1686,9 @@ hipError_t attend_run(const AttendArgs &A, hipStream_t st) {
   void (*few_kernel)(AttendArgs) = attend_few_kernel<T, BYTES, DP>;
   if (token) few_kernel = attend_token_kernel<T, BYTES, kTokenDim>;
   void (*many_kernel)(AttendArgs);
+  int many_threads = 256;
   if constexpr (DP <= kWideDim)
-    many_kernel = attend_wide_kernel<T, BYTES, DP>;
+    many_kernel = attend_wide_kernel<T, BYTES, DP>, many_threads = 64 * Wide<T, BYTES, DP>::kWaves;
   else
     many_kernel = attend_many_kernel<T, BYTES, DP>;
   for (int i = 0; i < 2; ++i)  // LDS beyond 64 KiB is asked for
@@ -1664,7 +1698,7 @@ hipError_t attend_run(const AttendArgs &A, hipStream_t st) {
       if (e != hipSuccess) return e;
     }
   few_kernel<<<grid_of((int64_t)A.few_units * A.heads), 64 * waves, few, st>>>(A);
-  if (A.tiles) many_kernel<<<grid_of((int64_t)A.tiles * A.heads * A.many_parts), 256, many, st>>>(A);
+  if (A.tiles) many_kernel<<<grid_of((int64_t)A.tiles * A.heads * A.many_parts), many_threads, many, st>>>(A);
   const int64_t joins = (A.joined ? (int64_t)few_joins(A) * A.s.n_seqs : 0) + (A.many_parts > 1 ? A.s.n_tokens * many_joins(A) : 0);
   if (joins) attend_join_kernel<T><<<grid_of(joins), kJoinThreads, 0, st>>>(A);
   return hipGetLastError();
