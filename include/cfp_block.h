@@ -168,6 +168,7 @@ int cfp_experts_bwd(const cfp_experts_desc *d, const void *dy, int64_t dy_stride
 #define CFP_DT_E4M3 3
 #define CFP_CACHE_MAX_DIM 256
 #define CFP_CACHE_MAX_PAGE 256
+#define CFP_MAX_SEQUENCES (1 << 20)
 
 /* Keys [n_pages][heads][page][dim] and values [n_pages][heads][dim][page]: a value's tokens lie behind each other, as
  * the product over tokens takes them.  Entries of CFP_DT_E4M3 stand for themselves times 2^(scale - 127) with a scale
@@ -229,8 +230,9 @@ typedef struct {
  * [n_tokens][n_q] float (or NULL): the logarithm of the sum of the weights.  A row that sees nothing gets zeros and -inf.
  * What a row does not see has no effect on it, whatever it holds.  A row that sees a token of a page outside the
  * cache, and all rows of a sequence longer than its table or with more rows than max_new, become NaN.
- * The weights are rounded to `dtype` as operands of the product with the values, relative to the largest so far;
- * sums, maxima and what is held between parts of a long sequence are in 32 bits. */
+ * The weights are rounded to `dtype` as operands of the product with the values; sums, maxima and what is held between
+ * parts of a long sequence are in 32 bits.  The sums are divided at the end: bfloat16 values beyond 2^80 may leave the
+ * range before. */
 size_t cfp_attend_workspace_bytes(const cfp_attend_desc *a, const cfp_cache_desc *c, const cfp_sequences_desc *s);
 int cfp_attend(const cfp_attend_desc *a, const cfp_cache_desc *c, const cfp_sequences_desc *s, void *out, float *lse, void *ws,
                size_t ws_bytes, void *stream);

@@ -550,7 +550,7 @@ class KVCache:
     k_scale, v_scale [pages][heads][page] uint8: an entry stands for itself times 2^(scale - 127), scales from 1 to 254.  Pages may lie apart (a
     view of a larger tensor), what is in one is contiguous.  page is 16, 32, 64, 128 or 256, dim a multiple of 16 up to 256."""
 
-    __slots__ = ("k", "v", "k_scale", "v_scale", "_desc")
+    __slots__ = ("k", "v", "k_scale", "v_scale", "_desc", "_held", "_heads", "_dim", "_at")
 
     def __init__(self, k, v, k_scale=None, v_scale=None):
         torch = _torch()
@@ -574,6 +574,7 @@ class KVCache:
             strides.append(t.stride(0) if n > 1 else t[0].numel() if n else 0)
         _same_device(k, v, k_scale, v_scale)
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self._held, self._heads, self._dim, self._at = k.dtype, h, d, k.get_device()
         self._desc = _CACHE(n, page, h, d, held[k.dtype], k.data_ptr(), v.data_ptr(), _ptr(k_scale), _ptr(v_scale),
                             *(strides + [0, 0])[:4])
 
@@ -601,7 +602,7 @@ class Sequences:
     ascends; rows outside it belong to no sequence.  max_new: the most rows that a sequence has, or
     more (None: any number); attend lays its work out for it, and for table's width."""
 
-    __slots__ = ("table", "starts", "lengths", "max_new", "_desc")
+    __slots__ = ("table", "starts", "lengths", "max_new", "_desc", "_at")
 
     def __init__(self, table, starts, lengths, *, max_new=None):
         torch = _torch()
@@ -616,7 +617,7 @@ class Sequences:
         _same_device(table, starts, lengths)
         if max_new is not None and max_new < 0:
             raise ValueError("max_new must not be negative")
-        self.table, self.starts, self.lengths, self.max_new = table, starts, lengths, max_new
+        self.table, self.starts, self.lengths, self.max_new, self._at = table, starts, lengths, max_new, table.get_device()
         most = 0x7FFFFFFF if max_new is None else min(max_new, 0x7FFFFFFF)
         self._desc = _SEQUENCES(n, width, table.data_ptr(), _rows("table", table), starts.data_ptr(), lengths.data_ptr(), most)
 
@@ -624,25 +625,30 @@ class Sequences:
         return self.table, self.starts, self.lengths
 
 
-def _paged(torch, cache, seqs, *others):
-    """Checks what the operators over a cache share; returns its device."""
+def _paged(torch, cache, seqs):
+    """Checks what the operators over a cache share."""
     if not isinstance(cache, KVCache):
         raise TypeError("cache must be a KVCache")
     if not isinstance(seqs, Sequences):
         raise TypeError("seqs must be Sequences")
-    at = cache.k.get_device()
-    if seqs.table.get_device() != at or any(t is not None and t.get_device() != at for t in others):
+    if seqs._at != cache._at:
         raise ValueError("all tensors must be on one device")
-    return cache.k.device
 
 
-def _heads(name, t, torch, dim, held):
-    """Checks rows of heads of a cache's dim; `held`: its type."""
+def _rows_fit(t, cache):
+    """Whether t is rows of heads of the cache's dim and a type that it takes, on its device."""
+    return (t.get_device() == cache._at and t.dim() == 3 and t.shape[2] == cache._dim and t.stride(2) == 1 and
+            (t.dtype is cache._held or (cache._held not in _DT and t.dtype in _DT and _DT[t.dtype] != CFP_DT_F32)))
+
+
+def _rows_refuse(name, t, torch, cache):
+    """Raises what is wrong with such rows."""
     _tensor(name, t, torch, (torch.float16, torch.bfloat16), 3)
-    if t.shape[2] != dim or (dim > 1 and t.stride(2) != 1):
+    if t.shape[2] != cache._dim or t.stride(2) != 1:
         raise ValueError(f"{name} must be [T][heads][dim] with the cache's dim, the last dimension contiguous")
-    if held is not torch.float8_e4m3fn and t.dtype is not held:
+    if cache._held in _DT and t.dtype is not cache._held:
         raise TypeError(f"{name} must be of the cache's type")
+    _same_device(cache.k, t)
 
 
 def _no_gradient(torch, name, *inputs):
@@ -665,17 +671,21 @@ def cache_write(cache, k, v, seqs, *, stream=None):
     which no finite entry passes 448, and every entry over it rounded to the nearest; infinities and NaN become NaN.  A token
     whose page is not one of the cache's is not written.  Two rows must not have one place."""
     torch = _torch()
-    device = _paged(torch, cache, seqs, k, v) if isinstance(k, torch.Tensor) and isinstance(v, torch.Tensor) else None
-    held, (_, heads, _, dim) = cache.k.dtype, cache.k.shape
-    _heads("k", k, torch, dim, held)
-    _heads("v", v, torch, dim, held)
-    if k.shape != v.shape or k.shape[1] != heads or k.dtype is not v.dtype:
+    _paged(torch, cache, seqs)
+    for name, t in (("k", k), ("v", v)):
+        if not isinstance(t, torch.Tensor) or not _rows_fit(t, cache):
+            _rows_refuse(name, t, torch, cache)
+            raise ValueError("unsupported arguments")
+    T, heads, _ = k.shape
+    if heads != cache._heads or v.shape != k.shape or v.dtype is not k.dtype:
         raise ValueError("k and v are [T][the cache's heads][dim], of one type")
     _no_gradient(torch, "cache_write", k, v)
-    _used_on(stream, k, v, *cache._tensors(), *seqs._tensors())
+    if stream is not None:
+        _used_on(stream, k, v, *cache._tensors(), *seqs._tensors())
+    (kt, kh, _), (vt, vh, _), device = k.stride(), v.stride(), k.device
     with _on(torch, device, stream):
-        rc = _lib.cfp_cache_write(cache._desc, seqs._desc, k.shape[0], _DT[k.dtype], k.data_ptr(), k.stride(0), k.stride(1),
-                                  v.data_ptr(), v.stride(0), v.stride(1), _raw(torch, device))
+        rc = _lib.cfp_cache_write(cache._desc, seqs._desc, T, _DT[k.dtype], k.data_ptr(), kt, kh, v.data_ptr(), vt, vh,
+                                  _raw(torch, device))
     if rc:
         _check("cfp_cache_write", rc)
 
@@ -686,15 +696,15 @@ def cache_read(cache, seqs, n_tokens, *, dtype=None, out=None, stream=None):
     whole sequences.  A token whose page is not one of the cache's reads as NaN.  Rows of no sequence are left as they
     are: unspecified, or with out=(k, v) what these held."""
     torch = _torch()
-    device = _paged(torch, cache, seqs)
-    held, (_, heads, _, dim) = cache.k.dtype, cache.k.shape
+    _paged(torch, cache, seqs)
+    held, device = cache._held, cache.k.device
     if dtype is None:
-        dtype = torch.bfloat16 if held is torch.float8_e4m3fn else held
-    if dtype not in (torch.float16, torch.bfloat16) or (held is not torch.float8_e4m3fn and dtype is not held):
+        dtype = held if held in _DT else torch.bfloat16
+    if dtype is not held and (held in _DT or dtype not in (torch.float16, torch.bfloat16)):
         raise TypeError("dtype must be the cache's, or float16 or bfloat16 of float8_e4m3fn")
     if n_tokens < 0:
         raise ValueError("n_tokens must not be negative")
-    shape = (n_tokens, heads, dim)
+    shape = (n_tokens, cache._heads, cache._dim)
     if out is not None:
         for name, t in zip(("k", "v"), out, strict=True):
             _tensor(name, t, torch, (dtype,), 3)
@@ -702,7 +712,8 @@ def cache_read(cache, seqs, n_tokens, *, dtype=None, out=None, stream=None):
                 raise ValueError("out must be contiguous [n_tokens][heads][dim]")
         _same_device(cache.k, *out)
         _used_on(stream, *out)
-    _used_on(stream, *cache._tensors(), *seqs._tensors())
+    if stream is not None:
+        _used_on(stream, *cache._tensors(), *seqs._tensors())
     with _on(torch, device, stream):
         k, v = out if out is not None else (torch.empty(shape, dtype=dtype, device=device) for _ in range(2))
         rc = _lib.cfp_cache_read(cache._desc, seqs._desc, n_tokens, _DT[dtype], k.data_ptr(), v.data_ptr(), _raw(torch, device))
@@ -723,15 +734,17 @@ def attend(q, cache, seqs, *, scale=None, causal=True, window=0, with_lse=False,
     longer than its table and one with more rows than max_new get NaN.  Rows of no sequence are left as they are: unspecified,
     or what `out` (or out=(y, lse) with `with_lse`) held."""
     torch = _torch()
-    device = _paged(torch, cache, seqs, q) if isinstance(q, torch.Tensor) else None
-    held, (_, heads, _, dim) = cache.k.dtype, cache.k.shape
-    _heads("q", q, torch, dim, held)
-    if heads == 0 or q.shape[1] == 0 or q.shape[1] % heads:
+    _paged(torch, cache, seqs)
+    if not isinstance(q, torch.Tensor) or not _rows_fit(q, cache):
+        _rows_refuse("q", q, torch, cache)
+        raise ValueError("unsupported arguments")
+    T, hq, dim = q.shape
+    if hq == 0 or cache._heads == 0 or hq % cache._heads:
         raise ValueError("q's heads must be a multiple of the cache's")
     if scale is None:
         scale = dim ** -0.5
     _no_gradient(torch, "attend", q)
-    T, hq = q.shape[:2]
+    device = q.device
     y, lse = out if with_lse and out is not None else (out, None)
     if out is not None:
         _tensor("out", y, torch, (q.dtype,), 3)
@@ -743,9 +756,11 @@ def attend(q, cache, seqs, *, scale=None, causal=True, window=0, with_lse=False,
                 raise ValueError("lse must be contiguous [T][heads]")
         _same_device(q, y, lse)
         _used_on(stream, y, lse)
-    d = _ATTEND(T, hq, _DT[q.dtype], q.data_ptr(), q.stride(0), q.stride(1), scale, 1 if causal else 0,
+    tok, head, _ = q.stride()
+    d = _ATTEND(T, hq, _DT[q.dtype], q.data_ptr(), tok, head, scale, 1 if causal else 0,
                 window if 0 <= window < 1 << 31 else -1 if window < 0 else 0x7FFFFFFF)
-    _used_on(stream, q, ws, *cache._tensors(), *seqs._tensors())
+    if stream is not None:
+        _used_on(stream, q, ws, *cache._tensors(), *seqs._tensors())
     with _on(torch, device, stream):
         if out is None:
             y = torch.empty(q.shape, dtype=q.dtype, device=device)

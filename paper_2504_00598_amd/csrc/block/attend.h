@@ -151,11 +151,12 @@ __device__ __forceinline__ uint32_t few_parts(const AttendArgs &A, const Seq &q,
   return f.lost ? 1u : f.few ? max((uint32_t)((f.tokens + per - 1) / per), 1u) : 0u;
 }
 __device__ __forceinline__ int few_share(const AttendArgs &A, float tokens) {
-  const int per = (int)ceilf(tokens * 1.001f / (float)A.few_target);
+  const int per = (int)fminf(ceilf(tokens * 1.002f / (float)A.few_target), 0x1p30f);  // no sequence is longer
   return __builtin_amdgcn_readfirstlane(max((per + kFewStep - 1) & ~(kFewStep - 1), A.few_least));
 }
-// All 64 lanes of a wave call it.  The sum is in 32-bit floats: the share is taken a little larger than it says, so that there
-// are never more than few_target parts beside each sequence's last.
+// All 64 lanes of a wave call it.  The sum, of up to 2^20 sequences by 64 lanes, is in 32-bit floats and so at most 0.1% too
+// small: the share is taken that much larger, so that there are never more than few_target parts beside each
+// sequence's last.
 __device__ __forceinline__ int few_per(const AttendArgs &A) {
   float sum = 0.f;
   for (int first = 0; first < A.s.n_seqs; first += 64) {

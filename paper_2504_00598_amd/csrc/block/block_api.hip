@@ -111,7 +111,7 @@ int check_cache(const cfp_cache_desc *c) {
 
 int check_sequences(const cfp_sequences_desc *s, const cfp_cache_desc &c, int64_t n_tokens) {
   if (!s || s->n_seqs < 0 || s->width < 0 || n_tokens < 0 || s->max_new < 0) return CFP_ERR_ARG;
-  if (n_tokens >= kMaxTokens || n_tokens * c.heads >= kMaxTokens || (int64_t)s->n_seqs * c.heads >= kMaxTokens / 16 ||
+  if (n_tokens >= kMaxTokens || n_tokens * c.heads >= kMaxTokens || s->n_seqs > CFP_MAX_SEQUENCES || (int64_t)s->n_seqs * c.heads >= kMaxTokens / 16 ||
       (int64_t)s->width * c.page >= (int64_t)1 << 30)
     return CFP_ERR_UNSUPPORTED;
   if (s->n_seqs > 0 && n_tokens > 0 &&
