@@ -21,18 +21,21 @@ void parts_of(const cfp_attend_desc &a, const cfp_cache_desc &c, const cfp_seque
   A.tiles = 0, A.many_parts = 1;
   if (new_rows > A.few_rows) {
     A.tiles = (uint32_t)std::min<int64_t>(a.n_tokens * g / A.many_rows + s.n_seqs, (a.n_tokens * g + A.few_rows) / (A.few_rows + 1));
-    // Time in tiles: rounds of the chip (a workgroup a compute unit; a sixteenth more is not counted as a round) times a
+    // Time in tiles: rounds of the chip (a workgroup a compute unit; sixteen more are not counted as a round) times a
     // part's tiles and about five that a workgroup takes before its first and behind its last; a launch more joins the
-    // parts (three).  The sequences are taken to be alike.
+    // parts (three).  The sequences are taken to be alike; as they may not be, one part stays where others save little.
     const int64_t each = a.n_tokens * g / s.n_seqs;
     const int64_t groups = c.heads * (each > A.few_rows ? s.n_seqs * ((each + A.many_rows - 1) / A.many_rows)
                                                         : (a.n_tokens * g + A.many_rows - 1) / A.many_rows);
     const int64_t most_tiles = (most_len + kManyStep - 1) / kManyStep;
     int64_t least = 0;
-    for (int parts = 1; parts <= 16 && (parts == 1 || most_tiles * kManyStep >= (int64_t)parts * kManyLeast); ++parts) {
-      const int64_t rounds = (groups * parts * 15 / 16 + 255) / 256;
+    for (int parts = 1; parts <= 64 && (parts == 1 || most_tiles * kManyStep >= (int64_t)parts * kManyLeast); ++parts) {
+      const int64_t rounds = (std::max<int64_t>(groups * parts - 16, 1) + 255) / 256;
       const int64_t time = rounds * ((most_tiles + parts - 1) / parts + 5) + (parts > 1 ? 3 : 0);
-      if (parts == 1 || time < least) least = time, A.many_parts = parts;
+      if (parts == 1)
+        least = time * 7 / 8;
+      else if (time < least)
+        least = time, A.many_parts = parts;
     }
   }
 }
