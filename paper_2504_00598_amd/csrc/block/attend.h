@@ -15,6 +15,18 @@
 //
 // What is masked is left out by a choice, not by arithmetic: scores become -inf, and where a tile that some row sees in part
 // holds values that are not finite, these are taken out of the product and added to the rows that see them.
+//
+// Single tokens do 2 (query heads a key head) operations a byte and are bound by memory; chunks by the matrix units, beside
+// which the exponentials take as long: 32 x 32 scores at dim 128 are 512 cycles of products and about 450 of vector work a SIMD.
+// Measured, 32 or 40 query heads over 8, dim 128 (a copy of 1 GiB reaches 5.1 TB/s, a product of 8192 1.4 PFLOP/s):
+//     64 sequences of 16 to 16384 tokens, one new each, bfloat16: 392 us, 5.5 TB/s; 32 of 4000 to 12000 in 8 bits: 103 us,
+//     5.1 TB/s; one of 777 in 13 us, of which the dependent loads (starts, table, keys) are most;
+//     8192 new of 32768 tokens, bfloat16: 3640 us, 1.06 PFLOP/s; 2048 of 8192 in 8 bits: 361 us, 0.68 PFLOP/s.
+// The chunk's kernel keeps the matrix unit busy 49% of its cycles at about 2.1 GHz.  What it was before, for the first of these
+// chunks: 128 rows a workgroup, two of them a compute unit, tiles through registers 6800 us; 64 rows a wave so that
+// an operand read from LDS serves two products, one wave a SIMD, with copies straight to LDS one tile ahead 8500, two ahead 4950, the
+// pages of a tile chosen by masks and not by an index 4060, the first operands of a stage read in the one before it 3860;
+// eight waves of 32 rows, two a SIMD, which hide each other's waits, 3640.
 #pragma once
 
 #include <algorithm>
@@ -396,7 +408,8 @@ __device__ __forceinline__ void write_few(const AttendArgs &A, const float *shar
 // ---- up to 16 rows, as a token's heads that share a key head are: like the kernel for up to 32 below, with 16x16x32 products of
 // 16 tokens and 16 rows and 64 tokens a wave at a time.  Row i of product u is token 16 (i / 4) + 4 u + i % 4, so lane l has
 // scores of tokens 16 (l / 16) .. + 15 of row l % 16, which are its share of the two products with the values.  Half the
-// registers of the wider products, so twice the bytes are on their way, and half the exponentials.
+// registers of the wider products, so twice the bytes are on their way, and half the exponentials (64 uneven contexts:
+// 516 us with the wider ones, 32 in 8 bits 170).
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 template <typename T>
 __device__ __forceinline__ f32x4 mfma16(vec<T, 8> a, vec<T, 8> b, f32x4 c) {
@@ -437,7 +450,7 @@ __global__ __launch_bounds__(64 * kTokenWaves, DP <= 128 ? 2 : 1) void attend_to
   Seq sq;
   if (unit >= (uint32_t)A.few_units || !find_few(A, unit, b, part, sq, per)) return;
   const Few few = few_of(A, sq);
-  const int g = A.group, hq = A.heads * g, D = A.dim;
+  const int g = A.group, D = A.dim;
   if (few.lost) return write_lost<T, kStep>(A, sq, head);
   const int rows = sq.n * g, len = sq.pos + sq.n;
   const bool whole = few.tokens <= per;
@@ -658,7 +671,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_few_kernel(Atte
   Seq sq;
   if (unit >= (uint32_t)A.few_units || !find_few(A, unit, b, part, sq, per)) return;
   const Few few = few_of(A, sq);
-  const int g = A.group, hq = A.heads * g, D = A.dim;
+  const int g = A.group, D = A.dim;
   if (few.lost) return write_lost<T, 256>(A, sq, head);
   const int rows = sq.n * g, len = sq.pos + sq.n;
   const bool whole = few.tokens <= per;
@@ -823,8 +836,10 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_few_kernel(Atte
   write_few<T, 4, kFewRows, kLd>(A, shared, ml, sq, head, rows, whole, (int64_t)id * A.few_rows);
 }
 
-// ---- many rows: a workgroup takes 128 rows of one sequence and key head, 32 a wave, over tiles of 64 tokens whose keys
-// and values lie in LDS (two tiles, so that the next one's lands while this one is worked on).
+// ---- many rows of heads over 128: a workgroup takes 128 rows of one sequence and key head, 32 a wave, over tiles of 64
+// tokens whose keys and values lie in LDS (two tiles, so that the next one's lands while this one is worked on).  Their
+// rings would not fit LDS as the kernel below holds them.  4096 tokens of 32 heads over 8: 0.45 PFLOP/s at dim 192, 0.42 at
+// 256, where one wave a SIMD has nothing to do while it waits.
 template <typename T, bool BYTES, int DP>
 __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many_kernel(AttendArgs A) {
   typedef std::conditional_t<BYTES, uint8_t, T> H;
@@ -1040,11 +1055,11 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many_kernel(Att
   }
 }
 
-// ---- many rows of heads up to 128: a workgroup takes 256 rows, 64 a wave in two columns of 32, so that every operand read
-// from LDS serves two products; one wave a SIMD, with its 512 registers.  Tiles of 64 tokens are copied straight into
-// rings in LDS, two tiles ahead of their use (8 bits: as they are, and widened from there into rings of T).  The work
-// on a half tile i is three stages of three halves at a time, which do not wait for each other: scores of i + 1, weights of i,
-// the product of i - 1 with its values; so the matrix unit works while the vector unit takes exponentials.
+// ---- many rows of heads up to 128: a workgroup of eight waves takes 256 rows, 32 a wave, two waves a SIMD.  Tiles of 64
+// tokens are copied straight into rings in LDS, two tiles ahead of their use (8 bits: as they are, and widened from
+// there into rings of T).  The work on a half tile i is three stages of three halves at a time, which do not wait for
+// each other: scores of i + 1, weights of i, the product of i - 1 with its values; so the matrix unit works while the vector unit
+// takes exponentials.  One workgroup fills a compute unit: 130 KB of LDS (8 bits: 152) and all registers.
 
 // Copies of 16 bytes a lane from memory to LDS: lane l's land at `to` + 16 l, `to` the same for all lanes.  Instructions of
 // their own, as the compiler would wait for every copy before each read of LDS; nothing else in the kernel uses
@@ -1078,7 +1093,7 @@ __device__ __forceinline__ void add_product(f32x16 &c, vec<T, 8> a, vec<T, 8> b)
   else
     asm volatile("v_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
 }
-// Scores: s = a q, or with the products before them.  They are read by the vector unit after two more products of 8 passes
+// Scores: s = a q, or with the products before them.  The vector unit reads them after one more product and apart(), 8 cycles
 // each (11 are asked for).
 template <typename T>
 __device__ __forceinline__ void score_product(f32x16 &s, vec<T, 8> a, vec<T, 8> q, bool first) {
@@ -1103,12 +1118,7 @@ __device__ __forceinline__ void settle_products(f32x16 (&o)[N]) {
 }
 // Between a product and one that adds to its result, or (behind one more product) what reads it.
 __device__ __forceinline__ void apart() { asm volatile("s_nop 7" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void settle_scores(f32x16 (&s)[N]) {
-  asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
-#pragma unroll
-  for (int i = 0; i < N; ++i) asm volatile("" : "+v"(s[i]));
-}
+__device__ __forceinline__ void settle_scores(f32x16 &s) { asm volatile("s_nop 15\n\ts_nop 15" : "+v"(s)::"memory"); }
 template <int N>
 __device__ __forceinline__ void before_products(f32x16 (&o)[N]) {
 #pragma unroll
@@ -1149,13 +1159,13 @@ __device__ __forceinline__ int value_place(int d, int c) { return c ^ (d >> 1 & 
 // scales; the bits of take_odd.
 template <typename T, bool BYTES, int DP>
 struct Wide {
-  static constexpr int kCols = 1, kWaves = 8 / kCols;                 // columns of 32 rows of a wave; waves
+  static constexpr int kWaves = kWideRows / 32;                       // of 32 rows
   static constexpr int kRing = BYTES ? 3 : 4, kLead = BYTES ? 4 : 3;  // tiles; how far ahead of its use a tile of keys is copied
   static constexpr int kTile = 64 * DP;                               // entries
   static constexpr int kRaw = BYTES ? (DP + 63) / 64 : 0;             // copies of a wave for a tile as it is, of keys and of values
-  static constexpr int kCopies = (BYTES ? kRaw : DP / 32) * (kWaves == 8 ? 1 : 2) + (BYTES ? 1 : 0);  // of a wave for a tile of keys and one of values
+  static constexpr int kCopies = BYTES ? kRaw + 1 : DP / 32;          // of a wave for a tile of keys or of values, and scales
   static constexpr uint32_t kKeys = 0, kValues = kRing * kTile * 2, kRawKeys = 2 * kValues, kRawValues = kRawKeys + 3 * kRaw * 4096,
-                            kScales = kRawValues + 3 * kRaw * 4096, kOdds = kScales + (BYTES ? 3 * 1024 : 0),
+                            kScales = kRawValues + 3 * kRaw * 4096, kOdds = kScales + (BYTES ? 3 * 2048 : 0),
                             kOddAt = kOdds + DP * 16, kBytes = kOddAt + 16;
 };
 
@@ -1164,7 +1174,7 @@ __global__ __launch_bounds__(64 * (Wide<T, BYTES, DP>::kWaves), (Wide<T, BYTES, 
   typedef std::conditional_t<BYTES, uint8_t, T> H;
   typedef vec<T, 8> Vec8;
   typedef Wide<T, BYTES, DP> W;
-  constexpr int kMt = DP / 32, kC = DP / 16, kTile = W::kTile, kLead = W::kLead, kX = W::kCols, kThreads = 64 * W::kWaves;
+  constexpr int kMt = DP / 32, kC = DP / 16, kTile = W::kTile, kLead = W::kLead, kThreads = 64 * W::kWaves;
   extern __shared__ __align__(1024) char shared_bytes[];
   const T *keys = reinterpret_cast<const T *>(shared_bytes + W::kKeys);
   T *values = reinterpret_cast<T *>(shared_bytes + W::kValues);
@@ -1195,24 +1205,21 @@ __global__ __launch_bounds__(64 * (Wide<T, BYTES, DP>::kWaves), (Wide<T, BYTES, 
   const int begin = sp.begin + part * sp.per, end = min(sp.end, begin + sp.per);
   const int n = end > begin ? (end - begin + 63) / 64 : 0;  // tiles
   const int all_hi = A.causal ? p0 : len - 1, all_lo = A.window > 0 ? p1 - A.window + 1 : 0;
-  const bool active = r0 + wave * 32 * kX < rows;  // of the wave
+  const bool active = r0 + wave * 32 < rows;  // of the wave
 
-  Vec8 q[kX][kC];
-  int hi[kX], lo[kX];
+  Vec8 q[kC];
+  const int r = r0 + wave * 32 + col, i = r / g;
+  const bool mine = r < rows;
+  const int hi = mine ? (A.causal ? sq.pos + i : len - 1) : -1, lo = A.window > 0 ? sq.pos + i - A.window + 1 : 0;
+  const T *qp = reinterpret_cast<const T *>(A.q) + (int64_t)(sq.row + i) * A.qt + (int64_t)(head * g + r % g) * A.qh;
 #pragma unroll
-  for (int x = 0; x < kX; ++x) {
-    const int r = r0 + (wave * kX + x) * 32 + col, i = r / g;
-    const bool mine = r < rows;
-    hi[x] = mine ? (A.causal ? sq.pos + i : len - 1) : -1, lo[x] = A.window > 0 ? sq.pos + i - A.window + 1 : 0;
-    const T *qp = reinterpret_cast<const T *>(A.q) + (int64_t)(sq.row + i) * A.qt + (int64_t)(head * g + r % g) * A.qh;
-#pragma unroll
-    for (int c = 0; c < kC; ++c) q[x][c] = load_q<T>(qp, 16 * c + 8 * h, D, mine, A.wide != 0);
-  }
+  for (int c = 0; c < kC; ++c) q[c] = load_q<T>(qp, 16 * c + 8 * h, D, mine, A.wide != 0);
 
-  // ---- copies.  Of eight waves four copy keys and four values.  Keys: wave w copies tokens 16 w .. + 15, which lie in one page; values: a lane's 16 bytes of every row
-  // that it copies are of the same tokens.  In pages of 64 and more a tile lies in one, and all bases are scalars.
+  // ---- copies.  Four waves copy keys and four values.  Keys: the first copies tokens 0 .. 15 of the tile, the next 16 .. 31, ..,
+  // which lie in one page; values: a lane's 16 bytes of every row that it copies are of the same tokens.  In pages of 64
+  // and more a tile lies in one, and all bases are scalars.
   const int quarter = wave & 3;
-  const bool for_keys = W::kWaves == 4 || wave < 4, for_values = W::kWaves == 4 || wave >= 4;
+  const bool for_keys = wave < 4;
   const int page = 1 << A.s.page_shift, inner = page - 1;
   const bool single = page >= 64;
   typedef Pages4 Pages;
@@ -1236,18 +1243,18 @@ __global__ __launch_bounds__(64 * (Wide<T, BYTES, DP>::kWaves), (Wide<T, BYTES, 
   const H *kbase = reinterpret_cast<const H *>(A.k) + (int64_t)head * page * D;
   const H *vbase = reinterpret_cast<const H *>(A.v) + (int64_t)head * page * D;
   constexpr int kRowPieces = DP / (16 / (int)sizeof(H));  // of 16 bytes, of a row of keys in LDS
-  constexpr int kKeyCopies = BYTES ? W::kRaw : DP / 32, kValueCopies = kKeyCopies;
+  constexpr int kPieces = BYTES ? W::kRaw : DP / 32;      // copies of a wave for a tile
   constexpr bool kRagged = BYTES && DP == 96;             // a wave's keys do not fill its copies
-  uint32_t key_off[kKeyCopies], value_off[kValueCopies];  // bytes from the wave's first token's key (~0: nothing); from the tokens
+  uint32_t off[kPieces];  // bytes from the wave's first token's key (~0: nothing), or from the tokens in the first row of values
   const int value_row = BYTES ? quarter * 16 + lane / 4 : quarter * 8 + lane / 8;
-  const int value_tok = BYTES ? lane % 4 * 16 : 8 * value_place(value_row, lane % 8);
+  auto value_tok = [&](int l) { return BYTES ? l % 4 * 16 : 8 * value_place(quarter * 8 + l / 8, l % 8); };
 #pragma unroll
-  for (int e = 0; e < kKeyCopies; ++e) {
+  for (int e = 0; e < kPieces; ++e) {
     const int m = e * 64 + lane, row = m / kRowPieces;
     const int d = BYTES ? m % kRowPieces * 16 : 8 * key_piece<DP>(16 * quarter + row, m % kRowPieces);
-    key_off[e] = row < 16 && d < D ? (uint32_t)((row * D + d) * sizeof(H)) : ~0u;
     // rows of values behind the last entry are copies of it: what comes of them is not stored
-    value_off[e] = (uint32_t)(((int64_t)min(value_row + e * (BYTES ? 64 : 32), D - 1) * page + value_tok) * sizeof(H));
+    off[e] = for_keys ? (row < 16 && d < D ? (uint32_t)((row * D + d) * sizeof(H)) : ~0u)
+                      : (uint32_t)(((int64_t)min(value_row + e * (BYTES ? 64 : 32), D - 1) * page + value_tok(lane)) * sizeof(H));
   }
   auto copy_keys = [&](int j, const Pages &pg) {
     const int t = begin + 64 * j + 16 * quarter;
@@ -1255,11 +1262,11 @@ __global__ __launch_bounds__(64 * (Wide<T, BYTES, DP>::kWaves), (Wide<T, BYTES, 
     const uint32_t to = BYTES ? W::kRawKeys + (j % 3) * W::kRaw * 4096 + quarter * W::kRaw * 1024 : W::kKeys + slot(j) * kTile * 2 + quarter * 32 * DP;
     if (D == DP && !kRagged) {
 #pragma unroll
-      for (int e = 0; e < kKeyCopies; ++e) copy_piece(base, key_off[e], to + e * 1024);
+      for (int e = 0; e < kPieces; ++e) copy_piece(base, off[e], to + e * 1024);
     } else {
 #pragma unroll
-      for (int e = 0; e < kKeyCopies; ++e)
-        if (key_off[e] != ~0u) copy_piece(base, key_off[e], to + e * 1024);
+      for (int e = 0; e < kPieces; ++e)
+        if (off[e] != ~0u) copy_piece(base, off[e], to + e * 1024);
     }
   };
   auto copy_values = [&](int j, const Pages &pg) {
@@ -1268,20 +1275,31 @@ __global__ __launch_bounds__(64 * (Wide<T, BYTES, DP>::kWaves), (Wide<T, BYTES, 
     if (single) {
       const H *base = uniform_pointer(vbase + pick(pg, 0) * A.vp + (t & inner));
 #pragma unroll
-      for (int e = 0; e < kValueCopies; ++e) copy_piece(base, value_off[e], to + e * 4096);
+      for (int e = 0; e < kPieces; ++e) copy_piece(base, off[e], to + e * 4096);
     } else {
-      const int at = value_tok & ~15;  // value_off counts from the tile's first token
+      int l = lane;
+      asm volatile("" : "+v"(l));  // computed here: a register kept for it is one too many, and its reload would wait for all copies
+      const int at = value_tok(l) & ~15;  // off counts from the tile's first token
       const char *from = reinterpret_cast<const char *>(vbase + pick(pg, at >> 4) * A.vp + (((t + at) & inner) - at));
 #pragma unroll
-      for (int e = 0; e < kValueCopies; ++e) copy_piece(from + value_off[e], to + e * 4096);
+      for (int e = 0; e < kPieces; ++e) copy_piece(from + off[e], to + e * 4096);
     }
   };
-  // 8 bits: scales of the keys of a tile and of the values of the one before it, 64 bytes each (every wave copies all)
+  // 8 bits: scales of the keys of a tile and of the values of the one before it, 64 bytes of either (and again every 64, by every
+  // wave of four)
   auto copy_scales = [&](int j, const Pages &pk, const Pages &pv) {
-    const int gr = lane & 3;
-    const int64_t in = head * page + ((begin + 64 * j + 16 * gr) & inner), before = head * page + ((begin + 64 * (j - 1) + 16 * gr) & inner);
-    const uint8_t *from = lane & 4 ? A.vs + pick(pv, gr) * A.vsp + before : A.ks + pick(pk, gr) * A.ksp + in;
-    copy_piece(from, W::kScales + (j % 3) * 1024);
+    const Pages pg = for_keys ? pk : pv;
+    const uint8_t *base = (for_keys ? A.ks : A.vs) + head * page;
+    const int64_t step = for_keys ? A.ksp : A.vsp;
+    const int t = begin + 64 * (for_keys ? j : j - 1);
+    const uint32_t to = W::kScales + (j % 3) * 2048 + (for_keys ? 0 : 1024);
+    int l = lane;
+    asm volatile("" : "+v"(l));  // as above
+    const int gr = l & 3;
+    if (single)
+      copy_piece(uniform_pointer(base + pick(pg, 0) * step + (t & inner)), 16 * gr, to);
+    else
+      copy_piece(base + pick(pg, gr) * step + ((t + 16 * gr) & inner), to);
   };
   // 8 bits: a copied tile to the rings
   auto widen_keys = [&](int j) {
@@ -1291,7 +1309,7 @@ __global__ __launch_bounds__(64 * (Wide<T, BYTES, DP>::kWaves), (Wide<T, BYTES, 
         const int w = m / (W::kRaw * 64), i = m % (W::kRaw * 64), row = 16 * w + i / kRowPieces, c = i % kRowPieces * 2;
         if (i >= 16 * kRowPieces || 8 * c >= D) continue;
         const u32x4 x = *reinterpret_cast<const u32x4 *>(shared_bytes + W::kRawKeys + (j % 3) * W::kRaw * 4096 + m * 16);
-        const float by = scale_of((uint8_t)shared_bytes[W::kScales + (j % 3) * 1024 + row]);
+        const float by = scale_of((uint8_t)shared_bytes[W::kScales + (j % 3) * 2048 + row]);
         T *to = const_cast<T *>(keys) + slot(j) * kTile + row * DP;
         *reinterpret_cast<Vec8 *>(to + 8 * key_place<DP>(row, c)) = widen<T>(u32x2{x[0], x[1]}, by);
         *reinterpret_cast<Vec8 *>(to + 8 * key_place<DP>(row, c + 1)) = widen<T>(u32x2{x[2], x[3]}, by);
@@ -1300,7 +1318,7 @@ __global__ __launch_bounds__(64 * (Wide<T, BYTES, DP>::kWaves), (Wide<T, BYTES, 
   };
   auto widen_values = [&](int j) {
     if constexpr (BYTES) {
-      const u32x4 by = *reinterpret_cast<const u32x4 *>(shared_bytes + W::kScales + ((j + 1) % 3) * 1024 + 64 + tid % 4 * 16);
+      const u32x4 by = *reinterpret_cast<const u32x4 *>(shared_bytes + W::kScales + ((j + 1) % 3) * 2048 + 1024 + tid % 4 * 16);
 #pragma unroll
       for (int m = tid; m < W::kRaw * 256; m += kThreads) {
         const int d = m / 4, c = m % 4 * 2;
@@ -1313,9 +1331,8 @@ __global__ __launch_bounds__(64 * (Wide<T, BYTES, DP>::kWaves), (Wide<T, BYTES, 
     }
   };
 
-  Rows<T, DP> st[kX];
-#pragma unroll
-  for (int x = 0; x < kX; ++x) st[x].clear();
+  Rows<T, DP> st;
+  st.clear();
   const int ki = 16 * (col >> 2 & 1) + 4 * (col >> 3) + (col & 3);
   int koff[kC], voff[4];
 #pragma unroll
@@ -1335,52 +1352,41 @@ __global__ __launch_bounds__(64 * (Wide<T, BYTES, DP>::kWaves), (Wide<T, BYTES, 
 #pragma unroll
     for (int c = 0; c < kAhead; ++c) first_k[c] = key_piece_of(k, ku, c), first_v[c] = value_piece_of(v, vu, c);
   };
-  auto stage = [&](f32x16 (&s)[kX], Vec8 (&p)[kX][2], f32x16 (&next)[kX], const T *k, int ku, const T *v, int vu, const Vec8 (&pp)[kX][2],
+  auto stage = [&](const f32x16 &s, Vec8 (&p)[2], f32x16 &next, const T *k, int ku, const T *v, int vu, const Vec8 (&pp)[2],
                    const T *then_k, int then_ku, const T *then_v, int then_vu) {
-    constexpr int kSlots = 2 * kX * kC, kFirst = 4, kOver = kSlots - kFirst - 2;  // products; the first kFirst share the maxima
+    constexpr int kSlots = 2 * kC, kFirst = 4, kOver = kSlots - kFirst - 2;  // products; the first kFirst share the maxima
     Vec8 ka[kHeld], va[kHeld];
 #pragma unroll
     for (int c = 0; c < kAhead; ++c) ka[c] = first_k[c], va[c] = first_v[c];
-    float top[kX][4], to[kX], by[kX], from[kX], sum[kX] = {}, w[16 * kX];
+    float top[4], to, by, from, sum = 0.f, w[16];
     bool grows = false;
     auto vector_share = [&](int slot) {
       if (slot == 0) {
 #pragma unroll
-        for (int x = 0; x < kX; ++x)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) top[x][i] = max3(s[x][4 * i], s[x][4 * i + 1], s[x][4 * i + 2]);
+        for (int i = 0; i < 4; ++i) top[i] = max3(s[4 * i], s[4 * i + 1], s[4 * i + 2]);
       } else if (slot == 1) {
-#pragma unroll
-        for (int x = 0; x < kX; ++x) {
-          top[x][0] = max3(top[x][0], s[x][3], s[x][7]), top[x][1] = max3(top[x][1], s[x][11], s[x][15]);
-          top[x][0] = max3(top[x][0], top[x][2], top[x][3]);
-        }
+        top[0] = max3(top[0], s[3], s[7]), top[1] = max3(top[1], s[11], s[15]);
+        top[0] = max3(top[0], top[2], top[3]);
       } else if (slot == 2) {
-#pragma unroll
-        for (int x = 0; x < kX; ++x) {
-          const float t = max3(top[x][0], top[x][1], partner(max3(top[x][0], top[x][1], top[x][1]))) * A.scale;
-          const bool more = t > st[x].m + kGrowth<T>;
-          grows = grows || more;
-          to[x] = more ? t - kBelow<T> : st[x].m;
-          from[x] = to[x] == -__builtin_inff() ? 0.f : to[x];
-        }
+        const float t = max3(top[0], top[1], partner(max3(top[0], top[1], top[1]))) * A.scale;
+        const bool more = t > st.m + kGrowth<T>;
+        grows = grows || more;
+        to = more ? t - kBelow<T> : st.m;
+        from = to == -__builtin_inff() ? 0.f : to;
       } else if (slot == 3) {
-#pragma unroll
-        for (int x = 0; x < kX; ++x) {
-          by[x] = to[x] == st[x].m ? 1.f : __builtin_amdgcn_exp2f(st[x].m - to[x]);
-          st[x].m = to[x];
-        }
+        by = to == st.m ? 1.f : __builtin_amdgcn_exp2f(st.m - to);
+        st.m = to;
       }
 #pragma unroll
-      for (int e = 0; e < 16 * kX; ++e) {
-        const int x = e / 16, i = e % 16, at = kFirst + e * kOver / (16 * kX);
+      for (int e = 0; e < 16; ++e) {
+        const int at = kFirst + e * kOver / 16;
         if (slot == at + 2) {
-          sum[x] += w[e];
-          if (i % 2) p[x][i / 8][i % 8 - 1] = (T)w[e - 1], p[x][i / 8][i % 8] = (T)w[e];
-          if (i % 8 == 7) asm volatile("" : "+v"(p[x][i / 8]), "+v"(sum[x]));  // here, not behind the branch at the stage's end
+          sum += w[e];
+          if (e % 2) p[e / 8][e % 8 - 1] = (T)w[e - 1], p[e / 8][e % 8] = (T)w[e];
+          if (e % 8 == 7) asm volatile("" : "+v"(p[e / 8]), "+v"(sum));  // here, not behind the branch at the stage's end
         }
         if (slot == at + 1) w[e] = __builtin_amdgcn_exp2f(w[e]);
-        if (slot == at) w[e] = fmaf(s[x][i], A.scale, -from[x]);
+        if (slot == at) w[e] = fmaf(s[e], A.scale, -from);
       }
     };
 #pragma unroll
@@ -1392,39 +1398,26 @@ __global__ __launch_bounds__(64 * (Wide<T, BYTES, DP>::kWaves), (Wide<T, BYTES, 
         first_k[c + kAhead - kC] = key_piece_of(then_k, then_ku, c + kAhead - kC);
         first_v[c + kAhead - kC] = value_piece_of(then_v, then_vu, c + kAhead - kC);
       }
-#pragma unroll
-      for (int x = 0; x < kX; ++x) {
-        score_product<T>(next[x], ka[c % kHeld], q[x][c], c == 0);
-        vector_share(2 * kX * c + x);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-#pragma unroll
-      for (int x = 0; x < kX; ++x) {
-        add_product<T>(st[x].o[c / 2], va[c % kHeld], pp[x][c % 2]);
-        vector_share(2 * kX * c + kX + x);
-        __builtin_amdgcn_sched_barrier(0);
-      }
+      score_product<T>(next, ka[c % kHeld], q[c], c == 0);
+      vector_share(2 * c);
+      __builtin_amdgcn_sched_barrier(0);
+      add_product<T>(st.o[c / 2], va[c % kHeld], pp[c % 2]);
+      vector_share(2 * c + 1);
+      __builtin_amdgcn_sched_barrier(0);
     }
-#pragma unroll
-    for (int x = 0; x < kX; ++x) st[x].l = st[x].l * by[x] + sum[x];
-    if constexpr (kX == 1) apart();  // one product has followed the last score
+    st.l = st.l * by + sum;
+    apart();  // behind the last score
     if (__any(grows)) {
+      settle_products(st.o);
 #pragma unroll
-      for (int x = 0; x < kX; ++x) {
-        settle_products(st[x].o);
-#pragma unroll
-        for (int mt = 0; mt < kMt; ++mt) times_sums(st[x].o[mt], by[x]);
-        before_products(st[x].o);
-      }
+      for (int mt = 0; mt < kMt; ++mt) times_sums(st.o[mt], by);
+      before_products(st.o);
     }
   };
 
+  before_products(st.o);
 #pragma unroll
-  for (int x = 0; x < kX; ++x) before_products(st[x].o);
-#pragma unroll
-  for (int x = 0; x < kX; ++x)
-#pragma unroll
-    for (int c = 0; c < kC; ++c) asm volatile("" : "+a"(q[x][c]));  // queries stay in accumulation registers too
+  for (int c = 0; c < kC; ++c) asm volatile("" : "+a"(q[c]));  // queries stay in accumulation registers too
   if (n > 0) {
     // zeros where no key's entry is written to, and in the tile of values that stands before the first
     constexpr uint32_t kBefore = W::kValues + (W::kRing - 1) * kTile * 2;
@@ -1442,7 +1435,7 @@ __global__ __launch_bounds__(64 * (Wide<T, BYTES, DP>::kWaves), (Wide<T, BYTES, 
       if constexpr (BYTES) {
         if (j - 1 < n) copy_scales(j, pk, pv);
       }
-      if (for_values && j > 0 && j - 1 < n) copy_values(j - 1, pv);
+      if (!for_keys && j > 0 && j - 1 < n) copy_values(j - 1, pv);
     };
 #pragma unroll
     for (int j = 0; j < 3; ++j) {
@@ -1463,22 +1456,18 @@ __global__ __launch_bounds__(64 * (Wide<T, BYTES, DP>::kWaves), (Wide<T, BYTES, 
       if (5 < n) pn = pages(5);
       bad >>= 4;
     }
-    f32x16 s0[kX], s1[kX];
-    Vec8 pa[kX][2], pb[kX][2];
+    f32x16 s0, s1;
+    Vec8 pa[2], pb[2];
 #pragma unroll
-    for (int x = 0; x < kX; ++x)
+    for (int j = 0; j < 2; ++j)
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) pb[x][j][i] = (T)0.f;
+      for (int i = 0; i < 8; ++i) pb[j][i] = (T)0.f;
     if (active)
 #pragma unroll
-      for (int c = 0; c < kC; ++c)
-#pragma unroll
-        for (int x = 0; x < kX; ++x) {
-          score_product<T>(s0[x], key_piece_of(keys, 0, c), q[x][c], c == 0);
-          apart();
-        }
+      for (int c = 0; c < kC; ++c) {
+        score_product<T>(s0, key_piece_of(keys, 0, c), q[c], c == 0);
+        apart();
+      }
     settle_scores(s0);
     first_pieces(keys, 1, values + (W::kRing - 1) * kTile, 1);
     for (int j = 0; j < n; ++j) {
@@ -1508,31 +1497,26 @@ __global__ __launch_bounds__(64 * (Wide<T, BYTES, DP>::kWaves), (Wide<T, BYTES, 
         }
         __syncthreads();
         if (*odd_at == t + 1) {
+          int d0 = 4 * h;
+          asm volatile("" : "+v"(d0));  // places and bounds of all entries would be kept through the loop
+          const uint32_t sees[2] = {bits_of(hi + 1 - t) & ~bits_of(lo - t), bits_of(hi + 1 - t - 32) & ~bits_of(lo - t - 32)};
 #pragma unroll
-          for (int x = 0; x < kX; ++x) {
-            const uint32_t sees[2] = {bits_of(hi[x] + 1 - t) & ~bits_of(lo[x] - t), bits_of(hi[x] + 1 - t - 32) & ~bits_of(lo[x] - t - 32)};
+          for (int mt = 0; mt < kMt; ++mt)
 #pragma unroll
-            for (int mt = 0; mt < kMt; ++mt)
-#pragma unroll
-              for (int i = 0; i < 16; ++i) {
-                const int d = 32 * mt + 8 * (i / 4) + 4 * h + i % 4;
-                const u32x4 w = *reinterpret_cast<const u32x4 *>(odds + d * 16);
-                st[x].add_odd(mt, i, d < D && ((w[0] & sees[0]) | (w[1] & sees[1])), d < D && ((w[2] & sees[0]) | (w[3] & sees[1])));
-                __builtin_amdgcn_sched_barrier(0);  // one after the other: seldom run, and not worth registers
-              }
-          }
+            for (int i = 0; i < 16; ++i) {
+              const int d = d0 + 32 * mt + 8 * (i / 4) + i % 4;
+              const u32x4 w = *reinterpret_cast<const u32x4 *>(odds + d * 16);
+              st.add_odd(mt, i, d < D && ((w[0] & sees[0]) | (w[1] & sees[1])), d < D && ((w[2] & sees[0]) | (w[3] & sees[1])));
+              __builtin_amdgcn_sched_barrier(0);  // one after the other: seldom run, and not worth registers
+            }
         }
       }
       if (active) {
         const bool edge = partly || (bad & 15);
         const int first = t + 16 * h;
-        if (edge)
-#pragma unroll
-          for (int x = 0; x < kX; ++x) mask16(s0[x], first, lo[x], hi[x], bad >> h & 1);
+        if (edge) mask16(s0, first, lo, hi, bad >> h & 1);
         stage(s0, pa, s1, k0, 1, v1, 1, pb, k1, 0, v0, 0);
-        if (edge)
-#pragma unroll
-          for (int x = 0; x < kX; ++x) mask16(s1[x], first + 32, lo[x], hi[x], bad >> (2 + h) & 1);
+        if (edge) mask16(s1, first + 32, lo, hi, bad >> (2 + h) & 1);
         stage(s1, pb, s0, k1, 0, v0, 0, pa, k1, 1, v0, 1);
       }
       if constexpr (BYTES) {
@@ -1546,46 +1530,39 @@ __global__ __launch_bounds__(64 * (Wide<T, BYTES, DP>::kWaves), (Wide<T, BYTES, 
     if (active) {
       const T *v = values + slot(n - 1) * kTile;
 #pragma unroll
-      for (int m = 0; m < kC; ++m)
-#pragma unroll
-        for (int x = 0; x < kX; ++x) {
-          add_product<T>(st[x].o[m / 2], value_piece_of(v, 1, m), pb[x][m % 2]);
-          apart();
-        }
+      for (int m = 0; m < kC; ++m) {
+        add_product<T>(st.o[m / 2], value_piece_of(v, 1, m), pb[m % 2]);
+        apart();
+      }
     }
   }
   if (!active) return;
+  settle_products(st.o);
+  st.finish();
+  if (r >= rows) return;
+  const int64_t row = (int64_t)(sq.row + i) * hq + head * g + r % g;
+  if (sp.parts <= 1) {
+    const float inv = st.l == 0.f ? 0.f : 1.f / st.l;
+    T *to = reinterpret_cast<T *>(A.out) + row * D + 4 * h;
 #pragma unroll
-  for (int x = 0; x < kX; ++x) settle_products(st[x].o);
+    for (int mt = 0; mt < kMt; ++mt)
 #pragma unroll
-  for (int x = 0; x < kX; ++x) {
-    st[x].finish();
-    const int r = r0 + (wave * kX + x) * 32 + col;
-    if (r >= rows) continue;
-    const int64_t row = (int64_t)(sq.row + r / g) * hq + head * g + r % g;
-    if (sp.parts <= 1) {
-      const float inv = st[x].l == 0.f ? 0.f : 1.f / st[x].l;
-      T *to = reinterpret_cast<T *>(A.out) + row * D + 4 * h;
+      for (int a = 0; a < 4; ++a) {
+        const float y[4] = {st.o[mt][4 * a] * inv, st.o[mt][4 * a + 1] * inv, st.o[mt][4 * a + 2] * inv, st.o[mt][4 * a + 3] * inv};
+        if (32 * mt + 8 * a + 4 * h < D) store_vec<T, 4>(to + 32 * mt + 8 * a, y);
+      }
+    if (h == 0 && A.lse) A.lse[row] = (st.m + __builtin_amdgcn_logf(st.l)) * kLn2F;
+  } else {
+    const int64_t at = part * A.s.n_tokens * hq + row;
+    float *to = A.many_o + at * D + 4 * h;
 #pragma unroll
-      for (int mt = 0; mt < kMt; ++mt)
+    for (int mt = 0; mt < kMt; ++mt)
 #pragma unroll
-        for (int a = 0; a < 4; ++a) {
-          const float y[4] = {st[x].o[mt][4 * a] * inv, st[x].o[mt][4 * a + 1] * inv, st[x].o[mt][4 * a + 2] * inv, st[x].o[mt][4 * a + 3] * inv};
-          if (32 * mt + 8 * a + 4 * h < D) store_vec<T, 4>(to + 32 * mt + 8 * a, y);
-        }
-      if (h == 0 && A.lse) A.lse[row] = (st[x].m + __builtin_amdgcn_logf(st[x].l)) * kLn2F;
-    } else {
-      const int64_t at = part * A.s.n_tokens * hq + row;
-      float *to = A.many_o + at * D + 4 * h;
-#pragma unroll
-      for (int mt = 0; mt < kMt; ++mt)
-#pragma unroll
-        for (int a = 0; a < 4; ++a) {
-          const float y[4] = {st[x].o[mt][4 * a], st[x].o[mt][4 * a + 1], st[x].o[mt][4 * a + 2], st[x].o[mt][4 * a + 3]};
-          if (32 * mt + 8 * a + 4 * h < D) store_vec<float, 4>(to + 32 * mt + 8 * a, y);
-        }
-      if (h == 0) A.many_ml[2 * at] = st[x].m, A.many_ml[2 * at + 1] = st[x].l;
-    }
+      for (int a = 0; a < 4; ++a) {
+        const float y[4] = {st.o[mt][4 * a], st.o[mt][4 * a + 1], st.o[mt][4 * a + 2], st.o[mt][4 * a + 3]};
+        if (32 * mt + 8 * a + 4 * h < D) store_vec<float, 4>(to + 32 * mt + 8 * a, y);
+      }
+    if (h == 0) A.many_ml[2 * at] = st.m, A.many_ml[2 * at + 1] = st.l;
   }
 }
 
