@@ -20,7 +20,8 @@
  * errors are returned as CFP_ERR_* before any HIP call.  16-bit and 32-bit element
  * types are CFP_DT_*; sums are held in 32 bits; a result is rounded to its type once.  The
  * experts' products round operands between them as well, see there.
- * The experts' workspaces and what they keep start on 16 bytes, other workspaces on 4 (CFP_ERR_ARG); tensors on their type.
+ * The experts' workspaces, what they keep and the attention's workspace start on 16 bytes, other workspaces on 4 (CFP_ERR_ARG);
+ * tensors on their type, but a cache's pages, what cfp_cache_read writes and the result of cfp_attend on 16 bytes.
  * Results do not depend on the order in which workgroups run.  A call with no tokens
  * writes what does not depend on them (the plan's offsets, gradients of zero) and returns CFP_OK.
  */

@@ -21,8 +21,8 @@
 // Measured, 32 or 40 query heads over 8, dim 128 (a copy of 1 GiB reaches 5.1 TB/s, a product of 8192 1.4 PFLOP/s):
 //     64 sequences of 16 to 16384 tokens, one new each, bfloat16: 392 us, 5.5 TB/s; 32 of 4000 to 12000 in 8 bits: 103 us,
 //     5.1 TB/s; one of 777 in 13 us, of which the dependent loads (starts, table, keys) are most;
-//     8192 new of 32768 tokens, bfloat16: 3640 us, 1.06 PFLOP/s; 2048 of 8192 in 8 bits: 361 us, 0.68 PFLOP/s.
-// The chunk's kernel keeps the matrix unit busy 49% of its cycles at about 2.1 GHz.  What it was before, for the first of these
+//     8192 new of 32768 tokens, bfloat16: 3640 us, 1.06 PFLOP/s; 2048 of 8192 in 8 bits: 323 us, 0.76 PFLOP/s.
+// The chunk's kernel keeps the matrix unit busy half of its cycles at about 2.1 GHz.  What it was before, for the first of these
 // chunks: 128 rows a workgroup, two of them a compute unit, tiles through registers 6800 us; 64 rows a wave so that
 // an operand read from LDS serves two products, one wave a SIMD, with copies straight to LDS one tile ahead 8500, two ahead 4950, the
 // pages of a tile chosen by masks and not by an index 4060, the first operands of a stage read in the one before it 3860;
