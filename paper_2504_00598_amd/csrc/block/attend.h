@@ -42,6 +42,9 @@ constexpr int kWideRows = 256, kWideDim = 128;
 constexpr int kFewParts = 768;
 constexpr int kFewStep = 64, kManyStep = 64;     // parts start and end on these
 constexpr int kFewLeast = 256, kTokenLeast = 512, kManyLeast = 256;  // tokens of a part, at least
+constexpr int kGroups = 256, kSpare = 16, kManyRounds = 2;  // workgroups at a time; more that are no round; rounds up to which tiles are cut
+constexpr int kUncut = 1 << 30;
+constexpr int kJoinThreads = 256;
 
 struct AttendArgs {
   SeqArgs s;
@@ -57,8 +60,11 @@ struct AttendArgs {
   int32_t few_units, few_target;  // parts of all sequences with few rows: at most, and for their tokens alone
   int32_t few_least;              // tokens of a part, at least
   int32_t few_rows, joined;       // few_rows: of a sequence and key head, at most; joined: there may be parts
-  int32_t many_parts, many_rows;  // many_rows: of a workgroup
-  uint32_t tiles;                 // of many_rows rows, at most
+  int32_t *plan;                  // how the other sequences are cut: tokens of a part, parts of all tiles
+  int32_t many_rows;              // of a workgroup
+  uint32_t tiles, many_units;     // of many_rows rows, and their parts, at most
+  uint32_t many_most;             // parts where tiles are cut, at most; 0: they never are
+  int32_t many_joined;            // workgroups that join those parts
   float scale;     // times log2(e)
 };
 
@@ -128,19 +134,92 @@ __device__ __forceinline__ vec<T, 8> widen(u32x2 w, u32x2 s) {
   return r;
 }
 
-// What rows with first and last token p0 <= p1 of a sequence of `len` see, cut into parts.
+// What rows with first and last token p0 <= p1 of a sequence of `len` see, cut into parts of `per`.
 struct Span {
-  int32_t begin, end, per, parts;
+  int32_t begin, end, parts;
 };
-template <int STEP, int LEAST>
-__device__ __forceinline__ Span span_of(const AttendArgs &A, int p0, int p1, int len, int most) {
+__device__ __forceinline__ Span span_of(const AttendArgs &A, int p0, int p1, int len, int per) {
   Span r;
   r.end = A.causal ? p1 + 1 : len;
-  r.begin = (A.window > 0 ? max(p0 - A.window + 1, 0) : 0) & ~(STEP - 1);
+  r.begin = (A.window > 0 ? max(p0 - A.window + 1, 0) : 0) & ~(kManyStep - 1);
   const int n = r.end - r.begin;
-  r.per = max(((n + most - 1) / most + STEP - 1) & ~(STEP - 1), LEAST);
-  r.parts = n > 0 ? (n + r.per - 1) / r.per : 0;
+  r.parts = n > 0 ? (n + per - 1) / per : 0;
   return r;
+}
+
+// Sequences with many rows: their tiles of rows, the most tokens that one of these sees, into how many parts each is cut.
+__device__ __forceinline__ uint32_t many_tiles(const AttendArgs &A, const Seq &q) {
+  const int64_t r = (int64_t)q.n * A.group;
+  const bool many = r > A.few_rows && q.n <= A.max_new && q.pos + q.n <= (A.s.width << A.s.page_shift);
+  return many ? (uint32_t)((r + A.many_rows - 1) / A.many_rows) : 0u;
+}
+__device__ __forceinline__ int many_span(const AttendArgs &A, const Seq &q) {
+  const int len = q.pos + q.n;
+  return A.causal && A.window > 0 ? min(len, A.window + A.many_rows / A.group + kManyStep + 1) : len;
+}
+__device__ __forceinline__ uint32_t many_parts(const AttendArgs &A, const Seq &q, int per) {
+  return (uint32_t)max((many_span(A, q) + per - 1) / per, 1);
+}
+__device__ __forceinline__ uint32_t many_units(const AttendArgs &A, const Seq &q, int per) {
+  const uint32_t tiles = many_tiles(A, q);
+  return tiles ? tiles * many_parts(A, q, per) : 0u;
+}
+// One wave of the first kernel cuts them for the ones that follow: into parts of the same length, so that workgroups have equal work, no
+// more of them than fill the rounds that the tiles take anyhow.  A workgroup fills a compute unit; its time is its 64-token
+// steps and about five that it takes before the first and behind the last; a launch more joins the parts (three).  Whole tiles in more
+// than one round take their mean time, and half of the longest's as the last ones end.  The tiles stay whole
+// where parts save less than an eighth, and where they take more than two rounds.  (A chunk of 108 rows in two tiles of 8 heads over
+// 12009 tokens of dim 192, beside six single tokens: cut by bounds that the host knows, as if these might be chunks too, 210 us.)
+__device__ __forceinline__ void plan_many(const AttendArgs &A) {
+  const int lane = threadIdx.x & 63;
+  float work = 0.f;
+  uint32_t tiles = 0;
+  int longest = 0;
+  Seq q = {0, 0, 0};  // up to 64 sequences are read once
+  for (int first = 0; first < A.s.n_seqs; first += 64) {
+    q = {0, 0, 0};
+    if (first + lane < A.s.n_seqs) q = seq_of(A.s, first + lane);
+    const uint32_t t = many_tiles(A, q);
+    const int span = t ? many_span(A, q) : 0;
+    // of a chunk that sees itself as a triangle half of it
+    work += (float)t * (float)(A.causal ? max(span - q.n / 2, span / 2) : span), tiles += t, longest = max(longest, span);
+  }
+  work = group_sum<64>(work);
+  tiles = (uint32_t)__builtin_amdgcn_readlane((int)lanes_before(tiles), 63);
+  for (int m = 32; m > 0; m /= 2) longest = max(longest, __shfl_xor(longest, m));
+  int per = kUncut;
+  uint32_t units = tiles;
+  const int64_t rounds = (max((int64_t)tiles * A.heads - kSpare, (int64_t)1) + kGroups - 1) / kGroups;
+  const uint32_t most = min((uint32_t)(rounds * kGroups / A.heads), A.many_most);
+  if (tiles && most && rounds <= kManyRounds) {
+    auto step = [](int n) { return (n + kManyStep - 1) & ~(kManyStep - 1); };
+    const float steps = (float)longest / kManyStep + 5.f;
+    const float whole = rounds == 1 ? steps : (work / kManyStep + 5.f * (float)tiles) * (float)A.heads / kGroups + steps / 2;
+    int p = max(max(step((int)fminf(work / (float)most, 0x1p29f) + 1), step(longest / 64)), kManyLeast);
+    for (;; p += max(p / 32 & ~(kManyStep - 1), kManyStep)) {
+      p = __builtin_amdgcn_readfirstlane(p);
+      if ((float)rounds * ((float)p / kManyStep + 5.f) + 3.f >= whole * 7 / 8) break;  // and so for all that are longer
+      uint32_t u = 0;
+      if (A.s.n_seqs <= 64)
+        u = many_units(A, q, p);
+      else
+        for (int first = 0; first < A.s.n_seqs; first += 64)
+          if (first + lane < A.s.n_seqs) u += many_units(A, seq_of(A.s, first + lane), p);
+      u = (uint32_t)__builtin_amdgcn_readlane((int)lanes_before(u), 63);
+      if (u > most) continue;
+      per = p, units = u;
+      break;
+    }
+  }
+  if (lane == 0) A.plan[0] = per, A.plan[1] = (int32_t)units;
+}
+// What it wrote, in kernels behind that one.
+struct Plan {
+  int32_t per, units;
+};
+__device__ __forceinline__ Plan plan_of(const AttendArgs &A) {
+  const const_i32 *p = reinterpret_cast<const const_i32 *>(reinterpret_cast<uintptr_t>(A.plan));
+  return {p[0], p[1]};
 }
 
 // Sequences with few rows are cut into parts of `per` tokens, the same for all, so that workgroups have equal work.
@@ -448,6 +527,7 @@ __global__ __launch_bounds__(64 * kTokenWaves, DP <= 128 ? 2 : 1) void attend_to
   int b, per;
   uint32_t part;
   Seq sq;
+  if (A.tiles && id == (uint32_t)A.few_units * A.heads - 1 && wave == 0) plan_many(A);
   if (unit >= (uint32_t)A.few_units || !find_few(A, unit, b, part, sq, per)) return;
   const Few few = few_of(A, sq);
   const int g = A.group, D = A.dim;
@@ -669,6 +749,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_few_kernel(Atte
   int b, per;
   uint32_t part;
   Seq sq;
+  if (A.tiles && id == (uint32_t)A.few_units * A.heads - 1 && wave == 0) plan_many(A);
   if (unit >= (uint32_t)A.few_units || !find_few(A, unit, b, part, sq, per)) return;
   const Few few = few_of(A, sq);
   const int g = A.group, D = A.dim;
@@ -841,7 +922,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_few_kernel(Atte
 // rings would not fit LDS as the kernel below holds them.  4096 tokens of 32 heads over 8: 0.45 PFLOP/s at dim 192, 0.42 at
 // 256, where one wave a SIMD has nothing to do while it waits.
 template <typename T, bool BYTES, int DP>
-__global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many_kernel(AttendArgs A) {
+__global__ __launch_bounds__(256, 1) void attend_many_kernel(AttendArgs A) {
   typedef std::conditional_t<BYTES, uint8_t, T> H;
   // rows of LDS are 16 bytes longer than their entries: then 16 lanes that read one piece of 16 rows meet all banks
   constexpr int kKLd = DP + 8, kVLd = kManyStep + 8;
@@ -855,26 +936,24 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many_kernel(Att
   uint8_t *odds = reinterpret_cast<uint8_t *>(lds + 2 * kTile);
   volatile int *odd_at = reinterpret_cast<volatile int *>(odds + 2 * DP * 16);
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, h = lane >> 5;
-  uint32_t id = block_id();
+  const uint32_t id = block_id();
   const int head = (int)(id % A.heads);
-  id /= A.heads;
-  const int part = (int)(id % A.many_parts);
-  id /= A.many_parts;
-  if (id >= A.tiles) return;
+  const Plan plan = plan_of(A);
+  // The last tiles of a chunk see the most and come first, but for workgroups with no unit, which end at once: behind
+  // the others they would wait for a compute unit each (2048 rows of 4 in 8 bits over 8192 tokens: 369 us, so 358).
+  const uint32_t unit = A.many_units - 1u - id / A.heads;
   int b;
   uint32_t tile;
   Seq sq;
   const int g = A.group, hq = A.heads * g, D = A.dim;
-  if (!find_unit(A.s, A.tiles - 1 - id, [&](const Seq &s) {
-        const int64_t r = (int64_t)s.n * g;
-        return r > A.few_rows && s.n <= A.max_new ? (uint32_t)((r + kManyRows - 1) / kManyRows) : 0u;
-      }, b, tile, sq))
-    return;
+  if (!find_unit(A.s, unit, [&](const Seq &s) { return many_units(A, s, plan.per); }, b, tile, sq)) return;
+  const uint32_t parts = many_parts(A, sq, plan.per);
+  const int part = (int)(tile % parts);
+  tile /= parts;
   const int len = sq.pos + sq.n, rows = sq.n * g;
-  if (len > (A.s.width << A.s.page_shift)) return;  // the kernel for few writes what such rows become
   const int r0 = (int)tile * kManyRows, r1 = min(r0 + kManyRows, rows);
   const int p0 = sq.pos + r0 / g, p1 = sq.pos + (r1 - 1) / g;
-  const Span sp = span_of<kManyStep, kManyLeast>(A, p0, p1, len, A.many_parts);
+  const Span sp = span_of(A, p0, p1, len, plan.per);
   if (part >= max(sp.parts, 1)) return;
   const int r = r0 + wave * 32 + col;
   const bool mine = r < rows;
@@ -966,8 +1045,8 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many_kernel(Att
 
   Rows<T, DP> st;
   st.clear();
-  int t = sp.begin + part * sp.per;
-  const int end = min(sp.end, t + sp.per);
+  int t = sp.begin + part * plan.per;
+  const int end = min(sp.end, t + plan.per);
   if (t < end) {
     if (tid < 2) odd_at[tid] = 0;
     if (D < DP)  // what no entry is written to is zero
@@ -1042,7 +1121,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many_kernel(Att
       }
     if (h == 0 && A.lse) A.lse[row] = (st.m + __builtin_amdgcn_logf(st.l)) * kLn2F;
   } else {
-    const int64_t at = part * A.s.n_tokens * hq + row;
+    const int64_t at = ((int64_t)unit * A.heads + head) * A.many_rows + r - r0;
     float *to = A.many_o + at * D + 4 * h;
 #pragma unroll
     for (int mt = 0; mt < DP / 32; ++mt)
@@ -1181,28 +1260,26 @@ __global__ __launch_bounds__(64 * (Wide<T, BYTES, DP>::kWaves), (Wide<T, BYTES, 
   uint8_t *odds = reinterpret_cast<uint8_t *>(shared_bytes + W::kOdds);  // as in the kernel above, of one tile
   volatile int *odd_at = reinterpret_cast<volatile int *>(shared_bytes + W::kOddAt);
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, h = lane >> 5;
-  uint32_t id = block_id();
+  const uint32_t id = block_id();
   const int head = (int)(id % A.heads);
-  id /= A.heads;
-  const int part = (int)(id % A.many_parts);
-  id /= A.many_parts;
-  if (id >= A.tiles) return;
+  const Plan plan = plan_of(A);
+  // The last tiles of a chunk see the most and come first, but for workgroups with no unit, which end at once: behind
+  // the others they would wait for a compute unit each (2048 rows of 4 in 8 bits over 8192 tokens: 369 us, so 358).
+  const uint32_t unit = A.many_units - 1u - id / A.heads;
   int b;
   uint32_t tile;
   Seq sq;
   const int g = A.group, hq = A.heads * g, D = A.dim;
-  if (!find_unit(A.s, A.tiles - 1 - id, [&](const Seq &s) {
-        const int64_t r = (int64_t)s.n * g;
-        return r > A.few_rows && s.n <= A.max_new ? (uint32_t)((r + kWideRows - 1) / kWideRows) : 0u;
-      }, b, tile, sq))
-    return;
+  if (!find_unit(A.s, unit, [&](const Seq &s) { return many_units(A, s, plan.per); }, b, tile, sq)) return;
+  const uint32_t parts = many_parts(A, sq, plan.per);
+  const int part = (int)(tile % parts);
+  tile /= parts;
   const int len = sq.pos + sq.n, rows = sq.n * g;
-  if (len > (A.s.width << A.s.page_shift)) return;  // the kernel for few writes what such rows become
   const int r0 = (int)tile * kWideRows, r1 = min(r0 + kWideRows, rows);
   const int p0 = sq.pos + r0 / g, p1 = sq.pos + (r1 - 1) / g;
-  const Span sp = span_of<kManyStep, kManyLeast>(A, p0, p1, len, A.many_parts);
+  const Span sp = span_of(A, p0, p1, len, plan.per);
   if (part >= max(sp.parts, 1)) return;
-  const int begin = sp.begin + part * sp.per, end = min(sp.end, begin + sp.per);
+  const int begin = sp.begin + part * plan.per, end = min(sp.end, begin + plan.per);
   const int n = end > begin ? (end - begin + 63) / 64 : 0;  // tiles
   const int all_hi = A.causal ? p0 : len - 1, all_lo = A.window > 0 ? p1 - A.window + 1 : 0;
   const bool active = r0 + wave * 32 < rows;  // of the wave
@@ -1553,7 +1630,7 @@ __global__ __launch_bounds__(64 * (Wide<T, BYTES, DP>::kWaves), (Wide<T, BYTES, 
       }
     if (h == 0 && A.lse) A.lse[row] = (st.m + __builtin_amdgcn_logf(st.l)) * kLn2F;
   } else {
-    const int64_t at = part * A.s.n_tokens * hq + row;
+    const int64_t at = ((int64_t)unit * A.heads + head) * A.many_rows + r - r0;
     float *to = A.many_o + at * D + 4 * h;
 #pragma unroll
     for (int mt = 0; mt < kMt; ++mt)
@@ -1568,8 +1645,8 @@ __global__ __launch_bounds__(64 * (Wide<T, BYTES, DP>::kWaves), (Wide<T, BYTES, 
 
 // ---- the parts of a row together, in their order.  The first workgroups take sequences with few rows: 32 times four entries,
 // and of each eight threads every eighth part, whose sums meet in LDS.  The others take the tokens of the other
-// sequences, whose parts are few: a thread four entries.
-constexpr int kJoinThreads = 256, kJoinQuads = kJoinThreads / 8;
+// sequences, whose parts are few: a thread four entries at a time.
+constexpr int kJoinQuads = kJoinThreads / 8;
 
 // All threads of a workgroup call it; `there`: this thread's entries are some row's.
 template <typename T, int SPLIT>
@@ -1638,19 +1715,25 @@ __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendArgs A)
     return;
   }
   id -= few_all;
+  if (id >= (uint32_t)A.many_joined) return;
+  const Plan plan = plan_of(A);
+  if (plan.per == kUncut) return;
   const uint32_t many = many_joins(A);
-  const int64_t token = id / many;
-  if (A.many_parts == 1 || token >= A.s.n_tokens) return;
-  uint32_t k;
-  Seq sq;
-  if (token < A.s.starts[0] || !find_unit(A.s, (uint32_t)(token - A.s.starts[0]), [](const Seq &s) { return (uint32_t)s.n; }, b, k, sq)) return;
-  const int len = sq.pos + sq.n, rows = sq.n * g, e = (int)(id % many) * kJoinThreads + threadIdx.x;
-  if (sq.n > A.max_new || len > (A.s.width << A.s.page_shift) || rows <= A.few_rows) return;
-  const int head = min(e / quads, hq - 1), i = (int)k, r = i * g + head % g;
-  const int r0 = r / A.many_rows * A.many_rows, r1 = min(r0 + A.many_rows, rows);
-  const Span sp = span_of<kManyStep, kManyLeast>(A, sq.pos + r0 / g, sq.pos + (r1 - 1) / g, len, A.many_parts);
-  const int64_t row = (int64_t)(sq.row + i) * hq + head;
-  join_row<T, 1>(A, A.many_o, A.many_ml, row, A.s.n_tokens * hq, sp.parts, row, e % quads * 4, sp.parts > 1 && e < hq * quads);
+  for (int64_t at = id; at < A.s.n_tokens * many; at += A.many_joined) {
+    const int64_t token = at / many;
+    uint32_t k;
+    Seq sq;
+    if (token < A.s.starts[0] || !find_unit(A.s, (uint32_t)(token - A.s.starts[0]), [](const Seq &s) { return (uint32_t)s.n; }, b, k, sq)) continue;
+    if (!many_tiles(A, sq)) continue;
+    const uint32_t unit = units_before(A.s, b, [&](const Seq &s) { return many_units(A, s, plan.per); });
+    const int len = sq.pos + sq.n, rows = sq.n * g, e = (int)(at % many) * kJoinThreads + threadIdx.x;
+    const int head = min(e / quads, hq - 1), i = (int)k, r = i * g + head % g;
+    const int tile = r / A.many_rows, r0 = tile * A.many_rows, r1 = min(r0 + A.many_rows, rows);
+    const Span sp = span_of(A, sq.pos + r0 / g, sq.pos + (r1 - 1) / g, len, plan.per);
+    const int64_t first = unit + (int64_t)tile * many_parts(A, sq, plan.per);
+    join_row<T, 1>(A, A.many_o, A.many_ml, (first * A.heads + head / g) * A.many_rows + r - r0, (int64_t)A.heads * A.many_rows, sp.parts,
+                   (int64_t)(sq.row + i) * hq + head, e % quads * 4, sp.parts > 1 && e < hq * quads);
+  }
 }
 
 template <typename T, bool BYTES, int DP>
@@ -1676,8 +1759,8 @@ hipError_t attend_run(const AttendArgs &A, hipStream_t st) {
       if (e != hipSuccess) return e;
     }
   few_kernel<<<grid_of((int64_t)A.few_units * A.heads), 64 * waves, few, st>>>(A);
-  if (A.tiles) many_kernel<<<grid_of((int64_t)A.tiles * A.heads * A.many_parts), many_threads, many, st>>>(A);
-  const int64_t joins = (A.joined ? (int64_t)few_joins(A) * A.s.n_seqs : 0) + (A.many_parts > 1 ? A.s.n_tokens * many_joins(A) : 0);
+  if (A.tiles) many_kernel<<<grid_of((int64_t)A.many_units * A.heads), many_threads, many, st>>>(A);
+  const int64_t joins = (A.joined ? (int64_t)few_joins(A) * A.s.n_seqs : 0) + A.many_joined;
   if (joins) attend_join_kernel<T><<<grid_of(joins), kJoinThreads, 0, st>>>(A);
   return hipGetLastError();
 }

@@ -18,41 +18,35 @@ void parts_of(const cfp_attend_desc &a, const cfp_cache_desc &c, const cfp_seque
   A.few_target = (int32_t)std::max<int64_t>(kFewParts / c.heads, 1);
   A.few_units = s.n_seqs + (A.joined ? (int32_t)std::min<int64_t>(A.few_target, most_len / A.few_least * s.n_seqs) : 0);
   A.many_rows = c.dim <= kWideDim ? kWideRows : kManyRows;
-  A.tiles = 0, A.many_parts = 1;
+  A.tiles = A.many_units = A.many_most = 0, A.many_joined = 0;
   if (new_rows > A.few_rows) {
-    A.tiles = (uint32_t)std::min<int64_t>(a.n_tokens * g / A.many_rows + s.n_seqs, (a.n_tokens * g + A.few_rows) / (A.few_rows + 1));
-    // Time in tiles: rounds of the chip (a workgroup a compute unit; sixteen more are not counted as a round) times a
-    // part's tiles and about five that a workgroup takes before its first and behind its last; a launch more joins the
-    // parts (three).  The sequences are taken to be alike; as they may not be, one part stays where others save little.
-    const int64_t each = a.n_tokens * g / s.n_seqs;
-    const int64_t groups = c.heads * (each > A.few_rows ? s.n_seqs * ((each + A.many_rows - 1) / A.many_rows)
-                                                        : (a.n_tokens * g + A.many_rows - 1) / A.many_rows);
-    const int64_t most_tiles = (most_len + kManyStep - 1) / kManyStep;
-    int64_t least = 0;
-    for (int parts = 1; parts <= 64 && (parts == 1 || most_tiles * kManyStep >= (int64_t)parts * kManyLeast); ++parts) {
-      const int64_t rounds = (std::max<int64_t>(groups * parts - 16, 1) + 255) / 256;
-      const int64_t time = rounds * ((most_tiles + parts - 1) / parts + 5) + (parts > 1 ? 3 : 0);
-      if (parts == 1)
-        least = time * 7 / 8;
-      else if (time < least)
-        least = time, A.many_parts = parts;
+    const int64_t rows = a.n_tokens * g;
+    const int64_t most_span = a.causal && a.window > 0 ? std::min<int64_t>(most_len, a.window + A.many_rows / g + kManyStep) : most_len;
+    A.tiles = (uint32_t)std::min<int64_t>(rows / A.many_rows + s.n_seqs, (rows + A.few_rows) / (A.few_rows + 1));
+    // The device cuts tiles into parts where there are few, and where they see so much that parts may save something.  There are
+    // these at least, if all rows are some sequence's:
+    const int64_t least = std::max<int64_t>((rows - (int64_t)s.n_seqs * A.few_rows + A.many_rows - 1) / A.many_rows, 1);
+    if (least * c.heads <= kManyRounds * kGroups + kSpare && most_span > 2 * kManyLeast + kManyStep) {
+      const int64_t rounds = std::min<int64_t>(((int64_t)A.tiles * c.heads + kGroups - 1) / kGroups, kManyRounds);
+      A.many_most = (uint32_t)std::min<int64_t>(rounds * kGroups / c.heads, A.tiles * ((most_len + kManyLeast - 1) / kManyLeast));
+      A.many_joined = (int32_t)std::min<int64_t>(a.n_tokens * ((a.n_q * (int64_t)c.dim / 4 + kJoinThreads - 1) / kJoinThreads), 2048);
     }
+    A.many_units = std::max(A.tiles, A.many_most);
   }
 }
 
 size_t few_slots(const cfp_cache_desc &c, const AttendArgs &A) {
   return A.joined ? (size_t)A.few_units * c.heads * A.few_rows : 0;
 }
-size_t many_slots(const cfp_attend_desc &a, const AttendArgs &A) {
-  return A.many_parts > 1 ? (size_t)a.n_tokens * a.n_q * A.many_parts : 0;
-}
+size_t many_slots(const cfp_cache_desc &c, const AttendArgs &A) { return (size_t)A.many_most * c.heads * A.many_rows; }
+constexpr size_t kPlanBytes = 16;
 
 }  // namespace
 
 size_t attend_bytes(const cfp_attend_desc &a, const cfp_cache_desc &c, const cfp_sequences_desc &s) {
   AttendArgs A{};
   parts_of(a, c, s, A);
-  return (few_slots(c, A) + many_slots(a, A)) * (c.dim + 2) * 4;
+  return (few_slots(c, A) + many_slots(c, A)) * (c.dim + 2) * 4 + (A.tiles ? kPlanBytes : 0);
 }
 
 hipError_t launch_attend(const cfp_attend_desc &a, const cfp_cache_desc &c, const cfp_sequences_desc &s, void *out, float *lse,
@@ -64,8 +58,9 @@ hipError_t launch_attend(const cfp_attend_desc &a, const cfp_cache_desc &c, cons
   A.kp = c.k_page_stride, A.vp = c.v_page_stride, A.ksp = c.k_scale_page_stride, A.vsp = c.v_scale_page_stride;
   A.qt = a.q_token_stride, A.qh = a.q_head_stride;
   A.out = out, A.lse = lse;
-  const size_t few = few_slots(c, A), many = many_slots(a, A);
-  A.few_o = (float *)ws, A.many_o = A.few_o + few * c.dim;
+  const size_t few = few_slots(c, A), many = many_slots(c, A);
+  A.plan = (int32_t *)ws;
+  A.few_o = (float *)((char *)ws + (A.tiles ? kPlanBytes : 0)), A.many_o = A.few_o + few * c.dim;
   A.few_ml = A.many_o + many * c.dim, A.many_ml = A.few_ml + 2 * few;
   A.heads = c.heads, A.group = a.n_q / c.heads, A.dim = c.dim, A.max_new = s.max_new;
   A.causal = a.causal != 0, A.window = std::min(a.window, 1 << 30);

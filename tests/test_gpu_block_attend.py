@@ -319,6 +319,28 @@ def test_more_sequences_than_lanes_in_parts():
         check(y, lse, q, k, v, table, starts, lens, 32 ** -0.5, True, 0, most)
 
 
+@pytest.mark.parametrize("dim,held", [(64, "bf16"), (96, "e4m3"), (192, "bf16")])
+@pytest.mark.parametrize("lengths,new,hq,heads,causal,window", [
+    ([2300, 900, 40, 1700], [70, 1, 1, 1], 8, 2, True, 0),  # a chunk among tokens
+    ([2477, 1301, 333], [133, 90, 300], 8, 1, True, 0),  # chunks of unlike lengths
+    ([2000, 30, 1999], [129, 20, 40], 4, 1, True, 700),  # windows over several parts
+    ([1500, 1500], [40, 41], 8, 2, False, 100),
+    ([700 + b % 3 * 350 if b % 9 == 4 else b for b in range(150)], [34 if b % 9 == 4 else min(b, 1) for b in range(150)], 2, 1, True, 0),
+])
+def test_chunks_that_are_cut_into_parts(lengths, new, hq, heads, causal, window, dim, held):
+    from paper_2504_00598_amd import block
+    g = gen(23)
+    table, starts, lens, pages = layout(lengths, new, 16, g)
+    cache, k, v = held_cache(pages, 16, heads, dim, "bf16", held, g)
+    q = torch.randn(int(starts[-1]), hq, dim, generator=g).bfloat16()
+    seqs = block.Sequences(table.cuda(), starts.cuda(), lens.cuda())
+    y, lse = block.attend(q.cuda(), cache, seqs, causal=causal, window=window, with_lse=True)
+    rows = set(range(0, q.shape[0], 13)) | {int(s) - 1 for s in starts[1:] if s > 0} | {int(s) for s in starts[:-1] if s < q.shape[0]}
+    check(y, lse, q, k, v, table, starts, lens, dim ** -0.5, causal, window, "cut", rows)
+    again = block.attend(q.cuda(), cache, seqs, causal=causal, window=window, with_lse=True)
+    assert torch.equal(y, again[0]) and torch.equal(lse, again[1])
+
+
 def test_pages_that_lie_apart_and_beyond_32_bits():
     from paper_2504_00598_amd import block
     heads, dim, page, layers = 2, 128, 64, 4
