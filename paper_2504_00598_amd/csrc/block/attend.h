@@ -413,6 +413,14 @@ __device__ __forceinline__ void times_scales(f32x16 &s, u32x4 w) {
   for (int i = 0; i < 16; ++i) s[i] *= scale_of(w[i / 4] >> (8 * (i % 4)) & 0xff);
 }
 
+// Scale bytes of 255 as 254.  No token that was written has one, but an unwritten place may: its scale would be infinite, and times
+// a weight of zero no number.  For tiles that some row sees in part.
+__device__ __forceinline__ u32x4 finite_scales(u32x4 w) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] -= (((w[i] & 0x7f7f7f7fu) + 0x01010101u) & w[i] & 0x80808080u) >> 7;
+  return w;
+}
+
 // The largest of three, without a step for each operand that makes signalling NaN quiet.
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float r;
@@ -631,6 +639,7 @@ __global__ __launch_bounds__(64 * kTokenWaves, DP <= 128 ? 2 : 1) void attend_to
           const float x = bad ? __builtin_nanf("") : s[e / 4][e % 4];
           s[e / 4][e % 4] = first + e >= lo && first + e <= hi ? x : -__builtin_inff();
         }
+        if constexpr (kWeightsScaled<T, BYTES>) vsr = finite_scales(vsr);
       }
       float top = s[0][0];
 #pragma unroll
@@ -839,7 +848,10 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_few_kernel(Atte
       if (t + 128 < end) load_k(t + 128, next);
       const bool edge = t + 31 > all_hi || t < all_lo || !inside(now.at[0]) || !inside(now.at[1]);
       const int first = t + 16 * h;
-      if (edge) mask16(s[0], first, lo, hi, !inside(h ? now.at[1] : now.at[0]));
+      if (edge) {
+        mask16(s[0], first, lo, hi, !inside(h ? now.at[1] : now.at[0]));
+        if constexpr (kWeightsScaled<T, BYTES>) vsr = finite_scales(vsr);
+      }
       vec<T, 8> w[2];
       st.weigh(s, A.scale);
       if constexpr (kWeightsScaled<T, BYTES>) times_scales(s[0], vsr);
