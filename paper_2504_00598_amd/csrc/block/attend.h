@@ -14,7 +14,8 @@
 // halves of a wave read whole 16-token runs of one page each.
 //
 // What is masked is left out by a choice, not by arithmetic: scores become -inf, and where a tile that some row sees in part
-// holds values that are not finite, these are taken out of the product and added to the rows that see them.
+// holds values that are not finite in the type and under the scale that the product takes them with, these are taken out of the
+// product and added to the rows that see them.
 //
 // Single tokens do 2 (query heads a key head) operations a byte and are bound by memory; chunks by the matrix units, beside
 // which the exponentials take as long: 32 x 32 scores at dim 128 are 512 cycles of products and about 450 of vector work a SIMD.
@@ -292,37 +293,84 @@ __device__ __forceinline__ vec<T, 8> load_q(const T *q, int d, int dim, bool the
   return r;
 }
 
-// What is infinite or not a number among a word's entries of type H (the first in the lowest bits): cleared in the word, and
+// What is infinite or not a number among a word's two entries (the first in the lowest bits): cleared in the word, and
 // its bits by sign in `up` and `down` (what is not a number is both).
-template <typename T, typename H>
+template <typename T>
 __device__ __forceinline__ uint32_t take_odd(uint32_t w, uint32_t &up, uint32_t &down) {
+  constexpr uint32_t kInf = std::is_same<T, bf16_t>::value ? 0x7f80 : 0x7c00;
   up = down = 0;
-  if constexpr (sizeof(H) == 1) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if ((w >> (8 * i) & 0x7f) == 0x7f) up |= 1u << i, down |= 1u << i, w &= ~(0xffu << (8 * i));
-  } else {
-    constexpr uint32_t kInf = std::is_same<T, bf16_t>::value ? 0x7f80 : 0x7c00;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const uint32_t x = w >> (16 * i) & 0xffff;
-      if ((x & kInf) != kInf) continue;
-      if ((x & 0x7fff) != kInf || !(x & 0x8000)) up |= 1u << i;
-      if ((x & 0x7fff) != kInf || (x & 0x8000)) down |= 1u << i;
-      w &= ~(0xffffu << (16 * i));
-    }
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t x = w >> (16 * i) & 0xffff;
+    if ((x & kInf) != kInf) continue;
+    if ((x & 0x7fff) != kInf || !(x & 0x8000)) up |= 1u << i;
+    if ((x & 0x7fff) != kInf || (x & 0x8000)) down |= 1u << i;
+    w &= ~(0xffffu << (16 * i));
   }
   return w;
 }
 // The same of 16 bytes.
-template <typename T, typename H>
+template <typename T>
 __device__ __forceinline__ void take_odd(u32x4 &w, uint32_t &up, uint32_t &down) {
   up = down = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     uint32_t u, d;
-    w[i] = take_odd<T, H>(w[i], u, d);
-    up |= u << (4 / (int)sizeof(H) * i), down |= d << (4 / (int)sizeof(H) * i);
+    w[i] = take_odd<T>(w[i], u, d);
+    up |= u << (2 * i), down |= d << (2 * i);
+  }
+}
+
+// Scale bytes of 255 as 254.  No token that was written has one, but an unwritten place may: its scale would be infinite, and times
+// a weight of zero no number.  For tiles that some row sees in part.
+__device__ __forceinline__ u32x4 finite_scales(u32x4 w) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] -= (((w[i] & 0x7f7f7f7fu) + 0x01010101u) & w[i] & 0x80808080u) >> 7;
+  return w;
+}
+
+// Of 16 tokens with the scales s (none of them 255) the least magnitude, as a byte of 8 bits without its sign, that is not finite once
+// it is widened to T: that of 2^k with k = 16 (float16) or 128 less the scale's exponent, as nothing that is held lies between T's
+// largest value and that power; any but zero where k is below the least that is held, and only what is not a number where
+// 448 stays in the range, as it does under every scale that was written for rows of T.
+template <typename T>
+__device__ __forceinline__ u32x4 odd_from(u32x4 s) {
+  constexpr bool kHalf = std::is_same<T, f16_t>::value;
+  constexpr int kTop = kHalf ? 127 + 16 : 127 + 128;
+  constexpr uint32_t kLow = (kTop - 8 - 128) * 0x01010101u;  // scales from kTop - 8 on, without their highest bits
+  uint32_t large = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) large |= ((s[i] | 0x80808080u) - kLow) & s[i];
+  u32x4 r = {0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu};
+  if (large & 0x80808080u) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t w = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int k = kTop - (int)(s[i] >> (8 * j) & 0xff);
+        w |= (uint32_t)(k > 8 ? 0x7f : k >= -6 ? 8 * (k + 7) : 8 >> min(-6 - k, 3)) << (8 * j);
+      }
+      r[i] = w;
+    }
+  }
+  return r;
+}
+// take_odd of 16 entries of 8 bits: those from the magnitudes `least` on.
+__device__ __forceinline__ void take_odd_bytes(u32x4 &w, u32x4 least, uint32_t &up, uint32_t &down) {
+  constexpr uint32_t kSigns = 0x80808080u;
+  up = down = 0;
+  uint32_t any = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) any |= (w[i] | kSigns) - least[i];  // no byte borrows from the next: least is 1 to 0x7f
+  if (any & kSigns) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t odd = ((w[i] | kSigns) - least[i]) & kSigns, nan = ((w[i] | kSigns) - 0x7f7f7f7fu) & kSigns;
+      auto four = [](uint32_t x) { return (x >> 7) * 0x01020408u >> 24; };  // the bytes' highest bits behind each other
+      up |= four(odd & (~w[i] | nan)) << (4 * i), down |= four(odd & (w[i] | nan)) << (4 * i);
+      w[i] &= ~((odd >> 7) * 0xffu);
+    }
   }
 }
 
@@ -411,14 +459,6 @@ constexpr bool kWeightsScaled = BYTES && std::is_same<T, bf16_t>::value;
 __device__ __forceinline__ void times_scales(f32x16 &s, u32x4 w) {
 #pragma unroll
   for (int i = 0; i < 16; ++i) s[i] *= scale_of(w[i / 4] >> (8 * (i % 4)) & 0xff);
-}
-
-// Scale bytes of 255 as 254.  No token that was written has one, but an unwritten place may: its scale would be infinite, and times
-// a weight of zero no number.  For tiles that some row sees in part.
-__device__ __forceinline__ u32x4 finite_scales(u32x4 w) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) w[i] -= (((w[i] & 0x7f7f7f7fu) + 0x01010101u) & w[i] & 0x80808080u) >> 7;
-  return w;
 }
 
 // The largest of three, without a step for each operand that makes signalling NaN quiet.
@@ -639,7 +679,7 @@ __global__ __launch_bounds__(64 * kTokenWaves, DP <= 128 ? 2 : 1) void attend_to
           const float x = bad ? __builtin_nanf("") : s[e / 4][e % 4];
           s[e / 4][e % 4] = first + e >= lo && first + e <= hi ? x : -__builtin_inff();
         }
-        if constexpr (kWeightsScaled<T, BYTES>) vsr = finite_scales(vsr);
+        if constexpr (BYTES) vsr = finite_scales(vsr);
       }
       float top = s[0][0];
 #pragma unroll
@@ -666,15 +706,17 @@ __global__ __launch_bounds__(64 * kTokenWaves, DP <= 128 ? 2 : 1) void attend_to
       }
       if (edge) {
         bool any = false;
+        u32x4 least = {0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu};
+        if constexpr (BYTES && !kWeightsScaled<T, BYTES>) least = odd_from<T>(vsr);
 #pragma unroll
         for (int mt = 0; mt < kMt; ++mt) {
           uint32_t up, down;
           if constexpr (BYTES) {
-            take_odd<T, H>(vr[mt][0], up, down);
+            take_odd_bytes(vr[mt][0], least, up, down);
           } else {
             uint32_t up1, down1;
-            take_odd<T, H>(vr[mt][0], up, down);
-            take_odd<T, H>(vr[mt][1], up1, down1);
+            take_odd<T>(vr[mt][0], up, down);
+            take_odd<T>(vr[mt][1], up1, down1);
             up |= up1 << 8, down |= down1 << 8;
           }
           odds[h * DP + 16 * mt + col] = up | down << 16;
@@ -850,7 +892,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_few_kernel(Atte
       const int first = t + 16 * h;
       if (edge) {
         mask16(s[0], first, lo, hi, !inside(h ? now.at[1] : now.at[0]));
-        if constexpr (kWeightsScaled<T, BYTES>) vsr = finite_scales(vsr);
+        if constexpr (BYTES) vsr = finite_scales(vsr);
       }
       vec<T, 8> w[2];
       st.weigh(s, A.scale);
@@ -858,15 +900,17 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_few_kernel(Atte
       st.pack(s, w);
       if (edge) {
         bool any = false;
+        u32x4 least = {0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu};
+        if constexpr (BYTES && !kWeightsScaled<T, BYTES>) least = odd_from<T>(vsr);
 #pragma unroll
         for (int mt = 0; mt < DP / 32; ++mt) {
           uint32_t up, down;
           if constexpr (BYTES) {
-            take_odd<T, H>(vr[mt][0], up, down);
+            take_odd_bytes(vr[mt][0], least, up, down);
           } else {
             uint32_t up1, down1;
-            take_odd<T, H>(vr[mt][0], up, down);
-            take_odd<T, H>(vr[mt][1], up1, down1);
+            take_odd<T>(vr[mt][0], up, down);
+            take_odd<T>(vr[mt][1], up1, down1);
             up |= up1 << 8, down |= down1 << 8;
           }
           odds[h * DP + 32 * mt + col] = up | down << 16;
@@ -946,7 +990,8 @@ __global__ __launch_bounds__(256, 1) void attend_many_kernel(AttendArgs A) {
   // of a tile that some row sees in part: the tokens whose values are not finite, a bit each, [2][DP][sign][8 bytes], and
   // in odd_at the tile (its first token + 1) that last had any
   uint8_t *odds = reinterpret_cast<uint8_t *>(lds + 2 * kTile);
-  volatile int *odd_at = reinterpret_cast<volatile int *>(odds + 2 * DP * 16);
+  typedef volatile __attribute__((address_space(3))) int lds_int;
+  lds_int *odd_at = (lds_int *)(odds + 2 * DP * 16);
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, h = lane >> 5;
   const uint32_t id = block_id();
   const int head = (int)(id % A.heads);
@@ -1016,6 +1061,9 @@ __global__ __launch_bounds__(256, 1) void attend_many_kernel(AttendArgs A) {
   auto store = [&](int buf, int t) {
     T *k = lds + buf * kTile, *v = k + kManyStep * kKLd;
     const bool edge = partly(t);
+    u32x4 least = {0, 0, 0, 0};
+    if constexpr (BYTES)
+      if (edge) vsr = finite_scales(vsr), least = odd_from<T>(vsr);
 #pragma unroll
     for (int e = 0; e < kPieces; ++e) {
       const int n = e * 256 + tid;
@@ -1038,7 +1086,10 @@ __global__ __launch_bounds__(256, 1) void attend_many_kernel(AttendArgs A) {
         if (n < kAll && d < D) {
           if (edge) {
             uint32_t up, down;
-            take_odd<T, H>(vr[e], up, down);
+            if constexpr (BYTES)
+              take_odd_bytes(vr[e], least, up, down);
+            else
+              take_odd<T>(vr[e], up, down);
             uint8_t *at = odds + (buf * DP + d) * 16 + tok / 8;
             at[0] = (uint8_t)up, at[8] = (uint8_t)down;
             if constexpr (BYTES) at[1] = (uint8_t)(up >> 8), at[9] = (uint8_t)(down >> 8);
@@ -1577,7 +1628,7 @@ __global__ __launch_bounds__(64 * (Wide<T, BYTES, DP>::kWaves), (Wide<T, BYTES, 
           const int d = m / 8, c = value_place(d, m % 8);
           u32x4 w = reinterpret_cast<const u32x4 *>(v0)[m];
           uint32_t up, down;
-          take_odd<T, T>(w, up, down);
+          take_odd<T>(w, up, down);
           odds[d * 16 + c] = (uint8_t)up, odds[d * 16 + 8 + c] = (uint8_t)down;
           if (up | down) {
             reinterpret_cast<u32x4 *>(v0)[m] = w;

@@ -72,3 +72,69 @@ def unseen(new, group, dim, dt, window):
 def test_scales_that_no_row_sees_where_weights_take_them(new, group, dim, window):
     """Up to 32 rows a key head in bfloat16: a weight of zero is multiplied by the scale of what it masks."""
     unseen(new, group, dim, "bf16", window)
+
+
+WIDENED = [(1, 1, 64, "f16"), (3, 4, 96, "f16"), (5, 4, 64, "f16"), (5, 4, 256, "f16"), (70, 4, 128, "f16"), (70, 4, 192, "f16"),
+           (40, 1, 256, "f16"), (70, 4, 64, "bf16"), (70, 4, 192, "bf16"), (40, 1, 256, "bf16")]
+
+
+@pytest.mark.parametrize("window", [0, 20])
+@pytest.mark.parametrize("new,group,dim,dt", WIDENED)
+def test_scales_that_no_row_sees_where_values_take_them(new, group, dim, dt, window):
+    """A value under such a scale is beyond the range of the rows' type, and a zero under 255 no number."""
+    unseen(new, group, dim, dt, window)
+
+
+@pytest.mark.parametrize("window", [0, 20])
+@pytest.mark.parametrize("new,group,dim,dt", WIDENED[1:])
+def test_values_beyond_the_range_reach_the_rows_that_see_them(new, group, dim, dt, window):
+    """A token of the chunk itself, whose values are more than the rows' type holds: the rows behind it have infinities (or what
+    comes of them), those before it, and those whose window starts behind it, the same bits as without."""
+    from paper_2504_00598_amd import block
+    say("beyond", new, group, dim, dt, window)
+    g = gen(dim + new + 1)
+    cache, _, _, table = make(dim, dt, g)
+    starts, lens = torch.tensor([0, new], dtype=torch.int32), torch.tensor([L], dtype=torch.int32)
+    q = torch.randn(new, HEADS * group, dim, generator=g).to(DT[dt]).cuda()
+    seqs = block.Sequences(table.cuda(), starts.cuda(), lens.cuda(), max_new=new)
+    clean = block.attend(q, cache, seqs, window=window, with_lse=True)
+    tok = torch.arange(new) + L - new
+    for p in (L - 2, L - 1 - new // 2):
+        pg, at = int(table[0, p // PAGE]), p % PAGE
+        held = cache.v.clone(), cache.v_scale.clone()
+        cache.v.view(torch.uint8)[pg, :, :, at] = 0x7e  # 448
+        cache.v_scale[pg, :, at] = 135 if dt == "f16" else 254  # 448 2^8, 448 2^127
+        y, lse = block.attend(q, cache, seqs, window=window, with_lse=True)
+        sees = ((tok >= p) & ((tok - window < p) if window else (tok >= 0))).cuda()
+        assert torch.equal(lse, clean[1]) and torch.equal(y[~sees], clean[0][~sees]), (p, y[~sees].isnan().sum())
+        if dt == "f16":
+            assert bool((y[sees] == torch.inf).all()), p
+        cache.v.copy_(held[0]), cache.v_scale.copy_(held[1])
+
+
+@pytest.mark.parametrize("new,group,dt", [(3, 4, "f16"), (5, 4, "f16"), (40, 1, "f16"), (40, 1, "bf16")])
+def test_every_byte_under_scales_at_the_end_of_the_range(new, group, dt):
+    """Entry d of the last token's value is the byte d: it is infinite, no number or finite as the widened value is."""
+    from paper_2504_00598_amd import block
+    say("every byte", new, group, dt)
+    g = gen(new)
+    cache, _, _, table = make(256, dt, g)
+    starts, lens = torch.tensor([0, new], dtype=torch.int32), torch.tensor([L], dtype=torch.int32)
+    q = torch.randn(new, HEADS * group, 256, generator=g).to(DT[dt]).cuda()
+    seqs = block.Sequences(table.cuda(), starts.cuda(), lens.cuda(), max_new=new)
+    clean = block.attend(q, cache, seqs)
+    every = torch.arange(256, dtype=torch.uint8)
+    pg, at = int(table[0, (L - 1) // PAGE]), (L - 1) % PAGE
+    cache.v.view(torch.uint8)[pg, :, :, at] = every.cuda()
+    for scale in list(range(130, 156)) + [200, 254] if dt == "f16" else range(240, 255):
+        cache.v_scale[pg, :, at] = scale
+        x = (every.view(torch.float8_e4m3fn).double() * 2.0 ** (scale - 127)).to(DT[dt])
+        y = block.attend(q, cache, seqs)
+        assert torch.equal(y[:-1], clean[:-1]), scale
+        last = y[-1].cpu()
+        # bfloat16 values from 2^80 on, as all of these are, may leave the range before the division
+        some = torch.ones(256, dtype=torch.bool) if dt == "f16" else ~torch.isfinite(x)
+        for h in range(HEADS * group):
+            assert torch.equal(last[h][some].isnan(), x[some].isnan()), (scale, h)
+            assert torch.equal(last[h][some].isposinf(), x[some].isposinf()), (scale, h)
+            assert torch.equal(last[h][some].isneginf(), x[some].isneginf()), (scale, h)
