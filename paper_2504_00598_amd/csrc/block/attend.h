@@ -1783,10 +1783,10 @@ __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendArgs A)
   if (plan.per == kUncut) return;
   const uint32_t many = many_joins(A);
   for (int64_t at = id; at < A.s.n_tokens * many; at += A.many_joined) {
-    const int64_t token = at / many;
     uint32_t k;
     Seq sq;
-    if (token < A.s.starts[0] || !find_unit(A.s, (uint32_t)(token - A.s.starts[0]), [](const Seq &s) { return (uint32_t)s.n; }, b, k, sq)) continue;
+    // the rows that are some sequence's are counted, as what starts before the call's rows is none
+    if (!find_unit(A.s, (uint32_t)(at / many), [](const Seq &s) { return (uint32_t)s.n; }, b, k, sq)) continue;
     if (!many_tiles(A, sq)) continue;
     const uint32_t unit = units_before(A.s, b, [&](const Seq &s) { return many_units(A, s, plan.per); });
     const int len = sq.pos + sq.n, rows = sq.n * g, e = (int)(at % many) * kJoinThreads + threadIdx.x;
