@@ -1756,6 +1756,8 @@ inline __host__ __device__ uint32_t few_joins(const AttendArgs &A) {
 inline __host__ __device__ uint32_t many_joins(const AttendArgs &A) {
   return (uint32_t)(((int64_t)A.heads * A.group * (A.dim / 4) + kJoinThreads - 1) / kJoinThreads);
 }
+// All of them: below 2^31, so that the kernel counts them in 32 bits (a call with more is refused).
+inline int64_t joins_of(const AttendArgs &A) { return (A.joined ? (int64_t)few_joins(A) * A.s.n_seqs : 0) + A.many_joined; }
 
 template <typename T>
 __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendArgs A) {
@@ -1823,7 +1825,7 @@ hipError_t attend_run(const AttendArgs &A, hipStream_t st) {
     }
   few_kernel<<<grid_of((int64_t)A.few_units * A.heads), 64 * waves, few, st>>>(A);
   if (A.tiles) many_kernel<<<grid_of((int64_t)A.many_units * A.heads), many_threads, many, st>>>(A);
-  const int64_t joins = (A.joined ? (int64_t)few_joins(A) * A.s.n_seqs : 0) + A.many_joined;
+  const int64_t joins = joins_of(A);
   if (joins) attend_join_kernel<T><<<grid_of(joins), kJoinThreads, 0, st>>>(A);
   return hipGetLastError();
 }

@@ -9,7 +9,9 @@ namespace {
 // How the work is laid out: bounds from what the host knows; the device cuts by the lengths that it finds.  Sequences with few
 // rows are cut into about kFewParts equal parts over all (512 workgroups are at work at a time).
 void parts_of(const cfp_attend_desc &a, const cfp_cache_desc &c, const cfp_sequences_desc &s, AttendArgs &A) {
-  const int64_t g = a.n_q / c.heads, most_len = (int64_t)s.width * c.page;
+  A.s = seq_args(c, s, a.n_tokens);
+  A.heads = c.heads, A.group = a.n_q / c.heads, A.dim = c.dim;
+  const int64_t g = A.group, most_len = (int64_t)s.width * c.page;
   const int64_t new_rows = std::min<int64_t>(s.max_new, a.n_tokens) * g;
   // all sequences have few rows, or those that have go with the narrow kernel and the others with the one for many
   A.few_rows = (int32_t)(new_rows <= kFewRows ? new_rows : g <= kTokenRows ? kTokenRows : kFewRows);
@@ -43,6 +45,12 @@ constexpr size_t kPlanBytes = 16;
 
 }  // namespace
 
+bool attend_fits(const cfp_attend_desc &a, const cfp_cache_desc &c, const cfp_sequences_desc &s) {
+  AttendArgs A{};
+  parts_of(a, c, s, A);
+  return joins_of(A) < (int64_t)1 << 31;
+}
+
 size_t attend_bytes(const cfp_attend_desc &a, const cfp_cache_desc &c, const cfp_sequences_desc &s) {
   AttendArgs A{};
   parts_of(a, c, s, A);
@@ -53,7 +61,6 @@ hipError_t launch_attend(const cfp_attend_desc &a, const cfp_cache_desc &c, cons
                          void *ws, hipStream_t st) {
   AttendArgs A{};
   parts_of(a, c, s, A);
-  A.s = seq_args(c, s, a.n_tokens);
   A.q = a.q, A.k = c.k, A.v = c.v, A.ks = c.k_scale, A.vs = c.v_scale;
   A.kp = c.k_page_stride, A.vp = c.v_page_stride, A.ksp = c.k_scale_page_stride, A.vsp = c.v_scale_page_stride;
   A.qt = a.q_token_stride, A.qh = a.q_head_stride;
@@ -62,7 +69,7 @@ hipError_t launch_attend(const cfp_attend_desc &a, const cfp_cache_desc &c, cons
   A.plan = (int32_t *)ws;
   A.few_o = (float *)((char *)ws + (A.tiles ? kPlanBytes : 0)), A.many_o = A.few_o + few * c.dim;
   A.few_ml = A.many_o + many * c.dim, A.many_ml = A.few_ml + 2 * few;
-  A.heads = c.heads, A.group = a.n_q / c.heads, A.dim = c.dim, A.max_new = s.max_new;
+  A.max_new = s.max_new;
   A.causal = a.causal != 0, A.window = std::min(a.window, 1 << 30);
   A.wide = reinterpret_cast<uintptr_t>(a.q) % 16 == 0 && a.q_token_stride % 8 == 0 && a.q_head_stride % 8 == 0;
   A.scale = a.scale * 1.44269504088896341f;

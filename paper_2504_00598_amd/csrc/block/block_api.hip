@@ -135,6 +135,7 @@ int check_attend(const cfp_attend_desc *a, const cfp_cache_desc *c, const cfp_se
   if (a->n_tokens * a->n_q >= kMaxTokens || (int64_t)a->n_q * c->dim >= kMaxTokens ||
       a->n_tokens * (((int64_t)a->n_q * c->dim / 4 + 31) / 32) >= kMaxTokens)
     return CFP_ERR_UNSUPPORTED;
+  if (!attend_fits(*a, *c, *s)) return CFP_ERR_UNSUPPORTED;
   return a->n_tokens > 0 && !a->q ? CFP_ERR_ARG : CFP_OK;
 }
 

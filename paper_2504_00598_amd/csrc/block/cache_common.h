@@ -114,6 +114,8 @@ hipError_t launch_cache_write(const cfp_cache_desc &c, const cfp_sequences_desc 
 hipError_t launch_cache_read(const cfp_cache_desc &c, const cfp_sequences_desc &s, int64_t n_tokens, int dtype, void *k,
                              void *v, hipStream_t st);
 
+// Whether the workgroups that join parts can be numbered.
+bool attend_fits(const cfp_attend_desc &a, const cfp_cache_desc &c, const cfp_sequences_desc &s);
 size_t attend_bytes(const cfp_attend_desc &a, const cfp_cache_desc &c, const cfp_sequences_desc &s);
 hipError_t launch_attend(const cfp_attend_desc &a, const cfp_cache_desc &c, const cfp_sequences_desc &s, void *out, float *lse,
                          void *ws, hipStream_t st);
