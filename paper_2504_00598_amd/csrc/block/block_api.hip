@@ -36,20 +36,20 @@ int check_axes(const cfp_qk_desc *d, const uint8_t *axis, int n_axes) {
   return CFP_OK;
 }
 
-int qk_fwd(const cfp_qk_desc &d, const uint8_t *axis, int n_axes, void *yq, void *yk, void *stream) {
+int qk_fwd(const cfp_qk_desc &d, const uint8_t *axis, void *yq, void *yk, void *stream) {
   if (d.n_tokens == 0 || d.n_q + d.n_k == 0) return CFP_OK;
   if ((d.n_q && !yq) || (d.n_k && !yk)) return CFP_ERR_ARG;
-  return status(launch_qk_fwd(d, d.rot ? axis : nullptr, n_axes, yq, yk, (hipStream_t)stream));
+  return status(launch_qk_fwd(d, d.rot ? axis : nullptr, yq, yk, (hipStream_t)stream));
 }
 
-int qk_bwd(const cfp_qk_desc &d, const uint8_t *axis, int n_axes, const void *dyq, HeadStrides sq, const void *dyk,
+int qk_bwd(const cfp_qk_desc &d, const uint8_t *axis, const void *dyq, HeadStrides sq, const void *dyk,
            HeadStrides sk, void *dq, void *dk, float *dwq, float *dwk, void *ws, size_t ws_bytes, void *stream) {
   const bool none = d.n_tokens == 0;
   if (!none && ((d.n_q && (!dyq || !dq)) || (d.n_k && (!dyk || !dk)))) return CFP_ERR_ARG;
   const size_t need = none || d.n_q + d.n_k == 0 ? 0 : qk_bwd_bytes(d);
   if (need && (!ws || ws_bytes < need)) return CFP_ERR_WORKSPACE;
   if (need && !on(ws, 4)) return CFP_ERR_ARG;
-  return status(launch_qk_bwd(d, d.rot ? axis : nullptr, n_axes, dyq, dyk, sq, sk, dq, dk, dwq, dwk, (float *)ws,
+  return status(launch_qk_bwd(d, d.rot ? axis : nullptr, dyq, dyk, sq, sk, dq, dk, dwq, dwk, (float *)ws,
                               (hipStream_t)stream));
 }
 
@@ -151,7 +151,7 @@ extern "C" {
 
 int cfp_qk_norm_rope(const cfp_qk_desc *d, void *yq, void *yk, void *stream) {
   if (int e = check_qk(d)) return e;
-  return qk_fwd(*d, nullptr, 0, yq, yk, stream);
+  return qk_fwd(*d, nullptr, yq, yk, stream);
 }
 
 size_t cfp_qk_workspace_bytes(const cfp_qk_desc *d) {
@@ -163,13 +163,13 @@ int cfp_qk_norm_rope_bwd(const cfp_qk_desc *d, const void *dyq, int64_t dyq_toke
                          const void *dyk, int64_t dyk_token_stride, int64_t dyk_head_stride, void *dq, void *dk,
                          float *dwq, float *dwk, void *ws, size_t ws_bytes, void *stream) {
   if (int e = check_qk(d)) return e;
-  return qk_bwd(*d, nullptr, 0, dyq, {dyq_token_stride, dyq_head_stride}, dyk, {dyk_token_stride, dyk_head_stride}, dq, dk,
+  return qk_bwd(*d, nullptr, dyq, {dyq_token_stride, dyq_head_stride}, dyk, {dyk_token_stride, dyk_head_stride}, dq, dk,
                 dwq, dwk, ws, ws_bytes, stream);
 }
 
 int cfp_qk_norm_rope_axes(const cfp_qk_desc *d, const uint8_t *axis, int32_t n_axes, void *yq, void *yk, void *stream) {
   if (int e = check_axes(d, axis, n_axes)) return e;
-  return qk_fwd(*d, axis, n_axes, yq, yk, stream);
+  return qk_fwd(*d, axis, yq, yk, stream);
 }
 
 int cfp_qk_norm_rope_axes_bwd(const cfp_qk_desc *d, const uint8_t *axis, int32_t n_axes, const void *dyq,
@@ -177,7 +177,7 @@ int cfp_qk_norm_rope_axes_bwd(const cfp_qk_desc *d, const uint8_t *axis, int32_t
                               int64_t dyk_head_stride, void *dq, void *dk, float *dwq, float *dwk, void *ws,
                               size_t ws_bytes, void *stream) {
   if (int e = check_axes(d, axis, n_axes)) return e;
-  return qk_bwd(*d, axis, n_axes, dyq, {dyq_token_stride, dyq_head_stride}, dyk, {dyk_token_stride, dyk_head_stride}, dq, dk,
+  return qk_bwd(*d, axis, dyq, {dyq_token_stride, dyq_head_stride}, dyk, {dyk_token_stride, dyk_head_stride}, dq, dk,
                 dwq, dwk, ws, ws_bytes, stream);
 }
 

@@ -98,10 +98,10 @@ struct HeadStrides {
   int64_t tok, head;
 };
 
-// axis: that of each rotated pair, 0 .. n_axes - 1 (at most 4), with d.pos [n_axes][n_tokens]; or NULL
-hipError_t launch_qk_fwd(const cfp_qk_desc &d, const uint8_t *axis, int n_axes, void *yq, void *yk, hipStream_t st);
+// axis: that of each rotated pair, below CFP_QK_MAX_AXES, a row of d.pos [axes][n_tokens]; or NULL
+hipError_t launch_qk_fwd(const cfp_qk_desc &d, const uint8_t *axis, void *yq, void *yk, hipStream_t st);
 size_t qk_bwd_bytes(const cfp_qk_desc &d);
-hipError_t launch_qk_bwd(const cfp_qk_desc &d, const uint8_t *axis, int n_axes, const void *dyq, const void *dyk,
+hipError_t launch_qk_bwd(const cfp_qk_desc &d, const uint8_t *axis, const void *dyq, const void *dyk,
                          HeadStrides sq, HeadStrides sk, void *dq, void *dk, float *dwq, float *dwk, float *part,
                          hipStream_t st);
 

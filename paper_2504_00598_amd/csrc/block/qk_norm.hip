@@ -48,7 +48,6 @@ struct QkArgs {
   int32_t dim, rot, interleaved, wdtype;
   float eps;
   uint32_t axis[CFP_QK_MAX_DIM / 32];  // axes: that of each pair, two bits
-  int32_t n_axes;
 };
 
 template <int V>
@@ -413,9 +412,8 @@ hipError_t with_form(const QkArgs &A, int dtype, bool bwd, F f) {
   });
 }
 
-QkArgs args_of(const cfp_qk_desc &d, const uint8_t *axis, int n_axes) {
+QkArgs args_of(const cfp_qk_desc &d, const uint8_t *axis) {
   QkArgs A{};
-  A.n_axes = n_axes;
   for (int i = 0; axis && i < d.rot / 2; ++i) A.axis[i / 16] |= (uint32_t)axis[i] << (2 * (i % 16));
   A.x[0] = d.q, A.x[1] = d.k;
   A.sx[0] = {d.q_token_stride, d.q_head_stride};
@@ -443,8 +441,8 @@ void bwd_blocks(const cfp_qk_desc &d, int &bq, int &bk) {
 
 }  // namespace
 
-hipError_t launch_qk_fwd(const cfp_qk_desc &d, const uint8_t *axis, int n_axes, void *yq, void *yk, hipStream_t st) {
-  QkArgs A = args_of(d, axis, n_axes);
+hipError_t launch_qk_fwd(const cfp_qk_desc &d, const uint8_t *axis, void *yq, void *yk, hipStream_t st) {
+  QkArgs A = args_of(d, axis);
   A.out[0] = yq, A.out[1] = yk;
   return with_form(A, d.dtype, false, [&](auto t, auto v, auto g, auto u) {
     using T = decltype(t);
@@ -465,10 +463,10 @@ size_t qk_bwd_bytes(const cfp_qk_desc &d) {
   return (size_t)(bq + bk) * d.dim * 4;
 }
 
-hipError_t launch_qk_bwd(const cfp_qk_desc &d, const uint8_t *axis, int n_axes, const void *dyq, const void *dyk,
+hipError_t launch_qk_bwd(const cfp_qk_desc &d, const uint8_t *axis, const void *dyq, const void *dyk,
                          HeadStrides sq, HeadStrides sk, void *dq, void *dk, float *dwq, float *dwk, float *part,
                          hipStream_t st) {
-  QkArgs A = args_of(d, axis, n_axes);
+  QkArgs A = args_of(d, axis);
   A.dy[0] = dyq, A.dy[1] = dyk, A.sdy[0] = sq, A.sdy[1] = sk;
   A.out[0] = dq, A.out[1] = dk, A.part = part;
   int bq, bk;
