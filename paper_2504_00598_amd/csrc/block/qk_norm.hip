@@ -103,7 +103,7 @@ __device__ __forceinline__ void angles_of(const QkArgs &A, int64_t t, int u, flo
 // cos, then sin, of up to N pairs: rows of the workgroup times their pairs.
 template <int N>
 struct Gathered {
-  float cs[2][N];
+  alignas(16) float cs[2][N];  // read 16 bytes at a time
   // the tokens of rows first .. last
   __device__ __forceinline__ void gather(const QkArgs &A, int64_t first, int64_t last, int heads) {
     const int half = A.rot / 2;
