@@ -209,7 +209,8 @@ int cfp_cache_write(const cfp_cache_desc *c, const cfp_sequences_desc *s, int64_
                     int64_t v_head_stride, void *stream);
 
 /* The tokens of the rows back, as the values that they stand for: k, v [n_tokens][heads][dim] contiguous, of the cache's type
- * or, from CFP_DT_E4M3, in `dtype`.  A token before the first reads as zeros, one behind the table's width or in a page
+ * or, from CFP_DT_E4M3, rounded to `dtype`: exact in the type that was written and in CFP_DT_BF16; in CFP_DT_F16 what was written
+ * from CFP_DT_BF16 is an infinity beyond its range and has fewer bits below 2^-14.  A token before the first reads as zeros, one behind the table's width or in a page
  * outside the cache as NaN. */
 int cfp_cache_read(const cfp_cache_desc *c, const cfp_sequences_desc *s, int64_t n_tokens, int32_t dtype, void *k, void *v,
                    void *stream);
@@ -228,12 +229,14 @@ typedef struct {
 } cfp_attend_desc;
 
 /* out [n_tokens][n_q][dim]: for every row the mean of the values that it sees, weighted by exp(scale q . k); lse
- * [n_tokens][n_q] float (or NULL): the logarithm of the sum of the weights.  A row that sees nothing gets zeros and -inf.
- * What a row does not see has no effect on it, whatever it holds.  A row that sees a token of a page outside the
+ * [n_tokens][n_q] float (or NULL): the logarithm of the sum of the weights.  A row that sees nothing, or nothing but scores
+ * of -infinity, gets zeros and -inf.  What a row does not see has no effect on it, whatever it holds: entries, and scales outside 1 to 254 too.
+ * A value that a row sees and that is infinite, or no number, leaves the entry infinite or no number whatever its weight; which
+ * of them is unspecified where the weight is zero.  Keys and values of CFP_DT_E4M3 are those that cfp_cache_read gives in `dtype`.  A row that sees a token of a page outside the
  * cache, and all rows of a sequence longer than its table or with more rows than max_new, become NaN.
  * The weights are rounded to `dtype` as operands of the product with the values; sums, maxima and what is held between
  * parts of a long sequence are in 32 bits.  The sums are divided at the end: bfloat16 values beyond 2^80 may leave the
- * range before. */
+ * range before, and of such below 2^-96 bits may be lost. */
 size_t cfp_attend_workspace_bytes(const cfp_attend_desc *a, const cfp_cache_desc *c, const cfp_sequences_desc *s);
 int cfp_attend(const cfp_attend_desc *a, const cfp_cache_desc *c, const cfp_sequences_desc *s, void *out, float *lse, void *ws,
                size_t ws_bytes, void *stream);

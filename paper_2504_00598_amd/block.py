@@ -692,8 +692,8 @@ def cache_write(cache, k, v, seqs, *, stream=None):
 
 def cache_read(cache, seqs, n_tokens, *, dtype=None, out=None, stream=None):
     """The tokens of `seqs` back from the cache, as the values that they stand for: (k, v) [n_tokens][heads][dim] of the
-    cache's type, or of `dtype` (float8_e4m3fn: bfloat16, or float16).  With starts as the sums of lengths these are
-    whole sequences.  A token whose page is not one of the cache's reads as NaN.  Rows of no sequence are left as they
+    cache's type, or of `dtype` (float8_e4m3fn: bfloat16, or float16, to which what bfloat16 rows wrote is rounded, beyond its
+    range to an infinity).  With starts as the sums of lengths these are whole sequences.  A token whose page is not one of the cache's reads as NaN.  Rows of no sequence are left as they
     are: unspecified, or with out=(k, v) what these held."""
     torch = _torch()
     _paged(torch, cache, seqs)
@@ -729,8 +729,9 @@ def attend(q, cache, seqs, *, scale=None, causal=True, window=0, with_lse=False,
     h // (heads / cache heads).  A row that is token p of its sequence sees the tokens up to p, or all without `causal`, and with a
     window > 0 none before p - window + 1.  Its result is the mean of their values weighted by exp(scale q . k)
     (scale > 0; None: 1 / sqrt(dim)).  Returns [T][heads][dim] of q's type, or with `with_lse` also the logarithm of the
-    sum of the weights, [T][heads] float32, by which results over parts of a context are joined.  A row that sees nothing gets
-    zeros and -inf; what it does not see has no effect on it.  A row that sees a page outside the cache, a sequence
+    sum of the weights, [T][heads] float32, by which results over parts of a context are joined.  A row that sees nothing, or only scores
+    of -infinity, gets zeros and -inf; what it does not see has no effect on it, whatever its memory holds.  An infinite value that it sees
+    leaves the entry infinite or NaN.  Keys and values of float8_e4m3fn are those that cache_read gives in q's type.  A row that sees a page outside the cache, a sequence
     longer than its table and one with more rows than max_new get NaN.  Rows of no sequence are left as they are: unspecified,
     or what `out` (or out=(y, lse) with `with_lse`) held."""
     torch = _torch()

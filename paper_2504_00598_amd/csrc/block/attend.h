@@ -20,14 +20,14 @@
 // Single tokens do 2 (query heads a key head) operations a byte and are bound by memory; chunks by the matrix units, beside
 // which the exponentials take as long: 32 x 32 scores at dim 128 are 512 cycles of products and about 450 of vector work a SIMD.
 // Measured, 32 or 40 query heads over 8, dim 128 (a copy of 1 GiB reaches 5.1 TB/s, a product of 8192 1.4 PFLOP/s):
-//     64 sequences of 16 to 16384 tokens, one new each, bfloat16: 392 us, 5.5 TB/s; 32 of 4000 to 12000 in 8 bits: 103 us,
-//     5.1 TB/s; one of 777 in 13 us, of which the dependent loads (starts, table, keys) are most;
-//     8192 new of 32768 tokens, bfloat16: 3640 us, 1.06 PFLOP/s; 2048 of 8192 in 8 bits: 323 us, 0.76 PFLOP/s.
+//     64 sequences of 16 to 16384 tokens, one new each, bfloat16: 396 us, 5.4 TB/s; 32 of 4000 to 12000 in 8 bits: 102 us,
+//     5.2 TB/s; one of 777 in 13 us: starts, then the table, then keys and values, two steps of 256 tokens in its first part;
+//     8192 new of 32768 tokens, bfloat16: 3530 us, 1.09 PFLOP/s; 2048 of 8192 in 8 bits: 316 to 343 us, 0.72 to 0.77 PFLOP/s.
 // The chunk's kernel keeps the matrix unit busy half of its cycles at about 2.1 GHz.  What it was before, for the first of these
 // chunks: 128 rows a workgroup, two of them a compute unit, tiles through registers 6800 us; 64 rows a wave so that
 // an operand read from LDS serves two products, one wave a SIMD, with copies straight to LDS one tile ahead 8500, two ahead 4950, the
 // pages of a tile chosen by masks and not by an index 4060, the first operands of a stage read in the one before it 3860;
-// eight waves of 32 rows, two a SIMD, which hide each other's waits, 3640.
+// eight waves of 32 rows, two a SIMD, which hide each other's waits, 3640 (on another card 3530).
 #pragma once
 
 #include <algorithm>
@@ -974,8 +974,8 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_few_kernel(Atte
 }
 
 // ---- many rows of heads over 128: a workgroup takes 128 rows of one sequence and key head, 32 a wave, over tiles of 64
-// tokens whose keys and values lie in LDS (two tiles, so that the next one's lands while this one is worked on).  Their
-// rings would not fit LDS as the kernel below holds them.  4096 tokens of 32 heads over 8: 0.45 PFLOP/s at dim 192, 0.42 at
+// tokens whose keys and values lie in LDS (two tiles, so that the next one's lands while this one is worked on).  Rings of four
+// such tiles, as the kernel below holds them, would be 192 and 256 KiB; rings of 32 tokens have not been tried.  4096 tokens of 32 heads over 8: 0.45 PFLOP/s at dim 192, 0.42 at
 // 256, where one wave a SIMD has nothing to do while it waits.
 template <typename T, bool BYTES, int DP>
 __global__ __launch_bounds__(256, 1) void attend_many_kernel(AttendArgs A) {

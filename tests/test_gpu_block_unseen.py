@@ -138,3 +138,34 @@ def test_every_byte_under_scales_at_the_end_of_the_range(new, group, dt):
             assert torch.equal(last[h][some].isnan(), x[some].isnan()), (scale, h)
             assert torch.equal(last[h][some].isposinf(), x[some].isposinf()), (scale, h)
             assert torch.equal(last[h][some].isneginf(), x[some].isneginf()), (scale, h)
+
+
+@pytest.mark.parametrize("dt,held", [("bf16", "e4m3"), ("f16", "e4m3"), ("bf16", "bf16"), ("f16", "f16")])
+@pytest.mark.parametrize("dim", [64, 192])
+def test_a_fresh_cache_may_hold_anything(dim, dt, held):
+    """Written and attended over in chunks and token by token, as a program does it, in memory that held zeros, ones or any bytes."""
+    from paper_2504_00598_amd import block
+    say("fresh", dim, dt, held)
+    g = gen(dim)
+    x = torch.randn(L, 4 * HEADS + 2 * HEADS, dim, generator=g).to(DT[dt]).cuda()
+    table = torch.full((1, 12), -1, dtype=torch.int32)
+    table[0, :10] = torch.randperm(13, generator=g)[:10].int() + 1
+    table = table.cuda()
+    i32 = lambda *n: torch.tensor(n, dtype=torch.int32, device="cuda")  # noqa: E731
+    got = []
+    for what in ("zeros", "ones", "any"):
+        cache = block.KVCache.empty(14, PAGE, HEADS, dim, DT[held])
+        for t in cache._tensors():
+            if t is not None:
+                bits = t.view(torch.uint8)
+                bits.fill_(0xff if what == "ones" else 0)
+                if what == "any":
+                    bits.copy_(torch.randint(0, 256, bits.shape, dtype=torch.uint8, generator=g))
+        ys = []
+        for lo, hi in zip([0, 1, 40, 41, 44, 127, 128], [1, 40, 41, 44, 127, 128, L]):
+            seqs = block.Sequences(table, i32(0, hi - lo), i32(hi), max_new=hi - lo)
+            block.cache_write(cache, x[lo:hi, 4 * HEADS:5 * HEADS], x[lo:hi, 5 * HEADS:], seqs)
+            ys.append(block.attend(x[lo:hi, :4 * HEADS], cache, seqs))
+        got.append(torch.cat(ys))
+    assert bool(torch.isfinite(got[0]).all())
+    assert torch.equal(got[0], got[1]) and torch.equal(got[0], got[2])
